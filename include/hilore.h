@@ -401,6 +401,158 @@ int hilore_plan_apply(const hilore_unit *units_dev, const hilore_unit *units_hos
                       float tau_hi, const uint8_t *avail, uint8_t *action_io, float *psi, uint8_t *recompute,
                       uint64_t *retained_bytes, void *stream);
 
+/* ================================================================================================================
+ * The two ends of the actor update that touch the model: from logits to the log-probabilities that
+ * hilore_grpo_coeffs reads, from its coefficients back to a gradient of the logits, and the optimizer step
+ * (Algorithm 1, lines "Forward", "Backward", "OptimizerStep").  The paper leaves these to its learner; their
+ * definitions are stated here.
+ * ================================================================================================================ */
+
+/* ---- element types of logits, parameters and gradients ---- */
+enum { HILORE_BF16 = 0, HILORE_F32 = 1 };
+
+/*
+ * What was imposed on the logits of a row when its token was sampled.  A HOST struct of DEVICE pointers, read during
+ * the call; every part is optional (NULL) and has one entry per row unless it says otherwise.  For token v with logit x
+ * in row r:
+ *     c_all = occurrences of v in the row's history, c_out = those in its generated part
+ *     z = x;   c_all > 0:  z = x > 0 ? x / repetition : x * repetition
+ *     z = z - frequency * c_out - (c_out > 0 ? presence : 0)
+ *     z = z + bias of v
+ *     z = z / temperature;      v denied by the grammar:  z = -inf (also where x is NaN or Inf)
+ * evaluated in fp32, rounded once to the type of the result.
+ *   temperature   [n_rows] fp32; a value that is not > 0 (0: greedy) leaves the row unscaled.
+ *   repetition, frequency, presence   [n_rows] fp32 each; NULL = 1, 0, 0.  repetition > 0.
+ *   tokens        [n_tokens] int32, the sequences of the batch packed back to back.  Row r's history is
+ *                 tokens[hist_begin[r] .. hist_end[r]-1], of which the part from resp_begin[r] on was generated, the
+ *                 part before it is the prompt.  Rows may share and overlap: the slots of one training sequence are rows
+ *                 with the same hist_begin and growing hist_end.  Any length, 0 included; ranges are clamped to
+ *                 [0, n_tokens); entries outside [0, V) (padding) count nowhere.  tokens may be NULL iff n_tokens = 0.
+ *   bias_tokens, bias_values   [n_bias] int32 / fp32;  bias_offsets [n_rows + 1] int64: row r's list is entries
+ *                 bias_offsets[r] .. bias_offsets[r+1]-1.  Where a list names a token twice, the last entry counts.
+ *   allow         [n_allow, allow_ld] 32-bit words, allow_ld >= ceil(V / 32): bit v % 32 of word v / 32 is 1 where the
+ *                 grammar allows token v.   allow_row [n_rows] int32 selects the mask of a row; an index outside
+ *                 [0, n_allow) (-1) leaves it free.  NULL = row r uses mask r (n_allow >= n_rows).
+ */
+typedef struct hilore_logit_rules {
+    const float *temperature, *repetition, *frequency, *presence;
+    const int32_t *tokens;
+    int64_t n_tokens;
+    const int64_t *hist_begin, *resp_begin, *hist_end;
+    const int32_t *bias_tokens;
+    const float *bias_values;
+    int64_t n_bias;
+    const int64_t *bias_offsets;
+    const int32_t *allow;
+    const int32_t *allow_row;
+    int64_t n_allow, allow_ld;
+} hilore_logit_rules;
+
+/*
+ * Applies the rules to n_rows rows of V logits (one row per sequence at a decoding step, one per slot of a training
+ * microbatch), and the gradient of that: grad_in = grad_out * dz/dx, with dz/dx = 1 / temperature, times 1 / repetition
+ * (x > 0) or repetition (x <= 0) for a token of the history, and 0 for a denied one (whatever grad_out holds there).
+ *   logits       [n_rows, ld] of dtype (HILORE_BF16 or HILORE_F32), ld >= V: any ld and any address that the element
+ *                type allows; 32-byte aligned rows of equal alignment on both sides are the fast case.
+ *   out          [n_rows, ld_out] of the same type; may be `logits` itself with the same ld.
+ *   grad_out, grad_in   [n_rows, ld_..] of the same type; grad_in may be grad_out with the same ld.  Of `logits` only
+ *                the entries of history tokens are read.
+ *   Limits: V and n_rows below 2^31 - 2^16, and n_rows * ceil(V / 8192) below 2^31 (HILORE_SHAPE).
+ */
+int hilore_logits_apply(const void *logits, int32_t dtype, int64_t n_rows, int64_t V, int64_t ld,
+                        const hilore_logit_rules *rules, void *out, int64_t ld_out, void *stream);
+int hilore_logits_apply_backward(const void *logits, int32_t dtype, int64_t n_rows, int64_t V, int64_t ld,
+                                 const hilore_logit_rules *rules, const void *grad_out, int64_t ld_grad_out,
+                                 void *grad_in, int64_t ld_grad_in, void *stream);
+
+/*
+ * Log-probability of one token per row under the processed logits z (rules may be NULL: z = logits), the s_t of
+ * Eq. "grpo-objective", in one pass over the logits:
+ *     lse_r = ln sum_v exp(z_v);   logp_r = z_a - lse_r, a = targets[r];   entropy_r = lse_r - sum_v p_v z_v
+ * with fp32 statistics relative to the row's running maximum.
+ *   targets      [n_rows] int32; a row whose target lies outside [0, V) is a slot without a token: it is not read and
+ *                its logp, lse and entropy are 0.
+ *   logp         [n_rows] fp32.    lse  opt [n_rows] fp32, what hilore_token_logp_backward needs.
+ *   entropy      opt [n_rows] fp32 (a statistic: the gradient below is that of logp alone).
+ *   A denied target has logp = -inf.  A row in which nothing is allowed has logp = lse = -inf, entropy 0.  A NaN among
+ *   the allowed logits makes the row NaN; +Inf gives lse = +Inf and entropy NaN.
+ *   A row is the work of one CTA, or of a thread-block cluster of up to 8 when there are few rows (never with
+ *   HILORE_DISABLE_CLUSTER_LAUNCH): logp, lse and entropy of a row depend on that choice in their last bits, not on
+ *   anything else; the same call gives the same bits.
+ *
+ * hilore_token_logp_backward: grad_v = omega_r (1[v = a] - exp(z_v - lse_r)) dz_v/dx_v, the gradient of sum_r omega_r
+ * logp_r with respect to the logits, for the omega of hilore_grpo_coeffs.
+ *   omega, lse   [n_rows] fp32.    grad  [n_rows, ld_grad] of dtype; may be `logits` with the same ld.
+ *   Rows with omega = 0, without a token, with a denied target or with lse <= -1e30 (nothing to choose from) get zeros
+ *   and are not read.
+ */
+int hilore_token_logp(const void *logits, int32_t dtype, int64_t n_rows, int64_t V, int64_t ld,
+                      const hilore_logit_rules *rules, const int32_t *targets, float *logp, float *lse, float *entropy,
+                      void *stream);
+int hilore_token_logp_backward(const void *logits, int32_t dtype, int64_t n_rows, int64_t V, int64_t ld,
+                               const hilore_logit_rules *rules, const int32_t *targets, const float *lse,
+                               const float *omega, void *grad, int64_t ld_grad, void *stream);
+
+/* ---- storage of the optimizer's moments ---- */
+enum {
+    HILORE_STATE_F32 = 0,    /* m, v fp32                                                                  */
+    HILORE_STATE_E4M3FN = 1  /* m and sqrt(v) as E4M3FN codes with one fp32 scale per 64 elements, the block
+                                format of HILORE_FMT_E4M3FN_BLK: 2.125 bytes per element instead of 8        */
+};
+#define HILORE_PARAM_TILE 1024
+
+/* One tensor of an optimizer step.  A DEVICE array of these is passed beside the same array on the HOST. */
+typedef struct hilore_param {
+    void *p;               /* [n] parameters of p_dtype, updated                                              */
+    float *master;         /* opt [n] fp32 copy of a bf16 parameter: it is updated and p is its rounding (p is not read) */
+    const void *g;         /* [n] gradients of g_dtype                                                        */
+    void *m, *v;           /* [n] fp32 moments, or [n] u8 codes of m and of sqrt(v)                           */
+    float *m_scale, *v_scale; /* [ceil(n / 64)] fp32 scales of HILORE_STATE_E4M3FN, else NULL                 */
+    int64_t n;             /* elements; 0 is allowed                                                          */
+    int64_t first;         /* sum of ceil(n / HILORE_PARAM_TILE) over the entries before this one (HILORE_SHAPE if not) */
+    int32_t p_dtype, g_dtype, state;
+    float weight_decay;
+} hilore_param;
+
+/*
+ * Global norm of the gradients of a table, ||g|| = sqrt(sum over all tensors of g^2), and the factor that clips it:
+ * scale = min(1, max_norm / (norm + 1e-6)), NaN where the norm is not finite.  Squares are added in fp32 per 32
+ * elements (fp64 where that overflows) and in fp64 beyond, in a fixed order: run-to-run deterministic.
+ *   Of the table only g, g_dtype, n and first are read.    max_norm >= 0 (Inf: no clipping).
+ *   norm, scale   opt one fp32 each on the device, at least one of them.
+ *   workspace     hilore_grad_norm_workspace_bytes() bytes, 16-byte aligned.
+ */
+int hilore_grad_norm(const hilore_param *params_dev, const hilore_param *params_host, int32_t n_params, double max_norm,
+                     float *norm, float *scale, void *workspace, size_t workspace_bytes, void *stream);
+size_t hilore_grad_norm_workspace_bytes(void);
+
+/*
+ * One AdamW step over all tensors of a table in ONE launch.  Per element, in fp32, with g = grad_scale * gradient:
+ *     m = beta1 m + (1 - beta1) g;        v = beta2 v + (1 - beta2) g^2
+ *     p = p - lr ( weight_decay p + (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps) )
+ * m, sqrt(v) and the codes made from them take every operation rounded by itself, in this order ((1 - beta2) g first,
+ * then times g), so they are the same bits in any evaluation that does so.
+ * The parameter (or its fp32 master copy) is rounded to its type to nearest even.
+ *   HILORE_STATE_E4M3FN: the moments of the step enter the update in fp32; then, per block of 64 consecutive elements of
+ *     a tensor (the last one may be shorter), m and sqrt(v) are stored as codes by the rule of HILORE_FMT_E4M3FN_BLK in
+ *     hilore_compress (amax over finite elements, RNE; zeros and what is too small to be scaled get scale 1), with
+ *     scale = fl32(amax * fl32(1 / 448)) and inv = fl32(448 * fl32(1 / amax)), and one addition: a positive sqrt(v)
+ *     that would round to zero takes the smallest code, so that a later step never divides by eps alone where a
+ *     gradient has been.  Codes and scales of a first step are zeros.
+ *   params_dev, params_host   the table, as for hilore_plan_apply: [n_params] on the device and the same on the host
+ *             (read during the call for validation and launch sizing).  Tensors may be of different types, sizes and
+ *             state formats.  Any alignment that the types allow; tensors whose p, master and g are 32-byte aligned and
+ *             whose m and v are 32-byte (fp32) or 16-byte (codes) aligned move in vectors.  They must not overlap.
+ *   lr, lr_dev       lr_dev (opt, one fp32 on the device) replaces lr.
+ *   step, step_dev   t >= 1; step_dev (opt, one int64 on the device, >= 1) replaces it: with both, a captured graph can
+ *             be replayed over a schedule.
+ *   grad_scale       opt, one fp32 on the device, e.g. the scale of hilore_grad_norm.  Where it is not finite the step
+ *             leaves parameters and moments as they are.
+ */
+int hilore_adamw_step(const hilore_param *params_dev, const hilore_param *params_host, int32_t n_params, double lr,
+                      const float *lr_dev, double beta1, double beta2, double eps, int64_t step, const int64_t *step_dev,
+                      const float *grad_scale, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

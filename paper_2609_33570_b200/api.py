@@ -20,6 +20,9 @@ FMT_E4M3FN_RAW, FMT_E4M3FN_BLK, FMT_INT8_BLK = 0, 1, 2
 ACT_R, ACT_H, ACT_L = 0, 1, 2
 PHASE_DECIDE, PHASE_CAPTURE, PHASE_ENCODE, PHASE_RECOVER = 0, 1, 2, 3
 BLOCK = 64
+BF16, F32 = 0, 1
+STATE_F32, STATE_E4M3FN = 0, 1
+PARAM_TILE = 1024
 
 EXPORTS = ("hilore_status_string", "hilore_abi_version", "hilore_mask_count", "hilore_grpo_coeffs",
            "hilore_unit_exposure", "hilore_workspace_bytes", "hilore_compress", "hilore_recover",
@@ -28,7 +31,9 @@ EXPORTS = ("hilore_status_string", "hilore_abi_version", "hilore_mask_count", "h
            "hilore_relative_error", "hilore_relative_error_workspace_bytes", "hilore_fit_kappa",
            "hilore_grpo_coeffs_variant", "hilore_omega_diagnostics", "hilore_omega_diagnostics_workspace_bytes",
            "hilore_grpo_coeffs_packed", "hilore_unit_exposure_packed", "hilore_codec_relative_error",
-           "hilore_coeffs_exposure", "hilore_scores_plan", "hilore_scores_plan_workspace_bytes")
+           "hilore_coeffs_exposure", "hilore_scores_plan", "hilore_scores_plan_workspace_bytes",
+           "hilore_logits_apply", "hilore_logits_apply_backward", "hilore_token_logp", "hilore_token_logp_backward",
+           "hilore_grad_norm", "hilore_grad_norm_workspace_bytes", "hilore_adamw_step")
 
 
 class HiloreUnit(C.Structure):
@@ -36,6 +41,22 @@ class HiloreUnit(C.Structure):
     _fields_ = [("x", C.c_void_p), ("codes", C.c_void_p), ("scales", C.c_void_p), ("out", C.c_void_p),
                 ("row_rms", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64), ("ld", C.c_int64),
                 ("fmt", C.c_int32), ("block", C.c_int32)]
+
+
+class HiloreLogitRules(C.Structure):
+    """Mirror of ``struct hilore_logit_rules``."""
+    _fields_ = [("temperature", C.c_void_p), ("repetition", C.c_void_p), ("frequency", C.c_void_p), ("presence", C.c_void_p),
+                ("tokens", C.c_void_p), ("n_tokens", C.c_int64), ("hist_begin", C.c_void_p), ("resp_begin", C.c_void_p),
+                ("hist_end", C.c_void_p), ("bias_tokens", C.c_void_p), ("bias_values", C.c_void_p), ("n_bias", C.c_int64),
+                ("bias_offsets", C.c_void_p), ("allow", C.c_void_p), ("allow_row", C.c_void_p), ("n_allow", C.c_int64),
+                ("allow_ld", C.c_int64)]
+
+
+class HiloreParam(C.Structure):
+    """Mirror of ``struct hilore_param``."""
+    _fields_ = [("p", C.c_void_p), ("master", C.c_void_p), ("g", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
+                ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("n", C.c_int64), ("first", C.c_int64),
+                ("p_dtype", C.c_int32), ("g_dtype", C.c_int32), ("state", C.c_int32), ("weight_decay", C.c_float)]
 
 
 class HiloreError(RuntimeError):
@@ -101,8 +122,16 @@ def lib() -> C.CDLL:
         _lib.hilore_compress.argtypes = [vp, i64, i64, i64, i32, i32, vp, vp, vp, vp]
         _lib.hilore_recover.argtypes = [vp, vp, i64, i64, i32, i32, vp, i64, vp]
         _lib.hilore_plan_apply.argtypes = [vp, vp, i32, i32, vp, vp, vp, f32, f32, vp, vp, vp, vp, vp, vp]
+        _lib.hilore_logits_apply.argtypes = [vp, i32, i64, i64, i64, vp, vp, i64, vp]
+        _lib.hilore_logits_apply_backward.argtypes = [vp, i32, i64, i64, i64, vp, vp, i64, vp, i64, vp]
+        _lib.hilore_token_logp.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, vp, vp, vp]
+        _lib.hilore_token_logp_backward.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, vp, vp, i64, vp]
+        _lib.hilore_grad_norm.argtypes = [vp, vp, i32, C.c_double, vp, vp, vp, C.c_size_t, vp]
+        _lib.hilore_grad_norm_workspace_bytes.restype = C.c_size_t
+        _lib.hilore_grad_norm_workspace_bytes.argtypes = []
+        _lib.hilore_adamw_step.argtypes = [vp, vp, i32, C.c_double, vp, C.c_double, C.c_double, C.c_double, i64, vp, vp, vp]
         for name in EXPORTS:
-            if name not in ("hilore_status_string", "hilore_workspace_bytes", "hilore_static_scratch_bytes",
+            if name not in ("hilore_grad_norm_workspace_bytes", "hilore_status_string", "hilore_workspace_bytes", "hilore_static_scratch_bytes",
                             "hilore_allocate_workspace_bytes", "hilore_risk_budget",
                             "hilore_relative_error_workspace_bytes", "hilore_fit_kappa",
                             "hilore_omega_diagnostics_workspace_bytes", "hilore_scores_plan_workspace_bytes"):
@@ -323,4 +352,113 @@ def make_unit_table(units, device="cuda"):
     raw = bytes(arr)
     host = torch.frombuffer(bytearray(raw), dtype=torch.uint8)
     dev = host.to(device)
+    return dev, arr
+
+
+def _host(struct):
+    """Address of a host-side ctypes struct or array, or None."""
+    return None if struct is None else C.addressof(struct)
+
+
+def hilore_logits_apply(logits, dtype, n_rows, V, ld, rules, out, ld_out, stream=None, check=True):
+    """rules: a HiloreLogitRules on the host (make_logit_rules)."""
+    st = lib().hilore_logits_apply(_ptr(logits), dtype, n_rows, V, ld, _host(rules), _ptr(out), ld_out, _stream(stream))
+    return _check(st, "hilore_logits_apply", check)
+
+
+def hilore_logits_apply_backward(logits, dtype, n_rows, V, ld, rules, grad_out, ld_grad_out, grad_in, ld_grad_in,
+                                 stream=None, check=True):
+    st = lib().hilore_logits_apply_backward(_ptr(logits), dtype, n_rows, V, ld, _host(rules), _ptr(grad_out), ld_grad_out,
+                                            _ptr(grad_in), ld_grad_in, _stream(stream))
+    return _check(st, "hilore_logits_apply_backward", check)
+
+
+def hilore_token_logp(logits, dtype, n_rows, V, ld, rules, targets, logp, lse, entropy, stream=None, check=True):
+    st = lib().hilore_token_logp(_ptr(logits), dtype, n_rows, V, ld, _host(rules), _ptr(targets), _ptr(logp), _ptr(lse),
+                                 _ptr(entropy), _stream(stream))
+    return _check(st, "hilore_token_logp", check)
+
+
+def hilore_token_logp_backward(logits, dtype, n_rows, V, ld, rules, targets, lse, omega, grad, ld_grad, stream=None,
+                               check=True):
+    st = lib().hilore_token_logp_backward(_ptr(logits), dtype, n_rows, V, ld, _host(rules), _ptr(targets), _ptr(lse),
+                                          _ptr(omega), _ptr(grad), ld_grad, _stream(stream))
+    return _check(st, "hilore_token_logp_backward", check)
+
+
+def hilore_grad_norm_workspace_bytes():
+    return int(lib().hilore_grad_norm_workspace_bytes())
+
+
+def hilore_grad_norm(params_dev, params_host, n_params, max_norm, norm, scale, workspace, workspace_bytes, stream=None,
+                     check=True):
+    """params_dev / params_host: the two halves of make_param_table."""
+    st = lib().hilore_grad_norm(_ptr(params_dev), _host(params_host), n_params, max_norm, _ptr(norm), _ptr(scale),
+                                _ptr(workspace), workspace_bytes, _stream(stream))
+    return _check(st, "hilore_grad_norm", check)
+
+
+def hilore_adamw_step(params_dev, params_host, n_params, lr, lr_dev, beta1, beta2, eps, step, step_dev, grad_scale,
+                      stream=None, check=True):
+    st = lib().hilore_adamw_step(_ptr(params_dev), _host(params_host), n_params, lr, _ptr(lr_dev), beta1, beta2, eps, step,
+                                 _ptr(step_dev), _ptr(grad_scale), _stream(stream))
+    return _check(st, "hilore_adamw_step", check)
+
+
+def _typed(t, name, *dtypes):
+    """`t` if it is None or a contiguous tensor of one of `dtypes`: the structs below carry addresses only."""
+    if t is not None and t.dtype not in dtypes:
+        raise TypeError(f"{name}: expected {' or '.join(map(str, dtypes))}, got {t.dtype}")
+    if t is not None and not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous tensor")
+    return t
+
+
+def make_logit_rules(temperature=None, repetition=None, frequency=None, presence=None, tokens=None, hist_begin=None,
+                     resp_begin=None, hist_end=None, bias_tokens=None, bias_values=None, bias_offsets=None, allow=None,
+                     allow_row=None):
+    """Marshal the tensors of ``struct hilore_logit_rules`` (fp32 levels, int32 tokens, int64 ranges, int32 mask words
+    [n_allow, allow_ld]).  The struct holds addresses and keeps the tensors alive."""
+    f, i, j = (torch.float32,), (torch.int32,), (torch.int64,)
+    parts = dict(temperature=_typed(temperature, "temperature", *f), repetition=_typed(repetition, "repetition", *f),
+                 frequency=_typed(frequency, "frequency", *f), presence=_typed(presence, "presence", *f),
+                 tokens=_typed(tokens, "tokens", *i), hist_begin=_typed(hist_begin, "hist_begin", *j),
+                 resp_begin=_typed(resp_begin, "resp_begin", *j), hist_end=_typed(hist_end, "hist_end", *j),
+                 bias_tokens=_typed(bias_tokens, "bias_tokens", *i), bias_values=_typed(bias_values, "bias_values", *f),
+                 bias_offsets=_typed(bias_offsets, "bias_offsets", *j), allow=_typed(allow, "allow", *i),
+                 allow_row=_typed(allow_row, "allow_row", *i))
+    r = HiloreLogitRules(**{k: _ptr(t) for k, t in parts.items()})
+    r.n_tokens = 0 if tokens is None else tokens.numel()
+    r.n_bias = 0 if bias_tokens is None else bias_tokens.numel()
+    if allow is not None:
+        r.n_allow, r.allow_ld = allow.shape
+    r.keep = parts
+    return r
+
+
+def make_param_table(params, device="cuda"):
+    """Marshal a list of dicts (p, g, m, v tensors; master, m_scale, v_scale tensors or None; weight_decay) into the
+    host ctypes array and a device copy of it.  Types are taken from the tensors: one-byte m and v are codes.  Returns
+    (params_dev tensor, params_host array); the array keeps the tensors alive."""
+    kinds = {torch.bfloat16: BF16, torch.float32: F32}
+    arr = (HiloreParam * len(params))()
+    first = 0
+    for i, e in enumerate(params):
+        p, g, m, v = (_typed(e[k], k, *t) for k, t in (("p", tuple(kinds)), ("g", tuple(kinds)),
+                                                       ("m", (torch.float32, torch.uint8, torch.float8_e4m3fn)),
+                                                       ("v", (torch.float32, torch.uint8, torch.float8_e4m3fn))))
+        n, coded = p.numel(), m.element_size() == 1
+        master, ms, vs = (_typed(e.get(k), k, torch.float32) for k in ("master", "m_scale", "v_scale"))
+        blocks = (n + BLOCK - 1) // BLOCK
+        for name, t, want in (("g", g, n), ("m", m, n), ("v", v, n), ("master", master, n), ("m_scale", ms, blocks),
+                              ("v_scale", vs, blocks)):
+            if t is not None and t.numel() != want:
+                raise ValueError(f"entry {i}: {name} has {t.numel()} elements, expected {want}")
+        if (v.element_size() == 1) != coded or coded != (ms is not None) or coded != (vs is not None):
+            raise ValueError(f"entry {i}: m and v are both fp32 without scales, or both codes with scales")
+        arr[i] = HiloreParam(_ptr(p), _ptr(master), _ptr(g), _ptr(m), _ptr(v), _ptr(ms), _ptr(vs), n, first, kinds[p.dtype],
+                             kinds[g.dtype], STATE_E4M3FN if coded else STATE_F32, e.get("weight_decay", 0.0))
+        first += (n + PARAM_TILE - 1) // PARAM_TILE
+    arr.keep = params
+    dev = torch.frombuffer(bytearray(bytes(arr)), dtype=torch.uint8).to(device) if len(params) else None
     return dev, arr
