@@ -13,7 +13,7 @@ namespace hilore {
 constexpr int kTile = HILORE_PARAM_TILE; // elements of a warp's tile
 constexpr int kOptThreads = 256, kOptWarps = kOptThreads / 32;
 constexpr int kNormMaxGrid = 2048; // partial sums in the workspace
-constexpr float kE4m3Max = 448.0f, kE4m3Min = 0.001953125f; // largest and smallest positive value
+constexpr float kE4m3Max = 448.0f;
 
 __device__ __forceinline__ float load_one(const void *p, int32_t dtype, int64_t i)
 {
@@ -26,55 +26,64 @@ __device__ __forceinline__ void store_one(void *p, int32_t dtype, int64_t i, flo
     else static_cast<float *>(p)[i] = v;
 }
 
-// Eight consecutive values from element i on (a multiple of 8), `n` of them real; vectors where the tensor allows it.
-__device__ __forceinline__ void load8(const void *p, int32_t dtype, int64_t i, int n, bool vec, float (&x)[8])
+__device__ __forceinline__ float max_nan(float a, float b)
 {
-    if (vec && n == 8) {
-        if (dtype == HILORE_BF16) {
-            const uint4 w = ld_global_128_stream(static_cast<const uint16_t *>(p) + i);
-            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                x[2 * k] = bf16_lo(u[k]);
-                x[2 * k + 1] = bf16_hi(u[k]);
-            }
-        } else {
-            uint32_t w[8];
-            ld_global_256(static_cast<const float *>(p) + i, w);
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-                x[k] = __uint_as_float(w[k]);
-        }
-        return;
-    }
-#pragma unroll
-    for (int k = 0; k < 8; ++k)
-        x[k] = k < n ? load_one(p, dtype, i + k) : 0.0f;
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
 }
 
-__device__ __forceinline__ void store8(void *p, int32_t dtype, int64_t i, int n, bool vec, const float (&x)[8])
-{
-    if (vec && n == 8) {
-        if (dtype == HILORE_BF16) {
-            uint4 w;
-            w.x = cvt_bf16x2(x[1], x[0]);
-            w.y = cvt_bf16x2(x[3], x[2]);
-            w.z = cvt_bf16x2(x[5], x[4]);
-            w.w = cvt_bf16x2(x[7], x[6]);
-            *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p) + i) = w;
+// N consecutive values (8 or 16) in vectors, kept as loaded: bf16 pairs or fp32.
+template <int DTYPE, int N> struct Raw {
+    static constexpr int W = DTYPE == HILORE_BF16 ? N / 2 : N;
+    uint32_t w[W];
+    __device__ __forceinline__ void load(const void *p, int64_t i)
+    {
+        if (W == 4) {
+            const uint4 q = ld_global_128_stream(static_cast<const uint16_t *>(p) + i);
+            w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
         } else {
-            uint32_t w[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                w[k] = __float_as_uint(x[k]);
-            st_global_256(static_cast<float *>(p) + i, w);
+            for (int k = 0; k < W / 8; ++k) {
+                uint32_t t[8];
+                ld_global_256(static_cast<const char *>(p) + i * (DTYPE == HILORE_BF16 ? 2 : 4) + 32 * k, t);
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    w[8 * k + j] = t[j];
+            }
         }
-        return;
     }
+    __device__ __forceinline__ float get(int k) const
+    {
+        if (DTYPE == HILORE_F32) return __uint_as_float(w[k]);
+        return k & 1 ? bf16_hi(w[k >> 1]) : bf16_lo(w[k >> 1]);
+    }
+    __device__ __forceinline__ uint64_t pair(int k) const { return f32x2_pack(get(k), get(k + 1)); }
+    __device__ __forceinline__ void set2(int k, float x0, float x1) // k even
+    {
+        if (DTYPE == HILORE_F32) {
+            w[k] = __float_as_uint(x0);
+            w[k + 1] = __float_as_uint(x1);
+        } else {
+            w[k >> 1] = cvt_bf16x2(x1, x0);
+        }
+    }
+    __device__ __forceinline__ void store(void *p, int64_t i) const
+    {
+        if (W == 4) {
+            *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p) + i) = make_uint4(w[0], w[1], w[2], w[3]);
+        } else {
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
-        if (k < n) store_one(p, dtype, i + k, x[k]);
-}
+            for (int k = 0; k < W / 8; ++k) {
+                uint32_t t[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    t[j] = w[8 * k + j];
+                st_global_256(static_cast<char *>(p) + i * (DTYPE == HILORE_BF16 ? 2 : 4) + 32 * k, t);
+            }
+        }
+    }
+};
 
 // Index of the tensor that owns `tile`: the last entry whose first tile is not beyond it.  Called by whole warps.
 __device__ __forceinline__ int owner_of(const hilore_param *params, int n_params, int64_t tile)
@@ -92,40 +101,91 @@ __device__ __forceinline__ int owner_of(const hilore_param *params, int n_params
     return lo;
 }
 
+// A warp's way through consecutive tiles: the entry that owns the current one, looked up only when the tile leaves it.  The
+// entry lives in shared memory: its seven pointers would take a quarter of the registers.
+struct Walk {
+    const hilore_param *params;
+    int n_params;
+    int64_t begin, end; // tiles of entry `e`
+    hilore_param *e;    // the warp's copy
+    __device__ __forceinline__ Walk(const hilore_param *p, int n, hilore_param *copies)
+        : params(p), n_params(n), begin(0), end(0), e(copies + (threadIdx.x >> 5))
+    {
+    }
+    __device__ __forceinline__ bool at(int64_t tile) // true where the entry is a new one
+    {
+        if (tile < end)
+            return false;
+        const uint32_t *from = reinterpret_cast<const uint32_t *>(params + owner_of(params, n_params, tile));
+        __syncwarp();
+        for (int i = threadIdx.x & 31; i < (int)(sizeof(hilore_param) / 4); i += 32)
+            reinterpret_cast<uint32_t *>(e)[i] = __ldg(from + i);
+        __syncwarp();
+        begin = e->first;
+        end = begin + (e->n + kTile - 1) / kTile;
+        return true;
+    }
+};
+
+// Tiles of a warp: up to eight in a row, so that the look-up (two to three dependent loads) is paid once in 8192 elements,
+// fewer while that would leave SMs without two rounds of full occupancy.
+static int tiles_per_warp(int64_t tiles)
+{
+    int64_t k = tiles / ((int64_t)sm_count() * 64);
+    return k < 1 ? 1 : k > 8 ? 8 : (int)k;
+}
+
 // ------------------------------------------------------------------------------------------------------------------- norm
 // Squares in fp32 over the 32 elements of a lane's tile, fp64 beyond; a lane whose fp32 sum leaves the range redoes its
 // elements in fp64.  Partial sums in fixed slots: the result does not depend on scheduling.
-__global__ void __launch_bounds__(kOptThreads) grad_norm_kernel(const hilore_param *params, int n_params, int64_t n_tiles, double *partial)
+template <int DTYPE> __device__ __forceinline__ double tile_squares(const void *g, int64_t base, int64_t n, bool vec)
 {
     const int lane = threadIdx.x & 31;
-    double sum = 0.0;
-    for (int64_t tile = (int64_t)blockIdx.x * kOptWarps + (threadIdx.x >> 5); tile < n_tiles; tile += (int64_t)gridDim.x * kOptWarps) {
-        const hilore_param &e = params[owner_of(params, n_params, tile)];
-        const void *g = e.g;
-        const int32_t dtype = e.g_dtype;
-        const int64_t base = (tile - e.first) * kTile, n = e.n;
-        const bool vec = (reinterpret_cast<uintptr_t>(g) & 31) == 0;
-        float x[kTile / 256][8], s = 0.0f;
+    float s = 0.0f;
+    if (vec && base + kTile <= n) {
+        Raw<DTYPE, 8> x[kTile / 256];
 #pragma unroll
-        for (int k = 0; k < kTile / 256; ++k) {
-            const int64_t i = base + k * 256 + lane * 8;
-            load8(g, dtype, i, (int)max((int64_t)0, min((int64_t)8, n - i)), vec, x[k]);
-        }
+        for (int k = 0; k < kTile / 256; ++k)
+            x[k].load(g, base + k * 256 + lane * 8);
 #pragma unroll
         for (int k = 0; k < kTile / 256; ++k)
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                s = fmaf(x[k][i], x[k][i], s);
-        if (s < INFINITY) {
-            sum += (double)s;
-        } else {
-#pragma unroll
-            for (int k = 0; k < kTile / 256; ++k)
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    sum += (double)x[k][i] * (double)x[k][i];
+                s = fmaf(x[k].get(i), x[k].get(i), s);
+    } else {
+        for (int64_t i = base + lane; i < min(n, base + kTile); i += 32) {
+            const float x = load_one(g, DTYPE, i);
+            s = fmaf(x, x, s);
         }
     }
+    double d = (double)s;
+    if (!(s < INFINITY)) {
+        d = 0.0;
+        const bool dealt = vec && base + kTile <= n; // which elements were this lane's
+        for (int k = 0; k < kTile / 32; ++k) {
+            const int64_t i = base + (dealt ? (k >> 3) * 256 + lane * 8 + (k & 7) : k * 32 + lane);
+            const double x = i < n ? (double)load_one(g, DTYPE, i) : 0.0;
+            d += x * x;
+        }
+    }
+    return d;
+}
+
+__global__ void __launch_bounds__(kOptThreads, 4) grad_norm_kernel(const hilore_param *params, int n_params, int64_t n_tiles, int per_warp, double *partial)
+{
+    const int lane = threadIdx.x & 31;
+    double sum = 0.0;
+    __shared__ hilore_param copies[kOptWarps];
+    Walk walk(params, n_params, copies);
+    const int64_t stride = (int64_t)gridDim.x * kOptWarps * per_warp;
+    for (int64_t t0 = ((int64_t)blockIdx.x * kOptWarps + (threadIdx.x >> 5)) * per_warp; t0 < n_tiles; t0 += stride)
+        for (int64_t tile = t0; tile < min(t0 + per_warp, n_tiles); ++tile) {
+            walk.at(tile);
+            const int64_t base = (tile - walk.begin) * kTile;
+            const hilore_param &e = *walk.e;
+            const bool vec = (reinterpret_cast<uintptr_t>(e.g) & 31) == 0;
+            sum += e.g_dtype == HILORE_BF16 ? tile_squares<HILORE_BF16>(e.g, base, e.n, vec) : tile_squares<HILORE_F32>(e.g, base, e.n, vec);
+        }
     __shared__ double sm[kOptWarps];
     sum = warp_sum(sum);
     if (lane == 0) sm[threadIdx.x >> 5] = sum;
@@ -164,183 +224,362 @@ struct AdamArgs {
     const int64_t *step_dev;
 };
 
+// What one element's update takes, in registers.
 struct AdamStep {
-    float lr, step, rsqrt_bc2; // step = lr / (1 - beta1^t)
+    float gscale, b1, omb1, b2, omb2, eps, rsqrt_bc2;
+    float step, lrwd; // lr / (1 - beta1^t), lr * weight decay of the entry
 };
 
-// The moments, every operation rounded by itself in the order of the formula.  With 8-bit states the last bit decides the
-// codes of values near a tie, and a code of the next step's largest value moves the scale of 64 elements: contracted
-// operations would make them depend on the compiler.
-__device__ __forceinline__ float next_m(const AdamArgs &a, float m, float g) { return __fadd_rn(__fmul_rn(a.b1, m), __fmul_rn(a.omb1, g)); }
-__device__ __forceinline__ float next_v(const AdamArgs &a, float v, float g)
+__device__ __forceinline__ uint64_t both(float x) { return f32x2_pack(x, x); }
+
+// Two elements at a time, in packed fp32 pairs.  The moments take every operation rounded by itself in the order of the
+// formula: with 8-bit states the last bit decides the codes of values near a tie, and a code of the next step's largest value
+// moves the scale of 64 elements; contracted operations would make them depend on the compiler.
+__device__ __forceinline__ void next_moments(const AdamStep &h, uint64_t g, uint64_t &m, uint64_t &v)
 {
-    return __fadd_rn(__fmul_rn(a.b2, v), __fmul_rn(__fmul_rn(a.omb2, g), g));
+    const uint64_t x = f32x2_mul(g, both(h.gscale));
+    m = f32x2_add(f32x2_mul(both(h.b1), m), f32x2_mul(both(h.omb1), x));
+    v = f32x2_add(f32x2_mul(both(h.b2), v), f32x2_mul(f32x2_mul(both(h.omb2), x), x));
 }
 
-// One step of a 32-bit lane of eight elements.
-__device__ __forceinline__ void adam_f32(const hilore_param &e, const AdamArgs &a, const AdamStep &h, float gscale, int64_t i, int n, bool vec)
+__device__ __forceinline__ float rcp_approx(float x)
 {
-    float g[8], m[8], v[8], p[8];
-    load8(e.g, e.g_dtype, i, n, vec, g);
-    load8(e.m, HILORE_F32, i, n, vec, m);
-    load8(e.v, HILORE_F32, i, n, vec, v);
-    if (e.master) load8(e.master, HILORE_F32, i, n, vec, p);
-    else load8(e.p, e.p_dtype, i, n, vec, p);
-    const float lrwd = h.lr * e.weight_decay;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        const float x = __fmul_rn(g[k], gscale);
-        m[k] = next_m(a, m[k], x);
-        v[k] = next_v(a, v[k], x);
-        const float den = fmaf(__fsqrt_rn(v[k]), h.rsqrt_bc2, a.eps);
-        p[k] -= fmaf(lrwd, p[k], h.step * __fdiv_rn(m[k], den));
-    }
-    store8(e.m, HILORE_F32, i, n, vec, m);
-    store8(e.v, HILORE_F32, i, n, vec, v);
-    if (e.master) store8(e.master, HILORE_F32, i, n, vec, p);
-    store8(e.p, e.p_dtype, i, n, vec, p);
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
 }
 
-__device__ __forceinline__ void load_codes(const uint8_t *c, int64_t i, int n, bool vec, float s, float (&x)[16])
+// p - lr (wd p + m^ / (sqrt(v^) + eps)) from the new moment m and root r = sqrt(v): the 32-bit states' form, and the packed one of
+// the 8-bit states, whose quotient is within three units in the last place (a denominator is zero or above 2^-63).
+__device__ __forceinline__ float next_param(const AdamStep &h, float p, float m, float r)
 {
-    uint32_t w[4] = {0, 0, 0, 0};
-    if (vec && n == 16) {
-        const uint4 q = ld_global_128_stream(c + i);
-        w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
-    } else {
-#pragma unroll
-        for (int k = 0; k < 16; ++k)
-            if (k < n) w[k >> 2] |= (uint32_t)c[i + k] << (8 * (k & 3));
-    }
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const uint32_t lo = cvt_e4m3x2_to_f16x2(w[k]), hi = cvt_e4m3x2_to_f16x2(w[k] >> 16);
-        x[4 * k] = f16_lo_to_f32(lo) * s;
-        x[4 * k + 1] = f16_hi_to_f32(lo) * s;
-        x[4 * k + 2] = f16_lo_to_f32(hi) * s;
-        x[4 * k + 3] = f16_hi_to_f32(hi) * s;
-    }
+    return p - fmaf(h.lrwd, p, h.step * __fdiv_rn(m, fmaf(r, h.rsqrt_bc2, h.eps)));
+}
+__device__ __forceinline__ uint64_t next_param2(const AdamStep &h, uint64_t p, uint64_t m, uint64_t r)
+{
+    float d0, d1;
+    f32x2_unpack(f32x2_fma(r, both(h.rsqrt_bc2), both(h.eps)), d0, d1);
+    const uint64_t q = f32x2_mul(f32x2_mul(m, both(h.step)), f32x2_pack(rcp_approx(d0), rcp_approx(d1)));
+    return f32x2_sub(p, f32x2_fma(both(h.lrwd), p, q));
 }
 
-__device__ __forceinline__ void store_codes(uint8_t *c, int64_t i, int n, bool vec, const float (&q)[16])
+// Square roots of a pair of v: Newton's step r + (v - r^2) / (2 r) from r = v * rsqrt(v), the residual formed exactly by a fused
+// operation, which leaves an error far below the final rounding; v below 2^-126 counts as zero, Inf and NaN give NaN (the
+// caller takes __fsqrt_rn where a block holds one).  3.5 issue slots against ten for __fsqrt_rn, whose range test is a branch per element.
+__device__ __forceinline__ uint64_t root2(uint64_t v)
 {
-    uint32_t w[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-        w[k] = cvt_e4m3x4(q[4 * k], q[4 * k + 1], q[4 * k + 2], q[4 * k + 3]);
-    if (vec && n == 16) {
-        *reinterpret_cast<uint4 *>(c + i) = make_uint4(w[0], w[1], w[2], w[3]);
-        return;
-    }
-#pragma unroll
-    for (int k = 0; k < 16; ++k)
-        if (k < n) c[i + k] = (uint8_t)(w[k >> 2] >> (8 * (k & 3)));
+    float v0, v1, y0, y1;
+    f32x2_unpack(v, v0, v1);
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y0) : "f"(v0));
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y1) : "f"(v1));
+    const uint64_t y = f32x2_pack(v0 < 1.17549435e-38f ? 0.0f : y0, v1 < 1.17549435e-38f ? 0.0f : y1);
+    const uint64_t r = f32x2_mul(v, y), minus_h = f32x2_mul(y, both(-0.5f));
+    return f32x2_fma(f32x2_fma(r, r, f32x2_mul(v, both(-1.0f))), minus_h, r);
 }
 
-// Largest finite magnitude of a block of 64: 16 values of each of the four lanes of a quad.
-__device__ __forceinline__ float block_max(const float (&x)[16])
+__device__ __forceinline__ uint64_t decode2(uint32_t codes, float s) // two codes in the low half
+{
+    const uint32_t h = cvt_e4m3x2_to_f16x2(codes);
+    return f32x2_mul(f32x2_pack(f16_lo_to_f32(h), f16_hi_to_f32(h)), both(s));
+}
+
+// Largest magnitude of a block of 64: 16 values of each of the four lanes of a quad; Inf and NaN count as Inf.
+__device__ __forceinline__ float quad_max(const uint64_t (&x)[8])
 {
     float a = 0.0f;
 #pragma unroll
-    for (int k = 0; k < 16; ++k)
-        a = fmaxf(a, fabsf(x[k]));
-    a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 1));
-    a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 2));
-    if (__any_sync(0xFFFFFFFFu, a == INFINITY)) { // fmaxf passes over NaN but not over Inf
-        a = 0.0f;
-#pragma unroll
-        for (int k = 0; k < 16; ++k)
-            a = fabsf(x[k]) < INFINITY ? fmaxf(a, fabsf(x[k])) : a;
-        a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 1));
-        a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 2));
+    for (int k = 0; k < 8; ++k) {
+        float x0, x1;
+        f32x2_unpack(x[k], x0, x1);
+        a = max_nan(a, max_nan(fabsf(x0), fabsf(x1)));
     }
+    a = a < INFINITY ? a : INFINITY;
+    a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 1));
+    return fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 2));
+}
+
+// The same over the finite values alone.
+__device__ __forceinline__ float quad_max_finite(const uint64_t (&x)[8])
+{
+    float a = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        float x0, x1;
+        f32x2_unpack(x[k], x0, x1);
+        a = fabsf(x0) < INFINITY ? fmaxf(a, fabsf(x0)) : a;
+        a = fabsf(x1) < INFINITY ? fmaxf(a, fabsf(x1)) : a;
+    }
+    a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 1));
+    return fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 2));
+}
+
+// And of two values of each lane of a warp.
+__device__ __forceinline__ float warp_max_finite(float x0, float x1)
+{
+    float a = fabsf(x0) < INFINITY ? fabsf(x0) : 0.0f;
+    a = fabsf(x1) < INFINITY ? fmaxf(a, fabsf(x1)) : a;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+        a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, o));
     return a;
 }
 
-__device__ __forceinline__ void load16(const void *p, int32_t dtype, int64_t i, int n, bool vec, float (&x)[16])
+// Scale of a block whose largest magnitude is `top`, and its inverse.  A block of zeros, without a finite value, or too small
+// for 448 / top takes scale 1.
+struct BlockScale {
+    float scale, inv;
+    bool fits; // not one of those
+};
+__device__ __forceinline__ BlockScale block_scale(float top)
 {
-    float lo[8], hi[8];
-    load8(p, dtype, i, min(n, 8), vec, lo);
-    load8(p, dtype, i + 8, max(n - 8, 0), vec, hi);
+    BlockScale s{__fmul_rn(top, 1.0f / kE4m3Max), __fmul_rn(kE4m3Max, __frcp_rn(top)), true};
+    if (!(s.inv < INFINITY)) {
+        s.scale = s.inv = 1.0f;
+        s.fits = false;
+    }
+    return s;
+}
+
+// Codes of 16 values of a block.  ROOT: the values are square roots of v, of which a positive one is never rounded to zero (it
+// would turn the next step's division into one by eps) but takes the smallest code; words without a zero code, the usual
+// ones, skip the test of their four values.
+template <bool ROOT> __device__ __forceinline__ void encode16(const uint64_t (&x)[8], const BlockScale &s, uint32_t (&w)[4])
+{
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        x[k] = lo[k];
-        x[8 + k] = hi[k];
+    for (int k = 0; k < 4; ++k) {
+        float q[4];
+        f32x2_unpack(f32x2_mul(x[2 * k], both(s.inv)), q[0], q[1]);
+        f32x2_unpack(f32x2_mul(x[2 * k + 1], both(s.inv)), q[2], q[3]);
+        w[k] = cvt_e4m3x4(q[0], q[1], q[2], q[3]);
+        if (ROOT && ((w[k] - 0x01010101u) & ~w[k] & 0x80808080u) && s.fits) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (q[i] > 0.0f && !(w[k] >> (8 * i) & 0xFFu)) w[k] |= 1u << (8 * i);
+        }
     }
 }
 
-__device__ __forceinline__ void store16(void *p, int32_t dtype, int64_t i, int n, bool vec, const float (&x)[16])
-{
-    float lo[8], hi[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        lo[k] = x[k];
-        hi[k] = x[8 + k];
-    }
-    store8(p, dtype, i, min(n, 8), vec, lo);
-    store8(p, dtype, i + 8, max(n - 8, 0), vec, hi);
-}
-
-// One step of a lane of sixteen elements with 8-bit moments.  The four lanes of a quad own one block of 64; the moments of
-// this step enter the update in fp32, before they are rounded to codes.  v holds the codes of sqrt(v): the square root
-// halves the range that the codes have to span, and a positive root is never rounded to zero (it would turn the next
-// step's division into one by eps), it takes the smallest code instead.
-__device__ __forceinline__ void adam_e4m3(const hilore_param &e, const AdamArgs &a, const AdamStep &h, float gscale, int64_t i, int n, bool vec)
+// ---- whole tiles: vectors, types known at compile time ----
+template <int P, int G, bool MASTER> __device__ __forceinline__ void tile_f32(const hilore_param &e, const AdamStep &h, int64_t base)
 {
     const int lane = threadIdx.x & 31;
-    float g[16], m[16], r[16], p[16];
-    const bool some = n > 0;
-    uint8_t *mc = static_cast<uint8_t *>(e.m), *vc = static_cast<uint8_t *>(e.v);
-    load16(e.g, e.g_dtype, i, n, vec, g);
-    load_codes(mc, i, n, vec, some ? e.m_scale[i >> 6] : 0.0f, m);
-    load_codes(vc, i, n, vec, some ? e.v_scale[i >> 6] : 0.0f, r);
-    if (e.master) load16(e.master, HILORE_F32, i, n, vec, p);
-    else load16(e.p, e.p_dtype, i, n, vec, p);
-    const float lrwd = h.lr * e.weight_decay;
+#pragma unroll 1
+    for (int k = 0; k < kTile / 256; ++k) {
+        const int64_t i = base + k * 256 + lane * 8;
+        Raw<G, 8> g;
+        Raw<HILORE_F32, 8> m, v;
+        Raw<MASTER ? HILORE_F32 : P, 8> p;
+        g.load(e.g, i);
+        m.load(e.m, i);
+        v.load(e.v, i);
+        p.load(MASTER ? (const void *)e.master : e.p, i);
+        Raw<P, 8> out;
 #pragma unroll
-    for (int k = 0; k < 16; ++k) {
-        const float x = __fmul_rn(g[k], gscale);
-        m[k] = next_m(a, m[k], x);
-        r[k] = __fsqrt_rn(next_v(a, __fmul_rn(r[k], r[k]), x));
-        const float den = fmaf(r[k], h.rsqrt_bc2, a.eps);
-        p[k] -= fmaf(lrwd, p[k], h.step * __fdividef(m[k], den));
-    }
-    if (e.master) store16(e.master, HILORE_F32, i, n, vec, p);
-    store16(e.p, e.p_dtype, i, n, vec, p);
-    const float am = block_max(m), ar = block_max(r);
-    float ms = __fmul_rn(am, 1.0f / kE4m3Max), mi = __fmul_rn(kE4m3Max, __frcp_rn(am));
-    float rs = __fmul_rn(ar, 1.0f / kE4m3Max), ri = __fmul_rn(kE4m3Max, __frcp_rn(ar));
-    if (!(mi < INFINITY)) ms = mi = 1.0f; // nothing finite but zeros, or too small to be scaled
-    float least = kE4m3Min;
-    if (!(ri < INFINITY)) {
-        rs = ri = 1.0f;
-        least = 0.0f;
-    }
-#pragma unroll
-    for (int k = 0; k < 16; ++k) {
-        m[k] = __fmul_rn(m[k], mi);
-        const float x = __fmul_rn(r[k], ri);
-        r[k] = x > 0.0f ? fmaxf(x, least) : x;
-    }
-    store_codes(mc, i, n, vec, m);
-    store_codes(vc, i, n, vec, r);
-    if ((lane & 3) == 0 && some) {
-        e.m_scale[i >> 6] = ms;
-        e.v_scale[i >> 6] = rs;
+        for (int j = 0; j < 8; j += 2) {
+            uint64_t mm = m.pair(j), vv = v.pair(j);
+            next_moments(h, g.pair(j), mm, vv);
+            float m0, m1, v0, v1;
+            f32x2_unpack(mm, m0, m1);
+            f32x2_unpack(vv, v0, v1);
+            const float p0 = next_param(h, p.get(j), m0, __fsqrt_rn(v0)), p1 = next_param(h, p.get(j + 1), m1, __fsqrt_rn(v1));
+            m.set2(j, m0, m1);
+            v.set2(j, v0, v1);
+            if (MASTER) p.set2(j, p0, p1);
+            out.set2(j, p0, p1);
+        }
+        m.store(e.m, i);
+        v.store(e.v, i);
+        if (MASTER) p.store(e.master, i);
+        out.store(e.p, i);
     }
 }
 
-__global__ void __launch_bounds__(kOptThreads) adamw_kernel(const hilore_param *params, int n_params, int64_t n_tiles, AdamArgs a)
+// The four lanes of a quad own one block of 64.  The moments of this step enter the update in fp32, before they are rounded
+// to codes; v holds the codes of sqrt(v), as the square root halves the range that the codes have to span.
+template <int P, int G, bool MASTER> __device__ __forceinline__ void tile_e4m3(const hilore_param &e, const AdamStep &h, int64_t base)
 {
     const int lane = threadIdx.x & 31;
-    const int64_t tile = (int64_t)blockIdx.x * kOptWarps + (threadIdx.x >> 5);
-    if (tile >= n_tiles)
-        return;
-    const float gscale = a.grad_scale ? *a.grad_scale : 1.0f;
-    if (!(fabsf(gscale) < INFINITY)) // the gradients are not finite: parameters and moments stay as they are
+#pragma unroll 1
+    for (int t = 0; t < kTile / 512; ++t) {
+        const int64_t i = base + t * 512 + lane * 16;
+        Raw<G, 16> g;
+        Raw<MASTER ? HILORE_F32 : P, 16> p;
+        const uint4 mc = ld_global_128_stream(static_cast<const uint8_t *>(e.m) + i), rc = ld_global_128_stream(static_cast<const uint8_t *>(e.v) + i);
+        const float ms = e.m_scale[i >> 6], rs = e.v_scale[i >> 6];
+        g.load(e.g, i);
+        p.load(MASTER ? (const void *)e.master : e.p, i);
+        const uint32_t mw[4] = {mc.x, mc.y, mc.z, mc.w}, rw[4] = {rc.x, rc.y, rc.z, rc.w};
+        uint64_t m[8], r[8]; // r: v until its root is taken
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            m[k] = decode2(mw[k >> 1] >> (16 * (k & 1)), ms);
+            r[k] = decode2(rw[k >> 1] >> (16 * (k & 1)), rs);
+            r[k] = f32x2_mul(r[k], r[k]);
+            next_moments(h, g.pair(2 * k), m[k], r[k]);
+        }
+        float am = quad_max(m), ar = quad_max(r); // of v: the root is monotone
+        const bool odd = __any_sync(0xFFFFFFFFu, fmaxf(am, ar) == INFINITY);
+        Raw<P, 16> out;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if (odd) {
+                float v0, v1;
+                f32x2_unpack(r[k], v0, v1);
+                r[k] = f32x2_pack(__fsqrt_rn(v0), __fsqrt_rn(v1));
+            } else {
+                r[k] = root2(r[k]);
+            }
+            float p0, p1;
+            f32x2_unpack(next_param2(h, p.pair(2 * k), m[k], r[k]), p0, p1);
+            if (MASTER) p.set2(2 * k, p0, p1);
+            out.set2(2 * k, p0, p1);
+        }
+        if (MASTER) p.store(e.master, i);
+        out.store(e.p, i);
+        if (odd) {
+            am = quad_max_finite(m);
+            ar = quad_max_finite(r);
+        } else {
+            float unused;
+            f32x2_unpack(root2(both(ar)), ar, unused);
+        }
+        const BlockScale sm = block_scale(am), sr = block_scale(ar);
+        uint32_t w[4];
+        encode16<false>(m, sm, w);
+        *reinterpret_cast<uint4 *>(static_cast<uint8_t *>(e.m) + i) = make_uint4(w[0], w[1], w[2], w[3]);
+        encode16<true>(r, sr, w);
+        *reinterpret_cast<uint4 *>(static_cast<uint8_t *>(e.v) + i) = make_uint4(w[0], w[1], w[2], w[3]);
+        if ((lane & 3) == 0) {
+            e.m_scale[i >> 6] = sm.scale;
+            e.v_scale[i >> 6] = sr.scale;
+        }
+    }
+}
+
+// ---- the last tile of a tensor and tensors off the vectors' alignment: the same arithmetic on single elements, two of
+// every block of 64 in each lane, so that a warp's accesses are next to each other ----
+template <int DTYPE> __device__ __forceinline__ uint32_t load_bits(const void *p, int64_t i) // nothing waits for it here
+{
+    return DTYPE == HILORE_BF16 ? (uint32_t)static_cast<const uint16_t *>(p)[i] : static_cast<const uint32_t *>(p)[i];
+}
+template <int DTYPE> __device__ __forceinline__ float from_bits(uint32_t w) { return __uint_as_float(DTYPE == HILORE_BF16 ? w << 16 : w); }
+
+template <bool CODED, int P, int G, bool MASTER> __device__ __noinline__ void tile_ragged(const hilore_param *entry, const AdamStep h, int64_t base)
+{
+    constexpr int B = 4; // blocks in flight
+    constexpr int Q = MASTER ? HILORE_F32 : P;
+    const int lane = threadIdx.x & 31;
+    const int64_t n = entry->n;
+    void *const out = entry->p;
+    float *const master = entry->master;
+    void *const from = MASTER ? (void *)master : out;
+    const void *const grad = entry->g;
+    uint8_t *const mc = static_cast<uint8_t *>(entry->m), *const rc = static_cast<uint8_t *>(entry->v);
+    float *const m32 = static_cast<float *>(entry->m), *const v32 = static_cast<float *>(entry->v);
+    float *const m_scale = entry->m_scale, *const v_scale = entry->v_scale;
+    for (int64_t b0 = base; b0 < min(n, base + kTile); b0 += 64 * B) {
+        uint32_t g[B][2], p[B][2], m[B][2], v[B][2];
+        float ms[B], rs[B];
+#pragma unroll
+        for (int k = 0; k < B; ++k) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int64_t i = b0 + 64 * k + 32 * u + lane;
+                g[k][u] = p[k][u] = m[k][u] = v[k][u] = 0;
+                if (i < n) {
+                    g[k][u] = load_bits<G>(grad, i);
+                    p[k][u] = load_bits<Q>(from, i);
+                    m[k][u] = CODED ? mc[i] : __float_as_uint(m32[i]);
+                    v[k][u] = CODED ? rc[i] : __float_as_uint(v32[i]);
+                }
+            }
+            const bool some = CODED && b0 + 64 * k < n;
+            ms[k] = some ? m_scale[(b0 >> 6) + k] : 0.0f;
+            rs[k] = some ? v_scale[(b0 >> 6) + k] : 0.0f;
+        }
+#pragma unroll
+        for (int k = 0; k < B; ++k) {
+            const int64_t i0 = b0 + 64 * k + lane;
+            uint64_t mm = u32x2_pack(m[k][0], m[k][1]), vv = u32x2_pack(v[k][0], v[k][1]);
+            if (CODED) {
+                mm = decode2(m[k][0] | m[k][1] << 8, ms[k]);
+                vv = decode2(v[k][0] | v[k][1] << 8, rs[k]);
+                vv = f32x2_mul(vv, vv);
+            }
+            next_moments(h, f32x2_pack(from_bits<G>(g[k][0]), from_bits<G>(g[k][1])), mm, vv);
+            float m1[2], v1[2], r[2], q[2];
+            f32x2_unpack(mm, m1[0], m1[1]);
+            f32x2_unpack(vv, v1[0], v1[1]);
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+                r[u] = CODED && v1[u] < 1.17549435e-38f ? 0.0f : __fsqrt_rn(v1[u]);
+            const float p0 = from_bits<Q>(p[k][0]), p1 = from_bits<Q>(p[k][1]);
+            if (CODED) {
+                f32x2_unpack(next_param2(h, f32x2_pack(p0, p1), mm, f32x2_pack(r[0], r[1])), q[0], q[1]);
+            } else {
+                q[0] = next_param(h, p0, m1[0], r[0]);
+                q[1] = next_param(h, p1, m1[1], r[1]);
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int64_t i = i0 + 32 * u;
+                if (i >= n)
+                    continue;
+                if (!CODED) {
+                    m32[i] = m1[u];
+                    v32[i] = v1[u];
+                }
+                if (MASTER) master[i] = q[u];
+                store_one(out, P, i, q[u]);
+            }
+            if (!CODED)
+                continue;
+            const BlockScale sm = block_scale(warp_max_finite(m1[0], m1[1])), sr = block_scale(warp_max_finite(r[0], r[1]));
+            const uint32_t cm = cvt_e4m3x2(__fmul_rn(m1[1], sm.inv), __fmul_rn(m1[0], sm.inv));
+            r[0] = __fmul_rn(r[0], sr.inv);
+            r[1] = __fmul_rn(r[1], sr.inv);
+            uint32_t cr = cvt_e4m3x2(r[1], r[0]);
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                if (sr.fits && r[u] > 0.0f && !(cr >> (8 * u) & 0xFFu)) cr |= 1u << (8 * u);
+                if (i0 + 32 * u < n) {
+                    mc[i0 + 32 * u] = (uint8_t)(cm >> (8 * u));
+                    rc[i0 + 32 * u] = (uint8_t)(cr >> (8 * u));
+                }
+            }
+            if (lane == 0 && b0 + 64 * k < n) {
+                m_scale[(b0 >> 6) + k] = sm.scale;
+                v_scale[(b0 >> 6) + k] = sr.scale;
+            }
+        }
+    }
+}
+
+// Kinds of tables: KIND = state * 6 + gradient type * 3 + (0: bf16, 1: fp32, 2: bf16 with a master copy); kMixed: entries of
+// several kinds, told apart at run time.
+constexpr int kMixed = 12;
+static int kind_of(const hilore_param &e) { return e.state * 6 + e.g_dtype * 3 + (e.master ? 2 : e.p_dtype); }
+
+template <int KIND> __device__ __forceinline__ void tile_of_kind(const hilore_param &e, const AdamStep &h, int64_t base, bool vec)
+{
+    constexpr int G = KIND / 3 % 2, PK = KIND % 3;
+    constexpr int P = PK == 1 ? HILORE_F32 : HILORE_BF16;
+    if (!vec || base + kTile > e.n) tile_ragged<KIND / 6 == HILORE_STATE_E4M3FN, P, G, PK == 2>(&e, h, base);
+    else if (KIND / 6 == HILORE_STATE_F32) tile_f32<P, G, PK == 2>(e, h, base);
+    else tile_e4m3<P, G, PK == 2>(e, h, base);
+}
+
+template <int KIND>
+__global__ void __launch_bounds__(kOptThreads, KIND == kMixed ? 2 : KIND < 6 ? 4 : 3) adamw_kernel(const hilore_param *params, int n_params, int64_t n_tiles, int per_warp, AdamArgs a)
+{
+    const int64_t t0 = ((int64_t)blockIdx.x * kOptWarps + (threadIdx.x >> 5)) * per_warp;
+    if (t0 >= n_tiles)
         return;
     AdamStep h;
-    h.lr = a.lr_dev ? *a.lr_dev : a.lr;
+    h.gscale = a.grad_scale ? *a.grad_scale : 1.0f;
+    if (!(fabsf(h.gscale) < INFINITY)) // the gradients are not finite: parameters and moments stay as they are
+        return;
+    const float lr = a.lr_dev ? *a.lr_dev : a.lr;
     float inv_bc1 = a.inv_bc1;
     h.rsqrt_bc2 = a.rsqrt_bc2;
     if (a.step_dev) {
@@ -348,34 +587,46 @@ __global__ void __launch_bounds__(kOptThreads) adamw_kernel(const hilore_param *
         inv_bc1 = (float)(1.0 / -expm1(t * log(a.beta1)));
         h.rsqrt_bc2 = (float)rsqrt(-expm1(t * log(a.beta2)));
     }
-    h.step = h.lr * inv_bc1;
-    const hilore_param e = params[owner_of(params, n_params, tile)];
-    const int64_t base = (tile - e.first) * kTile;
-    const uintptr_t wide = reinterpret_cast<uintptr_t>(e.p) | reinterpret_cast<uintptr_t>(e.g) | reinterpret_cast<uintptr_t>(e.master);
-    const uintptr_t st = reinterpret_cast<uintptr_t>(e.m) | reinterpret_cast<uintptr_t>(e.v);
-    if (e.state == HILORE_STATE_F32) {
-        const bool vec = ((wide | st) & 31) == 0;
-#pragma unroll 1
-        for (int k = 0; k < kTile / 256; ++k) {
-            const int64_t i = base + k * 256 + lane * 8;
-            const int n = (int)max((int64_t)0, min((int64_t)8, e.n - i));
-            if (n > 0) adam_f32(e, a, h, gscale, i, n, vec);
+    h.b1 = a.b1, h.omb1 = a.omb1, h.b2 = a.b2, h.omb2 = a.omb2, h.eps = a.eps;
+    h.step = lr * inv_bc1;
+    __shared__ hilore_param copies[kOptWarps];
+    Walk walk(params, n_params, copies);
+    const hilore_param &e = *walk.e;
+    bool vec = false;
+    for (int64_t tile = t0; tile < min(t0 + per_warp, n_tiles); ++tile) {
+        if (walk.at(tile)) {
+            const uintptr_t wide = reinterpret_cast<uintptr_t>(e.p) | reinterpret_cast<uintptr_t>(e.g) | reinterpret_cast<uintptr_t>(e.master);
+            const uintptr_t st = reinterpret_cast<uintptr_t>(e.m) | reinterpret_cast<uintptr_t>(e.v);
+            vec = (wide & 31) == 0 && (st & (e.state == HILORE_STATE_F32 ? 31 : 15)) == 0;
+            h.lrwd = lr * e.weight_decay;
         }
-    } else {
-        const bool vec = (wide & 31) == 0 && (st & 15) == 0;
-#pragma unroll 1
-        for (int k = 0; k < kTile / 512; ++k) { // all lanes together: blocks are reduced by shuffles
-            const int64_t i = base + k * 512 + lane * 16;
-            const int n = (int)max((int64_t)0, min((int64_t)16, e.n - i));
-            adam_e4m3(e, a, h, gscale, i, n, vec);
+        const int64_t base = (tile - walk.begin) * kTile;
+        if (KIND < kMixed) {
+            tile_of_kind<KIND == kMixed ? 0 : KIND>(e, h, base, vec);
+        } else {
+            switch (e.state * 6 + e.g_dtype * 3 + (e.master ? 2 : e.p_dtype)) {
+            case 0: tile_of_kind<0>(e, h, base, vec); break;
+            case 1: tile_of_kind<1>(e, h, base, vec); break;
+            case 2: tile_of_kind<2>(e, h, base, vec); break;
+            case 3: tile_of_kind<3>(e, h, base, vec); break;
+            case 4: tile_of_kind<4>(e, h, base, vec); break;
+            case 5: tile_of_kind<5>(e, h, base, vec); break;
+            case 6: tile_of_kind<6>(e, h, base, vec); break;
+            case 7: tile_of_kind<7>(e, h, base, vec); break;
+            case 8: tile_of_kind<8>(e, h, base, vec); break;
+            case 9: tile_of_kind<9>(e, h, base, vec); break;
+            case 10: tile_of_kind<10>(e, h, base, vec); break;
+            default: tile_of_kind<11>(e, h, base, vec); break;
+            }
         }
     }
 }
 
-// Checks a table and counts its tiles; `for_step`: everything, not the gradients alone.
-static int check_params(const hilore_param *dev, const hilore_param *host, int32_t n, bool for_step, int64_t &tiles)
+// Checks a table, counts its tiles and finds its kind; `for_step`: everything, not the gradients alone.
+static int check_params(const hilore_param *dev, const hilore_param *host, int32_t n, bool for_step, int64_t &tiles, int &kind)
 {
     tiles = 0;
+    kind = -1;
     if (n < 0)
         return HILORE_INVALID_ARG;
     if (n == 0)
@@ -407,6 +658,7 @@ static int check_params(const hilore_param *dev, const hilore_param *host, int32
             return HILORE_ALIGN;
         if (!coded && (!aligned(e.m, 4) || !aligned(e.v, 4)))
             return HILORE_ALIGN;
+        if (e.n > 0) kind = kind < 0 || kind == kind_of(e) ? kind_of(e) : kMixed;
     }
     return status;
 }
@@ -421,9 +673,10 @@ extern "C" int hilore_grad_norm(const hilore_param *params_dev, const hilore_par
                                 float *scale, void *workspace, size_t workspace_bytes, void *stream)
 {
     int64_t tiles = 0;
+    int kind = 0;
     if (!(max_norm >= 0.0) || !workspace || (!norm && !scale))
         return HILORE_INVALID_ARG;
-    const int bad = check_params(params_dev, params_host, n_params, false, tiles);
+    const int bad = check_params(params_dev, params_host, n_params, false, tiles, kind);
     if (bad)
         return bad;
     if (!aligned(norm, 4) || !aligned(scale, 4) || !aligned(workspace, 16))
@@ -432,10 +685,12 @@ extern "C" int hilore_grad_norm(const hilore_param *params_dev, const hilore_par
         return HILORE_WORKSPACE;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     int64_t grid = (int64_t)sm_count() * ctas_per_sm(grad_norm_kernel, kOptThreads, 0, 4);
+    const int per_warp = tiles_per_warp(tiles);
+    const int64_t share = (int64_t)kOptWarps * per_warp;
     if (grid > kNormMaxGrid) grid = kNormMaxGrid;
-    if (grid > (tiles + kOptWarps - 1) / kOptWarps) grid = (tiles + kOptWarps - 1) / kOptWarps;
+    if (grid > (tiles + share - 1) / share) grid = (tiles + share - 1) / share;
     double *partial = static_cast<double *>(workspace);
-    if (grid > 0) grad_norm_kernel<<<(unsigned)grid, kOptThreads, 0, st>>>(params_dev, n_params, tiles, partial);
+    if (grid > 0) grad_norm_kernel<<<(unsigned)grid, kOptThreads, 0, st>>>(params_dev, n_params, tiles, per_warp, partial);
     grad_norm_final_kernel<<<1, kOptThreads, 0, st>>>(partial, (int)grid, max_norm, norm, scale);
     return cudaGetLastError() == cudaSuccess ? HILORE_OK : HILORE_CUDA;
 }
@@ -445,18 +700,20 @@ extern "C" int hilore_adamw_step(const hilore_param *params_dev, const hilore_pa
                                  void *stream)
 {
     int64_t tiles = 0;
+    int kind = 0;
     if (!(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !(eps >= 0.0) || !std::isfinite(lr))
         return HILORE_INVALID_ARG;
     if (!step_dev && step < 1)
         return HILORE_INVALID_ARG;
-    const int bad = check_params(params_dev, params_host, n_params, true, tiles);
+    const int bad = check_params(params_dev, params_host, n_params, true, tiles, kind);
     if (bad)
         return bad;
     if (!aligned(lr_dev, 4) || !aligned(step_dev, 8) || !aligned(grad_scale, 4))
         return HILORE_ALIGN;
     if (tiles == 0)
         return HILORE_OK;
-    const int64_t grid = (tiles + kOptWarps - 1) / kOptWarps;
+    const int per_warp = tiles_per_warp(tiles);
+    const int64_t share = (int64_t)kOptWarps * per_warp, grid = (tiles + share - 1) / share;
     if (grid > 0x7FFFFFFF)
         return HILORE_SHAPE;
     AdamArgs a{};
@@ -475,6 +732,9 @@ extern "C" int hilore_adamw_step(const hilore_param *params_dev, const hilore_pa
     a.lr_dev = lr_dev;
     a.grad_scale = grad_scale;
     a.step_dev = step_dev;
-    adamw_kernel<<<(unsigned)grid, kOptThreads, 0, static_cast<cudaStream_t>(stream)>>>(params_dev, n_params, tiles, a);
+    static void (*const kernels[])(const hilore_param *, int, int64_t, int, AdamArgs) = {
+        adamw_kernel<0>, adamw_kernel<1>, adamw_kernel<2>, adamw_kernel<3>, adamw_kernel<4>,  adamw_kernel<5>,  adamw_kernel<6>,
+        adamw_kernel<7>, adamw_kernel<8>, adamw_kernel<9>, adamw_kernel<10>, adamw_kernel<11>, adamw_kernel<kMixed>};
+    kernels[kind]<<<(unsigned)grid, kOptThreads, 0, static_cast<cudaStream_t>(stream)>>>(params_dev, n_params, tiles, per_warp, a);
     return cudaGetLastError() == cudaSuccess ? HILORE_OK : HILORE_CUDA;
 }
