@@ -10,7 +10,7 @@ LIB = os.path.join(HERE, "libhilore_b200.so")
 SOURCES = ["codec.cu", "grpo.cu", "allocate.cu", "calib.cu", "diag.cu", "logits.cu", "optim.cu"]
 HEADERS = ["common.cuh", "codec.cuh", os.path.join("..", "..", "include", "hilore.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
-              "-Xcompiler", "-fPIC", "-shared"]
+              "-Xcompiler", "-fPIC", "-shared", "--threads", "0"]
 
 
 def _stale() -> bool:

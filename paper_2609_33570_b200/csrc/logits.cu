@@ -228,7 +228,7 @@ __device__ __forceinline__ bool is_denied(const uint32_t *words, int v) { return
 
 // The listed tokens of a range [first, last) of positions: a table with one word per position -- kSeen if the token occurs
 // in the prompt part of the history, 11 bits of the number of the last bias entry that names it, 20 bits of its occurrences
-// in the generated part -- and the places that are not zero, in the order they were found (which no result depends on).
+// in the generated part -- and the places that are not zero, in the order they were found.
 // A row with a longer bias list or a longer generated part takes two words per position and ranges of half the width.
 constexpr int kWords = 8192;
 constexpr int kCountBits = 20, kBiasBits = 11;
@@ -318,6 +318,29 @@ __device__ __forceinline__ void fill_listed(const hilore_logit_rules &R, const R
             }
         }
     }
+    __syncthreads();
+}
+
+// Puts the list in the order of positions, from the touch bits: a sum over listed tokens must not depend on the order in which
+// atomics found them.  `sums`: one word per warp.  Ends with the CTA synchronised.
+template <int THREADS> __device__ __forceinline__ void order_listed(const Listed &t, uint32_t *sums)
+{
+    static_assert(THREADS == kWords / 32, "one word of touch bits per thread");
+    const int tid = threadIdx.x, lane = tid & 31;
+    uint32_t w = t.touch[tid];
+    uint32_t at = (uint32_t)__popc(w);
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t below = __shfl_up_sync(0xFFFFFFFFu, at, o);
+        if (lane >= o) at += below;
+    }
+    if (lane == 31) sums[tid >> 5] = at;
+    __syncthreads();
+    at -= (uint32_t)__popc(w);
+    for (int k = 0; k < (tid >> 5); ++k)
+        at += sums[k];
+    for (; w; w &= w - 1)
+        t.list[at++] = (uint16_t)(tid * 32 + __ffs((int)w) - 1);
     __syncthreads();
 }
 
@@ -620,6 +643,7 @@ __global__ void __launch_bounds__(kLogpThreads, RULES && sizeof(T) == 4 ? 3 : 4)
     constexpr uint32_t kAll = (1u << N) - 1u;
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ Soft part[kLogpThreads / 32];
+    __shared__ uint32_t sums[kLogpThreads / 32];
     __shared__ Soft shares[kMaxRowCtas];
     __shared__ float target_z; // the target's logit under penalties and bias; in the cluster's first CTA
     __shared__ int n_listed;
@@ -697,6 +721,7 @@ __global__ void __launch_bounds__(kLogpThreads, RULES && sizeof(T) == 4 ? 3 : 4)
                 t.first = a;
                 __syncthreads(); // the previous range is done with the table
                 fill_listed<kLogpThreads>(R, q, V, src.lead, e, t, head);
+                order_listed<kLogpThreads>(t, sums);
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     const int s = (u * kLogpThreads + tid) * N;

@@ -175,6 +175,8 @@ __global__ void __launch_bounds__(kOptThreads, 4) grad_norm_kernel(const hilore_
 {
     const int lane = threadIdx.x & 31;
     double sum = 0.0;
+    grid_dependency_wait();
+    grid_dependency_release();
     __shared__ hilore_param copies[kOptWarps];
     Walk walk(params, n_params, copies);
     const int64_t stride = (int64_t)gridDim.x * kOptWarps * per_warp;
@@ -201,6 +203,8 @@ __global__ void __launch_bounds__(kOptThreads) grad_norm_final_kernel(const doub
 {
     __shared__ double sm[kOptWarps];
     double sum = 0.0;
+    grid_dependency_wait();
+    grid_dependency_release();
     for (int i = threadIdx.x; i < n; i += kOptThreads)
         sum += partial[i];
     sum = warp_sum(sum);
@@ -360,12 +364,12 @@ template <bool ROOT> __device__ __forceinline__ void encode16(const uint64_t (&x
 }
 
 // ---- whole tiles: vectors, types known at compile time ----
-template <int P, int G, bool MASTER> __device__ __forceinline__ void tile_f32(const hilore_param &e, const AdamStep &h, int64_t base)
+template <int P, int G, bool MASTER, int LEN> __device__ __forceinline__ void tile_f32(const hilore_param &e, const AdamStep &h, int64_t base)
 {
     const int lane = threadIdx.x & 31;
 #pragma unroll 1
-    for (int k = 0; k < kTile / 256; ++k) {
-        const int64_t i = base + k * 256 + lane * 8;
+    for (int k = 0; k < LEN; k += 256) {
+        const int64_t i = base + k + lane * 8;
         Raw<G, 8> g;
         Raw<HILORE_F32, 8> m, v;
         Raw<MASTER ? HILORE_F32 : P, 8> p;
@@ -396,12 +400,12 @@ template <int P, int G, bool MASTER> __device__ __forceinline__ void tile_f32(co
 
 // The four lanes of a quad own one block of 64.  The moments of this step enter the update in fp32, before they are rounded
 // to codes; v holds the codes of sqrt(v), as the square root halves the range that the codes have to span.
-template <int P, int G, bool MASTER> __device__ __forceinline__ void tile_e4m3(const hilore_param &e, const AdamStep &h, int64_t base)
+template <int P, int G, bool MASTER, int LEN> __device__ __forceinline__ void tile_e4m3(const hilore_param &e, const AdamStep &h, int64_t base)
 {
     const int lane = threadIdx.x & 31;
 #pragma unroll 1
-    for (int t = 0; t < kTile / 512; ++t) {
-        const int64_t i = base + t * 512 + lane * 16;
+    for (int t = 0; t < LEN; t += 512) {
+        const int64_t i = base + t + lane * 16;
         Raw<G, 16> g;
         Raw<MASTER ? HILORE_F32 : P, 16> p;
         const uint4 mc = ld_global_128_stream(static_cast<const uint8_t *>(e.m) + i), rc = ld_global_128_stream(static_cast<const uint8_t *>(e.v) + i);
@@ -464,7 +468,7 @@ template <int DTYPE> __device__ __forceinline__ uint32_t load_bits(const void *p
 }
 template <int DTYPE> __device__ __forceinline__ float from_bits(uint32_t w) { return __uint_as_float(DTYPE == HILORE_BF16 ? w << 16 : w); }
 
-template <bool CODED, int P, int G, bool MASTER> __device__ __noinline__ void tile_ragged(const hilore_param *entry, const AdamStep h, int64_t base)
+template <bool CODED, int P, int G, bool MASTER> __device__ __noinline__ void tile_ragged(const hilore_param *entry, const AdamStep h, int64_t base, int len)
 {
     constexpr int B = 4; // blocks in flight
     constexpr int Q = MASTER ? HILORE_F32 : P;
@@ -477,7 +481,7 @@ template <bool CODED, int P, int G, bool MASTER> __device__ __noinline__ void ti
     uint8_t *const mc = static_cast<uint8_t *>(entry->m), *const rc = static_cast<uint8_t *>(entry->v);
     float *const m32 = static_cast<float *>(entry->m), *const v32 = static_cast<float *>(entry->v);
     float *const m_scale = entry->m_scale, *const v_scale = entry->v_scale;
-    for (int64_t b0 = base; b0 < min(n, base + kTile); b0 += 64 * B) {
+    for (int64_t b0 = base; b0 < min(n, base + len); b0 += 64 * B) {
         uint32_t g[B][2], p[B][2], m[B][2], v[B][2];
         float ms[B], rs[B];
 #pragma unroll
@@ -560,23 +564,33 @@ template <bool CODED, int P, int G, bool MASTER> __device__ __noinline__ void ti
 constexpr int kMixed = 12;
 static int kind_of(const hilore_param &e) { return e.state * 6 + e.g_dtype * 3 + (e.master ? 2 : e.p_dtype); }
 
-template <int KIND> __device__ __forceinline__ void tile_of_kind(const hilore_param &e, const AdamStep &h, int64_t base, bool vec)
+template <int KIND, int LEN> __device__ __forceinline__ void tile_of_kind(const hilore_param &e, const AdamStep &h, int64_t base, bool vec)
 {
     constexpr int G = KIND / 3 % 2, PK = KIND % 3;
     constexpr int P = PK == 1 ? HILORE_F32 : HILORE_BF16;
-    if (!vec || base + kTile > e.n) tile_ragged<KIND / 6 == HILORE_STATE_E4M3FN, P, G, PK == 2>(&e, h, base);
-    else if (KIND / 6 == HILORE_STATE_F32) tile_f32<P, G, PK == 2>(e, h, base);
-    else tile_e4m3<P, G, PK == 2>(e, h, base);
+    if (!vec || base + LEN > e.n) tile_ragged<KIND / 6 == HILORE_STATE_E4M3FN, P, G, PK == 2>(&e, h, base, LEN);
+    else if (KIND / 6 == HILORE_STATE_F32) tile_f32<P, G, PK == 2, LEN>(e, h, base);
+    else tile_e4m3<P, G, PK == 2, LEN>(e, h, base);
 }
 
-template <int KIND>
-__global__ void __launch_bounds__(kOptThreads, KIND == kMixed ? 2 : KIND < 6 ? 4 : 3) adamw_kernel(const hilore_param *params, int n_params, int64_t n_tiles, int per_warp, AdamArgs a)
+// Registers: 64 for 32-bit states and for all-bf16 tables with 8-bit ones (900 M elements 1.70 ms, 1.80 with 80 registers), 80 where
+// fp32 parameters or gradients are held beside 8-bit states (33 M elements 99.4 us, 101.6 with 64).
+// SPLIT: warps per tile; two where there are few tiles, for the latency.
+template <int KIND, int SPLIT>
+__global__ void __launch_bounds__(kOptThreads, KIND == kMixed ? 2 : KIND <= 6 ? 4 : 3) adamw_kernel(const hilore_param *params, int n_params, int64_t n_tiles, int per_warp, AdamArgs a)
 {
-    const int64_t t0 = ((int64_t)blockIdx.x * kOptWarps + (threadIdx.x >> 5)) * per_warp;
+    // From the last tile to the first: a norm taken just before has left the end of the gradients in L2.
+    const int64_t w = (int64_t)(gridDim.x - 1 - blockIdx.x) * kOptWarps + (threadIdx.x >> 5), t0 = w / SPLIT * per_warp;
+    const int skip = (int)(w % SPLIT) * (kTile / SPLIT);
+    grid_dependency_wait();
     if (t0 >= n_tiles)
         return;
     AdamStep h;
     h.gscale = a.grad_scale ? *a.grad_scale : 1.0f;
+    __shared__ hilore_param copies[kOptWarps];
+    Walk walk(params, n_params, copies);
+    const hilore_param &e = *walk.e;
+    if (SPLIT > 1) walk.at(t0); // while the scale is on its way
     if (!(fabsf(h.gscale) < INFINITY)) // the gradients are not finite: parameters and moments stay as they are
         return;
     const float lr = a.lr_dev ? *a.lr_dev : a.lr;
@@ -589,34 +603,31 @@ __global__ void __launch_bounds__(kOptThreads, KIND == kMixed ? 2 : KIND < 6 ? 4
     }
     h.b1 = a.b1, h.omb1 = a.omb1, h.b2 = a.b2, h.omb2 = a.omb2, h.eps = a.eps;
     h.step = lr * inv_bc1;
-    __shared__ hilore_param copies[kOptWarps];
-    Walk walk(params, n_params, copies);
-    const hilore_param &e = *walk.e;
     bool vec = false;
     for (int64_t tile = t0; tile < min(t0 + per_warp, n_tiles); ++tile) {
-        if (walk.at(tile)) {
+        if (walk.at(tile) || (SPLIT > 1 && tile == t0)) {
             const uintptr_t wide = reinterpret_cast<uintptr_t>(e.p) | reinterpret_cast<uintptr_t>(e.g) | reinterpret_cast<uintptr_t>(e.master);
             const uintptr_t st = reinterpret_cast<uintptr_t>(e.m) | reinterpret_cast<uintptr_t>(e.v);
             vec = (wide & 31) == 0 && (st & (e.state == HILORE_STATE_F32 ? 31 : 15)) == 0;
             h.lrwd = lr * e.weight_decay;
         }
-        const int64_t base = (tile - walk.begin) * kTile;
+        const int64_t base = (tile - walk.begin) * kTile + skip;
         if (KIND < kMixed) {
-            tile_of_kind<KIND == kMixed ? 0 : KIND>(e, h, base, vec);
+            tile_of_kind<KIND == kMixed ? 0 : KIND, kTile / SPLIT>(e, h, base, vec);
         } else {
             switch (e.state * 6 + e.g_dtype * 3 + (e.master ? 2 : e.p_dtype)) {
-            case 0: tile_of_kind<0>(e, h, base, vec); break;
-            case 1: tile_of_kind<1>(e, h, base, vec); break;
-            case 2: tile_of_kind<2>(e, h, base, vec); break;
-            case 3: tile_of_kind<3>(e, h, base, vec); break;
-            case 4: tile_of_kind<4>(e, h, base, vec); break;
-            case 5: tile_of_kind<5>(e, h, base, vec); break;
-            case 6: tile_of_kind<6>(e, h, base, vec); break;
-            case 7: tile_of_kind<7>(e, h, base, vec); break;
-            case 8: tile_of_kind<8>(e, h, base, vec); break;
-            case 9: tile_of_kind<9>(e, h, base, vec); break;
-            case 10: tile_of_kind<10>(e, h, base, vec); break;
-            default: tile_of_kind<11>(e, h, base, vec); break;
+            case 0: tile_of_kind<0, kTile / SPLIT>(e, h, base, vec); break;
+            case 1: tile_of_kind<1, kTile / SPLIT>(e, h, base, vec); break;
+            case 2: tile_of_kind<2, kTile / SPLIT>(e, h, base, vec); break;
+            case 3: tile_of_kind<3, kTile / SPLIT>(e, h, base, vec); break;
+            case 4: tile_of_kind<4, kTile / SPLIT>(e, h, base, vec); break;
+            case 5: tile_of_kind<5, kTile / SPLIT>(e, h, base, vec); break;
+            case 6: tile_of_kind<6, kTile / SPLIT>(e, h, base, vec); break;
+            case 7: tile_of_kind<7, kTile / SPLIT>(e, h, base, vec); break;
+            case 8: tile_of_kind<8, kTile / SPLIT>(e, h, base, vec); break;
+            case 9: tile_of_kind<9, kTile / SPLIT>(e, h, base, vec); break;
+            case 10: tile_of_kind<10, kTile / SPLIT>(e, h, base, vec); break;
+            default: tile_of_kind<11, kTile / SPLIT>(e, h, base, vec); break;
             }
         }
     }
@@ -690,8 +701,10 @@ extern "C" int hilore_grad_norm(const hilore_param *params_dev, const hilore_par
     if (grid > kNormMaxGrid) grid = kNormMaxGrid;
     if (grid > (tiles + share - 1) / share) grid = (tiles + share - 1) / share;
     double *partial = static_cast<double *>(workspace);
-    if (grid > 0) grad_norm_kernel<<<(unsigned)grid, kOptThreads, 0, st>>>(params_dev, n_params, tiles, per_warp, partial);
-    grad_norm_final_kernel<<<1, kOptThreads, 0, st>>>(partial, (int)grid, max_norm, norm, scale);
+    if (grid > 0 && launch_dependent(grad_norm_kernel, dim3((unsigned)grid), dim3(kOptThreads), 0, st, params_dev, n_params, tiles, per_warp, partial) != cudaSuccess)
+        return HILORE_CUDA;
+    if (launch_dependent(grad_norm_final_kernel, dim3(1), dim3(kOptThreads), 0, st, partial, (int)grid, max_norm, norm, scale) != cudaSuccess)
+        return HILORE_CUDA;
     return cudaGetLastError() == cudaSuccess ? HILORE_OK : HILORE_CUDA;
 }
 
@@ -713,7 +726,8 @@ extern "C" int hilore_adamw_step(const hilore_param *params_dev, const hilore_pa
     if (tiles == 0)
         return HILORE_OK;
     const int per_warp = tiles_per_warp(tiles);
-    const int64_t share = (int64_t)kOptWarps * per_warp, grid = (tiles + share - 1) / share;
+    const int split = tiles <= 8 * (int64_t)sm_count() ? 2 : 1;
+    const int64_t share = (int64_t)kOptWarps * per_warp, grid = (tiles * split + share - 1) / share;
     if (grid > 0x7FFFFFFF)
         return HILORE_SHAPE;
     AdamArgs a{};
@@ -732,9 +746,13 @@ extern "C" int hilore_adamw_step(const hilore_param *params_dev, const hilore_pa
     a.lr_dev = lr_dev;
     a.grad_scale = grad_scale;
     a.step_dev = step_dev;
-    static void (*const kernels[])(const hilore_param *, int, int64_t, int, AdamArgs) = {
-        adamw_kernel<0>, adamw_kernel<1>, adamw_kernel<2>, adamw_kernel<3>, adamw_kernel<4>,  adamw_kernel<5>,  adamw_kernel<6>,
-        adamw_kernel<7>, adamw_kernel<8>, adamw_kernel<9>, adamw_kernel<10>, adamw_kernel<11>, adamw_kernel<kMixed>};
-    kernels[kind]<<<(unsigned)grid, kOptThreads, 0, static_cast<cudaStream_t>(stream)>>>(params_dev, n_params, tiles, per_warp, a);
+#define HILORE_KINDS(S)                                                                                                                         \
+    {adamw_kernel<0, S>, adamw_kernel<1, S>, adamw_kernel<2, S>, adamw_kernel<3, S>,  adamw_kernel<4, S>,  adamw_kernel<5, S>,                   \
+     adamw_kernel<6, S>, adamw_kernel<7, S>, adamw_kernel<8, S>, adamw_kernel<9, S>, adamw_kernel<10, S>, adamw_kernel<11, S>, adamw_kernel<kMixed, S>}
+    static void (*const kernels[2][kMixed + 1])(const hilore_param *, int, int64_t, int, AdamArgs) = {HILORE_KINDS(1), HILORE_KINDS(2)};
+#undef HILORE_KINDS
+    if (launch_dependent(kernels[split - 1][kind], dim3((unsigned)grid), dim3(kOptThreads), 0, static_cast<cudaStream_t>(stream), params_dev, n_params, tiles, per_warp, a) !=
+        cudaSuccess)
+        return HILORE_CUDA;
     return cudaGetLastError() == cudaSuccess ? HILORE_OK : HILORE_CUDA;
 }

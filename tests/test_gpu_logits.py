@@ -337,6 +337,18 @@ def test_rows_of_a_cluster_and_of_one_cta_agree(monkeypatch):
             assert same.all(), (p, q)
 
 
+def test_the_same_call_gives_the_same_bits():
+    """Twenty calls over dense histories: sums do not depend on the order in which listed tokens were found."""
+    rng = np.random.default_rng(12)
+    rows, V = 24, 20011
+    x = logits(rng, rows, V, V, "f32")
+    r = make_rules(rng, rows, V, history=9000, bias=60, grammar="indexed")
+    t = rng.integers(0, V, rows).astype(np.int32)
+    first = run_logp(x, V, r, t, "f32")
+    for _ in range(20):
+        assert all(np.array_equal(a, b, equal_nan=True) for a, b in zip(run_logp(x, V, r, t, "f32"), first))
+
+
 def test_gradient_in_place_and_on_another_stream():
     rng = np.random.default_rng(4)
     rows, V = 33, 12345
