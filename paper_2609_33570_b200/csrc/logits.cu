@@ -3,13 +3,15 @@
 // coefficients omega_t = dL/dlogp_t that the coefficient pass writes.
 //
 // All of it streams rows of V logits once, so HBM is the bound; what a row's rules say about single tokens is kept
-// off that stream.  A CTA owns a range of 8192 tokens of a row.  It scans the row's history and bias list into a table with
-// one word per token in shared memory, with a list of the tokens that occur; the stream runs as if no token were listed,
-// the listed ones are worked out on their own, one per thread, and written over the stream's results or, where a sum is
-// wanted, left out of the stream by one bit per token.  (Counts in global memory would cost 4 bytes per logit, twice the
-// bf16 logits themselves.  Asking the table inside the stream serialises a warp over its listed tokens: gradients of
-// 2048 x 128256 bf16 rows under prefixes of up to 1536 tokens took 329 us that way.  A hash table over a larger range needs
-// fewer scans but probes and overflows: 96 rows of 151936 fp32 logits with histories up to 16384 took 320 us, 111 before.)
+// off that stream.  A CTA owns a range of the vocabulary and walks a block of consecutive rows.  It keeps the tokens of the
+// row's history in a table of counts in shared memory, with a list of those that occur.  The slots of a training sequence
+// have growing prefixes of one sequence as their histories: going to the next row then adds a token or two to the table
+// where a first version cleared it and scanned the history again (gradients of 2048 x 128256 bf16 rows under prefixes of up
+// to 1536 tokens 301 us).  The stream runs as if no token were listed; the listed ones are worked out on their own,
+// one per thread, and written over the stream's results or, where a sum is wanted, left out of the stream by one bit per
+// token.  (Counts in global memory would cost 4 bytes per logit, twice the bf16 logits themselves.  Asking the table inside
+// the stream serialises a warp over its listed tokens: 329 us.  A hash table over a larger range needs fewer scans but probes and
+// overflows: 96 rows of 151936 fp32 logits with histories up to 16384 took 320 us, 111 with the table asked in the stream.)
 #include "common.cuh"
 
 #include <cooperative_groups.h>
@@ -185,27 +187,36 @@ struct RowRules {
     int64_t hist_lo, hist_mid, hist_hi; // history; empty where the penalties of the row are neutral
     int64_t bias_lo, bias_hi;
     const uint32_t *mask; // words of the grammar, or nullptr
+    __device__ __forceinline__ bool history() const { return hist_lo < hist_hi; }
     __device__ __forceinline__ bool listed() const { return hist_lo < hist_hi || bias_lo < bias_hi; }
 };
+
+__device__ __forceinline__ float inverse_temperature(const float *temperature, int64_t row)
+{
+    const float t = temperature ? temperature[row] : 1.0f;
+    return t > 0.0f ? __fdiv_rn(1.0f, t) : 1.0f; // 0 (greedy) and what is no temperature: not scaled
+}
 
 __device__ __forceinline__ RowRules row_rules(const hilore_logit_rules &R, int64_t row)
 {
     RowRules q;
-    const float t = R.temperature ? R.temperature[row] : 1.0f;
-    q.inv_temp = t > 0.0f ? __fdiv_rn(1.0f, t) : 1.0f; // 0 (greedy) and what is no temperature: not scaled
+    q.inv_temp = inverse_temperature(R.temperature, row);
     q.rep = R.repetition ? R.repetition[row] : 1.0f;
     q.inv_rep = __fdiv_rn(1.0f, q.rep);
     q.freq = R.frequency ? R.frequency[row] : 0.0f;
     q.pres = R.presence ? R.presence[row] : 0.0f;
     q.hist_lo = q.hist_hi = q.hist_mid = q.bias_lo = q.bias_hi = 0;
-    if (R.tokens && !(q.rep == 1.0f && q.freq == 0.0f && q.pres == 0.0f)) {
-        q.hist_lo = max((int64_t)0, R.hist_begin[row]);
-        q.hist_hi = min(R.n_tokens, R.hist_end[row]);
-        q.hist_mid = R.resp_begin[row];
+    if (R.tokens) {
+        const int64_t lo = max((int64_t)0, R.hist_begin[row]), mid = R.resp_begin[row], hi = min(R.n_tokens, R.hist_end[row]);
+        if (lo < hi && !(q.rep == 1.0f && q.freq == 0.0f && q.pres == 0.0f)) {
+            q.hist_lo = lo;
+            q.hist_mid = min(max(mid, lo), hi);
+            q.hist_hi = hi;
+        }
     }
     if (R.bias_tokens) {
         q.bias_lo = max((int64_t)0, R.bias_offsets[row]);
-        q.bias_hi = min(R.n_bias, R.bias_offsets[row + 1]);
+        q.bias_hi = max(q.bias_lo, min(R.n_bias, R.bias_offsets[row + 1]));
     }
     q.mask = nullptr;
     if (R.allow) {
@@ -226,149 +237,226 @@ template <int N> __device__ __forceinline__ uint32_t denied(const uint32_t *word
 
 __device__ __forceinline__ bool is_denied(const uint32_t *words, int v) { return words != nullptr && !(__ldg(words + (v >> 5)) >> (v & 31) & 1u); }
 
-// The listed tokens of a range [first, last) of positions: a table with one word per position -- kSeen if the token occurs
-// in the prompt part of the history, 11 bits of the number of the last bias entry that names it, 20 bits of its occurrences
-// in the generated part -- and the places that are not zero, in the order they were found.
-// A row with a longer bias list or a longer generated part takes two words per position and ranges of half the width.
-constexpr int kWords = 8192;
-constexpr int kCountBits = 20, kBiasBits = 11;
+// The tokens of a row's history that fall into a range of `width` tokens from v0 on, in a table of counts: occurrences in the
+// generated part, with the top bit set if the token occurs in the prompt part.  Three forms of the table:
+//   kCount16  16 bits per token, for generated parts below 2^15 tokens;
+//   kCount32  32 bits per token;
+//   kBiased   two words per token, the second one the number of the last entry of the bias list that names it, for lists of
+//             more than kBiasCap entries.  Shorter ones are kept beside the table: bias_v[k] is the token of entry k if it is in
+//             the range (else -1), and `biased` has its bit.
+// Places that are not zero are also listed, in the order they were found, as far as the list reaches.
+enum { kCount16 = 0, kCount32 = 1, kBiased = 2 };
+constexpr int kBiasCap = 512;
+constexpr int kSlack = 16;    // a range of positions [a, e) covers tokens from a - 15 on, depending on the row's alignment
+constexpr int kBlockRows = 8; // rows of a block at most
 
-struct Listed {
-    uint32_t *word;  // [kWords]
-    uint16_t *list;  // [kWords]
-    uint32_t *touch; // [kWords / 32] bit f - first: the token at position f is listed; nullptr where the stream does not ask
-    int *n;          // entries of the list
-    int first;
-    bool wide;
+__device__ __forceinline__ int table_words(int form, int width) { return form == kCount16 ? (width + 1) >> 1 : form == kCount32 ? width : 2 * width; }
+
+// A row of a CTA's block: its rules, and how to get from the table of the row before to this one's.
+struct RowPlan {
+    RowRules q;
+    int form, n_bias;         // n_bias: entries of a short list
+    bool used;                // the row is worked on
+    bool follows;             // its history is that of the last row with a table and the `fresh` tokens from `from` on
+    int fresh, fresh_prompt;  // ... of which the first fresh_prompt are prompt
+    const int32_t *from;
 };
 
-constexpr size_t kListedBytes = kWords * 6 + kWords / 8;
-
-__device__ __forceinline__ Listed listed_at(unsigned char *smem, const RowRules &q, bool bits, int *n)
+// Plans of a block's rows, one thread each.  `used` is set.  Ends with the CTA synchronised.
+__device__ __forceinline__ void plan_rows(RowPlan *plan, int rows, const hilore_logit_rules &R)
 {
-    Listed t;
-    t.word = reinterpret_cast<uint32_t *>(smem);
-    t.touch = bits ? t.word + kWords : nullptr;
-    t.list = reinterpret_cast<uint16_t *>(t.word + kWords + kWords / 32);
-    t.n = n;
-    t.first = 0;
-    t.wide = q.hist_hi - q.hist_mid >= (1 << kCountBits) || q.bias_hi - q.bias_lo >= (1 << kBiasBits);
-    return t;
-}
-
-__device__ __forceinline__ void list_place(const Listed &t, uint32_t s)
-{
-    t.list[atomicAdd(t.n, 1)] = (uint16_t)s;
-    if (t.touch) atomicOr(t.touch + (s >> 5), 1u << (s & 31));
-}
-
-constexpr int kScan = 8; // history tokens in flight per thread
-
-// Up to kScan * THREADS tokens of the history from i0 on (-1 past its end).
-template <int THREADS> __device__ __forceinline__ void history_load(const hilore_logit_rules &R, const RowRules &q, int64_t i0, int (&v)[kScan])
-{
-#pragma unroll
-    for (int u = 0; u < kScan; ++u) {
-        const int64_t i = i0 + u * THREADS + threadIdx.x;
-        v[u] = i < q.hist_hi ? __ldg(R.tokens + i) : -1;
+    const int i = threadIdx.x;
+    if (i < rows) {
+        RowPlan &p = plan[i];
+        const int64_t list = p.q.bias_hi - p.q.bias_lo;
+        p.n_bias = list <= kBiasCap ? (int)list : 0;
+        p.form = list > kBiasCap ? kBiased : p.q.hist_hi - p.q.hist_mid < (1 << 15) ? kCount16 : kCount32;
     }
+    __syncthreads();
+    if (i < rows) {
+        RowPlan &p = plan[i];
+        p.follows = false;
+        p.fresh = p.fresh_prompt = 0;
+        p.from = R.tokens;
+        int j = -1; // the last row before this one that leaves a table
+        for (int k = 0; k < i; ++k)
+            if (plan[k].used && (plan[k].q.history() || plan[k].form == kBiased)) j = k;
+        if (j >= 0 && p.q.history() && p.form != kBiased && plan[j].form == p.form) {
+            const RowRules &a = plan[j].q, &b = p.q;
+            // the same tokens of the common part are prompt, and few enough come after it
+            p.follows = a.hist_lo == b.hist_lo && a.hist_hi <= b.hist_hi && a.hist_mid == min(b.hist_mid, a.hist_hi) && b.hist_hi - a.hist_hi < (1 << 20);
+            if (p.follows) {
+                p.from = R.tokens + a.hist_hi;
+                p.fresh = (int)(b.hist_hi - a.hist_hi);
+                p.fresh_prompt = (int)max((int64_t)0, b.hist_mid - a.hist_hi);
+            }
+        }
+    }
+    __syncthreads();
 }
 
-// Fills table and list for positions [t.first, last).  `head`: the first kScan * THREADS tokens of the history, which a
-// caller with several ranges keeps in registers.  Ends with the CTA synchronised.
-template <int THREADS>
-__device__ __forceinline__ void fill_listed(const hilore_logit_rules &R, const RowRules &q, int V, int lead, int last, const Listed &t,
-                                            const int (&head)[kScan])
-{
-    const int tid = threadIdx.x;
-    const int words = kWords + (t.touch ? kWords / 32 : 0);
-    for (int i = tid; i < words / 4; i += THREADS)
-        reinterpret_cast<uint4 *>(t.word)[i] = make_uint4(0, 0, 0, 0);
-    if (tid == 0) *t.n = 0;
-    __syncthreads();
-    const int v0 = t.first - lead;
-    const uint32_t width = (uint32_t)(last - t.first);
-    if (q.bias_lo < q.bias_hi) { // before the counts: the largest number of a word is that of the last entry
-        for (int64_t i = q.bias_lo + tid; i < q.bias_hi; i += THREADS) {
-            const int v = __ldg(R.bias_tokens + i);
-            const uint32_t s = (uint32_t)(v - v0), k = (uint32_t)(i - q.bias_lo) + 1u;
-            if (s < width && (uint32_t)v < (uint32_t)V) {
-                const uint32_t old = t.wide ? atomicMax(t.word + 2 * s + 1, k) : atomicMax(t.word + s, k << kCountBits);
-                if (old == 0) list_place(t, s);
+// Layout in shared memory: biased [BITS] (bit v - v0: a short bias list names the token), touch [BITS] where TOUCH (bit v - v0:
+// the history names the token), bias_v [kBiasCap], then the table.
+template <int BITS, bool TOUCH> struct Listed {
+    static constexpr int kFixed = BITS * 4 * (TOUCH ? 2 : 1) + kBiasCap * 4; // bytes before the table
+    static_assert(BITS % 4 == 0, "16-byte pieces");
+    unsigned char *base;
+    int *n; // places found; above the capacity of the list it is not complete
+
+    __device__ __forceinline__ uint32_t *biased() const { return reinterpret_cast<uint32_t *>(base); }
+    __device__ __forceinline__ uint32_t *touch() const { return reinterpret_cast<uint32_t *>(base + (TOUCH ? BITS * 4 : 0)); }
+    __device__ __forceinline__ int *bias_v() const { return reinterpret_cast<int *>(base + BITS * 4 * (TOUCH ? 2 : 1)); }
+    __device__ __forceinline__ uint32_t *word() const { return reinterpret_cast<uint32_t *>(base + kFixed); }
+    __device__ __forceinline__ uint32_t count_at(int s, int form) const
+    {
+        if (form == kCount32) return word()[s];
+        if (form == kBiased) return word()[2 * s];
+        const uint32_t h = word()[s >> 1] >> (16 * (s & 1)) & 0xFFFFu;
+        return (h & 0x7FFFu) | (h >> 15 << 31);
+    }
+    __device__ __forceinline__ bool is_biased(int s) const { return biased()[s >> 5] >> (s & 31) & 1u; }
+    __device__ __forceinline__ void place(uint32_t s, uint16_t *list, int cap) const
+    {
+        const int at = atomicAdd(n, 1);
+        if (at < cap) list[at] = (uint16_t)s;
+        if (TOUCH) atomicOr(touch() + (s >> 5), 1u << (s & 31));
+    }
+    __device__ __forceinline__ void add(int v, bool prompt, int V, int v0, int width, int form, uint16_t *list, int cap) const
+    {
+        const uint32_t s = (uint32_t)(v - v0);
+        if (s >= (uint32_t)width || (uint32_t)v >= (uint32_t)V)
+            return;
+        uint32_t old;
+        if (form == kCount16) {
+            const int sh = 16 * (s & 1);
+            old = prompt ? atomicOr(word() + (s >> 1), 0x8000u << sh) : atomicAdd(word() + (s >> 1), 1u << sh);
+            old = old >> sh & 0xFFFFu;
+        } else {
+            uint32_t *w = word() + (form == kBiased ? 2 * s : s);
+            old = prompt ? atomicOr(w, kSeen) : atomicAdd(w, 1u);
+            if (form == kBiased) old |= w[1];
+        }
+        if (old == 0) place(s, list, cap);
+    }
+
+    // Brings table and bias entries to the row's rules for tokens [v0, v0 + width).  `follow`: by adding the plan's fresh tokens to the
+    // table of the row before.  Ends with the CTA synchronised.
+    template <int THREADS>
+    __device__ __forceinline__ void fill(const hilore_logit_rules &R, const RowPlan &p, int V, int v0, int width, int form, bool follow, uint16_t *list,
+                                         int cap) const
+    {
+        const int tid = threadIdx.x;
+        const bool counts = p.q.history() || form == kBiased, clear = counts && !follow;
+        if (clear || p.n_bias > 0) {
+            __syncthreads(); // the row before is done with both
+            if (clear) {
+                const int quads = (table_words(form, width) + 3) >> 2;
+                for (int i = tid; i < quads; i += THREADS)
+                    reinterpret_cast<uint4 *>(word())[i] = make_uint4(0, 0, 0, 0);
+                if (TOUCH)
+                    for (int i = tid; i < BITS / 4; i += THREADS)
+                        reinterpret_cast<uint4 *>(touch())[i] = make_uint4(0, 0, 0, 0);
+                if (tid == 0) *n = 0;
+            }
+            if (p.n_bias > 0)
+                for (int i = tid; i < BITS / 4; i += THREADS)
+                    reinterpret_cast<uint4 *>(biased())[i] = make_uint4(0, 0, 0, 0);
+            __syncthreads();
+            for (int64_t i = p.q.bias_lo + tid; i < p.q.bias_hi; i += THREADS) {
+                const int v = __ldg(R.bias_tokens + i), k = (int)(i - p.q.bias_lo);
+                const uint32_t s = (uint32_t)(v - v0);
+                const bool in = s < (uint32_t)width && (uint32_t)v < (uint32_t)V;
+                if (form != kBiased) {
+                    bias_v()[k] = in ? v : -1;
+                    if (in) atomicOr(biased() + (s >> 5), 1u << (s & 31));
+                } else if (in && atomicMax(word() + 2 * s + 1, (uint32_t)k + 1u) == 0) {
+                    place(s, list, cap);
+                }
+            }
+            if (form == kBiased) __syncthreads();
+        }
+        if (follow) {
+            for (int i = tid; i < p.fresh; i += THREADS)
+                add(__ldg(p.from + i), i < p.fresh_prompt, V, v0, width, form, list, cap);
+        } else if (p.q.history()) {
+            constexpr int U = 8; // tokens in flight per thread
+            const int32_t *from = R.tokens + p.q.hist_lo;
+            int64_t left = p.q.hist_hi - p.q.hist_lo, prompt = p.q.hist_mid - p.q.hist_lo;
+            for (; left > 0; left -= THREADS * U, prompt -= THREADS * U, from += THREADS * U) {
+                const int here = (int)min(left, (int64_t)(THREADS * U)), first = (int)max((int64_t)0, min(prompt, (int64_t)(THREADS * U)));
+                int v[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    v[u] = u * THREADS + tid < here ? __ldg(from + u * THREADS + tid) : -1;
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    if (u * THREADS >= here)
+                        break;
+                    add(v[u], u * THREADS + tid < first, V, v0, width, form, list, cap);
+                }
             }
         }
         __syncthreads();
     }
-    for (int64_t i0 = q.hist_lo; i0 < q.hist_hi; i0 += THREADS * kScan) {
-        int v[kScan];
-        if (i0 == q.hist_lo) {
-#pragma unroll
-            for (int u = 0; u < kScan; ++u)
-                v[u] = head[u];
-        } else {
-            history_load<THREADS>(R, q, i0, v);
-        }
-#pragma unroll
-        for (int u = 0; u < kScan; ++u) {
-            const uint32_t s = (uint32_t)(v[u] - v0);
-            if (s < width && (uint32_t)v[u] < (uint32_t)V) {
-                uint32_t *w = t.word + (t.wide ? 2 * s : s);
-                const uint32_t old = i0 + u * THREADS + tid < q.hist_mid ? atomicOr(w, kSeen) : atomicAdd(w, 1u);
-                if (old == 0 && !(t.wide && w[1] != 0)) list_place(t, s);
-            }
-        }
-    }
-    __syncthreads();
-}
 
-// Puts the list in the order of positions, from the touch bits: a sum over listed tokens must not depend on the order in which
-// atomics found them.  `sums`: one word per warp.  Ends with the CTA synchronised.
-template <int THREADS> __device__ __forceinline__ void order_listed(const Listed &t, uint32_t *sums)
-{
-    static_assert(THREADS == kWords / 32, "one word of touch bits per thread");
-    const int tid = threadIdx.x, lane = tid & 31;
-    uint32_t w = t.touch[tid];
-    uint32_t at = (uint32_t)__popc(w);
+    // Puts the list in the order of places, from the touch bits: a sum over listed tokens must not depend on the order in
+    // which atomics found them.  `sums`: one word per warp.  Ends with the CTA synchronised.
+    template <int THREADS> __device__ __forceinline__ void order(uint32_t *sums, uint16_t *list) const
+    {
+        constexpr int W = (BITS + THREADS - 1) / THREADS;
+        const int tid = threadIdx.x, lane = tid & 31;
+        uint32_t w[W], own = 0;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t below = __shfl_up_sync(0xFFFFFFFFu, at, o);
-        if (lane >= o) at += below;
+        for (int j = 0; j < W; ++j) {
+            w[j] = tid * W + j < BITS ? touch()[tid * W + j] : 0u;
+            own += (uint32_t)__popc(w[j]);
+        }
+        uint32_t at = own;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t below = __shfl_up_sync(0xFFFFFFFFu, at, o);
+            if (lane >= o) at += below;
+        }
+        if (lane == 31) sums[tid >> 5] = at;
+        __syncthreads();
+        at -= own;
+        for (int k = 0; k < (tid >> 5); ++k)
+            at += sums[k];
+#pragma unroll
+        for (int j = 0; j < W; ++j)
+            for (; w[j]; w[j] &= w[j] - 1)
+                list[at++] = (uint16_t)((tid * W + j) * 32 + __ffs((int)w[j]) - 1);
+        __syncthreads();
     }
-    if (lane == 31) sums[tid >> 5] = at;
-    __syncthreads();
-    at -= (uint32_t)__popc(w);
-    for (int k = 0; k < (tid >> 5); ++k)
-        at += sums[k];
-    for (; w; w &= w - 1)
-        t.list[at++] = (uint16_t)(tid * 32 + __ffs((int)w) - 1);
-    __syncthreads();
-}
 
-// Place, count and bias entry of the i-th listed token.
-__device__ __forceinline__ int listed_token(const Listed &t, int i, uint32_t &count, uint32_t &bias)
-{
-    const int s = t.list[i];
-    if (t.wide) {
-        count = t.word[2 * s];
-        bias = t.word[2 * s + 1];
-    } else {
-        const uint32_t w = t.word[s];
-        count = w & (kSeen | ((1u << kCountBits) - 1u));
-        bias = w >> kCountBits & ((1u << kBiasBits) - 1u);
+    // Whether entry k of a short bias list is the last one that names its token (which bias_v has).
+    __device__ __forceinline__ bool counts_as_bias(int k, int n_bias) const
+    {
+        const int v = bias_v()[k];
+        if (v < 0)
+            return false;
+        for (int j = k + 1; j < n_bias; ++j)
+            if (bias_v()[j] == v)
+                return false;
+        return true;
     }
-    return s;
-}
+};
 
 // The logit of a listed token under the penalties and its bias, before the temperature.
-__device__ __forceinline__ float adjusted(float x, uint32_t count, uint32_t bias, const RowRules &q, const hilore_logit_rules &R)
+__device__ __forceinline__ float adjusted(float x, uint32_t count, float bias, const RowRules &q)
 {
     if (count) {
         x = x > 0.0f ? x * q.inv_rep : x * q.rep;
         const uint32_t c = count & ~kSeen;
         if (c) x = x - fmaf(q.freq, (float)c, q.pres);
     }
-    if (bias) x += __ldg(R.bias_values + q.bias_lo + bias - 1);
-    return x;
+    return x + bias;
+}
+
+// Value of entry `number` - 1 of the row's bias list; 0 for number 0.
+__device__ __forceinline__ float bias_value(const hilore_logit_rules &R, const RowRules &q, uint32_t number)
+{
+    return number == 0u ? 0.0f : __ldg(R.bias_values + (q.bias_lo + (int64_t)number - 1));
 }
 
 // d(adjusted logit) / d(logit) of a listed token.
@@ -391,9 +479,9 @@ struct MapApply { // z from x
         for (int i = 0; i < N; ++i)
             z[i] *= inv_temp;
     }
-    __device__ __forceinline__ float listed(float in, float, int, uint32_t c, uint32_t b, const RowRules &q, const hilore_logit_rules &R) const
+    __device__ __forceinline__ float listed(float in, float, int, uint32_t c, float b, const RowRules &q) const
     {
-        return adjusted(in, c, b, q, R) * inv_temp;
+        return adjusted(in, c, b, q) * inv_temp;
     }
     static __device__ __forceinline__ float off() { return -INFINITY; }
 };
@@ -407,7 +495,7 @@ struct MapApplyGrad { // dx from dz; x is read at listed tokens only (the side o
         for (int i = 0; i < N; ++i)
             z[i] *= inv_temp;
     }
-    __device__ __forceinline__ float listed(float in, float x, int, uint32_t c, uint32_t, const RowRules &q, const hilore_logit_rules &) const
+    __device__ __forceinline__ float listed(float in, float x, int, uint32_t c, float, const RowRules &q) const
     {
         return in * slope_of(x, c, q) * inv_temp;
     }
@@ -430,17 +518,15 @@ struct MapLogpGrad { // omega (1[v = a] - exp(z - lse)) dz/dx from x
         for (int i = 0; i < N; ++i)
             z[i] = one(z[i], i == at);
     }
-    __device__ __forceinline__ float listed(float in, float, int f, uint32_t c, uint32_t b, const RowRules &q, const hilore_logit_rules &R) const
+    __device__ __forceinline__ float listed(float in, float, int f, uint32_t c, float b, const RowRules &q) const
     {
-        return one(adjusted(in, c, b, q, R), f == target) * slope_of(in, c, q);
+        return one(adjusted(in, c, b, q), f == target) * slope_of(in, c, q);
     }
     static __device__ __forceinline__ float off() { return 0.0f; }
 };
 
 // 32 logits of every thread: the vectors of kMapThreads * 32 positions from `f0` on, in flight together.
 constexpr int kMapStage = kMapThreads * 32;
-static_assert(kMapStage == kWords, "a range with listed tokens is one stage of the stream");
-
 template <typename T> struct Stage {
     static constexpr int N = Lane<T>::N, U = 32 / N;
     static constexpr uint32_t kAll = (1u << N) - 1u;
@@ -479,99 +565,217 @@ template <typename T> struct Stage {
     }
 };
 
-template <typename T, bool SHIFTED, typename Map>
-__device__ __forceinline__ void map_range(const Row<T> &dst, const Source<T> &src, const T *in, const T *x, const Map &map, const RowRules &q,
-                                          const hilore_logit_rules &R, int V, int a, int b, unsigned char *smem, int *n)
-{
-    const int n_words = (V + 31) >> 5;
-    Stage<T> stage;
-    if (!q.listed()) {
-        for (; a < b; a += kMapStage) {
-            stage.template load<SHIFTED>(dst, src, q.mask, n_words, a, b);
-            stage.store(dst, map, a, b);
-        }
-        return;
-    }
-    Listed t = listed_at(smem, q, false, n);
-    int head[kScan];
-    history_load<kMapThreads>(R, q, q.hist_lo, head);
-    for (; a < b; a += t.wide ? kWords / 2 : kWords) {
-        const int e = min(b, a + (t.wide ? kWords / 2 : kWords));
-        stage.template load<SHIFTED>(dst, src, q.mask, n_words, a, e);
-        t.first = a;
-        fill_listed<kMapThreads>(R, q, V, dst.lead, e, t, head);
-        // their results take the place of their words; all are read before anything is stored, as `out` may be `in`
-        for (int i = threadIdx.x; i < *n; i += kMapThreads) {
-            uint32_t c, k;
-            const int s = listed_token(t, i, c, k), f = a + s, v = f - dst.lead;
-            const float r = is_denied(q.mask, v) ? Map::off() : map.listed(Lane<T>::one(in + v), Map::kGrad ? Lane<T>::one(x + v) : 0.0f, f, c, k, q, R);
-            t.word[t.wide ? 2 * s : s] = __float_as_uint(r);
-        }
-        __syncthreads();
-        stage.store(dst, map, a, e);
-        __syncthreads(); // the stream's results of listed tokens are there to be written over
-        for (int i = threadIdx.x; i < *n; i += kMapThreads) {
-            const int s = t.list[i];
-            Lane<T>::put(dst.origin + (a + s), __uint_as_float(t.word[t.wide ? 2 * s : s]));
-        }
-        if (e < b) __syncthreads();
-    }
-}
+// Shared memory of a CTA with listed tokens: bits, bias entries and their results, and a pool for the table, the list and the
+// results of the listed tokens.  Whatever the pool leaves beside the table bounds the list; a range with more listed tokens
+// is worked on in parts of half the size, which always fit from 2048 tokens down.
+constexpr int kMapRange = 3 * kMapStage; // positions of a CTA's range at most: a table of 16-bit counts
+constexpr int kMapBits = (kMapRange + kSlack + 127) / 128 * 4;
+constexpr int kMapPool = 15 * 1024; // words
+using MapListed = Listed<kMapBits, false>;
+constexpr size_t kMapShared = MapListed::kFixed + kMapPool * 4;
+static_assert(6 * (2048 + kSlack) <= 4 * (kMapPool - 2 * (2048 + kSlack) - 4), "parts of 2048 tokens fit in every form");
+static_assert(kMapRange / 2 + kSlack + 2048 <= kMapPool, "the largest table leaves room for a list");
+constexpr uint32_t kNoResult = 0xFFFFFFFFu; // no result of an operation: NaNs are 0x7FFFFFFF
 
+// Positions [a, b) of a row without listed tokens.
 template <typename T, typename Map>
-__device__ __forceinline__ void map_row(const Row<T> &dst, const T *in, const T *x, const Map &map, const RowRules &q, const hilore_logit_rules &R,
-                                        int V, int a, int b, unsigned char *smem, int *n)
+__device__ __forceinline__ void map_plain(const Row<T> &dst, const T *in, const Map &map, const uint32_t *mask, int V, int a, int b)
 {
     const Source<T> src(in, V, dst);
-    if (src.shift == 0) map_range<T, false>(dst, src, in, x, map, q, R, V, a, b, smem, n);
-    else map_range<T, true>(dst, src, in, x, map, q, R, V, a, b, smem, n);
+    const int n_words = (V + 31) >> 5;
+    Stage<T> stage;
+    for (; a < b; a += kMapStage) {
+        if (src.shift == 0) stage.template load<false>(dst, src, mask, n_words, a, b);
+        else stage.template load<true>(dst, src, mask, n_words, a, b);
+        stage.store(dst, map, a, b);
+    }
 }
 
-// One CTA per (row, range).
-template <typename T, bool GRAD>
-__global__ void __launch_bounds__(kMapThreads, sizeof(T) == 2 ? 4 : 3)
-    logits_apply_kernel(const T *x, int64_t ld, const T *in, int64_t ld_in, T *out, int64_t ld_out, int V, int n_ranges, int width,
-                        const __grid_constant__ hilore_logit_rules R)
+// What a CTA carries from row to row.
+struct MapState {
+    int part;    // positions that are worked on at once, as far as the form of the table allows
+    bool intact; // the table holds the last row with one, over the whole range
+};
+
+// Result of listed token v as bits, or kNoResult where it is not this range's or denied.
+template <typename T, typename Map>
+__device__ __forceinline__ uint32_t listed_result(const Map &map, const T *in, const T *x, const RowRules &q, int v, int lead, int a, int e, uint32_t count,
+                                                  float bias)
 {
-    extern __shared__ __align__(16) unsigned char smem[];
-    __shared__ int n_listed;
-    const int64_t row = blockIdx.x / n_ranges;
-    const int a = (int)(blockIdx.x - row * n_ranges) * width;
-    const Row<T> dst(out + row * ld_out, V);
-    if (a >= dst.end)
-        return;
-    const int b = min(dst.end, a + width);
-    const RowRules q = row_rules(R, row);
-    if (GRAD) map_row(dst, in + row * ld_in, x + row * ld, MapApplyGrad{q.inv_temp}, q, R, V, a, b, smem, &n_listed);
-    else map_row(dst, in + row * ld_in, x + row * ld, MapApply{q.inv_temp}, q, R, V, a, b, smem, &n_listed);
+    const int f = v + lead;
+    if (f < a || f >= e || is_denied(q.mask, v))
+        return kNoResult;
+    const float other = Map::kGrad ? Lane<T>::one(x + v) : 0.0f;
+    return __float_as_uint(map.listed(Lane<T>::one(in + v), other, f, count, bias, q));
 }
 
-// One CTA per (row, range); rows whose coefficient is zero, that have no token, whose token the grammar denies or that had
-// nothing to choose from get zeros without being read.
-template <typename T>
-__global__ void __launch_bounds__(kMapThreads, sizeof(T) == 2 ? 4 : 3)
-    token_logp_backward_kernel(const T *x, int64_t ld, int V, int n_ranges, int width, const int32_t *targets, const float *lse,
-                               const float *omega, T *grad, int64_t ld_grad, const __grid_constant__ hilore_logit_rules R)
+// Positions [a, b) of a row with listed tokens.  `in_place`: the output is the input.
+template <typename T, typename Map>
+__device__ __forceinline__ void map_listed(const Row<T> &dst, const T *in, const T *x, const Map &map, const RowPlan &plan, const hilore_logit_rules &R,
+                                           int V, int a, int b, int range, bool in_place, const MapListed &t, uint32_t *bias_result, MapState &m)
 {
-    constexpr int N = Lane<T>::N;
-    extern __shared__ __align__(16) unsigned char smem[];
-    __shared__ int n_listed;
-    const int64_t row = blockIdx.x / n_ranges;
-    const int a = (int)(blockIdx.x - row * n_ranges) * width;
-    const Row<T> dst(grad + row * ld_grad, V);
-    if (a >= dst.end)
-        return;
-    const int b = min(dst.end, a + width);
-    const int target = targets[row];
-    const float om = omega[row], l = lse[row];
-    const RowRules q = row_rules(R, row);
-    if ((uint32_t)target >= (uint32_t)V || om == 0.0f || l <= kNothing || is_denied(q.mask, target)) {
-        const float zero[N] = {};
-        for (int f = a + (int)threadIdx.x * N; f < b; f += kMapThreads * N)
-            dst.store(f, zero);
+    const RowRules &q = plan.q;
+    const int tid = threadIdx.x, n_bias = plan.n_bias, form = plan.form, lead = dst.lead;
+    const bool counts = q.history() || form == kBiased;
+    int step = min(m.part, form == kCount16 ? kMapRange : form == kCount32 ? kMapRange / 3 : kMapRange / 6);
+    while (a < b) {
+        const int e = min(b, a + step), v0 = a - kSlack, words = (table_words(form, step + kSlack) + 3) & ~3;
+        uint16_t *list = reinterpret_cast<uint16_t *>(t.word() + words);
+        const int cap = (kMapPool - words) * 4 / 6 & ~1;
+        uint32_t *result = t.word() + words + cap / 2;
+        t.template fill<kMapThreads>(R, plan, V, v0, step + kSlack, form, plan.follows && m.intact && step == range, list, cap);
+        const int n = counts ? *t.n : 0;
+        if (n > cap) {
+            m.part = step = (step / 2 + 127) & ~127;
+            m.intact = false;
+            continue;
+        }
+        // Everything is read before anything is stored, as the output may be the input.
+        for (int i = tid; i < n; i += kMapThreads) {
+            const int p = list[i];
+            uint32_t r = kNoResult;
+            if (n_bias == 0 || !t.is_biased(p)) {
+                const float bias = form == kBiased ? bias_value(R, q, t.word()[2 * p + 1]) : 0.0f;
+                r = listed_result(map, in, x, q, v0 + p, lead, a, e, t.count_at(p, form), bias);
+            }
+            result[i] = r;
+        }
+        for (int k = tid; k < n_bias; k += kMapThreads) {
+            uint32_t r = kNoResult;
+            if (t.counts_as_bias(k, n_bias)) {
+                const int v = t.bias_v()[k];
+                r = listed_result(map, in, x, q, v, lead, a, e, counts ? t.count_at(v - v0, form) : 0u, bias_value(R, q, (uint32_t)k + 1u));
+            }
+            bias_result[k] = r;
+        }
+        if (in_place) __syncthreads();
+        map_plain(dst, in, map, q.mask, V, a, e);
+        __syncthreads(); // the stream's results of listed tokens are there to be written over
+        T *row = dst.origin + lead;
+        for (int i = tid; i < n; i += kMapThreads)
+            if (result[i] != kNoResult) Lane<T>::put(row + (v0 + (int)list[i]), __uint_as_float(result[i]));
+        for (int k = tid; k < n_bias; k += kMapThreads)
+            if (bias_result[k] != kNoResult) Lane<T>::put(row + t.bias_v()[k], __uint_as_float(bias_result[k]));
+        if (counts) m.intact = step == range && form != kBiased;
+        a += step;
+    }
+}
+
+// What a CTA keeps of the rows of its block.
+struct RowLoss { // of the gradient of a log-probability
+    int target;
+    float omega, lse;
+    bool live;
+};
+
+// One CTA per (block of rows, range).  LISTS: rows may have listed tokens; otherwise a block is one row.
+template <typename T, bool GRAD, bool LISTS>
+__global__ void __launch_bounds__(kMapThreads, !LISTS && sizeof(T) == 2 ? 4 : 3)
+    logits_apply_kernel(const T *x, int64_t ld, const T *in, int64_t ld_in, T *out, int64_t ld_out, int64_t n_rows, int V, int block_rows, int n_ranges,
+                        int width, const __grid_constant__ hilore_logit_rules R)
+{
+    const int64_t row0 = (int64_t)(blockIdx.x / n_ranges) * block_rows;
+    const int a = (int)(blockIdx.x % n_ranges) * width;
+    if (!LISTS) {
+        const RowRules q = row_rules(R, row0);
+        const Row<T> dst(out + row0 * ld_out, V);
+        if (a >= dst.end)
+            return;
+        if (GRAD) map_plain(dst, in + row0 * ld_in, MapApplyGrad{q.inv_temp}, q.mask, V, a, min(dst.end, a + width));
+        else map_plain(dst, in + row0 * ld_in, MapApply{q.inv_temp}, q.mask, V, a, min(dst.end, a + width));
         return;
     }
-    map_row(dst, x + row * ld, x + row * ld, MapLogpGrad{q.inv_temp, l, om * q.inv_temp, target + dst.lead}, q, R, V, a, b, smem, &n_listed);
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ RowPlan plan[kBlockRows];
+    __shared__ uint32_t bias_result[kBiasCap];
+    __shared__ int count;
+    const int rows = (int)min((int64_t)block_rows, n_rows - row0);
+    if ((int)threadIdx.x < rows) {
+        plan[threadIdx.x].q = row_rules(R, row0 + threadIdx.x);
+        plan[threadIdx.x].used = true;
+    }
+    plan_rows(plan, rows, R);
+    const MapListed t{smem, &count};
+    MapState m{width, false};
+    for (int i = 0; i < rows; ++i) {
+        const RowRules &q = plan[i].q;
+        const Row<T> dst(out + (row0 + i) * ld_out, V);
+        const T *from = in + (row0 + i) * ld_in, *at = x + (row0 + i) * ld;
+        const int b = min(dst.end, a + width);
+        if (a >= b)
+            continue;
+        if (!q.listed()) {
+            if (GRAD) map_plain(dst, from, MapApplyGrad{q.inv_temp}, q.mask, V, a, b);
+            else map_plain(dst, from, MapApply{q.inv_temp}, q.mask, V, a, b);
+        } else {
+            if (GRAD) map_listed(dst, from, at, MapApplyGrad{q.inv_temp}, plan[i], R, V, a, b, width, in == out, t, bias_result, m);
+            else map_listed(dst, from, at, MapApply{q.inv_temp}, plan[i], R, V, a, b, width, in == out, t, bias_result, m);
+        }
+    }
+}
+
+// The same for the gradient of a log-probability.  Rows whose coefficient is zero, that have no token, whose token the grammar
+// denies or that had nothing to choose from get zeros without being read.
+__device__ __forceinline__ RowLoss row_loss(const RowRules &q, const int32_t *targets, const float *lse, const float *omega, int64_t row, int V)
+{
+    RowLoss p{targets[row], omega[row], lse[row], false};
+    p.live = (uint32_t)p.target < (uint32_t)V && p.omega != 0.0f && !(p.lse <= kNothing) && !is_denied(q.mask, p.target);
+    return p;
+}
+
+template <typename T> __device__ __forceinline__ void zero_range(const Row<T> &dst, int a, int b)
+{
+    const float zero[Lane<T>::N] = {};
+    for (int f = a + (int)threadIdx.x * Lane<T>::N; f < b; f += kMapThreads * Lane<T>::N)
+        dst.store(f, zero);
+}
+
+template <typename T, bool LISTS>
+__global__ void __launch_bounds__(kMapThreads, !LISTS && sizeof(T) == 2 ? 4 : 3)
+    token_logp_backward_kernel(const T *x, int64_t ld, int64_t n_rows, int V, int block_rows, int n_ranges, int width, const int32_t *targets,
+                               const float *lse, const float *omega, T *grad, int64_t ld_grad, const __grid_constant__ hilore_logit_rules R)
+{
+    const int64_t row0 = (int64_t)(blockIdx.x / n_ranges) * block_rows;
+    const int a = (int)(blockIdx.x % n_ranges) * width;
+    if (!LISTS) {
+        const RowRules q = row_rules(R, row0);
+        const RowLoss p = row_loss(q, targets, lse, omega, row0, V);
+        const Row<T> dst(grad + row0 * ld_grad, V);
+        if (a >= dst.end)
+            return;
+        const int b = min(dst.end, a + width);
+        if (p.live) map_plain(dst, x + row0 * ld, MapLogpGrad{q.inv_temp, p.lse, p.omega * q.inv_temp, p.target + dst.lead}, q.mask, V, a, b);
+        else zero_range(dst, a, b);
+        return;
+    }
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ RowPlan plan[kBlockRows];
+    __shared__ RowLoss losses[kBlockRows];
+    __shared__ uint32_t bias_result[kBiasCap];
+    __shared__ int count;
+    const int rows = (int)min((int64_t)block_rows, n_rows - row0);
+    if ((int)threadIdx.x < rows) {
+        const RowRules q = row_rules(R, row0 + threadIdx.x);
+        plan[threadIdx.x].q = q;
+        losses[threadIdx.x] = row_loss(q, targets, lse, omega, row0 + threadIdx.x, V);
+        plan[threadIdx.x].used = losses[threadIdx.x].live;
+    }
+    plan_rows(plan, rows, R);
+    const MapListed t{smem, &count};
+    MapState m{width, false};
+    for (int i = 0; i < rows; ++i) {
+        const RowRules &q = plan[i].q;
+        const RowLoss p = losses[i];
+        const Row<T> dst(grad + (row0 + i) * ld_grad, V);
+        const T *from = x + (row0 + i) * ld;
+        const int b = min(dst.end, a + width);
+        if (a >= b)
+            continue;
+        const MapLogpGrad map{q.inv_temp, p.lse, p.omega * q.inv_temp, p.target + dst.lead};
+        if (!p.live) zero_range(dst, a, b);
+        else if (!q.listed()) map_plain(dst, from, map, q.mask, V, a, b);
+        else map_listed(dst, from, from, map, plan[i], R, V, a, b, width, x == grad, t, bias_result, m);
+    }
 }
 
 // ---------------------------------------------------------------------------------------------- log-probability of a token
@@ -630,24 +834,55 @@ template <bool ENTROPY> __device__ __forceinline__ void soft_one(Soft &q, float 
     soft_add<2, ENTROPY>(q, one, c);
 }
 
-constexpr int kLogpThreads = 256, kMaxRowCtas = 8;
+constexpr int kLogpThreads = 256, kLogpWarps = kLogpThreads / 32, kMaxRowCtas = 8;
 
-// A row belongs to `row_ctas` CTAs (a thread-block cluster if more than one); each takes a share of its vectors.  RULES: more
-// than a temperature.
-template <typename T, bool RULES, bool ENTROPY>
-__global__ void __launch_bounds__(kLogpThreads, RULES && sizeof(T) == 4 ? 3 : 4)
+template <bool ENTROPY> __device__ __forceinline__ Soft warp_soft(Soft acc, float c)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        Soft other;
+        other.m = __shfl_xor_sync(0xFFFFFFFFu, acc.m, o);
+        other.s = __shfl_xor_sync(0xFFFFFFFFu, acc.s, o);
+        other.t = ENTROPY ? __shfl_xor_sync(0xFFFFFFFFu, acc.t, o) : 0.0f;
+        acc = soft_join<ENTROPY>(acc, other, c);
+    }
+    return acc;
+}
+
+// Results of a row from its statistics; z: the target's logit under penalties and bias, -inf where denied.
+template <bool ENTROPY>
+__device__ __forceinline__ void finish_row(const Soft &acc, float z, float inv_temp, int64_t row, float *logp, float *lse, float *entropy)
+{
+    const float ln_s = logf(acc.s);
+    float l = fmaf(acc.m, inv_temp, ln_s), p = fmaf(z - acc.m, inv_temp, -ln_s), h = 0.0f;
+    const bool nothing = acc.m == kLowest && acc.s == 0.0f;
+    if (acc.m == INFINITY) { // the sum has no value (inf - inf); its logarithm has
+        l = INFINITY;
+        p = z - acc.m;
+    } else if (nothing) {
+        l = -INFINITY;
+        p = -INFINITY;
+    }
+    if (ENTROPY) { // H = ln s - sum p u ln 2
+        h = nothing ? 0.0f : fmaf(-acc.t / acc.s, 0.6931471805599453f, ln_s);
+        if (acc.m != acc.m || acc.m == INFINITY) h = acc.m - acc.m;
+        entropy[row] = h;
+    }
+    logp[row] = p;
+    if (lse) lse[row] = l;
+}
+
+// Without rules beyond a temperature.  A row belongs to `row_ctas` CTAs (a thread-block cluster if more than one); each takes a
+// share of its vectors.
+template <typename T, bool ENTROPY>
+__global__ void __launch_bounds__(kLogpThreads, 4)
     token_logp_kernel(const T *x, int64_t ld, int V, int row_ctas, const int32_t *targets, float *logp, float *lse, float *entropy,
-                      const __grid_constant__ hilore_logit_rules R)
+                      const float *temperature)
 {
     constexpr int N = Lane<T>::N, U = 32 / N;
-    constexpr uint32_t kAll = (1u << N) - 1u;
-    extern __shared__ __align__(16) unsigned char smem[];
-    __shared__ Soft part[kLogpThreads / 32];
-    __shared__ uint32_t sums[kLogpThreads / 32];
+    __shared__ Soft part[kLogpWarps];
     __shared__ Soft shares[kMaxRowCtas];
-    __shared__ float target_z; // the target's logit under penalties and bias; in the cluster's first CTA
-    __shared__ int n_listed;
-    const int tid = threadIdx.x, lane = tid & 31;
+    const int tid = threadIdx.x;
     const int64_t row = blockIdx.x / row_ctas;
     const int rank = (int)(blockIdx.x - row * row_ctas);
     cg::cluster_group cl = cg::this_cluster();
@@ -660,136 +895,206 @@ __global__ void __launch_bounds__(kLogpThreads, RULES && sizeof(T) == 4 ? 3 : 4)
         }
         return;
     }
-    const T *xrow = x + row * ld;
-    const RowRules q = row_rules(R, row);
-    if (rank == 0 && tid == 0) target_z = is_denied(q.mask, target) ? -INFINITY : Lane<T>::one(xrow + target);
-    if (row_ctas > 1)
-        cl.sync(); // every CTA of the row runs, and target_z is set, before anything is sent to the first one
-    float *first_z = row_ctas > 1 ? cl.map_shared_rank(&target_z, 0) : &target_z;
-
-    const Row<T> src(xrow, V);
-    const int n_vec = (src.end + N - 1) / N, n_words = (V + 31) >> 5;
-    int a = (int)((int64_t)n_vec * rank / row_ctas) * N;
-    const int b = (int)((int64_t)n_vec * (rank + 1) / row_ctas) * N;
-    const float c = kLog2eF * q.inv_temp;
+    if (row_ctas > 1) cl.barrier_arrive(); // once all have arrived, every CTA of the row runs
+    const float inv_temp = inverse_temperature(temperature, row), c = kLog2eF * inv_temp;
+    const Row<T> src(x + row * ld, V);
+    const int n_vec = (src.end + N - 1) / N;
+    const int a = (int)((int64_t)n_vec * rank / row_ctas) * N, b = (int)((int64_t)n_vec * (rank + 1) / row_ctas) * N;
+    float z = 0.0f;
+    if (rank == 0 && tid == 0) z = Lane<T>::one(x + row * ld + target);
     Soft acc{kLowest, 0.0f, 0.0f};
-    if (!RULES) {
-        for (int f0 = a + tid * N; f0 < b; f0 += kLogpThreads * 32) {
-            uint32_t w[U][8];
+    for (int f0 = a + tid * N; f0 < b; f0 += kLogpThreads * 32) {
+        uint32_t w[U][8];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int f = f0 + u * kLogpThreads * N;
-                if (f < b) src.load(f, w[u]);
+        for (int u = 0; u < U; ++u) {
+            const int f = f0 + u * kLogpThreads * N;
+            if (f < b) src.load(f, w[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int f = f0 + u * kLogpThreads * N;
+            if (f < b) {
+                float v[N];
+                Lane<T>::unpack(w[u], v);
+                if (!src.whole(f)) {
+                    const uint32_t ok = src.valid(f);
+#pragma unroll
+                    for (int i = 0; i < N; ++i)
+                        if (!(ok >> i & 1u)) v[i] = -INFINITY;
+                }
+                soft_add<N, ENTROPY>(acc, v, c);
             }
+        }
+    }
+    acc = warp_soft<ENTROPY>(acc, c);
+    if ((tid & 31) == 0) part[tid >> 5] = acc;
+    __syncthreads();
+    if (tid == 0)
+        for (int w = 1; w < kLogpWarps; ++w)
+            acc = soft_join<ENTROPY>(acc, part[w], c);
+    if (row_ctas > 1) {
+        cl.barrier_wait();
+        if (tid == 0) *cl.map_shared_rank(&shares[rank], 0) = acc;
+        cl.sync(); // the shares have arrived in the first CTA
+    }
+    if (rank != 0 || tid != 0)
+        return;
+    for (int r = 1; r < row_ctas; ++r)
+        acc = soft_join<ENTROPY>(acc, shares[r], c);
+    finish_row<ENTROPY>(acc, z, inv_temp, row, logp, lse, entropy);
+}
+
+// Under rules.  A cluster of `row_ctas` CTAs (or one CTA) walks a block of consecutive rows; each CTA owns `width` positions of
+// every row, so that its table of counts serves one row after the other.  The statistics of every warp go to the first
+// CTA, which joins them when the block is done.
+constexpr int kLogpTokens = 20480; // tokens of a table of 16-bit counts at most: 8 CTAs take vocabularies up to 163712
+constexpr int kLogpBits = kLogpTokens / 32 + 8, kLogpCap = 2048;
+using LogpListed = Listed<kLogpBits, true>;
+constexpr size_t kLogpFixed = LogpListed::kFixed; // bytes before the table; the list is in static shared memory
+
+template <typename T, bool ENTROPY>
+__global__ void __launch_bounds__(kLogpThreads, sizeof(T) == 4 ? 3 : 4)
+    token_logp_rules_kernel(const T *x, int64_t ld, int64_t n_rows, int V, int block_rows, int row_ctas, int width, int words, const int32_t *targets,
+                            float *logp, float *lse, float *entropy, const __grid_constant__ hilore_logit_rules R)
+{
+    constexpr int N = Lane<T>::N, U = 32 / N;
+    constexpr uint32_t kAll = (1u << N) - 1u;
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ RowPlan plan[kBlockRows];
+    __shared__ int targets_of[kBlockRows];
+    __shared__ int count;
+    __shared__ uint16_t list[kLogpCap];
+    __shared__ uint32_t sums[kLogpWarps];
+    __shared__ Soft part[kBlockRows][kMaxRowCtas * kLogpWarps]; // in the first CTA: of all warps of the cluster
+    __shared__ float target_z[kBlockRows];                      // in the first CTA: the targets' logits under penalties and bias
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int64_t row0 = (int64_t)(blockIdx.x / row_ctas) * block_rows;
+    const int rank = (int)(blockIdx.x % row_ctas);
+    const int rows = (int)min((int64_t)block_rows, n_rows - row0);
+    cg::cluster_group cl = cg::this_cluster();
+    if (row_ctas > 1) cl.barrier_arrive(); // once all have arrived, every CTA of the cluster runs
+    if (tid < rows) {
+        plan[tid].q = row_rules(R, row0 + tid);
+        targets_of[tid] = targets[row0 + tid];
+        plan[tid].used = (uint32_t)targets_of[tid] < (uint32_t)V;
+    }
+    plan_rows(plan, rows, R);
+    if (row_ctas > 1) cl.barrier_wait();
+    const LogpListed t{smem, &count};
+    bool intact = false; // the table holds the last row with one, over the whole range
+    Soft(*to_part)[kMaxRowCtas * kLogpWarps] = row_ctas > 1 ? cl.map_shared_rank(&part[0], 0) : &part[0];
+    float *to_z = row_ctas > 1 ? cl.map_shared_rank(&target_z[0], 0) : &target_z[0];
+    const int n_words = (V + 31) >> 5;
+    for (int r = 0; r < rows; ++r) {
+        const RowRules &q = plan[r].q;
+        const int target = targets_of[r];
+        if ((uint32_t)target >= (uint32_t)V)
+            continue;
+        const T *xrow = x + (row0 + r) * ld;
+        const Row<T> src(xrow, V);
+        const float c = kLog2eF * q.inv_temp;
+        const uint32_t *mask = q.mask;
+        int a = rank * width;
+        const int b = min(src.end, a + width);
+        const int form = plan[r].form, n_bias = plan[r].n_bias;
+        const bool lists = q.listed(), counts = q.history() || form == kBiased;
+        const int room = (form == kCount16 ? 2 * words : form == kCount32 ? words : words / 2) - kSlack;
+        const int step = lists && width > room ? room & ~127 : width;
+        Soft acc{kLowest, 0.0f, 0.0f};
+        for (; a < b; a += step) {
+            const int e = min(b, a + step), v0 = a - kSlack, ft = target + src.lead;
+            if (lists) {
+                __syncthreads(); // the last range or row is done with the table
+                const bool follow = plan[r].follows && intact && step == width;
+                const int before = follow ? count : 0;
+                if (follow) __syncthreads();
+                t.template fill<kLogpThreads>(R, plan[r], V, v0, step + kSlack, form, follow, list, kLogpCap);
+                const int n = counts ? count : 0;
+                const bool whole = n <= kLogpCap; // the list is complete; otherwise every place of the table is asked
+                if (counts && whole && (!follow || n > before + 1)) t.template order<kLogpThreads>(sums, list);
+                if (counts) intact = step == width && form != kBiased;
+                for (int i = tid; i < (whole ? n : counts ? step + kSlack : 0); i += kLogpThreads) {
+                    const int p = whole ? (int)list[i] : i, v = v0 + p, f = v + src.lead;
+                    const uint32_t k = t.count_at(p, form), j = form == kBiased ? t.word()[2 * p + 1] : 0u;
+                    if ((k | j) == 0 || f < a || f >= e || (n_bias > 0 && t.is_biased(p)))
+                        continue;
+                    const float z = is_denied(mask, v) ? -INFINITY : adjusted(Lane<T>::one(xrow + v), k, bias_value(R, q, j), q);
+                    if (v == target) to_z[r] = z;
+                    soft_one<ENTROPY>(acc, z, c);
+                }
+                for (int k = tid; k < n_bias; k += kLogpThreads)
+                    if (t.counts_as_bias(k, n_bias)) {
+                        const int v = t.bias_v()[k], f = v + src.lead;
+                        if (f < a || f >= e)
+                            continue;
+                        const float z = is_denied(mask, v) ? -INFINITY
+                                                           : adjusted(Lane<T>::one(xrow + v), counts ? t.count_at(v - v0, form) : 0u, bias_value(R, q, (uint32_t)k + 1u), q);
+                        if (v == target) to_z[r] = z;
+                        soft_one<ENTROPY>(acc, z, c);
+                    }
+            }
+            const bool touched = counts, biased = n_bias > 0;
+            if (tid == 0 && ft >= a && ft < e) {
+                const int p = target - v0;
+                if (!(touched && (t.touch()[p >> 5] >> (p & 31) & 1u)) && !(biased && t.is_biased(p)))
+                    to_z[r] = is_denied(mask, target) ? -INFINITY : Lane<T>::one(xrow + target);
+            }
+            for (int f0 = a + tid * N; f0 < e; f0 += kLogpThreads * 32) {
+                uint32_t w[U][8], off[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int f = f0 + u * kLogpThreads * N;
-                if (f < b) {
+                for (int u = 0; u < U; ++u) {
+                    const int f = f0 + u * kLogpThreads * N;
+                    off[u] = f < e ? ~src.valid(f) & kAll : kAll;
+                    if (off[u] == kAll)
+                        continue;
+                    if (mask) off[u] |= denied<N>(mask, n_words, f - src.lead);
+                    const int p = f - src.lead - v0;
+                    if (touched) off[u] |= __funnelshift_r(t.touch()[p >> 5], t.touch()[(p >> 5) + 1], p & 31) & kAll;
+                    if (biased) off[u] |= __funnelshift_r(t.biased()[p >> 5], t.biased()[(p >> 5) + 1], p & 31) & kAll;
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (off[u] != kAll) src.load(f0 + u * kLogpThreads * N, w[u]); // a vector without an allowed token is not read
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    if (off[u] == kAll)
+                        continue;
                     float z[N];
                     Lane<T>::unpack(w[u], z);
-                    if (!src.whole(f)) {
-                        const uint32_t ok = src.valid(f);
+                    if (off[u]) {
 #pragma unroll
                         for (int i = 0; i < N; ++i)
-                            if (!(ok >> i & 1u)) z[i] = -INFINITY;
+                            if (off[u] >> i & 1u) z[i] = -INFINITY;
                     }
                     soft_add<N, ENTROPY>(acc, z, c);
                 }
             }
         }
-    } else {
-        const bool lists = q.listed();
-        Listed t = listed_at(smem, q, true, &n_listed);
-        int head[kScan];
-        if (lists) history_load<kLogpThreads>(R, q, q.hist_lo, head);
-        const int width = lists && t.wide ? kWords / 2 : kWords;
-        for (; a < b; a += width) {
-            const int e = min(b, a + width);
-            uint32_t w[U][8], off[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int f = a + (u * kLogpThreads + tid) * N;
-                off[u] = f < e && q.mask ? denied<N>(q.mask, n_words, f - src.lead) : 0u;
-                off[u] |= f < e ? ~src.valid(f) & kAll : kAll;
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int f = a + (u * kLogpThreads + tid) * N;
-                if (off[u] != kAll) src.load(f, w[u]); // a vector without an allowed token is not read
-            }
-            if (lists) {
-                t.first = a;
-                __syncthreads(); // the previous range is done with the table
-                fill_listed<kLogpThreads>(R, q, V, src.lead, e, t, head);
-                order_listed<kLogpThreads>(t, sums);
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const int s = (u * kLogpThreads + tid) * N;
-                    off[u] |= t.touch[s >> 5] >> (s & 31) & kAll;
-                }
-                for (int i = tid; i < n_listed; i += kLogpThreads) {
-                    uint32_t n, k;
-                    const int v = a + listed_token(t, i, n, k) - src.lead;
-                    if (is_denied(q.mask, v))
-                        continue;
-                    const float z = adjusted(Lane<T>::one(xrow + v), n, k, q, R);
-                    if (v == target) *first_z = z;
-                    soft_one<ENTROPY>(acc, z, c);
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (off[u] == kAll)
-                    continue;
-                float z[N];
-                Lane<T>::unpack(w[u], z);
-                if (off[u]) {
-#pragma unroll
-                    for (int i = 0; i < N; ++i)
-                        if (off[u] >> i & 1u) z[i] = -INFINITY;
-                }
-                soft_add<N, ENTROPY>(acc, z, c);
-            }
-        }
+        acc = warp_soft<ENTROPY>(acc, c);
+        if (lane == 0) to_part[r][rank * kLogpWarps + warp] = acc;
     }
-
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        Soft other;
-        other.m = __shfl_xor_sync(0xFFFFFFFFu, acc.m, o);
-        other.s = __shfl_xor_sync(0xFFFFFFFFu, acc.s, o);
-        other.t = ENTROPY ? __shfl_xor_sync(0xFFFFFFFFu, acc.t, o) : 0.0f;
-        acc = soft_join<ENTROPY>(acc, other, c);
-    }
-    if (lane == 0) part[tid >> 5] = acc;
-    __syncthreads();
-    if (tid == 0) {
-        for (int w = 1; w < kLogpThreads / 32; ++w)
-            acc = soft_join<ENTROPY>(acc, part[w], c);
-        if (row_ctas > 1) *cl.map_shared_rank(&shares[rank], 0) = acc;
-    }
-    if (row_ctas > 1)
-        cl.sync(); // the shares have arrived in the first CTA
-    if (rank != 0 || tid != 0)
+    if (row_ctas > 1) cl.sync(); // everything has arrived in the first CTA
+    else __syncthreads();
+    if (rank != 0)
         return;
-    for (int r = 1; r < row_ctas; ++r)
-        acc = soft_join<ENTROPY>(acc, shares[r], c);
-    const float ln_s = logf(acc.s);
-    float l = fmaf(acc.m, q.inv_temp, ln_s), p = fmaf(target_z - acc.m, q.inv_temp, -ln_s), h = 0.0f;
-    if (acc.m == INFINITY) { // the sum has no value (inf - inf); its logarithm has
-        l = INFINITY;
-        p = target_z - acc.m;
-    } else if (acc.m == kLowest && acc.s == 0.0f) { // nothing to choose from
-        l = -INFINITY;
-        p = -INFINITY;
+    for (int r = warp; r < rows; r += kLogpWarps) {
+        const int target = targets_of[r];
+        const int64_t row = row0 + r;
+        if ((uint32_t)target >= (uint32_t)V) { // a slot without a token
+            if (lane == 0) {
+                logp[row] = 0.0f;
+                if (lse) lse[row] = 0.0f;
+                if (ENTROPY) entropy[row] = 0.0f;
+            }
+            continue;
+        }
+        const float inv_temp = plan[r].q.inv_temp, c = kLog2eF * inv_temp;
+        Soft acc{kLowest, 0.0f, 0.0f};
+        for (int k = lane; k < row_ctas * kLogpWarps; k += 32)
+            acc = soft_join<ENTROPY>(acc, part[r][k], c);
+        acc = warp_soft<ENTROPY>(acc, c);
+        if (lane == 0) finish_row<ENTROPY>(acc, target_z[r], inv_temp, row, logp, lse, entropy);
     }
-    if (ENTROPY) { // H = ln s - sum p u ln 2
-        h = acc.m == kLowest && acc.s == 0.0f ? 0.0f : fmaf(-acc.t / acc.s, 0.6931471805599453f, ln_s);
-        if (acc.m != acc.m || acc.m == INFINITY) h = acc.m - acc.m;
-        entropy[row] = h;
-    }
-    logp[row] = p;
-    if (lse) lse[row] = l;
 }
 
 // ------------------------------------------------------------------------------------------------------------ host side
@@ -836,35 +1141,55 @@ static hilore_logit_rules used_rules(const hilore_logit_rules *r)
 
 static bool more_than_temperature(const hilore_logit_rules &q) { return q.tokens || q.bias_tokens || q.allow; }
 
-// Dynamic shared memory beyond 48 KB (with the kernels' static few hundred bytes) needs an opt-in.
+// More than 48 KB of shared memory, the kernels' own 12 KB at most included, needs an opt-in.
 template <typename K> static bool allow_smem(K kernel, size_t bytes)
 {
-    return bytes <= 47 * 1024 || cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess;
+    return bytes <= 32 * 1024 || cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess;
 }
 
-// Positions of a CTA's range in the element-wise calls: one table of listed tokens, twice that where there are none, and less
-// while that leaves SMs without four CTAs.
-static int64_t range_width(int64_t n_rows, int64_t V, const hilore_logit_rules &R)
+static bool has_lists(const hilore_logit_rules &q) { return q.tokens || q.bias_tokens; }
+
+// Work split of the element-wise calls.  Where rows may have listed tokens: ranges of one table, and blocks of up to eight rows
+// that share it as far as four rounds of CTAs remain.  Otherwise: one row, ranges of two stages.  Either way shorter ranges while SMs are
+// left without four CTAs.
+struct Split {
+    int64_t block_rows, width, n_ranges, grid;
+};
+static Split map_split(int64_t n_rows, int64_t V, bool lists)
 {
-    int64_t width = R.tokens || R.bias_tokens ? kWords : 2 * kWords;
-    while (width > 2048 && n_rows * ((V + width - 1) / width) < 4 * (int64_t)sm_count())
-        width /= 2;
-    return width;
+    const int64_t sms = sm_count();
+    Split p{1, lists ? kMapRange : 2 * kMapStage, 0, 0};
+    const auto ranges = [&] { return (V + 15 + p.width - 1) / p.width; };
+    while (p.width > 2048 && n_rows * ranges() < 4 * sms)
+        p.width = (p.width / 2 + 127) / 128 * 128;
+    p.n_ranges = ranges();
+    if (lists) p.block_rows = n_rows * p.n_ranges / (12 * sms);
+    p.block_rows = p.block_rows < 1 ? 1 : p.block_rows > kBlockRows ? kBlockRows : p.block_rows;
+    p.grid = (n_rows + p.block_rows - 1) / p.block_rows * p.n_ranges;
+    return p;
+}
+
+template <typename T, bool GRAD, bool LISTS>
+static int launch_apply_as(const T *x, int64_t ld, const T *in, int64_t ld_in, T *out, int64_t ld_out, int64_t n_rows, int64_t V,
+                           const hilore_logit_rules &R, cudaStream_t st)
+{
+    const Split p = map_split(n_rows, V, LISTS);
+    if (p.grid > 0x7FFFFFFF)
+        return HILORE_SHAPE;
+    auto kernel = logits_apply_kernel<T, GRAD, LISTS>;
+    const size_t smem = LISTS ? kMapShared : 0;
+    if (!allow_smem(kernel, smem))
+        return HILORE_CUDA;
+    kernel<<<(unsigned)p.grid, kMapThreads, smem, st>>>(x, ld, in, ld_in, out, ld_out, n_rows, (int)V, (int)p.block_rows, (int)p.n_ranges, (int)p.width, R);
+    return cudaGetLastError() == cudaSuccess ? HILORE_OK : HILORE_CUDA;
 }
 
 template <typename T, bool GRAD>
 static int launch_apply(const T *x, int64_t ld, const T *in, int64_t ld_in, T *out, int64_t ld_out, int64_t n_rows, int64_t V,
                         const hilore_logit_rules &R, cudaStream_t st)
 {
-    const int64_t width = range_width(n_rows, V, R), n = (V + Lane<T>::N - 1 + width - 1) / width;
-    if (n * n_rows > 0x7FFFFFFF)
-        return HILORE_SHAPE;
-    auto kernel = logits_apply_kernel<T, GRAD>;
-    const size_t smem = R.tokens || R.bias_tokens ? kListedBytes : 0;
-    if (!allow_smem(kernel, smem))
-        return HILORE_CUDA;
-    kernel<<<(unsigned)(n * n_rows), kMapThreads, smem, st>>>(x, ld, in, ld_in, out, ld_out, (int)V, (int)n, (int)width, R);
-    return cudaGetLastError() == cudaSuccess ? HILORE_OK : HILORE_CUDA;
+    return has_lists(R) ? launch_apply_as<T, GRAD, true>(x, ld, in, ld_in, out, ld_out, n_rows, V, R, st)
+                        : launch_apply_as<T, GRAD, false>(x, ld, in, ld_in, out, ld_out, n_rows, V, R, st);
 }
 
 static bool clusters_on()
@@ -873,35 +1198,75 @@ static bool clusters_on()
     return off == nullptr || off[0] == '\0' || (off[0] == '0' && off[1] == '\0');
 }
 
-template <typename T, bool RULES, bool ENTROPY>
-static int launch_logp(const T *x, int64_t ld, int64_t n_rows, int64_t V, const int32_t *targets, float *logp, float *lse, float *entropy,
-                       const hilore_logit_rules &R, cudaStream_t st)
+// CTAs of a row: as many as keep the SMs busy with two each, at most a portable cluster, none with less than 2048 logits.
+static int row_ctas_for(int64_t n_rows, int64_t V)
 {
-    auto kernel = token_logp_kernel<T, RULES, ENTROPY>;
-    // CTAs per row: as many as keep the SMs busy with two each, at most a portable cluster, none with less than 2048 logits
-    int row_ctas = 1;
+    int k = 1;
     if (clusters_on())
-        while (row_ctas < kMaxRowCtas && n_rows * row_ctas < 2 * (int64_t)sm_count() && V / (2 * row_ctas) >= 2048)
-            row_ctas *= 2;
-    if (n_rows * row_ctas > 0x7FFFFFFF)
+        while (k < kMaxRowCtas && n_rows * k < 2 * (int64_t)sm_count() && V / (2 * k) >= 2048)
+            k *= 2;
+    return k;
+}
+
+template <typename... KArgs, typename... Args>
+static int launch_rows(void (*kernel)(KArgs...), int64_t grid, int cluster, size_t smem, cudaStream_t st, Args... args)
+{
+    if (grid > 0x7FFFFFFF)
         return HILORE_SHAPE;
-    const size_t smem = R.tokens || R.bias_tokens ? kListedBytes : 0;
     if (!allow_smem(kernel, smem))
         return HILORE_CUDA;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(n_rows * row_ctas));
+    cfg.gridDim = dim3((unsigned)grid);
     cfg.blockDim = dim3(kLogpThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)row_ctas;
+    attr[0].val.clusterDim.x = (unsigned)cluster;
     attr[0].val.clusterDim.y = 1;
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = row_ctas > 1 ? 1 : 0;
-    if (cudaLaunchKernelEx(&cfg, kernel, x, ld, (int)V, row_ctas, targets, logp, lse, entropy, R) != cudaSuccess)
+    cfg.numAttrs = cluster > 1 ? 1 : 0;
+    if (cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...) != cudaSuccess)
         return HILORE_CUDA;
+    return cudaGetLastError() == cudaSuccess ? HILORE_OK : HILORE_CUDA;
+}
+
+template <typename T, bool ENTROPY>
+static int launch_logp(const T *x, int64_t ld, int64_t n_rows, int64_t V, const int32_t *targets, float *logp, float *lse, float *entropy,
+                       const hilore_logit_rules &R, cudaStream_t st)
+{
+    int k = row_ctas_for(n_rows, V);
+    if (!more_than_temperature(R))
+        return launch_rows(token_logp_kernel<T, ENTROPY>, n_rows * k, k, 0, st, x, ld, (int)V, k, targets, logp, lse, entropy, R.temperature);
+    // Enough CTAs for a row that a table of 16-bit counts takes a share of it; blocks of rows as far as four rounds of CTAs remain.
+    if (clusters_on() && has_lists(R))
+        while (k < kMaxRowCtas && V / k > kLogpTokens - 256)
+            k *= 2;
+    const int64_t width = ((V + 15 + k - 1) / k + 127) / 128 * 128;
+    int64_t words = width + kSlack; // at least two words for 128 tokens and the slack, the narrowest part of a range
+    words = words < 512 ? 512 : words > kLogpTokens / 2 ? kLogpTokens / 2 : (words + 3) & ~(int64_t)3;
+    int64_t block = n_rows * k / (16 * (int64_t)sm_count());
+    block = block < 1 || !has_lists(R) ? 1 : block > kBlockRows ? kBlockRows : block;
+    const int64_t grid = (n_rows + block - 1) / block * k;
+    const size_t smem = has_lists(R) ? kLogpFixed + (size_t)words * 4 : 0;
+    return launch_rows(token_logp_rules_kernel<T, ENTROPY>, grid, k, smem, st, x, ld, n_rows, (int)V, (int)block, k, (int)width, (int)words, targets, logp,
+                       lse, entropy, R);
+}
+
+template <typename T, bool LISTS>
+static int launch_logp_backward_as(const T *x, int64_t ld, int64_t n_rows, int64_t V, const int32_t *targets, const float *lse, const float *omega,
+                                   T *grad, int64_t ld_grad, const hilore_logit_rules &R, cudaStream_t st)
+{
+    const Split p = map_split(n_rows, V, LISTS);
+    if (p.grid > 0x7FFFFFFF)
+        return HILORE_SHAPE;
+    auto kernel = token_logp_backward_kernel<T, LISTS>;
+    const size_t smem = LISTS ? kMapShared : 0;
+    if (!allow_smem(kernel, smem))
+        return HILORE_CUDA;
+    kernel<<<(unsigned)p.grid, kMapThreads, smem, st>>>(x, ld, n_rows, (int)V, (int)p.block_rows, (int)p.n_ranges, (int)p.width, targets, lse, omega, grad,
+                                                       ld_grad, R);
     return cudaGetLastError() == cudaSuccess ? HILORE_OK : HILORE_CUDA;
 }
 
@@ -909,15 +1274,8 @@ template <typename T>
 static int launch_logp_backward(const T *x, int64_t ld, int64_t n_rows, int64_t V, const int32_t *targets, const float *lse, const float *omega,
                                 T *grad, int64_t ld_grad, const hilore_logit_rules &R, cudaStream_t st)
 {
-    const int64_t width = range_width(n_rows, V, R), n = (V + Lane<T>::N - 1 + width - 1) / width;
-    if (n * n_rows > 0x7FFFFFFF)
-        return HILORE_SHAPE;
-    auto kernel = token_logp_backward_kernel<T>;
-    const size_t smem = R.tokens || R.bias_tokens ? kListedBytes : 0;
-    if (!allow_smem(kernel, smem))
-        return HILORE_CUDA;
-    kernel<<<(unsigned)(n * n_rows), kMapThreads, smem, st>>>(x, ld, (int)V, (int)n, (int)width, targets, lse, omega, grad, ld_grad, R);
-    return cudaGetLastError() == cudaSuccess ? HILORE_OK : HILORE_CUDA;
+    return has_lists(R) ? launch_logp_backward_as<T, true>(x, ld, n_rows, V, targets, lse, omega, grad, ld_grad, R, st)
+                        : launch_logp_backward_as<T, false>(x, ld, n_rows, V, targets, lse, omega, grad, ld_grad, R, st);
 }
 
 } // namespace hilore
@@ -997,11 +1355,8 @@ extern "C" int hilore_token_logp(const void *logits, int32_t dtype, int64_t n_ro
     cudaStream_t st = static_cast<cudaStream_t>(stream);
 #define HILORE_PICK(T)                                                                                                                          \
     const T *p = static_cast<const T *>(logits);                                                                                                \
-    if (more_than_temperature(R))                                                                                                                        \
-        return entropy ? launch_logp<T, true, true>(p, ld, n_rows, V, targets, logp, lse, entropy, R, st)                                       \
-                       : launch_logp<T, true, false>(p, ld, n_rows, V, targets, logp, lse, entropy, R, st);                                     \
-    return entropy ? launch_logp<T, false, true>(p, ld, n_rows, V, targets, logp, lse, entropy, R, st)                                          \
-                   : launch_logp<T, false, false>(p, ld, n_rows, V, targets, logp, lse, entropy, R, st)
+    return entropy ? launch_logp<T, true>(p, ld, n_rows, V, targets, logp, lse, entropy, R, st)                                                 \
+                   : launch_logp<T, false>(p, ld, n_rows, V, targets, logp, lse, entropy, R, st)
     if (dtype == HILORE_BF16) { HILORE_PICK(uint16_t); }
     HILORE_PICK(float);
 #undef HILORE_PICK
