@@ -244,13 +244,16 @@ __device__ __forceinline__ bool is_denied(const uint32_t *words, int v) { return
 //   kBiased   two words per token, the second one the number of the last entry of the bias list that names it, for lists of
 //             more than kBiasCap entries.  Shorter ones are kept beside the table: bias_v[k] is the token of entry k if it is in
 //             the range (else -1), and `biased` has its bit.
-// Places that are not zero are also listed, in the order they were found, as far as the list reaches.
+// A bit per token says that its place is not zero, and those places are listed as far as the list reaches.  A whole history goes in by
+// atomics without a result (counts and bits; nothing waits for them), and the list is made from the bits, in the order of places; fresh
+// tokens of a following row are appended.  (Lists made by atomics that return the count before cost a round trip to shared memory
+// per token, and their order, which sums would depend on, is not the same in every call.)
 enum { kCount16 = 0, kCount32 = 1, kBiased = 2 };
 constexpr int kBiasCap = 512;
 constexpr int kSlack = 16;    // a range of positions [a, e) covers tokens from a - 15 on, depending on the row's alignment
 constexpr int kBlockRows = 8; // rows of a block at most
 
-__device__ __forceinline__ int table_words(int form, int width) { return form == kCount16 ? (width + 1) >> 1 : form == kCount32 ? width : 2 * width; }
+__host__ __device__ constexpr int table_words(int form, int width) { return form == kCount16 ? (width + 1) >> 1 : form == kCount32 ? width : 2 * width; }
 
 // A row of a CTA's block: its rules, and how to get from the table of the row before to this one's.
 struct RowPlan {
@@ -295,17 +298,18 @@ __device__ __forceinline__ void plan_rows(RowPlan *plan, int rows, const hilore_
     __syncthreads();
 }
 
-// Layout in shared memory: biased [BITS] (bit v - v0: a short bias list names the token), touch [BITS] where TOUCH (bit v - v0:
-// the history names the token), bias_v [kBiasCap], then the table.
-template <int BITS, bool TOUCH> struct Listed {
-    static constexpr int kFixed = BITS * 4 * (TOUCH ? 2 : 1) + kBiasCap * 4; // bytes before the table
+// Layout in shared memory: biased [BITS] (bit v - v0: a short bias list names the token), touch [BITS] (bit v - v0: the place is
+// listed), bias_v [kBiasCap], then the table.
+template <int BITS> struct Listed {
+    static constexpr int kFixed = BITS * 8 + kBiasCap * 4; // bytes before the table
     static_assert(BITS % 4 == 0, "16-byte pieces");
     unsigned char *base;
-    int *n; // places found; above the capacity of the list it is not complete
+    int *n;         // places listed; above the capacity of the list it is not complete
+    uint32_t *sums; // one word per warp
 
     __device__ __forceinline__ uint32_t *biased() const { return reinterpret_cast<uint32_t *>(base); }
-    __device__ __forceinline__ uint32_t *touch() const { return reinterpret_cast<uint32_t *>(base + (TOUCH ? BITS * 4 : 0)); }
-    __device__ __forceinline__ int *bias_v() const { return reinterpret_cast<int *>(base + BITS * 4 * (TOUCH ? 2 : 1)); }
+    __device__ __forceinline__ uint32_t *touch() const { return reinterpret_cast<uint32_t *>(base + BITS * 4); }
+    __device__ __forceinline__ int *bias_v() const { return reinterpret_cast<int *>(base + BITS * 8); }
     __device__ __forceinline__ uint32_t *word() const { return reinterpret_cast<uint32_t *>(base + kFixed); }
     __device__ __forceinline__ uint32_t count_at(int s, int form) const
     {
@@ -315,51 +319,40 @@ template <int BITS, bool TOUCH> struct Listed {
         return (h & 0x7FFFu) | (h >> 15 << 31);
     }
     __device__ __forceinline__ bool is_biased(int s) const { return biased()[s >> 5] >> (s & 31) & 1u; }
-    __device__ __forceinline__ void place(uint32_t s, uint16_t *list, int cap) const
+    __device__ __forceinline__ void count(uint32_t s, bool prompt, int form) const
     {
-        const int at = atomicAdd(n, 1);
-        if (at < cap) list[at] = (uint16_t)s;
-        if (TOUCH) atomicOr(touch() + (s >> 5), 1u << (s & 31));
-    }
-    __device__ __forceinline__ void add(int v, bool prompt, int V, int v0, int width, int form, uint16_t *list, int cap) const
-    {
-        const uint32_t s = (uint32_t)(v - v0);
-        if (s >= (uint32_t)width || (uint32_t)v >= (uint32_t)V)
-            return;
-        uint32_t old;
         if (form == kCount16) {
             const int sh = 16 * (s & 1);
-            old = prompt ? atomicOr(word() + (s >> 1), 0x8000u << sh) : atomicAdd(word() + (s >> 1), 1u << sh);
-            old = old >> sh & 0xFFFFu;
+            if (prompt) atomicOr(word() + (s >> 1), 0x8000u << sh);
+            else atomicAdd(word() + (s >> 1), 1u << sh);
         } else {
             uint32_t *w = word() + (form == kBiased ? 2 * s : s);
-            old = prompt ? atomicOr(w, kSeen) : atomicAdd(w, 1u);
-            if (form == kBiased) old |= w[1];
+            if (prompt) atomicOr(w, kSeen);
+            else atomicAdd(w, 1u);
         }
-        if (old == 0) place(s, list, cap);
     }
 
     // Brings table and bias entries to the row's rules for tokens [v0, v0 + width).  `follow`: by adding the plan's fresh tokens to the
-    // table of the row before.  Ends with the CTA synchronised.
+    // table of the row before; `sorted`: the list has to be in the order of places after that as well.  Ends with the CTA
+    // synchronised.
     template <int THREADS>
-    __device__ __forceinline__ void fill(const hilore_logit_rules &R, const RowPlan &p, int V, int v0, int width, int form, bool follow, uint16_t *list,
-                                         int cap) const
+    __device__ __forceinline__ void fill(const hilore_logit_rules &R, const RowPlan &p, int V, int v0, int width, int form, bool follow, bool sorted,
+                                         uint16_t *list, int cap) const
     {
-        const int tid = threadIdx.x;
+        const int tid = threadIdx.x, bits = ((width + 127) >> 7) * 4;
         const bool counts = p.q.history() || form == kBiased, clear = counts && !follow;
+        int before = 0;
         if (clear || p.n_bias > 0) {
             __syncthreads(); // the row before is done with both
             if (clear) {
                 const int quads = (table_words(form, width) + 3) >> 2;
                 for (int i = tid; i < quads; i += THREADS)
                     reinterpret_cast<uint4 *>(word())[i] = make_uint4(0, 0, 0, 0);
-                if (TOUCH)
-                    for (int i = tid; i < BITS / 4; i += THREADS)
-                        reinterpret_cast<uint4 *>(touch())[i] = make_uint4(0, 0, 0, 0);
-                if (tid == 0) *n = 0;
+                for (int i = tid; i < bits / 4; i += THREADS)
+                    reinterpret_cast<uint4 *>(touch())[i] = make_uint4(0, 0, 0, 0);
             }
             if (p.n_bias > 0)
-                for (int i = tid; i < BITS / 4; i += THREADS)
+                for (int i = tid; i < bits / 4; i += THREADS)
                     reinterpret_cast<uint4 *>(biased())[i] = make_uint4(0, 0, 0, 0);
             __syncthreads();
             for (int64_t i = p.q.bias_lo + tid; i < p.q.bias_hi; i += THREADS) {
@@ -369,15 +362,28 @@ template <int BITS, bool TOUCH> struct Listed {
                 if (form != kBiased) {
                     bias_v()[k] = in ? v : -1;
                     if (in) atomicOr(biased() + (s >> 5), 1u << (s & 31));
-                } else if (in && atomicMax(word() + 2 * s + 1, (uint32_t)k + 1u) == 0) {
-                    place(s, list, cap);
+                } else if (in) {
+                    atomicMax(word() + 2 * s + 1, (uint32_t)k + 1u);
+                    atomicOr(touch() + (s >> 5), 1u << (s & 31));
                 }
             }
-            if (form == kBiased) __syncthreads();
         }
         if (follow) {
-            for (int i = tid; i < p.fresh; i += THREADS)
-                add(__ldg(p.from + i), i < p.fresh_prompt, V, v0, width, form, list, cap);
+            if (sorted) {
+                before = *n;
+                __syncthreads();
+            }
+            for (int i = tid; i < p.fresh; i += THREADS) {
+                const int v = __ldg(p.from + i);
+                const uint32_t s = (uint32_t)(v - v0), bit = 1u << (s & 31);
+                if (s >= (uint32_t)width || (uint32_t)v >= (uint32_t)V)
+                    continue;
+                count(s, i < p.fresh_prompt, form);
+                if (!(atomicOr(touch() + (s >> 5), bit) & bit)) {
+                    const int at = atomicAdd(n, 1);
+                    if (at < cap) list[at] = (uint16_t)s;
+                }
+            }
         } else if (p.q.history()) {
             constexpr int U = 8; // tokens in flight per thread
             const int32_t *from = R.tokens + p.q.hist_lo;
@@ -390,42 +396,46 @@ template <int BITS, bool TOUCH> struct Listed {
                     v[u] = u * THREADS + tid < here ? __ldg(from + u * THREADS + tid) : -1;
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    if (u * THREADS >= here)
-                        break;
-                    add(v[u], u * THREADS + tid < first, V, v0, width, form, list, cap);
+                    const uint32_t s = (uint32_t)(v[u] - v0);
+                    if (s < (uint32_t)width && (uint32_t)v[u] < (uint32_t)V) {
+                        count(s, u * THREADS + tid < first, form);
+                        atomicOr(touch() + (s >> 5), 1u << (s & 31));
+                    }
                 }
             }
         }
         __syncthreads();
+        if (clear || (follow && sorted && *n > before + 1 && *n <= cap)) order<THREADS>(bits, list, cap);
     }
 
-    // Puts the list in the order of places, from the touch bits: a sum over listed tokens must not depend on the order in
-    // which atomics found them.  `sums`: one word per warp.  Ends with the CTA synchronised.
-    template <int THREADS> __device__ __forceinline__ void order(uint32_t *sums, uint16_t *list) const
+    // Makes the list from the touch bits.  Ends with the CTA synchronised.
+    template <int THREADS> __device__ __forceinline__ void order(int bits, uint16_t *list, int cap) const
     {
         constexpr int W = (BITS + THREADS - 1) / THREADS;
         const int tid = threadIdx.x, lane = tid & 31;
-        uint32_t w[W], own = 0;
+        uint32_t w[W];
+        int own = 0;
 #pragma unroll
         for (int j = 0; j < W; ++j) {
-            w[j] = tid * W + j < BITS ? touch()[tid * W + j] : 0u;
-            own += (uint32_t)__popc(w[j]);
+            w[j] = tid * W + j < bits ? touch()[tid * W + j] : 0u;
+            own += __popc(w[j]);
         }
-        uint32_t at = own;
+        int at = own;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const uint32_t below = __shfl_up_sync(0xFFFFFFFFu, at, o);
+            const int below = __shfl_up_sync(0xFFFFFFFFu, at, o);
             if (lane >= o) at += below;
         }
-        if (lane == 31) sums[tid >> 5] = at;
+        if (lane == 31) sums[tid >> 5] = (uint32_t)at;
         __syncthreads();
         at -= own;
         for (int k = 0; k < (tid >> 5); ++k)
-            at += sums[k];
+            at += (int)sums[k];
+        if (tid == THREADS - 1) *n = at + own;
 #pragma unroll
         for (int j = 0; j < W; ++j)
-            for (; w[j]; w[j] &= w[j] - 1)
-                list[at++] = (uint16_t)((tid * W + j) * 32 + __ffs((int)w[j]) - 1);
+            for (; w[j]; w[j] &= w[j] - 1, ++at)
+                if (at < cap) list[at] = (uint16_t)((tid * W + j) * 32 + __ffs((int)w[j]) - 1);
         __syncthreads();
     }
 
@@ -565,17 +575,23 @@ template <typename T> struct Stage {
     }
 };
 
-// Shared memory of a CTA with listed tokens: bits, bias entries and their results, and a pool for the table, the list and the
-// results of the listed tokens.  Whatever the pool leaves beside the table bounds the list; a range with more listed tokens
-// is worked on in parts of half the size, which always fit from 2048 tokens down.
+// Shared memory of a CTA with listed tokens: bits, bias entries, and a pool for the table, the list and the results of the listed
+// tokens.  A range is worked on as a whole where the row's lists cannot outgrow what the pool leaves beside the table, otherwise in
+// parts whose every token may be listed.
 constexpr int kMapRange = 3 * kMapStage; // positions of a CTA's range at most: a table of 16-bit counts
 constexpr int kMapBits = (kMapRange + kSlack + 127) / 128 * 4;
 constexpr int kMapPool = 15 * 1024; // words
-using MapListed = Listed<kMapBits, false>;
+constexpr int kMapDense = 7552;     // part whose every token may be listed, 16-bit counts
+using MapListed = Listed<kMapBits>;
 constexpr size_t kMapShared = MapListed::kFixed + kMapPool * 4;
-static_assert(6 * (2048 + kSlack) <= 4 * (kMapPool - 2 * (2048 + kSlack) - 4), "parts of 2048 tokens fit in every form");
-static_assert(kMapRange / 2 + kSlack + 2048 <= kMapPool, "the largest table leaves room for a list");
 constexpr uint32_t kNoResult = 0xFFFFFFFFu; // no result of an operation: NaNs are 0x7FFFFFFF
+
+__host__ __device__ constexpr int map_table_words(int form, int step) { return (table_words(form, step + kSlack) + 3) & ~3; }
+__host__ __device__ constexpr int map_capacity(int form, int step) { return (kMapPool - map_table_words(form, step)) * 4 / 6 & ~1; } // of the list
+__host__ __device__ constexpr int map_dense(int form) { return form == kCount16 ? kMapDense : form == kCount32 ? 5888 : 4352; }
+static_assert(map_capacity(kCount16, map_dense(kCount16)) >= map_dense(kCount16) + kSlack && map_capacity(kCount32, map_dense(kCount32)) >= map_dense(kCount32) + kSlack &&
+                  map_capacity(kBiased, map_dense(kBiased)) >= map_dense(kBiased) + kSlack && map_capacity(kCount16, kMapRange) > 2000,
+              "sizes of tables and lists");
 
 // Positions [a, b) of a row without listed tokens.
 template <typename T, typename Map>
@@ -590,12 +606,6 @@ __device__ __forceinline__ void map_plain(const Row<T> &dst, const T *in, const 
         stage.store(dst, map, a, b);
     }
 }
-
-// What a CTA carries from row to row.
-struct MapState {
-    int part;    // positions that are worked on at once, as far as the form of the table allows
-    bool intact; // the table holds the last row with one, over the whole range
-};
 
 // Result of listed token v as bits, or kNoResult where it is not this range's or denied.
 template <typename T, typename Map>
@@ -612,24 +622,20 @@ __device__ __forceinline__ uint32_t listed_result(const Map &map, const T *in, c
 // Positions [a, b) of a row with listed tokens.  `in_place`: the output is the input.
 template <typename T, typename Map>
 __device__ __forceinline__ void map_listed(const Row<T> &dst, const T *in, const T *x, const Map &map, const RowPlan &plan, const hilore_logit_rules &R,
-                                           int V, int a, int b, int range, bool in_place, const MapListed &t, uint32_t *bias_result, MapState &m)
+                                           int V, int a, int b, int range, bool in_place, const MapListed &t, uint32_t *bias_result, bool &intact)
 {
     const RowRules &q = plan.q;
     const int tid = threadIdx.x, n_bias = plan.n_bias, form = plan.form, lead = dst.lead;
     const bool counts = q.history() || form == kBiased;
-    int step = min(m.part, form == kCount16 ? kMapRange : form == kCount32 ? kMapRange / 3 : kMapRange / 6);
+    const int64_t most = q.hist_hi - q.hist_lo + (form == kBiased ? q.bias_hi - q.bias_lo : 0); // different tokens of the row at most
+    const int step = form == kCount16 && most <= map_capacity(kCount16, kMapRange) ? range : min(range, map_dense(form));
+    const int cap = map_capacity(form, step);
+    uint16_t *list = reinterpret_cast<uint16_t *>(t.word() + map_table_words(form, step));
+    uint32_t *result = t.word() + map_table_words(form, step) + cap / 2;
     while (a < b) {
-        const int e = min(b, a + step), v0 = a - kSlack, words = (table_words(form, step + kSlack) + 3) & ~3;
-        uint16_t *list = reinterpret_cast<uint16_t *>(t.word() + words);
-        const int cap = (kMapPool - words) * 4 / 6 & ~1;
-        uint32_t *result = t.word() + words + cap / 2;
-        t.template fill<kMapThreads>(R, plan, V, v0, step + kSlack, form, plan.follows && m.intact && step == range, list, cap);
+        const int e = min(b, a + step), v0 = a - kSlack;
+        t.template fill<kMapThreads>(R, plan, V, v0, step + kSlack, form, plan.follows && intact && step == range, false, list, cap);
         const int n = counts ? *t.n : 0;
-        if (n > cap) {
-            m.part = step = (step / 2 + 127) & ~127;
-            m.intact = false;
-            continue;
-        }
         // Everything is read before anything is stored, as the output may be the input.
         for (int i = tid; i < n; i += kMapThreads) {
             const int p = list[i];
@@ -656,7 +662,7 @@ __device__ __forceinline__ void map_listed(const Row<T> &dst, const T *in, const
             if (result[i] != kNoResult) Lane<T>::put(row + (v0 + (int)list[i]), __uint_as_float(result[i]));
         for (int k = tid; k < n_bias; k += kMapThreads)
             if (bias_result[k] != kNoResult) Lane<T>::put(row + t.bias_v()[k], __uint_as_float(bias_result[k]));
-        if (counts) m.intact = step == range && form != kBiased;
+        if (counts) intact = step == range && form != kBiased; // the table holds the last row with one, over the whole range
         a += step;
     }
 }
@@ -687,7 +693,7 @@ __global__ void __launch_bounds__(kMapThreads, !LISTS && sizeof(T) == 2 ? 4 : 3)
     }
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ RowPlan plan[kBlockRows];
-    __shared__ uint32_t bias_result[kBiasCap];
+    __shared__ uint32_t bias_result[kBiasCap], sums[kMapThreads / 32];
     __shared__ int count;
     const int rows = (int)min((int64_t)block_rows, n_rows - row0);
     if ((int)threadIdx.x < rows) {
@@ -695,8 +701,8 @@ __global__ void __launch_bounds__(kMapThreads, !LISTS && sizeof(T) == 2 ? 4 : 3)
         plan[threadIdx.x].used = true;
     }
     plan_rows(plan, rows, R);
-    const MapListed t{smem, &count};
-    MapState m{width, false};
+    const MapListed t{smem, &count, sums};
+    bool intact = false;
     for (int i = 0; i < rows; ++i) {
         const RowRules &q = plan[i].q;
         const Row<T> dst(out + (row0 + i) * ld_out, V);
@@ -708,8 +714,8 @@ __global__ void __launch_bounds__(kMapThreads, !LISTS && sizeof(T) == 2 ? 4 : 3)
             if (GRAD) map_plain(dst, from, MapApplyGrad{q.inv_temp}, q.mask, V, a, b);
             else map_plain(dst, from, MapApply{q.inv_temp}, q.mask, V, a, b);
         } else {
-            if (GRAD) map_listed(dst, from, at, MapApplyGrad{q.inv_temp}, plan[i], R, V, a, b, width, in == out, t, bias_result, m);
-            else map_listed(dst, from, at, MapApply{q.inv_temp}, plan[i], R, V, a, b, width, in == out, t, bias_result, m);
+            if (GRAD) map_listed(dst, from, at, MapApplyGrad{q.inv_temp}, plan[i], R, V, a, b, width, in == out, t, bias_result, intact);
+            else map_listed(dst, from, at, MapApply{q.inv_temp}, plan[i], R, V, a, b, width, in == out, t, bias_result, intact);
         }
     }
 }
@@ -751,7 +757,7 @@ __global__ void __launch_bounds__(kMapThreads, !LISTS && sizeof(T) == 2 ? 4 : 3)
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ RowPlan plan[kBlockRows];
     __shared__ RowLoss losses[kBlockRows];
-    __shared__ uint32_t bias_result[kBiasCap];
+    __shared__ uint32_t bias_result[kBiasCap], sums[kMapThreads / 32];
     __shared__ int count;
     const int rows = (int)min((int64_t)block_rows, n_rows - row0);
     if ((int)threadIdx.x < rows) {
@@ -761,8 +767,8 @@ __global__ void __launch_bounds__(kMapThreads, !LISTS && sizeof(T) == 2 ? 4 : 3)
         plan[threadIdx.x].used = losses[threadIdx.x].live;
     }
     plan_rows(plan, rows, R);
-    const MapListed t{smem, &count};
-    MapState m{width, false};
+    const MapListed t{smem, &count, sums};
+    bool intact = false;
     for (int i = 0; i < rows; ++i) {
         const RowRules &q = plan[i].q;
         const RowLoss p = losses[i];
@@ -774,7 +780,7 @@ __global__ void __launch_bounds__(kMapThreads, !LISTS && sizeof(T) == 2 ? 4 : 3)
         const MapLogpGrad map{q.inv_temp, p.lse, p.omega * q.inv_temp, p.target + dst.lead};
         if (!p.live) zero_range(dst, a, b);
         else if (!q.listed()) map_plain(dst, from, map, q.mask, V, a, b);
-        else map_listed(dst, from, from, map, plan[i], R, V, a, b, width, x == grad, t, bias_result, m);
+        else map_listed(dst, from, from, map, plan[i], R, V, a, b, width, x == grad, t, bias_result, intact);
     }
 }
 
@@ -949,7 +955,7 @@ __global__ void __launch_bounds__(kLogpThreads, 4)
 // CTA, which joins them when the block is done.
 constexpr int kLogpTokens = 20480; // tokens of a table of 16-bit counts at most: 8 CTAs take vocabularies up to 163712
 constexpr int kLogpBits = kLogpTokens / 32 + 8, kLogpCap = 2048;
-using LogpListed = Listed<kLogpBits, true>;
+using LogpListed = Listed<kLogpBits>;
 constexpr size_t kLogpFixed = LogpListed::kFixed; // bytes before the table; the list is in static shared memory
 
 template <typename T, bool ENTROPY>
@@ -980,7 +986,7 @@ __global__ void __launch_bounds__(kLogpThreads, sizeof(T) == 4 ? 3 : 4)
     }
     plan_rows(plan, rows, R);
     if (row_ctas > 1) cl.barrier_wait();
-    const LogpListed t{smem, &count};
+    const LogpListed t{smem, &count, sums};
     bool intact = false; // the table holds the last row with one, over the whole range
     Soft(*to_part)[kMaxRowCtas * kLogpWarps] = row_ctas > 1 ? cl.map_shared_rank(&part[0], 0) : &part[0];
     float *to_z = row_ctas > 1 ? cl.map_shared_rank(&target_z[0], 0) : &target_z[0];
@@ -1006,12 +1012,9 @@ __global__ void __launch_bounds__(kLogpThreads, sizeof(T) == 4 ? 3 : 4)
             if (lists) {
                 __syncthreads(); // the last range or row is done with the table
                 const bool follow = plan[r].follows && intact && step == width;
-                const int before = follow ? count : 0;
-                if (follow) __syncthreads();
-                t.template fill<kLogpThreads>(R, plan[r], V, v0, step + kSlack, form, follow, list, kLogpCap);
+                t.template fill<kLogpThreads>(R, plan[r], V, v0, step + kSlack, form, follow, true, list, kLogpCap);
                 const int n = counts ? count : 0;
                 const bool whole = n <= kLogpCap; // the list is complete; otherwise every place of the table is asked
-                if (counts && whole && (!follow || n > before + 1)) t.template order<kLogpThreads>(sums, list);
                 if (counts) intact = step == width && form != kBiased;
                 for (int i = tid; i < (whole ? n : counts ? step + kSlack : 0); i += kLogpThreads) {
                     const int p = whole ? (int)list[i] : i, v = v0 + p, f = v + src.lead;
@@ -1155,10 +1158,11 @@ static bool has_lists(const hilore_logit_rules &q) { return q.tokens || q.bias_t
 struct Split {
     int64_t block_rows, width, n_ranges, grid;
 };
-static Split map_split(int64_t n_rows, int64_t V, bool lists)
+static Split map_split(int64_t n_rows, int64_t V, const hilore_logit_rules &R, bool lists)
 {
     const int64_t sms = sm_count();
     Split p{1, lists ? kMapRange : 2 * kMapStage, 0, 0};
+    if (lists && R.n_tokens / n_rows > map_capacity(kCount16, kMapRange)) p.width = kMapDense; // long histories of their own
     const auto ranges = [&] { return (V + 15 + p.width - 1) / p.width; };
     while (p.width > 2048 && n_rows * ranges() < 4 * sms)
         p.width = (p.width / 2 + 127) / 128 * 128;
@@ -1173,7 +1177,7 @@ template <typename T, bool GRAD, bool LISTS>
 static int launch_apply_as(const T *x, int64_t ld, const T *in, int64_t ld_in, T *out, int64_t ld_out, int64_t n_rows, int64_t V,
                            const hilore_logit_rules &R, cudaStream_t st)
 {
-    const Split p = map_split(n_rows, V, LISTS);
+    const Split p = map_split(n_rows, V, R, LISTS);
     if (p.grid > 0x7FFFFFFF)
         return HILORE_SHAPE;
     auto kernel = logits_apply_kernel<T, GRAD, LISTS>;
@@ -1239,14 +1243,14 @@ static int launch_logp(const T *x, int64_t ld, int64_t n_rows, int64_t V, const 
     int k = row_ctas_for(n_rows, V);
     if (!more_than_temperature(R))
         return launch_rows(token_logp_kernel<T, ENTROPY>, n_rows * k, k, 0, st, x, ld, (int)V, k, targets, logp, lse, entropy, R.temperature);
-    // Enough CTAs for a row that a table of 16-bit counts takes a share of it; blocks of rows as far as four rounds of CTAs remain.
+    // Enough CTAs for a row that a table of 16-bit counts takes a share of it; blocks of rows while a round of CTAs remains.
     if (clusters_on() && has_lists(R))
         while (k < kMaxRowCtas && V / k > kLogpTokens - 256)
             k *= 2;
     const int64_t width = ((V + 15 + k - 1) / k + 127) / 128 * 128;
     int64_t words = width + kSlack; // at least two words for 128 tokens and the slack, the narrowest part of a range
     words = words < 512 ? 512 : words > kLogpTokens / 2 ? kLogpTokens / 2 : (words + 3) & ~(int64_t)3;
-    int64_t block = n_rows * k / (16 * (int64_t)sm_count());
+    int64_t block = n_rows * k / (4 * (int64_t)sm_count());
     block = block < 1 || !has_lists(R) ? 1 : block > kBlockRows ? kBlockRows : block;
     const int64_t grid = (n_rows + block - 1) / block * k;
     const size_t smem = has_lists(R) ? kLogpFixed + (size_t)words * 4 : 0;
@@ -1258,7 +1262,7 @@ template <typename T, bool LISTS>
 static int launch_logp_backward_as(const T *x, int64_t ld, int64_t n_rows, int64_t V, const int32_t *targets, const float *lse, const float *omega,
                                    T *grad, int64_t ld_grad, const hilore_logit_rules &R, cudaStream_t st)
 {
-    const Split p = map_split(n_rows, V, LISTS);
+    const Split p = map_split(n_rows, V, R, LISTS);
     if (p.grid > 0x7FFFFFFF)
         return HILORE_SHAPE;
     auto kernel = token_logp_backward_kernel<T, LISTS>;

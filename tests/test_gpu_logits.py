@@ -133,6 +133,10 @@ CASES = [  # rows, V, ld, shift, ld_out, history, bias, grammar, prefix
     (9, 20011, 20011, 2, 20011, 5000, 40, "indexed", True),
     (2, 70001, 70016, 0, 70001, 90000, 500, "rows", False),
     (300, 257, 257, 0, 257, 100, 8, "rows", False),
+    (3, 30011, 30011, 1, 30011, 3000, 1500, "indexed", False),      # bias lists too long to be kept beside the counts
+    (4000, 301, 301, 0, 301, 500, 0, None, True),                   # blocks of rows: prefixes of one sequence, started anew ...
+    (3700, 300, 305, 3, 300, 90, 3, "indexed", True),               # ... with bias lists and masks between
+    (3600, 517, 517, 0, 520, 60, 0, None, False),                   # ... and histories that have nothing in common
 ]
 
 
