@@ -24,7 +24,7 @@ namespace hilore {
 constexpr float kLog2eF = 1.4426950408889634f;
 constexpr float kLowest = -3.402823466e38f; // the running maximum of a row starts here: a row of -inf keeps a finite one
 constexpr float kNothing = -1e30f;          // an lse at or below this belongs to a row without a token to choose from
-constexpr uint32_t kSeen = 0x80000000u;     // bit of a count: the token occurs in the prompt part of the history
+constexpr uint32_t kSeen = 0x80000000u;     // bit of a count: the token occurs in the history
 
 __device__ __forceinline__ float ex2_ftz(float x)
 {
@@ -80,8 +80,8 @@ template <> struct Lane<float> {
 };
 
 // A row in the frame of its 32-byte vectors: position f = v + lead, so that position 0 is 32-byte aligned whatever the
-// leading dimension is.  Only the first and the last vector of a row can hold positions of other rows; their elements
-// are loaded and stored one by one.
+// leading dimension is.  Vectors are moved where they lie wholly in the row; what is left at its two ends goes element by
+// element, a thread each, out of the way of the vectors' code.
 template <typename T> struct Row {
     T *origin; // address of position 0; never dereferenced outside [lead, end)
     int lead, end;
@@ -91,43 +91,37 @@ template <typename T> struct Row {
         origin = const_cast<T *>(row) - lead;
         end = lead + V;
     }
-    __device__ __forceinline__ bool whole(int f) const { return f >= lead && f + Lane<T>::N <= end; }
-    __device__ __forceinline__ uint32_t valid(int f) const // bit i: position f + i belongs to the row
+    // Positions [a, b) as far as they are the row's: elements [lo, fa), vectors [fa, fb), elements [fb, hi).
+    struct Parts {
+        int lo, fa, fb, hi;
+    };
+    __device__ __forceinline__ Parts parts(int a, int b) const { return parts(a, b, lead, end); }
+    __device__ __forceinline__ Parts parts(int a, int b, int first, int last) const // vectors within [first, last) alone
     {
         constexpr int N = Lane<T>::N;
-        uint32_t m = (1u << N) - 1u;
-        if (f < lead) m &= m << (lead - f);
-        if (f + N > end) m = (f >= end) ? 0u : m & ((1u << (end - f)) - 1u);
-        return m;
+        Parts p{max(a, lead), 0, 0, min(b, end)};
+        p.fa = (max(p.lo, first) + N - 1) & ~(N - 1);
+        p.fb = min(p.hi, last) & ~(N - 1);
+        if (p.fa >= p.fb) p.fa = p.fb = p.hi;
+        return p;
     }
-    __device__ __forceinline__ void load(int f, uint32_t (&w)[8]) const
-    {
-        if (whole(f)) ld_global_256(origin + f, w);
-        else load_part(origin, valid(f), f, w);
-    }
-    // Elements f .. f + N - 1 of `m` from base + f.
-    static __device__ __forceinline__ void load_part(const T *base, uint32_t m, int f, uint32_t (&w)[8])
-    {
-        float z[Lane<T>::N];
-#pragma unroll
-        for (int i = 0; i < Lane<T>::N; ++i)
-            z[i] = (m >> i & 1u) ? Lane<T>::one(base + f + i) : 0.0f;
-        Lane<T>::pack(z, w);
-    }
+    __device__ __forceinline__ void load(int f, uint32_t (&w)[8]) const { ld_global_256(origin + f, w); }
     __device__ __forceinline__ void store(int f, const float (&z)[Lane<T>::N]) const
     {
-        if (whole(f)) {
-            uint32_t w[8];
-            Lane<T>::pack(z, w);
-            st_global_256(origin + f, w);
-            return;
-        }
-        const uint32_t m = valid(f);
-#pragma unroll
-        for (int i = 0; i < Lane<T>::N; ++i)
-            if (m >> i & 1u) Lane<T>::put(origin + f + i, z[i]);
+        uint32_t w[8];
+        Lane<T>::pack(z, w);
+        st_global_256(origin + f, w);
     }
 };
+
+// Calls f(position) for the elements of `p` that are in no vector.
+template <int THREADS, typename P, typename F> __device__ __forceinline__ void each_edge(const P &p, const F &f)
+{
+    const int left = max(p.fa - p.lo, 0), n = left + max(p.hi - p.fb, 0);
+#pragma unroll 1
+    for (int i = threadIdx.x; i < n; i += THREADS)
+        f(i < left ? p.lo + i : p.fb + (i - left));
+}
 
 // Reads of a row in the frame of another one (the row that is written).  Where the two addresses differ modulo 32 bytes, a
 // vector is put together from two neighbouring aligned ones by a shift of whole words and, for bf16, of half a word; the
@@ -144,18 +138,20 @@ template <typename T> struct Source {
         shift = d < 0 ? d + Lane<T>::N : d;
         aligned = own.origin + (d - shift);  // d - shift is 0 or -N
     }
-    template <bool SHIFTED> __device__ __forceinline__ void load(const Row<T> &frame, int f, uint32_t (&w)[8]) const
+    // Parts of positions [a, b) of the frame whose vectors can be read.
+    __device__ __forceinline__ typename Row<T>::Parts parts(const Row<T> &frame, int a, int b) const
     {
-        constexpr int N = Lane<T>::N;
+        if (shift == 0) return frame.parts(a, b);
+        const int to_own = (int)(aligned - own.origin); // position f of the frame: the vectors at f + to_own and the next one
+        return frame.parts(a, b, max(frame.lead, own.lead - to_own), min(frame.end, own.end - to_own - Lane<T>::N));
+    }
+    template <bool SHIFTED> __device__ __forceinline__ void load(int f, uint32_t (&w)[8]) const
+    {
         if (!SHIFTED) {
-            frame.whole(f) ? ld_global_256(exact + f, w) : Row<T>::load_part(exact, frame.valid(f), f, w);
+            ld_global_256(exact + f, w);
             return;
         }
-        const int lo = (int)(aligned - own.origin) + f; // position of the first aligned vector in the read row's own frame
-        if (!own.whole(lo) || !own.whole(lo + N)) {
-            Row<T>::load_part(exact, frame.valid(f), f, w);
-            return;
-        }
+        constexpr int N = Lane<T>::N;
         uint32_t v[16];
         ld_cached(aligned + f, v);
         ld_cached(aligned + f + N, v + 8);
@@ -237,15 +233,15 @@ template <int N> __device__ __forceinline__ uint32_t denied(const uint32_t *word
 
 __device__ __forceinline__ bool is_denied(const uint32_t *words, int v) { return words != nullptr && !(__ldg(words + (v >> 5)) >> (v & 31) & 1u); }
 
-// The tokens of a row's history that fall into a range of `width` tokens from v0 on, in a table of counts: occurrences in the
-// generated part, with the top bit set if the token occurs in the prompt part.  Three forms of the table:
-//   kCount16  16 bits per token, for generated parts below 2^15 tokens;
+// The tokens of a row's history that fall into a range of `width` tokens from v0 on: a bit per token, and a table of the
+// occurrences in the generated part.  Three forms of the table:
+//   kCount16  16 bits per token, for generated parts below 2^16 tokens;
 //   kCount32  32 bits per token;
-//   kBiased   two words per token, the second one the number of the last entry of the bias list that names it, for lists of
-//             more than kBiasCap entries.  Shorter ones are kept beside the table: bias_v[k] is the token of entry k if it is in
+//   kBiased   two words per token, kSeen and the occurrences, and the number of the last entry of the bias list that names it, for
+//             lists of more than kBiasCap entries.  Shorter ones are kept beside the table: bias_v[k] is the token of entry k if it is in
 //             the range (else -1), and `biased` has its bit.
 // A bit per token says that its place is not zero, and those places are listed as far as the list reaches.  A whole history goes in by
-// atomics without a result (counts and bits; nothing waits for them), and the list is made from the bits, in the order of places; fresh
+// atomics without a result (counts and bits; nothing waits for them), and the list is made from the bits; fresh
 // tokens of a following row are appended.  (Lists made by atomics that return the count before cost a round trip to shared memory
 // per token, and their order, which sums would depend on, is not the same in every call.)
 enum { kCount16 = 0, kCount32 = 1, kBiased = 2 };
@@ -263,6 +259,7 @@ struct RowPlan {
     bool follows;             // its history is that of the last row with a table and the `fresh` tokens from `from` on
     int fresh, fresh_prompt;  // ... of which the first fresh_prompt are prompt
     const int32_t *from;
+    int first[4];             // the first four of them
 };
 
 // Plans of a block's rows, one thread each.  `used` is set.  Ends with the CTA synchronised.
@@ -273,7 +270,7 @@ __device__ __forceinline__ void plan_rows(RowPlan *plan, int rows, const hilore_
         RowPlan &p = plan[i];
         const int64_t list = p.q.bias_hi - p.q.bias_lo;
         p.n_bias = list <= kBiasCap ? (int)list : 0;
-        p.form = list > kBiasCap ? kBiased : p.q.hist_hi - p.q.hist_mid < (1 << 15) ? kCount16 : kCount32;
+        p.form = list > kBiasCap ? kBiased : p.q.hist_hi - p.q.hist_mid < (1 << 16) ? kCount16 : kCount32;
     }
     __syncthreads();
     if (i < rows) {
@@ -292,6 +289,8 @@ __device__ __forceinline__ void plan_rows(RowPlan *plan, int rows, const hilore_
                 p.from = R.tokens + a.hist_hi;
                 p.fresh = (int)(b.hist_hi - a.hist_hi);
                 p.fresh_prompt = (int)max((int64_t)0, b.hist_mid - a.hist_hi);
+                for (int k = 0; k < 4; ++k)
+                    p.first[k] = k < p.fresh ? __ldg(p.from + k) : -1;
             }
         }
     }
@@ -299,41 +298,38 @@ __device__ __forceinline__ void plan_rows(RowPlan *plan, int rows, const hilore_
 }
 
 // Layout in shared memory: biased [BITS] (bit v - v0: a short bias list names the token), touch [BITS] (bit v - v0: the place is
-// listed), bias_v [kBiasCap], then the table.
+// listed), bias_v and bias_x [kBiasCap] (token and value of the entries of a short bias list), then the table.
 template <int BITS> struct Listed {
-    static constexpr int kFixed = BITS * 8 + kBiasCap * 4; // bytes before the table
+    static constexpr int kFixed = BITS * 8 + kBiasCap * 8; // bytes before the table
     static_assert(BITS % 4 == 0, "16-byte pieces");
     unsigned char *base;
     int *n;         // places listed; above the capacity of the list it is not complete
+    uint32_t *doubles; // 1: a token is named twice by the short bias list
     uint32_t *sums; // one word per warp
 
     __device__ __forceinline__ uint32_t *biased() const { return reinterpret_cast<uint32_t *>(base); }
     __device__ __forceinline__ uint32_t *touch() const { return reinterpret_cast<uint32_t *>(base + BITS * 4); }
     __device__ __forceinline__ int *bias_v() const { return reinterpret_cast<int *>(base + BITS * 8); }
+    __device__ __forceinline__ float *bias_x() const { return reinterpret_cast<float *>(base + BITS * 8 + kBiasCap * 4); }
     __device__ __forceinline__ uint32_t *word() const { return reinterpret_cast<uint32_t *>(base + kFixed); }
+    // Occurrences in the generated part with kSeen if there are any at all: of a listed place, and of any place.
     __device__ __forceinline__ uint32_t count_at(int s, int form) const
     {
-        if (form == kCount32) return word()[s];
         if (form == kBiased) return word()[2 * s];
-        const uint32_t h = word()[s >> 1] >> (16 * (s & 1)) & 0xFFFFu;
-        return (h & 0x7FFFu) | (h >> 15 << 31);
+        return kSeen | (form == kCount32 ? word()[s] : word()[s >> 1] >> (16 * (s & 1)) & 0xFFFFu);
     }
+    __device__ __forceinline__ uint32_t count_of(int s, int form) const { return touch()[s >> 5] >> (s & 31) & 1u ? count_at(s, form) : 0u; }
     __device__ __forceinline__ bool is_biased(int s) const { return biased()[s >> 5] >> (s & 31) & 1u; }
-    __device__ __forceinline__ void count(uint32_t s, bool prompt, int form) const
+    __device__ __forceinline__ void count(int s, bool prompt, int form) const
     {
-        if (form == kCount16) {
-            const int sh = 16 * (s & 1);
-            if (prompt) atomicOr(word() + (s >> 1), 0x8000u << sh);
-            else atomicAdd(word() + (s >> 1), 1u << sh);
-        } else {
-            uint32_t *w = word() + (form == kBiased ? 2 * s : s);
-            if (prompt) atomicOr(w, kSeen);
-            else atomicAdd(w, 1u);
-        }
+        const int odd = form == kCount16 ? s & 1 : 0;
+        uint32_t *w = word() + (form == kCount16 ? s >> 1 : form == kBiased ? 2 * s : s);
+        if (!prompt) atomicAdd(w, 1u << (16 * odd));
+        if (form == kBiased) atomicOr(w, kSeen);
     }
 
     // Brings table and bias entries to the row's rules for tokens [v0, v0 + width).  `follow`: by adding the plan's fresh tokens to the
-    // table of the row before; `sorted`: the list has to be in the order of places after that as well.  Ends with the CTA
+    // table of the row before; `sorted`: the list has to be as it would be made from the bits after that as well.  Ends with the CTA
     // synchronised.
     template <int THREADS>
     __device__ __forceinline__ void fill(const hilore_logit_rules &R, const RowPlan &p, int V, int v0, int width, int form, bool follow, bool sorted,
@@ -341,6 +337,8 @@ template <int BITS> struct Listed {
     {
         const int tid = threadIdx.x, bits = ((width + 127) >> 7) * 4;
         const bool counts = p.q.history() || form == kBiased, clear = counts && !follow;
+        const int low = max(v0, 0);
+        const uint32_t span = (uint32_t)max(min(v0 + width, V) - low, 0); // tokens [low, low + span)
         int before = 0;
         if (clear || p.n_bias > 0) {
             __syncthreads(); // the row before is done with both
@@ -354,14 +352,16 @@ template <int BITS> struct Listed {
             if (p.n_bias > 0)
                 for (int i = tid; i < bits / 4; i += THREADS)
                     reinterpret_cast<uint4 *>(biased())[i] = make_uint4(0, 0, 0, 0);
+            if (tid == 0) *doubles = 0;
             __syncthreads();
             for (int64_t i = p.q.bias_lo + tid; i < p.q.bias_hi; i += THREADS) {
                 const int v = __ldg(R.bias_tokens + i), k = (int)(i - p.q.bias_lo);
-                const uint32_t s = (uint32_t)(v - v0);
-                const bool in = s < (uint32_t)width && (uint32_t)v < (uint32_t)V;
+                const int s = v - v0;
+                const bool in = (uint32_t)(v - low) < span;
                 if (form != kBiased) {
                     bias_v()[k] = in ? v : -1;
-                    if (in) atomicOr(biased() + (s >> 5), 1u << (s & 31));
+                    bias_x()[k] = __ldg(R.bias_values + i);
+                    if (in && (atomicOr(biased() + (s >> 5), 1u << (s & 31)) >> (s & 31) & 1u)) atomicOr(doubles, 1u);
                 } else if (in) {
                     atomicMax(word() + 2 * s + 1, (uint32_t)k + 1u);
                     atomicOr(touch() + (s >> 5), 1u << (s & 31));
@@ -374,10 +374,10 @@ template <int BITS> struct Listed {
                 __syncthreads();
             }
             for (int i = tid; i < p.fresh; i += THREADS) {
-                const int v = __ldg(p.from + i);
-                const uint32_t s = (uint32_t)(v - v0), bit = 1u << (s & 31);
-                if (s >= (uint32_t)width || (uint32_t)v >= (uint32_t)V)
+                const int v = i < 4 ? p.first[i] : __ldg(p.from + i), s = v - v0;
+                if ((uint32_t)(v - low) >= span)
                     continue;
+                const uint32_t bit = 1u << (s & 31);
                 count(s, i < p.fresh_prompt, form);
                 if (!(atomicOr(touch() + (s >> 5), bit) & bit)) {
                     const int at = atomicAdd(n, 1);
@@ -396,10 +396,10 @@ template <int BITS> struct Listed {
                     v[u] = u * THREADS + tid < here ? __ldg(from + u * THREADS + tid) : -1;
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    const uint32_t s = (uint32_t)(v[u] - v0);
-                    if (s < (uint32_t)width && (uint32_t)v[u] < (uint32_t)V) {
-                        count(s, u * THREADS + tid < first, form);
+                    if ((uint32_t)(v[u] - low) < span) {
+                        const int s = v[u] - v0;
                         atomicOr(touch() + (s >> 5), 1u << (s & 31));
+                        count(s, u * THREADS + tid < first, form);
                     }
                 }
             }
@@ -408,7 +408,7 @@ template <int BITS> struct Listed {
         if (clear || (follow && sorted && *n > before + 1 && *n <= cap)) order<THREADS>(bits, list, cap);
     }
 
-    // Makes the list from the touch bits.  Ends with the CTA synchronised.
+    // Makes the list from the touch bits: a thread's words lie apart, as frequent tokens are neighbours.  Ends with the CTA synchronised.
     template <int THREADS> __device__ __forceinline__ void order(int bits, uint16_t *list, int cap) const
     {
         constexpr int W = (BITS + THREADS - 1) / THREADS;
@@ -417,7 +417,7 @@ template <int BITS> struct Listed {
         int own = 0;
 #pragma unroll
         for (int j = 0; j < W; ++j) {
-            w[j] = tid * W + j < bits ? touch()[tid * W + j] : 0u;
+            w[j] = tid + j * THREADS < bits ? touch()[tid + j * THREADS] : 0u;
             own += __popc(w[j]);
         }
         int at = own;
@@ -435,8 +435,35 @@ template <int BITS> struct Listed {
 #pragma unroll
         for (int j = 0; j < W; ++j)
             for (; w[j]; w[j] &= w[j] - 1, ++at)
-                if (at < cap) list[at] = (uint16_t)((tid * W + j) * 32 + __ffs((int)w[j]) - 1);
+                if (at < cap) list[at] = (uint16_t)((tid + j * THREADS) * 32 + __ffs((int)w[j]) - 1);
         __syncthreads();
+    }
+
+    // For every listed place: v = load(place), then use(place, v), with four loads of a thread in flight.  From the list where it is
+    // complete (a thread per entry), otherwise from the bits (a warp per word, the words dealt out one by one as frequent tokens are
+    // neighbours).  Either way a place goes to the same thread in every call.
+    template <int THREADS, typename Load, typename Use>
+    __device__ __forceinline__ void each(int n_listed, int width, const uint16_t *list, int cap, const Load &load, const Use &use) const
+    {
+        const bool whole = n_listed <= cap;
+        const int items = whole ? n_listed : (width + 31) & ~31;
+        for (int i0 = threadIdx.x; i0 < items; i0 += 1 * THREADS) {
+            int p[1];
+            decltype(load(0)) v[1];
+#pragma unroll
+            for (int u = 0; u < 1; ++u) {
+                const int i = i0 + u * THREADS;
+                p[u] = -1;
+                if (i < items) {
+                    if (whole) p[u] = list[i];
+                    else if (touch()[i >> 5] >> (i & 31) & 1u) p[u] = i;
+                }
+                if (p[u] >= 0) v[u] = load(p[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < 1; ++u)
+                if (p[u] >= 0) use(p[u], v[u]);
+        }
     }
 
     // Whether entry k of a short bias list is the last one that names its token (which bias_v has).
@@ -445,6 +472,8 @@ template <int BITS> struct Listed {
         const int v = bias_v()[k];
         if (v < 0)
             return false;
+        if (*doubles == 0)
+            return true;
         for (int j = k + 1; j < n_bias; ++j)
             if (bias_v()[j] == v)
                 return false;
@@ -478,17 +507,12 @@ __device__ __forceinline__ float slope_of(float x, uint32_t count, const RowRule
 // ------------------------------------------------------------------------------------------ element-wise results of a row
 // What all three element-wise calls share: out[v] = plain(in[v]) for every token, listed(...) for the listed ones, `off` where
 // the grammar denies.  One CTA per (row, range of `width` positions).
-constexpr int kMapThreads = 256;
 
 struct MapApply { // z from x
     static constexpr bool kGrad = false;
     float inv_temp;
-    template <int N> __device__ __forceinline__ void plain(float (&z)[N], int) const
-    {
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            z[i] *= inv_temp;
-    }
+    static constexpr int target = -1;
+    __device__ __forceinline__ float one(float in, bool) const { return in * inv_temp; }
     __device__ __forceinline__ float listed(float in, float, int, uint32_t c, float b, const RowRules &q) const
     {
         return adjusted(in, c, b, q) * inv_temp;
@@ -499,12 +523,8 @@ struct MapApply { // z from x
 struct MapApplyGrad { // dx from dz; x is read at listed tokens only (the side of zero they are on)
     static constexpr bool kGrad = true;
     float inv_temp;
-    template <int N> __device__ __forceinline__ void plain(float (&z)[N], int) const
-    {
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            z[i] *= inv_temp;
-    }
+    static constexpr int target = -1;
+    __device__ __forceinline__ float one(float in, bool) const { return in * inv_temp; }
     __device__ __forceinline__ float listed(float in, float x, int, uint32_t c, float, const RowRules &q) const
     {
         return in * slope_of(x, c, q) * inv_temp;
@@ -521,13 +541,6 @@ struct MapLogpGrad { // omega (1[v = a] - exp(z - lse)) dz/dx from x
         const float p = ex2_ftz(fmaf(z, inv_temp, -lse) * kLog2eF);
         return (hit ? 1.0f - p : -p) * scale;
     }
-    template <int N> __device__ __forceinline__ void plain(float (&z)[N], int f) const
-    {
-        const int at = target - f;
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            z[i] = one(z[i], i == at);
-    }
     __device__ __forceinline__ float listed(float in, float, int f, uint32_t c, float b, const RowRules &q) const
     {
         return one(adjusted(in, c, b, q), f == target) * slope_of(in, c, q);
@@ -535,36 +548,63 @@ struct MapLogpGrad { // omega (1[v = a] - exp(z - lse)) dz/dx from x
     static __device__ __forceinline__ float off() { return 0.0f; }
 };
 
-// 32 logits of every thread: the vectors of kMapThreads * 32 positions from `f0` on, in flight together.
-constexpr int kMapStage = kMapThreads * 32;
-template <typename T> struct Stage {
-    static constexpr int N = Lane<T>::N, U = 32 / N;
-    static constexpr uint32_t kAll = (1u << N) - 1u;
-    uint32_t w[U][8], deny[U];
-    template <bool SHIFTED>
-    __device__ __forceinline__ void load(const Row<T> &dst, const Source<T> &src, const uint32_t *mask, int n_words, int f0, int b)
-    {
+// Shapes of a CTA of THREADS threads.  A stage is 32 logits of every thread, in flight together.  Shared memory where tokens may be listed:
+// bits, bias entries, and a pool for the table, the list and -- where the output is the input and everything has to be read before
+// anything is stored -- the results of the listed tokens.  In that case a range is worked on as a whole where the row's lists cannot
+// outgrow what the pool leaves beside the table, otherwise in parts whose every token may be listed.
+//   hilore_logits_apply: 512 threads, two CTAs per SM (96 rows of 151936 fp32 logits, histories of up to 16384: 60 us; 70 with 256, three
+//   per SM).  The gradient of a log-probability holds more in registers: 256 (1500 x 32063 bf16 rows under prefixes 71 us; 94 with 512).
+template <int THREADS> struct MapShape {
+    static constexpr int kStage = THREADS * 32;
+    static constexpr int kRange = THREADS == 512 ? 2 * kStage : 3 * kStage; // positions of a CTA's range at most: a table of 16-bit counts
+    static constexpr int kBits = (kRange + kSlack + 127) / 128 * 4;
+    static constexpr int kPool = THREADS == 512 ? 40 * 512 : 31 * 512; // words
+    static constexpr int kCtas = THREADS == 512 ? 2 : 3;               // per SM
+    using Table = Listed<kBits>;
+    static constexpr size_t kShared = Table::kFixed + kPool * 4;
+    static __host__ __device__ constexpr int words(int form, int step) { return (table_words(form, step + kSlack) + 3) & ~3; }
+    static __host__ __device__ constexpr int capacity(int form, int step) { return (kPool - words(form, step)) * 4 / 6 & ~1; } // list and results
+    static __host__ __device__ constexpr int most(int form) { return form == kCount16 ? kRange : form == kCount32 ? kRange / 2 : kRange / 4; }
+    static __host__ __device__ constexpr int dense(int form) { return form == kCount16 ? 6144 : form == kCount32 ? 4864 : 3712; } // every token may be listed
+    static_assert(words(kCount16, most(kCount16)) <= kPool && words(kCount32, most(kCount32)) <= kPool && words(kBiased, most(kBiased)) <= kPool, "tables fit");
+};
+static_assert(MapShape<256>::capacity(kCount16, MapShape<256>::dense(kCount16)) >= MapShape<256>::dense(kCount16) + kSlack + kBiasCap &&
+                  MapShape<256>::capacity(kCount32, MapShape<256>::dense(kCount32)) >= MapShape<256>::dense(kCount32) + kSlack + kBiasCap &&
+                  MapShape<256>::capacity(kBiased, MapShape<256>::dense(kBiased)) >= MapShape<256>::dense(kBiased) + kSlack,
+              "lists of dense parts fit");
+constexpr int kApplyThreads = 512, kGradThreads = 256;
+constexpr uint32_t kNoResult = 0xFFFFFFFFu; // no result of an operation: NaNs are 0x7FFFFFFF
+
+// Positions [a, b) of a row as if no token were listed.
+template <int THREADS, typename T, bool SHIFTED, typename Map>
+__device__ __forceinline__ void map_vectors(const Row<T> &dst, const Source<T> &src, const Map &map, const uint32_t *mask, int n_words, int fa, int fb)
+{
+    constexpr int N = Lane<T>::N, U = 32 / N;
+    constexpr uint32_t kAll = (1u << N) - 1u;
+#pragma unroll 1
+    for (int f0 = fa + (int)threadIdx.x * N; f0 < fb; f0 += THREADS * 32) {
+        uint32_t w[U][8], deny[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int f = f0 + (u * kMapThreads + (int)threadIdx.x) * N;
-            deny[u] = f < b && mask ? denied<N>(mask, n_words, f - dst.lead) : 0u;
+            const int f = f0 + u * THREADS * N;
+            deny[u] = f < fb && mask ? denied<N>(mask, n_words, f - dst.lead) : 0u;
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int f = f0 + (u * kMapThreads + (int)threadIdx.x) * N;
-            if (f < b && deny[u] != kAll) src.template load<SHIFTED>(dst, f, w[u]); // a vector without an allowed token is not read
+            const int f = f0 + u * THREADS * N;
+            if (f < fb && deny[u] != kAll) src.template load<SHIFTED>(f, w[u]); // a vector without an allowed token is not read
         }
-    }
-    template <typename Map> __device__ __forceinline__ void store(const Row<T> &dst, const Map &map, int f0, int b)
-    {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int f = f0 + (u * kMapThreads + (int)threadIdx.x) * N;
-            if (f >= b)
+            const int f = f0 + u * THREADS * N;
+            if (f >= fb)
                 break;
             float z[N];
             Lane<T>::unpack(w[u], z);
-            map.plain(z, f);
+            const int at = map.target - f; // the target's place in this vector, if it is in it
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                z[i] = map.one(z[i], i == at);
             if (deny[u]) {
 #pragma unroll
                 for (int i = 0; i < N; ++i)
@@ -573,97 +613,117 @@ template <typename T> struct Stage {
             dst.store(f, z);
         }
     }
-};
+}
 
-// Shared memory of a CTA with listed tokens: bits, bias entries, and a pool for the table, the list and the results of the listed
-// tokens.  A range is worked on as a whole where the row's lists cannot outgrow what the pool leaves beside the table, otherwise in
-// parts whose every token may be listed.
-constexpr int kMapRange = 3 * kMapStage; // positions of a CTA's range at most: a table of 16-bit counts
-constexpr int kMapBits = (kMapRange + kSlack + 127) / 128 * 4;
-constexpr int kMapPool = 15 * 1024; // words
-constexpr int kMapDense = 7552;     // part whose every token may be listed, 16-bit counts
-using MapListed = Listed<kMapBits>;
-constexpr size_t kMapShared = MapListed::kFixed + kMapPool * 4;
-constexpr uint32_t kNoResult = 0xFFFFFFFFu; // no result of an operation: NaNs are 0x7FFFFFFF
-
-__host__ __device__ constexpr int map_table_words(int form, int step) { return (table_words(form, step + kSlack) + 3) & ~3; }
-__host__ __device__ constexpr int map_capacity(int form, int step) { return (kMapPool - map_table_words(form, step)) * 4 / 6 & ~1; } // of the list
-__host__ __device__ constexpr int map_dense(int form) { return form == kCount16 ? kMapDense : form == kCount32 ? 5888 : 4352; }
-static_assert(map_capacity(kCount16, map_dense(kCount16)) >= map_dense(kCount16) + kSlack && map_capacity(kCount32, map_dense(kCount32)) >= map_dense(kCount32) + kSlack &&
-                  map_capacity(kBiased, map_dense(kBiased)) >= map_dense(kBiased) + kSlack && map_capacity(kCount16, kMapRange) > 2000,
-              "sizes of tables and lists");
-
-// Positions [a, b) of a row without listed tokens.
-template <typename T, typename Map>
+template <int THREADS, typename T, typename Map>
 __device__ __forceinline__ void map_plain(const Row<T> &dst, const T *in, const Map &map, const uint32_t *mask, int V, int a, int b)
 {
     const Source<T> src(in, V, dst);
+    const typename Row<T>::Parts p = src.parts(dst, a, b);
     const int n_words = (V + 31) >> 5;
-    Stage<T> stage;
-    for (; a < b; a += kMapStage) {
-        if (src.shift == 0) stage.template load<false>(dst, src, mask, n_words, a, b);
-        else stage.template load<true>(dst, src, mask, n_words, a, b);
-        stage.store(dst, map, a, b);
+    if (src.shift == 0) map_vectors<THREADS, T, false>(dst, src, map, mask, n_words, p.fa, p.fb);
+    else map_vectors<THREADS, T, true>(dst, src, map, mask, n_words, p.fa, p.fb);
+    each_edge<THREADS>(p, [&](int f) {
+        const int v = f - dst.lead;
+        Lane<T>::put(dst.origin + f, is_denied(mask, v) ? Map::off() : map.one(Lane<T>::one(in + v), f == map.target));
+    });
+}
+
+// What the result of a listed token is made from; `ours`: it is this range's and allowed (otherwise the stream's result stays).
+struct Pick {
+    float in, x;
+    bool ours;
+};
+template <bool GRAD, typename T> __device__ __forceinline__ Pick pick(const T *in, const T *x, const uint32_t *mask, int v, int lead, int a, int e)
+{
+    Pick k{0.0f, 0.0f, v + lead >= a && v + lead < e};
+    if (k.ours) {
+        k.in = Lane<T>::one(in + v);
+        if (GRAD) k.x = Lane<T>::one(x + v);
+        k.ours = !is_denied(mask, v);
     }
+    return k;
 }
 
-// Result of listed token v as bits, or kNoResult where it is not this range's or denied.
-template <typename T, typename Map>
-__device__ __forceinline__ uint32_t listed_result(const Map &map, const T *in, const T *x, const RowRules &q, int v, int lead, int a, int e, uint32_t count,
-                                                  float bias)
+// Asks L2 for positions [a, b) of the row that `row` points to, as far as whole 16-byte pieces of them go.
+template <typename T> __device__ __forceinline__ void prefetch_range(const T *row, int V, int a, int b)
 {
-    const int f = v + lead;
-    if (f < a || f >= e || is_denied(q.mask, v))
-        return kNoResult;
-    const float other = Map::kGrad ? Lane<T>::one(x + v) : 0.0f;
-    return __float_as_uint(map.listed(Lane<T>::one(in + v), other, f, count, bias, q));
+    const Row<T> own(row, V);
+    const int lo = max(a, own.lead), hi = min(b, own.end);
+    if (hi <= lo)
+        return;
+    const uintptr_t first = (reinterpret_cast<uintptr_t>(own.origin + lo) + 15) & ~(uintptr_t)15, last = reinterpret_cast<uintptr_t>(own.origin + hi) & ~(uintptr_t)15;
+    if (last > first) prefetch_l2_bulk(reinterpret_cast<const void *>(first), (uint32_t)(last - first));
 }
 
-// Positions [a, b) of a row with listed tokens.  `in_place`: the output is the input.
-template <typename T, typename Map>
+// Positions [a, b) of a row that may have listed tokens.  `in_place`: the output is the input.
+template <int THREADS, typename T, typename Map>
 __device__ __forceinline__ void map_listed(const Row<T> &dst, const T *in, const T *x, const Map &map, const RowPlan &plan, const hilore_logit_rules &R,
-                                           int V, int a, int b, int range, bool in_place, const MapListed &t, uint32_t *bias_result, bool &intact)
+                                           int V, int a, int b, int range, bool in_place, const typename MapShape<THREADS>::Table &t, bool &intact)
 {
+    using Shape = MapShape<THREADS>;
     const RowRules &q = plan.q;
     const int tid = threadIdx.x, n_bias = plan.n_bias, form = plan.form, lead = dst.lead;
     const bool counts = q.history() || form == kBiased;
-    const int64_t most = q.hist_hi - q.hist_lo + (form == kBiased ? q.bias_hi - q.bias_lo : 0); // different tokens of the row at most
-    const int step = form == kCount16 && most <= map_capacity(kCount16, kMapRange) ? range : min(range, map_dense(form));
-    const int cap = map_capacity(form, step);
-    uint16_t *list = reinterpret_cast<uint16_t *>(t.word() + map_table_words(form, step));
-    uint32_t *result = t.word() + map_table_words(form, step) + cap / 2;
-    while (a < b) {
-        const int e = min(b, a + step), v0 = a - kSlack;
-        t.template fill<kMapThreads>(R, plan, V, v0, step + kSlack, form, plan.follows && intact && step == range, false, list, cap);
+    const int64_t most = q.hist_hi - q.hist_lo + q.bias_hi - q.bias_lo; // different tokens of the row at most
+    int step = min(range, Shape::most(form));
+    if (in_place && most > Shape::capacity(form, step)) step = min(step, Shape::dense(form));
+    const int cap = in_place ? Shape::capacity(form, step) : (Shape::kPool - Shape::words(form, step)) * 2; // without results the list has it all
+    uint16_t *list = reinterpret_cast<uint16_t *>(t.word() + Shape::words(form, step));
+    uint32_t *result = t.word() + Shape::words(form, step) + cap / 2;
+    T *row = dst.origin + lead;
+    for (; a < b; a += step) {
+        const int e = min(b, a + step), v0 = a - kSlack, width = step + kSlack;
+        if (q.listed()) t.template fill<THREADS>(R, plan, V, v0, width, form, plan.follows && intact && step == range, false, list, cap);
         const int n = counts ? *t.n : 0;
-        // Everything is read before anything is stored, as the output may be the input.
-        for (int i = tid; i < n; i += kMapThreads) {
-            const int p = list[i];
-            uint32_t r = kNoResult;
-            if (n_bias == 0 || !t.is_biased(p)) {
-                const float bias = form == kBiased ? bias_value(R, q, t.word()[2 * p + 1]) : 0.0f;
-                r = listed_result(map, in, x, q, v0 + p, lead, a, e, t.count_at(p, form), bias);
+        const auto load = [&](int p) { return pick<Map::kGrad>(in, x, q.mask, v0 + p, lead, a, e); };
+        const auto of_history = [&](int p, const Pick &k) {
+            const float bias = form == kBiased ? bias_value(R, q, t.word()[2 * p + 1]) : 0.0f;
+            return map.listed(k.in, k.x, v0 + p + lead, t.count_at(p, form), bias, q);
+        };
+        const auto of_bias = [&](int j, const Pick &k) {
+            const int v = t.bias_v()[j];
+            return map.listed(k.in, k.x, v + lead, counts ? t.count_of(v - v0, form) : 0u, t.bias_x()[j], q);
+        };
+        if (in_place) { // n entries and then those of the bias list: both fit, as `most` of them do
+            for (int i = tid; i < n; i += THREADS) {
+                const int p = list[i];
+                const Pick k = load(p);
+                const bool any = k.ours && !(n_bias > 0 && t.is_biased(p));
+                if (any) result[i] = __float_as_uint(of_history(p, k));
+                else list[i] = 0xFFFFu;
             }
-            result[i] = r;
-        }
-        for (int k = tid; k < n_bias; k += kMapThreads) {
-            uint32_t r = kNoResult;
-            if (t.counts_as_bias(k, n_bias)) {
-                const int v = t.bias_v()[k];
-                r = listed_result(map, in, x, q, v, lead, a, e, counts ? t.count_at(v - v0, form) : 0u, bias_value(R, q, (uint32_t)k + 1u));
+            for (int j = tid; j < n_bias; j += THREADS) {
+                const bool last = t.counts_as_bias(j, n_bias);
+                const Pick k = last ? load(t.bias_v()[j] - v0) : Pick{0.0f, 0.0f, false};
+                if (k.ours) result[n + j] = __float_as_uint(of_bias(j, k));
+                list[n + j] = k.ours ? 0u : 0xFFFFu;
             }
-            bias_result[k] = r;
+            __syncthreads();
+        } else if (Map::kGrad && n <= cap) {
+            for (int i = tid; i < n; i += THREADS)
+                prefetch_l2(x + max(v0 + (int)list[i], 0));
         }
-        if (in_place) __syncthreads();
-        map_plain(dst, in, map, q.mask, V, a, e);
+        map_plain<THREADS>(dst, in, map, q.mask, V, a, e);
+        if (!q.listed())
+            continue;
         __syncthreads(); // the stream's results of listed tokens are there to be written over
-        T *row = dst.origin + lead;
-        for (int i = tid; i < n; i += kMapThreads)
-            if (result[i] != kNoResult) Lane<T>::put(row + (v0 + (int)list[i]), __uint_as_float(result[i]));
-        for (int k = tid; k < n_bias; k += kMapThreads)
-            if (bias_result[k] != kNoResult) Lane<T>::put(row + t.bias_v()[k], __uint_as_float(bias_result[k]));
-        if (counts) intact = step == range && form != kBiased; // the table holds the last row with one, over the whole range
-        a += step;
+        if (in_place) {
+            for (int i = tid; i < n + n_bias; i += THREADS)
+                if (list[i] != 0xFFFFu) Lane<T>::put(row + (i < n ? v0 + (int)list[i] : t.bias_v()[i - n]), __uint_as_float(result[i]));
+            if (counts) intact = false; // its list has gaps
+        } else {
+            t.template each<THREADS>(n, width, list, cap, load, [&](int p, const Pick &k) {
+                if (k.ours && !(n_bias > 0 && t.is_biased(p))) Lane<T>::put(row + (v0 + p), of_history(p, k));
+            });
+            for (int j = tid; j < n_bias; j += THREADS)
+                if (t.counts_as_bias(j, n_bias)) {
+                    const Pick k = load(t.bias_v()[j] - v0);
+                    if (k.ours) Lane<T>::put(row + t.bias_v()[j], of_bias(j, k));
+                }
+            if (counts) intact = step == range && form != kBiased; // the table holds the last row with one, over the whole range
+        }
+        __syncthreads(); // the table may be changed
     }
 }
 
@@ -675,8 +735,8 @@ struct RowLoss { // of the gradient of a log-probability
 };
 
 // One CTA per (block of rows, range).  LISTS: rows may have listed tokens; otherwise a block is one row.
-template <typename T, bool GRAD, bool LISTS>
-__global__ void __launch_bounds__(kMapThreads, !LISTS && sizeof(T) == 2 ? 4 : 3)
+template <int THREADS, typename T, bool GRAD, bool LISTS>
+__global__ void __launch_bounds__(THREADS, LISTS ? MapShape<THREADS>::kCtas : sizeof(T) == 2 ? 1024 / THREADS : 768 / THREADS)
     logits_apply_kernel(const T *x, int64_t ld, const T *in, int64_t ld_in, T *out, int64_t ld_out, int64_t n_rows, int V, int block_rows, int n_ranges,
                         int width, const __grid_constant__ hilore_logit_rules R)
 {
@@ -687,36 +747,36 @@ __global__ void __launch_bounds__(kMapThreads, !LISTS && sizeof(T) == 2 ? 4 : 3)
         const Row<T> dst(out + row0 * ld_out, V);
         if (a >= dst.end)
             return;
-        if (GRAD) map_plain(dst, in + row0 * ld_in, MapApplyGrad{q.inv_temp}, q.mask, V, a, min(dst.end, a + width));
-        else map_plain(dst, in + row0 * ld_in, MapApply{q.inv_temp}, q.mask, V, a, min(dst.end, a + width));
+        if (GRAD) map_plain<THREADS>(dst, in + row0 * ld_in, MapApplyGrad{q.inv_temp}, q.mask, V, a, min(dst.end, a + width));
+        else map_plain<THREADS>(dst, in + row0 * ld_in, MapApply{q.inv_temp}, q.mask, V, a, min(dst.end, a + width));
         return;
     }
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ RowPlan plan[kBlockRows];
-    __shared__ uint32_t bias_result[kBiasCap], sums[kMapThreads / 32];
+    __shared__ uint32_t sums[THREADS / 32];
     __shared__ int count;
+    __shared__ uint32_t doubles;
     const int rows = (int)min((int64_t)block_rows, n_rows - row0);
     if ((int)threadIdx.x < rows) {
         plan[threadIdx.x].q = row_rules(R, row0 + threadIdx.x);
         plan[threadIdx.x].used = true;
     }
     plan_rows(plan, rows, R);
-    const MapListed t{smem, &count, sums};
+    const typename MapShape<THREADS>::Table t{smem, &count, &doubles, sums};
     bool intact = false;
     for (int i = 0; i < rows; ++i) {
         const RowRules &q = plan[i].q;
         const Row<T> dst(out + (row0 + i) * ld_out, V);
         const T *from = in + (row0 + i) * ld_in, *at = x + (row0 + i) * ld;
         const int b = min(dst.end, a + width);
+        if (threadIdx.x == 0) { // the next row's input while this one is worked on (of a masked row, only what is allowed is read)
+            if (i == 0 && q.mask == nullptr) prefetch_range(from, V, a, a + width);
+            if (i + 1 < rows && plan[i + 1].q.mask == nullptr) prefetch_range(from + ld_in, V, a, a + width);
+        }
         if (a >= b)
             continue;
-        if (!q.listed()) {
-            if (GRAD) map_plain(dst, from, MapApplyGrad{q.inv_temp}, q.mask, V, a, b);
-            else map_plain(dst, from, MapApply{q.inv_temp}, q.mask, V, a, b);
-        } else {
-            if (GRAD) map_listed(dst, from, at, MapApplyGrad{q.inv_temp}, plan[i], R, V, a, b, width, in == out, t, bias_result, intact);
-            else map_listed(dst, from, at, MapApply{q.inv_temp}, plan[i], R, V, a, b, width, in == out, t, bias_result, intact);
-        }
+        if (GRAD) map_listed<THREADS>(dst, from, at, MapApplyGrad{q.inv_temp}, plan[i], R, V, a, b, width, in == out, t, intact);
+        else map_listed<THREADS>(dst, from, at, MapApply{q.inv_temp}, plan[i], R, V, a, b, width, in == out, t, intact);
     }
 }
 
@@ -729,15 +789,18 @@ __device__ __forceinline__ RowLoss row_loss(const RowRules &q, const int32_t *ta
     return p;
 }
 
-template <typename T> __device__ __forceinline__ void zero_range(const Row<T> &dst, int a, int b)
+template <int THREADS, typename T> __device__ __forceinline__ void zero_range(const Row<T> &dst, int a, int b)
 {
     const float zero[Lane<T>::N] = {};
-    for (int f = a + (int)threadIdx.x * Lane<T>::N; f < b; f += kMapThreads * Lane<T>::N)
+    const typename Row<T>::Parts p = dst.parts(a, b);
+#pragma unroll 4
+    for (int f = p.fa + (int)threadIdx.x * Lane<T>::N; f < p.fb; f += THREADS * Lane<T>::N)
         dst.store(f, zero);
+    each_edge<THREADS>(p, [&](int f) { Lane<T>::put(dst.origin + f, 0.0f); });
 }
 
-template <typename T, bool LISTS>
-__global__ void __launch_bounds__(kMapThreads, !LISTS && sizeof(T) == 2 ? 4 : 3)
+template <int THREADS, typename T, bool LISTS>
+__global__ void __launch_bounds__(THREADS, LISTS ? MapShape<THREADS>::kCtas : sizeof(T) == 2 ? 1024 / THREADS : 768 / THREADS)
     token_logp_backward_kernel(const T *x, int64_t ld, int64_t n_rows, int V, int block_rows, int n_ranges, int width, const int32_t *targets,
                                const float *lse, const float *omega, T *grad, int64_t ld_grad, const __grid_constant__ hilore_logit_rules R)
 {
@@ -750,15 +813,16 @@ __global__ void __launch_bounds__(kMapThreads, !LISTS && sizeof(T) == 2 ? 4 : 3)
         if (a >= dst.end)
             return;
         const int b = min(dst.end, a + width);
-        if (p.live) map_plain(dst, x + row0 * ld, MapLogpGrad{q.inv_temp, p.lse, p.omega * q.inv_temp, p.target + dst.lead}, q.mask, V, a, b);
-        else zero_range(dst, a, b);
+        if (p.live) map_plain<THREADS>(dst, x + row0 * ld, MapLogpGrad{q.inv_temp, p.lse, p.omega * q.inv_temp, p.target + dst.lead}, q.mask, V, a, b);
+        else zero_range<THREADS>(dst, a, b);
         return;
     }
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ RowPlan plan[kBlockRows];
     __shared__ RowLoss losses[kBlockRows];
-    __shared__ uint32_t bias_result[kBiasCap], sums[kMapThreads / 32];
+    __shared__ uint32_t sums[THREADS / 32];
     __shared__ int count;
+    __shared__ uint32_t doubles;
     const int rows = (int)min((int64_t)block_rows, n_rows - row0);
     if ((int)threadIdx.x < rows) {
         const RowRules q = row_rules(R, row0 + threadIdx.x);
@@ -767,7 +831,7 @@ __global__ void __launch_bounds__(kMapThreads, !LISTS && sizeof(T) == 2 ? 4 : 3)
         plan[threadIdx.x].used = losses[threadIdx.x].live;
     }
     plan_rows(plan, rows, R);
-    const MapListed t{smem, &count, sums};
+    const typename MapShape<THREADS>::Table t{smem, &count, &doubles, sums};
     bool intact = false;
     for (int i = 0; i < rows; ++i) {
         const RowRules &q = plan[i].q;
@@ -775,12 +839,15 @@ __global__ void __launch_bounds__(kMapThreads, !LISTS && sizeof(T) == 2 ? 4 : 3)
         const Row<T> dst(grad + (row0 + i) * ld_grad, V);
         const T *from = x + (row0 + i) * ld;
         const int b = min(dst.end, a + width);
+        if (threadIdx.x == 0) {
+            if (i == 0 && p.live && q.mask == nullptr) prefetch_range(from, V, a, a + width);
+            if (i + 1 < rows && losses[i + 1].live && plan[i + 1].q.mask == nullptr) prefetch_range(from + ld, V, a, a + width);
+        }
         if (a >= b)
             continue;
         const MapLogpGrad map{q.inv_temp, p.lse, p.omega * q.inv_temp, p.target + dst.lead};
-        if (!p.live) zero_range(dst, a, b);
-        else if (!q.listed()) map_plain(dst, from, map, q.mask, V, a, b);
-        else map_listed(dst, from, from, map, plan[i], R, V, a, b, width, x == grad, t, bias_result, intact);
+        if (!p.live) zero_range<THREADS>(dst, a, b);
+        else map_listed<THREADS>(dst, from, from, map, plan[i], R, V, a, b, width, x == grad, t, intact);
     }
 }
 
@@ -909,29 +976,25 @@ __global__ void __launch_bounds__(kLogpThreads, 4)
     float z = 0.0f;
     if (rank == 0 && tid == 0) z = Lane<T>::one(x + row * ld + target);
     Soft acc{kLowest, 0.0f, 0.0f};
-    for (int f0 = a + tid * N; f0 < b; f0 += kLogpThreads * 32) {
+    const typename Row<T>::Parts p = src.parts(a, b);
+    for (int f0 = p.fa + tid * N; f0 < p.fb; f0 += kLogpThreads * 32) {
         uint32_t w[U][8];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int f = f0 + u * kLogpThreads * N;
-            if (f < b) src.load(f, w[u]);
+            if (f < p.fb) src.load(f, w[u]);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int f = f0 + u * kLogpThreads * N;
-            if (f < b) {
+            if (f < p.fb) {
                 float v[N];
                 Lane<T>::unpack(w[u], v);
-                if (!src.whole(f)) {
-                    const uint32_t ok = src.valid(f);
-#pragma unroll
-                    for (int i = 0; i < N; ++i)
-                        if (!(ok >> i & 1u)) v[i] = -INFINITY;
-                }
                 soft_add<N, ENTROPY>(acc, v, c);
             }
         }
     }
+    each_edge<kLogpThreads>(p, [&](int f) { soft_one<ENTROPY>(acc, Lane<T>::one(src.origin + f), c); });
     acc = warp_soft<ENTROPY>(acc, c);
     if ((tid & 31) == 0) part[tid >> 5] = acc;
     __syncthreads();
@@ -953,7 +1016,7 @@ __global__ void __launch_bounds__(kLogpThreads, 4)
 // Under rules.  A cluster of `row_ctas` CTAs (or one CTA) walks a block of consecutive rows; each CTA owns `width` positions of
 // every row, so that its table of counts serves one row after the other.  The statistics of every warp go to the first
 // CTA, which joins them when the block is done.
-constexpr int kLogpTokens = 20480; // tokens of a table of 16-bit counts at most: 8 CTAs take vocabularies up to 163712
+constexpr int kLogpTokens = 32768; // tokens of a table of 16-bit counts at most: 8 CTAs take vocabularies up to 163712
 constexpr int kLogpBits = kLogpTokens / 32 + 8, kLogpCap = 2048;
 using LogpListed = Listed<kLogpBits>;
 constexpr size_t kLogpFixed = LogpListed::kFixed; // bytes before the table; the list is in static shared memory
@@ -969,6 +1032,7 @@ __global__ void __launch_bounds__(kLogpThreads, sizeof(T) == 4 ? 3 : 4)
     __shared__ RowPlan plan[kBlockRows];
     __shared__ int targets_of[kBlockRows];
     __shared__ int count;
+    __shared__ uint32_t doubles;
     __shared__ uint16_t list[kLogpCap];
     __shared__ uint32_t sums[kLogpWarps];
     __shared__ Soft part[kBlockRows][kMaxRowCtas * kLogpWarps]; // in the first CTA: of all warps of the cluster
@@ -986,7 +1050,7 @@ __global__ void __launch_bounds__(kLogpThreads, sizeof(T) == 4 ? 3 : 4)
     }
     plan_rows(plan, rows, R);
     if (row_ctas > 1) cl.barrier_wait();
-    const LogpListed t{smem, &count, sums};
+    const LogpListed t{smem, &count, &doubles, sums};
     bool intact = false; // the table holds the last row with one, over the whole range
     Soft(*to_part)[kMaxRowCtas * kLogpWarps] = row_ctas > 1 ? cl.map_shared_rank(&part[0], 0) : &part[0];
     float *to_z = row_ctas > 1 ? cl.map_shared_rank(&target_z[0], 0) : &target_z[0];
@@ -1009,51 +1073,28 @@ __global__ void __launch_bounds__(kLogpThreads, sizeof(T) == 4 ? 3 : 4)
         Soft acc{kLowest, 0.0f, 0.0f};
         for (; a < b; a += step) {
             const int e = min(b, a + step), v0 = a - kSlack, ft = target + src.lead;
+            int n = 0;
             if (lists) {
                 __syncthreads(); // the last range or row is done with the table
                 const bool follow = plan[r].follows && intact && step == width;
                 t.template fill<kLogpThreads>(R, plan[r], V, v0, step + kSlack, form, follow, true, list, kLogpCap);
-                const int n = counts ? count : 0;
-                const bool whole = n <= kLogpCap; // the list is complete; otherwise every place of the table is asked
+                n = counts ? count : 0;
                 if (counts) intact = step == width && form != kBiased;
-                for (int i = tid; i < (whole ? n : counts ? step + kSlack : 0); i += kLogpThreads) {
-                    const int p = whole ? (int)list[i] : i, v = v0 + p, f = v + src.lead;
-                    const uint32_t k = t.count_at(p, form), j = form == kBiased ? t.word()[2 * p + 1] : 0u;
-                    if ((k | j) == 0 || f < a || f >= e || (n_bias > 0 && t.is_biased(p)))
-                        continue;
-                    const float z = is_denied(mask, v) ? -INFINITY : adjusted(Lane<T>::one(xrow + v), k, bias_value(R, q, j), q);
-                    if (v == target) to_z[r] = z;
-                    soft_one<ENTROPY>(acc, z, c);
-                }
-                for (int k = tid; k < n_bias; k += kLogpThreads)
-                    if (t.counts_as_bias(k, n_bias)) {
-                        const int v = t.bias_v()[k], f = v + src.lead;
-                        if (f < a || f >= e)
-                            continue;
-                        const float z = is_denied(mask, v) ? -INFINITY
-                                                           : adjusted(Lane<T>::one(xrow + v), counts ? t.count_at(v - v0, form) : 0u, bias_value(R, q, (uint32_t)k + 1u), q);
-                        if (v == target) to_z[r] = z;
-                        soft_one<ENTROPY>(acc, z, c);
-                    }
             }
             const bool touched = counts, biased = n_bias > 0;
-            if (tid == 0 && ft >= a && ft < e) {
-                const int p = target - v0;
-                if (!(touched && (t.touch()[p >> 5] >> (p & 31) & 1u)) && !(biased && t.is_biased(p)))
-                    to_z[r] = is_denied(mask, target) ? -INFINITY : Lane<T>::one(xrow + target);
-            }
-            for (int f0 = a + tid * N; f0 < e; f0 += kLogpThreads * 32) {
+            const typename Row<T>::Parts parts = src.parts(a, e);
+            for (int f0 = parts.fa + tid * N; f0 < parts.fb; f0 += kLogpThreads * 32) {
                 uint32_t w[U][8], off[U];
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     const int f = f0 + u * kLogpThreads * N;
-                    off[u] = f < e ? ~src.valid(f) & kAll : kAll;
-                    if (off[u] == kAll)
-                        continue;
-                    if (mask) off[u] |= denied<N>(mask, n_words, f - src.lead);
-                    const int p = f - src.lead - v0;
-                    if (touched) off[u] |= __funnelshift_r(t.touch()[p >> 5], t.touch()[(p >> 5) + 1], p & 31) & kAll;
-                    if (biased) off[u] |= __funnelshift_r(t.biased()[p >> 5], t.biased()[(p >> 5) + 1], p & 31) & kAll;
+                    off[u] = kAll;
+                    if (f < parts.fb) {
+                        const int p = f - src.lead - v0;
+                        off[u] = mask ? denied<N>(mask, n_words, f - src.lead) : 0u;
+                        if (touched) off[u] |= __funnelshift_r(t.touch()[p >> 5], t.touch()[(p >> 5) + 1], p & 31) & kAll;
+                        if (biased) off[u] |= __funnelshift_r(t.biased()[p >> 5], t.biased()[(p >> 5) + 1], p & 31) & kAll;
+                    }
                 }
 #pragma unroll
                 for (int u = 0; u < U; ++u)
@@ -1071,6 +1112,38 @@ __global__ void __launch_bounds__(kLogpThreads, sizeof(T) == 4 ? 3 : 4)
                     }
                     soft_add<N, ENTROPY>(acc, z, c);
                 }
+            }
+            each_edge<kLogpThreads>(parts, [&](int f) {
+                const int p = f - src.lead - v0;
+                if (is_denied(mask, f - src.lead) || (touched && (t.touch()[p >> 5] >> (p & 31) & 1u)) || (biased && t.is_biased(p)))
+                    return;
+                soft_one<ENTROPY>(acc, Lane<T>::one(src.origin + f), c);
+            });
+            // listed tokens after the stream: most of them are in L2 by now
+            const auto load = [&](int p) { return pick<false>(xrow, xrow, mask, v0 + p, src.lead, a, e); };
+            t.template each<kLogpThreads>(n, step + kSlack, list, kLogpCap, load, [&](int p, const Pick &k) {
+                const int v = v0 + p;
+                if (v + src.lead < a || v + src.lead >= e || (biased && t.is_biased(p)))
+                    return;
+                const float bias = form == kBiased ? bias_value(R, q, t.word()[2 * p + 1]) : 0.0f;
+                const float z = k.ours ? adjusted(k.in, t.count_at(p, form), bias, q) : -INFINITY;
+                if (v == target) to_z[r] = z;
+                soft_one<ENTROPY>(acc, z, c);
+            });
+            for (int j = tid; j < n_bias; j += kLogpThreads)
+                if (t.counts_as_bias(j, n_bias)) {
+                    const int v = t.bias_v()[j];
+                    if (v + src.lead < a || v + src.lead >= e)
+                        continue;
+                    const Pick k = load(v - v0);
+                    const float z = k.ours ? adjusted(k.in, counts ? t.count_of(v - v0, form) : 0u, t.bias_x()[j], q) : -INFINITY;
+                    if (v == target) to_z[r] = z;
+                    soft_one<ENTROPY>(acc, z, c);
+                }
+            if (tid == 0 && ft >= a && ft < e) {
+                const int p = target - v0;
+                if (!(touched && (t.touch()[p >> 5] >> (p & 31) & 1u)) && !(biased && t.is_biased(p)))
+                    to_z[r] = is_denied(mask, target) ? -INFINITY : Lane<T>::one(xrow + target);
             }
         }
         acc = warp_soft<ENTROPY>(acc, c);
@@ -1152,24 +1225,44 @@ template <typename K> static bool allow_smem(K kernel, size_t bytes)
 
 static bool has_lists(const hilore_logit_rules &q) { return q.tokens || q.bias_tokens; }
 
-// Work split of the element-wise calls.  Where rows may have listed tokens: ranges of one table, and blocks of up to eight rows
-// that share it as far as four rounds of CTAs remain.  Otherwise: one row, ranges of two stages.  Either way shorter ranges while SMs are
-// left without four CTAs.
+// Work split.  A CTA takes a block of rows and a range of positions; its time is taken as proportional to
+// rows * (positions + per-row overhead) + start, the start being the scan of a history, and the split is the one with the least number of
+// rounds times that.  Overheads in positions, from fits to measured times.
 struct Split {
     int64_t block_rows, width, n_ranges, grid;
 };
-static Split map_split(int64_t n_rows, int64_t V, const hilore_logit_rules &R, bool lists)
+static Split best_split(int64_t n_rows, int64_t positions, int64_t slots, int max_block, int64_t max_width, int64_t min_width, int64_t per_row, int64_t start)
 {
-    const int64_t sms = sm_count();
-    Split p{1, lists ? kMapRange : 2 * kMapStage, 0, 0};
-    if (lists && R.n_tokens / n_rows > map_capacity(kCount16, kMapRange)) p.width = kMapDense; // long histories of their own
-    const auto ranges = [&] { return (V + 15 + p.width - 1) / p.width; };
+    Split best{1, max_width, 0, 0};
+    double least = 1e300;
+    for (int64_t n = (positions + max_width - 1) / max_width; n <= (positions + min_width - 1) / min_width && n <= 4096; n += n < 16 ? 1 : n / 8) {
+        const int64_t width = ((positions + n - 1) / n + 127) / 128 * 128, ranges = (positions + width - 1) / width;
+        for (int b = 1; b <= max_block && b <= n_rows; ++b) {
+            const int64_t grid = (n_rows + b - 1) / b * ranges, rounds = (grid + slots - 1) / slots;
+            // the last round's CTAs run among fewer others
+            const double time = ((double)(rounds - 1) + 0.5 + 0.5 * (double)(grid - (rounds - 1) * slots) / (double)slots) * (double)(b * (width + per_row) + start);
+            if (time < least) {
+                least = time;
+                best = Split{b, width, ranges, grid};
+            }
+        }
+    }
+    return best;
+}
+
+template <int THREADS> static Split map_split(int64_t n_rows, int64_t V, const hilore_logit_rules &R, bool lists)
+{
+    const int64_t sms = sm_count(), positions = V + 15;
+    if (lists) {
+        const int64_t history = R.n_tokens / n_rows;
+        return best_split(n_rows, positions, MapShape<THREADS>::kCtas * sms, kBlockRows, MapShape<THREADS>::kRange, 2048, 8192, 8192 + (history < 65536 ? history : 65536));
+    }
+    Split p{1, 16384, 0, 0}; // one row, less of it while SMs are left without four CTAs
+    const auto ranges = [&] { return (positions + p.width - 1) / p.width; };
     while (p.width > 2048 && n_rows * ranges() < 4 * sms)
-        p.width = (p.width / 2 + 127) / 128 * 128;
+        p.width /= 2;
     p.n_ranges = ranges();
-    if (lists) p.block_rows = n_rows * p.n_ranges / (12 * sms);
-    p.block_rows = p.block_rows < 1 ? 1 : p.block_rows > kBlockRows ? kBlockRows : p.block_rows;
-    p.grid = (n_rows + p.block_rows - 1) / p.block_rows * p.n_ranges;
+    p.grid = n_rows * p.n_ranges;
     return p;
 }
 
@@ -1177,14 +1270,16 @@ template <typename T, bool GRAD, bool LISTS>
 static int launch_apply_as(const T *x, int64_t ld, const T *in, int64_t ld_in, T *out, int64_t ld_out, int64_t n_rows, int64_t V,
                            const hilore_logit_rules &R, cudaStream_t st)
 {
-    const Split p = map_split(n_rows, V, R, LISTS);
+    // Without listed tokens one CTA shape serves all.
+    constexpr int THREADS = LISTS ? kApplyThreads : kGradThreads;
+    const Split p = map_split<THREADS>(n_rows, V, R, LISTS);
     if (p.grid > 0x7FFFFFFF)
         return HILORE_SHAPE;
-    auto kernel = logits_apply_kernel<T, GRAD, LISTS>;
-    const size_t smem = LISTS ? kMapShared : 0;
+    auto kernel = logits_apply_kernel<THREADS, T, GRAD, LISTS>;
+    const size_t smem = LISTS ? MapShape<THREADS>::kShared : 0;
     if (!allow_smem(kernel, smem))
         return HILORE_CUDA;
-    kernel<<<(unsigned)p.grid, kMapThreads, smem, st>>>(x, ld, in, ld_in, out, ld_out, n_rows, (int)V, (int)p.block_rows, (int)p.n_ranges, (int)p.width, R);
+    kernel<<<(unsigned)p.grid, THREADS, smem, st>>>(x, ld, in, ld_in, out, ld_out, n_rows, (int)V, (int)p.block_rows, (int)p.n_ranges, (int)p.width, R);
     return cudaGetLastError() == cudaSuccess ? HILORE_OK : HILORE_CUDA;
 }
 
@@ -1243,15 +1338,14 @@ static int launch_logp(const T *x, int64_t ld, int64_t n_rows, int64_t V, const 
     int k = row_ctas_for(n_rows, V);
     if (!more_than_temperature(R))
         return launch_rows(token_logp_kernel<T, ENTROPY>, n_rows * k, k, 0, st, x, ld, (int)V, k, targets, logp, lse, entropy, R.temperature);
-    // Enough CTAs for a row that a table of 16-bit counts takes a share of it; blocks of rows while a round of CTAs remains.
+    // Enough CTAs for a row that a table of 16-bit counts takes a share of it.
     if (clusters_on() && has_lists(R))
         while (k < kMaxRowCtas && V / k > kLogpTokens - 256)
             k *= 2;
     const int64_t width = ((V + 15 + k - 1) / k + 127) / 128 * 128;
-    int64_t words = width + kSlack; // at least two words for 128 tokens and the slack, the narrowest part of a range
+    int64_t words = (width + kSlack) / 2; // 16-bit counts; at least two words for 128 tokens and the slack, the narrowest part of a range
     words = words < 512 ? 512 : words > kLogpTokens / 2 ? kLogpTokens / 2 : (words + 3) & ~(int64_t)3;
-    int64_t block = n_rows * k / (4 * (int64_t)sm_count());
-    block = block < 1 || !has_lists(R) ? 1 : block > kBlockRows ? kBlockRows : block;
+    const int64_t block = has_lists(R) ? best_split(n_rows, width * k, 3 * (int64_t)sm_count(), kBlockRows, width, width, 8192, 8192).block_rows : 1;
     const int64_t grid = (n_rows + block - 1) / block * k;
     const size_t smem = has_lists(R) ? kLogpFixed + (size_t)words * 4 : 0;
     return launch_rows(token_logp_rules_kernel<T, ENTROPY>, grid, k, smem, st, x, ld, n_rows, (int)V, (int)block, k, (int)width, (int)words, targets, logp,
@@ -1262,14 +1356,15 @@ template <typename T, bool LISTS>
 static int launch_logp_backward_as(const T *x, int64_t ld, int64_t n_rows, int64_t V, const int32_t *targets, const float *lse, const float *omega,
                                    T *grad, int64_t ld_grad, const hilore_logit_rules &R, cudaStream_t st)
 {
-    const Split p = map_split(n_rows, V, R, LISTS);
+    constexpr int THREADS = kGradThreads;
+    const Split p = map_split<THREADS>(n_rows, V, R, LISTS);
     if (p.grid > 0x7FFFFFFF)
         return HILORE_SHAPE;
-    auto kernel = token_logp_backward_kernel<T, LISTS>;
-    const size_t smem = LISTS ? kMapShared : 0;
+    auto kernel = token_logp_backward_kernel<THREADS, T, LISTS>;
+    const size_t smem = LISTS ? MapShape<THREADS>::kShared : 0;
     if (!allow_smem(kernel, smem))
         return HILORE_CUDA;
-    kernel<<<(unsigned)p.grid, kMapThreads, smem, st>>>(x, ld, n_rows, (int)V, (int)p.block_rows, (int)p.n_ranges, (int)p.width, targets, lse, omega, grad,
+    kernel<<<(unsigned)p.grid, THREADS, smem, st>>>(x, ld, n_rows, (int)V, (int)p.block_rows, (int)p.n_ranges, (int)p.width, targets, lse, omega, grad,
                                                        ld_grad, R);
     return cudaGetLastError() == cudaSuccess ? HILORE_OK : HILORE_CUDA;
 }
