@@ -311,3 +311,49 @@ def test_a_tensor_beyond_2_31_elements():
         q = p[a:a + 512].float()
         assert torch.allclose(q, -0.5 * torch.sign(x.float()), rtol=2.0 ** -8)               # the first step is lr * sign(g)
     assert int((p != 0).sum()) == sum(int((x != 0).sum()) for x in vals)
+
+
+@pytest.mark.parametrize("shift", [0, 1], ids=["vectors", "elements"])
+def test_roots_of_eight_bit_states_are_rounded_once(shift):
+    """One gradient per block, beta2 = 1/2, no state before: v = fl(fl(g / 2) g) and v_scale = fl(root / 448).  A root of relative
+    error 2^-22.9 (the approximation's bound) after one Newton step is off by 2^-43 before it is rounded."""
+    blocks = 1 << 18
+    n = blocks * 64
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    g = torch.zeros(n, device="cuda")
+    some = torch.exp2(torch.rand(blocks, generator=gen, device="cuda") * 2 - 5) * torch.exp2(torch.randint(-40, 20, (blocks,), generator=gen, device="cuda").float())
+    at = torch.arange(blocks, device="cuda") * 64 + torch.arange(blocks, device="cuda") % 64
+    g[at] = some
+    p = torch.zeros(n + shift, device="cuda")[shift:]              # off the vectors' alignment: element by element
+    code = lambda: torch.zeros(n, dtype=torch.uint8, device="cuda")
+    e = dict(p=p, g=g, m=code(), v=code(), m_scale=torch.zeros(blocks, device="cuda"), v_scale=torch.zeros(blocks, device="cuda"))
+    dev, host = api.make_param_table([e])
+    api.hilore_adamw_step(dev, host, 1, 1.0, None, 0.5, 0.5, 1e-8, 1, None, None)
+    x = some.cpu().numpy()
+    v = (x * np.float32(0.5) * x).astype(np.float64)                                 # both products rounded to fp32
+    exact = np.sqrt(v)
+    ulp = np.spacing(exact.astype(np.float32)).astype(np.float64)
+    lo, hi = exact - ulp / 2 - exact * 2.0 ** -43, exact + ulp / 2 + exact * 2.0 ** -43
+    c = np.float64(np.float32(1 / 448))
+    got = e["v_scale"].cpu().numpy()
+    assert ((got >= (lo * c).astype(np.float32)) & (got <= (hi * c).astype(np.float32))).all()
+    assert bool((e["v"][at] == 0x7E).all()) and int((e["v"] != 0).sum()) == blocks   # 448, and nothing else
+
+
+@pytest.mark.parametrize("shift", [0, 1], ids=["vectors", "elements"])
+@pytest.mark.parametrize("state", [32, 8])
+def test_moments_round_every_operation(state, shift):
+    """Moments of fp32 states, and the scales of 8-bit ones, have the bits of operation-by-operation evaluation in fp32."""
+    f = np.float32
+    rng = np.random.default_rng(1)
+    x = Tensor(rng, 64 * 3000, "f32", "f32", state, shift=shift)
+    m0 = x.m if state == 32 else R.E4M3[x.m].astype(f) * np.repeat(x.ms, 64)
+    v0 = x.v if state == 32 else (R.E4M3[x.v].astype(f) * np.repeat(x.vs, 64)) ** 2
+    b1, b2, a1, a2 = f(HYPER["b1"]), f(HYPER["b2"]), f(1 - HYPER["b1"]), f(1 - HYPER["b2"])
+    m, v = b1 * m0 + a1 * x.g, b2 * v0 + a2 * x.g * x.g
+    assert m.dtype == v.dtype == f
+    step([x])
+    if state == 32:
+        assert np.array_equal(x.get("m"), m) and np.array_equal(x.get("v"), v)
+    else:
+        assert np.array_equal(x.get("ms"), np.abs(m).reshape(-1, 64).max(1) * f(1 / 448))
