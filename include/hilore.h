@@ -453,11 +453,12 @@ typedef struct hilore_logit_rules {
  * microbatch), and the gradient of that: grad_in = grad_out * dz/dx, with dz/dx = 1 / temperature, times 1 / repetition
  * (x > 0) or repetition (x <= 0) for a token of the history, and 0 for a denied one (whatever grad_out holds there).
  *   logits       [n_rows, ld] of dtype (HILORE_BF16 or HILORE_F32), ld >= V: any ld and any address that the element
- *                type allows; 32-byte aligned rows of equal alignment on both sides are the fast case.
- *   out          [n_rows, ld_out] of the same type; may be `logits` itself with the same ld.
- *   grad_out, grad_in   [n_rows, ld_..] of the same type; grad_in may be grad_out with the same ld.  Of `logits` only
- *                the entries of history tokens are read.
- *   Limits: V and n_rows below 2^31 - 2^16, and n_rows * ceil(V / 8192) below 2^31 (HILORE_SHAPE).
+ *                type allows; rows whose addresses agree modulo 32 bytes with those of the output are the fast case.
+ *   out          [n_rows, ld_out] of the same type; may be `logits` itself with the same ld (HILORE_SHAPE if they differ).
+ *   grad_out, grad_in   [n_rows, ld_..] of the same type; grad_in may be grad_out with the same ld, but not `logits`
+ *                (HILORE_INVALID_ARG).  Of `logits` only the entries of history tokens are read.
+ *   Otherwise the output must not overlap an input.  Nothing is read or written between the rows.
+ *   Limits: V and n_rows at most 2^31 - 2^16, and n_rows * ceil((V + 15) / 2048) below 2^31 (HILORE_SHAPE).
  */
 int hilore_logits_apply(const void *logits, int32_t dtype, int64_t n_rows, int64_t V, int64_t ld,
                         const hilore_logit_rules *rules, void *out, int64_t ld_out, void *stream);
@@ -482,7 +483,7 @@ int hilore_logits_apply_backward(const void *logits, int32_t dtype, int64_t n_ro
  *
  * hilore_token_logp_backward: grad_v = omega_r (1[v = a] - exp(z_v - lse_r)) dz_v/dx_v, the gradient of sum_r omega_r
  * logp_r with respect to the logits, for the omega of hilore_grpo_coeffs.
- *   omega, lse   [n_rows] fp32.    grad  [n_rows, ld_grad] of dtype; may be `logits` with the same ld.
+ *   omega, lse   [n_rows] fp32.    grad  [n_rows, ld_grad] of dtype; may be `logits` with the same ld (HILORE_SHAPE if they differ).
  *   Rows with omega = 0, without a token, with a denied target or with lse <= -1e30 (nothing to choose from) get zeros
  *   and are not read.
  */
@@ -538,7 +539,8 @@ size_t hilore_grad_norm_workspace_bytes(void);
  *     hilore_compress (amax over finite elements, RNE; zeros and what is too small to be scaled get scale 1), with
  *     scale = fl32(amax * fl32(1 / 448)) and inv = fl32(448 * fl32(1 / amax)), and one addition: a positive sqrt(v)
  *     that would round to zero takes the smallest code, so that a later step never divides by eps alone where a
- *     gradient has been.  Codes and scales of a first step are zeros.
+ *     gradient has been.  v below 2^-126 counts as zero, and so does an eps below that.  Codes and scales of a first step
+ *     are zeros.
  *   params_dev, params_host   the table, as for hilore_plan_apply: [n_params] on the device and the same on the host
  *             (read during the call for validation and launch sizing).  Tensors may be of different types, sizes and
  *             state formats.  Any alignment that the types allow; tensors whose p, master and g are 32-byte aligned and

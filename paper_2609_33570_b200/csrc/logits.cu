@@ -6,12 +6,13 @@
 // off that stream.  A CTA owns a range of the vocabulary and walks a block of consecutive rows.  It keeps the tokens of the
 // row's history in a table of counts in shared memory, with a list of those that occur.  The slots of a training sequence
 // have growing prefixes of one sequence as their histories: going to the next row then adds a token or two to the table
-// where a first version cleared it and scanned the history again (gradients of 2048 x 128256 bf16 rows under prefixes of up
-// to 1536 tokens 301 us).  The stream runs as if no token were listed; the listed ones are worked out on their own,
-// one per thread, and written over the stream's results or, where a sum is wanted, left out of the stream by one bit per
-// token.  (Counts in global memory would cost 4 bytes per logit, twice the bf16 logits themselves.  Asking the table inside
-// the stream serialises a warp over its listed tokens: 329 us.  A hash table over a larger range needs fewer scans but probes and
-// overflows: 96 rows of 151936 fp32 logits with histories up to 16384 took 320 us, 111 with the table asked in the stream.)
+// instead of clearing it and scanning the history again (gradient of 2048 x 128256 bf16 rows under prefixes of up
+// to 1536 tokens: 245 us, 301 with a scan per row; the bytes alone 163).  The stream runs as if no token were listed; the listed
+// ones are worked out on their own, one per thread, and written over the stream's results or, where a sum is wanted, left out of
+// the stream by one bit per token.  Other ways: counts asked for inside the stream, where a warp takes its listed tokens one
+// by one, took 930 us for that gradient; a hash table over a larger range, which probes and overflows, 320 us for 96 rows of 151936
+// fp32 logits with histories of up to 16384 tokens, now 60 (the bytes 19).  Counts in global memory would cost 4 bytes per
+// logit, twice the bf16 logits themselves.
 #include "common.cuh"
 
 #include <cooperative_groups.h>
@@ -125,7 +126,7 @@ template <int THREADS, typename P, typename F> __device__ __forceinline__ void e
 
 // Reads of a row in the frame of another one (the row that is written).  Where the two addresses differ modulo 32 bytes, a
 // vector is put together from two neighbouring aligned ones by a shift of whole words and, for bf16, of half a word; the
-// second one hits L1.  (Element-wise stores instead, as a first version had, took 8.6 times as long as the bytes.)
+// second one hits L1.  (Element-wise stores instead took 8.6 times as long as the bytes.)
 template <typename T> struct Source {
     const T *exact;   // exact + f is the element of position f
     const T *aligned; // aligned + f starts the aligned vector of the read row that holds it, `shift` elements earlier
@@ -439,30 +440,18 @@ template <int BITS> struct Listed {
         __syncthreads();
     }
 
-    // For every listed place: v = load(place), then use(place, v), with four loads of a thread in flight.  From the list where it is
-    // complete (a thread per entry), otherwise from the bits (a warp per word, the words dealt out one by one as frequent tokens are
-    // neighbours).  Either way a place goes to the same thread in every call.
+    // For every listed place: v = load(place), then use(place, v).  From the list where it is complete (a thread per entry),
+    // otherwise from the bits (a thread per place).  Either way a place goes to the same thread in every call.  (Four or eight loads of a
+    // thread in flight were slower: the copies of `use` cost the stream more than the waits.)
     template <int THREADS, typename Load, typename Use>
     __device__ __forceinline__ void each(int n_listed, int width, const uint16_t *list, int cap, const Load &load, const Use &use) const
     {
         const bool whole = n_listed <= cap;
         const int items = whole ? n_listed : (width + 31) & ~31;
-        for (int i0 = threadIdx.x; i0 < items; i0 += 1 * THREADS) {
-            int p[1];
-            decltype(load(0)) v[1];
-#pragma unroll
-            for (int u = 0; u < 1; ++u) {
-                const int i = i0 + u * THREADS;
-                p[u] = -1;
-                if (i < items) {
-                    if (whole) p[u] = list[i];
-                    else if (touch()[i >> 5] >> (i & 31) & 1u) p[u] = i;
-                }
-                if (p[u] >= 0) v[u] = load(p[u]);
-            }
-#pragma unroll
-            for (int u = 0; u < 1; ++u)
-                if (p[u] >= 0) use(p[u], v[u]);
+#pragma unroll 1
+        for (int i = threadIdx.x; i < items; i += THREADS) {
+            const int p = whole ? list[i] : i;
+            if (whole || (touch()[i >> 5] >> (i & 31) & 1u)) use(p, load(p));
         }
     }
 
@@ -1016,7 +1005,7 @@ __global__ void __launch_bounds__(kLogpThreads, 4)
 // Under rules.  A cluster of `row_ctas` CTAs (or one CTA) walks a block of consecutive rows; each CTA owns `width` positions of
 // every row, so that its table of counts serves one row after the other.  The statistics of every warp go to the first
 // CTA, which joins them when the block is done.
-constexpr int kLogpTokens = 32768; // tokens of a table of 16-bit counts at most: 8 CTAs take vocabularies up to 163712
+constexpr int kLogpTokens = 32768; // tokens of a table of 16-bit counts at most: 8 CTAs take vocabularies up to 260000 in one part
 constexpr int kLogpBits = kLogpTokens / 32 + 8, kLogpCap = 2048;
 using LogpListed = Listed<kLogpBits>;
 constexpr size_t kLogpFixed = LogpListed::kFixed; // bytes before the table; the list is in static shared memory
@@ -1235,7 +1224,8 @@ static Split best_split(int64_t n_rows, int64_t positions, int64_t slots, int ma
 {
     Split best{1, max_width, 0, 0};
     double least = 1e300;
-    for (int64_t n = (positions + max_width - 1) / max_width; n <= (positions + min_width - 1) / min_width && n <= 4096; n += n < 16 ? 1 : n / 8) {
+    const int64_t fewest = (positions + max_width - 1) / max_width, most = (positions + min_width - 1) / min_width;
+    for (int64_t n = fewest; n <= most; n += n < 16 ? 1 : n / 8) {
         const int64_t width = ((positions + n - 1) / n + 127) / 128 * 128, ranges = (positions + width - 1) / width;
         for (int b = 1; b <= max_block && b <= n_rows; ++b) {
             const int64_t grid = (n_rows + b - 1) / b * ranges, rounds = (grid + slots - 1) / slots;
@@ -1399,6 +1389,8 @@ extern "C" int hilore_logits_apply(const void *logits, int32_t dtype, int64_t n_
     const size_t es = dtype == HILORE_BF16 ? 2 : 4;
     if (!aligned(logits, es) || !aligned(out, es))
         return HILORE_ALIGN;
+    if (out == logits && ld_out != ld && n_rows > 1)
+        return HILORE_SHAPE;
     const hilore_logit_rules R = used_rules(rules);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (dtype == HILORE_BF16) {
@@ -1428,6 +1420,10 @@ extern "C" int hilore_logits_apply_backward(const void *logits, int32_t dtype, i
     const size_t es = dtype == HILORE_BF16 ? 2 : 4;
     if (!aligned(logits, es) || !aligned(grad_out, es) || !aligned(grad_in, es))
         return HILORE_ALIGN;
+    if (grad_in == logits) // the side of zero that a listed logit is on would be lost
+        return HILORE_INVALID_ARG;
+    if (grad_in == grad_out && ld_grad_in != ld_grad_out && n_rows > 1)
+        return HILORE_SHAPE;
     const hilore_logit_rules R = used_rules(rules);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (dtype == HILORE_BF16)
@@ -1478,6 +1474,8 @@ extern "C" int hilore_token_logp_backward(const void *logits, int32_t dtype, int
     const size_t es = dtype == HILORE_BF16 ? 2 : 4;
     if (!aligned(logits, es) || !aligned(grad, es) || !aligned(targets, 4) || !aligned(lse, 4) || !aligned(omega, 4))
         return HILORE_ALIGN;
+    if (grad == logits && ld_grad != ld && n_rows > 1)
+        return HILORE_SHAPE;
     const hilore_logit_rules R = used_rules(rules);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
 #define HILORE_PICK(T)                                                                                                                          \

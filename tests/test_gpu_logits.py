@@ -401,3 +401,51 @@ def test_rows_beyond_32_bit_offsets():
         l = float(lse[i])
         got = to_f64(big[i * ld:i * ld + V].cpu().numpy().view(np.uint16))
         check(got, R.grad_row(z, k, t[i], 1.0, l), R.grad_bound(z, e, k, 1.0, l, 0.0), "bf16")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lists", [(9000, 60, False), (300, 1500, False), (5000, 0, True), (90000, 500, False), (0, 7, False)],
+                         ids=lambda l: "-".join(map(str, l)))
+def test_in_place_gives_the_bits_of_out_of_place(lists, dtype):
+    """Few and dense lists, short and long bias lists, and prefixes of one sequence, with a grammar beside them."""
+    history, bias, prefix = lists
+    rng = np.random.default_rng(history + bias)
+    rows, V = 9, 20011
+    kind, npt = DT[dtype]
+    x, g = logits(rng, rows, V, V, dtype), logits(rng, rows, V, V, dtype)
+    r = make_rules(rng, rows, V, history=history, bias=bias, grammar="indexed", prefix=prefix)
+    h = device_rules(r)
+    t = G.dev(x)
+    api.hilore_logits_apply(t, kind, rows, V, V, h, t, V)
+    assert np.array_equal(to_f64(t.cpu().numpy().view(npt)), apply(x, V, r, dtype, V))
+    t = G.dev(g)
+    api.hilore_logits_apply_backward(G.dev(x), kind, rows, V, V, h, t, V, t, V)
+    assert np.array_equal(to_f64(t.cpu().numpy().view(npt)), apply(x, V, r, dtype, V, backward=g))
+    targets = rng.integers(0, V, rows).astype(np.int32)
+    _, lse, _ = run_logp(x, V, r, targets, dtype)
+    omega = rng.standard_normal(rows)
+    t = G.dev(x)
+    api.hilore_token_logp_backward(t, kind, rows, V, V, h, G.dev(targets), G.dev(lse.astype(np.float32)), G.dev(omega.astype(np.float32)), t, V)
+    assert np.array_equal(to_f64(t.cpu().numpy().view(npt)), run_grad(x, V, r, targets, lse, omega, dtype))
+
+
+def test_a_row_of_more_ranges_than_a_few_thousand():
+    """One row of 2^27 + 5 bf16 logits with three biased tokens: both ends of the row, and every range between them."""
+    V = (1 << 27) + 5
+    x = torch.randn(V, device="cuda").to(torch.bfloat16)
+    at = torch.tensor([0, 70000001, V - 1], dtype=torch.int32, device="cuda")
+    h = api.make_logit_rules(bias_tokens=at, bias_values=torch.tensor([1.0, 2.0, 4.0], device="cuda"),
+                             bias_offsets=torch.tensor([0, 3], device="cuda"))
+    y = torch.full_like(x, 7.0)
+    api.hilore_logits_apply(x, api.BF16, 1, V, V, h, y, V)
+    want = x.clone()
+    want[at.long()] = (x[at.long()].float() + torch.tensor([1.0, 2.0, 4.0], device="cuda")).to(torch.bfloat16)
+    assert torch.equal(y, want)
+    api.hilore_token_logp_backward(x, api.BF16, 1, V, V, h, torch.tensor([V - 1], dtype=torch.int32, device="cuda"),
+                                   torch.tensor([9.0], device="cuda"), torch.ones(1, device="cuda"), y, V)
+    z = x.float()
+    z[at.long()] += torch.tensor([1.0, 2.0, 4.0], device="cuda")
+    p = -(z - 9.0).exp_()
+    p[V - 1] += 1.0
+    # the rounding to bf16, and the exponent's fp32 error: |z - 9| < 32 at 2^-23, three roundings and the function's two units
+    assert bool(((y.float() - p).abs() <= p.abs() * (2.0 ** -8 + 2.0 ** -16) + 2.0 ** -22 + 1e-38).all())

@@ -155,6 +155,8 @@ def test_refusals_of_the_logit_calls(lib):
         assert call(ld_out=99) == api.SHAPE
         assert call(out=A + 1) == api.ALIGN
     assert apply_bw(g=None) == api.INVALID_ARG and apply_bw(ld_g=99) == api.SHAPE and apply_bw(g=A + 1) == api.ALIGN
+    assert apply(ld_out=101) == api.SHAPE and logp_bw(ld_out=101) == api.SHAPE             # in place, at another distance
+    assert apply_bw(g=2 * A) == api.INVALID_ARG and apply_bw(x=2 * A, ld_g=101) == api.SHAPE
     assert logp(t=None) == api.INVALID_ARG and logp(logp=None) == api.INVALID_ARG and logp(h=A + 1) == api.ALIGN
     assert logp_bw(lse=None) == api.INVALID_ARG and logp_bw(omega=None) == api.INVALID_ARG
     with pytest.raises(api.HiloreError, match="hilore_token_logp"):
