@@ -539,8 +539,8 @@ size_t hilore_grad_norm_workspace_bytes(void);
  *     hilore_compress (amax over finite elements, RNE; zeros and what is too small to be scaled get scale 1), with
  *     scale = fl32(amax * fl32(1 / 448)) and inv = fl32(448 * fl32(1 / amax)), and one addition: a positive sqrt(v)
  *     that would round to zero takes the smallest code, so that a later step never divides by eps alone where a
- *     gradient has been.  v below 2^-126 counts as zero, and so does an eps below that.  Codes and scales of a first step
- *     are zeros.
+ *     gradient has been.  v and each of its two terms count as zero below 2^-126, and so does an eps below that.  Codes
+ *     and scales of a first step are zeros.
  *   params_dev, params_host   the table, as for hilore_plan_apply: [n_params] on the device and the same on the host
  *             (read during the call for validation and launch sizing).  Tensors may be of different types, sizes and
  *             state formats.  Any alignment that the types allow; tensors whose p, master and g are 32-byte aligned and

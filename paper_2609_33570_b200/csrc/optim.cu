@@ -4,9 +4,9 @@
 // Both are streams of a few bytes and a few operations per element: HBM is the bound.  A warp owns a tile of 1024
 // consecutive elements of one tensor and finds that tensor by a 32-ary search over the table's `first` column (two
 // dependent loads for a thousand tensors), so tensors of any size share one launch without a map of tiles.
-// Measured: the norm of 900 M bf16 gradients 260 us (6.9 TB/s); their step with 8-bit moments 1637 us (10.25 bytes an element,
-// 5.6 TB/s: the arithmetic of decoding, root and encoding takes as many issue slots as the loads leave); a step with fp32 moments and
-// master copies over 11.2 GB 1845 us (6.1 TB/s).
+// Measured: the norm of 900 M bf16 gradients 267 us (6.7 TB/s); their step with 8-bit moments 1690 us (10.25 bytes an element,
+// 5.5 TB/s: some 40 operations per element fill two thirds of the issue slots; asynchronous copies of the next 512 elements into shared memory
+// changed nothing); a step with fp32 moments and master copies over 11.2 GB 1807 us (6.2 TB/s).
 #include "common.cuh"
 
 #include <cmath>
@@ -251,6 +251,15 @@ __device__ __forceinline__ void next_moments(const AdamStep &h, uint64_t g, uint
     v = f32x2_fma(f32x2_mul(both(h.b2), v), both(h.one), f32x2_mul(f32x2_mul(both(h.omb2), x), x));
 }
 
+// The same with minus v for the 8-bit states, which flush what is below 2^-126 on the way; `h` has b2 and omb2 negated.
+__device__ __forceinline__ void next_moments_negated(const AdamStep &h, uint64_t g, uint64_t &m, uint64_t &v)
+{
+    const uint64_t x = f32x2_mul(g, both(h.gscale));
+    m = f32x2_fma(f32x2_mul(both(h.b1), m), both(h.one), f32x2_mul(both(h.omb1), x));
+    const uint64_t a = f32x2_mul(both(h.b2), v), b = f32x2_mul(f32x2_mul(both(h.omb2), x), x);
+    asm("fma.rn.ftz.f32x2 %0, %1, %2, %3;" : "=l"(v) : "l"(a), "l"(both(h.one)), "l"(b));
+}
+
 __device__ __forceinline__ float rcp_approx(float x)
 {
     float r;
@@ -272,19 +281,19 @@ __device__ __forceinline__ uint64_t next_param2(const AdamStep &h, uint64_t p, u
     return f32x2_sub(p, f32x2_fma(both(h.lrwd), p, q));
 }
 
-// Square roots of a pair of v: Newton's step r + (v - r^2) / (2 r) from r = v * rsqrt(v), the residual formed exactly by a fused
-// operation: an error of 2^-43 is left before the final rounding.  v below 2^-126 counts as zero, Inf and NaN give NaN (the
-// caller takes __fsqrt_rn where a block holds one).  Two roots at a time in packed operations without a branch; with __fsqrt_rn for
-// each the arithmetic, not the bytes, bounds the 8-bit tiles.
-__device__ __forceinline__ uint64_t root2(uint64_t v)
+// Square roots of a pair of v from minus v (zero, or at least 2^-126 in size): Newton's step r - (r^2 - v) / (2 r) from
+// r = v * rsqrt(v), the residual formed exactly by a fused operation: an error of 2^-43 is left before the final rounding.
+// Inf and NaN need another way (__fsqrt_rn where a block holds one).  Two roots at a time in packed operations without a branch.
+__device__ __forceinline__ uint64_t root2(uint64_t minus_v)
 {
+    constexpr float kMost = 9.223372036854775808e18f; // 2^63, of 2^-126; of zero this instead of Inf
     float v0, v1, y0, y1;
-    f32x2_unpack(v, v0, v1);
-    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y0) : "f"(v0));
-    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y1) : "f"(v1));
-    const uint64_t y = f32x2_pack(v0 < 1.17549435e-38f ? 0.0f : y0, v1 < 1.17549435e-38f ? 0.0f : y1);
-    const uint64_t r = f32x2_mul(v, y), minus_h = f32x2_mul(y, both(-0.5f));
-    return f32x2_fma(f32x2_fma(r, r, f32x2_mul(v, both(-1.0f))), minus_h, r);
+    f32x2_unpack(minus_v, v0, v1);
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y0) : "f"(-v0));
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y1) : "f"(-v1));
+    const uint64_t y = f32x2_pack(fmaxf(-y0, -kMost), fmaxf(-y1, -kMost)); // minus 1 / sqrt(v)
+    const uint64_t r = f32x2_mul(minus_v, y);
+    return f32x2_fma(f32x2_fma(r, r, minus_v), f32x2_mul(y, both(0.5f)), r);
 }
 
 __device__ __forceinline__ uint64_t decode2(uint32_t codes, float s) // two codes in the low half
@@ -351,30 +360,37 @@ __device__ __forceinline__ BlockScale block_scale(float top)
 }
 
 // Codes of 16 values of a block.  ROOT: the values are square roots of v, of which a positive one is never rounded to zero (it
-// would turn the next step's division into one by eps) but takes the smallest code; words without a zero code, the usual
-// ones, skip the test of their four values.
+// would turn the next step's division into one by eps) but takes the smallest code; lanes without a zero code, the usual
+// ones, skip the test of their values.
 template <bool ROOT> __device__ __forceinline__ void encode16(const uint64_t (&x)[8], const BlockScale &s, uint32_t (&w)[4])
 {
+    uint32_t zeros = 0;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         float q[4];
         f32x2_unpack(f32x2_mul(x[2 * k], both(s.inv)), q[0], q[1]);
         f32x2_unpack(f32x2_mul(x[2 * k + 1], both(s.inv)), q[2], q[3]);
         w[k] = cvt_e4m3x4(q[0], q[1], q[2], q[3]);
-        if (ROOT && ((w[k] - 0x01010101u) & ~w[k] & 0x80808080u) && s.fits) {
+        if (ROOT) zeros |= (w[k] - 0x01010101u) & ~w[k];
+    }
+    if (ROOT && (zeros & 0x80808080u) && s.fits) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (q[i] > 0.0f && !(w[k] >> (8 * i) & 0xFFu)) w[k] |= 1u << (8 * i);
+        for (int k = 0; k < 8; ++k) {
+            float x0, x1;
+            f32x2_unpack(x[k], x0, x1);
+            const int at = 16 * (k & 1);
+            if (x0 > 0.0f && !(w[k >> 1] >> at & 0xFFu)) w[k >> 1] |= 1u << at;
+            if (x1 > 0.0f && !(w[k >> 1] >> (at + 8) & 0xFFu)) w[k >> 1] |= 1u << (at + 8);
         }
     }
 }
 
 // ---- whole tiles: vectors, types known at compile time ----
-template <int P, int G, bool MASTER, int LEN> __device__ __forceinline__ void tile_f32(const hilore_param &e, const AdamStep &h, int64_t base)
+template <int P, int G, bool MASTER> __device__ __forceinline__ void run_f32(const hilore_param &e, const AdamStep &h, int64_t base, int len)
 {
     const int lane = threadIdx.x & 31;
 #pragma unroll 1
-    for (int k = 0; k < LEN; k += 256) {
+    for (int k = 0; k < len; k += 256) {
         const int64_t i = base + k + lane * 8;
         Raw<G, 8> g;
         Raw<HILORE_F32, 8> m, v;
@@ -406,11 +422,12 @@ template <int P, int G, bool MASTER, int LEN> __device__ __forceinline__ void ti
 
 // The four lanes of a quad own one block of 64.  The moments of this step enter the update in fp32, before they are rounded
 // to codes; v holds the codes of sqrt(v), as the square root halves the range that the codes have to span.
-template <int P, int G, bool MASTER, int LEN> __device__ __forceinline__ void tile_e4m3(const hilore_param &e, const AdamStep &h, int64_t base)
+template <int P, int G, bool MASTER>
+__device__ __forceinline__ void run_e4m3(const hilore_param &e, const AdamStep &h, int64_t base, int len)
 {
     const int lane = threadIdx.x & 31;
 #pragma unroll 1
-    for (int t = 0; t < LEN; t += 512) {
+    for (int t = 0; t < len; t += 512) {
         const int64_t i = base + t + lane * 16;
         Raw<G, 16> g;
         Raw<MASTER ? HILORE_F32 : P, 16> p;
@@ -425,20 +442,25 @@ template <int P, int G, bool MASTER, int LEN> __device__ __forceinline__ void ti
             m[k] = decode2(mw[k >> 1] >> (16 * (k & 1)), ms);
             r[k] = decode2(rw[k >> 1] >> (16 * (k & 1)), rs);
             r[k] = f32x2_mul(r[k], r[k]);
-            next_moments(h, g.pair(2 * k), m[k], r[k]);
+            next_moments_negated(h, g.pair(2 * k), m[k], r[k]);
         }
         float am = quad_max(m), ar = quad_max(r); // of v: the root is monotone
         const bool odd = __any_sync(0xFFFFFFFFu, fmaxf(am, ar) == INFINITY);
+        if (odd) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                float v0, v1;
+                f32x2_unpack(r[k], v0, v1);
+                r[k] = f32x2_pack(__fsqrt_rn(-v0), __fsqrt_rn(-v1));
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                r[k] = root2(r[k]);
+        }
         Raw<P, 16> out;
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            if (odd) {
-                float v0, v1;
-                f32x2_unpack(r[k], v0, v1);
-                r[k] = f32x2_pack(__fsqrt_rn(v0), __fsqrt_rn(v1));
-            } else {
-                r[k] = root2(r[k]);
-            }
             float p0, p1;
             f32x2_unpack(next_param2(h, p.pair(2 * k), m[k], r[k]), p0, p1);
             if (MASTER) p.set2(2 * k, p0, p1);
@@ -451,7 +473,7 @@ template <int P, int G, bool MASTER, int LEN> __device__ __forceinline__ void ti
             ar = quad_max_finite(r);
         } else {
             float unused;
-            f32x2_unpack(root2(both(ar)), ar, unused);
+            f32x2_unpack(root2(both(-ar)), ar, unused);
         }
         const BlockScale sm = block_scale(am), sr = block_scale(ar);
         uint32_t w[4];
@@ -516,13 +538,15 @@ template <bool CODED, int P, int G, bool MASTER> __device__ __noinline__ void ti
                 vv = decode2(v[k][0] | v[k][1] << 8, rs[k]);
                 vv = f32x2_mul(vv, vv);
             }
-            next_moments(h, f32x2_pack(from_bits<G>(g[k][0]), from_bits<G>(g[k][1])), mm, vv);
+            const uint64_t gg = f32x2_pack(from_bits<G>(g[k][0]), from_bits<G>(g[k][1]));
+            if (CODED) next_moments_negated(h, gg, mm, vv);
+            else next_moments(h, gg, mm, vv);
             float m1[2], v1[2], r[2], q[2];
             f32x2_unpack(mm, m1[0], m1[1]);
             f32x2_unpack(vv, v1[0], v1[1]);
 #pragma unroll
             for (int u = 0; u < 2; ++u)
-                r[u] = CODED && v1[u] < 1.17549435e-38f ? 0.0f : __fsqrt_rn(v1[u]);
+                r[u] = __fsqrt_rn(CODED ? -v1[u] : v1[u]);
             const float p0 = from_bits<Q>(p[k][0]), p1 = from_bits<Q>(p[k][1]);
             if (CODED) {
                 f32x2_unpack(next_param2(h, f32x2_pack(p0, p1), mm, f32x2_pack(r[0], r[1])), q[0], q[1]);
@@ -570,20 +594,21 @@ template <bool CODED, int P, int G, bool MASTER> __device__ __noinline__ void ti
 constexpr int kMixed = 12;
 static int kind_of(const hilore_param &e) { return e.state * 6 + e.g_dtype * 3 + (e.master ? 2 : e.p_dtype); }
 
-template <int KIND, int LEN> __device__ __forceinline__ void tile_of_kind(const hilore_param &e, const AdamStep &h, int64_t base, bool vec)
+// Elements [base, base + len): whole tiles (or halves of one) in vectors, or single elements.
+template <int KIND>
+__device__ __forceinline__ void run_of_kind(const hilore_param &e, const AdamStep &h, int64_t base, int len, bool whole)
 {
     constexpr int G = KIND / 3 % 2, PK = KIND % 3;
     constexpr int P = PK == 1 ? HILORE_F32 : HILORE_BF16;
-    if (!vec || base + LEN > e.n) tile_ragged<KIND / 6 == HILORE_STATE_E4M3FN, P, G, PK == 2>(&e, h, base, LEN);
-    else if (KIND / 6 == HILORE_STATE_F32) tile_f32<P, G, PK == 2, LEN>(e, h, base);
-    else tile_e4m3<P, G, PK == 2, LEN>(e, h, base);
+    if (!whole) tile_ragged<KIND / 6 == HILORE_STATE_E4M3FN, P, G, PK == 2>(&e, h, base, len);
+    else if (KIND / 6 == HILORE_STATE_F32) run_f32<P, G, PK == 2>(e, h, base, len);
+    else run_e4m3<P, G, PK == 2>(e, h, base, len);
 }
 
-// Registers: 64 for 32-bit states and for all-bf16 tables with 8-bit ones (900 M elements 1.70 ms, 1.80 with 80 registers), 80 where
-// fp32 parameters or gradients are held beside 8-bit states (33 M elements 99.4 us, 101.6 with 64).
+// Registers: 64 for 32-bit states, 80 for 8-bit ones (900 M bf16 elements 1690 us, 1750 with 64).
 // SPLIT: warps per tile; two where there are few tiles, for the latency.
 template <int KIND, int SPLIT>
-__global__ void __launch_bounds__(kOptThreads, KIND == kMixed ? 2 : KIND <= 6 ? 4 : 3) adamw_kernel(const hilore_param *params, int n_params, int64_t n_tiles, int per_warp, AdamArgs a)
+__global__ void __launch_bounds__(kOptThreads, KIND == kMixed ? 2 : KIND <= 5 ? 4 : 3) adamw_kernel(const hilore_param *params, int n_params, int64_t n_tiles, int per_warp, AdamArgs a)
 {
     // From the last tile to the first: a norm taken just before has left the end of the gradients in L2.
     const int64_t w = (int64_t)(gridDim.x - 1 - blockIdx.x) * kOptWarps + (threadIdx.x >> 5), t0 = w / SPLIT * per_warp;
@@ -607,33 +632,40 @@ __global__ void __launch_bounds__(kOptThreads, KIND == kMixed ? 2 : KIND <= 6 ? 
         inv_bc1 = (float)(1.0 / -expm1(t * log(a.beta1)));
         h.rsqrt_bc2 = (float)rsqrt(-expm1(t * log(a.beta2)));
     }
-    h.b1 = a.b1, h.omb1 = a.omb1, h.b2 = a.b2, h.omb2 = a.omb2, h.eps = a.eps, h.one = a.one;
+    h.b1 = a.b1, h.omb1 = a.omb1, h.eps = a.eps, h.one = a.one;
     h.step = lr * inv_bc1;
     bool vec = false;
-    for (int64_t tile = t0; tile < min(t0 + per_warp, n_tiles); ++tile) {
+    const int64_t t1 = min(t0 + per_warp, n_tiles);
+    for (int64_t tile = t0; tile < t1;) {
         if (walk.at(tile) || (SPLIT > 1 && tile == t0)) {
             const uintptr_t wide = reinterpret_cast<uintptr_t>(e.p) | reinterpret_cast<uintptr_t>(e.g) | reinterpret_cast<uintptr_t>(e.master);
             const uintptr_t st = reinterpret_cast<uintptr_t>(e.m) | reinterpret_cast<uintptr_t>(e.v);
             vec = (wide & 31) == 0 && (st & (e.state == HILORE_STATE_F32 ? 31 : 15)) == 0;
             h.lrwd = lr * e.weight_decay;
+            const bool coded = (KIND < kMixed ? KIND / 6 : e.state) == HILORE_STATE_E4M3FN;
+            h.b2 = coded ? -a.b2 : a.b2;
+            h.omb2 = coded ? -a.omb2 : a.omb2;
         }
-        const int64_t base = (tile - walk.begin) * kTile + skip;
+        const int64_t base = (tile - walk.begin) * kTile;
+        const int tiles = vec ? (int)min((e.n - base) / kTile, t1 - tile) : 0; // whole ones of this entry
+        const int len = SPLIT > 1 ? kTile / SPLIT : max(tiles, 1) * kTile;
+        tile += max(tiles, 1);
         if (KIND < kMixed) {
-            tile_of_kind<KIND == kMixed ? 0 : KIND, kTile / SPLIT>(e, h, base, vec);
+            run_of_kind<KIND == kMixed ? 0 : KIND>(e, h, base + skip, len, tiles > 0);
         } else {
             switch (e.state * 6 + e.g_dtype * 3 + (e.master ? 2 : e.p_dtype)) {
-            case 0: tile_of_kind<0, kTile / SPLIT>(e, h, base, vec); break;
-            case 1: tile_of_kind<1, kTile / SPLIT>(e, h, base, vec); break;
-            case 2: tile_of_kind<2, kTile / SPLIT>(e, h, base, vec); break;
-            case 3: tile_of_kind<3, kTile / SPLIT>(e, h, base, vec); break;
-            case 4: tile_of_kind<4, kTile / SPLIT>(e, h, base, vec); break;
-            case 5: tile_of_kind<5, kTile / SPLIT>(e, h, base, vec); break;
-            case 6: tile_of_kind<6, kTile / SPLIT>(e, h, base, vec); break;
-            case 7: tile_of_kind<7, kTile / SPLIT>(e, h, base, vec); break;
-            case 8: tile_of_kind<8, kTile / SPLIT>(e, h, base, vec); break;
-            case 9: tile_of_kind<9, kTile / SPLIT>(e, h, base, vec); break;
-            case 10: tile_of_kind<10, kTile / SPLIT>(e, h, base, vec); break;
-            default: tile_of_kind<11, kTile / SPLIT>(e, h, base, vec); break;
+            case 0: run_of_kind<0>(e, h, base + skip, len, tiles > 0); break;
+            case 1: run_of_kind<1>(e, h, base + skip, len, tiles > 0); break;
+            case 2: run_of_kind<2>(e, h, base + skip, len, tiles > 0); break;
+            case 3: run_of_kind<3>(e, h, base + skip, len, tiles > 0); break;
+            case 4: run_of_kind<4>(e, h, base + skip, len, tiles > 0); break;
+            case 5: run_of_kind<5>(e, h, base + skip, len, tiles > 0); break;
+            case 6: run_of_kind<6>(e, h, base + skip, len, tiles > 0); break;
+            case 7: run_of_kind<7>(e, h, base + skip, len, tiles > 0); break;
+            case 8: run_of_kind<8>(e, h, base + skip, len, tiles > 0); break;
+            case 9: run_of_kind<9>(e, h, base + skip, len, tiles > 0); break;
+            case 10: run_of_kind<10>(e, h, base + skip, len, tiles > 0); break;
+            default: run_of_kind<11>(e, h, base + skip, len, tiles > 0); break;
             }
         }
     }
