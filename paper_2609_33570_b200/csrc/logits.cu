@@ -562,7 +562,6 @@ static_assert(MapShape<256>::capacity(kCount16, MapShape<256>::dense(kCount16)) 
                   MapShape<256>::capacity(kBiased, MapShape<256>::dense(kBiased)) >= MapShape<256>::dense(kBiased) + kSlack,
               "lists of dense parts fit");
 constexpr int kApplyThreads = 512, kGradThreads = 256;
-constexpr uint32_t kNoResult = 0xFFFFFFFFu; // no result of an operation: NaNs are 0x7FFFFFFF
 
 // Positions [a, b) of a row as if no token were listed.
 template <int THREADS, typename T, bool SHIFTED, typename Map>
@@ -869,24 +868,28 @@ template <int N, bool ENTROPY> __device__ __forceinline__ void soft_add(Soft &q,
     if (ENTROPY) q.t = e * fmaf(d, q.s, q.t);
     q.s *= e;
     q.m = m;
-    float s0 = 0.0f, s1 = 0.0f, t0 = 0.0f, t1 = 0.0f;
+    const uint64_t minus_m = f32x2_pack(-m, -m), cc = f32x2_pack(c, c);
+    uint64_t sum = 0, mean = 0; // of pairs
 #pragma unroll
     for (int i = 0; i < N; i += 2) {
-        float u0 = (z[i] - m) * c, u1 = (z[i + 1] - m) * c;
+        const uint64_t u = f32x2_mul(f32x2_add(f32x2_pack(z[i], z[i + 1]), minus_m), cc);
+        float u0, u1;
+        f32x2_unpack(u, u0, u1);
         if (ENTROPY) { // 2^-256 is zero in fp32: keeps -inf out of the product
             u0 = fmaxf(u0, -256.0f);
             u1 = fmaxf(u1, -256.0f);
         }
-        const float e0 = ex2_ftz(u0), e1 = ex2_ftz(u1);
-        s0 += e0;
-        s1 += e1;
-        if (ENTROPY) {
-            t0 = fmaf(e0, u0, t0);
-            t1 = fmaf(e1, u1, t1);
-        }
+        const uint64_t e2 = f32x2_pack(ex2_ftz(u0), ex2_ftz(u1));
+        sum = f32x2_add(sum, e2);
+        if (ENTROPY) mean = f32x2_fma(e2, f32x2_pack(u0, u1), mean);
     }
-    q.s += s0 + s1;
-    if (ENTROPY) q.t += t0 + t1;
+    float lo, hi;
+    f32x2_unpack(sum, lo, hi);
+    q.s += lo + hi;
+    if (ENTROPY) {
+        f32x2_unpack(mean, lo, hi);
+        q.t += lo + hi;
+    }
 }
 
 // Adds one logit.
