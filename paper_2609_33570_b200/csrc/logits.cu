@@ -942,7 +942,7 @@ __device__ __forceinline__ void finish_row(const Soft &acc, float z, float inv_t
 
 // Without rules beyond a temperature: one pass with the running maximum, sum and mean exponent of every thread, 32 logits in
 // flight, exponentials in base 2 relative to the maximum, differences and sums in packed pairs (three quarters of 8192 rows of 151936 bf16 logits with
-// entropy 312 us, 6.0 TB/s; 329 with scalar sums, as the exponentials alone take 207 us of their units).  A row belongs to `row_ctas` CTAs (a thread-block cluster if more than one); each takes a
+// entropy 300 us, 6.2 TB/s; the exponentials alone take 207 us of their units).  A row belongs to `row_ctas` CTAs (a thread-block cluster if more than one); each takes a
 // share of its vectors.
 template <typename T, bool ENTROPY>
 __global__ void __launch_bounds__(kLogpThreads, 4)
@@ -974,8 +974,13 @@ __global__ void __launch_bounds__(kLogpThreads, 4)
     if (rank == 0 && tid == 0) z = Lane<T>::one(x + row * ld + target);
     Soft acc{kLowest, 0.0f, 0.0f};
     const typename Row<T>::Parts p = src.parts(a, b);
+    // L2 is asked for the next stage of bf16 logits, whose arithmetic takes long enough to wait for them (312 us without, 313 six stages ahead;
+    // fp32 logits gain nothing from it).
+    constexpr int kAhead = sizeof(T) == 2 ? kLogpThreads * 32 : 0;
+    if (kAhead > 0 && tid == 0) prefetch_range(x + row * ld, V, a, min(b, a + kAhead));
     for (int f0 = p.fa + tid * N; f0 < p.fb; f0 += kLogpThreads * 32) {
         uint32_t w[U][8];
+        if (kAhead > 0 && tid == 0 && f0 + kAhead < p.fb) prefetch_range(x + row * ld, V, f0 + kAhead, min(b, f0 + kAhead + kLogpThreads * 32));
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int f = f0 + u * kLogpThreads * N;
