@@ -763,8 +763,10 @@ __global__ void __launch_bounds__(THREADS, LISTS ? MapShape<THREADS>::kCtas : si
             if (i == 0 && q.mask == nullptr) prefetch_range(from, V, a, a + width);
             if (i + 1 < rows && plan[i + 1].q.mask == nullptr) prefetch_range(from + ld_in, V, a, a + width);
         }
-        if (a >= b)
+        if (a >= b) { // the row ends before the range, which depends on its alignment: the table stays that of a row before it
+            intact = false;
             continue;
+        }
         if (GRAD) map_listed<THREADS>(dst, from, at, MapApplyGrad{q.inv_temp}, plan[i], R, V, a, b, width, in == out, t, intact);
         else map_listed<THREADS>(dst, from, at, MapApply{q.inv_temp}, plan[i], R, V, a, b, width, in == out, t, intact);
     }
@@ -834,8 +836,10 @@ __global__ void __launch_bounds__(THREADS, LISTS ? MapShape<THREADS>::kCtas : si
             if (i == 0 && p.live && q.mask == nullptr) prefetch_range(from, V, a, a + width);
             if (i + 1 < rows && losses[i + 1].live && plan[i + 1].q.mask == nullptr) prefetch_range(from + ld, V, a, a + width);
         }
-        if (a >= b)
+        if (a >= b) { // the row ends before the range, which depends on its alignment: the table stays that of a row before it
+            intact = false;
             continue;
+        }
         const MapLogpGrad map{q.inv_temp, p.lse, p.omega * q.inv_temp, p.target + dst.lead};
         if (!p.live) zero_range<THREADS>(dst, a, b);
         else map_listed<THREADS>(dst, from, from, map, plan[i], R, V, a, b, width, x == grad, t, intact);

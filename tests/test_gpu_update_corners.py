@@ -1,0 +1,47 @@
+"""Corners of the logit rules, the token log-probabilities and the optimizer calls: work splits that only large or many-row calls
+take, rows of different alignment, equal bits on different paths, and values at the ends of the ranges."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2609_33570_b200 import api
+from tests import gpu_util as G
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("call", ["apply", "apply_backward", "logp_backward"])
+def test_rows_that_end_before_the_last_range(call):
+    """Prefix rows whose leading elements alternate between 15 and 7 (8 and 0 for the gradient of logp), with the last token of the
+    vocabulary as a fresh one of the second row.  At 148 SMs the last range of these vocabularies begins 14 (2) positions behind V, so
+    every other row has none in it.  All values are powers of two, or far from a rounding point of bf16."""
+    rows, V, ld, lead, n = (21, 2018302, 2018312, 8, 21000) if call == "logp_backward" else (16, 2427250, 2427256, 15, 16)
+    assert ld % 16 == 8
+    raw = torch.full((rows * ld + 16,), 1.0, dtype=torch.bfloat16, device="cuda")
+    assert raw.data_ptr() % 32 == 0
+    at = raw.data_ptr() + 2 * lead
+    tokens = torch.arange(100, 100 + n, dtype=torch.int32, device="cuda")
+    tokens[1] = V - 1
+    rules = api.make_logit_rules(repetition=torch.full((rows,), 2.0, device="cuda"), tokens=tokens,
+                                 hist_begin=torch.zeros(rows, dtype=torch.int64, device="cuda"),
+                                 resp_begin=torch.zeros(rows, dtype=torch.int64, device="cuda"),
+                                 hist_end=torch.arange(1, rows + 1, device="cuda"))
+    out = torch.full_like(raw, 9.0)
+    got = out[lead:lead + rows * ld].view(rows, ld)[:, :V]
+    to = out.data_ptr() + 2 * lead
+    plain, seen = 1.0, 0.5
+    if call == "apply":
+        api.hilore_logits_apply(at, api.BF16, rows, V, ld, rules, to, ld)
+    elif call == "apply_backward":
+        api.hilore_logits_apply_backward(at, api.BF16, rows, V, ld, rules, at, ld, to, ld)
+    else:
+        targets = torch.full((rows,), 7, dtype=torch.int32, device="cuda")
+        api.hilore_token_logp_backward(at, api.BF16, rows, V, ld, rules, targets, torch.full((rows,), 3.0, device="cuda"),
+                                       torch.ones(rows, device="cuda"), to, ld)
+        plain, seen = -np.exp(-2.0), -0.5 * np.exp(-2.5)
+    want = torch.full((rows, V), plain, dtype=torch.bfloat16, device="cuda")
+    for i in range(rows):
+        want[i, tokens[:i + 1].long()] = seen
+    if call == "logp_backward":
+        want[:, 7] = 1.0 - np.exp(-2.0)
+    assert torch.equal(got, want), torch.argwhere(got != want)[:5].tolist()
