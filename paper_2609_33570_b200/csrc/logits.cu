@@ -1224,10 +1224,12 @@ static hilore_logit_rules used_rules(const hilore_logit_rules *r)
 
 static bool more_than_temperature(const hilore_logit_rules &q) { return q.tokens || q.bias_tokens || q.allow; }
 
-// More than 48 KB of shared memory, the kernels' own 12 KB at most included, needs an opt-in.
-template <typename K> static bool allow_smem(K kernel, size_t bytes)
+// More than 48 KB of shared memory, the kernels' own 12 KB at most included, needs an opt-in.  It is always one for `most`, the
+// largest size that any call gives the kernel: the attribute belongs to the process, and a smaller one set by another thread
+// between this call's opt-in and its launch would have the launch refused.
+template <typename K> static bool allow_smem(K kernel, size_t bytes, size_t most)
 {
-    return bytes <= 32 * 1024 || cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess;
+    return bytes <= 32 * 1024 || cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most) == cudaSuccess;
 }
 
 static bool has_lists(const hilore_logit_rules &q) { return q.tokens || q.bias_tokens; }
@@ -1285,7 +1287,7 @@ static int launch_apply_as(const T *x, int64_t ld, const T *in, int64_t ld_in, T
         return HILORE_SHAPE;
     auto kernel = logits_apply_kernel<THREADS, T, GRAD, LISTS>;
     const size_t smem = LISTS ? MapShape<THREADS>::kShared : 0;
-    if (!allow_smem(kernel, smem))
+    if (!allow_smem(kernel, smem, smem))
         return HILORE_CUDA;
     kernel<<<(unsigned)p.grid, THREADS, smem, st>>>(x, ld, in, ld_in, out, ld_out, n_rows, (int)V, (int)p.block_rows, (int)p.n_ranges, (int)p.width, R);
     return cudaGetLastError() == cudaSuccess ? HILORE_OK : HILORE_CUDA;
@@ -1320,7 +1322,7 @@ static int launch_rows(void (*kernel)(KArgs...), int64_t grid, int cluster, size
 {
     if (grid > 0x7FFFFFFF)
         return HILORE_SHAPE;
-    if (!allow_smem(kernel, smem))
+    if (!allow_smem(kernel, smem, kLogpFixed + kLogpTokens * 2))
         return HILORE_CUDA;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)grid);
@@ -1370,7 +1372,7 @@ static int launch_logp_backward_as(const T *x, int64_t ld, int64_t n_rows, int64
         return HILORE_SHAPE;
     auto kernel = token_logp_backward_kernel<THREADS, T, LISTS>;
     const size_t smem = LISTS ? MapShape<THREADS>::kShared : 0;
-    if (!allow_smem(kernel, smem))
+    if (!allow_smem(kernel, smem, smem))
         return HILORE_CUDA;
     kernel<<<(unsigned)p.grid, THREADS, smem, st>>>(x, ld, n_rows, (int)V, (int)p.block_rows, (int)p.n_ranges, (int)p.width, targets, lse, omega, grad,
                                                        ld_grad, R);

@@ -1,5 +1,8 @@
 """Corners of the logit rules, the token log-probabilities and the optimizer calls: work splits that only large or many-row calls
 take, rows of different alignment, equal bits on different paths, and values at the ends of the ranges."""
+import ctypes
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -45,3 +48,40 @@ def test_rows_that_end_before_the_last_range(call):
     if call == "logp_backward":
         want[:, 7] = 1.0 - np.exp(-2.0)
     assert torch.equal(got, want), torch.argwhere(got != want)[:5].tolist()
+
+
+def test_threads_with_tables_of_unequal_size(monkeypatch):
+    """Log-probabilities under rules from three host threads on streams of their own: the shared memory of a call goes by the size
+    of its vocabulary (76 KB and 36 KB here, a CTA per row), and no thread's opt-in may take away another's.  Every call
+    has to be accepted; the last one gives the bits of the first, which was issued alone.  Two rows and the plain ctypes call, so
+    that the threads spend their time in the library."""
+    monkeypatch.setenv("HILORE_DISABLE_CLUSTER_LAUNCH", "1")
+    rows, calls = 2, 20000
+    jobs = []
+    for i, V in enumerate((32000, 12000, 12000)):
+        gen = torch.Generator(device="cuda").manual_seed(i)
+        x = torch.randn(rows, V, generator=gen, device="cuda").to(torch.bfloat16)
+        where = torch.arange(rows, device="cuda")
+        rules = api.make_logit_rules(repetition=torch.full((rows,), 1.5, device="cuda"), hist_begin=torch.zeros_like(where),
+                                     tokens=torch.randint(0, V, (rows,), generator=gen, device="cuda", dtype=torch.int32),
+                                     resp_begin=torch.zeros_like(where), hist_end=where + 1)
+        targets = torch.randint(0, V, (rows,), generator=gen, device="cuda", dtype=torch.int32)
+        alone, logp, stream = torch.zeros(rows, device="cuda"), torch.zeros(rows, device="cuda"), torch.cuda.Stream()
+        api.hilore_token_logp(x, api.BF16, rows, V, V, rules, targets, alone, None, None)
+        args = (x.data_ptr(), api.BF16, rows, V, V, ctypes.addressof(rules), targets.data_ptr(), logp.data_ptr(), None, None, stream.cuda_stream)
+        jobs.append(dict(args=args, alone=alone, logp=logp, refused=0, keep=(x, rules, targets, stream)))
+
+    def run(job):
+        call, args = api.lib().hilore_token_logp, job["args"]
+        for _ in range(calls):
+            job["refused"] += call(*args) != api.OK
+
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=run, args=(job,)) for job in jobs]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert [job["refused"] for job in jobs] == [0, 0, 0]
+    assert all(torch.equal(job["alone"], job["logp"]) for job in jobs)
