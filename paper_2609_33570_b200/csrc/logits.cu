@@ -256,7 +256,7 @@ __host__ __device__ constexpr int table_words(int form, int width) { return form
 struct RowPlan {
     RowRules q;
     int form, n_bias;         // n_bias: entries of a short list
-    bool used;                // the row is worked on
+    bool used;                // the row is worked on: one that ends before the CTA's range, which its alignment decides, is not
     bool follows;             // its history is that of the last row with a table and the `fresh` tokens from `from` on
     int fresh, fresh_prompt;  // ... of which the first fresh_prompt are prompt
     const int32_t *from;
@@ -749,7 +749,7 @@ __global__ void __launch_bounds__(THREADS, LISTS ? MapShape<THREADS>::kCtas : si
     const int rows = (int)min((int64_t)block_rows, n_rows - row0);
     if ((int)threadIdx.x < rows) {
         plan[threadIdx.x].q = row_rules(R, row0 + threadIdx.x);
-        plan[threadIdx.x].used = true;
+        plan[threadIdx.x].used = a < Row<T>(out + (row0 + threadIdx.x) * ld_out, V).end;
     }
     plan_rows(plan, rows, R);
     const typename MapShape<THREADS>::Table t{smem, &count, &doubles, sums};
@@ -763,10 +763,8 @@ __global__ void __launch_bounds__(THREADS, LISTS ? MapShape<THREADS>::kCtas : si
             if (i == 0 && q.mask == nullptr) prefetch_range(from, V, a, a + width);
             if (i + 1 < rows && plan[i + 1].q.mask == nullptr) prefetch_range(from + ld_in, V, a, a + width);
         }
-        if (a >= b) { // the row ends before the range, which depends on its alignment: the table stays that of a row before it
-            intact = false;
+        if (a >= b)
             continue;
-        }
         if (GRAD) map_listed<THREADS>(dst, from, at, MapApplyGrad{q.inv_temp}, plan[i], R, V, a, b, width, in == out, t, intact);
         else map_listed<THREADS>(dst, from, at, MapApply{q.inv_temp}, plan[i], R, V, a, b, width, in == out, t, intact);
     }
@@ -821,7 +819,7 @@ __global__ void __launch_bounds__(THREADS, LISTS ? MapShape<THREADS>::kCtas : si
         const RowRules q = row_rules(R, row0 + threadIdx.x);
         plan[threadIdx.x].q = q;
         losses[threadIdx.x] = row_loss(q, targets, lse, omega, row0 + threadIdx.x, V);
-        plan[threadIdx.x].used = losses[threadIdx.x].live;
+        plan[threadIdx.x].used = losses[threadIdx.x].live && a < Row<T>(grad + (row0 + threadIdx.x) * ld_grad, V).end;
     }
     plan_rows(plan, rows, R);
     const typename MapShape<THREADS>::Table t{smem, &count, &doubles, sums};
@@ -836,10 +834,8 @@ __global__ void __launch_bounds__(THREADS, LISTS ? MapShape<THREADS>::kCtas : si
             if (i == 0 && p.live && q.mask == nullptr) prefetch_range(from, V, a, a + width);
             if (i + 1 < rows && losses[i + 1].live && plan[i + 1].q.mask == nullptr) prefetch_range(from + ld, V, a, a + width);
         }
-        if (a >= b) { // the row ends before the range, which depends on its alignment: the table stays that of a row before it
-            intact = false;
+        if (a >= b)
             continue;
-        }
         const MapLogpGrad map{q.inv_temp, p.lse, p.omega * q.inv_temp, p.target + dst.lead};
         if (!p.live) zero_range<THREADS>(dst, a, b);
         else map_listed<THREADS>(dst, from, from, map, plan[i], R, V, a, b, width, x == grad, t, intact);
