@@ -478,8 +478,8 @@ int hilore_logits_apply_backward(const void *logits, int32_t dtype, int64_t n_ro
  *   A denied target has logp = -inf.  A row in which nothing is allowed has logp = lse = -inf, entropy 0.  A NaN among
  *   the allowed logits makes the row NaN; +Inf gives lse = +Inf and entropy NaN.
  *   A row is the work of one CTA, or of a thread-block cluster of up to 8 when there are few rows (never with
- *   HILORE_DISABLE_CLUSTER_LAUNCH): logp, lse and entropy of a row depend on that choice in their last bits, not on
- *   anything else; the same call gives the same bits.
+ *   HILORE_DISABLE_CLUSTER_LAUNCH): logp, lse and entropy of a row depend in their last bits on that choice and on the
+ *   row's address modulo 32 bytes, not on the other rows of the call; the same call gives the same bits.
  *
  * hilore_token_logp_backward: grad_v = omega_r (1[v = a] - exp(z_v - lse_r)) dz_v/dx_v, the gradient of sum_r omega_r
  * logp_r with respect to the logits, for the omega of hilore_grpo_coeffs.

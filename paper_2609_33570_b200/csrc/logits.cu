@@ -330,8 +330,8 @@ template <int BITS> struct Listed {
     }
 
     // Brings table and bias entries to the row's rules for tokens [v0, v0 + width).  `follow`: by adding the plan's fresh tokens to the
-    // table of the row before; `sorted`: the list has to be as it would be made from the bits after that as well.  Ends with the CTA
-    // synchronised.
+    // table of the row before; `sorted`: the list has to be as it would be made from the bits after that as well, so that sums over it
+    // do not depend on where the row's block began.  Ends with the CTA synchronised.
     template <int THREADS>
     __device__ __forceinline__ void fill(const hilore_logit_rules &R, const RowPlan &p, int V, int v0, int width, int form, bool follow, bool sorted,
                                          uint16_t *list, int cap) const
@@ -406,7 +406,7 @@ template <int BITS> struct Listed {
             }
         }
         __syncthreads();
-        if (clear || (follow && sorted && *n > before + 1 && *n <= cap)) order<THREADS>(bits, list, cap);
+        if (clear || (follow && sorted && *n > before && *n <= cap)) order<THREADS>(bits, list, cap);
     }
 
     // Makes the list from the touch bits: a thread's words lie apart, as frequent tokens are neighbours.  Ends with the CTA synchronised.
@@ -1018,7 +1018,7 @@ __global__ void __launch_bounds__(kLogpThreads, 4)
 // Under rules.  A cluster of `row_ctas` CTAs (or one CTA) walks a block of consecutive rows; each CTA owns `width` positions of
 // every row, so that its table of counts serves one row after the other.  The statistics of every warp go to the first
 // CTA, which joins them when the block is done.  Bound by the waits of a row's steps, not by bytes: 1021 rows of 50001 fp32 logits
-// under prefixes of up to 900 tokens, 24 biases and masks on a third take 98 us (the bytes 29), 60 without masks, biases and history.
+// under prefixes of up to 900 tokens, 24 biases and masks on a third take 102 us (the bytes 29; 98 with a single fresh token left out of order), 60 without masks, biases and history.
 constexpr int kLogpTokens = 32768; // tokens of a table of 16-bit counts at most: 8 CTAs take vocabularies up to 260000 in one part
 constexpr int kLogpBits = kLogpTokens / 32 + 8, kLogpCap = 2048;
 using LogpListed = Listed<kLogpBits>;

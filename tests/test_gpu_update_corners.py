@@ -85,3 +85,32 @@ def test_threads_with_tables_of_unequal_size(monkeypatch):
     torch.cuda.synchronize()
     assert [job["refused"] for job in jobs] == [0, 0, 0]
     assert all(torch.equal(job["alone"], job["logp"]) for job in jobs)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_row_has_the_same_bits_in_every_batch(dtype, monkeypatch):
+    """Prefix rows, whose tables are carried from row to row of a block, against the same rows called alone and by sevens: equal
+    alignment, one CTA per row in every call, so the sums are the same, whichever row a block began with."""
+    monkeypatch.setenv("HILORE_DISABLE_CLUSTER_LAUNCH", "1")
+    kind, tt = (api.BF16, torch.bfloat16) if dtype == "bf16" else (api.F32, torch.float32)
+    rows, V, ld, length = 3000, 5003, 5008, 300
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    x = (torch.randn(rows, ld, generator=gen, device="cuda") * 3).to(tt)
+    row = torch.arange(rows, device="cuda")
+    tokens = (torch.rand(rows, generator=gen, device="cuda") ** 2 * V).int()
+    parts = dict(repetition=torch.full((rows,), 1.3, device="cuda"), frequency=torch.full((rows,), 0.2, device="cuda"),
+                 presence=torch.full((rows,), 0.1, device="cuda"), hist_begin=row // length * length, hist_end=row,
+                 resp_begin=torch.minimum(row // length * length + length // 4, row))
+    targets = torch.randint(0, V, (rows,), generator=gen, device="cuda", dtype=torch.int32)
+
+    def call(a, b):
+        rules = api.make_logit_rules(tokens=tokens, **{k: v[a:b].contiguous() for k, v in parts.items()})
+        out = torch.zeros(3, b - a, device="cuda")
+        api.hilore_token_logp(x[a:b], kind, b - a, V, ld, rules, targets[a:b], out[0], out[1], out[2])
+        return out
+
+    whole = call(0, rows)
+    for a in list(range(0, 16)) + list(range(1000, 1040)) + [rows - 1]:
+        assert torch.equal(call(a, a + 1), whole[:, a:a + 1]), a
+    for a in (3, 290, 2001, rows - 7):
+        assert torch.equal(call(a, a + 7), whole[:, a:a + 7]), a
