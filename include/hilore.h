@@ -531,8 +531,10 @@ size_t hilore_grad_norm_workspace_bytes(void);
  * One AdamW step over all tensors of a table in ONE launch.  Per element, in fp32, with g = grad_scale * gradient:
  *     m = beta1 m + (1 - beta1) g;        v = beta2 v + (1 - beta2) g^2
  *     p = p - lr ( weight_decay p + (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps) )
- * m, sqrt(v) and the codes made from them take every operation rounded by itself, in this order ((1 - beta2) g first,
- * then times g), so they are the same bits in any evaluation that does so.
+ * m, v and the codes made from them take every operation rounded by itself, in this order ((1 - beta2) g first,
+ * then times g), so they are the same bits in any evaluation that does so.  sqrt(v) of HILORE_STATE_E4M3FN is rounded to
+ * nearest; below v = 2^-102 it may be the next number instead.  No result depends on a tensor's alignment or place in the
+ * table, nor on the values of other blocks of 64.
  * The parameter (or its fp32 master copy) is rounded to its type to nearest even.
  *   HILORE_STATE_E4M3FN: the moments of the step enter the update in fp32; then, per block of 64 consecutive elements of
  *     a tensor (the last one may be shorter), m and sqrt(v) are stored as codes by the rule of HILORE_FMT_E4M3FN_BLK in

@@ -282,8 +282,10 @@ __device__ __forceinline__ uint64_t next_param2(const AdamStep &h, uint64_t p, u
 }
 
 // Square roots of a pair of v from minus v (zero, or at least 2^-126 in size): Newton's step r - (r^2 - v) / (2 r) from
-// r = v * rsqrt(v), the residual formed exactly by a fused operation: an error of 2^-43 is left before the final rounding.
-// Inf and NaN need another way (__fsqrt_rn where a block holds one).  Two roots at a time in packed operations without a branch.
+// r = v * rsqrt(v), the residual formed exactly by a fused operation down to v = 2^-102: an error of 2^-43 is left before the final
+// rounding, and of all numbers from there on none was found rounded to the wrong neighbour.  Below, where the residual loses bits to
+// 2^-149, 1.8 of 201 million are (one in ten at 2^-126).  Every path of the 8-bit states takes its roots
+// here: a tensor's results do not depend on its alignment.  Two roots at a time in packed operations without a branch.
 __device__ __forceinline__ uint64_t root2(uint64_t minus_v)
 {
     constexpr float kMost = 9.223372036854775808e18f; // 2^63, of 2^-126; of zero this instead of Inf
@@ -294,6 +296,15 @@ __device__ __forceinline__ uint64_t root2(uint64_t minus_v)
     const uint64_t y = f32x2_pack(fmaxf(-y0, -kMost), fmaxf(-y1, -kMost)); // minus 1 / sqrt(v)
     const uint64_t r = f32x2_mul(minus_v, y);
     return f32x2_fma(f32x2_fma(r, r, minus_v), f32x2_mul(y, both(0.5f)), r);
+}
+
+// The same where v may be Inf or NaN, which are their own roots.
+__device__ __forceinline__ uint64_t root2_any(uint64_t minus_v)
+{
+    float v0, v1, r0, r1;
+    f32x2_unpack(minus_v, v0, v1);
+    f32x2_unpack(root2(minus_v), r0, r1);
+    return f32x2_pack(fabsf(v0) < INFINITY ? r0 : fabsf(v0), fabsf(v1) < INFINITY ? r1 : fabsf(v1));
 }
 
 __device__ __forceinline__ uint64_t decode2(uint32_t codes, float s) // two codes in the low half
@@ -448,11 +459,8 @@ __device__ __forceinline__ void run_e4m3(const hilore_param &e, const AdamStep &
         const bool odd = __any_sync(0xFFFFFFFFu, fmaxf(am, ar) == INFINITY);
         if (odd) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                float v0, v1;
-                f32x2_unpack(r[k], v0, v1);
-                r[k] = f32x2_pack(__fsqrt_rn(-v0), __fsqrt_rn(-v1));
-            }
+            for (int k = 0; k < 8; ++k)
+                r[k] = root2_any(r[k]);
         } else {
 #pragma unroll
             for (int k = 0; k < 8; ++k)
@@ -544,9 +552,12 @@ template <bool CODED, int P, int G, bool MASTER> __device__ __noinline__ void ti
             float m1[2], v1[2], r[2], q[2];
             f32x2_unpack(mm, m1[0], m1[1]);
             f32x2_unpack(vv, v1[0], v1[1]);
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-                r[u] = __fsqrt_rn(CODED ? -v1[u] : v1[u]);
+            if (CODED) {
+                f32x2_unpack(root2_any(vv), r[0], r[1]);
+            } else {
+                r[0] = __fsqrt_rn(v1[0]);
+                r[1] = __fsqrt_rn(v1[1]);
+            }
             const float p0 = from_bits<Q>(p[k][0]), p1 = from_bits<Q>(p[k][1]);
             if (CODED) {
                 f32x2_unpack(next_param2(h, f32x2_pack(p0, p1), mm, f32x2_pack(r[0], r[1])), q[0], q[1]);
