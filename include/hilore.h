@@ -517,8 +517,9 @@ typedef struct hilore_param {
 
 /*
  * Global norm of the gradients of a table, ||g|| = sqrt(sum over all tensors of g^2), and the factor that clips it:
- * scale = min(1, max_norm / (norm + 1e-6)), NaN where the norm is not finite.  Squares are added in fp32 per 32
- * elements (fp64 where that overflows) and in fp64 beyond, in a fixed order: run-to-run deterministic.
+ * scale = min(1, max_norm / (norm + 1e-6)), NaN where a gradient is not finite.  Squares are added in fp32 per 32
+ * elements (fp64 where that overflows or loses bits to the smallest numbers) and in fp64 beyond, in a fixed order: run-to-run
+ * deterministic.  A norm beyond fp32 is stored as Inf; its scale is right.
  *   Of the table only g, g_dtype, n and first are read.    max_norm >= 0 (Inf: no clipping).
  *   norm, scale   opt one fp32 each on the device, at least one of them.
  *   workspace     hilore_grad_norm_workspace_bytes() bytes, 16-byte aligned.

@@ -139,12 +139,15 @@ static int tiles_per_warp(int64_t tiles)
 }
 
 // ------------------------------------------------------------------------------------------------------------------- norm
-// Squares in fp32 over the 32 elements of a lane's tile, fp64 beyond; a lane whose fp32 sum leaves the range redoes its
-// elements in fp64.  Partial sums in fixed slots: the result does not depend on scheduling.
+// Squares in fp32 over the 32 elements of a lane's tile, fp64 beyond; a lane whose fp32 sum overflows, or is so small that squares have
+// lost bits to 2^-149 (at 2^-100 all 32 lose 2^-45 of it at most), redoes its elements in fp64; zeros alone do not.  Partial sums in
+// fixed slots: the result does not depend on scheduling.
 template <int DTYPE> __device__ __forceinline__ double tile_squares(const void *g, int64_t base, int64_t n, bool vec)
 {
+    constexpr float kExact = 7.888609052e-31f; // 2^-100
     const int lane = threadIdx.x & 31;
     float s = 0.0f;
+    uint32_t any = 0; // bits of the magnitudes, for a small sum
     if (vec && base + kTile <= n) {
         Raw<DTYPE, 8> x[kTile / 256];
 #pragma unroll
@@ -155,14 +158,22 @@ template <int DTYPE> __device__ __forceinline__ double tile_squares(const void *
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 s = fmaf(x[k].get(i), x[k].get(i), s);
+        if (s < kExact) {
+#pragma unroll
+            for (int k = 0; k < kTile / 256; ++k)
+#pragma unroll
+                for (int i = 0; i < Raw<DTYPE, 8>::W; ++i)
+                    any |= x[k].w[i] & (DTYPE == HILORE_BF16 ? 0x7FFF7FFFu : 0x7FFFFFFFu);
+        }
     } else {
         for (int64_t i = base + lane; i < min(n, base + kTile); i += 32) {
             const float x = load_one(g, DTYPE, i);
             s = fmaf(x, x, s);
+            any |= __float_as_uint(x) & 0x7FFFFFFFu;
         }
     }
     double d = (double)s;
-    if (!(s < INFINITY)) {
+    if (!(s < INFINITY) || (s < kExact && any)) {
         d = 0.0;
         const bool dealt = vec && base + kTile <= n; // which elements were this lane's
         for (int k = 0; k < kTile / 32; ++k) {

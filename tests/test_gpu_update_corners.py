@@ -178,3 +178,24 @@ def test_eight_bit_step_of_shifted_tensors_has_the_same_bits(kind):
         done.append({k: t.contiguous().view(torch.int16).int() if t.dtype == torch.bfloat16 else t.clone() for k, t in e.items() if isinstance(t, torch.Tensor)})
     names = [k for k in done[0] if k != "g"]
     assert same_bits(done[0], done[1], names) == [] and same_bits(done[0], done[2], names) == []
+
+
+@pytest.mark.parametrize("shift", [0, 1], ids=["vectors", "elements"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_norm_of_gradients_whose_squares_leave_fp32(dtype, shift):
+    """Sizes from subnormal numbers to 1e38, alone and beside zeros and ordinary ones: 32 additions in fp32 and the rest in fp64, so a
+    relative error of 33 * 2^-24 at most.  The norm of 1e38s does not fit fp32, its scale does."""
+    tt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    n = 40 * 1024 + 333
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    ws = torch.zeros(api.hilore_grad_norm_workspace_bytes(), dtype=torch.uint8, device="cuda")
+    for sizes in ((1e-24,), (1e-19,), (1e-16,), (3e-39,), (0.0, 1e-30), (1e-24, 1e-3), (0.0,), (1e18, 1e20), (1e38,)):
+        g = torch.randn(n, generator=gen, device="cuda").clamp_(-3, 3).double() * torch.tensor(sizes, device="cuda", dtype=torch.float64).repeat_interleave(64).repeat(n)[:n]
+        g = torch.cat([torch.zeros(shift, device="cuda", dtype=tt), g.to(tt)])[shift:]
+        z = torch.zeros(n, device="cuda")
+        dev, host = api.make_param_table([dict(p=z, g=g, m=z, v=z)])
+        norm, scale = torch.full((1,), -1.0, device="cuda"), torch.full((1,), -1.0, device="cuda")
+        api.hilore_grad_norm(dev, host, 1, 1e-2, norm, scale, ws, ws.numel())
+        want = float(g.double().norm())
+        assert want < 3.4e38 and float(norm) == pytest.approx(want, rel=33 * 2.0 ** -24, abs=1e-45) or want > 3.5e38 and float(norm) == float("inf"), (sizes, float(norm), want)
+        assert float(scale) == pytest.approx(min(1.0, 1e-2 / (want + 1e-6)), rel=35 * 2.0 ** -24, abs=1e-45), sizes
