@@ -50,6 +50,7 @@ class HiloreLogitRules(C.Structure):
                 ("hist_end", C.c_void_p), ("bias_tokens", C.c_void_p), ("bias_values", C.c_void_p), ("n_bias", C.c_int64),
                 ("bias_offsets", C.c_void_p), ("allow", C.c_void_p), ("allow_row", C.c_void_p), ("n_allow", C.c_int64),
                 ("allow_ld", C.c_int64)]
+    rows, on_host = None, ()  # rows that the tensors reach for and parts that a kernel cannot read, where make_logit_rules has seen them
 
 
 class HiloreParam(C.Structure):
@@ -355,33 +356,48 @@ def make_unit_table(units, device="cuda"):
     return dev, arr
 
 
-def _host(struct):
-    """Address of a host-side ctypes struct or array, or None."""
-    return None if struct is None else C.addressof(struct)
+def _rules(rules, n_rows):
+    """Address of the rules, or None.  Those made from tensors have to reach for all rows, and from the device."""
+    if rules is None:
+        return None
+    if rules.rows is not None and n_rows > rules.rows:
+        raise ValueError(f"rules of {rules.rows} rows in a call of {n_rows}")
+    if rules.on_host:
+        raise ValueError(f"{', '.join(rules.on_host)}: expected device tensors")
+    return C.addressof(rules)
+
+
+def _table(params_host, n_params):
+    """Address of the host half of a table, or None."""
+    if params_host is None:
+        return None
+    if n_params > len(params_host):
+        raise ValueError(f"a table of {len(params_host)} entries in a call of {n_params}")
+    return C.addressof(params_host)
 
 
 def hilore_logits_apply(logits, dtype, n_rows, V, ld, rules, out, ld_out, stream=None, check=True):
     """rules: a HiloreLogitRules on the host (make_logit_rules)."""
-    st = lib().hilore_logits_apply(_ptr(logits), dtype, n_rows, V, ld, _host(rules), _ptr(out), ld_out, _stream(stream))
+    st = lib().hilore_logits_apply(_ptr(logits), dtype, n_rows, V, ld, _rules(rules, n_rows), _ptr(out), ld_out, _stream(stream))
     return _check(st, "hilore_logits_apply", check)
 
 
 def hilore_logits_apply_backward(logits, dtype, n_rows, V, ld, rules, grad_out, ld_grad_out, grad_in, ld_grad_in,
                                  stream=None, check=True):
-    st = lib().hilore_logits_apply_backward(_ptr(logits), dtype, n_rows, V, ld, _host(rules), _ptr(grad_out), ld_grad_out,
+    st = lib().hilore_logits_apply_backward(_ptr(logits), dtype, n_rows, V, ld, _rules(rules, n_rows), _ptr(grad_out), ld_grad_out,
                                             _ptr(grad_in), ld_grad_in, _stream(stream))
     return _check(st, "hilore_logits_apply_backward", check)
 
 
 def hilore_token_logp(logits, dtype, n_rows, V, ld, rules, targets, logp, lse, entropy, stream=None, check=True):
-    st = lib().hilore_token_logp(_ptr(logits), dtype, n_rows, V, ld, _host(rules), _ptr(targets), _ptr(logp), _ptr(lse),
+    st = lib().hilore_token_logp(_ptr(logits), dtype, n_rows, V, ld, _rules(rules, n_rows), _ptr(targets), _ptr(logp), _ptr(lse),
                                  _ptr(entropy), _stream(stream))
     return _check(st, "hilore_token_logp", check)
 
 
 def hilore_token_logp_backward(logits, dtype, n_rows, V, ld, rules, targets, lse, omega, grad, ld_grad, stream=None,
                                check=True):
-    st = lib().hilore_token_logp_backward(_ptr(logits), dtype, n_rows, V, ld, _host(rules), _ptr(targets), _ptr(lse),
+    st = lib().hilore_token_logp_backward(_ptr(logits), dtype, n_rows, V, ld, _rules(rules, n_rows), _ptr(targets), _ptr(lse),
                                           _ptr(omega), _ptr(grad), ld_grad, _stream(stream))
     return _check(st, "hilore_token_logp_backward", check)
 
@@ -393,14 +409,14 @@ def hilore_grad_norm_workspace_bytes():
 def hilore_grad_norm(params_dev, params_host, n_params, max_norm, norm, scale, workspace, workspace_bytes, stream=None,
                      check=True):
     """params_dev / params_host: the two halves of make_param_table."""
-    st = lib().hilore_grad_norm(_ptr(params_dev), _host(params_host), n_params, max_norm, _ptr(norm), _ptr(scale),
+    st = lib().hilore_grad_norm(_ptr(params_dev), _table(params_host, n_params), n_params, max_norm, _ptr(norm), _ptr(scale),
                                 _ptr(workspace), workspace_bytes, _stream(stream))
     return _check(st, "hilore_grad_norm", check)
 
 
 def hilore_adamw_step(params_dev, params_host, n_params, lr, lr_dev, beta1, beta2, eps, step, step_dev, grad_scale,
                       stream=None, check=True):
-    st = lib().hilore_adamw_step(_ptr(params_dev), _host(params_host), n_params, lr, _ptr(lr_dev), beta1, beta2, eps, step,
+    st = lib().hilore_adamw_step(_ptr(params_dev), _table(params_host, n_params), n_params, lr, _ptr(lr_dev), beta1, beta2, eps, step,
                                  _ptr(step_dev), _ptr(grad_scale), _stream(stream))
     return _check(st, "hilore_adamw_step", check)
 
@@ -414,11 +430,17 @@ def _typed(t, name, *dtypes):
     return t
 
 
+def _on_host(t):
+    """Whether `t` is a tensor in host memory that kernels cannot read."""
+    return t is not None and t.device.type != "cuda" and not (t.device.type == "cpu" and t.is_pinned())
+
+
 def make_logit_rules(temperature=None, repetition=None, frequency=None, presence=None, tokens=None, hist_begin=None,
                      resp_begin=None, hist_end=None, bias_tokens=None, bias_values=None, bias_offsets=None, allow=None,
                      allow_row=None):
     """Marshal the tensors of ``struct hilore_logit_rules`` (fp32 levels, int32 tokens, int64 ranges, int32 mask words
-    [n_allow, allow_ld]).  The struct holds addresses and keeps the tensors alive."""
+    [n_allow, allow_ld]).  The struct holds addresses and keeps the tensors alive.  A call may have as many rows as the
+    shortest of its tensors with an entry per row."""
     f, i, j = (torch.float32,), (torch.int32,), (torch.int64,)
     parts = dict(temperature=_typed(temperature, "temperature", *f), repetition=_typed(repetition, "repetition", *f),
                  frequency=_typed(frequency, "frequency", *f), presence=_typed(presence, "presence", *f),
@@ -427,11 +449,23 @@ def make_logit_rules(temperature=None, repetition=None, frequency=None, presence
                  bias_tokens=_typed(bias_tokens, "bias_tokens", *i), bias_values=_typed(bias_values, "bias_values", *f),
                  bias_offsets=_typed(bias_offsets, "bias_offsets", *j), allow=_typed(allow, "allow", *i),
                  allow_row=_typed(allow_row, "allow_row", *i))
+    needs = dict(hist_begin="tokens", resp_begin="tokens", hist_end="tokens", bias_offsets="bias_tokens", bias_values="bias_tokens",
+                 allow_row="allow")  # parts that are read beside another one alone
+    filled = {k: t for k, t in parts.items() if t is not None and t.numel()}
+    read = {k: t for k, t in filled.items() if needs.get(k, k) in filled}
+    per_row = {k: t.numel() - (k == "bias_offsets") for k, t in read.items()
+               if k not in ("tokens", "bias_tokens", "bias_values", "allow")}
+    if bias_tokens is not None and bias_values is not None and bias_values.numel() < bias_tokens.numel():
+        raise ValueError(f"{bias_values.numel()} bias_values of {bias_tokens.numel()} bias_tokens")
+    if allow is not None and allow.dim() != 2:
+        raise ValueError(f"allow: expected [n_allow, allow_ld], got {tuple(allow.shape)}")
     r = HiloreLogitRules(**{k: _ptr(t) for k, t in parts.items()})
     r.n_tokens = 0 if tokens is None else tokens.numel()
     r.n_bias = 0 if bias_tokens is None else bias_tokens.numel()
     if allow is not None:
         r.n_allow, r.allow_ld = allow.shape
+    r.rows = min(per_row.values(), default=None)
+    r.on_host = tuple(k for k, t in read.items() if _on_host(t))
     r.keep = parts
     return r
 
@@ -450,15 +484,17 @@ def make_param_table(params, device="cuda"):
         n, coded = p.numel(), m.element_size() == 1
         master, ms, vs = (_typed(e.get(k), k, torch.float32) for k in ("master", "m_scale", "v_scale"))
         blocks = (n + BLOCK - 1) // BLOCK
-        for name, t, want in (("g", g, n), ("m", m, n), ("v", v, n), ("master", master, n), ("m_scale", ms, blocks),
+        for name, t, want in (("p", p, n), ("g", g, n), ("m", m, n), ("v", v, n), ("master", master, n), ("m_scale", ms, blocks),
                               ("v_scale", vs, blocks)):
             if t is not None and t.numel() != want:
                 raise ValueError(f"entry {i}: {name} has {t.numel()} elements, expected {want}")
+            if torch.device(device).type == "cuda" and _on_host(t):
+                raise ValueError(f"entry {i}: {name} is on the host, the table on {device}")
         if (v.element_size() == 1) != coded or coded != (ms is not None) or coded != (vs is not None):
             raise ValueError(f"entry {i}: m and v are both fp32 without scales, or both codes with scales")
         arr[i] = HiloreParam(_ptr(p), _ptr(master), _ptr(g), _ptr(m), _ptr(v), _ptr(ms), _ptr(vs), n, first, kinds[p.dtype],
                              kinds[g.dtype], STATE_E4M3FN if coded else STATE_F32, e.get("weight_decay", 0.0))
         first += (n + PARAM_TILE - 1) // PARAM_TILE
-    arr.keep = params
+    arr.keep = [dict(e) for e in params]
     dev = torch.frombuffer(bytearray(bytes(arr)), dtype=torch.uint8).to(device) if len(params) else None
     return dev, arr
