@@ -421,7 +421,7 @@ enum { HILORE_BF16 = 0, HILORE_F32 = 1 };
  *     z = z + bias of v
  *     z = z / temperature;      v denied by the grammar:  z = -inf (also where x is NaN or Inf)
  * evaluated in fp32, rounded once to the type of the result.
- *   temperature   [n_rows] fp32; a value that is not > 0 (0: greedy) leaves the row unscaled.
+ *   temperature   [n_rows] fp32; a value that is not > 0 (0: greedy) leaves the row unscaled, Inf makes its allowed tokens alike.
  *   repetition, frequency, presence   [n_rows] fp32 each; NULL = 1, 0, 0.  repetition > 0.
  *   tokens        [n_tokens] int32, the sequences of the batch packed back to back.  Row r's history is
  *                 tokens[hist_begin[r] .. hist_end[r]-1], of which the part from resp_begin[r] on was generated, the

@@ -194,6 +194,10 @@ __device__ __forceinline__ float inverse_temperature(const float *temperature, i
     return t > 0.0f ? __fdiv_rn(1.0f, t) : 1.0f; // 0 (greedy) and what is no temperature: not scaled
 }
 
+// The inverse temperature of a softmax: that of an infinite temperature is the smallest number instead of zero, whose product with
+// the -inf of a denied token would be NaN.
+__device__ __forceinline__ float softmax_factor(float inv_temp) { return fmaxf(inv_temp, __uint_as_float(1u)); }
+
 __device__ __forceinline__ RowRules row_rules(const hilore_logit_rules &R, int64_t row)
 {
     RowRules q;
@@ -804,7 +808,7 @@ __global__ void __launch_bounds__(THREADS, LISTS ? MapShape<THREADS>::kCtas : si
         if (a >= dst.end)
             return;
         const int b = min(dst.end, a + width);
-        if (p.live) map_plain<THREADS>(dst, x + row0 * ld, MapLogpGrad{q.inv_temp, p.lse, p.omega * q.inv_temp, p.target + dst.lead}, q.mask, V, a, b);
+        if (p.live) map_plain<THREADS>(dst, x + row0 * ld, MapLogpGrad{softmax_factor(q.inv_temp), p.lse, p.omega * q.inv_temp, p.target + dst.lead}, q.mask, V, a, b);
         else zero_range<THREADS>(dst, a, b);
         return;
     }
@@ -836,7 +840,7 @@ __global__ void __launch_bounds__(THREADS, LISTS ? MapShape<THREADS>::kCtas : si
         }
         if (a >= b)
             continue;
-        const MapLogpGrad map{q.inv_temp, p.lse, p.omega * q.inv_temp, p.target + dst.lead};
+        const MapLogpGrad map{softmax_factor(q.inv_temp), p.lse, p.omega * q.inv_temp, p.target + dst.lead};
         if (!p.live) zero_range<THREADS>(dst, a, b);
         else map_listed<THREADS>(dst, from, from, map, plan[i], R, V, a, b, width, x == grad, t, intact);
     }
@@ -966,7 +970,7 @@ __global__ void __launch_bounds__(kLogpThreads, 4)
         return;
     }
     if (row_ctas > 1) cl.barrier_arrive(); // once all have arrived, every CTA of the row runs
-    const float inv_temp = inverse_temperature(temperature, row), c = kLog2eF * inv_temp;
+    const float inv_temp = softmax_factor(inverse_temperature(temperature, row)), c = kLog2eF * inv_temp;
     const Row<T> src(x + row * ld, V);
     const int n_vec = (src.end + N - 1) / N;
     const int a = (int)((int64_t)n_vec * rank / row_ctas) * N, b = (int)((int64_t)n_vec * (rank + 1) / row_ctas) * N;
@@ -1065,7 +1069,7 @@ __global__ void __launch_bounds__(kLogpThreads, sizeof(T) == 4 ? 3 : 4)
             continue;
         const T *xrow = x + (row0 + r) * ld;
         const Row<T> src(xrow, V);
-        const float c = kLog2eF * q.inv_temp;
+        const float c = kLog2eF * softmax_factor(q.inv_temp);
         const uint32_t *mask = q.mask;
         int a = rank * width;
         const int b = min(src.end, a + width);
@@ -1167,7 +1171,7 @@ __global__ void __launch_bounds__(kLogpThreads, sizeof(T) == 4 ? 3 : 4)
             }
             continue;
         }
-        const float inv_temp = plan[r].q.inv_temp, c = kLog2eF * inv_temp;
+        const float inv_temp = softmax_factor(plan[r].q.inv_temp), c = kLog2eF * inv_temp;
         Soft acc{kLowest, 0.0f, 0.0f};
         for (int k = lane; k < row_ctas * kLogpWarps; k += 32)
             acc = soft_join<ENTROPY>(acc, part[r][k], c);

@@ -199,3 +199,47 @@ def test_norm_of_gradients_whose_squares_leave_fp32(dtype, shift):
         want = float(g.double().norm())
         assert want < 3.4e38 and float(norm) == pytest.approx(want, rel=33 * 2.0 ** -24, abs=1e-45) or want > 3.5e38 and float(norm) == float("inf"), (sizes, float(norm), want)
         assert float(scale) == pytest.approx(min(1.0, 1e-2 / (want + 1e-6)), rel=35 * 2.0 ** -24, abs=1e-45), sizes
+
+
+@pytest.mark.parametrize("entropy", [True, False])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("ruled", ["temperature", "grammar", "lists"])
+def test_infinite_temperature_is_uniform_over_what_is_allowed(ruled, dtype, entropy):
+    """z = x / inf = 0 for every allowed token: logp = -ln n, lse = entropy = ln n (a logarithm and V / 256 + 40 additions of fp32), a
+    denied target -inf; the gradient is zero.  Odd sizes, so that both ends of a row are taken element by element."""
+    kind, tt = (api.BF16, torch.bfloat16) if dtype == "bf16" else (api.F32, torch.float32)
+    rows, V = 3, 1003
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    x = (torch.randn(rows, V, generator=gen, device="cuda") * 4).to(tt)
+    allow = torch.full((rows, 32), -1, dtype=torch.int32, device="cuda")
+    allow[:, 3] = 0
+    allow[2, 31] = 0
+    parts = dict(temperature=torch.full((rows,), float("inf"), device="cuda"))
+    if ruled != "temperature":
+        parts["allow"] = allow
+    if ruled == "lists":
+        parts.update(repetition=torch.full((rows,), 1.5, device="cuda"), tokens=torch.arange(90, 130, dtype=torch.int32, device="cuda"),
+                     hist_begin=torch.zeros(rows, dtype=torch.int64, device="cuda"), resp_begin=torch.zeros(rows, dtype=torch.int64, device="cuda"),
+                     hist_end=torch.full((rows,), 40, device="cuda"))
+    rules = api.make_logit_rules(**parts)
+    n = np.array([V, V, V] if ruled == "temperature" else [V - 32, V - 32, V - 32 - 11])
+    targets = torch.tensor([5, 100, 700], dtype=torch.int32, device="cuda")
+    out = torch.full((3, rows), 9.0, device="cuda")
+    api.hilore_token_logp(x, kind, rows, V, V, rules, targets, out[0], out[1], out[2] if entropy else None)
+    logp, lse, h = out.double().cpu().numpy()
+    want = -np.log(n)
+    if ruled != "temperature":
+        want[1] = -np.inf                                       # token 100 is denied
+    tol = (V / 256 + 48) * 2.0 ** -24 * 8
+    assert np.allclose(logp, want, rtol=0, atol=tol) and np.allclose(lse, np.log(n), rtol=0, atol=tol)
+    assert not entropy or np.allclose(h, np.log(n), rtol=0, atol=tol)
+    grad = torch.full_like(x, 7.0)
+    api.hilore_token_logp_backward(x, kind, rows, V, V, rules, targets, out[1], torch.ones(rows, device="cuda"), grad, V)
+    assert bool((grad == 0).all())
+    z = torch.full_like(x, 7.0)
+    api.hilore_logits_apply(x, kind, rows, V, V, rules, z, V)
+    denied = torch.zeros(rows, V, dtype=torch.bool, device="cuda")
+    if ruled != "temperature":
+        denied[:, 96:128] = True
+        denied[2, 992:] = True
+    assert bool((z[denied] == -float("inf")).all()) and bool((z[~denied] == 0).all())
