@@ -8,7 +8,8 @@ import pytest
 import torch
 
 from paper_2609_33570_b200 import api
-from tests import gpu_util as G
+from tests import update_ref as R
+from tests.test_gpu_logits import check, device_rules, make_rules
 
 pytestmark = pytest.mark.gpu
 
@@ -243,3 +244,109 @@ def test_infinite_temperature_is_uniform_over_what_is_allowed(ruled, dtype, entr
         denied[:, 96:128] = True
         denied[2, 992:] = True
     assert bool((z[denied] == -float("inf")).all()) and bool((z[~denied] == 0).all())
+
+
+SPLIT = [  # rows, V, leading dimensions of the input and the output, history, bias, grammar, prefix: in blocks x ranges on 148 SMs
+    (96, 151936, 151936, 151936, 16384, 48, "indexed", False),    # rules 2 x 6
+    (450, 128256, 128256, 128256, 1536, 0, None, True),           # rules 7 x 4
+    (450, 128251, 128257, 128252, 150, 6, "indexed", True),       # the same, every row of another alignment, input and output unlike
+    (1500, 32063, 32063, 32063, 1200, 0, None, True),             # gradient of logp 7 x 2
+    (900, 40001, 40003, 40009, 100, 600, "indexed", True),        # gradient of logp 5 x 2; bias lists in the table among others
+    (1021, 50001, 50008, 50001, 900, 24, "indexed", True),        # logp 5 rows of two CTAs
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", SPLIT, ids=lambda c: "x".join(str(v) for v in c[:3]))
+def test_blocks_of_rows_over_several_ranges(case, dtype):
+    """The work splits of large calls, whose tables go from row to row of a block in each of several ranges (or CTAs of a cluster): all
+    four calls against the definition, at the first rows, at the last and at one block's worth of others in between."""
+    rows, V, ld, ld_out, history, bias, grammar, prefix = case
+    kind, tt = (api.BF16, torch.bfloat16) if dtype == "bf16" else (api.F32, torch.float32)
+    rng = np.random.default_rng(rows + V)
+    gen = torch.Generator(device="cuda").manual_seed(V)
+    r = make_rules(rng, rows, V, history=history, bias=bias, grammar=grammar, prefix=prefix)
+    rules = device_rules(r)
+    x = (torch.randn(rows, ld, generator=gen, device="cuda") * 3).to(tt)
+    dz = (torch.randn(rows, ld_out, generator=gen, device="cuda") * 0.01).to(tt)
+    middle = int(rng.integers(10, rows - 20))
+    sample = sorted(set(range(10)) | set(range(middle, middle + 9)) | {rows - 2, rows - 1})
+    pull = lambda t: t[sample][:, :V].float().double().cpu().numpy()
+    xs, ds = pull(x), pull(dz)
+    ref = [R.rules_row(xs[j], r, i) for j, i in enumerate(sample)]
+    z, k, e = (np.stack([t[j] for t in ref]) for j in range(3))
+    y = torch.full((rows, ld_out), 7.0, dtype=tt, device="cuda")
+    api.hilore_logits_apply(x, kind, rows, V, ld, rules, y, ld_out)
+    check(pull(y), z, e, dtype)
+    assert bool((y[:, V:] == 7).all())
+    api.hilore_logits_apply_backward(x, kind, rows, V, ld, rules, dz, ld_out, y, ld_out)
+    check(pull(y), ds * k, 4 * R.U * np.abs(ds * k), dtype)
+    targets = rng.integers(0, V, rows).astype(np.int32)
+    targets[4] = -1
+    omega = rng.standard_normal(rows).astype(np.float32)
+    omega[6] = 0
+    t, w = torch.from_numpy(targets).cuda(), torch.from_numpy(omega).cuda()
+    out = torch.zeros(3, rows, device="cuda")
+    api.hilore_token_logp(x, kind, rows, V, ld, rules, t, out[0], out[1], out[2])
+    got = out[:, sample].double().cpu().numpy()
+    grads, errors = [], []
+    for j, i in enumerate(sample):
+        want, bound = R.logp_row(z[j], targets[i]), R.logp_bound(z[j], e[j], V)
+        for q in range(3):
+            assert got[q, j] == want[q] or abs(got[q, j] - want[q]) <= bound[q] + 4 * R.U * abs(want[q]), (q, i, got[q, j], want[q])
+        finite = np.isfinite(want[1])
+        grads.append(R.grad_row(z[j], k[j], targets[i], float(omega[i]), want[1]))
+        errors.append(R.grad_bound(z[j], e[j], k[j], float(omega[i]), want[1] if finite else 0.0, bound[1] + 4 * R.U * abs(want[1]) if finite else 0.0))
+    api.hilore_token_logp_backward(x, kind, rows, V, ld, rules, t, out[1], w, y, ld_out)
+    check(pull(y), np.stack(grads), np.stack(errors), dtype)
+    api.hilore_logits_apply(x, kind, rows, V, ld, rules, x, ld)                       # in place
+    check(pull(x), z, e, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V,ld,ld_out,shift", [(1, 1, 1, 0), (31, 33, 32, 1), (2051, 2051, 2051, 0), (40003, 40003, 40010, 5), (151936, 151936, 151936, 0)])
+def test_rules_without_lists(V, ld, ld_out, shift, dtype):
+    """Temperature and a grammar alone, at equal and unequal alignments, and the temperature alone in place, forward and backward."""
+    kind, tt = (api.BF16, torch.bfloat16) if dtype == "bf16" else (api.F32, torch.float32)
+    rows = 5
+    rng = np.random.default_rng(V)
+    r = make_rules(rng, rows, V, history=-1, grammar="indexed")
+    rules = device_rules(r)
+    raw = (torch.randn(rows * ld + shift, generator=torch.Generator(device="cuda").manual_seed(V), device="cuda") * 3).to(tt)
+    x = raw[shift:].view(rows, ld)
+    host = lambda t: t[:, :V].float().double().cpu().numpy()
+    xs = host(x)
+    ref = [R.rules_row(xs[i], r, i) for i in range(rows)]
+    z, k, e = (np.stack([t[j] for t in ref]) for j in range(3))
+    y = torch.full((rows, ld_out), 7.0, dtype=tt, device="cuda")
+    api.hilore_logits_apply(x, kind, rows, V, ld, rules, y, ld_out)
+    check(host(y), z, e, dtype)
+    g = torch.randn(rows, ld_out, device="cuda").to(tt)
+    gs = host(g)
+    api.hilore_logits_apply_backward(x, kind, rows, V, ld, rules, g, ld_out, y, ld_out)
+    check(host(y), gs * k, 4 * R.U * np.abs(gs * k), dtype)
+    assert bool((y[:, V:] == 7).all())
+    api.hilore_logits_apply_backward(x, kind, rows, V, ld, rules, g, ld_out, g, ld_out)
+    assert torch.equal(g[:, :V], y[:, :V])
+    t = np.float32(r["temperature"])[:, None].astype(np.float64)
+    api.hilore_logits_apply(x, kind, rows, V, ld, api.make_logit_rules(temperature=torch.from_numpy(r["temperature"]).cuda()), x, ld)
+    check(host(x), xs / t, 4 * R.U * np.abs(xs / t), dtype)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32", "master"])
+def test_step_with_fp32_moments_has_the_same_bits_at_any_address(kind):
+    n = 3 * 1024 + 77
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    w, g = torch.randn(n, generator=gen, device="cuda") * 0.02, torch.randn(n, generator=gen, device="cuda") * 1e-3
+    done = []
+    for shift in (0, 1, 5):
+        put = lambda t: torch.cat([t.new_zeros(shift), t])[shift:]
+        e = dict(p=put(w if kind == "f32" else w.bfloat16()), g=put(g.bfloat16()), m=put(g * 0.5), v=put(g * g), weight_decay=0.1)
+        if kind == "master":
+            e["master"] = put(w)
+        dev, host = api.make_param_table([e])
+        for t in range(1, 4):
+            api.hilore_adamw_step(dev, host, 1, 0.01, None, 0.9, 0.99, 1e-8, t, None, None)
+        done.append({k: t.contiguous().view(torch.int16).int() if t.dtype == torch.bfloat16 else t.clone() for k, t in e.items() if isinstance(t, torch.Tensor)})
+    names = [k for k in done[0] if k != "g"]
+    assert same_bits(done[0], done[1], names) == [] and same_bits(done[0], done[2], names) == []
