@@ -432,7 +432,7 @@ def _typed(t, name, *dtypes):
 
 def _on_host(t):
     """Whether `t` is a tensor in host memory that kernels cannot read."""
-    return t is not None and t.device.type != "cuda" and not (t.device.type == "cpu" and t.is_pinned())
+    return t is not None and not t.is_cuda and not (t.device.type == "cpu" and t.is_pinned())
 
 
 def make_logit_rules(temperature=None, repetition=None, frequency=None, presence=None, tokens=None, hist_begin=None,
@@ -476,6 +476,7 @@ def make_param_table(params, device="cuda"):
     (params_dev tensor, params_host array); the array keeps the tensors alive."""
     kinds = {torch.bfloat16: BF16, torch.float32: F32}
     arr = (HiloreParam * len(params))()
+    to_device = torch.device(device).type == "cuda"
     first = 0
     for i, e in enumerate(params):
         p, g, m, v = (_typed(e[k], k, *t) for k, t in (("p", tuple(kinds)), ("g", tuple(kinds)),
@@ -488,7 +489,7 @@ def make_param_table(params, device="cuda"):
                               ("v_scale", vs, blocks)):
             if t is not None and t.numel() != want:
                 raise ValueError(f"entry {i}: {name} has {t.numel()} elements, expected {want}")
-            if torch.device(device).type == "cuda" and _on_host(t):
+            if to_device and _on_host(t):
                 raise ValueError(f"entry {i}: {name} is on the host, the table on {device}")
         if (v.element_size() == 1) != coded or coded != (ms is not None) or coded != (vs is not None):
             raise ValueError(f"entry {i}: m and v are both fp32 without scales, or both codes with scales")

@@ -7,11 +7,11 @@
 // row's history in a table of counts in shared memory, with a list of those that occur.  The slots of a training sequence
 // have growing prefixes of one sequence as their histories: going to the next row then adds a token or two to the table
 // instead of clearing it and scanning the history again (gradient of 2048 x 128256 bf16 rows under prefixes of up
-// to 1536 tokens: 245 us, 301 with a scan per row; the bytes alone 163).  The stream runs as if no token were listed; the listed
+// to 1536 tokens: 248 us, 301 with a scan per row; the bytes alone 163).  The stream runs as if no token were listed; the listed
 // ones are worked out on their own, one per thread, and written over the stream's results or, where a sum is wanted, left out of
 // the stream by one bit per token.  Other ways: counts asked for inside the stream, where a warp takes its listed tokens one
 // by one, took 930 us for that gradient; a hash table over a larger range, which probes and overflows, 320 us for 96 rows of 151936
-// fp32 logits with histories of up to 16384 tokens, now 60 (the bytes 19).  Counts in global memory would cost 4 bytes per
+// fp32 logits with histories of up to 16384 tokens, now 55 (the bytes 19).  Counts in global memory would cost 4 bytes per
 // logit, twice the bf16 logits themselves.
 #include "common.cuh"
 
@@ -545,8 +545,8 @@ struct MapLogpGrad { // omega (1[v = a] - exp(z - lse)) dz/dx from x
 // bits, bias entries, and a pool for the table, the list and -- where the output is the input and everything has to be read before
 // anything is stored -- the results of the listed tokens.  In that case a range is worked on as a whole where the row's lists cannot
 // outgrow what the pool leaves beside the table, otherwise in parts whose every token may be listed.
-//   hilore_logits_apply: 512 threads, two CTAs per SM (96 rows of 151936 fp32 logits, histories of up to 16384: 60 us; 70 with 256, three
-//   per SM).  The gradient of a log-probability holds more in registers: 256 (1500 x 32063 bf16
+//   hilore_logits_apply: 512 threads, two CTAs per SM (96 rows of 151936 fp32 logits, histories of up to 16384: with 256 threads, three
+//   CTAs per SM, it took 70 us where this took 60; it takes 55 now).  The gradient of a log-probability holds more in registers: 256 (1500 x 32063 bf16
 //   rows under prefixes 69 us; 94 with 512, 74 with 128, whose 12000 rows take 403 us for 416).
 template <int THREADS> struct MapShape {
     static constexpr int kStage = THREADS * 32;
@@ -727,8 +727,9 @@ struct RowLoss { // of the gradient of a log-probability
     bool live;
 };
 
-// One CTA per (block of rows, range).  2048 x 128256 bf16 rows of a gradient under prefixes: 245 us, 205 with an empty history (the
-// bytes 163); 96 rows of 151936 fp32 logits with histories of up to 16384 tokens: 58 us, 38 without (the bytes 19).  LISTS: rows may have listed tokens; otherwise a block is one row.
+// One CTA per (block of rows, range).  2048 x 128256 bf16 rows of a gradient under prefixes: 248 us, 205 with an empty history (the
+// bytes 163); 96 rows of 151936 fp32 logits with masks on half: 55 us with histories of up to 16384 tokens, 42 up to 4096, 39 up to 1024, 35
+// without, 27 without lists (the bytes 19).  In place 124, 43, 39: lists of a long history go in parts, each with a scan of its own.  LISTS: rows may have listed tokens; otherwise a block is one row.
 template <int THREADS, typename T, bool GRAD, bool LISTS>
 __global__ void __launch_bounds__(THREADS, LISTS ? MapShape<THREADS>::kCtas : sizeof(T) == 2 ? 1024 / THREADS : 768 / THREADS)
     logits_apply_kernel(const T *x, int64_t ld, const T *in, int64_t ld_in, T *out, int64_t ld_out, int64_t n_rows, int V, int block_rows, int n_ranges,
@@ -946,7 +947,7 @@ __device__ __forceinline__ void finish_row(const Soft &acc, float z, float inv_t
 
 // Without rules beyond a temperature: one pass with the running maximum, sum and mean exponent of every thread, 32 logits in
 // flight, exponentials in base 2 relative to the maximum, differences and sums in packed pairs (three quarters of 8192 rows of 151936 bf16 logits with
-// entropy 300 us, 6.2 TB/s; the exponentials alone take 207 us of their units).  A row belongs to `row_ctas` CTAs (a thread-block cluster if more than one); each takes a
+// entropy 298 us back to back, 6.3 TB/s, 364 among other work; the exponentials alone take 207 us of their units).  A row belongs to `row_ctas` CTAs (a thread-block cluster if more than one); each takes a
 // share of its vectors.
 template <typename T, bool ENTROPY>
 __global__ void __launch_bounds__(kLogpThreads, 4)
@@ -1236,7 +1237,9 @@ static bool has_lists(const hilore_logit_rules &q) { return q.tokens || q.bias_t
 
 // Work split.  A CTA takes a block of rows and a range of positions; its time is taken as proportional to
 // rows * (positions + per-row overhead) + start, the start being the scan of a history, and the split is the one with the least number of
-// rounds times that.  Overheads in positions, from fits to measured times.
+// rounds times that.  Overheads in positions, from fits to measured times.  The scan is charged once per block, as for the prefixes of
+// one sequence; the caller knows the mean length only where rows share no tokens, and there every row is scanned, which makes blocks look
+// cheaper than they are.
 struct Split {
     int64_t block_rows, width, n_ranges, grid;
 };
