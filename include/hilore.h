@@ -558,6 +558,131 @@ int hilore_adamw_step(const hilore_param *params_dev, const hilore_param *params
                       const float *lr_dev, double beta1, double beta2, double eps, int64_t step, const int64_t *step_dev,
                       const float *grad_scale, void *stream);
 
+/* ================================================================================================================
+ * From rewards to the gradient of the log-probabilities beyond hilore_grpo_coeffs: advantages and returns per token,
+ * the clipped policy loss and the preference loss.  omega is dL/ds_t in all of them, what hilore_token_logp_backward
+ * reads.  The paper has GRPO alone; the definitions are stated here.
+ *
+ * Sequences, in every call of this part:
+ *   cu_seqlens   [n_seq + 1] int32 as in hilore_grpo_coeffs_packed, or NULL: n_seq rows of n_tok / n_seq slots each
+ *                (n_tok % n_seq must be 0, HILORE_SHAPE).  cu_seqlens[0] counts as 0.  Tokens from cu_seqlens[n_seq] on
+ *                belong to no sequence: nothing of theirs is read or written, so a captured call serves batches of any
+ *                number of tokens up to n_tok.  Whatever cu_seqlens holds, no kernel indexes outside [0, n_seq] or [0, n_tok).
+ *   mask         opt [n_tok] u8 (0 / not 0); NULL: every token is valid.  Masked tokens (prompt, tool outputs, padding) may
+ *                hold anything, NaN included: they change nothing and their outputs are 0.
+ *   Tensors with an entry per token may have any address that their type allows; with fp32 at 32, bf16 at 16 and masks at 8
+ *   bytes eight tokens move at a time.  Results do not depend on that, nor on scheduling; a sequence's results do not depend
+ *   on the other sequences.  n_seq and n_tok at most 2^31 - 2^16 (HILORE_SHAPE).
+ *   workspace    the bytes of the call's .._workspace_bytes, 16-byte aligned, overwritten.
+ * ================================================================================================================ */
+
+/*
+ * Advantages and returns of every valid token, a gated linear recurrence from the end of the sequence.  Over its valid tokens
+ * k = 1 .. n (masked ones are stepped over, so tool outputs do not part a response):
+ *     A_k = r_k + q_k - V_k + gamma lambda c_k A_{k+1},   A_{n+1} = 0
+ *     q_k = gamma V_{k+1} (k < n),   q_n = outcome + gamma bootstrap;        returns_k = A_k + V_k
+ * Generalised advantage estimation at c = 1; discounted rewards to go at lambda = 1 without values.  fp64 inside, rounded once.
+ *   rewards      opt [n_tok] fp32.    outcome  opt [n_seq] fp32, the reward of the whole response, earned at its last valid token.
+ *   values       opt [n_tok] of values_dtype (HILORE_BF16 or HILORE_F32).    bootstrap  opt [n_seq] fp32, the value behind a
+ *                response that was cut short.    trace  opt [n_tok] fp32: c_k, e.g. clipped importance ratios.
+ *   gamma, lambda   in [0, 1].
+ *   adv, returns    opt [n_tok] fp32.    moments  opt [2] fp32: mean and population standard deviation of the advantages of the call's
+ *                valid tokens (0, 0 where there are none), in a fixed order of additions.  At least one of the three.
+ *   What is not finite makes the tokens before it in its sequence NaN or infinite, and no others; so do products of trace beyond fp64.
+ *
+ * hilore_advantages_backward: the gradients of sum_k (grad_adv_k A_k + grad_returns_k returns_k),
+ *     G_k = grad_adv_k + grad_returns_k + gamma lambda c_{k-1} G_{k-1};     d r_k = G_k
+ *     d V_k = grad_returns_k - G_k + gamma G_{k-1};   d c_k = gamma lambda A_{k+1} G_k;   d outcome = G_n;   d bootstrap = gamma G_n
+ * (0 for a sequence without a valid token).
+ *   grad_adv, grad_returns   opt [n_tok] fp32 (NULL: zeros).    adv  [n_tok] fp32 as written by the forward call, needed for grad_trace.
+ *   grad_rewards, grad_values, grad_trace   opt [n_tok] fp32.    grad_outcome, grad_bootstrap  opt [n_seq] fp32.
+ */
+int hilore_advantages(const float *rewards, const float *outcome, const void *values, int32_t values_dtype,
+                      const float *bootstrap, const float *trace, const uint8_t *mask, const int32_t *cu_seqlens, int64_t n_seq,
+                      int64_t n_tok, double gamma, double lambda, float *adv, float *returns, float *moments, void *workspace,
+                      size_t workspace_bytes, void *stream);
+int hilore_advantages_backward(const float *grad_adv, const float *grad_returns, const float *adv, const float *trace,
+                               const uint8_t *mask, const int32_t *cu_seqlens, int64_t n_seq, int64_t n_tok, double gamma,
+                               double lambda, float *grad_rewards, float *grad_outcome, float *grad_values,
+                               float *grad_bootstrap, float *grad_trace, void *workspace, size_t workspace_bytes, void *stream);
+size_t hilore_advantages_workspace_bytes(int64_t n_tok);
+
+/* ---- ratios, means and KL estimators of the policy loss ---- */
+enum { HILORE_RATIO_TOKEN = 0, HILORE_RATIO_SEQUENCE = 1 };
+enum { HILORE_MEAN_TOKENS = 0, HILORE_MEAN_SEQUENCES = 1 };
+enum { HILORE_KL_K1 = 1, HILORE_KL_K2 = 2, HILORE_KL_K3 = 3 };
+
+/* What a policy loss is made of.  A HOST struct, read during the call. */
+typedef struct hilore_policy_terms {
+    double clip_low, clip_high; /* the ratio is held in [1 - clip_low, 1 + clip_high]; clip_low in [0, 1], clip_high >= 0, Inf: no bound */
+    double dual_clip;           /* 0: none; c >= 1: at A < 0 the ratio counts as c at most                  */
+    double beta;                /* weight of the KL term                                                    */
+    double rollout_cap;         /* > 0; most that a rollout weight may be (Inf: no bound)                   */
+    double adv_eps;             /* >= 0; added to the standard deviation where advantages are whitened      */
+    int32_t ratio, mean, kl;    /* HILORE_RATIO_.., HILORE_MEAN_.., HILORE_KL_..                            */
+    int32_t adv_per_token;      /* 1: adv has an entry per token, 0: per sequence (always 0 for HILORE_RATIO_SEQUENCE) */
+} hilore_policy_terms;
+
+/*
+ * Clipped policy loss over the valid tokens of a call and its gradient, forward and backward in one call:
+ *     rho = exp(s - s_old) per token, or exp(mean over the sequence's valid tokens of s - s_old) for HILORE_RATIO_SEQUENCE
+ *     u   = A >= 0: min(rho, 1 + clip_high);   A < 0: min(max(rho, 1 - clip_low), dual_clip)
+ *     i   = min(rollout_cap, exp(s_old - s_rollout)), of the sequence's mean likewise; a constant, 1 without logp_rollout
+ *     kl  = with e = s_ref - s:  K1 -e,  K2 e^2 / 2,  K3 exp(e) - e - 1
+ *     w   = 1 / N (HILORE_MEAN_TOKENS), 1 / (N |T_s|) with the sequence's valid tokens |T_s| (HILORE_MEAN_SEQUENCES)
+ *     L   = sum_t w ( -i A u + beta kl );     omega_t = dL/ds_t * grad_loss
+ * On a flat branch (u a bound) the policy term's gradient is exactly 0; rho on its bound is not beyond it.  Which side a
+ * token is on is decided on s - s_old in fp64, so it is decided as the formula does.
+ *   logp, logp_old   [n_tok] fp32.    logp_ref  opt [n_tok] fp32, needed unless beta = 0.    logp_rollout  opt [n_tok] fp32,
+ *                    what the engine that sampled reported.
+ *   adv              [n_tok] or [n_seq] fp32.    adv_moments  opt [2] fp32 as written by hilore_advantages:
+ *                    A = (adv - mean) / (standard deviation + adv_eps).
+ *   N_norm, N_norm_dev   as in hilore_grpo_coeffs: the whole batch's valid tokens or its sequences, so that the losses and
+ *                    gradients of microbatches add up.
+ *   grad_loss        opt one fp32 on the device: the gradient of L itself (loss scaling).  1 if NULL.
+ *   stats            [5] fp32, sums of this call: L; its policy term; sum w kl (0 without logp_ref); sum w over the tokens with A != 0
+ *                    on a flat branch; sum w (s_old - s).
+ *   omega            [n_tok] fp32.
+ */
+int hilore_policy_loss(const float *logp, const float *logp_old, const float *logp_ref, const float *logp_rollout,
+                       const uint8_t *mask, const float *adv, const float *adv_moments, const int32_t *cu_seqlens, int64_t n_seq,
+                       int64_t n_tok, const hilore_policy_terms *terms, int64_t N_norm, const int64_t *N_norm_dev,
+                       const float *grad_loss, float *stats, float *omega, void *workspace, size_t workspace_bytes, void *stream);
+size_t hilore_policy_loss_workspace_bytes(int64_t n_seq, int64_t n_tok);
+
+enum { HILORE_PREF_SIGMOID = 0, HILORE_PREF_HINGE = 1, HILORE_PREF_SQUARE = 2 };
+
+/* What a preference loss is made of.  A HOST struct, read during the call. */
+typedef struct hilore_preference_terms {
+    double beta;                  /* > 0, scale of the scores                                                    */
+    double margin, margin_reward; /* the gap asked for: margin + margin_reward (R_w - R_l)                       */
+    double smoothing;             /* in [0, 1], HILORE_PREF_SIGMOID alone: share of pairs taken the other way round */
+    double nll;                   /* weight of the winners' negative log-likelihood                              */
+    int32_t loss, length_mean;    /* HILORE_PREF_..; 1: scores are means over a response's tokens, 0: sums       */
+} hilore_preference_terms;
+
+/*
+ * Preference loss on pairs of responses to the same prompt, and its gradient.  The G responses of prompt p are sequences
+ * p*G .. p*G+G-1; each pair of them with R_w > R_l counts (G = 2 with rewards 1 and 0: chosen and rejected), unless one of
+ * the two has no valid token or a reward is NaN:
+ *     h  = beta * sum (or mean) over the valid tokens of s - s_ref
+ *     z  = h_w - h_l - margin - margin_reward (R_w - R_l)
+ *     l  = SIGMOID -(1 - smoothing) ln sigma(z) - smoothing ln sigma(-z);   HINGE max(0, 1 - z);   SQUARE ((z - 1/2) / beta)^2
+ *     L  = 1/N sum over pairs of ( l + nll * (-mean over the winner's valid tokens of s) );     omega_t = dL/ds_t * grad_loss
+ *   logp         [n_tok] fp32.    logp_ref  opt [n_tok] fp32 (NULL: without a reference).    rewards  [n_seq] fp32.
+ *                G in [1, 1024], n_seq % G must be 0 (HILORE_SHAPE).
+ *   N_norm, N_norm_dev   pairs of the whole batch; N_norm = 0: those of this call.  A device value <= 0 gives omega = 0 and stats 0.
+ *   scores       opt [n_seq] fp32: h (0 without a valid token).    pairs  opt one int64 on the device: the pairs of this call.
+ *   stats        [4] fp32, each the sum over this call's pairs divided by N: L; pairs with h_w > h_l; h_w - h_l; the mean
+ *                above, -mean s of the winner.
+ *   omega        [n_tok] fp32.    grad_loss as in hilore_policy_loss.
+ */
+int hilore_preference_loss(const float *logp, const float *logp_ref, const uint8_t *mask, const float *rewards, int32_t G,
+                           const int32_t *cu_seqlens, int64_t n_seq, int64_t n_tok, const hilore_preference_terms *terms,
+                           int64_t N_norm, const int64_t *N_norm_dev, const float *grad_loss, float *scores, int64_t *pairs,
+                           float *stats, float *omega, void *workspace, size_t workspace_bytes, void *stream);
+size_t hilore_preference_loss_workspace_bytes(int64_t n_seq, int64_t n_tok);
+
 #ifdef __cplusplus
 }
 #endif

@@ -23,6 +23,10 @@ BLOCK = 64
 BF16, F32 = 0, 1
 STATE_F32, STATE_E4M3FN = 0, 1
 PARAM_TILE = 1024
+RATIO_TOKEN, RATIO_SEQUENCE = 0, 1
+MEAN_TOKENS, MEAN_SEQUENCES = 0, 1
+KL_K1, KL_K2, KL_K3 = 1, 2, 3
+PREF_SIGMOID, PREF_HINGE, PREF_SQUARE = 0, 1, 2
 
 EXPORTS = ("hilore_status_string", "hilore_abi_version", "hilore_mask_count", "hilore_grpo_coeffs",
            "hilore_unit_exposure", "hilore_workspace_bytes", "hilore_compress", "hilore_recover",
@@ -33,7 +37,9 @@ EXPORTS = ("hilore_status_string", "hilore_abi_version", "hilore_mask_count", "h
            "hilore_grpo_coeffs_packed", "hilore_unit_exposure_packed", "hilore_codec_relative_error",
            "hilore_coeffs_exposure", "hilore_scores_plan", "hilore_scores_plan_workspace_bytes",
            "hilore_logits_apply", "hilore_logits_apply_backward", "hilore_token_logp", "hilore_token_logp_backward",
-           "hilore_grad_norm", "hilore_grad_norm_workspace_bytes", "hilore_adamw_step")
+           "hilore_grad_norm", "hilore_grad_norm_workspace_bytes", "hilore_adamw_step",
+           "hilore_advantages", "hilore_advantages_backward", "hilore_advantages_workspace_bytes", "hilore_policy_loss",
+           "hilore_policy_loss_workspace_bytes", "hilore_preference_loss", "hilore_preference_loss_workspace_bytes")
 
 
 class HiloreUnit(C.Structure):
@@ -58,6 +64,19 @@ class HiloreParam(C.Structure):
     _fields_ = [("p", C.c_void_p), ("master", C.c_void_p), ("g", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
                 ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("n", C.c_int64), ("first", C.c_int64),
                 ("p_dtype", C.c_int32), ("g_dtype", C.c_int32), ("state", C.c_int32), ("weight_decay", C.c_float)]
+
+
+class HilorePolicyTerms(C.Structure):
+    """Mirror of ``struct hilore_policy_terms``."""
+    _fields_ = [("clip_low", C.c_double), ("clip_high", C.c_double), ("dual_clip", C.c_double), ("beta", C.c_double),
+                ("rollout_cap", C.c_double), ("adv_eps", C.c_double), ("ratio", C.c_int32), ("mean", C.c_int32), ("kl", C.c_int32),
+                ("adv_per_token", C.c_int32)]
+
+
+class HilorePreferenceTerms(C.Structure):
+    """Mirror of ``struct hilore_preference_terms``."""
+    _fields_ = [("beta", C.c_double), ("margin", C.c_double), ("margin_reward", C.c_double), ("smoothing", C.c_double),
+                ("nll", C.c_double), ("loss", C.c_int32), ("length_mean", C.c_int32)]
 
 
 class HiloreError(RuntimeError):
@@ -131,8 +150,19 @@ def lib() -> C.CDLL:
         _lib.hilore_grad_norm_workspace_bytes.restype = C.c_size_t
         _lib.hilore_grad_norm_workspace_bytes.argtypes = []
         _lib.hilore_adamw_step.argtypes = [vp, vp, i32, C.c_double, vp, C.c_double, C.c_double, C.c_double, i64, vp, vp, vp]
+        f64, sz = C.c_double, C.c_size_t
+        _lib.hilore_advantages.argtypes = [vp, vp, vp, i32, vp, vp, vp, vp, i64, i64, f64, f64, vp, vp, vp, vp, sz, vp]
+        _lib.hilore_advantages_backward.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, f64, f64, vp, vp, vp, vp, vp, vp, sz, vp]
+        _lib.hilore_policy_loss.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i64, i64, vp, i64, vp, vp, vp, vp, vp, sz, vp]
+        _lib.hilore_preference_loss.argtypes = [vp, vp, vp, vp, i32, vp, i64, i64, vp, i64, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        _lib.hilore_advantages_workspace_bytes.argtypes = [i64]
+        for name in ("hilore_policy_loss_workspace_bytes", "hilore_preference_loss_workspace_bytes"):
+            getattr(_lib, name).argtypes = [i64, i64]
+        for name in ("hilore_advantages_workspace_bytes", "hilore_policy_loss_workspace_bytes", "hilore_preference_loss_workspace_bytes"):
+            getattr(_lib, name).restype = sz
         for name in EXPORTS:
-            if name not in ("hilore_grad_norm_workspace_bytes", "hilore_status_string", "hilore_workspace_bytes", "hilore_static_scratch_bytes",
+            if name not in ("hilore_advantages_workspace_bytes", "hilore_policy_loss_workspace_bytes",
+                            "hilore_preference_loss_workspace_bytes", "hilore_grad_norm_workspace_bytes", "hilore_status_string", "hilore_workspace_bytes", "hilore_static_scratch_bytes",
                             "hilore_allocate_workspace_bytes", "hilore_risk_budget",
                             "hilore_relative_error_workspace_bytes", "hilore_fit_kappa",
                             "hilore_omega_diagnostics_workspace_bytes", "hilore_scores_plan_workspace_bytes"):
@@ -419,6 +449,74 @@ def hilore_adamw_step(params_dev, params_host, n_params, lr, lr_dev, beta1, beta
     st = lib().hilore_adamw_step(_ptr(params_dev), _table(params_host, n_params), n_params, lr, _ptr(lr_dev), beta1, beta2, eps, step,
                                  _ptr(step_dev), _ptr(grad_scale), _stream(stream))
     return _check(st, "hilore_adamw_step", check)
+
+
+def hilore_advantages_workspace_bytes(n_tok):
+    return int(lib().hilore_advantages_workspace_bytes(n_tok))
+
+
+def hilore_advantages(rewards, outcome, values, values_dtype, bootstrap, trace, mask, cu_seqlens, n_seq, n_tok, gamma, lam, adv,
+                      returns, moments, workspace, workspace_bytes, stream=None, check=True):
+    st = lib().hilore_advantages(_ptr(rewards), _ptr(outcome), _ptr(values), values_dtype, _ptr(bootstrap), _ptr(trace), _ptr(mask),
+                                 _ptr(cu_seqlens), n_seq, n_tok, gamma, lam, _ptr(adv), _ptr(returns), _ptr(moments),
+                                 _ptr(workspace), workspace_bytes, _stream(stream))
+    return _check(st, "hilore_advantages", check)
+
+
+def hilore_advantages_backward(grad_adv, grad_returns, adv, trace, mask, cu_seqlens, n_seq, n_tok, gamma, lam, grad_rewards,
+                               grad_outcome, grad_values, grad_bootstrap, grad_trace, workspace, workspace_bytes, stream=None,
+                               check=True):
+    st = lib().hilore_advantages_backward(_ptr(grad_adv), _ptr(grad_returns), _ptr(adv), _ptr(trace), _ptr(mask), _ptr(cu_seqlens),
+                                          n_seq, n_tok, gamma, lam, _ptr(grad_rewards), _ptr(grad_outcome), _ptr(grad_values),
+                                          _ptr(grad_bootstrap), _ptr(grad_trace), _ptr(workspace), workspace_bytes, _stream(stream))
+    return _check(st, "hilore_advantages_backward", check)
+
+
+def _terms(terms, kind):
+    """Address of a struct of terms, or None."""
+    if terms is None:
+        return None
+    if not isinstance(terms, kind):
+        raise TypeError(f"terms: expected {kind.__name__}, got {type(terms).__name__}")
+    return C.addressof(terms)
+
+
+def make_policy_terms(clip_low=0.2, clip_high=0.2, dual_clip=0.0, beta=0.0, rollout_cap=float("inf"), adv_eps=1e-6,
+                      ratio=RATIO_TOKEN, mean=MEAN_TOKENS, kl=KL_K3, adv_per_token=False):
+    """The host struct that hilore_policy_loss reads."""
+    return HilorePolicyTerms(clip_low, clip_high, dual_clip, beta, rollout_cap, adv_eps, ratio, mean, kl, int(adv_per_token))
+
+
+def make_preference_terms(beta=0.1, margin=0.0, margin_reward=0.0, smoothing=0.0, nll=0.0, loss=PREF_SIGMOID, length_mean=False):
+    """The host struct that hilore_preference_loss reads."""
+    return HilorePreferenceTerms(beta, margin, margin_reward, smoothing, nll, loss, int(length_mean))
+
+
+def hilore_policy_loss_workspace_bytes(n_seq, n_tok):
+    return int(lib().hilore_policy_loss_workspace_bytes(n_seq, n_tok))
+
+
+def hilore_policy_loss(logp, logp_old, logp_ref, logp_rollout, mask, adv, adv_moments, cu_seqlens, n_seq, n_tok, terms, N_norm,
+                       N_norm_dev, grad_loss, stats, omega, workspace, workspace_bytes, stream=None, check=True):
+    """terms: make_policy_terms."""
+    st = lib().hilore_policy_loss(_ptr(logp), _ptr(logp_old), _ptr(logp_ref), _ptr(logp_rollout), _ptr(mask), _ptr(adv),
+                                  _ptr(adv_moments), _ptr(cu_seqlens), n_seq, n_tok, _terms(terms, HilorePolicyTerms), N_norm,
+                                  _ptr(N_norm_dev), _ptr(grad_loss), _ptr(stats), _ptr(omega), _ptr(workspace), workspace_bytes,
+                                  _stream(stream))
+    return _check(st, "hilore_policy_loss", check)
+
+
+def hilore_preference_loss_workspace_bytes(n_seq, n_tok):
+    return int(lib().hilore_preference_loss_workspace_bytes(n_seq, n_tok))
+
+
+def hilore_preference_loss(logp, logp_ref, mask, rewards, G, cu_seqlens, n_seq, n_tok, terms, N_norm, N_norm_dev, grad_loss, scores,
+                           pairs, stats, omega, workspace, workspace_bytes, stream=None, check=True):
+    """terms: make_preference_terms."""
+    st = lib().hilore_preference_loss(_ptr(logp), _ptr(logp_ref), _ptr(mask), _ptr(rewards), G, _ptr(cu_seqlens), n_seq, n_tok,
+                                      _terms(terms, HilorePreferenceTerms), N_norm, _ptr(N_norm_dev), _ptr(grad_loss), _ptr(scores),
+                                      _ptr(pairs), _ptr(stats), _ptr(omega), _ptr(workspace), workspace_bytes, _stream(stream))
+    return _check(st, "hilore_preference_loss", check)
 
 
 def _typed(t, name, *dtypes):

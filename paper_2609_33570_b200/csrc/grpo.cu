@@ -1639,7 +1639,7 @@ extern "C" const char *hilore_status_string(int status)
     }
 }
 
-extern "C" int hilore_abi_version(void) { return 1001; }
+extern "C" int hilore_abi_version(void) { return 1002; }
 
 // ------------------------------------------------------------------ exposure without caller scratch
 // Some callers cannot hand over a workspace: a saved-tensor hook that runs while the framework's
