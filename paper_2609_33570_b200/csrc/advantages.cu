@@ -1,4 +1,5 @@
 // Advantages and returns by a gated linear recurrence over the valid tokens of a sequence, and the backward pass of it.
+#include <algorithm>
 #include <cmath>
 
 #include "segments.cuh"
@@ -32,6 +33,7 @@ struct AdvantageOp {
         if (m.flag == 2) return State{m.B, m.c};
         return State{fma(m.P, s.x, fma(m.Q, s.q, m.B)), m.c};
     }
+    static __device__ __forceinline__ double last_weight(const Map &, double w) { return w; }
 };
 
 // From the first valid token of a sequence on, with y = w G of the valid token before and G its gradient:
@@ -62,8 +64,18 @@ struct AdvantageGradOp {
         const double G = m.flag == 2 ? m.B : fma(m.P, s.y, m.B);
         return State{m.wl * G, G, m.pos, 0};
     }
+    static __device__ __forceinline__ double last_weight(const Map &m, double w) { return m.flag ? m.wl : w; }
 };
 
+constexpr int kAdvThreads = 128; // four warps that know nothing of one another but at the end
+constexpr int kAdvWarps = kAdvThreads / 32;
+constexpr int kStages = 3;       // blocks of 256 tokens that a warp has in flight or at work
+constexpr uint32_t kAll = 0xFFFFFFFFu;
+
+// How the work is dealt out.  A warp owns the pieces that begin in its chunk of tokens.  A piece is a whole sequence, or `piece`
+// tokens (the last one fewer) of a longer one, so nothing but long sequences needs more than one pass: their pieces' maps are
+// made first, by a launch that has nothing to read where no sequence is long.  piece >= chunk, so no chunk holds the beginnings
+// of two pieces that are not the first of their sequence (or not the last), and a map's place is its chunk.
 struct AdvantageArgs {
     Sequences q;
     const float *rewards, *outcome, *bootstrap, *trace;
@@ -71,40 +83,36 @@ struct AdvantageArgs {
     int values_bf16;
     const uint8_t *mask;
     double gamma, weight; // gamma lambda
+    double small[9];      // weight^0 .. weight^8
+    double powers[5];     // weight^8, ^16, .. ^128
     float *adv, *returns;
     const float *grad_adv, *grad_returns, *adv_in;
     float *grad_rewards, *grad_outcome, *grad_values, *grad_bootstrap, *grad_trace;
-    void *maps;       // [tiles] maps of whole tiles
-    double *partials; // [tiles][3] count, mean, sum of squared deviations
-    int tiles, vec, moments;
+    void *maps;       // [chunks]
+    double *partials; // [CTAs][3] count, mean, sum of squared deviations
+    int chunks, chunk, piece, vec, moments;
 };
 
-// The state that comes into tile `tile`: back over the tiles before it (`dir` away) to the one that holds the end of a sequence,
-// then forward again, one map after the other, so that the bits do not depend on where the walk began.  By one warp; every
-// lane returns it.
-template <typename Op> __device__ typename Op::State state_into(const typename Op::Map *maps, int tile, int tiles, int dir, int lane)
+// The first beginning of a piece at or behind token t, or the end of the last sequence.
+__device__ __forceinline__ int piece_from(const AdvantageArgs &a, int t, int s, int live)
 {
-    using Map = typename Op::Map;
-    typename Op::State s = Op::start();
-    int far = tile;
-    for (;;) {
-        const int t = far + dir * (lane + 1);
-        const bool in = t >= 0 && t < tiles;
-        const uint32_t stop = __ballot_sync(0xFFFFFFFFu, !in || maps[in ? t : 0].flag == 2);
-        if (stop) {
-            far += dir * __ffs(stop);
-            break;
-        }
-        far += dir * 32;
-    }
-    // far: a tile with a sequence's end, or one step past the last tile
-    const int n = (far - tile) * dir; // tiles tile + dir .. far
-    for (int done = 0; done < n; done += 32) {
-        const int k = n - done < 32 ? n - done : 32;
-        const int t = far - dir * (done + lane);
-        Map m = Op::identity();
-        if (lane < k && t >= 0 && t < tiles) m = maps[t];
-        for (int j = 0; j < k; ++j) s = Op::apply(shfl_words(m, j), s);
+    if (t >= live) return live;
+    const int b = a.q.bound(s), e = a.q.bound(s + 1);
+    const int64_t p = b + ((int64_t)t - b + a.piece - 1) / a.piece * a.piece;
+    const int64_t at = p < e ? p : e;
+    return (int)(at < t ? t : (at > live ? live : at)); // boundaries out of order stay inside
+}
+
+// The state behind maps of `n` pieces, the piece of lane 0 first; maps(i) gives the map of piece i.
+template <typename Op, typename F> __device__ __forceinline__ typename Op::State behind_pieces(typename Op::State s, int64_t n, int lane, F maps, double &wl)
+{
+    for (int64_t done = 0; done < n; done += 32) {
+        typename Op::Map m = Op::identity(), all;
+        if (done + lane < n) m = maps(done + lane);
+        warp_scan<Op>(m, lane, all);
+        all = shfl_words(all, 31);
+        s = Op::apply(all, s);
+        wl = Op::last_weight(all, wl);
     }
     return s;
 }
@@ -131,244 +139,622 @@ __device__ __forceinline__ Moments warp_join(Moments m)
 #pragma unroll
     for (int by = 1; by < 32; by *= 2) {
         Moments o;
-        o.n = __shfl_down_sync(0xFFFFFFFFu, m.n, by);
-        o.mean = __shfl_down_sync(0xFFFFFFFFu, m.mean, by);
-        o.m2 = __shfl_down_sync(0xFFFFFFFFu, m.m2, by);
+        o.n = __shfl_down_sync(kAll, m.n, by);
+        o.mean = __shfl_down_sync(kAll, m.mean, by);
+        o.m2 = __shfl_down_sync(kAll, m.m2, by);
         m.join(o); // lane 0 has all of them in the end; what others have is not used
     }
     return m;
 }
 
-// One tile of 2048 tokens per CTA, the last tokens in the first threads.  MAPS: write the tile's map alone.  Otherwise the outputs,
-// with the maps of the other tiles complete.
-template <bool MAPS> __global__ void __launch_bounds__(kSegThreads) advantage_kernel(const __grid_constant__ AdvantageArgs a)
+// x' = P x + B over the lanes: this lane's from those before it (all the lanes' in the last one).
+struct Line {
+    double P, B;
+};
+__device__ __forceinline__ Line scan_lines(Line &m, int lane)
+{
+#pragma unroll
+    for (int by = 1; by < 32; by *= 2) {
+        const double P = __shfl_up_sync(kAll, m.P, by), B = __shfl_up_sync(kAll, m.B, by);
+        if (lane >= by) {
+            m.B = fma(m.P, B, m.B);
+            m.P *= P;
+        }
+    }
+    Line before;
+    before.P = __shfl_up_sync(kAll, m.P, 1);
+    before.B = __shfl_up_sync(kAll, m.B, 1);
+    return lane == 0 ? Line{1.0, 0.0} : before;
+}
+
+// The same where every lane's P is powers[0].
+__device__ __forceinline__ double scan_even(double B, const double (&powers)[5], int lane)
+{
+#pragma unroll
+    for (int i = 0; i < 5; ++i) {
+        const double before = __shfl_up_sync(kAll, B, 1 << i);
+        if (lane >= (1 << i)) B = fma(powers[i], before, B);
+    }
+    const double before = __shfl_up_sync(kAll, B, 1);
+    return lane == 0 ? 0.0 : before;
+}
+
+// A warp's way through the blocks of 256 tokens of [begin, end), from the last to the first (BACK: lane 0 has the last eight) or from
+// the first to the last.  Masks are read a block ahead of the tensors, and tokens that no bit asks for are not read.
+template <bool BACK, int TENSORS> struct Feed {
+    Stage8 (*stage)[TENSORS]; // [kStages]
+    const uint8_t *mask;
+    int begin, end, n_tok, lane, blocks, edge, at;
+    uint32_t pipe; // eight bits of each of the next kStages blocks
+    uint2 raw;
+    bool vec;
+
+    __device__ __forceinline__ int block(int i) const { return BACK ? edge - i : edge + i; }
+    __device__ __forceinline__ int place(int i) const { return (block(i) << 8) + (BACK ? 31 - lane : lane) * 8; }
+    __device__ __forceinline__ uint2 bytes(int i) const
+    {
+        if (i >= blocks) return make_uint2(0u, 0u);
+        const int k = place(i);
+        return k + 8 <= begin || k >= end ? make_uint2(0u, 0u) : mask_bytes(mask, k, n_tok, vec);
+    }
+    template <typename F> __device__ __forceinline__ void ask(int i, int into, uint2 w, int slot, F fetch)
+    {
+        const uint32_t v = i < blocks ? mask_bits(w) & range_bits(place(i), begin, end) : 0u;
+        pipe |= v << (8 * slot);
+        if (v) fetch(stage[into], place(i));
+        copy_commit();
+    }
+    template <typename F> __device__ __forceinline__ void start(F fetch)
+    {
+        edge = BACK ? (end - 1) >> 8 : begin >> 8;
+        blocks = ((end - 1) >> 8) - (begin >> 8) + 1;
+        pipe = 0;
+        at = 0;
+        uint2 w[kStages];
+#pragma unroll
+        for (int i = 0; i < kStages; ++i) w[i] = bytes(i);
+        raw = bytes(kStages);
+#pragma unroll
+        for (int i = 0; i < kStages; ++i) ask(i, i, w[i], i, fetch);
+    }
+    // The bits of block i; its tensors are in stage[at].
+    __device__ __forceinline__ uint32_t arrive()
+    {
+        const uint32_t v = pipe & 0xFFu;
+        pipe >>= 8;
+        copy_wait<kStages - 1>();
+        return v;
+    }
+    template <typename F> __device__ __forceinline__ void release(int i, F fetch)
+    {
+        ask(i + kStages, at, raw, kStages - 1, fetch);
+        raw = bytes(i + kStages + 1);
+        at = at + 1 == kStages ? 0 : at + 1;
+    }
+};
+
+// Bits of the tokens of block [base, base + 256) that end their sequence, with another beginning inside (lo, hi); the eight of lane
+// `of`.  Sequences are walked from `s` on, up or down, and s becomes the one that holds the block's last (first) token.
+template <bool BACK, typename F>
+__device__ __forceinline__ uint32_t ends_inside(const Sequences &q, int base, int lo, int hi, int lane, int of, int &s, F passed)
+{
+    uint32_t mine = 0;
+    for (;;) {
+        const int64_t o = (int64_t)s + (BACK ? -lane : lane);
+        // the token at which sequence o (BACK) or the one behind it begins
+        const int p = BACK ? (o >= 0 ? q.bound((int)o) : 0) : (o < q.n_seq ? q.bound((int)o + 1) : 0x7FFFFFFF);
+        const uint32_t out = __ballot_sync(kAll, BACK ? p <= lo : p >= hi);
+        const int n = out ? __ffs(out) - 1 : 32;
+        if (lane < n) passed((int)o, p);
+        for (int j = 0; j < n; ++j) {
+            const int at = __shfl_sync(kAll, p, j) - 1 - base;
+            if ((at >> 3) == of) mine |= 1u << (at & 7);
+        }
+        s += BACK ? -n : n;
+        if (out) break;
+    }
+    if (s < 0) s = 0;
+    if (s >= q.n_seq) s = (int)q.n_seq - 1;
+    return mine;
+}
+
+// MAPS: the map of the piece that begins in the chunk and is not its sequence's first.  Otherwise the outputs.
+//   Blocks inside one sequence (nearly all): a lane's rightmost valid token takes the discounted value that follows it from the
+//   nearest lane to the right, so that each lane's tokens are x' = P x + B; a scan of these gives every lane what comes in.
+//   Blocks with a sequence's end inside go through the general maps.
+template <bool TRACE, bool MOMENTS, bool MAPS> __global__ void __launch_bounds__(kAdvThreads, TRACE ? 5 : 6) advantage_kernel(const __grid_constant__ AdvantageArgs a)
 {
     using Op = AdvantageOp;
-    __shared__ TileShared sh;
-    __shared__ Op::Map totals[kSegWarps];
-    __shared__ Op::State incoming;
-    __shared__ Moments moments[kSegWarps];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, tile = blockIdx.x;
+    constexpr int kTensors = TRACE ? 3 : 2;
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ Moments joined[kAdvWarps];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, chunk = blockIdx.x * kAdvWarps + warp;
     grid_dependency_wait();
     grid_dependency_release();
-    const int lo = tile * kSegTile, live = a.q.live(), hi = live - lo < kSegTile ? live : lo + kSegTile;
-    if (hi <= lo) { // behind the last sequence
-        if (tid == 0) {
-            if (MAPS) static_cast<Op::Map *>(a.maps)[tile] = Op::identity();
-            else if (a.moments)
-                for (int i = 0; i < 3; ++i) a.partials[3 * tile + i] = 0.0;
+    const int live = a.q.live();
+    double n = 0.0, shift = 0.0, sum = 0.0, squares = 0.0; // moments about a value of the warp's own,
+    bool known = false;                                    // once there is one
+    if (chunk < a.chunks && (int64_t)chunk * a.chunk < live) {
+        const int t0 = chunk * a.chunk, t1 = live - t0 < a.chunk ? live : t0 + a.chunk;
+        int s, s1, begin, end, cur = 0; // cur: where the current sequence begins
+        a.q.owner_warp2(t0, t1 < live ? t1 : t1 - 1, lane, s, s1);
+        Op::State st = Op::start();
+        auto terminal = [&](int o) -> double {
+            return (a.outcome ? (double)__ldg(a.outcome + o) : 0.0) + a.gamma * (a.bootstrap ? (double)__ldg(a.bootstrap + o) : 0.0);
+        };
+        if (MAPS) {
+            const int b = a.q.bound(s), e = a.q.bound(s + 1);
+            const int64_t after = (int64_t)t0 - b > a.piece ? ((int64_t)t0 - b + a.piece - 1) / a.piece : 1, p = b + after * a.piece;
+            begin = end = 0;
+            if (p >= t0 && p < t1 && p < e) begin = (int)p, end = e - begin < a.piece ? e : begin + a.piece;
+        } else {
+            begin = piece_from(a, t0, s, live);
+            end = piece_from(a, t1, s1, live);
+            if (end > begin) {
+                s = s1;
+                cur = a.q.bound(s);
+                if (cur >= end) s = a.q.owner_warp(end - 1, lane), cur = a.q.bound(s);
+                st.q = terminal(s);
+                const int e = a.q.bound(s + 1);
+                const int64_t behind = e > end ? ((int64_t)e - end + a.piece - 1) / a.piece : 0;
+                double none = 0.0;
+                st = behind_pieces<Op>(st, behind, lane, [&](int64_t i) {
+                    return static_cast<const Op::Map *>(a.maps)[(end + (behind - 1 - i) * a.piece) / a.chunk]; }, none);
+            }
         }
-        return;
-    }
-    const int block = kSegThreads - 1 - tid, k = lo + block * kSegEach;
-    float r[8], v[8], c[8];
-    const uint32_t valid = load_mask8(a.mask, k, hi, a.vec);
-    if (a.rewards) load8(a.rewards, k, hi, a.vec, r);
-    if (a.values) {
-        if (a.values_bf16) load8(static_cast<const uint16_t *>(a.values), k, hi, a.vec, v);
-        else load8(static_cast<const float *>(a.values), k, hi, a.vec, v);
-    }
-    if (a.trace) load8(a.trace, k, hi, a.vec, c);
+        if (end > begin) {
+            Feed<true, kTensors> feed;
+            feed.stage = reinterpret_cast<Stage8 (*)[kTensors]>(smem) + warp * kStages;
+            feed.mask = a.mask, feed.begin = begin, feed.end = end, feed.n_tok = (int)a.q.n_tok, feed.lane = lane, feed.vec = a.vec;
+            auto fetch = [&](Stage8 (&to)[kTensors], int k) {
+                const int all = (int)a.q.n_tok;
+                if (a.rewards) fetch8(to[0], lane, a.rewards, k, all, a.vec);
+                if (a.values) {
+                    if (a.values_bf16) fetch8(to[1], lane, static_cast<const uint16_t *>(a.values), k, all, a.vec);
+                    else fetch8(to[1], lane, static_cast<const float *>(a.values), k, all, a.vec);
+                }
+                if (TRACE) fetch8(to[kTensors - 1], lane, a.trace, k, all, a.vec);
+            };
+            feed.start(fetch);
+            double P_all = 1.0, w_right = a.weight, ahead = 1.0; // MAPS: product of the weights but the rightmost one's, and that; weight^(8 lane)
+            int64_t count = 0;
+            if (!TRACE)
+                for (int i = 0; i < 5; ++i)
+                    if (lane >> i & 1) ahead *= a.powers[i];
+            for (int i = 0; i < feed.blocks; ++i) {
+                const uint32_t valid = feed.arrive();
+                const int base = feed.block(i) << 8, k = feed.place(i), lo = max(base, begin), hi = min(base + 256, end);
+                float r[8], v[8], c[8], adv[8], ret[8];
+                if (!MAPS && cur >= hi) { // on to the sequence before, whose end is where this block ends
+                    s = a.q.owner_warp(hi - 1, lane);
+                    cur = a.q.bound(s);
+                    st = Op::State{0.0, terminal(s)};
+                }
+                const uint32_t some = __ballot_sync(kAll, valid != 0);
+                if (some == 0 && (MAPS || cur <= lo)) {
+                    zero8(adv);
+                    zero8(ret);
+                } else {
+                    const Stage8 *x = feed.stage[feed.at];
+                    if (a.rewards) read8(x[0], lane, r);
+                    else zero8(r);
+                    if (!a.values) zero8(v);
+                    else if (a.values_bf16) read8_bf16(x[1], lane, v);
+                    else read8(x[1], lane, v);
+                    if (TRACE) read8(x[kTensors - 1], lane, c);
+                    double D[8];
+                    if (MAPS || cur <= lo) {
+                        if (!TRACE && __all_sync(kAll, valid == 0xFFu)) {
+                            const double first = a.gamma * (double)v[0], from = __shfl_up_sync(kAll, first, 1);
+                            double q = lane == 0 ? st.q : from, B = 0.0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        if (!a.rewards) r[e] = 0.0f;
-        if (!a.values) v[e] = 0.0f;
-        if (!a.trace) c[e] = 1.0f;
-    }
-    tile_sequences(a.q, lo, hi, sh);
-    const uint32_t ends = block_ends(sh, block);
-    auto terminal = [&](int p) -> double {
-        if (!a.outcome && !a.bootstrap) return 0.0;
-        const int s = a.q.owner(p, sh.s0, sh.s1);
-        return (a.outcome ? (double)a.outcome[s] : 0.0) + a.gamma * (a.bootstrap ? (double)a.bootstrap[s] : 0.0);
-    };
-    Op::Map mine = Op::identity();
+                            for (int e = 7; e >= 0; --e) {
+                                const double V = (double)v[e];
+                                D[e] = ((double)r[e] - V) + q;
+                                q = a.gamma * V;
+                                B = fma(a.weight, B, D[e]);
+                            }
+                            double z = fma(ahead, st.x, scan_even(B, a.powers, lane));
 #pragma unroll
-    for (int e = 7; e >= 0; --e) {
-        if (ends >> e & 1) mine = Op::Map{0.0, 0.0, 0.0, terminal(k + e), 2u, 0u};
-        if (valid >> e & 1) {
-            const double w = a.weight * (double)c[e], d = (double)r[e] - (double)v[e], q = a.gamma * (double)v[e];
-            if (mine.flag == 0) mine = Op::Map{w, 1.0, d, q, 1u, 0u};
-            else mine = Op::Map{w * mine.P, w * mine.Q, fma(w, mine.B, d + mine.c), q, mine.flag, 0u};
-        }
-    }
-    Op::Map all;
-    const Op::Map before = warp_scan<Op>(mine, lane, all);
-    if (lane == 31) totals[warp] = all;
-    if (MAPS) {
-        __syncthreads();
-        if (tid == 0) {
-            Op::Map m = totals[0];
-            for (int w = 1; w < kSegWarps; ++w) m = Op::then(m, totals[w]);
-            static_cast<Op::Map *>(a.maps)[tile] = m;
-        }
-        return;
-    }
-    if (warp == 0) {
-        const Op::State s = state_into<Op>(static_cast<const Op::Map *>(a.maps), tile, a.tiles, 1, lane);
-        if (lane == 0) incoming = s;
-    }
-    __syncthreads();
-    Op::State s = incoming;
-    for (int w = 0; w < warp; ++w) s = Op::apply(totals[w], s);
-    s = Op::apply(before, s);
-    float adv[8], ret[8];
-    double n = 0.0, shift = 0.0, sum = 0.0, squares = 0.0; // moments about the thread's first value
+                            for (int e = 7; e >= 0; --e) {
+                                D[e] = z = fma(a.weight, z, D[e]);
+                                adv[e] = (float)z;
+                                ret[e] = (float)(z + (double)v[e]);
+                            }
+                            st.x = __shfl_sync(kAll, z, 31);
+                            st.q = __shfl_sync(kAll, first, 31);
+                        } else {
+                            float leftmost = 0.0f;
 #pragma unroll
-    for (int e = 7; e >= 0; --e) {
-        adv[e] = ret[e] = 0.0f;
-        if (ends >> e & 1) s = Op::State{0.0, terminal(k + e)};
-        if (valid >> e & 1) {
-            const double w = a.weight * (double)c[e], V = v[e];
-            s.x = fma(w, s.x, ((double)r[e] - V) + s.q);
-            s.q = a.gamma * V;
-            adv[e] = (float)s.x;
-            ret[e] = (float)(s.x + V);
-            if (a.moments) {
-                if (n == 0.0) shift = s.x;
-                const double d = s.x - shift;
-                n += 1.0;
-                sum += d;
-                squares = fma(d, d, squares);
+                            for (int e = 7; e >= 0; --e) leftmost = valid >> e & 1 ? v[e] : leftmost;
+                            const uint32_t right = some & ((1u << lane) - 1);
+                            const double first = a.gamma * (double)leftmost, from = __shfl_sync(kAll, first, right ? 31 - __clz(right) : 0);
+                            double q = right ? from : st.q;
+                            Line m{1.0, 0.0};
+                            bool apart = MAPS && TRACE && count == 0 && right == 0; // this lane's first weight may be the piece's rightmost
+#pragma unroll
+                            for (int e = 7; e >= 0; --e) {
+                                const bool in = valid >> e & 1;
+                                const double V = (double)v[e], w = TRACE ? a.weight * (double)c[e] : a.weight;
+                                D[e] = ((double)r[e] - V) + q;
+                                const double B = fma(w, m.B, D[e]), qv = a.gamma * V;
+                                m.B = in ? B : m.B;
+                                q = in ? qv : q;
+                                if (TRACE) {
+                                    const double P = w * m.P;
+                                    m.P = in && !apart ? P : m.P;
+                                    if (MAPS && in && apart) w_right = w, apart = false;
+                                }
+                            }
+                            if (!TRACE) m.P = a.small[__popc(valid)];
+                            if (MAPS && TRACE && count == 0) w_right = __shfl_sync(kAll, w_right, __ffs(some) - 1);
+                            const Line before = scan_lines(m, lane);
+                            double z = fma(before.P, st.x, before.B);
+#pragma unroll
+                            for (int e = 7; e >= 0; --e) {
+                                const bool in = valid >> e & 1;
+                                D[e] = fma(TRACE ? a.weight * (double)c[e] : a.weight, z, D[e]);
+                                z = in ? D[e] : z;
+                                adv[e] = in ? (float)D[e] : 0.0f;
+                                ret[e] = in ? (float)(D[e] + (double)v[e]) : 0.0f;
+                            }
+                            if (MAPS && TRACE) P_all *= __shfl_sync(kAll, m.P, 31);
+                            st.x = __shfl_sync(kAll, z, 31);
+                            st.q = __shfl_sync(kAll, first, 31 - __clz(some));
+                        }
+                        if (MAPS) count += TRACE ? 1 : (int)__reduce_add_sync(kAll, (unsigned)__popc(valid));
+                    } else if (!MAPS) {
+                        const int s_right = s;
+                        const uint32_t ends = ends_inside<true>(a.q, base, lo, hi, lane, 31 - lane, s, [](int, int) {});
+                        cur = a.q.bound(s);
+                        Op::Map mine = Op::identity();
+#pragma unroll
+                        for (int e = 7; e >= 0; --e) {
+                            if (ends >> e & 1) mine = Op::Map{0.0, 0.0, 0.0, terminal(a.q.owner(k + e, s, s_right)), 2u, 0u};
+                            if (valid >> e & 1) {
+                                const double w = TRACE ? a.weight * (double)c[e] : a.weight, d = (double)r[e] - (double)v[e], q = a.gamma * (double)v[e];
+                                if (mine.flag == 0) mine = Op::Map{w, 1.0, d, q, 1u, 0u};
+                                else mine = Op::Map{w * mine.P, w * mine.Q, fma(w, mine.B, d + mine.c), q, mine.flag, 0u};
+                            }
+                        }
+                        Op::Map all;
+                        const Op::Map before = warp_scan<Op>(mine, lane, all);
+                        Op::State z = Op::apply(before, st);
+#pragma unroll
+                        for (int e = 7; e >= 0; --e) {
+                            adv[e] = ret[e] = 0.0f;
+                            if (ends >> e & 1) z = Op::State{0.0, terminal(a.q.owner(k + e, s, s_right))};
+                            if (valid >> e & 1) {
+                                const double V = (double)v[e];
+                                z.x = fma(TRACE ? a.weight * (double)c[e] : a.weight, z.x, ((double)r[e] - V) + z.q);
+                                z.q = a.gamma * V;
+                                adv[e] = (float)z.x;
+                                ret[e] = (float)(z.x + V);
+                            }
+                            D[e] = z.x;
+                        }
+                        st = shfl_words(z, 31);
+                    }
+                    if (MOMENTS && some != 0) {
+                        if (!known) { // an advantage of the warp's first block: one of the lane with the first bit
+                            double one = 0.0;
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) one = valid >> e & 1 ? D[e] : one;
+                            shift = __shfl_sync(kAll, one, __ffs(some) - 1);
+                            known = true;
+                        }
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const double d = valid >> e & 1 ? D[e] - shift : 0.0;
+                            sum += d;
+                            squares = fma(d, d, squares);
+                        }
+                        n += (double)__popc(valid);
+                    }
+                }
+                feed.release(i, fetch);
+                if (!MAPS) {
+                    if (a.adv) store8(a.adv, k, lo, hi, a.vec, adv);
+                    if (a.returns) store8(a.returns, k, lo, hi, a.vec, ret);
+                }
+            }
+            if (MAPS && lane == 0) {
+                // x' = Q (w x + q) + B,  q' = c
+                const double Q = TRACE ? P_all : (count > 0 ? pow(a.weight, (double)(count - 1)) : 1.0);
+                static_cast<Op::Map *>(a.maps)[chunk] = Op::Map{Q * w_right, Q, st.x, st.q, count > 0 ? 1u : 0u, 0u};
             }
         }
     }
-    if (a.adv) store8(a.adv, k, hi, a.vec, adv);
-    if (a.returns) store8(a.returns, k, hi, a.vec, ret);
-    if (a.moments) {
-        Moments m{n, n > 0.0 ? shift + sum / n : 0.0, n > 0.0 ? squares - sum * sum / n : 0.0};
-        m = warp_join(m);
-        if (lane == 0) moments[warp] = m;
+    if (MOMENTS) {
+        n = warp_sum(n);
+        sum = warp_sum(sum);
+        squares = warp_sum(squares);
+        if (lane == 0) joined[warp] = n > 0.0 ? Moments{n, shift + sum / n, squares - sum * sum / n} : Moments{0.0, 0.0, 0.0};
         __syncthreads();
-        if (tid == 0) {
-            for (int w = 1; w < kSegWarps; ++w) m.join(moments[w]);
-            a.partials[3 * tile] = m.n;
-            a.partials[3 * tile + 1] = m.mean;
-            a.partials[3 * tile + 2] = m.m2;
+        if (threadIdx.x == 0) {
+            Moments m = joined[0];
+            for (int w = 1; w < kAdvWarps; ++w) m.join(joined[w]);
+            double *slot = a.partials + 3 * (size_t)blockIdx.x;
+            slot[0] = m.n;
+            slot[1] = m.mean;
+            slot[2] = m.m2;
         }
     }
 }
 
-__global__ void __launch_bounds__(kSegThreads) advantage_moments_kernel(const double *partials, int tiles, float *moments)
+constexpr int kMomentThreads = 1024;
+
+__global__ void __launch_bounds__(kMomentThreads) advantage_moments_kernel(const double *partials, int ctas, float *moments)
 {
-    __shared__ Moments sh[kSegWarps];
+    __shared__ Moments sh[32];
     grid_dependency_wait();
     grid_dependency_release();
     Moments m{0.0, 0.0, 0.0};
-    for (int t = threadIdx.x; t < tiles; t += kSegThreads) m.join(Moments{partials[3 * t], partials[3 * t + 1], partials[3 * t + 2]});
+#pragma unroll 4
+    for (int t = threadIdx.x; t < ctas; t += kMomentThreads) m.join(Moments{partials[3 * (size_t)t], partials[3 * (size_t)t + 1], partials[3 * (size_t)t + 2]});
     m = warp_join(m);
     if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = m;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < kSegWarps; ++w) m.join(sh[w]);
-        moments[0] = (float)m.mean;
-        moments[1] = m.n > 0.0 ? (float)sqrt(fmax(m.m2 / m.n, 0.0) + (m.m2 - m.m2)) : 0.0f; // NaN stays
+    if (threadIdx.x < 32) {
+        m = warp_join(sh[threadIdx.x]);
+        if (threadIdx.x == 0) {
+            moments[0] = (float)m.mean;
+            moments[1] = m.n > 0.0 ? (float)sqrt(fmax(m.m2 / m.n, 0.0) + (m.m2 - m.m2)) : 0.0f; // NaN stays
+        }
     }
 }
 
-template <bool MAPS> __global__ void __launch_bounds__(kSegThreads) advantage_grad_kernel(const __grid_constant__ AdvantageArgs a)
+// The tokens of a chunk's pieces from the first to the last, 256 at a time.  MAPS: the map of the piece that begins in the chunk and
+// is not its sequence's last.  Blocks inside one sequence and blocks with an end inside as in the forward kernel; here a lane's first
+// valid token takes the weight of the valid token before it from the nearest lane to the left.  d c of a token needs the advantage
+// of its follower: where that is in a later block, the token stays open until then.
+template <bool TRACE, bool BY_TRACE, bool MAPS>
+__global__ void __launch_bounds__(kAdvThreads, TRACE || BY_TRACE ? 4 : 6) advantage_grad_kernel(const __grid_constant__ AdvantageArgs a)
 {
     using Op = AdvantageGradOp;
-    __shared__ TileShared sh;
-    __shared__ Op::Map totals[kSegWarps];
-    __shared__ Op::State incoming;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, tile = blockIdx.x;
+    constexpr int kTensors = 2 + TRACE + BY_TRACE;
+    extern __shared__ __align__(16) unsigned char smem[];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, chunk = blockIdx.x * kAdvWarps + warp;
     grid_dependency_wait();
     grid_dependency_release();
-    const int lo = tile * kSegTile, live = a.q.live(), hi = live - lo < kSegTile ? live : lo + kSegTile;
+    const int live = a.q.live();
     const bool per_sequence = a.grad_outcome || a.grad_bootstrap;
-    if (hi <= lo) { // behind the last sequence; sequences without a token have no gradient
-        if (MAPS && tid == 0) static_cast<Op::Map *>(a.maps)[tile] = Op::identity();
-        if (!MAPS && per_sequence && tile == 0)
-            for (int64_t s = tid; s < a.q.n_seq; s += kSegThreads) {
-                if (a.grad_outcome) a.grad_outcome[s] = 0.0f;
-                if (a.grad_bootstrap) a.grad_bootstrap[s] = 0.0f;
-            }
+    auto put = [&](int o, double G) {
+        if (a.grad_outcome) a.grad_outcome[o] = (float)G;
+        if (a.grad_bootstrap) a.grad_bootstrap[o] = (float)(a.gamma * G);
+    };
+    if (!MAPS && live <= 0) { // no tokens: no gradients
+        if (per_sequence)
+            for (int64_t o = (int64_t)blockIdx.x * kAdvThreads + threadIdx.x; o < a.q.n_seq; o += (int64_t)gridDim.x * kAdvThreads) put((int)o, 0.0);
         return;
     }
-    const int k = lo + tid * kSegEach;
-    float ga[8], gr[8], c[8], A[8];
-    const uint32_t valid = load_mask8(a.mask, k, hi, a.vec);
-    if (a.grad_adv) load8(a.grad_adv, k, hi, a.vec, ga);
-    if (a.grad_returns) load8(a.grad_returns, k, hi, a.vec, gr);
-    if (a.trace) load8(a.trace, k, hi, a.vec, c);
-    if (!MAPS && a.grad_trace) load8(a.adv_in, k, hi, a.vec, A);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        if (!a.grad_adv) ga[e] = 0.0f;
-        if (!a.grad_returns) gr[e] = 0.0f;
-        if (!a.trace) c[e] = 1.0f;
-    }
-    tile_sequences(a.q, lo, hi, sh);
-    const uint32_t ends = block_ends(sh, tid);
-    Op::Map mine = Op::identity();
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        if (valid >> e & 1) {
-            const double w = a.weight * (double)c[e], g = (double)ga[e] + (double)gr[e];
-            if (mine.flag == 0) mine = Op::Map{1.0, g, w, k + e, 1u};
-            else mine = Op::Map{mine.wl * mine.P, fma(mine.wl, mine.B, g), w, k + e, mine.flag};
-        }
-        if (ends >> e & 1) mine = Op::Map{0.0, 0.0, 0.0, -1, 2u};
-    }
-    Op::Map all;
-    const Op::Map before = warp_scan<Op>(mine, lane, all);
-    if (lane == 31) totals[warp] = all;
+    if (chunk >= a.chunks || (int64_t)chunk * a.chunk >= live)
+        return;
+    const int t0 = chunk * a.chunk, t1 = live - t0 < a.chunk ? live : t0 + a.chunk;
+    int s, s1, begin, end;
+    a.q.owner_warp2(t0, MAPS || t1 >= live ? t1 - 1 : t1, lane, s, s1);
+    Op::State st = Op::start();
+    double w_before = 0.0; // TRACE: weight of the valid token before
+    int e_cur = live;      // where the current sequence ends
     if (MAPS) {
-        __syncthreads();
-        if (tid == 0) {
-            Op::Map m = totals[0];
-            for (int w = 1; w < kSegWarps; ++w) m = Op::then(m, totals[w]);
-            static_cast<Op::Map *>(a.maps)[tile] = m;
+        begin = end = 0;
+        for (int which = 0; which < 2; ++which) { // of the chunk's first sequence, or of its last
+            const int o = which == 0 ? s : s1, b = a.q.bound(o), e = a.q.bound(o + 1);
+            const int64_t p = b >= t0 ? b : b + ((int64_t)t0 - b + a.piece - 1) / a.piece * a.piece;
+            if (p >= t0 && p < t1 && p + a.piece < e) begin = (int)p, end = begin + a.piece;
         }
+    } else {
+        begin = piece_from(a, t0, s, live);
+        end = piece_from(a, t1, s1, live);
+        if (per_sequence && t0 == 0) // sequences without a token ahead of the first one
+            for (int o = lane; o < s; o += 32) put(o, 0.0);
+    }
+    if (end <= begin)
         return;
+    if (!MAPS) {
+        int b = a.q.bound(s);
+        e_cur = a.q.bound(s + 1);
+        if (begin >= e_cur) s = a.q.owner_warp(begin, lane), b = a.q.bound(s), e_cur = a.q.bound(s + 1);
+        st = behind_pieces<Op>(st, ((int64_t)begin - b) / a.piece, lane,
+                               [&](int64_t i) { return static_cast<const Op::Map *>(a.maps)[(b + i * a.piece) / a.chunk]; }, w_before);
     }
-    if (warp == 0) {
-        Op::State s = state_into<Op>(static_cast<const Op::Map *>(a.maps), tile, a.tiles, -1, lane);
-        if (lane == 0) incoming = s;
-    }
-    __syncthreads();
-    Op::State s = incoming;
-    for (int w = 0; w < warp; ++w) s = Op::apply(totals[w], s);
-    s = Op::apply(before, s);
-    float dr[8], dv[8];
+    // The current sequence's last gradient, then on to the one that holds token `to`; those between without a token get zeros.
+    auto next_sequence = [&](int to) {
+        if (lane == 0) {
+            if (BY_TRACE && st.pos >= 0) a.grad_trace[st.pos] = 0.0f; // nothing follows
+            put(s, st.G);
+        }
+        for (int64_t base = (int64_t)s + 1;; base += 32) {
+            const int64_t o = base + lane;
+            const uint32_t hit = __ballot_sync(kAll, o >= a.q.n_seq || a.q.bound((int)o + 1) > to);
+            if (per_sequence && o < a.q.n_seq && lane < (hit ? __ffs(hit) - 1 : 32)) put((int)o, 0.0);
+            if (hit) {
+                const int64_t at = base + __ffs(hit) - 1;
+                s = (int)(at < a.q.n_seq ? at : a.q.n_seq - 1);
+                break;
+            }
+        }
+        e_cur = a.q.bound(s + 1);
+        if (e_cur <= to) e_cur = live; // behind the last one, or boundaries out of order
+        st = Op::start();
+        w_before = 0.0;
+    };
+    Feed<false, kTensors> feed;
+    feed.stage = reinterpret_cast<Stage8 (*)[kTensors]>(smem) + warp * kStages;
+    feed.mask = a.mask, feed.begin = begin, feed.end = end, feed.n_tok = (int)a.q.n_tok, feed.lane = lane, feed.vec = a.vec;
+    auto fetch = [&](Stage8 (&to)[kTensors], int k) {
+        const int all = (int)a.q.n_tok;
+        if (a.grad_adv) fetch8(to[0], lane, a.grad_adv, k, all, a.vec);
+        if (a.grad_returns) fetch8(to[1], lane, a.grad_returns, k, all, a.vec);
+        if (TRACE) fetch8(to[2], lane, a.trace, k, all, a.vec);
+        if (BY_TRACE) fetch8(to[kTensors - 1], lane, a.adv_in, k, all, a.vec);
+    };
+    feed.start(fetch);
+    double P_all = 1.0, ahead = 1.0; // MAPS: product of the weights but the last one's; weight^(8 lane)
+    int64_t count = 0;
+    if (!TRACE)
+        for (int i = 0; i < 5; ++i)
+            if (lane >> i & 1) ahead *= a.powers[i];
+    for (int i = 0; i < feed.blocks; ++i) {
+        const uint32_t valid = feed.arrive();
+        const int base = feed.block(i) << 8, k = feed.place(i), lo = max(base, begin), hi = min(base + 256, end);
+        float ga[8], gr[8], c[8], A[8], dr[8], dv[8], dc[8];
+        int open = -1; // this lane's token that waits for its follower
+        if (!MAPS && e_cur <= lo) next_sequence(lo);
+        const uint32_t some = __ballot_sync(kAll, valid != 0);
+        const bool inside = MAPS || e_cur >= hi;
+        if (some == 0 && inside) {
+            zero8(dr);
+            zero8(dv);
+            zero8(dc);
+        } else {
+            const Stage8 *x = feed.stage[feed.at];
+            if (a.grad_adv) read8(x[0], lane, ga);
+            else zero8(ga);
+            if (a.grad_returns) read8(x[1], lane, gr);
+            else zero8(gr);
+            if (TRACE) read8(x[2], lane, c);
+            if (BY_TRACE) read8(x[kTensors - 1], lane, A);
+            if (inside) {
+                const uint32_t left = some & ((1u << lane) - 1);
+                const int from = left ? 31 - __clz(left) : 0, tail = 31 - __clz(some);
+                double g[8], G;
+                if (!TRACE && __all_sync(kAll, valid == 0xFFu)) {
+                    double B = 0.0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        dr[e] = dv[e] = 0.0f;
-        if (valid >> e & 1) {
-            const double w = a.weight * (double)c[e], G = ((double)ga[e] + (double)gr[e]) + s.y;
-            if (a.grad_trace && s.pos >= 0) a.grad_trace[s.pos] = (float)(a.weight * (double)A[e] * s.G);
-            dr[e] = (float)G;
-            dv[e] = (float)(fma(a.gamma, s.G, (double)gr[e]) - G);
-            s = Op::State{w * G, G, k + e, 0};
-        } else if (a.grad_trace && k + e < hi) {
-            a.grad_trace[k + e] = 0.0f;
-        }
-        if (ends >> e & 1) {
-            if (a.grad_trace && s.pos >= 0) a.grad_trace[s.pos] = 0.0f; // nothing follows
-            if (per_sequence) {
-                const int o = a.q.owner(k + e, sh.s0, sh.s1);
-                if (a.grad_outcome) a.grad_outcome[o] = (float)s.G;
-                if (a.grad_bootstrap) a.grad_bootstrap[o] = (float)(a.gamma * s.G);
+                    for (int e = 0; e < 8; ++e) {
+                        g[e] = (double)ga[e] + (double)gr[e];
+                        B = fma(a.weight, B, g[e]);
+                    }
+                    G = fma(ahead, st.G, scan_even(B, a.powers, lane));
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const double now = fma(a.weight, G, g[e]);
+                        dr[e] = (float)now;
+                        dv[e] = (float)(fma(a.gamma, G, (double)gr[e]) - now);
+                        G = g[e] = now;
+                    }
+                } else {
+                    double w_in = a.weight;
+                    if (TRACE) {
+                        float c_last = 0.0f;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) c_last = valid >> e & 1 ? c[e] : c_last;
+                        const float before = __shfl_sync(kAll, c_last, from);
+                        w_in = left ? a.weight * (double)before : w_before;
+                        w_before = a.weight * (double)__shfl_sync(kAll, c_last, tail);
+                    }
+                    Line m{1.0, 0.0};
+                    double w = MAPS && count == 0 && !left ? 1.0 : w_in; // the weight of what comes into the piece is applied to it before
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const bool in = valid >> e & 1;
+                        g[e] = (double)ga[e] + (double)gr[e];
+                        const double B = fma(w, m.B, g[e]), P = w * m.P;
+                        m.B = in ? B : m.B;
+                        m.P = in ? P : m.P;
+                        if (TRACE) w = in ? a.weight * (double)c[e] : w;
+                        else w = in ? a.weight : w;
+                    }
+                    const Line before = scan_lines(m, lane);
+                    G = fma(before.P, st.G, before.B);
+                    if (MAPS && TRACE) P_all *= __shfl_sync(kAll, m.P, 31);
+                    w = w_in;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const bool in = valid >> e & 1;
+                        const double now = fma(w, G, g[e]);
+                        dr[e] = in ? (float)now : 0.0f;
+                        dv[e] = in ? (float)(fma(a.gamma, G, (double)gr[e]) - now) : 0.0f;
+                        g[e] = now;
+                        G = in ? now : G;
+                        if (TRACE) w = in ? a.weight * (double)c[e] : w;
+                    }
+                }
+                const int last_of = valid ? k + 31 - __clz(valid) : -1;
+                if (BY_TRACE && !MAPS) {
+                    float first_A = 0.0f;
+#pragma unroll
+                    for (int e = 7; e >= 0; --e) first_A = valid >> e & 1 ? A[e] : first_A;
+                    if (!left && valid && st.pos >= 0) // the token left open by a block before
+                        a.grad_trace[st.pos] = (float)(a.weight * (double)first_A * st.G);
+                    const uint32_t right = lane == 31 ? 0u : some & (0xFFFFFFFEu << lane);
+                    float next_A = __shfl_sync(kAll, first_A, right ? __ffs(right) - 1 : 0);
+                    bool known = right != 0;
+#pragma unroll
+                    for (int e = 7; e >= 0; --e) {
+                        const bool in = valid >> e & 1;
+                        dc[e] = in ? (float)(a.weight * (double)next_A * g[e]) : 0.0f;
+                        if (in && !known) open = k + e;
+                        next_A = in ? A[e] : next_A;
+                        known = known || in;
+                    }
+                }
+                st.G = __shfl_sync(kAll, G, tail);
+                st.pos = __shfl_sync(kAll, last_of, tail);
+                if (MAPS) count += TRACE ? 1 : (int)__reduce_add_sync(kAll, (unsigned)__popc(valid));
+            } else { // sequences end inside
+                const int s_left = s;
+                const uint32_t ends = ends_inside<false>(a.q, base, lo, hi, lane, lane, s, [&](int o, int p) {
+                    if (per_sequence && p <= a.q.bound(o)) put(o, 0.0);
+                });
+                e_cur = a.q.bound(s + 1);
+                if (e_cur < hi) e_cur = live; // boundaries out of order
+                Op::Map mine = Op::identity();
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    if (valid >> e & 1) {
+                        const double w = TRACE ? a.weight * (double)c[e] : a.weight, g = (double)ga[e] + (double)gr[e];
+                        if (mine.flag == 0) mine = Op::Map{1.0, g, w, k + e, 1u};
+                        else mine = Op::Map{mine.wl * mine.P, fma(mine.wl, mine.B, g), w, k + e, mine.flag};
+                    }
+                    if (ends >> e & 1) mine = Op::Map{0.0, 0.0, 0.0, -1, 2u};
+                }
+                Op::Map all;
+                const Op::Map before = warp_scan<Op>(mine, lane, all);
+                st.y = (TRACE ? w_before : a.weight) * st.G;
+                Op::State z = Op::apply(before, st);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    dr[e] = dv[e] = 0.0f;
+                    if (valid >> e & 1) {
+                        const double w = TRACE ? a.weight * (double)c[e] : a.weight, G = ((double)ga[e] + (double)gr[e]) + z.y;
+                        if (BY_TRACE && z.pos >= 0) a.grad_trace[z.pos] = (float)(a.weight * (double)A[e] * z.G);
+                        dr[e] = (float)G;
+                        dv[e] = (float)(fma(a.gamma, z.G, (double)gr[e]) - G);
+                        z = Op::State{w * G, G, k + e, 0};
+                    } else if (BY_TRACE && k + e >= lo && k + e < hi) {
+                        a.grad_trace[k + e] = 0.0f;
+                    }
+                    if (ends >> e & 1) {
+                        if (BY_TRACE && z.pos >= 0) a.grad_trace[z.pos] = 0.0f;
+                        if (per_sequence) put(a.q.owner(k + e, s_left, s), z.G);
+                        z = Op::start();
+                    }
+                }
+                st = shfl_words(z, 31);
+                w_before = Op::last_weight(shfl_words(all, 31), w_before);
             }
-            s = Op::start();
+        }
+        feed.release(i, fetch);
+        if (!MAPS) {
+            if (a.grad_rewards) store8(a.grad_rewards, k, lo, hi, a.vec, dr);
+            if (a.grad_values) store8(a.grad_values, k, lo, hi, a.vec, dv);
+            if (BY_TRACE && inside) {
+                if (open < 0) store8(a.grad_trace, k, lo, hi, a.vec, dc);
+                else
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (k + e >= lo && k + e < hi && k + e != open) a.grad_trace[k + e] = dc[e];
+            }
         }
     }
-    if (a.grad_rewards) store8(a.grad_rewards, k, hi, a.vec, dr);
-    if (a.grad_values) store8(a.grad_values, k, hi, a.vec, dv);
-    if (per_sequence) { // sequences without a token, from this tile's first sequence to the next tile's (or from and to the ends)
-        __shared__ int next;
-        __syncthreads();
-        if (warp == 0) {
-            const int o = hi < live ? a.q.owner_warp(hi, lane) : (int)a.q.n_seq - 1;
-            if (lane == 0) next = o;
-        }
-        __syncthreads();
-        for (int64_t o = (tile == 0 ? 0 : sh.s0) + tid; o <= next; o += kSegThreads)
-            if (a.q.bound((int)o + 1) <= a.q.bound((int)o)) {
-                if (a.grad_outcome) a.grad_outcome[o] = 0.0f;
-                if (a.grad_bootstrap) a.grad_bootstrap[o] = 0.0f;
-            }
+    if (MAPS) {
+        const double P = TRACE ? P_all : (count > 0 ? pow(a.weight, (double)(count - 1)) : 1.0);
+        if (lane == 0)
+            static_cast<Op::Map *>(a.maps)[chunk] = Op::Map{P, st.G, TRACE ? w_before : a.weight, st.pos, count > 0 ? 1u : 0u};
+    } else if (e_cur <= end) {
+        next_sequence(end);
     }
 }
 
@@ -378,14 +764,31 @@ static bool all_vectors(const AdvantageArgs &a)
            aligned(a.values, a.values_bf16 ? 16 : 32);
 }
 
+// Chunks: 2048 tokens a warp where that still gives every SM a full set of warps, down to one block of 256 tokens.
+constexpr int64_t kChunks = 148 * 24;
+static void deal(AdvantageArgs &a)
+{
+    a.chunk = 256;
+    while (a.chunk < 2048 && a.chunk * kChunks < a.q.n_tok) a.chunk *= 2;
+    a.piece = 4 * a.chunk;
+    a.chunks = (int)((a.q.n_tok + a.chunk - 1) / a.chunk);
+    for (int i = 0; i < 9; ++i) a.small[i] = std::pow(a.weight, i);
+    a.powers[0] = a.small[8];
+    for (int i = 1; i < 5; ++i) a.powers[i] = a.powers[i - 1] * a.powers[i - 1];
+}
+
+// Whether a sequence can be longer than a piece, as far as the host knows.
+static bool long_sequences(const AdvantageArgs &a) { return (a.q.cu ? a.q.n_tok : a.q.T) > a.piece; }
+
 } // namespace hilore
 
 using namespace hilore;
 
 extern "C" size_t hilore_advantages_workspace_bytes(int64_t n_tok)
 {
-    const size_t tiles = n_tok > 0 ? (size_t)((n_tok + kSegTile - 1) / kSegTile) : 0;
-    return (tiles + 1) * (sizeof(AdvantageOp::Map) + 3 * sizeof(double));
+    const int64_t n = n_tok > 0 ? n_tok : 0, small = (n + 255) / 256, large = (n + 2047) / 2048; // chunks, whatever their size, of n tokens or fewer
+    const size_t chunks = (size_t)std::max(std::min(small, kChunks), large);
+    return (chunks + 1) * sizeof(AdvantageOp::Map) + (chunks / kAdvWarps + 1) * 3 * sizeof(double);
 }
 
 extern "C" int hilore_advantages(const float *rewards, const float *outcome, const void *values, int32_t values_dtype, const float *bootstrap,
@@ -396,7 +799,7 @@ extern "C" int hilore_advantages(const float *rewards, const float *outcome, con
     AdvantageArgs a{};
     if (!(gamma >= 0.0 && gamma <= 1.0) || !(lambda >= 0.0 && lambda <= 1.0) || (values_dtype != HILORE_BF16 && values_dtype != HILORE_F32))
         return HILORE_INVALID_ARG;
-    const int bad = check_sequences(cu_seqlens, n_seq, n_tok, a.q, a.tiles);
+    const int bad = check_sequences(cu_seqlens, n_seq, n_tok, a.q);
     if (bad)
         return bad;
     if (!workspace || (n_tok > 0 && !adv && !returns && !moments))
@@ -409,14 +812,20 @@ extern "C" int hilore_advantages(const float *rewards, const float *outcome, con
     if (workspace_bytes < hilore_advantages_workspace_bytes(n_tok))
         return HILORE_WORKSPACE;
     a.maps = workspace;
-    a.partials = reinterpret_cast<double *>(static_cast<AdvantageOp::Map *>(workspace) + a.tiles + 1);
     a.vec = all_vectors(a);
+    deal(a);
+    a.partials = reinterpret_cast<double *>(static_cast<AdvantageOp::Map *>(workspace) + a.chunks + 1);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (a.tiles > 1 && launch_dependent(advantage_kernel<true>, dim3((unsigned)a.tiles), dim3(kSegThreads), 0, st, a) != cudaSuccess)
+    const unsigned grid = (unsigned)((a.chunks + kAdvWarps - 1) / kAdvWarps);
+    const size_t smem = kAdvWarps * kStages * sizeof(Stage8) * (trace ? 3 : 2);
+    if (grid > 0 && long_sequences(a) &&
+        launch_dependent(trace ? advantage_kernel<true, false, true> : advantage_kernel<false, false, true>, dim3(grid), dim3(kAdvThreads), smem, st, a) != cudaSuccess)
         return HILORE_CUDA;
-    if (a.tiles > 0 && launch_dependent(advantage_kernel<false>, dim3((unsigned)a.tiles), dim3(kSegThreads), 0, st, a) != cudaSuccess)
+    void (*kernel)(AdvantageArgs) = moments ? (trace ? advantage_kernel<true, true, false> : advantage_kernel<false, true, false>)
+                                            : (trace ? advantage_kernel<true, false, false> : advantage_kernel<false, false, false>);
+    if (grid > 0 && launch_dependent(kernel, dim3(grid), dim3(kAdvThreads), smem, st, a) != cudaSuccess)
         return HILORE_CUDA;
-    if (moments && launch_dependent(advantage_moments_kernel, dim3(1), dim3(kSegThreads), 0, st, (const double *)a.partials, a.tiles, moments) != cudaSuccess)
+    if (moments && launch_dependent(advantage_moments_kernel, dim3(1), dim3(kMomentThreads), 0, st, (const double *)a.partials, (int)grid, moments) != cudaSuccess)
         return HILORE_CUDA;
     return cudaGetLastError() == cudaSuccess ? HILORE_OK : HILORE_CUDA;
 }
@@ -429,7 +838,7 @@ extern "C" int hilore_advantages_backward(const float *grad_adv, const float *gr
     AdvantageArgs a{};
     if (!(gamma >= 0.0 && gamma <= 1.0) || !(lambda >= 0.0 && lambda <= 1.0))
         return HILORE_INVALID_ARG;
-    const int bad = check_sequences(cu_seqlens, n_seq, n_tok, a.q, a.tiles);
+    const int bad = check_sequences(cu_seqlens, n_seq, n_tok, a.q);
     if (bad)
         return bad;
     if (!workspace || (grad_trace && !adv && n_tok > 0))
@@ -446,13 +855,19 @@ extern "C" int hilore_advantages_backward(const float *grad_adv, const float *gr
         return HILORE_WORKSPACE;
     a.maps = workspace;
     a.vec = all_vectors(a);
+    deal(a);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (n_seq == 0)
         return HILORE_OK;
-    const unsigned grid = (unsigned)(a.tiles > 0 ? a.tiles : 1);
-    if (a.tiles > 1 && launch_dependent(advantage_grad_kernel<true>, dim3(grid), dim3(kSegThreads), 0, st, a) != cudaSuccess)
+    const unsigned grid = a.chunks > 0 ? (unsigned)((a.chunks + kAdvWarps - 1) / kAdvWarps) : 1u;
+    void (*const maps)(AdvantageArgs) = trace ? advantage_grad_kernel<true, false, true> : advantage_grad_kernel<false, false, true>;
+    void (*const kernel)(AdvantageArgs) =
+        grad_trace ? (trace ? advantage_grad_kernel<true, true, false> : advantage_grad_kernel<false, true, false>)
+                   : (trace ? advantage_grad_kernel<true, false, false> : advantage_grad_kernel<false, false, false>);
+    const size_t smem = kAdvWarps * kStages * sizeof(Stage8);
+    if (long_sequences(a) && launch_dependent(maps, dim3(grid), dim3(kAdvThreads), smem * (trace ? 3 : 2), st, a) != cudaSuccess)
         return HILORE_CUDA;
-    if (launch_dependent(advantage_grad_kernel<false>, dim3(grid), dim3(kSegThreads), 0, st, a) != cudaSuccess)
+    if (launch_dependent(kernel, dim3(grid), dim3(kAdvThreads), smem * (2 + (trace != nullptr) + (grad_trace != nullptr)), st, a) != cudaSuccess)
         return HILORE_CUDA;
     return cudaGetLastError() == cudaSuccess ? HILORE_OK : HILORE_CUDA;
 }

@@ -303,7 +303,7 @@ __global__ void __launch_bounds__(kSegThreads) policy_token_kernel(const __grid_
         }
 #pragma unroll
         for (int i = 1; i < kStats; ++i) v[i] += (double)part[i];
-        store8(a.omega, k, hi, a.vec, out);
+        store8(a.omega, k, lo, hi, a.vec, out);
         __syncthreads();
     }
     put_stats(v, a.partials + (size_t)(a.slots_before + blockIdx.x) * kStats);
@@ -473,7 +473,7 @@ __global__ void __launch_bounds__(kSegThreads) preference_token_kernel(const __g
             out[e] = c;
         }
     }
-    store8(a.omega, k, hi, a.vec, out);
+    store8(a.omega, k, lo, hi, a.vec, out);
 }
 
 constexpr int kMaxGroup = 1024;
@@ -528,9 +528,10 @@ extern "C" int hilore_policy_loss(const float *logp, const float *logp_old, cons
         t.kl < HILORE_KL_K1 || t.kl > HILORE_KL_K3 || (t.adv_per_token != 0 && t.adv_per_token != 1) ||
         (t.adv_per_token && t.ratio == HILORE_RATIO_SEQUENCE))
         return HILORE_INVALID_ARG;
-    const int bad = check_sequences(cu_seqlens, n_seq, n_tok, a.q, a.tiles);
+    const int bad = check_sequences(cu_seqlens, n_seq, n_tok, a.q);
     if (bad)
         return bad;
+    a.tiles = (int)((n_tok + kSegTile - 1) / kSegTile);
     if (n_tok > 0 && (!logp || !logp_old || !adv || !omega || (t.beta != 0.0 && !logp_ref)))
         return HILORE_INVALID_ARG;
     if (!N_norm_dev && N_norm <= 0)
@@ -593,9 +594,10 @@ extern "C" int hilore_preference_loss(const float *logp, const float *logp_ref, 
         !(t.smoothing >= 0.0 && t.smoothing <= 1.0) || t.loss < HILORE_PREF_SIGMOID || t.loss > HILORE_PREF_SQUARE ||
         (t.length_mean != 0 && t.length_mean != 1) || (t.smoothing != 0.0 && t.loss != HILORE_PREF_SIGMOID))
         return HILORE_INVALID_ARG;
-    const int bad = check_sequences(cu_seqlens, n_seq, n_tok, a.q, a.tiles);
+    const int bad = check_sequences(cu_seqlens, n_seq, n_tok, a.q);
     if (bad)
         return bad;
+    a.tiles = (int)((n_tok + kSegTile - 1) / kSegTile);
     if (n_seq % G != 0 || G > kMaxGroup)
         return HILORE_SHAPE;
     if ((n_tok > 0 && (!logp || !omega)) || (n_seq > 0 && !rewards))

@@ -34,7 +34,7 @@ struct Sequences {
     __device__ __forceinline__ int owner(int p, int first, int last) const
     {
         if (cu == nullptr)
-            return (int)(p / T);
+            return (int)((uint32_t)p / (uint32_t)T);
         while (first < last) {
             const int mid = first + (last - first + 1) / 2;
             if (bound(mid) <= p) first = mid;
@@ -43,23 +43,34 @@ struct Sequences {
         return first;
     }
 
-    // The same over all sequences by a whole warp: 32 probes at a time.
+    // The same over all sequences, of two tokens at once, by a whole warp: 32 probes for each at a time.
+    __device__ __forceinline__ void owner_warp2(int p0, int p1, int lane, int &s0, int &s1) const
+    {
+        if (cu == nullptr) {
+            s0 = (int)((uint32_t)p0 / (uint32_t)T);
+            s1 = (int)((uint32_t)p1 / (uint32_t)T);
+            return;
+        }
+        // the answers lie in [f0, f0 + count) and [f1, f1 + count), as far as these are in [0, n_seq)
+        int64_t f0 = 0, f1 = 0, count = n_seq;
+        while (count > 1) {
+            const int64_t step = (count + 31) / 32, a0 = f0 + lane * step, a1 = f1 + lane * step;
+            const int b0 = lane * step < count && a0 < n_seq ? bound((int)a0) : 0x7FFFFFFF;
+            const int b1 = lane * step < count && a1 < n_seq ? bound((int)a1) : 0x7FFFFFFF;
+            const uint32_t h0 = ~__ballot_sync(0xFFFFFFFFu, lane == 0 || b0 <= p0), h1 = ~__ballot_sync(0xFFFFFFFFu, lane == 0 || b1 <= p1);
+            // the leading run of hits: with boundaries in order that is every hit
+            f0 += (h0 ? __ffs(h0) - 2 : 31) * step;
+            f1 += (h1 ? __ffs(h1) - 2 : 31) * step;
+            count = step;
+        }
+        s0 = (int)f0;
+        s1 = (int)f1;
+    }
     __device__ __forceinline__ int owner_warp(int p, int lane) const
     {
-        if (cu == nullptr)
-            return (int)(p / T);
-        int64_t first = 0, count = n_seq; // the answer lies in [first, first + count)
-        while (count > 1) {
-            const int64_t step = (count + 31) / 32, at = first + lane * step;
-            const bool le = lane == 0 || (at < first + count && bound((int)at) <= p);
-            const uint32_t hit = __ballot_sync(0xFFFFFFFFu, le);
-            // the leading run of hits: with boundaries in order that is every hit
-            const int k = __ffs(~hit) == 0 ? 31 : __ffs(~hit) - 2;
-            const int64_t begin = first + k * step;
-            count = (first + count - begin) < step ? (first + count - begin) : step;
-            first = begin;
-        }
-        return (int)first;
+        int s0, s1;
+        owner_warp2(p, p, lane, s0, s1);
+        return s0;
     }
 };
 
@@ -145,9 +156,16 @@ __device__ __forceinline__ uint32_t load_mask8(const uint8_t *p, int k, int hi, 
     return m;
 }
 
-__device__ __forceinline__ void store8(float *p, int k, int hi, bool vec, const float (&x)[8])
+__device__ __forceinline__ void zero8(float (&x)[8])
 {
-    if (vec && k + 8 <= hi) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = 0.0f;
+}
+
+// Those of the eight tokens that lie in [lo, hi).
+__device__ __forceinline__ void store8(float *p, int k, int lo, int hi, bool vec, const float (&x)[8])
+{
+    if (vec && k >= lo && k + 8 <= hi) {
         uint32_t w[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) w[e] = __float_as_uint(x[e]);
@@ -155,11 +173,92 @@ __device__ __forceinline__ void store8(float *p, int k, int hi, bool vec, const 
     } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-            if (k + e < hi) p[k + e] = x[e];
+            if (k + e >= lo && k + e < hi) p[k + e] = x[e];
     }
 }
 
-// ---- scans over the threads of a CTA ----
+// ---- eight tokens of every lane of a warp, on their way through shared memory ----
+// cp.async holds no registers while the data is on its way, so a warp can have several blocks of 256 tokens in flight; a lane reads
+// back what it asked for itself, so nothing but its own wait is needed.  The two halves of a lane's eight numbers lie 512 bytes
+// apart: 16-byte accesses of neighbouring lanes then touch neighbouring addresses.
+struct Stage8 {
+    float x[2][32][4];
+};
+__device__ __forceinline__ void copy_async(void *to, const void *from, int bytes) // 4 or 16
+{
+    const uint32_t d = (uint32_t)__cvta_generic_to_shared(to);
+    if (bytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d), "l"(from) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(d), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+
+// Tokens k .. k + 7 below n.
+__device__ __forceinline__ void fetch8(Stage8 &to, int lane, const float *p, int k, int n, bool vec)
+{
+    if (vec && k + 8 <= n) {
+        copy_async(to.x[0][lane], p + k, 16);
+        copy_async(to.x[1][lane], p + k + 4, 16);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (k + e < n) copy_async(&to.x[e >> 2][lane][e & 3], p + k + e, 4);
+    }
+}
+__device__ __forceinline__ void fetch8(Stage8 &to, int lane, const uint16_t *p, int k, int n, bool vec) // bf16
+{
+    if (vec && k + 8 <= n) {
+        copy_async(to.x[0][lane], p + k, 16);
+    } else {
+        uint16_t *h = reinterpret_cast<uint16_t *>(to.x[0][lane]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (k + e < n) h[e] = p[k + e];
+    }
+}
+__device__ __forceinline__ void read8(const Stage8 &from, int lane, float (&x)[8])
+{
+    const float4 a = *reinterpret_cast<const float4 *>(from.x[0][lane]), b = *reinterpret_cast<const float4 *>(from.x[1][lane]);
+    x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+}
+__device__ __forceinline__ void read8_bf16(const Stage8 &from, int lane, float (&x)[8])
+{
+    const uint4 w = *reinterpret_cast<const uint4 *>(from.x[0][lane]);
+    const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        x[2 * e] = bf16_lo(v[e]);
+        x[2 * e + 1] = bf16_hi(v[e]);
+    }
+}
+
+// The eight mask bytes from token k on, those at or behind n as zeros; and a bit for each that is not zero.
+__device__ __forceinline__ uint2 mask_bytes(const uint8_t *p, int k, int n, bool vec)
+{
+    if (p == nullptr) return make_uint2(0x01010101u, 0x01010101u);
+    if (vec && k + 8 <= n) return ld_global_64_stream(p + k);
+    uint32_t w[2] = {0, 0};
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (k + e < n) w[e >> 2] |= (uint32_t)p[k + e] << (8 * (e & 3));
+    return make_uint2(w[0], w[1]);
+}
+__device__ __forceinline__ uint32_t mask_bits(uint2 w)
+{
+    // every byte that is not zero to 0xFF, one bit of each kept, and these gathered in the top byte
+    const uint32_t a = __vcmpne4(w.x, 0u) & 0x08040201u, b = __vcmpne4(w.y, 0u) & 0x80402010u;
+    return ((a | b) * 0x01010101u) >> 24;
+}
+// Bits of the tokens k .. k + 7 that lie in [lo, hi).
+__device__ __forceinline__ uint32_t range_bits(int k, int lo, int hi)
+{
+    if (k >= lo && k + 8 <= hi) return 0xFFu;
+    if (k + 8 <= lo || k >= hi) return 0u;
+    const uint32_t from = k < lo ? 0xFFu << (lo - k) : 0xFFu, to = k + 8 > hi ? 0xFFu >> (k + 8 - hi) : 0xFFu;
+    return from & to & 0xFFu;
+}
+
+// ---- scans over the lanes of a warp ----
 // Op::Map is what a run of tokens does to the state that comes in; Op::then(a, b) is a followed by b, Op::apply(m, s) the state
 // behind the run.  A run that holds the start of a sequence does not depend on what comes in, and says so in its flag.
 template <typename T> __device__ __forceinline__ T shfl_up_words(const T &v, int by)
@@ -199,8 +298,8 @@ template <typename Op> __device__ __forceinline__ typename Op::Map warp_scan(typ
 // ---- host side ----
 constexpr int64_t kMaxTokens = (int64_t(1) << 31) - (int64_t(1) << 16); // token numbers of a whole tile stay in 31 bits
 
-// The sequences and tiles of a call, or why there are none.
-inline int check_sequences(const int32_t *cu, int64_t n_seq, int64_t n_tok, Sequences &q, int &tiles)
+// The sequences of a call, or why there are none.
+inline int check_sequences(const int32_t *cu, int64_t n_seq, int64_t n_tok, Sequences &q)
 {
     if (n_seq < 0 || n_tok < 0)
         return HILORE_INVALID_ARG;
@@ -209,7 +308,6 @@ inline int check_sequences(const int32_t *cu, int64_t n_seq, int64_t n_tok, Sequ
     if (!aligned(cu, 4))
         return HILORE_ALIGN;
     q = Sequences{cu, n_seq, n_tok, n_seq > 0 ? n_tok / n_seq : 0};
-    tiles = (int)((n_tok + kSegTile - 1) / kSegTile);
     return HILORE_OK;
 }
 
