@@ -69,10 +69,11 @@ struct AdvantageGradOp {
 
 constexpr int kAdvThreads = 128; // four warps that know nothing of one another but at the end
 constexpr int kAdvWarps = kAdvThreads / 32;
-constexpr int kStages = 3;       // blocks of 256 tokens that a warp has in flight or at work
+constexpr int kStages = 3;       // blocks of 256 tokens whose tensors a warp has in flight or at work
+constexpr int kMaskStages = 8;   // and their masks, which say what to read of the tensors: more than 2 kStages, a power of two
 constexpr uint32_t kAll = 0xFFFFFFFFu;
 
-// How the work is dealt out.  A warp owns the pieces that begin in its chunk of tokens.  A piece is a whole sequence, or `piece`
+// How the work is dealt out.  A warp owns the pieces that begin in its chunk of tokens.  A piece is a whole sequence, or 2^piece
 // tokens (the last one fewer) of a longer one, so nothing but long sequences needs more than one pass: their pieces' maps are
 // made first, by a launch that has nothing to read where no sequence is long.  piece >= chunk, so no chunk holds the beginnings
 // of two pieces that are not the first of their sequence (or not the last), and a map's place is its chunk.
@@ -90,23 +91,43 @@ struct AdvantageArgs {
     float *grad_rewards, *grad_outcome, *grad_values, *grad_bootstrap, *grad_trace;
     void *maps;       // [chunks]
     double *partials; // [CTAs][3] count, mean, sum of squared deviations
-    int chunks, chunk, piece, vec, moments;
+    int chunks, chunk, piece, vec, moments; // chunk, piece: logarithms
+    int warm, second; // second: a launch of this call came first, and what it did not write is there without waiting for it
 };
 
-// The first beginning of a piece at or behind token t, or the end of the last sequence.
+// In a call whose warps all run at once there is nothing but latency: its first launch asks for the chunks' tokens to be brought into
+// L2 before it is known which of them will be read.
+template <bool MAPS>
+__device__ __forceinline__ void warm(const AdvantageArgs &a, int chunk, int lane, const float *x0, const float *x1, const float *x2, const float *x3)
+{
+    if (!a.warm || chunk >= a.chunks || (!MAPS && a.second)) return;
+    const int t0 = chunk << a.chunk, t1 = (int)min(a.q.n_tok, (int64_t)t0 + (1 << a.chunk));
+#pragma unroll 1
+    for (int t = t0 + lane * 32; t < t1; t += 32 * 32) { // 128 bytes of fp32
+        if (x0) prefetch_l2(x0 + t);
+        if (x1) prefetch_l2(x1 + t);
+        if (x2) prefetch_l2(x2 + t);
+        if (x3) prefetch_l2(x3 + t);
+        if (a.values && a.values_bf16 && (lane & 1) == 0) prefetch_l2(static_cast<const uint16_t *>(a.values) + t);
+        if (a.mask && (lane & 3) == 0) prefetch_l2(a.mask + t);
+    }
+}
+
+// The first beginning of a piece at or behind token t of sequence s, or the end of the last sequence.
 __device__ __forceinline__ int piece_from(const AdvantageArgs &a, int t, int s, int live)
 {
     if (t >= live) return live;
     const int b = a.q.bound(s), e = a.q.bound(s + 1);
-    const int64_t p = b + ((int64_t)t - b + a.piece - 1) / a.piece * a.piece;
-    const int64_t at = p < e ? p : e;
+    const uint32_t off = t > b ? (uint32_t)(t - b) : 0u, up = ((off + (1u << a.piece) - 1) >> a.piece) << a.piece;
+    const int64_t p = (int64_t)b + up, at = p < e ? p : e;
     return (int)(at < t ? t : (at > live ? live : at)); // boundaries out of order stay inside
 }
 
-// The state behind maps of `n` pieces, the piece of lane 0 first; maps(i) gives the map of piece i.
-template <typename Op, typename F> __device__ __forceinline__ typename Op::State behind_pieces(typename Op::State s, int64_t n, int lane, F maps, double &wl)
+// The state behind the maps of `n` pieces, first to last; maps(i) gives the map of piece i.
+template <typename Op, typename F> __device__ __forceinline__ typename Op::State behind_pieces(typename Op::State s, int n, int lane, F maps, double &wl)
 {
-    for (int64_t done = 0; done < n; done += 32) {
+#pragma unroll 1
+    for (int done = 0; done < n; done += 32) {
         typename Op::Map m = Op::identity(), all;
         if (done + lane < n) m = maps(done + lane);
         warp_scan<Op>(m, lane, all);
@@ -136,7 +157,7 @@ struct Moments { // count, mean and sum of squared deviations of a set of values
 
 __device__ __forceinline__ Moments warp_join(Moments m)
 {
-#pragma unroll
+#pragma unroll 1
     for (int by = 1; by < 32; by *= 2) {
         Moments o;
         o.n = __shfl_down_sync(kAll, m.n, by);
@@ -180,61 +201,85 @@ __device__ __forceinline__ double scan_even(double B, const double (&powers)[5],
 }
 
 // A warp's way through the blocks of 256 tokens of [begin, end), from the last to the first (BACK: lane 0 has the last eight) or from
-// the first to the last.  Masks are read a block ahead of the tensors, and tokens that no bit asks for are not read.
+// the first to the last.  Masks run ahead of the tensors, and blocks of which no bit asks for anything are not read.
+template <int TENSORS> struct FeedMemory { // of a warp
+    Stage stage[kStages][TENSORS];
+    uint2 mask[kMaskStages][32];
+};
 template <bool BACK, int TENSORS> struct Feed {
-    Stage8 (*stage)[TENSORS]; // [kStages]
+    FeedMemory<TENSORS> *mem;
     const uint8_t *mask;
-    int begin, end, n_tok, lane, blocks, edge, at;
-    uint32_t pipe; // eight bits of each of the next kStages blocks
-    uint2 raw;
+    int begin, end, n_tok, off; // off: this lane's first token in a block
+    int left;                   // blocks from this one on
+    int base, i;                // this block's first token, its number
+    uint32_t pipe;              // eight bits of each of the blocks that have been asked for
     bool vec;
 
-    __device__ __forceinline__ int block(int i) const { return BACK ? edge - i : edge + i; }
-    __device__ __forceinline__ int place(int i) const { return (block(i) << 8) + (BACK ? 31 - lane : lane) * 8; }
-    __device__ __forceinline__ uint2 bytes(int i) const
+    __device__ __forceinline__ static int ahead(int by) { return BACK ? -by * kBlock : by * kBlock; }
+    // Whether the block from token b on can be read eight tokens at a time.
+    __device__ __forceinline__ bool whole(int b) const { return vec && b + kBlock <= n_tok; }
+    __device__ __forceinline__ void ask_mask(int by) const
     {
-        if (i >= blocks) return make_uint2(0u, 0u);
-        const int k = place(i);
-        return k + 8 <= begin || k >= end ? make_uint2(0u, 0u) : mask_bytes(mask, k, n_tok, vec);
+        if (mask == nullptr || by >= left) return;
+        const int b = base + ahead(by);
+        uint2 *to = &mem->mask[(i + by) & (kMaskStages - 1)][threadIdx.x & 31];
+        if (whole(b)) copy_async(to, mask + b + off, 8);
+        else *to = mask_bytes(mask, b + off, n_tok);
     }
-    template <typename F> __device__ __forceinline__ void ask(int i, int into, uint2 w, int slot, F fetch)
+    template <typename F> __device__ __forceinline__ void ask(int by, int slot, F fetch)
     {
-        const uint32_t v = i < blocks ? mask_bits(w) & range_bits(place(i), begin, end) : 0u;
-        pipe |= v << (8 * slot);
-        if (v) fetch(stage[into], place(i));
-        copy_commit();
+        uint32_t v = 0;
+        if (by < left) {
+            const int b = base + ahead(by);
+            v = b >= begin && b + kBlock <= end ? 0xFFu : range_bits(b + off, begin, end);
+            if (mask != nullptr) v &= mask_bits(mem->mask[(i + by) & (kMaskStages - 1)][threadIdx.x & 31]);
+            if (__any_sync(kAll, v != 0)) fetch(mem->stage[slot], b, whole(b));
+        }
+        pipe |= v << (8 * by);
     }
     template <typename F> __device__ __forceinline__ void start(F fetch)
     {
-        edge = BACK ? (end - 1) >> 8 : begin >> 8;
-        blocks = ((end - 1) >> 8) - (begin >> 8) + 1;
+        const int last = (end - 1) & ~(kBlock - 1), first = begin & ~(kBlock - 1);
+        base = BACK ? last : first;
+        left = (last - first) / kBlock + 1;
+        i = 0;
         pipe = 0;
-        at = 0;
-        uint2 w[kStages];
-#pragma unroll
-        for (int i = 0; i < kStages; ++i) w[i] = bytes(i);
-        raw = bytes(kStages);
-#pragma unroll
-        for (int i = 0; i < kStages; ++i) ask(i, i, w[i], i, fetch);
+#pragma unroll 1
+        for (int by = 0; by < kMaskStages; ++by) ask_mask(by);
+        copy_commit();
+        copy_wait<0>();
+#pragma unroll 1
+        for (int by = 0; by < kStages; ++by) {
+            ask(by, by, fetch);
+            copy_commit();
+        }
     }
-    // The bits of block i; its tensors are in stage[at].
-    __device__ __forceinline__ uint32_t arrive()
+    // Waits for this block: its bits; its tensors are in stage[slot], and the masks of the next blocks are there.
+    __device__ __forceinline__ uint32_t arrive() const
     {
-        const uint32_t v = pipe & 0xFFu;
-        pipe >>= 8;
         copy_wait<kStages - 1>();
-        return v;
+        __syncwarp();
+        return pipe & 0xFFu;
     }
-    template <typename F> __device__ __forceinline__ void release(int i, F fetch)
+    // Once the block's tensors are in registers: asks for a later one in their place.
+    template <typename F> __device__ __forceinline__ void release(int slot, F fetch)
     {
-        ask(i + kStages, at, raw, kStages - 1, fetch);
-        raw = bytes(i + kStages + 1);
-        at = at + 1 == kStages ? 0 : at + 1;
+        __syncwarp();
+        ask(kStages, slot, fetch);
+        ask_mask(kMaskStages);
+        copy_commit();
+    }
+    __device__ __forceinline__ void next()
+    {
+        pipe >>= 8;
+        base += ahead(1);
+        ++i;
+        --left;
     }
 };
 
-// Bits of the tokens of block [base, base + 256) that end their sequence, with another beginning inside (lo, hi); the eight of lane
-// `of`.  Sequences are walked from `s` on, up or down, and s becomes the one that holds the block's last (first) token.
+// A block's tokens that end their sequence, with another beginning inside (lo, hi): bits of the eight tokens of block place `of`.
+// Sequences are walked from `s` on, up or down, and s becomes the one that holds the block's last (first) token.
 template <bool BACK, typename F>
 __device__ __forceinline__ uint32_t ends_inside(const Sequences &q, int base, int lo, int hi, int lane, int of, int &s, F passed)
 {
@@ -246,6 +291,7 @@ __device__ __forceinline__ uint32_t ends_inside(const Sequences &q, int base, in
         const uint32_t out = __ballot_sync(kAll, BACK ? p <= lo : p >= hi);
         const int n = out ? __ffs(out) - 1 : 32;
         if (lane < n) passed((int)o, p);
+#pragma unroll 1
         for (int j = 0; j < n; ++j) {
             const int at = __shfl_sync(kAll, p, j) - 1 - base;
             if ((at >> 3) == of) mine |= 1u << (at & 7);
@@ -261,7 +307,7 @@ __device__ __forceinline__ uint32_t ends_inside(const Sequences &q, int base, in
 // MAPS: the map of the piece that begins in the chunk and is not its sequence's first.  Otherwise the outputs.
 //   Blocks inside one sequence (nearly all): a lane's rightmost valid token takes the discounted value that follows it from the
 //   nearest lane to the right, so that each lane's tokens are x' = P x + B; a scan of these gives every lane what comes in.
-//   Blocks with a sequence's end inside go through the general maps.
+//   Blocks with a sequence's end inside go through the general maps, token by token out of shared memory.
 template <bool TRACE, bool MOMENTS, bool MAPS> __global__ void __launch_bounds__(kAdvThreads, TRACE ? 5 : 6) advantage_kernel(const __grid_constant__ AdvantageArgs a)
 {
     using Op = AdvantageOp;
@@ -269,24 +315,27 @@ template <bool TRACE, bool MOMENTS, bool MAPS> __global__ void __launch_bounds__
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ Moments joined[kAdvWarps];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, chunk = blockIdx.x * kAdvWarps + warp;
-    grid_dependency_wait();
+    if (MAPS || !a.second) grid_dependency_wait();
     grid_dependency_release();
+    warm<MAPS>(a, chunk, lane, a.rewards, static_cast<const float *>(a.values_bf16 ? nullptr : a.values), a.trace, nullptr);
     const int live = a.q.live();
     double n = 0.0, shift = 0.0, sum = 0.0, squares = 0.0; // moments about a value of the warp's own,
     bool known = false;                                    // once there is one
-    if (chunk < a.chunks && (int64_t)chunk * a.chunk < live) {
-        const int t0 = chunk * a.chunk, t1 = live - t0 < a.chunk ? live : t0 + a.chunk;
+    if (chunk < a.chunks && (chunk << a.chunk) < live) {
+        const int t0 = chunk << a.chunk, t1 = min(live - t0, 1 << a.chunk) + t0;
         int s, s1, begin, end, cur = 0; // cur: where the current sequence begins
         a.q.owner_warp2(t0, t1 < live ? t1 : t1 - 1, lane, s, s1);
         Op::State st = Op::start();
+        int behind = 0; // pieces of the last sequence behind this chunk's
         auto terminal = [&](int o) -> double {
             return (a.outcome ? (double)__ldg(a.outcome + o) : 0.0) + a.gamma * (a.bootstrap ? (double)__ldg(a.bootstrap + o) : 0.0);
         };
         if (MAPS) {
             const int b = a.q.bound(s), e = a.q.bound(s + 1);
-            const int64_t after = (int64_t)t0 - b > a.piece ? ((int64_t)t0 - b + a.piece - 1) / a.piece : 1, p = b + after * a.piece;
+            const uint32_t off = t0 > b ? (uint32_t)(t0 - b) : 0u, up = (off + (1u << a.piece) - 1) >> a.piece;
+            const int64_t p = b + ((int64_t)max(up, 1u) << a.piece);
             begin = end = 0;
-            if (p >= t0 && p < t1 && p < e) begin = (int)p, end = e - begin < a.piece ? e : begin + a.piece;
+            if (p >= t0 && p < t1 && p < e) begin = (int)p, end = e - begin < (1 << a.piece) ? e : begin + (1 << a.piece);
         } else {
             begin = piece_from(a, t0, s, live);
             end = piece_from(a, t1, s1, live);
@@ -296,55 +345,63 @@ template <bool TRACE, bool MOMENTS, bool MAPS> __global__ void __launch_bounds__
                 if (cur >= end) s = a.q.owner_warp(end - 1, lane), cur = a.q.bound(s);
                 st.q = terminal(s);
                 const int e = a.q.bound(s + 1);
-                const int64_t behind = e > end ? ((int64_t)e - end + a.piece - 1) / a.piece : 0;
-                double none = 0.0;
-                st = behind_pieces<Op>(st, behind, lane, [&](int64_t i) {
-                    return static_cast<const Op::Map *>(a.maps)[(end + (behind - 1 - i) * a.piece) / a.chunk]; }, none);
+                behind = e > end ? (int)(((uint32_t)(e - end) + (1u << a.piece) - 1) >> a.piece) : 0;
             }
         }
         if (end > begin) {
             Feed<true, kTensors> feed;
-            feed.stage = reinterpret_cast<Stage8 (*)[kTensors]>(smem) + warp * kStages;
-            feed.mask = a.mask, feed.begin = begin, feed.end = end, feed.n_tok = (int)a.q.n_tok, feed.lane = lane, feed.vec = a.vec;
-            auto fetch = [&](Stage8 (&to)[kTensors], int k) {
+            feed.mem = reinterpret_cast<FeedMemory<kTensors> *>(smem) + warp;
+            feed.mask = a.mask, feed.begin = begin, feed.end = end, feed.n_tok = (int)a.q.n_tok, feed.off = (31 - lane) * 8, feed.vec = a.vec;
+            auto fetch = [&](Stage (&to)[kTensors], int first, bool whole) {
                 const int all = (int)a.q.n_tok;
-                if (a.rewards) fetch8(to[0], lane, a.rewards, k, all, a.vec);
+                if (a.rewards) fetch_block(to[0], lane, a.rewards, first, all, whole);
                 if (a.values) {
-                    if (a.values_bf16) fetch8(to[1], lane, static_cast<const uint16_t *>(a.values), k, all, a.vec);
-                    else fetch8(to[1], lane, static_cast<const float *>(a.values), k, all, a.vec);
+                    if (a.values_bf16) fetch_block(to[1], lane, static_cast<const uint16_t *>(a.values), first, all, whole);
+                    else fetch_block(to[1], lane, static_cast<const float *>(a.values), first, all, whole);
                 }
-                if (TRACE) fetch8(to[kTensors - 1], lane, a.trace, k, all, a.vec);
+                if (TRACE) fetch_block(to[kTensors - 1], lane, a.trace, first, all, whole);
             };
             feed.start(fetch);
+            if (!MAPS && a.second) {
+                grid_dependency_wait();
+                double none = 0.0;
+                st = behind_pieces<Op>(st, behind, lane, [&](int i) {
+                    return static_cast<const Op::Map *>(a.maps)[(end + ((int64_t)(behind - 1 - i) << a.piece)) >> a.chunk]; }, none);
+            }
             double P_all = 1.0, w_right = a.weight, ahead = 1.0; // MAPS: product of the weights but the rightmost one's, and that; weight^(8 lane)
-            int64_t count = 0;
+            int count = 0;
             if (!TRACE)
                 for (int i = 0; i < 5; ++i)
                     if (lane >> i & 1) ahead *= a.powers[i];
-            for (int i = 0; i < feed.blocks; ++i) {
+            int slot = 0;
+#pragma unroll 1
+            for (; feed.left > 0; feed.next(), slot = slot + 1 == kStages ? 0 : slot + 1) {
                 const uint32_t valid = feed.arrive();
-                const int base = feed.block(i) << 8, k = feed.place(i), lo = max(base, begin), hi = min(base + 256, end);
-                float r[8], v[8], c[8], adv[8], ret[8];
+                const int base = feed.base, k = base + feed.off, lo = max(base, begin), hi = min(base + kBlock, end);
+                const uint32_t some = __ballot_sync(kAll, valid != 0);
+                float adv[8], ret[8];
                 if (!MAPS && cur >= hi) { // on to the sequence before, whose end is where this block ends
                     s = a.q.owner_warp(hi - 1, lane);
                     cur = a.q.bound(s);
                     st = Op::State{0.0, terminal(s)};
                 }
-                const uint32_t some = __ballot_sync(kAll, valid != 0);
-                if (some == 0 && (MAPS || cur <= lo)) {
-                    zero8(adv);
-                    zero8(ret);
-                } else {
-                    const Stage8 *x = feed.stage[feed.at];
-                    if (a.rewards) read8(x[0], lane, r);
-                    else zero8(r);
-                    if (!a.values) zero8(v);
-                    else if (a.values_bf16) read8_bf16(x[1], lane, v);
-                    else read8(x[1], lane, v);
-                    if (TRACE) read8(x[kTensors - 1], lane, c);
-                    double D[8];
-                    if (MAPS || cur <= lo) {
-                        if (!TRACE && __all_sync(kAll, valid == 0xFFu)) {
+                Stage *x = feed.mem->stage[slot];
+                if (MAPS || cur <= lo) {
+                    if (some == 0) {
+                        feed.release(slot, fetch);
+                        zero8(adv);
+                        zero8(ret);
+                    } else {
+                        float r[8], v[8], c[8];
+                        double D[8];
+                        if (a.rewards) read8(x[0], 31 - lane, r);
+                        else zero8(r);
+                        if (!a.values) zero8(v);
+                        else if (a.values_bf16) read8_bf16(x[1], 31 - lane, v);
+                        else read8(x[1], 31 - lane, v);
+                        if (TRACE) read8(x[kTensors - 1], 31 - lane, c);
+                        feed.release(slot, fetch);
+                        if (!TRACE && __all_sync(kAll, valid == 0xFFu)) { // every lane's P is weight^8
                             const double first = a.gamma * (double)v[0], from = __shfl_up_sync(kAll, first, 1);
                             double q = lane == 0 ? st.q : from, B = 0.0;
 #pragma unroll
@@ -363,8 +420,10 @@ template <bool TRACE, bool MOMENTS, bool MAPS> __global__ void __launch_bounds__
                             }
                             st.x = __shfl_sync(kAll, z, 31);
                             st.q = __shfl_sync(kAll, first, 31);
+                            if (MAPS) count += kBlock;
                         } else {
-                            float leftmost = 0.0f;
+                            // masked tokens hold the value that follows them, and leave B and z as they are
+                            float leftmost = v[0];
 #pragma unroll
                             for (int e = 7; e >= 0; --e) leftmost = valid >> e & 1 ? v[e] : leftmost;
                             const uint32_t right = some & ((1u << lane) - 1);
@@ -401,59 +460,98 @@ template <bool TRACE, bool MOMENTS, bool MAPS> __global__ void __launch_bounds__
                             if (MAPS && TRACE) P_all *= __shfl_sync(kAll, m.P, 31);
                             st.x = __shfl_sync(kAll, z, 31);
                             st.q = __shfl_sync(kAll, first, 31 - __clz(some));
+                            if (MAPS) count += TRACE ? 1 : (int)__reduce_add_sync(kAll, (unsigned)__popc(valid));
                         }
-                        if (MAPS) count += TRACE ? 1 : (int)__reduce_add_sync(kAll, (unsigned)__popc(valid));
-                    } else if (!MAPS) {
-                        const int s_right = s;
-                        const uint32_t ends = ends_inside<true>(a.q, base, lo, hi, lane, 31 - lane, s, [](int, int) {});
-                        cur = a.q.bound(s);
-                        Op::Map mine = Op::identity();
+                        if (MOMENTS) {
+                            if (!known) { // an advantage of the warp's first block: one of the lane with the first bit
+                                double one = D[0];
 #pragma unroll
-                        for (int e = 7; e >= 0; --e) {
-                            if (ends >> e & 1) mine = Op::Map{0.0, 0.0, 0.0, terminal(a.q.owner(k + e, s, s_right)), 2u, 0u};
-                            if (valid >> e & 1) {
-                                const double w = TRACE ? a.weight * (double)c[e] : a.weight, d = (double)r[e] - (double)v[e], q = a.gamma * (double)v[e];
-                                if (mine.flag == 0) mine = Op::Map{w, 1.0, d, q, 1u, 0u};
-                                else mine = Op::Map{w * mine.P, w * mine.Q, fma(w, mine.B, d + mine.c), q, mine.flag, 0u};
+                                for (int e = 1; e < 8; ++e) one = valid >> e & 1 ? D[e] : one;
+                                shift = __shfl_sync(kAll, one, __ffs(some) - 1);
+                                known = true;
+                            }
+                            double s1[2] = {0.0, 0.0}, s2[2] = {0.0, 0.0};
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                const double d = valid >> e & 1 ? D[e] - shift : 0.0;
+                                s1[e & 1] += d;
+                                s2[e & 1] = fma(d, d, s2[e & 1]);
+                            }
+                            sum += s1[0] + s1[1];
+                            squares += s2[0] + s2[1];
+                            n += (double)__popc(valid);
+                        }
+                    }
+                    if (!MAPS) {
+                        if (a.vec && hi - lo == kBlock) {
+                            if (a.adv) store8(a.adv + k, adv);
+                            if (a.returns) store8(a.returns + k, ret);
+                        } else {
+                            if (a.adv) store8(a.adv, k, lo, hi, a.vec, adv);
+                            if (a.returns) store8(a.returns, k, lo, hi, a.vec, ret);
+                        }
+                    }
+                } else if (!MAPS) {
+                    const int s_right = s;
+                    const uint32_t ends = ends_inside<true>(a.q, base, lo, hi, lane, 31 - lane, s, [](int, int) {});
+                    cur = a.q.bound(s);
+                    auto number = [&](int tensor, int e) -> float { return stage_at(x[tensor], feed.off + e); };
+                    if (a.values && a.values_bf16) widen(x[1], lane);
+                    auto advantage = [&](int e, double &d, double &V, double &w) {
+                        V = a.values ? (double)number(1, e) : 0.0;
+                        d = (a.rewards ? (double)number(0, e) : 0.0) - V;
+                        w = TRACE ? a.weight * (double)number(kTensors - 1, e) : a.weight;
+                    };
+                    Op::Map mine = Op::identity();
+                    double d, V, w;
+#pragma unroll 1
+                    for (int e = 7; e >= 0; --e) {
+                        if (ends >> e & 1) mine = Op::Map{0.0, 0.0, 0.0, terminal(a.q.owner(k + e, s, s_right)), 2u, 0u};
+                        if (valid >> e & 1) {
+                            advantage(e, d, V, w);
+                            if (mine.flag == 0) mine = Op::Map{w, 1.0, d, a.gamma * V, 1u, 0u};
+                            else mine = Op::Map{w * mine.P, w * mine.Q, fma(w, mine.B, d + mine.c), a.gamma * V, mine.flag, 0u};
+                        }
+                    }
+                    Op::Map all;
+                    const Op::Map before = warp_scan<Op>(mine, lane, all);
+                    Op::State z = Op::apply(before, st);
+                    double own = shift, m0 = 0.0, m1 = 0.0, m2 = 0.0; // about the lane's first advantage while the warp has none
+#pragma unroll 1
+                    for (int e = 7; e >= 0; --e) {
+                        if (ends >> e & 1) z = Op::State{0.0, terminal(a.q.owner(k + e, s, s_right))};
+                        float A = 0.0f, R = 0.0f;
+                        if (valid >> e & 1) {
+                            advantage(e, d, V, w);
+                            z.x = fma(w, z.x, d + z.q);
+                            z.q = a.gamma * V;
+                            A = (float)z.x;
+                            R = (float)(z.x + V);
+                            if (MOMENTS) {
+                                if (!known && m0 == 0.0) own = z.x;
+                                const double o = z.x - own;
+                                m0 += 1.0;
+                                m1 += o;
+                                m2 = fma(o, o, m2);
                             }
                         }
-                        Op::Map all;
-                        const Op::Map before = warp_scan<Op>(mine, lane, all);
-                        Op::State z = Op::apply(before, st);
-#pragma unroll
-                        for (int e = 7; e >= 0; --e) {
-                            adv[e] = ret[e] = 0.0f;
-                            if (ends >> e & 1) z = Op::State{0.0, terminal(a.q.owner(k + e, s, s_right))};
-                            if (valid >> e & 1) {
-                                const double V = (double)v[e];
-                                z.x = fma(TRACE ? a.weight * (double)c[e] : a.weight, z.x, ((double)r[e] - V) + z.q);
-                                z.q = a.gamma * V;
-                                adv[e] = (float)z.x;
-                                ret[e] = (float)(z.x + V);
-                            }
-                            D[e] = z.x;
-                        }
-                        st = shfl_words(z, 31);
+                        stage_at(x[0], feed.off + e) = A;
+                        stage_at(x[1], feed.off + e) = R;
                     }
                     if (MOMENTS && some != 0) {
-                        if (!known) { // an advantage of the warp's first block: one of the lane with the first bit
-                            double one = 0.0;
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) one = valid >> e & 1 ? D[e] : one;
-                            shift = __shfl_sync(kAll, one, __ffs(some) - 1);
-                            known = true;
+                        if (!known) shift = __shfl_sync(kAll, own, __ffs(some) - 1), known = true;
+                        const double d0 = own - shift;
+                        if (m0 > 0.0) {
+                            n += m0;
+                            squares += m2 + d0 * (2.0 * m1 + m0 * d0);
+                            sum += m1 + m0 * d0;
                         }
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const double d = valid >> e & 1 ? D[e] - shift : 0.0;
-                            sum += d;
-                            squares = fma(d, d, squares);
-                        }
-                        n += (double)__popc(valid);
                     }
-                }
-                feed.release(i, fetch);
-                if (!MAPS) {
+                    st = shfl_words(z, 31);
+                    __syncwarp();
+                    read8(x[0], 31 - lane, adv);
+                    read8(x[1], 31 - lane, ret);
+                    feed.release(slot, fetch);
                     if (a.adv) store8(a.adv, k, lo, hi, a.vec, adv);
                     if (a.returns) store8(a.returns, k, lo, hi, a.vec, ret);
                 }
@@ -465,6 +563,7 @@ template <bool TRACE, bool MOMENTS, bool MAPS> __global__ void __launch_bounds__
             }
         }
     }
+    if (!MAPS && a.second) grid_dependency_wait(); // no CTA ends before the maps' launch has
     if (MOMENTS) {
         n = warp_sum(n);
         sum = warp_sum(sum);
@@ -504,19 +603,23 @@ __global__ void __launch_bounds__(kMomentThreads) advantage_moments_kernel(const
     }
 }
 
+constexpr int kGradThreads = 96; // three warps, as four of up to four tensors would not fit into 48 KB
+constexpr int kGradWarps = kGradThreads / 32;
+
 // The tokens of a chunk's pieces from the first to the last, 256 at a time.  MAPS: the map of the piece that begins in the chunk and
 // is not its sequence's last.  Blocks inside one sequence and blocks with an end inside as in the forward kernel; here a lane's first
 // valid token takes the weight of the valid token before it from the nearest lane to the left.  d c of a token needs the advantage
 // of its follower: where that is in a later block, the token stays open until then.
 template <bool TRACE, bool BY_TRACE, bool MAPS>
-__global__ void __launch_bounds__(kAdvThreads, TRACE || BY_TRACE ? 4 : 6) advantage_grad_kernel(const __grid_constant__ AdvantageArgs a)
+__global__ void __launch_bounds__(kGradThreads, TRACE || BY_TRACE ? 5 : 8) advantage_grad_kernel(const __grid_constant__ AdvantageArgs a)
 {
     using Op = AdvantageGradOp;
     constexpr int kTensors = 2 + TRACE + BY_TRACE;
     extern __shared__ __align__(16) unsigned char smem[];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, chunk = blockIdx.x * kAdvWarps + warp;
-    grid_dependency_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, chunk = blockIdx.x * kGradWarps + warp;
+    if (MAPS || !a.second) grid_dependency_wait();
     grid_dependency_release();
+    warm<MAPS>(a, chunk, lane, a.grad_adv, a.grad_returns, a.trace, a.adv_in);
     const int live = a.q.live();
     const bool per_sequence = a.grad_outcome || a.grad_bootstrap;
     auto put = [&](int o, double G) {
@@ -524,40 +627,55 @@ __global__ void __launch_bounds__(kAdvThreads, TRACE || BY_TRACE ? 4 : 6) advant
         if (a.grad_bootstrap) a.grad_bootstrap[o] = (float)(a.gamma * G);
     };
     if (!MAPS && live <= 0) { // no tokens: no gradients
+        if (a.second) grid_dependency_wait();
         if (per_sequence)
-            for (int64_t o = (int64_t)blockIdx.x * kAdvThreads + threadIdx.x; o < a.q.n_seq; o += (int64_t)gridDim.x * kAdvThreads) put((int)o, 0.0);
+            for (int64_t o = (int64_t)blockIdx.x * kGradThreads + threadIdx.x; o < a.q.n_seq; o += (int64_t)gridDim.x * kGradThreads) put((int)o, 0.0);
         return;
     }
-    if (chunk >= a.chunks || (int64_t)chunk * a.chunk >= live)
-        return;
-    const int t0 = chunk * a.chunk, t1 = live - t0 < a.chunk ? live : t0 + a.chunk;
-    int s, s1, begin, end;
-    a.q.owner_warp2(t0, MAPS || t1 >= live ? t1 - 1 : t1, lane, s, s1);
-    Op::State st = Op::start();
-    double w_before = 0.0; // TRACE: weight of the valid token before
-    int e_cur = live;      // where the current sequence ends
-    if (MAPS) {
-        begin = end = 0;
-        for (int which = 0; which < 2; ++which) { // of the chunk's first sequence, or of its last
-            const int o = which == 0 ? s : s1, b = a.q.bound(o), e = a.q.bound(o + 1);
-            const int64_t p = b >= t0 ? b : b + ((int64_t)t0 - b + a.piece - 1) / a.piece * a.piece;
-            if (p >= t0 && p < t1 && p + a.piece < e) begin = (int)p, end = begin + a.piece;
+    int s = 0, s1, b = 0, begin = 0, end = 0, e_cur = live; // e_cur: where the current sequence ends
+    if (chunk < a.chunks && (chunk << a.chunk) < live) {
+        const int t0 = chunk << a.chunk, t1 = min(live - t0, 1 << a.chunk) + t0;
+        a.q.owner_warp2(t0, MAPS || t1 >= live ? t1 - 1 : t1, lane, s, s1);
+        if (MAPS) {
+#pragma unroll 1
+            for (int which = 0; which < 2; ++which) { // of the chunk's first sequence, or of its last
+                const int o = which == 0 ? s : s1, from = a.q.bound(o), e = a.q.bound(o + 1);
+                const uint32_t off = t0 > from ? (uint32_t)(t0 - from) : 0u, up = ((off + (1u << a.piece) - 1) >> a.piece) << a.piece;
+                const int64_t p = (int64_t)from + up;
+                if (p >= t0 && p < t1 && p + (1 << a.piece) < e) begin = (int)p, end = begin + (1 << a.piece);
+            }
+        } else {
+            begin = piece_from(a, t0, s, live);
+            end = piece_from(a, t1, s1, live);
         }
-    } else {
-        begin = piece_from(a, t0, s, live);
-        end = piece_from(a, t1, s1, live);
-        if (per_sequence && t0 == 0) // sequences without a token ahead of the first one
-            for (int o = lane; o < s; o += 32) put(o, 0.0);
     }
-    if (end <= begin)
-        return;
-    if (!MAPS) {
-        int b = a.q.bound(s);
+    const int s_first = s;
+    if (!MAPS && end > begin) {
+        b = a.q.bound(s);
         e_cur = a.q.bound(s + 1);
         if (begin >= e_cur) s = a.q.owner_warp(begin, lane), b = a.q.bound(s), e_cur = a.q.bound(s + 1);
-        st = behind_pieces<Op>(st, ((int64_t)begin - b) / a.piece, lane,
-                               [&](int64_t i) { return static_cast<const Op::Map *>(a.maps)[(b + i * a.piece) / a.chunk]; }, w_before);
     }
+    Feed<false, kTensors> feed;
+    feed.mem = reinterpret_cast<FeedMemory<kTensors> *>(smem) + warp;
+    feed.mask = a.mask, feed.begin = begin, feed.end = end, feed.n_tok = (int)a.q.n_tok, feed.off = lane * 8, feed.vec = a.vec;
+    auto fetch = [&](Stage (&to)[kTensors], int first, bool whole) {
+        const int all = (int)a.q.n_tok;
+        if (a.grad_adv) fetch_block(to[0], lane, a.grad_adv, first, all, whole);
+        if (a.grad_returns) fetch_block(to[1], lane, a.grad_returns, first, all, whole);
+        if (TRACE) fetch_block(to[2], lane, a.trace, first, all, whole);
+        if (BY_TRACE) fetch_block(to[kTensors - 1], lane, a.adv_in, first, all, whole);
+    };
+    if (end > begin) feed.start(fetch);
+    if (!MAPS && a.second) grid_dependency_wait(); // for the maps; and no CTA ends before their launch has
+    if (!MAPS && per_sequence && chunk == 0)       // sequences without a token ahead of the first one
+        for (int o = lane; o < s_first; o += 32) put(o, 0.0);
+    if (end <= begin)
+        return;
+    Op::State st = Op::start();
+    double w_before = 0.0; // TRACE: weight of the valid token before
+    if (!MAPS && a.second)
+        st = behind_pieces<Op>(st, begin > b ? (begin - b) >> a.piece : 0, lane,
+                               [&](int i) { return static_cast<const Op::Map *>(a.maps)[(b + ((int64_t)i << a.piece)) >> a.chunk]; }, w_before);
     // The current sequence's last gradient, then on to the one that holds token `to`; those between without a token get zeros.
     auto next_sequence = [&](int to) {
         if (lane == 0) {
@@ -579,47 +697,40 @@ __global__ void __launch_bounds__(kAdvThreads, TRACE || BY_TRACE ? 4 : 6) advant
         st = Op::start();
         w_before = 0.0;
     };
-    Feed<false, kTensors> feed;
-    feed.stage = reinterpret_cast<Stage8 (*)[kTensors]>(smem) + warp * kStages;
-    feed.mask = a.mask, feed.begin = begin, feed.end = end, feed.n_tok = (int)a.q.n_tok, feed.lane = lane, feed.vec = a.vec;
-    auto fetch = [&](Stage8 (&to)[kTensors], int k) {
-        const int all = (int)a.q.n_tok;
-        if (a.grad_adv) fetch8(to[0], lane, a.grad_adv, k, all, a.vec);
-        if (a.grad_returns) fetch8(to[1], lane, a.grad_returns, k, all, a.vec);
-        if (TRACE) fetch8(to[2], lane, a.trace, k, all, a.vec);
-        if (BY_TRACE) fetch8(to[kTensors - 1], lane, a.adv_in, k, all, a.vec);
-    };
-    feed.start(fetch);
     double P_all = 1.0, ahead = 1.0; // MAPS: product of the weights but the last one's; weight^(8 lane)
-    int64_t count = 0;
+    int count = 0;
     if (!TRACE)
         for (int i = 0; i < 5; ++i)
             if (lane >> i & 1) ahead *= a.powers[i];
-    for (int i = 0; i < feed.blocks; ++i) {
+    int slot = 0;
+#pragma unroll 1
+    for (; feed.left > 0; feed.next(), slot = slot + 1 == kStages ? 0 : slot + 1) {
         const uint32_t valid = feed.arrive();
-        const int base = feed.block(i) << 8, k = feed.place(i), lo = max(base, begin), hi = min(base + 256, end);
-        float ga[8], gr[8], c[8], A[8], dr[8], dv[8], dc[8];
-        int open = -1; // this lane's token that waits for its follower
+        const int base = feed.base, k = base + feed.off, lo = max(base, begin), hi = min(base + kBlock, end);
         if (!MAPS && e_cur <= lo) next_sequence(lo);
         const uint32_t some = __ballot_sync(kAll, valid != 0);
-        const bool inside = MAPS || e_cur >= hi;
-        if (some == 0 && inside) {
-            zero8(dr);
-            zero8(dv);
-            zero8(dc);
-        } else {
-            const Stage8 *x = feed.stage[feed.at];
-            if (a.grad_adv) read8(x[0], lane, ga);
-            else zero8(ga);
-            if (a.grad_returns) read8(x[1], lane, gr);
-            else zero8(gr);
-            if (TRACE) read8(x[2], lane, c);
-            if (BY_TRACE) read8(x[kTensors - 1], lane, A);
-            if (inside) {
+        Stage *x = feed.mem->stage[slot];
+        float dr[8], dv[8], dc[8];
+        int open = -1; // this lane's token that waits for its follower
+        if (MAPS || e_cur >= hi) {
+            if (some == 0) {
+                feed.release(slot, fetch);
+                zero8(dr);
+                zero8(dv);
+                if (BY_TRACE) zero8(dc);
+            } else {
+                float ga[8], gr[8], c[8], A[8];
+                if (a.grad_adv) read8(x[0], lane, ga);
+                else zero8(ga);
+                if (a.grad_returns) read8(x[1], lane, gr);
+                else zero8(gr);
+                if (TRACE) read8(x[2], lane, c);
+                if (BY_TRACE) read8(x[kTensors - 1], lane, A);
+                feed.release(slot, fetch);
                 const uint32_t left = some & ((1u << lane) - 1);
                 const int from = left ? 31 - __clz(left) : 0, tail = 31 - __clz(some);
                 double g[8], G;
-                if (!TRACE && __all_sync(kAll, valid == 0xFFu)) {
+                if (!TRACE && __all_sync(kAll, valid == 0xFFu)) { // every lane's P is weight^8
                     double B = 0.0;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
@@ -645,17 +756,20 @@ __global__ void __launch_bounds__(kAdvThreads, TRACE || BY_TRACE ? 4 : 6) advant
                         w_before = a.weight * (double)__shfl_sync(kAll, c_last, tail);
                     }
                     Line m{1.0, 0.0};
-                    double w = MAPS && count == 0 && !left ? 1.0 : w_in; // the weight of what comes into the piece is applied to it before
+                    double w = MAPS && TRACE && count == 0 && !left ? 1.0 : w_in; // the weight of what comes into the piece is applied to it before
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const bool in = valid >> e & 1;
                         g[e] = (double)ga[e] + (double)gr[e];
-                        const double B = fma(w, m.B, g[e]), P = w * m.P;
+                        const double B = fma(w, m.B, g[e]);
                         m.B = in ? B : m.B;
-                        m.P = in ? P : m.P;
-                        if (TRACE) w = in ? a.weight * (double)c[e] : w;
-                        else w = in ? a.weight : w;
+                        if (TRACE) {
+                            const double P = w * m.P;
+                            m.P = in ? P : m.P;
+                            w = in ? a.weight * (double)c[e] : w;
+                        }
                     }
+                    if (!TRACE) m.P = a.small[__popc(valid)];
                     const Line before = scan_lines(m, lane);
                     G = fma(before.P, st.G, before.B);
                     if (MAPS && TRACE) P_all *= __shfl_sync(kAll, m.P, 31);
@@ -693,60 +807,80 @@ __global__ void __launch_bounds__(kAdvThreads, TRACE || BY_TRACE ? 4 : 6) advant
                 st.G = __shfl_sync(kAll, G, tail);
                 st.pos = __shfl_sync(kAll, last_of, tail);
                 if (MAPS) count += TRACE ? 1 : (int)__reduce_add_sync(kAll, (unsigned)__popc(valid));
-            } else { // sequences end inside
-                const int s_left = s;
-                const uint32_t ends = ends_inside<false>(a.q, base, lo, hi, lane, lane, s, [&](int o, int p) {
-                    if (per_sequence && p <= a.q.bound(o)) put(o, 0.0);
-                });
-                e_cur = a.q.bound(s + 1);
-                if (e_cur < hi) e_cur = live; // boundaries out of order
-                Op::Map mine = Op::identity();
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    if (valid >> e & 1) {
-                        const double w = TRACE ? a.weight * (double)c[e] : a.weight, g = (double)ga[e] + (double)gr[e];
-                        if (mine.flag == 0) mine = Op::Map{1.0, g, w, k + e, 1u};
-                        else mine = Op::Map{mine.wl * mine.P, fma(mine.wl, mine.B, g), w, k + e, mine.flag};
-                    }
-                    if (ends >> e & 1) mine = Op::Map{0.0, 0.0, 0.0, -1, 2u};
-                }
-                Op::Map all;
-                const Op::Map before = warp_scan<Op>(mine, lane, all);
-                st.y = (TRACE ? w_before : a.weight) * st.G;
-                Op::State z = Op::apply(before, st);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    dr[e] = dv[e] = 0.0f;
-                    if (valid >> e & 1) {
-                        const double w = TRACE ? a.weight * (double)c[e] : a.weight, G = ((double)ga[e] + (double)gr[e]) + z.y;
-                        if (BY_TRACE && z.pos >= 0) a.grad_trace[z.pos] = (float)(a.weight * (double)A[e] * z.G);
-                        dr[e] = (float)G;
-                        dv[e] = (float)(fma(a.gamma, z.G, (double)gr[e]) - G);
-                        z = Op::State{w * G, G, k + e, 0};
-                    } else if (BY_TRACE && k + e >= lo && k + e < hi) {
-                        a.grad_trace[k + e] = 0.0f;
-                    }
-                    if (ends >> e & 1) {
-                        if (BY_TRACE && z.pos >= 0) a.grad_trace[z.pos] = 0.0f;
-                        if (per_sequence) put(a.q.owner(k + e, s_left, s), z.G);
-                        z = Op::start();
-                    }
-                }
-                st = shfl_words(z, 31);
-                w_before = Op::last_weight(shfl_words(all, 31), w_before);
             }
-        }
-        feed.release(i, fetch);
-        if (!MAPS) {
+            if (!MAPS) {
+                if (a.vec && hi - lo == kBlock) {
+                    if (a.grad_rewards) store8(a.grad_rewards + k, dr);
+                    if (a.grad_values) store8(a.grad_values + k, dv);
+                } else {
+                    if (a.grad_rewards) store8(a.grad_rewards, k, lo, hi, a.vec, dr);
+                    if (a.grad_values) store8(a.grad_values, k, lo, hi, a.vec, dv);
+                }
+                if (BY_TRACE) {
+                    if (open < 0) store8(a.grad_trace, k, lo, hi, a.vec, dc);
+                    else
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (k + e >= lo && k + e < hi && k + e != open) a.grad_trace[k + e] = dc[e];
+                }
+            }
+        } else if (!MAPS) { // sequences end inside
+            const int s_left = s;
+            const uint32_t ends = ends_inside<false>(a.q, base, lo, hi, lane, lane, s, [&](int o, int p) {
+                if (per_sequence && p <= a.q.bound(o)) put(o, 0.0);
+            });
+            e_cur = a.q.bound(s + 1);
+            if (e_cur < hi) e_cur = live; // boundaries out of order
+            auto number = [&](int tensor, int e) -> double { return (double)stage_at(x[tensor], feed.off + e); };
+            auto token = [&](int e, double &g, double &r, double &w) {
+                r = a.grad_returns ? number(1, e) : 0.0;
+                g = (a.grad_adv ? number(0, e) : 0.0) + r;
+                w = TRACE ? a.weight * number(2, e) : a.weight;
+            };
+            Op::Map mine = Op::identity();
+            double g, r, w;
+#pragma unroll 1
+            for (int e = 0; e < 8; ++e) {
+                if (valid >> e & 1) {
+                    token(e, g, r, w);
+                    if (mine.flag == 0) mine = Op::Map{1.0, g, w, k + e, 1u};
+                    else mine = Op::Map{mine.wl * mine.P, fma(mine.wl, mine.B, g), w, k + e, mine.flag};
+                }
+                if (ends >> e & 1) mine = Op::Map{0.0, 0.0, 0.0, -1, 2u};
+            }
+            Op::Map all;
+            const Op::Map before = warp_scan<Op>(mine, lane, all);
+            st.y = (TRACE ? w_before : a.weight) * st.G;
+            Op::State z = Op::apply(before, st);
+#pragma unroll 1
+            for (int e = 0; e < 8; ++e) {
+                float R = 0.0f, V = 0.0f;
+                if (valid >> e & 1) {
+                    token(e, g, r, w);
+                    const double G = g + z.y;
+                    if (BY_TRACE && z.pos >= 0) a.grad_trace[z.pos] = (float)(a.weight * number(kTensors - 1, e) * z.G);
+                    R = (float)G;
+                    V = (float)(fma(a.gamma, z.G, r) - G);
+                    z = Op::State{w * G, G, k + e, 0};
+                } else if (BY_TRACE && k + e >= lo && k + e < hi) {
+                    a.grad_trace[k + e] = 0.0f;
+                }
+                if (ends >> e & 1) {
+                    if (BY_TRACE && z.pos >= 0) a.grad_trace[z.pos] = 0.0f;
+                    if (per_sequence) put(a.q.owner(k + e, s_left, s), z.G);
+                    z = Op::start();
+                }
+                stage_at(x[0], feed.off + e) = R;
+                stage_at(x[1], feed.off + e) = V;
+            }
+            st = shfl_words(z, 31);
+            w_before = Op::last_weight(shfl_words(all, 31), w_before);
+            __syncwarp();
+            read8(x[0], lane, dr);
+            read8(x[1], lane, dv);
+            feed.release(slot, fetch);
             if (a.grad_rewards) store8(a.grad_rewards, k, lo, hi, a.vec, dr);
             if (a.grad_values) store8(a.grad_values, k, lo, hi, a.vec, dv);
-            if (BY_TRACE && inside) {
-                if (open < 0) store8(a.grad_trace, k, lo, hi, a.vec, dc);
-                else
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (k + e >= lo && k + e < hi && k + e != open) a.grad_trace[k + e] = dc[e];
-            }
         }
     }
     if (MAPS) {
@@ -768,17 +902,18 @@ static bool all_vectors(const AdvantageArgs &a)
 constexpr int64_t kChunks = 148 * 24;
 static void deal(AdvantageArgs &a)
 {
-    a.chunk = 256;
-    while (a.chunk < 2048 && a.chunk * kChunks < a.q.n_tok) a.chunk *= 2;
-    a.piece = 4 * a.chunk;
-    a.chunks = (int)((a.q.n_tok + a.chunk - 1) / a.chunk);
+    a.chunk = 8;
+    while (a.chunk < 11 && (kChunks << a.chunk) < a.q.n_tok) ++a.chunk;
+    a.piece = a.chunk + 2;
+    a.chunks = (int)((a.q.n_tok + (1 << a.chunk) - 1) >> a.chunk);
     for (int i = 0; i < 9; ++i) a.small[i] = std::pow(a.weight, i);
+    a.warm = a.chunks <= kChunks;
     a.powers[0] = a.small[8];
     for (int i = 1; i < 5; ++i) a.powers[i] = a.powers[i - 1] * a.powers[i - 1];
 }
 
 // Whether a sequence can be longer than a piece, as far as the host knows.
-static bool long_sequences(const AdvantageArgs &a) { return (a.q.cu ? a.q.n_tok : a.q.T) > a.piece; }
+static bool long_sequences(const AdvantageArgs &a) { return (a.q.cu ? a.q.n_tok : a.q.T) > (int64_t)1 << a.piece; }
 
 } // namespace hilore
 
@@ -817,8 +952,9 @@ extern "C" int hilore_advantages(const float *rewards, const float *outcome, con
     a.partials = reinterpret_cast<double *>(static_cast<AdvantageOp::Map *>(workspace) + a.chunks + 1);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const unsigned grid = (unsigned)((a.chunks + kAdvWarps - 1) / kAdvWarps);
-    const size_t smem = kAdvWarps * kStages * sizeof(Stage8) * (trace ? 3 : 2);
-    if (grid > 0 && long_sequences(a) &&
+    const size_t smem = kAdvWarps * (trace ? sizeof(FeedMemory<3>) : sizeof(FeedMemory<2>));
+    a.second = long_sequences(a);
+    if (grid > 0 && a.second &&
         launch_dependent(trace ? advantage_kernel<true, false, true> : advantage_kernel<false, false, true>, dim3(grid), dim3(kAdvThreads), smem, st, a) != cudaSuccess)
         return HILORE_CUDA;
     void (*kernel)(AdvantageArgs) = moments ? (trace ? advantage_kernel<true, true, false> : advantage_kernel<false, true, false>)
@@ -859,15 +995,16 @@ extern "C" int hilore_advantages_backward(const float *grad_adv, const float *gr
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (n_seq == 0)
         return HILORE_OK;
-    const unsigned grid = a.chunks > 0 ? (unsigned)((a.chunks + kAdvWarps - 1) / kAdvWarps) : 1u;
+    const unsigned grid = a.chunks > 0 ? (unsigned)((a.chunks + kGradWarps - 1) / kGradWarps) : 1u;
     void (*const maps)(AdvantageArgs) = trace ? advantage_grad_kernel<true, false, true> : advantage_grad_kernel<false, false, true>;
     void (*const kernel)(AdvantageArgs) =
         grad_trace ? (trace ? advantage_grad_kernel<true, true, false> : advantage_grad_kernel<false, true, false>)
                    : (trace ? advantage_grad_kernel<true, false, false> : advantage_grad_kernel<false, false, false>);
-    const size_t smem = kAdvWarps * kStages * sizeof(Stage8);
-    if (long_sequences(a) && launch_dependent(maps, dim3(grid), dim3(kAdvThreads), smem * (trace ? 3 : 2), st, a) != cudaSuccess)
+    const size_t smem[3] = {kGradWarps * sizeof(FeedMemory<2>), kGradWarps * sizeof(FeedMemory<3>), kGradWarps * sizeof(FeedMemory<4>)};
+    a.second = long_sequences(a);
+    if (a.second && launch_dependent(maps, dim3(grid), dim3(kGradThreads), smem[trace != nullptr], st, a) != cudaSuccess)
         return HILORE_CUDA;
-    if (launch_dependent(kernel, dim3(grid), dim3(kAdvThreads), smem * (2 + (trace != nullptr) + (grad_trace != nullptr)), st, a) != cudaSuccess)
+    if (launch_dependent(kernel, dim3(grid), dim3(kGradThreads), smem[(trace != nullptr) + (grad_trace != nullptr)], st, a) != cudaSuccess)
         return HILORE_CUDA;
     return cudaGetLastError() == cudaSuccess ? HILORE_OK : HILORE_CUDA;
 }

@@ -162,6 +162,14 @@ __device__ __forceinline__ void zero8(float (&x)[8])
     for (int e = 0; e < 8; ++e) x[e] = 0.0f;
 }
 
+__device__ __forceinline__ void store8(float *p, const float (&x)[8])
+{
+    uint32_t w[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = __float_as_uint(x[e]);
+    st_global_256(p, w);
+}
+
 // Those of the eight tokens that lie in [lo, hi).
 __device__ __forceinline__ void store8(float *p, int k, int lo, int hi, bool vec, const float (&x)[8])
 {
@@ -177,54 +185,63 @@ __device__ __forceinline__ void store8(float *p, int k, int lo, int hi, bool vec
     }
 }
 
-// ---- eight tokens of every lane of a warp, on their way through shared memory ----
-// cp.async holds no registers while the data is on its way, so a warp can have several blocks of 256 tokens in flight; a lane reads
-// back what it asked for itself, so nothing but its own wait is needed.  The two halves of a lane's eight numbers lie 512 bytes
-// apart: 16-byte accesses of neighbouring lanes then touch neighbouring addresses.
-struct Stage8 {
-    float x[2][32][4];
+// ---- blocks of 256 tokens on their way through shared memory ----
+// cp.async holds no registers while the data is on its way, so a warp can have several blocks in flight.  Every instruction copies
+// 512 neighbouring bytes (sixteen bytes of every thirty-two would ask L2 for each sector twice), so lanes read what others asked
+// for.  Pieces of four numbers are swapped in pairs in every other row of eight, which lets lanes read their two without conflicts.
+constexpr int kBlock = 256;
+struct Stage {
+    float4 x[kBlock / 4];
 };
-__device__ __forceinline__ void copy_async(void *to, const void *from, int bytes) // 4 or 16
+__device__ __forceinline__ int swapped(int c) { return c ^ (c >> 3 & 1); }
+__device__ __forceinline__ void copy_async(void *to, const void *from, int bytes) // 4, 8 or 16
 {
     const uint32_t d = (uint32_t)__cvta_generic_to_shared(to);
     if (bytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d), "l"(from) : "memory");
+    else if (bytes == 8) asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(d), "l"(from) : "memory");
     else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(d), "l"(from) : "memory");
 }
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int LEFT> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 
-// Tokens k .. k + 7 below n.
-__device__ __forceinline__ void fetch8(Stage8 &to, int lane, const float *p, int k, int n, bool vec)
+// Tokens base .. base + 255, those in [0, n).  whole: all of them, at an address that moves eight at a time.
+__device__ __forceinline__ void fetch_block(Stage &to, int lane, const float *p, int base, int n, bool whole)
 {
-    if (vec && k + 8 <= n) {
-        copy_async(to.x[0][lane], p + k, 16);
-        copy_async(to.x[1][lane], p + k + 4, 16);
+    if (whole) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) copy_async(&to.x[swapped(32 * j + lane)], p + base + 128 * j + 4 * lane, 16);
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (k + e < n) copy_async(&to.x[e >> 2][lane][e & 3], p + k + e, 4);
+        for (int j = 0; j < 8; ++j) {
+            const int t = 32 * j + lane;
+            if (base + t < n) copy_async(reinterpret_cast<float *>(&to.x[swapped(t >> 2)]) + (t & 3), p + base + t, 4);
+        }
     }
 }
-__device__ __forceinline__ void fetch8(Stage8 &to, int lane, const uint16_t *p, int k, int n, bool vec) // bf16
+__device__ __forceinline__ void fetch_block(Stage &to, int lane, const uint16_t *p, int base, int n, bool whole) // bf16
 {
-    if (vec && k + 8 <= n) {
-        copy_async(to.x[0][lane], p + k, 16);
+    if (whole) {
+        copy_async(&to.x[lane], p + base + 8 * lane, 16);
     } else {
-        uint16_t *h = reinterpret_cast<uint16_t *>(to.x[0][lane]);
+        uint16_t *h = reinterpret_cast<uint16_t *>(to.x);
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (k + e < n) h[e] = p[k + e];
+        for (int j = 0; j < 8; ++j) {
+            const int t = 32 * j + lane;
+            if (base + t < n) h[t] = p[base + t];
+        }
     }
 }
-__device__ __forceinline__ void read8(const Stage8 &from, int lane, float (&x)[8])
+__device__ __forceinline__ float &stage_at(Stage &s, int t) { return reinterpret_cast<float *>(&s.x[swapped(t >> 2)])[t & 3]; }
+// Tokens 8 at .. 8 at + 7 of the block.
+__device__ __forceinline__ void read8(const Stage &from, int at, float (&x)[8])
 {
-    const float4 a = *reinterpret_cast<const float4 *>(from.x[0][lane]), b = *reinterpret_cast<const float4 *>(from.x[1][lane]);
+    const float4 a = from.x[swapped(2 * at)], b = from.x[swapped(2 * at + 1)];
     x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
 }
-__device__ __forceinline__ void read8_bf16(const Stage8 &from, int lane, float (&x)[8])
+__device__ __forceinline__ void read8_bf16(const Stage &from, int at, float (&x)[8])
 {
-    const uint4 w = *reinterpret_cast<const uint4 *>(from.x[0][lane]);
-    const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+    const float4 w = from.x[at];
+    const uint32_t v[4] = {__float_as_uint(w.x), __float_as_uint(w.y), __float_as_uint(w.z), __float_as_uint(w.w)};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         x[2 * e] = bf16_lo(v[e]);
@@ -232,11 +249,20 @@ __device__ __forceinline__ void read8_bf16(const Stage8 &from, int lane, float (
     }
 }
 
-// The eight mask bytes from token k on, those at or behind n as zeros; and a bit for each that is not zero.
-__device__ __forceinline__ uint2 mask_bytes(const uint8_t *p, int k, int n, bool vec)
+// bf16 to fp32 in place, by the whole warp.
+__device__ __forceinline__ void widen(Stage &s, int lane)
 {
-    if (p == nullptr) return make_uint2(0x01010101u, 0x01010101u);
-    if (vec && k + 8 <= n) return ld_global_64_stream(p + k);
+    float x[8];
+    read8_bf16(s, lane, x);
+    __syncwarp();
+    s.x[swapped(2 * lane)] = make_float4(x[0], x[1], x[2], x[3]);
+    s.x[swapped(2 * lane + 1)] = make_float4(x[4], x[5], x[6], x[7]);
+    __syncwarp();
+}
+
+// The eight mask bytes from token k on, those at or behind n as zeros; and a bit for each that is not zero.
+__device__ __forceinline__ uint2 mask_bytes(const uint8_t *p, int k, int n)
+{
     uint32_t w[2] = {0, 0};
 #pragma unroll
     for (int e = 0; e < 8; ++e)
