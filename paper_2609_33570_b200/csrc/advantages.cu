@@ -402,8 +402,8 @@ template <bool TRACE, bool MOMENTS, bool MAPS> __global__ void __launch_bounds__
                         if (TRACE) read8(x[kTensors - 1], 31 - lane, c);
                         feed.release(slot, fetch);
                         if (!TRACE && __all_sync(kAll, valid == 0xFFu)) { // every lane's P is weight^8
-                            const double first = a.gamma * (double)v[0], from = __shfl_up_sync(kAll, first, 1);
-                            double q = lane == 0 ? st.q : from, B = 0.0;
+                            const float from = __shfl_up_sync(kAll, v[0], 1);
+                            double q = lane == 0 ? st.q : a.gamma * (double)from, B = 0.0;
 #pragma unroll
                             for (int e = 7; e >= 0; --e) {
                                 const double V = (double)v[e];
@@ -419,16 +419,30 @@ template <bool TRACE, bool MOMENTS, bool MAPS> __global__ void __launch_bounds__
                                 ret[e] = (float)(z + (double)v[e]);
                             }
                             st.x = __shfl_sync(kAll, z, 31);
-                            st.q = __shfl_sync(kAll, first, 31);
+                            st.q = a.gamma * (double)__shfl_sync(kAll, v[0], 31);
                             if (MAPS) count += kBlock;
+                            if (MOMENTS) {
+                                if (!known) shift = __shfl_sync(kAll, z, 0), known = true;
+                                double s1[2] = {0.0, 0.0}, s2[2] = {0.0, 0.0};
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) {
+                                    const double d = D[e] - shift;
+                                    s1[e & 1] += d;
+                                    s2[e & 1] = fma(d, d, s2[e & 1]);
+                                }
+                                sum += s1[0] + s1[1];
+                                squares += s2[0] + s2[1];
+                                n += 8.0;
+                            }
                         } else {
                             // masked tokens hold the value that follows them, and leave B and z as they are
                             float leftmost = v[0];
 #pragma unroll
-                            for (int e = 7; e >= 0; --e) leftmost = valid >> e & 1 ? v[e] : leftmost;
+                            for (int e = 7; e >= 0; --e)
+                                if (valid >> e & 1) leftmost = v[e];
                             const uint32_t right = some & ((1u << lane) - 1);
-                            const double first = a.gamma * (double)leftmost, from = __shfl_sync(kAll, first, right ? 31 - __clz(right) : 0);
-                            double q = right ? from : st.q;
+                            const float from = __shfl_sync(kAll, leftmost, right ? 31 - __clz(right) : 0);
+                            double q = right ? a.gamma * (double)from : st.q;
                             Line m{1.0, 0.0};
                             bool apart = MAPS && TRACE && count == 0 && right == 0; // this lane's first weight may be the piece's rightmost
 #pragma unroll
@@ -436,12 +450,10 @@ template <bool TRACE, bool MOMENTS, bool MAPS> __global__ void __launch_bounds__
                                 const bool in = valid >> e & 1;
                                 const double V = (double)v[e], w = TRACE ? a.weight * (double)c[e] : a.weight;
                                 D[e] = ((double)r[e] - V) + q;
-                                const double B = fma(w, m.B, D[e]), qv = a.gamma * V;
-                                m.B = in ? B : m.B;
-                                q = in ? qv : q;
+                                if (in) m.B = fma(w, m.B, D[e]);
+                                if (in) q = a.gamma * V;
                                 if (TRACE) {
-                                    const double P = w * m.P;
-                                    m.P = in && !apart ? P : m.P;
+                                    if (in && !apart) m.P *= w;
                                     if (MAPS && in && apart) w_right = w, apart = false;
                                 }
                             }
@@ -451,35 +463,27 @@ template <bool TRACE, bool MOMENTS, bool MAPS> __global__ void __launch_bounds__
                             double z = fma(before.P, st.x, before.B);
 #pragma unroll
                             for (int e = 7; e >= 0; --e) {
-                                const bool in = valid >> e & 1;
-                                D[e] = fma(TRACE ? a.weight * (double)c[e] : a.weight, z, D[e]);
-                                z = in ? D[e] : z;
-                                adv[e] = in ? (float)D[e] : 0.0f;
-                                ret[e] = in ? (float)(D[e] + (double)v[e]) : 0.0f;
+                                adv[e] = ret[e] = 0.0f;
+                                if (valid >> e & 1) z = fma(TRACE ? a.weight * (double)c[e] : a.weight, z, D[e]);
+                                D[e] = z;
+                                if (valid >> e & 1) adv[e] = (float)z;
+                                if (valid >> e & 1) ret[e] = (float)(z + (double)v[e]);
                             }
                             if (MAPS && TRACE) P_all *= __shfl_sync(kAll, m.P, 31);
                             st.x = __shfl_sync(kAll, z, 31);
-                            st.q = __shfl_sync(kAll, first, 31 - __clz(some));
+                            st.q = a.gamma * (double)__shfl_sync(kAll, leftmost, 31 - __clz(some));
                             if (MAPS) count += TRACE ? 1 : (int)__reduce_add_sync(kAll, (unsigned)__popc(valid));
-                        }
-                        if (MOMENTS) {
-                            if (!known) { // an advantage of the warp's first block: one of the lane with the first bit
-                                double one = D[0];
+                            if (MOMENTS) {
+                                // an advantage of the warp's first block: where the lane with the first bit ended
+                                if (!known) shift = __shfl_sync(kAll, z, __ffs(some) - 1), known = true;
 #pragma unroll
-                                for (int e = 1; e < 8; ++e) one = valid >> e & 1 ? D[e] : one;
-                                shift = __shfl_sync(kAll, one, __ffs(some) - 1);
-                                known = true;
+                                for (int e = 0; e < 8; ++e) {
+                                    const double d = D[e] - shift;
+                                    if (valid >> e & 1) sum += d;
+                                    if (valid >> e & 1) squares = fma(d, d, squares);
+                                }
+                                n += (double)__popc(valid);
                             }
-                            double s1[2] = {0.0, 0.0}, s2[2] = {0.0, 0.0};
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) {
-                                const double d = valid >> e & 1 ? D[e] - shift : 0.0;
-                                s1[e & 1] += d;
-                                s2[e & 1] = fma(d, d, s2[e & 1]);
-                            }
-                            sum += s1[0] + s1[1];
-                            squares += s2[0] + s2[1];
-                            n += (double)__popc(valid);
                         }
                     }
                     if (!MAPS) {
@@ -898,12 +902,12 @@ static bool all_vectors(const AdvantageArgs &a)
            aligned(a.values, a.values_bf16 ? 16 : 32);
 }
 
-// Chunks: 2048 tokens a warp where that still gives every SM a full set of warps, down to one block of 256 tokens.
+// Chunks: 4096 tokens a warp where that still gives every SM a full set of warps, down to one block of 256 tokens.
 constexpr int64_t kChunks = 148 * 24;
 static void deal(AdvantageArgs &a)
 {
     a.chunk = 8;
-    while (a.chunk < 11 && (kChunks << a.chunk) < a.q.n_tok) ++a.chunk;
+    while (a.chunk < 12 && (kChunks << a.chunk) < a.q.n_tok) ++a.chunk;
     a.piece = a.chunk + 2;
     a.chunks = (int)((a.q.n_tok + (1 << a.chunk) - 1) >> a.chunk);
     for (int i = 0; i < 9; ++i) a.small[i] = std::pow(a.weight, i);
@@ -921,7 +925,7 @@ using namespace hilore;
 
 extern "C" size_t hilore_advantages_workspace_bytes(int64_t n_tok)
 {
-    const int64_t n = n_tok > 0 ? n_tok : 0, small = (n + 255) / 256, large = (n + 2047) / 2048; // chunks, whatever their size, of n tokens or fewer
+    const int64_t n = n_tok > 0 ? n_tok : 0, small = (n + 255) / 256, large = (n + 4095) / 4096; // chunks, whatever their size, of n tokens or fewer
     const size_t chunks = (size_t)std::max(std::min(small, kChunks), large);
     return (chunks + 1) * sizeof(AdvantageOp::Map) + (chunks / kAdvWarps + 1) * 3 * sizeof(double);
 }

@@ -135,6 +135,14 @@ __device__ __forceinline__ void load8(const uint16_t *p, int k, int hi, bool vec
     }
 }
 
+// A bit for each of eight bytes that is not zero.
+__device__ __forceinline__ uint32_t mask_bits(uint2 w)
+{
+    // the top bit of every byte that is not zero; these, 8 apart, gathered in four neighbouring bits
+    const uint32_t a = (((w.x & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) | w.x) & 0x80808080u, b = (((w.y & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) | w.y) & 0x80808080u;
+    return (a * 0x00204081u) >> 28 | ((b * 0x00204081u) >> 28) << 4;
+}
+
 __device__ __forceinline__ uint32_t load_mask8(const uint8_t *p, int k, int hi, bool vec)
 {
     const int n = hi - k;
@@ -144,10 +152,7 @@ __device__ __forceinline__ uint32_t load_mask8(const uint8_t *p, int k, int hi, 
         return n >= 8 ? 0xFFu : (1u << n) - 1;
     uint32_t m = 0;
     if (vec && n >= 8) {
-        const uint2 w = ld_global_64_stream(p + k);
-        // every byte that is not zero to 0xFF, then the top bits gathered
-        const uint32_t a = __vcmpne4(w.x, 0u) & 0x08040201u, b = __vcmpne4(w.y, 0u) & 0x80402010u;
-        m = ((a | b) * 0x01010101u) >> 24;
+        m = mask_bits(ld_global_64_stream(p + k));
     } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
@@ -260,7 +265,7 @@ __device__ __forceinline__ void widen(Stage &s, int lane)
     __syncwarp();
 }
 
-// The eight mask bytes from token k on, those at or behind n as zeros; and a bit for each that is not zero.
+// The eight mask bytes from token k on, those at or behind n as zeros.
 __device__ __forceinline__ uint2 mask_bytes(const uint8_t *p, int k, int n)
 {
     uint32_t w[2] = {0, 0};
@@ -268,12 +273,6 @@ __device__ __forceinline__ uint2 mask_bytes(const uint8_t *p, int k, int n)
     for (int e = 0; e < 8; ++e)
         if (k + e < n) w[e >> 2] |= (uint32_t)p[k + e] << (8 * (e & 3));
     return make_uint2(w[0], w[1]);
-}
-__device__ __forceinline__ uint32_t mask_bits(uint2 w)
-{
-    // every byte that is not zero to 0xFF, one bit of each kept, and these gathered in the top byte
-    const uint32_t a = __vcmpne4(w.x, 0u) & 0x08040201u, b = __vcmpne4(w.y, 0u) & 0x80402010u;
-    return ((a | b) * 0x01010101u) >> 24;
 }
 // Bits of the tokens k .. k + 7 that lie in [lo, hi).
 __device__ __forceinline__ uint32_t range_bits(int k, int lo, int hi)
