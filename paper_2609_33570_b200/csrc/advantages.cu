@@ -73,10 +73,13 @@ constexpr int kStages = 3;       // blocks of 256 tokens whose tensors a warp ha
 constexpr int kMaskStages = 8;   // and their masks, which say what to read of the tensors: more than 2 kStages, a power of two
 constexpr uint32_t kAll = 0xFFFFFFFFu;
 
-// How the work is dealt out.  A warp owns the pieces that begin in its chunk of tokens.  A piece is a whole sequence, or 2^piece
-// tokens (the last one fewer) of a longer one, so nothing but long sequences needs more than one pass: their pieces' maps are
-// made first, by a launch that has nothing to read where no sequence is long.  piece >= chunk, so no chunk holds the beginnings
-// of two pieces that are not the first of their sequence (or not the last), and a map's place is its chunk.
+// How the work is dealt out.  A warp has one chunk of `chunk` tokens.  A sequence that goes on in the next chunk needs what comes out of
+// that, or goes into it: maps of parts of chunks, made by a launch of their own before.  Two ways:
+//   Even: a warp owns the tokens of its chunk.  A chunk's map covers its first sequence (backward pass: its last one) where that one
+//   goes on in the chunk before (behind).  Every warp has as much to do as the others.
+//   By pieces: a warp owns the pieces that begin in its chunk.  A piece is a whole sequence, or 2^piece tokens (the last one fewer) of
+//   a longer one, so that nothing but long sequences needs more than one pass.  piece >= chunk, so no chunk holds the beginnings of
+//   two pieces that are not the first of their sequence (or not the last), and a map's place is its chunk.
 struct AdvantageArgs {
     Sequences q;
     const float *rewards, *outcome, *bootstrap, *trace;
@@ -91,32 +94,16 @@ struct AdvantageArgs {
     float *grad_rewards, *grad_outcome, *grad_values, *grad_bootstrap, *grad_trace;
     void *maps;       // [chunks]
     double *partials; // [CTAs][3] count, mean, sum of squared deviations
-    int chunks, chunk, piece, vec, moments; // chunk, piece: logarithms
-    int warm, second; // second: a launch of this call came first, and what it did not write is there without waiting for it
+    int chunks, chunk, piece, vec, moments;
+    int even;
+    int second; // second: a launch of this call came first, and what it did not write is there without waiting for it
 };
 
-// In a call whose warps all run at once there is nothing but latency: its first launch asks for the chunks' tokens to be brought into
-// L2 before it is known which of them will be read.
-template <bool MAPS>
-__device__ __forceinline__ void warm(const AdvantageArgs &a, int chunk, int lane, const float *x0, const float *x1, const float *x2, const float *x3)
-{
-    if (!a.warm || chunk >= a.chunks || (!MAPS && a.second)) return;
-    const int t0 = chunk << a.chunk, t1 = (int)min(a.q.n_tok, (int64_t)t0 + (1 << a.chunk));
-#pragma unroll 1
-    for (int t = t0 + lane * 32; t < t1; t += 32 * 32) { // 128 bytes of fp32
-        if (x0) prefetch_l2(x0 + t);
-        if (x1) prefetch_l2(x1 + t);
-        if (x2) prefetch_l2(x2 + t);
-        if (x3) prefetch_l2(x3 + t);
-        if (a.values && a.values_bf16 && (lane & 1) == 0) prefetch_l2(static_cast<const uint16_t *>(a.values) + t);
-        if (a.mask && (lane & 3) == 0) prefetch_l2(a.mask + t);
-    }
-}
-
-// The first beginning of a piece at or behind token t of sequence s, or the end of the last sequence.
-__device__ __forceinline__ int piece_from(const AdvantageArgs &a, int t, int s, int live)
+// Where a chunk's part begins that would begin at token t of sequence s; the end of the last sequence if there is none.
+__device__ __forceinline__ int part_from(const AdvantageArgs &a, int t, int s, int live)
 {
     if (t >= live) return live;
+    if (a.even) return t;
     const int b = a.q.bound(s), e = a.q.bound(s + 1);
     const uint32_t off = t > b ? (uint32_t)(t - b) : 0u, up = ((off + (1u << a.piece) - 1) >> a.piece) << a.piece;
     const int64_t p = (int64_t)b + up, at = p < e ? p : e;
@@ -317,35 +304,40 @@ template <bool TRACE, bool MOMENTS, bool MAPS> __global__ void __launch_bounds__
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, chunk = blockIdx.x * kAdvWarps + warp;
     if (MAPS || !a.second) grid_dependency_wait();
     grid_dependency_release();
-    warm<MAPS>(a, chunk, lane, a.rewards, static_cast<const float *>(a.values_bf16 ? nullptr : a.values), a.trace, nullptr);
     const int live = a.q.live();
     double n = 0.0, shift = 0.0, sum = 0.0, squares = 0.0; // moments about a value of the warp's own,
     bool known = false;                                    // once there is one
-    if (chunk < a.chunks && (chunk << a.chunk) < live) {
-        const int t0 = chunk << a.chunk, t1 = min(live - t0, 1 << a.chunk) + t0;
-        int s, s1, begin, end, cur = 0; // cur: where the current sequence begins
-        a.q.owner_warp2(t0, t1 < live ? t1 : t1 - 1, lane, s, s1);
+    if (chunk < a.chunks && (int64_t)chunk * a.chunk < live) {
+        const int t0 = chunk * a.chunk, t1 = min(live - t0, a.chunk) + t0;
+        int s, s1, begin = 0, end = 0, cur = 0; // cur: where the current sequence begins
+        a.q.owner_warp2(t0, !a.even && t1 < live ? t1 : t1 - 1, lane, s, s1);
         Op::State st = Op::start();
-        int behind = 0; // pieces of the last sequence behind this chunk's
+        bool closed = false; // MAPS: the part holds its sequence's end
+        int behind = 0;      // maps of the last sequence behind this chunk's part
         auto terminal = [&](int o) -> double {
             return (a.outcome ? (double)__ldg(a.outcome + o) : 0.0) + a.gamma * (a.bootstrap ? (double)__ldg(a.bootstrap + o) : 0.0);
         };
         if (MAPS) {
             const int b = a.q.bound(s), e = a.q.bound(s + 1);
-            const uint32_t off = t0 > b ? (uint32_t)(t0 - b) : 0u, up = (off + (1u << a.piece) - 1) >> a.piece;
-            const int64_t p = b + ((int64_t)max(up, 1u) << a.piece);
-            begin = end = 0;
-            if (p >= t0 && p < t1 && p < e) begin = (int)p, end = e - begin < (1 << a.piece) ? e : begin + (1 << a.piece);
+            if (a.even) {
+                if (b < t0) begin = t0, end = min(e, t1);
+            } else {
+                const uint32_t off = t0 > b ? (uint32_t)(t0 - b) : 0u, up = (off + (1u << a.piece) - 1) >> a.piece;
+                const int64_t p = b + ((int64_t)max(up, 1u) << a.piece);
+                if (p >= t0 && p < t1 && p < e) begin = (int)p, end = e - begin < (1 << a.piece) ? e : begin + (1 << a.piece);
+            }
+            closed = end == e;
+            if (end > begin && closed) st.q = terminal(s);
         } else {
-            begin = piece_from(a, t0, s, live);
-            end = piece_from(a, t1, s1, live);
+            begin = part_from(a, t0, s, live);
+            end = part_from(a, t1, s1, live);
             if (end > begin) {
                 s = s1;
                 cur = a.q.bound(s);
                 if (cur >= end) s = a.q.owner_warp(end - 1, lane), cur = a.q.bound(s);
                 st.q = terminal(s);
                 const int e = a.q.bound(s + 1);
-                behind = e > end ? (int)(((uint32_t)(e - end) + (1u << a.piece) - 1) >> a.piece) : 0;
+                if (e > end) behind = a.even ? (int)((uint32_t)(e - 1) / (uint32_t)a.chunk) - chunk : (int)(((uint32_t)(e - end) + (1u << a.piece) - 1) >> a.piece);
             }
         }
         if (end > begin) {
@@ -366,7 +358,8 @@ template <bool TRACE, bool MOMENTS, bool MAPS> __global__ void __launch_bounds__
                 grid_dependency_wait();
                 double none = 0.0;
                 st = behind_pieces<Op>(st, behind, lane, [&](int i) {
-                    return static_cast<const Op::Map *>(a.maps)[(end + ((int64_t)(behind - 1 - i) << a.piece)) >> a.chunk]; }, none);
+                    const int far = behind - 1 - i;
+                    return static_cast<const Op::Map *>(a.maps)[a.even ? chunk + 1 + far : (end + ((int64_t)far << a.piece)) / a.chunk]; }, none);
             }
             double P_all = 1.0, w_right = a.weight, ahead = 1.0; // MAPS: product of the weights but the rightmost one's, and that; weight^(8 lane)
             int count = 0;
@@ -563,7 +556,7 @@ template <bool TRACE, bool MOMENTS, bool MAPS> __global__ void __launch_bounds__
             if (MAPS && lane == 0) {
                 // x' = Q (w x + q) + B,  q' = c
                 const double Q = TRACE ? P_all : (count > 0 ? pow(a.weight, (double)(count - 1)) : 1.0);
-                static_cast<Op::Map *>(a.maps)[chunk] = Op::Map{Q * w_right, Q, st.x, st.q, count > 0 ? 1u : 0u, 0u};
+                static_cast<Op::Map *>(a.maps)[chunk] = Op::Map{Q * w_right, Q, st.x, st.q, closed ? 2u : (count > 0 ? 1u : 0u), 0u};
             }
         }
     }
@@ -623,7 +616,6 @@ __global__ void __launch_bounds__(kGradThreads, TRACE || BY_TRACE ? 5 : 8) advan
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, chunk = blockIdx.x * kGradWarps + warp;
     if (MAPS || !a.second) grid_dependency_wait();
     grid_dependency_release();
-    warm<MAPS>(a, chunk, lane, a.grad_adv, a.grad_returns, a.trace, a.adv_in);
     const int live = a.q.live();
     const bool per_sequence = a.grad_outcome || a.grad_bootstrap;
     auto put = [&](int o, double G) {
@@ -637,20 +629,25 @@ __global__ void __launch_bounds__(kGradThreads, TRACE || BY_TRACE ? 5 : 8) advan
         return;
     }
     int s = 0, s1, b = 0, begin = 0, end = 0, e_cur = live; // e_cur: where the current sequence ends
-    if (chunk < a.chunks && (chunk << a.chunk) < live) {
-        const int t0 = chunk << a.chunk, t1 = min(live - t0, 1 << a.chunk) + t0;
-        a.q.owner_warp2(t0, MAPS || t1 >= live ? t1 - 1 : t1, lane, s, s1);
-        if (MAPS) {
+    bool opened = false; // MAPS: the part holds its sequence's beginning
+    if (chunk < a.chunks && (int64_t)chunk * a.chunk < live) {
+        const int t0 = chunk * a.chunk, t1 = min(live - t0, a.chunk) + t0;
+        a.q.owner_warp2(t0, MAPS || a.even || t1 >= live ? t1 - 1 : t1, lane, s, s1);
+        if (MAPS && a.even) {
+            const int from = a.q.bound(s1);
+            if (a.q.bound(s1 + 1) > t1) begin = max(t0, from), end = t1;
+            opened = from >= t0;
+        } else if (MAPS) {
 #pragma unroll 1
             for (int which = 0; which < 2; ++which) { // of the chunk's first sequence, or of its last
                 const int o = which == 0 ? s : s1, from = a.q.bound(o), e = a.q.bound(o + 1);
                 const uint32_t off = t0 > from ? (uint32_t)(t0 - from) : 0u, up = ((off + (1u << a.piece) - 1) >> a.piece) << a.piece;
                 const int64_t p = (int64_t)from + up;
-                if (p >= t0 && p < t1 && p + (1 << a.piece) < e) begin = (int)p, end = begin + (1 << a.piece);
+                if (p >= t0 && p < t1 && p + (1 << a.piece) < e) begin = (int)p, end = begin + (1 << a.piece), opened = p == from;
             }
         } else {
-            begin = piece_from(a, t0, s, live);
-            end = piece_from(a, t1, s1, live);
+            begin = part_from(a, t0, s, live);
+            end = part_from(a, t1, s1, live);
         }
     }
     const int s_first = s;
@@ -678,8 +675,8 @@ __global__ void __launch_bounds__(kGradThreads, TRACE || BY_TRACE ? 5 : 8) advan
     Op::State st = Op::start();
     double w_before = 0.0; // TRACE: weight of the valid token before
     if (!MAPS && a.second)
-        st = behind_pieces<Op>(st, begin > b ? (begin - b) >> a.piece : 0, lane,
-                               [&](int i) { return static_cast<const Op::Map *>(a.maps)[(b + ((int64_t)i << a.piece)) >> a.chunk]; }, w_before);
+        st = behind_pieces<Op>(st, begin <= b ? 0 : (a.even ? chunk - b / a.chunk : (begin - b) >> a.piece), lane,
+                               [&](int i) { return static_cast<const Op::Map *>(a.maps)[a.even ? b / a.chunk + i : (b + ((int64_t)i << a.piece)) / a.chunk]; }, w_before);
     // The current sequence's last gradient, then on to the one that holds token `to`; those between without a token get zeros.
     auto next_sequence = [&](int to) {
         if (lane == 0) {
@@ -890,7 +887,7 @@ __global__ void __launch_bounds__(kGradThreads, TRACE || BY_TRACE ? 5 : 8) advan
     if (MAPS) {
         const double P = TRACE ? P_all : (count > 0 ? pow(a.weight, (double)(count - 1)) : 1.0);
         if (lane == 0)
-            static_cast<Op::Map *>(a.maps)[chunk] = Op::Map{P, st.G, TRACE ? w_before : a.weight, st.pos, count > 0 ? 1u : 0u};
+            static_cast<Op::Map *>(a.maps)[chunk] = Op::Map{P, st.G, TRACE ? w_before : a.weight, st.pos, opened ? 2u : (count > 0 ? 1u : 0u)};
     } else if (e_cur <= end) {
         next_sequence(end);
     }
@@ -902,22 +899,25 @@ static bool all_vectors(const AdvantageArgs &a)
            aligned(a.values, a.values_bf16 ? 16 : 32);
 }
 
-// Chunks: 4096 tokens a warp where that still gives every SM a full set of warps, down to one block of 256 tokens.
-constexpr int64_t kChunks = 148 * 24;
+constexpr int64_t kChunks = 148 * 24; // warps that run at once
 static void deal(AdvantageArgs &a)
 {
-    a.chunk = 8;
-    while (a.chunk < 12 && (kChunks << a.chunk) < a.q.n_tok) ++a.chunk;
-    a.piece = a.chunk + 2;
-    a.chunks = (int)((a.q.n_tok + (1 << a.chunk) - 1) >> a.chunk);
+    const int64_t share = (a.q.n_tok + kChunks - 1) / kChunks, blocks = (share + kBlock - 1) / kBlock;
+    a.even = blocks <= 8;
+    a.chunk = kBlock * (int)(blocks < 1 ? 1 : (blocks > 8 ? 16 : blocks));
+    a.piece = 13;
+    a.chunks = (int)((a.q.n_tok + a.chunk - 1) / a.chunk);
     for (int i = 0; i < 9; ++i) a.small[i] = std::pow(a.weight, i);
-    a.warm = a.chunks <= kChunks;
     a.powers[0] = a.small[8];
     for (int i = 1; i < 5; ++i) a.powers[i] = a.powers[i - 1] * a.powers[i - 1];
 }
 
-// Whether a sequence can be longer than a piece, as far as the host knows.
-static bool long_sequences(const AdvantageArgs &a) { return (a.q.cu ? a.q.n_tok : a.q.T) > (int64_t)1 << a.piece; }
+// Whether there can be maps to make, as far as the host knows.
+static bool long_sequences(const AdvantageArgs &a)
+{
+    if (a.even) return a.chunks > 1;
+    return (a.q.cu ? a.q.n_tok : a.q.T) > (int64_t)1 << a.piece;
+}
 
 } // namespace hilore
 
