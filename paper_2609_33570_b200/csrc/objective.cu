@@ -5,41 +5,36 @@
 
 namespace hilore {
 
-constexpr int kStats = 5;          // sums that a CTA hands to the final kernel
-constexpr int kObjectiveGrid = 2048; // most CTAs that do so
+constexpr int kThreads = 256;
+constexpr int kWarps = kThreads / 32;
+constexpr int kPerSm = 2;            // CTAs of the policy kernels on an SM,
+constexpr int kSumsPerSm = 4;        // and of the sums'
+constexpr int kStats = 5;            // sums that a CTA hands on
+constexpr int kMostCtas = 1024;      // that do so
+constexpr uint32_t kAll = 0xFFFFFFFFu;
 
-// Sums over the valid tokens of a sequence or of the part of it that lies in one tile.
+// Every warp has a share of neighbouring blocks of 256 tokens, eight to a lane; all of them run at once.
+struct Share {
+    int blocks, per_warp; // blocks of the call, of a warp
+};
+
+// Sums over the valid tokens of a sequence or of the part of it that lies in one share.
 struct Piece {
     double a, b, n;
 };
 
-// Tokens of a tile add to the sequence that they are in; a sequence's end starts anew.
-struct SumOp {
-    struct Map {
-        double a, b;
-        int32_t n;
-        uint32_t flag; // 1: holds a sequence's end, the sums are those behind it
-    };
-    typedef Map State;
-    static __device__ __forceinline__ Map identity() { return Map{0.0, 0.0, 0, 0u}; }
-    static __device__ __forceinline__ Map then(const Map &x, const Map &y)
-    {
-        if (y.flag) return y;
-        return Map{x.a + y.a, x.b + y.b, x.n + y.n, x.flag};
-    }
-    static __device__ __forceinline__ State apply(const Map &m, const State &s) { return then(s, m); }
-};
-
-// Where the sums of a call's sequences lie: of a sequence inside one tile in whole[s]; of one that goes over tiles t .. u in
+// Where the sums of a call's sequences lie: of a sequence inside one share in whole[s]; of one that goes over shares t .. u in
 // tail[t], head[t + 1] .. head[u].
 struct Pieces {
     Piece *head, *tail, *whole;
+    int share; // tokens
 
+    // By one thread.
     __device__ __forceinline__ Piece total(const Sequences &q, int s) const
     {
         const int lo = q.bound(s), hi = q.bound(s + 1);
         if (hi <= lo) return Piece{0.0, 0.0, 0.0};
-        const int t = lo / kSegTile, u = (hi - 1) / kSegTile;
+        const int t = lo / share, u = (hi - 1) / share;
         if (t == u) return whole[s];
         Piece p = tail[t];
         for (int i = t + 1; i <= u; ++i) {
@@ -49,89 +44,123 @@ struct Pieces {
         }
         return p;
     }
+    // By a warp; every lane returns it.
+    __device__ __forceinline__ Piece total_warp(const Sequences &q, int s, int lane) const
+    {
+        const int lo = q.bound(s), hi = q.bound(s + 1);
+        if (hi <= lo) return Piece{0.0, 0.0, 0.0};
+        const int t = lo / share, u = (hi - 1) / share;
+        if (t == u) return whole[s];
+        Piece p{0.0, 0.0, 0.0};
+        for (int i = t + lane; i <= u; i += 32) {
+            const Piece x = i == t ? tail[i] : head[i];
+            p.a += x.a;
+            p.b += x.b;
+            p.n += x.n;
+        }
+        return Piece{warp_sum(p.a), warp_sum(p.b), warp_sum(p.n)};
+    }
+};
+
+// A warp's way through the sequences of its tokens: the current one, which holds the first token not yet passed, and its end.
+struct Cursor {
+    int s, end;
+    __device__ __forceinline__ void at(const Sequences &q, int token, int lane)
+    {
+        s = q.owner_warp(token, lane);
+        end = q.bound(s + 1);
+    }
+    // On to the sequence of `token`, which is not in this one but behind it.
+    __device__ __forceinline__ void on(const Sequences &q, int token, int lane)
+    {
+        const int64_t o = (int64_t)s + 1 + lane;
+        const int e = o < q.n_seq ? q.bound((int)o + 1) : 0x7FFFFFFF;
+        const uint32_t hit = __ballot_sync(kAll, e > token);
+        if (hit == 0) {
+            at(q, token, lane);
+        } else {
+            const int j = __ffs(hit) - 1;
+            s = (int)(s + 1 + j < q.n_seq ? s + 1 + j : q.n_seq - 1);
+            end = __shfl_sync(kAll, e, j);
+        }
+        if (end <= token) end = 0x7FFFFFFF; // boundaries out of order
+    }
 };
 
 struct SumArgs {
     Sequences q;
+    Share w;
     const uint8_t *mask;
     const float *x, *minus; // a: sum of x - minus (or of x)
-    const float *y, *less;  // b: sum of y - less (or of y)
+    const float *y, *less;  // b: sum of y - less (or of y); y may be x
     Pieces out;
     int vec;
 };
 
-// Sums of every sequence over its valid tokens, one tile per CTA.
-__global__ void __launch_bounds__(kSegThreads) sequence_sums_kernel(const __grid_constant__ SumArgs a)
+// Sums of every sequence over its valid tokens.  X: whether there is a first sum, Y: 0 none, 1 of y - less, 2 of x.  A lane adds its tokens
+// of the current sequence; at the sequence's end, or the share's, the warp adds the lanes up.
+template <bool X, int Y> __global__ void __launch_bounds__(kThreads, kSumsPerSm) sequence_sums_kernel(const __grid_constant__ SumArgs a)
 {
-    using Op = SumOp;
-    __shared__ TileShared sh;
-    __shared__ Op::Map totals[kSegWarps];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, tile = blockIdx.x;
+    const int lane = threadIdx.x & 31, share = blockIdx.x * kWarps + (threadIdx.x >> 5);
     grid_dependency_wait();
     grid_dependency_release();
-    const int lo = tile * kSegTile, live = a.q.live(), hi = live - lo < kSegTile ? live : lo + kSegTile;
-    if (hi <= lo)
+    const int live = a.q.live(), tokens = a.w.per_warp * kBlock;
+    if ((int64_t)share * tokens >= live)
         return;
-    const int k = lo + tid * kSegEach;
-    float x[8], m[8], y[8], l[8];
-    const uint32_t valid = load_mask8(a.mask, k, hi, a.vec);
-    if (a.x) load8(a.x, k, hi, a.vec, x);
-    if (a.minus) load8(a.minus, k, hi, a.vec, m);
-    if (a.y && a.y != a.x) load8(a.y, k, hi, a.vec, y);
-    if (a.less) load8(a.less, k, hi, a.vec, l);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        if (!a.x) x[e] = 0.0f;
-        if (!a.minus) m[e] = 0.0f;
-        if (!a.y) y[e] = 0.0f;
-        else if (a.y == a.x) y[e] = x[e];
-        if (!a.less) l[e] = 0.0f;
-    }
-    tile_sequences(a.q, lo, hi, sh);
-    const uint32_t ends = block_ends(sh, tid);
-    auto add = [&](Op::Map &s, int e) {
-        if (!(valid >> e & 1)) return;
-        s.a += (double)x[e] - (double)m[e];
-        s.b += (double)y[e] - (double)l[e];
-        s.n += 1;
+    const int begin = share * tokens, stop = min(live - begin, tokens) + begin;
+    Cursor c;
+    c.at(a.q, begin, lane);
+    Piece sum{0.0, 0.0, 0.0};
+    int n = 0;
+    auto finish = [&](bool ends) {
+        const Piece p{X ? warp_sum(sum.a) : 0.0, Y ? warp_sum(sum.b) : 0.0, (double)__reduce_add_sync(kAll, (unsigned)n)};
+        if (lane == 0) {
+            if (a.q.bound(c.s) < begin) a.out.head[share] = p;
+            else if (ends) a.out.whole[c.s] = p;
+            else a.out.tail[share] = p;
+        }
+        sum = Piece{0.0, 0.0, 0.0};
+        n = 0;
     };
-    Op::Map mine = Op::identity();
+#pragma unroll 1
+    for (int base = begin; base < stop; base += kBlock) {
+        const int k = base + lane * 8, hi = min(base + kBlock, stop);
+        const uint32_t valid = load_mask8(a.mask, k, hi, a.vec);
+        float x[8] = {}, m[8] = {}, y[8] = {}, l[8] = {};
+        if (valid) {
+            if (X) load8(a.x, k, hi, a.vec, x);
+            if (X && a.minus) load8(a.minus, k, hi, a.vec, m);
+            if (Y == 1) load8(a.y, k, hi, a.vec, y);
+            if (Y == 1 && a.less) load8(a.less, k, hi, a.vec, l);
+        }
+#pragma unroll 1
+        for (int lo = base;;) { // the block's part of each sequence
+            const uint32_t run = c.end >= hi && lo == base ? valid : valid & range_bits(k, lo, c.end);
+            if (__any_sync(kAll, run != 0)) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        add(mine, e);
-        if (ends >> e & 1) mine = Op::Map{0.0, 0.0, 0, 1u};
-    }
-    Op::Map all;
-    const Op::Map before = warp_scan<Op>(mine, lane, all);
-    if (lane == 31) totals[warp] = all;
-    __syncthreads();
-    Op::Map s = Op::identity();
-    for (int w = 0; w < warp; ++w) s = Op::apply(totals[w], s);
-    s = Op::apply(before, s);
-    if (ends != 0 || tid == kSegThreads - 1) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            add(s, e);
-            if (ends >> e & 1) {
-                const int o = a.q.owner(k + e, sh.s0, sh.s1);
-                const Piece p{s.a, s.b, (double)s.n};
-                if (a.q.bound(o) >= lo) a.out.whole[o] = p;
-                else a.out.head[tile] = p;
-                s = Op::identity();
+                for (int e = 0; e < 8; ++e) {
+                    const bool in = run >> e & 1;
+                    if (X) sum.a += pick(in, (double)x[e] - (double)m[e], 0.0);
+                    if (Y == 1) sum.b += pick(in, (double)y[e] - (double)l[e], 0.0);
+                    if (Y == 2) sum.b += pick(in, (double)x[e], 0.0);
+                }
+                n += __popc(run);
             }
-        }
-        if (tid == kSegThreads - 1 && hi == lo + kSegTile && !(ends >> 7 & 1)) { // goes on in the next tile
-            const Piece p{s.a, s.b, (double)s.n};
-            if (a.q.bound(sh.s1) >= lo) a.out.tail[tile] = p;
-            else a.out.head[tile] = p;
+            if (c.end > hi) break;
+            finish(true);
+            if (c.end >= stop) return; // the share ends with it
+            lo = c.end;
+            c.on(a.q, lo, lane);
+            if (lo >= hi) break;
         }
     }
+    finish(false);
 }
 
-// Sums of a CTA's five numbers into its slots, in a fixed order.
+// Sums of a CTA's numbers into its slots, in a fixed order.
 __device__ __forceinline__ void put_stats(const double (&v)[kStats], double *slots)
 {
-    __shared__ double sh[kStats][kSegWarps];
+    __shared__ double sh[kStats][kWarps];
 #pragma unroll
     for (int i = 0; i < kStats; ++i) {
         const double t = warp_sum(v[i]);
@@ -140,15 +169,16 @@ __device__ __forceinline__ void put_stats(const double (&v)[kStats], double *slo
     __syncthreads();
     if (threadIdx.x < kStats) {
         double t = 0.0;
-        for (int w = 0; w < kSegWarps; ++w) t += sh[threadIdx.x][w];
+        for (int w = 0; w < kWarps; ++w) t += sh[threadIdx.x][w];
         slots[threadIdx.x] = t;
     }
 }
 
-// The sum over the CTAs' slots, number `i` of it in every lane of warp i.
+// The sum over the CTAs' slots, number `i` of it in every lane.
 __device__ __forceinline__ double sum_slots(const double *partials, int ctas, int i)
 {
     double t = 0.0;
+#pragma unroll 4
     for (int c = threadIdx.x & 31; c < ctas; c += 32) t += partials[(size_t)c * kStats + i];
     return warp_sum(t);
 }
@@ -159,7 +189,6 @@ __device__ __forceinline__ double sum_slots(const double *partials, int ctas, in
 // first term left out at |e| <= 1 is 2 / 13! of the first.
 __device__ __forceinline__ float exp_minus_line(float e)
 {
-    if (fabsf(e) > 1.0f) return expf(e) - e - 1.0f;
     float s = 1.0f / 479001600.0f;
     s = fmaf(s, e, 1.0f / 39916800.0f);
     s = fmaf(s, e, 1.0f / 3628800.0f);
@@ -171,26 +200,22 @@ __device__ __forceinline__ float exp_minus_line(float e)
     s = fmaf(s, e, 1.0f / 24.0f);
     s = fmaf(s, e, 1.0f / 6.0f);
     s = fmaf(s, e, 0.5f);
-    return e * e * s;
+    s *= e * e;
+    if (fabsf(e) > 1.0f) s = expf(e) - e - 1.0f;
+    return s;
 }
-
-// What the token kernel needs of a sequence.
-struct SequenceCoef {
-    float weight; // w of its tokens
-    float slope;  // sequence ratios: the policy term's gradient of every token
-};
 
 struct PolicyArgs {
     Sequences q;
+    Share w;
     const float *logp, *old, *ref, *rollout, *adv, *moments, *grad_loss;
     const uint8_t *mask;
     const int64_t *N_dev;
     double N, clip_low, clip_high, log_low, log_high, log_dual, dual, cap, beta, adv_eps;
-    int per_token, sequence_ratio, sequence_mean, kl, vec, tiles;
+    float near; // distance of a logarithm of a ratio from its bounds within which it is compared in fp64
+    int sequence_mean, k2, vec;
     Pieces pieces;
-    SequenceCoef *coef;
     double *partials;
-    int slots_before; // CTAs of the sequence kernel, whose slots come first
     float *omega;
 };
 
@@ -200,117 +225,202 @@ __device__ __forceinline__ double inverse_norm(const PolicyArgs &a)
     return N > 0.0 ? 1.0 / N : 0.0;
 }
 
-__device__ __forceinline__ float whitened(const PolicyArgs &a, float A)
+enum { kNoKl = 0, kEasyKl = 1, kK3 = 2 }; // kEasyKl: K1 or K2
+
+// The KL term and its derivative by s, at e = s_ref - s.
+template <int KL> __device__ __forceinline__ void kl_term(float e, bool k2, float &value, float &slope)
 {
-    return a.moments ? (float)(((double)A - (double)a.moments[0]) / ((double)a.moments[1] + a.adv_eps)) : A;
+    if (KL == kK3) {
+        value = exp_minus_line(e);
+        slope = -(value + e);
+        if (fabsf(e) > 1.0f) slope = 1.0f - expf(e);
+    } else {
+        value = k2 ? 0.5f * e * e : -e;
+        slope = k2 ? -e : 1.0f;
+    }
 }
 
-// Weights of the tokens of each sequence, and with ratios of whole sequences the policy term and its gradient, a thread per
-// sequence.
-__global__ void __launch_bounds__(kSegThreads) policy_sequence_kernel(const __grid_constant__ PolicyArgs a)
+// Ratios of tokens.  SEQ: there is something to a sequence, its weight or its advantage.  Which side of a bound a ratio is on is decided in
+// fp32 but for the few next to it.  What a sum has in common (1 / N, signs) is multiplied in at its end.
+template <bool SEQ, int KL, bool ROLLOUT, bool PER_TOKEN> __global__ void __launch_bounds__(kThreads, kPerSm) policy_token_kernel(const __grid_constant__ PolicyArgs a)
 {
+    const int lane = threadIdx.x & 31, share = blockIdx.x * kWarps + (threadIdx.x >> 5);
     grid_dependency_wait();
     grid_dependency_release();
+    const int live = a.q.live(), tokens = a.w.per_warp * kBlock;
+    const double inv = inverse_norm(a);
+    double v[kStats] = {};
+    if ((int64_t)share * tokens < live) {
+        const int begin = share * tokens, stop = min(live - begin, tokens) + begin;
+        const float g = a.grad_loss ? *a.grad_loss : 1.0f;
+        const float mean = a.moments ? a.moments[0] : 0.0f, scale = a.moments ? (float)(1.0 / ((double)a.moments[1] + a.adv_eps)) : 1.0f;
+        const float high = (float)a.log_high, low = (float)a.log_low, most = (float)a.log_dual;
+        const float up = (float)(1.0 + a.clip_high), down = (float)(1.0 - a.clip_low), dual = (float)a.dual, cap = (float)a.cap;
+        const float beta = a.beta != 0.0 ? (float)(a.beta * inv * g) : 0.0f, slope_of = (float)(-inv * g);
+        Cursor c{0, 0x7FFFFFFF};
+        float w = 1.0f, A_of = 0.0f; // of the sequence: weight / inv, advantage
+        auto enter = [&]() {
+            if (a.sequence_mean) {
+                const Piece p = a.pieces.total_warp(a.q, c.s, lane);
+                w = p.n > 0.0 ? (float)(1.0 / p.n) : 0.0f;
+            }
+            if (!PER_TOKEN) A_of = (__ldg(a.adv + c.s) - mean) * scale;
+        };
+        if (SEQ) {
+            c.at(a.q, begin, lane);
+            enter();
+        }
+        uint32_t next = inv > 0.0 ? load_mask8(a.mask, begin + lane * 8, min(begin + kBlock, stop), a.vec) : 0u;
+#pragma unroll 1
+        for (int base = begin; base < stop; base += kBlock) {
+            const int k = base + lane * 8, hi = min(base + kBlock, stop);
+            const uint32_t valid = next;
+            float s[8] = {}, o[8] = {}, r[8] = {}, b[8] = {}, A[8] = {}, out[8];
+            if (valid) {
+                load8(a.logp, k, hi, a.vec, s);
+                load8(a.old, k, hi, a.vec, o);
+                if (KL) load8(a.ref, k, hi, a.vec, r);
+                if (ROLLOUT) load8(a.rollout, k, hi, a.vec, b);
+                if (PER_TOKEN) load8(a.adv, k, hi, a.vec, A);
+            }
+            next = 0;
+            if (base + kBlock < stop && inv > 0.0) next = load_mask8(a.mask, k + kBlock, min(base + 2 * kBlock, stop), a.vec);
+            zero8(out);
+#pragma unroll 1
+            for (int lo = base;;) { // the block's part of each sequence
+                const uint32_t run = !SEQ || (c.end >= hi && lo == base) ? valid : valid & range_bits(k, lo, c.end);
+                if (__any_sync(kAll, run != 0)) {
+                    float term = 0.0f, kls = 0.0f, drift = 0.0f;
+                    int flats = 0;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const bool in = run >> e & 1;
+                        const float d = s[e] - o[e], Ae = PER_TOKEN ? (A[e] - mean) * scale : A_of;
+                        const float hi_of = Ae >= 0.0f ? high : most, lo_of = Ae >= 0.0f ? -INFINITY : low;
+                        const float over = d - hi_of, under = lo_of - d;
+                        bool flat = over > 0.0f || under > 0.0f, above = over > 0.0f;
+                        if (fminf(fabsf(over), fabsf(under)) <= a.near) { // compared as the formula does
+                            const double D = (double)s[e] - (double)o[e];
+                            above = D > (Ae >= 0.0f ? a.log_high : a.log_dual);
+                            flat = above || (Ae < 0.0f && D < a.log_low);
+                        }
+                        const float rho = expf(d), u = flat ? (above ? (Ae >= 0.0f ? up : dual) : down) : rho;
+                        float x = w * Ae;
+                        if (ROLLOUT) {
+                            const float i = expf(o[e] - b[e]);
+                            x *= i > cap ? cap : i; // NaN stays
+                        }
+                        float grad = flat ? 0.0f : slope_of * x * rho;
+                        term += in ? x * u : 0.0f;
+                        drift += in ? d : 0.0f;
+                        flats += in && flat && Ae != 0.0f;
+                        if (KL) {
+                            float value, slope;
+                            kl_term<KL>(r[e] - s[e], a.k2, value, slope);
+                            kls += in ? value : 0.0f;
+                            if (beta != 0.0f) grad = fmaf(beta * w, slope, grad);
+                        }
+                        if (in) out[e] = grad;
+                    }
+                    v[1] -= (double)term;
+                    v[2] += (double)(w * kls);
+                    v[3] += (double)(w * (float)flats);
+                    v[4] -= (double)(w * drift);
+                }
+                if (!SEQ || c.end > hi) break;
+                if (c.end >= stop) break; // the share ends with it
+                lo = c.end;
+                c.on(a.q, lo, lane);
+                enter();
+                if (lo >= hi) break;
+            }
+            if (a.vec && hi - base == kBlock) store8(a.omega + k, out);
+            else store8(a.omega, k, base, hi, a.vec, out);
+        }
+    }
+#pragma unroll
+    for (int i = 1; i < kStats; ++i) v[i] *= inv;
+    put_stats(v, a.partials + (size_t)blockIdx.x * kStats);
+}
+
+// Ratios of whole sequences: of a sequence the policy term's gradient is the same for every token.  The share that holds a sequence's
+// first token adds what the statistics have of it.
+template <int KL> __global__ void __launch_bounds__(kThreads, kPerSm) policy_sequence_kernel(const __grid_constant__ PolicyArgs a)
+{
+    const int lane = threadIdx.x & 31, share = blockIdx.x * kWarps + (threadIdx.x >> 5);
+    grid_dependency_wait();
+    grid_dependency_release();
+    const int live = a.q.live(), tokens = a.w.per_warp * kBlock;
     const double inv = inverse_norm(a), g = a.grad_loss ? (double)*a.grad_loss : 1.0;
     double v[kStats] = {};
-    for (int64_t s = (int64_t)blockIdx.x * kSegThreads + threadIdx.x; s < a.q.n_seq; s += (int64_t)gridDim.x * kSegThreads) {
-        const Piece p = a.pieces.total(a.q, (int)s);
-        SequenceCoef c{0.0f, 0.0f};
-        if (p.n > 0.0 && inv > 0.0) {
-            const double w = a.sequence_mean ? inv / p.n : inv;
-            c.weight = (float)w;
-            if (a.sequence_ratio) {
-                const double d = p.a / p.n, A = (double)whitened(a, a.adv[s]);
-                const double gap = a.rollout ? exp(p.b / p.n) : 1.0, i = gap > a.cap && a.rollout ? a.cap : gap; // NaN stays
-                const bool flat = A >= 0.0 ? d > a.log_high : (d < a.log_low || d > a.log_dual);
-                double u = exp(d);
-                if (flat) u = A >= 0.0 ? 1.0 + a.clip_high : (d < a.log_low ? 1.0 - a.clip_low : a.dual);
-                else c.slope = (float)(-w * i * A * u * g);
-                v[1] -= p.n * w * i * A * u;
-                if (flat && A != 0.0) v[3] += p.n * w;
-                v[4] -= w * p.a;
+    if ((int64_t)share * tokens < live) {
+        const int begin = share * tokens, stop = min(live - begin, tokens) + begin;
+        Cursor c{0, 0x7FFFFFFF};
+        float w = 0.0f, slope_of = 0.0f, beta = 0.0f;
+        auto enter = [&]() {
+            const Piece p = a.pieces.total_warp(a.q, c.s, lane);
+            w = slope_of = beta = 0.0f;
+            if (!(p.n > 0.0) || !(inv > 0.0)) return;
+            const double weight = a.sequence_mean ? inv / p.n : inv, d = p.a / p.n;
+            double A = (double)__ldg(a.adv + c.s);
+            if (a.moments) A = (A - (double)a.moments[0]) / ((double)a.moments[1] + a.adv_eps);
+            const double gap = a.rollout ? exp(p.b / p.n) : 1.0, i = a.rollout && gap > a.cap ? a.cap : gap; // NaN stays
+            const bool flat = A >= 0.0 ? d > a.log_high : (d < a.log_low || d > a.log_dual);
+            double u = exp(d);
+            w = (float)weight;
+            beta = (float)(a.beta * weight * g);
+            if (flat) u = A >= 0.0 ? 1.0 + a.clip_high : (d < a.log_low ? 1.0 - a.clip_low : a.dual);
+            else slope_of = (float)(-weight * i * A * u * g);
+            if (lane == 0 && a.q.bound(c.s) >= begin) {
+                v[1] -= p.n * weight * i * A * u;
+                if (flat && A != 0.0) v[3] += p.n * weight;
+                v[4] -= weight * p.a;
             }
+        };
+        c.at(a.q, begin, lane);
+        enter();
+#pragma unroll 1
+        for (int base = begin; base < stop; base += kBlock) {
+            const int k = base + lane * 8, hi = min(base + kBlock, stop);
+            const uint32_t valid = inv > 0.0 ? load_mask8(a.mask, k, hi, a.vec) : 0u;
+            float s[8] = {}, r[8] = {}, out[8];
+            if (KL && valid) {
+                load8(a.logp, k, hi, a.vec, s);
+                load8(a.ref, k, hi, a.vec, r);
+            }
+            zero8(out);
+#pragma unroll 1
+            for (int lo = base;;) {
+                const uint32_t run = c.end >= hi && lo == base ? valid : valid & range_bits(k, lo, c.end);
+                float kls = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const bool in = run >> e & 1;
+                    float grad = slope_of;
+                    if (KL) {
+                        float value, slope;
+                        kl_term<KL>(r[e] - s[e], a.k2, value, slope);
+                        kls += in ? value : 0.0f;
+                        if (beta != 0.0f) grad = fmaf(beta, slope, grad);
+                    }
+                    if (in) out[e] = grad;
+                }
+                if (KL) v[2] += (double)(w * kls);
+                if (c.end > hi || c.end >= stop) break;
+                lo = c.end;
+                c.on(a.q, lo, lane);
+                enter();
+                if (lo >= hi) break;
+            }
+            if (a.vec && hi - base == kBlock) store8(a.omega + k, out);
+            else store8(a.omega, k, base, hi, a.vec, out);
         }
-        a.coef[s] = c;
     }
     put_stats(v, a.partials + (size_t)blockIdx.x * kStats);
 }
 
-__global__ void __launch_bounds__(kSegThreads) policy_token_kernel(const __grid_constant__ PolicyArgs a)
-{
-    __shared__ TileShared sh;
-    const int tid = threadIdx.x;
-    grid_dependency_wait();
-    grid_dependency_release();
-    const int live = a.q.live();
-    const double inv = inverse_norm(a);
-    const float g = a.grad_loss ? *a.grad_loss : 1.0f, beta = (float)a.beta;
-    const bool by_sequence = a.sequence_ratio || a.sequence_mean;
-    const float up = (float)(1.0 + a.clip_high), down = (float)(1.0 - a.clip_low), dual = (float)a.dual, cap = (float)a.cap;
-    double v[kStats] = {};
-    for (int tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
-        const int lo = tile * kSegTile, hi = live - lo < kSegTile ? live : lo + kSegTile;
-        if (hi <= lo)
-            break;
-        const int k = lo + tid * kSegEach;
-        uint32_t valid = load_mask8(a.mask, k, hi, a.vec);
-        if (!(inv > 0.0)) valid = 0;
-        float s[8], o[8], r[8], b[8], A[8];
-        load8(a.logp, k, hi, a.vec, s);
-        if (!a.sequence_ratio) load8(a.old, k, hi, a.vec, o);
-        if (a.ref) load8(a.ref, k, hi, a.vec, r);
-        if (a.rollout && !a.sequence_ratio) load8(a.rollout, k, hi, a.vec, b);
-        if (a.per_token) load8(a.adv, k, hi, a.vec, A);
-        tile_sequences(a.q, lo, hi, sh);
-        const uint32_t ends = block_ends(sh, tid);
-        float w = (float)inv, slope = 0.0f, As = 0.0f, out[8];
-        int next = 0; // the token at which the next sequence's numbers are needed
-        if (!by_sequence && a.per_token) next = 8;
-        float part[kStats] = {};
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            out[e] = 0.0f;
-            if (valid >> e & 1) {
-                if (next <= e) {
-                    const int q = a.q.owner(k + e, sh.s0, sh.s1);
-                    if (by_sequence) w = a.coef[q].weight, slope = a.coef[q].slope;
-                    if (!a.per_token && !a.sequence_ratio) As = a.adv[q];
-                    const uint32_t rest = ends >> e; // this sequence's numbers hold up to its end
-                    next = rest ? e + __ffs(rest) : 8;
-                }
-                float grad = slope;
-                if (!a.sequence_ratio) {
-                    const double d = (double)s[e] - (double)o[e]; // exact next to a border
-                    const float rho = expf((float)d), Ae = whitened(a, a.per_token ? A[e] : As);
-                    const bool flat = Ae >= 0.0f ? d > a.log_high : (d < a.log_low || d > a.log_dual);
-                    const float gap = a.rollout ? expf(o[e] - b[e]) : 1.0f, wi = a.rollout ? w * (gap > cap ? cap : gap) : w; // NaN stays
-                    const float u = !flat ? rho : (Ae >= 0.0f ? up : (d < a.log_low ? down : dual));
-                    grad = flat ? 0.0f : -wi * Ae * rho * g;
-                    part[1] -= wi * Ae * u;
-                    if (flat && Ae != 0.0f) part[3] += w;
-                    part[4] += w * (o[e] - s[e]);
-                }
-                if (a.ref) {
-                    const float x = r[e] - s[e];
-                    const float line = exp_minus_line(x);
-                    const float kl = a.kl == HILORE_KL_K3 ? line : (a.kl == HILORE_KL_K2 ? 0.5f * x * x : -x);
-                    const float d = a.kl == HILORE_KL_K3 ? -(fabsf(x) > 1.0f ? expf(x) - 1.0f : line + x) : (a.kl == HILORE_KL_K2 ? -x : 1.0f);
-                    if (beta != 0.0f) grad = fmaf(beta * w * g, d, grad);
-                    part[2] += w * kl;
-                }
-                out[e] = grad;
-            }
-        }
-#pragma unroll
-        for (int i = 1; i < kStats; ++i) v[i] += (double)part[i];
-        store8(a.omega, k, lo, hi, a.vec, out);
-        __syncthreads();
-    }
-    put_stats(v, a.partials + (size_t)(a.slots_before + blockIdx.x) * kStats);
-}
-
 // stats: loss, policy term, KL term, share on flat branches, mean of old - new
-__global__ void __launch_bounds__(kSegThreads) policy_final_kernel(const double *partials, int ctas, double beta, float *stats)
+__global__ void __launch_bounds__(kThreads) policy_final_kernel(const double *partials, int ctas, double beta, float *stats)
 {
     __shared__ double sums[kStats];
     grid_dependency_wait();
@@ -328,16 +438,17 @@ __global__ void __launch_bounds__(kSegThreads) policy_final_kernel(const double 
 
 struct PreferenceArgs {
     Sequences q;
+    Share w;
     const float *rewards, *grad_loss;
     const uint8_t *mask;
     const int64_t *N_dev;
     double N, beta, margin, margin_reward, smoothing, nll;
-    int G, loss, length_mean, vec, tiles, groups, per_cta;
+    int G, loss, length_mean, vec, groups, per_cta, ctas;
     Pieces pieces;
     double *coef; // [n_seq] gradient of every valid token, before the division by N
     double *partials;
-    double *scale; // 1 / N, times the gradient of the loss
-    float *scores;
+    float *scores, *stats;
+    int64_t *pairs;
     float *omega;
 };
 
@@ -351,7 +462,7 @@ __device__ __forceinline__ void softplus_minus(double z, double &value, double &
 
 // A CTA takes `per_cta` whole groups at a time: scores of their sequences into shared memory, then each sequence against the
 // others of its group.
-__global__ void __launch_bounds__(kSegThreads) preference_pairs_kernel(const __grid_constant__ PreferenceArgs a)
+__global__ void __launch_bounds__(kThreads) preference_pairs_kernel(const __grid_constant__ PreferenceArgs a)
 {
     extern __shared__ double smem[];
     const int room = a.per_cta * a.G;
@@ -364,7 +475,7 @@ __global__ void __launch_bounds__(kSegThreads) preference_pairs_kernel(const __g
     for (int64_t first = (int64_t)blockIdx.x * a.per_cta; first < a.groups; first += (int64_t)gridDim.x * a.per_cta) {
         const int n = (int)(a.groups - first < a.per_cta ? a.groups - first : a.per_cta) * a.G;
         const int64_t base = first * a.G;
-        for (int i = threadIdx.x; i < n; i += kSegThreads) {
+        for (int i = threadIdx.x; i < n; i += kThreads) {
             const Piece p = a.pieces.total(a.q, (int)(base + i));
             const double inv = p.n > 0.0 ? 1.0 / p.n : 0.0;
             h[i] = p.n > 0.0 ? a.beta * (a.length_mean ? p.a / p.n : p.a) : 0.0;
@@ -374,7 +485,7 @@ __global__ void __launch_bounds__(kSegThreads) preference_pairs_kernel(const __g
             if (a.scores) a.scores[base + i] = (float)h[i];
         }
         __syncthreads();
-        for (int i = threadIdx.x; i < n; i += kSegThreads) {
+        for (int i = threadIdx.x; i < n; i += kThreads) {
             const int begin = i / a.G * a.G;
             const double hi = h[i];
             const float Ri = R[i];
@@ -419,80 +530,89 @@ __global__ void __launch_bounds__(kSegThreads) preference_pairs_kernel(const __g
     put_stats(v, a.partials + (size_t)blockIdx.x * kStats);
 }
 
-// stats: loss, share of pairs in the right order, mean gap of the scores, mean -log-probability per token of the winners
-__global__ void __launch_bounds__(kSegThreads) preference_final_kernel(const __grid_constant__ PreferenceArgs a, int ctas, int64_t *pairs, float *stats)
+// The gradient of a sequence to each of its valid tokens.  Every CTA adds up the pairs of the CTAs before for the division by N; the first
+// one writes the statistics: loss, share of pairs in the right order, mean gap of the scores, mean -log-probability per token of the winners.
+__global__ void __launch_bounds__(kThreads, 6) preference_token_kernel(const __grid_constant__ PreferenceArgs a)
 {
     __shared__ double sums[kStats];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, share = blockIdx.x * kWarps + warp;
     grid_dependency_wait();
     grid_dependency_release();
-    const int warp = threadIdx.x >> 5;
-    if (warp < kStats) {
-        const double t = sum_slots(a.partials, ctas, warp);
-        if ((threadIdx.x & 31) == 0) sums[warp] = t;
+    const bool count = !a.N_dev && !(a.N > 0.0);
+    if (blockIdx.x == 0 ? warp < kStats : (count && warp == kStats - 1)) {
+        const double t = sum_slots(a.partials, a.ctas, warp);
+        if (lane == 0) sums[warp] = t;
     }
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        const double N = a.N_dev ? (double)*a.N_dev : (a.N > 0.0 ? a.N : sums[4]);
-        const double inv = N > 0.0 ? 1.0 / N : 0.0;
-        *a.scale = inv * (a.grad_loss ? (double)*a.grad_loss : 1.0);
-        if (pairs) *pairs = (int64_t)sums[4];
-        if (stats) {
-            const bool none = !(inv > 0.0) || sums[4] == 0.0;
-            stats[0] = none ? 0.0f : (float)((sums[0] + (a.nll != 0.0 ? a.nll * sums[3] : 0.0)) * inv);
-            for (int i = 1; i < 4; ++i) stats[i] = none ? 0.0f : (float)(sums[i] * inv);
-        }
+    if (blockIdx.x == 0 || count) __syncthreads();
+    const double N = a.N_dev ? (double)*a.N_dev : (count ? sums[kStats - 1] : a.N);
+    const double inv = N > 0.0 ? 1.0 / N : 0.0;
+    if (blockIdx.x == 0 && threadIdx.x < 4) {
+        const int i = threadIdx.x;
+        const bool none = !(inv > 0.0) || sums[4] == 0.0;
+        if (i == 0 && a.pairs) *a.pairs = (int64_t)sums[4];
+        a.stats[i] = none ? 0.0f : (float)((i == 0 ? sums[0] + (a.nll != 0.0 ? a.nll * sums[3] : 0.0) : sums[i]) * inv);
     }
-}
-
-// The gradient of a sequence to each of its valid tokens.
-__global__ void __launch_bounds__(kSegThreads) preference_token_kernel(const __grid_constant__ PreferenceArgs a)
-{
-    __shared__ TileShared sh;
-    const int tid = threadIdx.x;
-    grid_dependency_wait();
-    grid_dependency_release();
-    const int tile = blockIdx.x, lo = tile * kSegTile, live = a.q.live(), hi = live - lo < kSegTile ? live : lo + kSegTile;
-    if (hi <= lo)
+    const double scale = inv * (a.grad_loss ? (double)*a.grad_loss : 1.0);
+    const int live = a.q.live(), tokens = a.w.per_warp * kBlock;
+    if ((int64_t)share * tokens >= live)
         return;
-    const int k = lo + tid * kSegEach;
-    const uint32_t valid = load_mask8(a.mask, k, hi, a.vec);
-    const double scale = *a.scale;
-    tile_sequences(a.q, lo, hi, sh);
-    const uint32_t ends = block_ends(sh, tid);
-    float out[8], c = 0.0f;
-    int next = 0;
+    const int begin = share * tokens, stop = min(live - begin, tokens) + begin;
+    Cursor c;
+    c.at(a.q, begin, lane);
+    float coef = inv > 0.0 ? (float)(__ldg(a.coef + c.s) * scale) : 0.0f;
+#pragma unroll 1
+    for (int base = begin; base < stop; base += kBlock) {
+        const int k = base + lane * 8, hi = min(base + kBlock, stop);
+        const uint32_t valid = load_mask8(a.mask, k, hi, a.vec);
+        float out[8];
+        zero8(out);
+#pragma unroll 1
+        for (int lo = base;;) {
+            const uint32_t run = c.end >= hi && lo == base ? valid : valid & range_bits(k, lo, c.end);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        out[e] = 0.0f;
-        if (valid >> e & 1) {
-            if (next <= e) {
-                c = scale != 0.0 ? (float)(a.coef[a.q.owner(k + e, sh.s0, sh.s1)] * scale) : 0.0f;
-                const uint32_t rest = ends >> e;
-                next = rest ? e + __ffs(rest) : 8;
-            }
-            out[e] = c;
+            for (int e = 0; e < 8; ++e) out[e] = run >> e & 1 ? coef : out[e];
+            if (c.end > hi || c.end >= stop) break;
+            lo = c.end;
+            c.on(a.q, lo, lane);
+            coef = inv > 0.0 ? (float)(__ldg(a.coef + c.s) * scale) : 0.0f;
+            if (lo >= hi) break;
         }
+        if (a.vec && hi - base == kBlock) store8(a.omega + k, out);
+        else store8(a.omega, k, base, hi, a.vec, out);
     }
-    store8(a.omega, k, lo, hi, a.vec, out);
 }
 
 constexpr int kMaxGroup = 1024;
 
-// Layout of a workspace: the CTAs' slots, the pieces of tiles and sequences, a number per sequence, one number.
+// All warps of a call run at once, `per_sm` CTAs on an SM.
+static Share share_of(int64_t n_tok, int per_sm)
+{
+    const int64_t blocks = (n_tok + kBlock - 1) / kBlock, warps = (int64_t)sm_count() * per_sm * kWarps;
+    return Share{(int)blocks, (int)((blocks + warps - 1) / warps < 1 ? 1 : (blocks + warps - 1) / warps)};
+}
+static unsigned ctas_of(const Share &w)
+{
+    const int64_t warps = ((int64_t)w.blocks + w.per_warp - 1) / w.per_warp;
+    return (unsigned)((warps + kWarps - 1) / kWarps);
+}
+
+// Layout of a workspace: the CTAs' slots, the pieces of shares and sequences, a number per sequence.
+constexpr int64_t kMostShares = 148 * 8 * kWarps; // on any device that this runs on, with up to eight CTAs of it on an SM
 struct Workspace {
-    size_t partials, head, tail, whole, coef, scale, bytes;
+    size_t partials, head, tail, whole, coef, bytes;
 };
 static Workspace layout(int64_t n_seq, int64_t n_tok)
 {
     Workspace w;
-    const size_t tiles = n_tok > 0 ? (size_t)((n_tok + kSegTile - 1) / kSegTile) : 0, S = n_seq > 0 ? (size_t)n_seq : 0;
+    const int64_t blocks = n_tok > 0 ? (n_tok + kBlock - 1) / kBlock : 0;
+    const size_t shares = (size_t)(blocks < kMostShares ? blocks : kMostShares), S = n_seq > 0 ? (size_t)n_seq : 0;
     w.partials = 0;
-    w.head = w.partials + sizeof(double) * kStats * 2 * kObjectiveGrid;
-    w.tail = w.head + sizeof(Piece) * tiles;
-    w.whole = w.tail + sizeof(Piece) * tiles;
+    w.head = w.partials + sizeof(double) * kStats * kMostCtas + 16;
+    w.head -= w.head % 16;
+    w.tail = w.head + sizeof(Piece) * shares;
+    w.whole = w.tail + sizeof(Piece) * shares;
     w.coef = w.whole + sizeof(Piece) * S;
-    w.scale = w.coef + sizeof(double) * S;
-    w.bytes = w.scale + 16;
+    w.bytes = w.coef + sizeof(double) * S + 16;
     return w;
 }
 
@@ -531,7 +651,6 @@ extern "C" int hilore_policy_loss(const float *logp, const float *logp_old, cons
     const int bad = check_sequences(cu_seqlens, n_seq, n_tok, a.q);
     if (bad)
         return bad;
-    a.tiles = (int)((n_tok + kSegTile - 1) / kSegTile);
     if (n_tok > 0 && (!logp || !logp_old || !adv || !omega || (t.beta != 0.0 && !logp_ref)))
         return HILORE_INVALID_ARG;
     if (!N_norm_dev && N_norm <= 0)
@@ -547,36 +666,49 @@ extern "C" int hilore_policy_loss(const float *logp, const float *logp_old, cons
     a.mask = mask, a.N_dev = N_norm_dev, a.N = (double)N_norm, a.clip_low = t.clip_low, a.clip_high = t.clip_high;
     a.log_low = std::log1p(-t.clip_low), a.log_high = std::log1p(t.clip_high);
     a.dual = t.dual_clip != 0.0 ? t.dual_clip : INFINITY, a.log_dual = std::log(a.dual), a.cap = t.rollout_cap, a.beta = t.beta, a.adv_eps = t.adv_eps;
-    a.per_token = t.adv_per_token, a.sequence_ratio = t.ratio == HILORE_RATIO_SEQUENCE, a.sequence_mean = t.mean == HILORE_MEAN_SEQUENCES, a.kl = t.kl;
-    a.vec = vectors({logp, logp_old, logp_ref, logp_rollout, a.per_token ? adv : nullptr, omega}, mask);
+    const bool sequence_ratio = t.ratio == HILORE_RATIO_SEQUENCE, per_token = t.adv_per_token != 0;
+    a.sequence_mean = t.mean == HILORE_MEAN_SEQUENCES, a.k2 = t.kl == HILORE_KL_K2;
+    double widest = 0.0; // of the bounds: a ratio's logarithm and they are rounded to fp32 where they are compared first
+    for (double b : {a.log_low, a.log_high, a.log_dual})
+        if (std::isfinite(b) && std::fabs(b) > widest) widest = std::fabs(b);
+    a.near = (float)(widest * 0x1p-21 + 0x1p-126);
+    a.vec = vectors({logp, logp_old, logp_ref, logp_rollout, per_token ? adv : nullptr, omega}, mask);
     unsigned char *ws = static_cast<unsigned char *>(workspace);
     a.pieces = pieces_of(workspace, w);
-    a.coef = reinterpret_cast<SequenceCoef *>(ws + w.coef);
     a.partials = reinterpret_cast<double *>(ws + w.partials);
     a.omega = omega;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    int ctas = 0;
-    if (a.tiles > 0 && (a.sequence_ratio || a.sequence_mean)) {
+    unsigned ctas = 0;
+    if (n_tok > 0 && (sequence_ratio || a.sequence_mean)) {
         SumArgs s{};
-        s.q = a.q, s.mask = mask, s.out = a.pieces, s.vec = a.vec;
-        if (a.sequence_ratio) s.x = logp, s.minus = logp_old;
-        if (a.sequence_ratio && logp_rollout) s.y = logp_old, s.less = logp_rollout;
-        if (launch_dependent(sequence_sums_kernel, dim3((unsigned)a.tiles), dim3(kSegThreads), 0, st, s) != cudaSuccess)
-            return HILORE_CUDA;
-        ctas = grid_of((n_seq + kSegThreads - 1) / kSegThreads, kObjectiveGrid);
-        if (launch_dependent(policy_sequence_kernel, dim3((unsigned)ctas), dim3(kSegThreads), 0, st, a) != cudaSuccess)
+        s.q = a.q, s.w = share_of(n_tok, kSumsPerSm), s.mask = mask, s.vec = a.vec;
+        s.out = a.pieces;
+        s.out.share = a.pieces.share = s.w.per_warp * kBlock;
+        if (sequence_ratio) s.x = logp, s.minus = logp_old;
+        if (sequence_ratio && logp_rollout) s.y = logp_old, s.less = logp_rollout;
+        void (*const sums)(SumArgs) = !sequence_ratio ? sequence_sums_kernel<false, 0> : (logp_rollout ? sequence_sums_kernel<true, 1> : sequence_sums_kernel<true, 0>);
+        if (launch_dependent(sums, dim3(ctas_of(s.w)), dim3(kThreads), 0, st, s) != cudaSuccess)
             return HILORE_CUDA;
     }
-    if (a.tiles > 0) {
-        a.slots_before = ctas;
-        int64_t most = (int64_t)sm_count() * ctas_per_sm(policy_token_kernel, kSegThreads, 0, 4);
-        if (most > kObjectiveGrid) most = kObjectiveGrid;
-        const int grid = grid_of(a.tiles, most);
-        if (launch_dependent(policy_token_kernel, dim3((unsigned)grid), dim3(kSegThreads), 0, st, a) != cudaSuccess)
+    if (n_tok > 0) {
+        a.w = share_of(n_tok, kPerSm);
+        ctas = ctas_of(a.w);
+        const int kl = !logp_ref ? kNoKl : (t.kl == HILORE_KL_K3 ? kK3 : kEasyKl);
+        void (*kernel)(PolicyArgs) = nullptr;
+        if (sequence_ratio) {
+            kernel = kl == kNoKl ? policy_sequence_kernel<kNoKl> : (kl == kK3 ? policy_sequence_kernel<kK3> : policy_sequence_kernel<kEasyKl>);
+        } else {
+#define HILORE_KLS(SEQ, ROLL, PER) {policy_token_kernel<SEQ, kNoKl, ROLL, PER>, policy_token_kernel<SEQ, kEasyKl, ROLL, PER>, policy_token_kernel<SEQ, kK3, ROLL, PER>}
+            static void (*const kernels[3][2][3])(PolicyArgs) = {{HILORE_KLS(false, false, true), HILORE_KLS(false, true, true)},
+                                                                 {HILORE_KLS(true, false, true), HILORE_KLS(true, true, true)},
+                                                                 {HILORE_KLS(true, false, false), HILORE_KLS(true, true, false)}};
+#undef HILORE_KLS
+            kernel = kernels[!per_token ? 2 : (a.sequence_mean ? 1 : 0)][logp_rollout != nullptr][kl];
+        }
+        if (launch_dependent(kernel, dim3(ctas), dim3(kThreads), 0, st, a) != cudaSuccess)
             return HILORE_CUDA;
-        ctas += grid;
     }
-    if (launch_dependent(policy_final_kernel, dim3(1), dim3(kSegThreads), 0, st, (const double *)a.partials, ctas, a.beta, stats) != cudaSuccess)
+    if (launch_dependent(policy_final_kernel, dim3(1), dim3(kThreads), 0, st, (const double *)a.partials, (int)ctas, a.beta, stats) != cudaSuccess)
         return HILORE_CUDA;
     return cudaGetLastError() == cudaSuccess ? HILORE_OK : HILORE_CUDA;
 }
@@ -597,7 +729,6 @@ extern "C" int hilore_preference_loss(const float *logp, const float *logp_ref, 
     const int bad = check_sequences(cu_seqlens, n_seq, n_tok, a.q);
     if (bad)
         return bad;
-    a.tiles = (int)((n_tok + kSegTile - 1) / kSegTile);
     if (n_seq % G != 0 || G > kMaxGroup)
         return HILORE_SHAPE;
     if ((n_tok > 0 && (!logp || !omega)) || (n_seq > 0 && !rewards))
@@ -615,31 +746,29 @@ extern "C" int hilore_preference_loss(const float *logp, const float *logp_ref, 
     a.margin_reward = t.margin_reward, a.smoothing = t.smoothing, a.nll = t.nll, a.G = G, a.loss = t.loss, a.length_mean = t.length_mean;
     a.vec = vectors({logp, logp_ref, omega}, mask);
     a.groups = (int)(n_seq / G);
-    a.per_cta = G >= kSegThreads ? 1 : kSegThreads / G;
+    a.per_cta = G >= kThreads ? 1 : kThreads / G;
     unsigned char *ws = static_cast<unsigned char *>(workspace);
     a.pieces = pieces_of(workspace, w);
     a.coef = reinterpret_cast<double *>(ws + w.coef);
     a.partials = reinterpret_cast<double *>(ws + w.partials);
-    a.scale = reinterpret_cast<double *>(ws + w.scale);
-    a.scores = scores;
-    a.omega = omega;
+    a.scores = scores, a.stats = stats, a.pairs = pairs, a.omega = omega;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    int ctas = 0;
-    if (a.tiles > 0) {
+    if (n_tok > 0) {
         SumArgs s{};
-        s.q = a.q, s.mask = mask, s.out = a.pieces, s.vec = a.vec, s.x = logp, s.minus = logp_ref, s.y = logp;
-        if (launch_dependent(sequence_sums_kernel, dim3((unsigned)a.tiles), dim3(kSegThreads), 0, st, s) != cudaSuccess)
+        s.q = a.q, s.w = share_of(n_tok, kSumsPerSm), s.mask = mask, s.vec = a.vec, s.x = logp, s.minus = logp_ref;
+        s.out = a.pieces;
+        s.out.share = a.pieces.share = s.w.per_warp * kBlock;
+        if (launch_dependent(sequence_sums_kernel<true, 2>, dim3(ctas_of(s.w)), dim3(kThreads), 0, st, s) != cudaSuccess)
             return HILORE_CUDA;
     }
     if (a.groups > 0) {
-        ctas = grid_of((a.groups + a.per_cta - 1) / a.per_cta, kObjectiveGrid);
+        a.ctas = grid_of((a.groups + a.per_cta - 1) / a.per_cta, kMostCtas);
         const size_t smem = (size_t)a.per_cta * G * (3 * sizeof(double) + sizeof(float));
-        if (launch_dependent(preference_pairs_kernel, dim3((unsigned)ctas), dim3(kSegThreads), smem, st, a) != cudaSuccess)
+        if (launch_dependent(preference_pairs_kernel, dim3((unsigned)a.ctas), dim3(kThreads), smem, st, a) != cudaSuccess)
             return HILORE_CUDA;
     }
-    if (launch_dependent(preference_final_kernel, dim3(1), dim3(kSegThreads), 0, st, a, ctas, pairs, stats) != cudaSuccess)
-        return HILORE_CUDA;
-    if (a.tiles > 0 && launch_dependent(preference_token_kernel, dim3((unsigned)a.tiles), dim3(kSegThreads), 0, st, a) != cudaSuccess)
+    a.w = share_of(n_tok, 6);
+    if (launch_dependent(preference_token_kernel, dim3(n_tok > 0 ? ctas_of(a.w) : 1u), dim3(kThreads), 0, st, a) != cudaSuccess)
         return HILORE_CUDA;
     return cudaGetLastError() == cudaSuccess ? HILORE_OK : HILORE_CUDA;
 }

@@ -283,6 +283,14 @@ __device__ __forceinline__ uint32_t range_bits(int k, int lo, int hi)
     return from & to & 0xFFu;
 }
 
+// yes ? a : b with both worked out, where the compiler would make a branch of it.
+__device__ __forceinline__ double pick(bool yes, double a, double b)
+{
+    double r;
+    asm("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %3, 0;\n\tselp.f64 %0, %1, %2, p;\n\t}" : "=d"(r) : "d"(a), "d"(b), "r"((uint32_t)yes));
+    return r;
+}
+
 // ---- scans over the lanes of a warp ----
 // Op::Map is what a run of tokens does to the state that comes in; Op::then(a, b) is a followed by b, Op::apply(m, s) the state
 // behind the run.  A run that holds the start of a sequence does not depend on what comes in, and says so in its flag.
