@@ -122,17 +122,34 @@ template <bool X, int Y> __global__ void __launch_bounds__(kThreads, kSumsPerSm)
         sum = Piece{0.0, 0.0, 0.0};
         n = 0;
     };
+    // a block's tensors are asked for while the block before is added up, its mask one block earlier
+    constexpr int kX = X ? 8 : 1, kY = Y == 1 ? 8 : 1;
+    struct {
+        uint32_t valid;
+        float x[kX], m[kX], y[kY], l[kY];
+    } now{}, then{};
+    Mask8 mask;
+    auto ask = [&](auto &to, int base) { // with the block's mask read
+        const int k = base + lane * 8, hi = min(base + kBlock, stop);
+        to.valid = base < stop ? mask.bits(k, hi) : 0u;
+        mask.read(a.mask, k + kBlock, stop, a.vec);
+        if (to.valid == 0) return;
+        if constexpr (X) {
+            load8(a.x, k, hi, a.vec, to.x);
+            if (a.minus) load8(a.minus, k, hi, a.vec, to.m);
+        }
+        if constexpr (Y == 1) {
+            load8(a.y, k, hi, a.vec, to.y);
+            if (a.less) load8(a.less, k, hi, a.vec, to.l);
+        }
+    };
+    mask.read(a.mask, begin + lane * 8, stop, a.vec);
+    ask(now, begin);
 #pragma unroll 1
     for (int base = begin; base < stop; base += kBlock) {
         const int k = base + lane * 8, hi = min(base + kBlock, stop);
-        const uint32_t valid = load_mask8(a.mask, k, hi, a.vec);
-        float x[8] = {}, m[8] = {}, y[8] = {}, l[8] = {};
-        if (valid) {
-            if (X) load8(a.x, k, hi, a.vec, x);
-            if (X && a.minus) load8(a.minus, k, hi, a.vec, m);
-            if (Y == 1) load8(a.y, k, hi, a.vec, y);
-            if (Y == 1 && a.less) load8(a.less, k, hi, a.vec, l);
-        }
+        const uint32_t valid = now.valid;
+        ask(then, base + kBlock);
 #pragma unroll 1
         for (int lo = base;;) { // the block's part of each sequence
             const uint32_t run = c.end >= hi && lo == base ? valid : valid & range_bits(k, lo, c.end);
@@ -140,9 +157,9 @@ template <bool X, int Y> __global__ void __launch_bounds__(kThreads, kSumsPerSm)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const bool in = run >> e & 1;
-                    if (X) sum.a += pick(in, (double)x[e] - (double)m[e], 0.0);
-                    if (Y == 1) sum.b += pick(in, (double)y[e] - (double)l[e], 0.0);
-                    if (Y == 2) sum.b += pick(in, (double)x[e], 0.0);
+                    if constexpr (X) sum.a += pick(in, (double)now.x[e] - (double)now.m[e], 0.0);
+                    if constexpr (Y == 1) sum.b += pick(in, (double)now.y[e] - (double)now.l[e], 0.0);
+                    if constexpr (Y == 2) sum.b += pick(in, (double)now.x[e], 0.0);
                 }
                 n += __popc(run);
             }
@@ -153,6 +170,7 @@ template <bool X, int Y> __global__ void __launch_bounds__(kThreads, kSumsPerSm)
             c.on(a.q, lo, lane);
             if (lo >= hi) break;
         }
+        now = then;
     }
     finish(false);
 }
@@ -185,24 +203,42 @@ __device__ __forceinline__ double sum_slots(const double *partials, int ctas, in
 
 // ------------------------------------------------------------------ policy loss
 
-// exp(e) - e - 1 without the cancellation at small e: there the Taylor series of it, sum over j of e^(j+2) / (j+2)!, whose
-// first term left out at |e| <= 1 is 2 / 13! of the first.
+// exp(e) - e - 1 without the cancellation at small e: the Taylor series, sum over j of e^(j+2) / (j+2)!, of which the first term left
+// out at |e| <= 2 is 2^14 2 / 16! = 1.6e-9 of the first.  Larger e need another form.  A number, or two at once.
+constexpr float kLargest = 2.0f;
+#define HILORE_TWICE(x) {1.0f / x, 1.0f / x}
+static __constant__ float2 kInverseFactorials[14] = {
+    HILORE_TWICE(2.0f), HILORE_TWICE(6.0f), HILORE_TWICE(24.0f), HILORE_TWICE(120.0f), HILORE_TWICE(720.0f),
+    HILORE_TWICE(5040.0f), HILORE_TWICE(40320.0f), HILORE_TWICE(362880.0f), HILORE_TWICE(3628800.0f), HILORE_TWICE(39916800.0f),
+    HILORE_TWICE(479001600.0f), HILORE_TWICE(6227020800.0f), HILORE_TWICE(87178291200.0f), HILORE_TWICE(1307674368000.0f)};
+#undef HILORE_TWICE
 __device__ __forceinline__ float exp_minus_line(float e)
 {
-    float s = 1.0f / 479001600.0f;
-    s = fmaf(s, e, 1.0f / 39916800.0f);
-    s = fmaf(s, e, 1.0f / 3628800.0f);
-    s = fmaf(s, e, 1.0f / 362880.0f);
-    s = fmaf(s, e, 1.0f / 40320.0f);
-    s = fmaf(s, e, 1.0f / 5040.0f);
-    s = fmaf(s, e, 1.0f / 720.0f);
-    s = fmaf(s, e, 1.0f / 120.0f);
-    s = fmaf(s, e, 1.0f / 24.0f);
-    s = fmaf(s, e, 1.0f / 6.0f);
-    s = fmaf(s, e, 0.5f);
-    s *= e * e;
-    if (fabsf(e) > 1.0f) s = expf(e) - e - 1.0f;
-    return s;
+    float s = kInverseFactorials[13].x;
+#pragma unroll
+    for (int j = 12; j >= 0; --j) s = fmaf(s, e, kInverseFactorials[j].x);
+    return s * (e * e);
+}
+__device__ __forceinline__ void exp_minus_line(float e0, float e1, float &v0, float &v1)
+{
+    const uint64_t *factors = reinterpret_cast<const uint64_t *>(kInverseFactorials);
+    const uint64_t e = f32x2_pack(e0, e1);
+    uint64_t s = factors[13];
+#pragma unroll
+    for (int j = 12; j >= 0; --j) s = f32x2_fma(s, e, factors[j]);
+    f32x2_unpack(f32x2_mul(s, f32x2_mul(e, e)), v0, v1);
+}
+
+constexpr float kNear = 80.0f;
+// exp(d) = 2^(d log2 e) for |d| <= kNear, with log2 e in two parts: the power of the first part's product, as it is rounded, and to first
+// order that of what the rounding and the second part leave.
+__device__ __forceinline__ float exp_near(float d)
+{
+    constexpr float kLog2e = 1.44269502162933349609375f, kRest = 1.925963033500011079e-8f, kLn2 = 0.693147180559945309f;
+    const float t = d * kLog2e, rest = fmaf(d, kRest, fmaf(d, kLog2e, -t));
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(t));
+    return fmaf(y, rest * kLn2, y);
 }
 
 struct PolicyArgs {
@@ -213,7 +249,7 @@ struct PolicyArgs {
     const int64_t *N_dev;
     double N, clip_low, clip_high, log_low, log_high, log_dual, dual, cap, beta, adv_eps;
     float near; // distance of a logarithm of a ratio from its bounds within which it is compared in fp64
-    int sequence_mean, k2, vec;
+    int sequence_mean, k2, dual_clip, vec;
     Pieces pieces;
     double *partials;
     float *omega;
@@ -231,9 +267,11 @@ enum { kNoKl = 0, kEasyKl = 1, kK3 = 2 }; // kEasyKl: K1 or K2
 template <int KL> __device__ __forceinline__ void kl_term(float e, bool k2, float &value, float &slope)
 {
     if (KL == kK3) {
-        value = exp_minus_line(e);
-        slope = -(value + e);
-        if (fabsf(e) > 1.0f) slope = 1.0f - expf(e);
+        // both forms, and a choice: a branch would cost as much
+        const float near = exp_minus_line(e), all = expf(e);
+        const bool far = fabsf(e) > kLargest;
+        value = far ? all - e - 1.0f : near;
+        slope = far ? 1.0f - all : -(near + e);
     } else {
         value = k2 ? 0.5f * e * e : -e;
         slope = k2 ? -e : 1.0f;
@@ -254,8 +292,8 @@ template <bool SEQ, int KL, bool ROLLOUT, bool PER_TOKEN> __global__ void __laun
         const int begin = share * tokens, stop = min(live - begin, tokens) + begin;
         const float g = a.grad_loss ? *a.grad_loss : 1.0f;
         const float mean = a.moments ? a.moments[0] : 0.0f, scale = a.moments ? (float)(1.0 / ((double)a.moments[1] + a.adv_eps)) : 1.0f;
-        const float high = (float)a.log_high, low = (float)a.log_low, most = (float)a.log_dual;
-        const float up = (float)(1.0 + a.clip_high), down = (float)(1.0 - a.clip_low), dual = (float)a.dual, cap = (float)a.cap;
+        const float high = (float)a.log_high, low = (float)a.log_low, dual_log = (float)a.log_dual;
+        const float most_up = (float)(1.0 + a.clip_high), most_down = (float)(1.0 - a.clip_low), dual = (float)a.dual, cap = (float)a.cap;
         const float beta = a.beta != 0.0 ? (float)(a.beta * inv * g) : 0.0f, slope_of = (float)(-inv * g);
         Cursor c{0, 0x7FFFFFFF};
         float w = 1.0f, A_of = 0.0f; // of the sequence: weight / inv, advantage
@@ -270,11 +308,12 @@ template <bool SEQ, int KL, bool ROLLOUT, bool PER_TOKEN> __global__ void __laun
             c.at(a.q, begin, lane);
             enter();
         }
-        uint32_t next = inv > 0.0 ? load_mask8(a.mask, begin + lane * 8, min(begin + kBlock, stop), a.vec) : 0u;
+        Mask8 mask;
+        mask.read(a.mask, begin + lane * 8, stop, a.vec);
 #pragma unroll 1
         for (int base = begin; base < stop; base += kBlock) {
             const int k = base + lane * 8, hi = min(base + kBlock, stop);
-            const uint32_t valid = next;
+            const uint32_t valid = inv > 0.0 ? mask.bits(k, hi) : 0u;
             float s[8] = {}, o[8] = {}, r[8] = {}, b[8] = {}, A[8] = {}, out[8];
             if (valid) {
                 load8(a.logp, k, hi, a.vec, s);
@@ -283,49 +322,139 @@ template <bool SEQ, int KL, bool ROLLOUT, bool PER_TOKEN> __global__ void __laun
                 if (ROLLOUT) load8(a.rollout, k, hi, a.vec, b);
                 if (PER_TOKEN) load8(a.adv, k, hi, a.vec, A);
             }
-            next = 0;
-            if (base + kBlock < stop && inv > 0.0) next = load_mask8(a.mask, k + kBlock, min(base + 2 * kBlock, stop), a.vec);
+            mask.read(a.mask, k + kBlock, stop, a.vec);
             zero8(out);
 #pragma unroll 1
             for (int lo = base;;) { // the block's part of each sequence
                 const uint32_t run = !SEQ || (c.end >= hi && lo == base) ? valid : valid & range_bits(k, lo, c.end);
-                if (__any_sync(kAll, run != 0)) {
-                    float term = 0.0f, kls = 0.0f, drift = 0.0f;
-                    int flats = 0;
+                // Nearly always a block has one sequence, no ratio within rounding of a bound, and nothing far out: then masked tokens go as
+                // zeros, which add nothing to any sum, and the objective is the smaller of two products.
+                bool plain = !SEQ || (lo == base && c.end >= hi);
+                if (plain) {
+                    if (run != 0xFFu) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (!(run >> e & 1)) {
+                                s[e] = o[e] = 0.0f;
+                                if (KL) r[e] = 0.0f;
+                                if (ROLLOUT) b[e] = 0.0f;
+                                if (PER_TOKEN) A[e] = mean;
+                            }
+                    }
+                    bool odd = false;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        const bool in = run >> e & 1;
-                        const float d = s[e] - o[e], Ae = PER_TOKEN ? (A[e] - mean) * scale : A_of;
-                        const float hi_of = Ae >= 0.0f ? high : most, lo_of = Ae >= 0.0f ? -INFINITY : low;
-                        const float over = d - hi_of, under = lo_of - d;
-                        bool flat = over > 0.0f || under > 0.0f, above = over > 0.0f;
-                        if (fminf(fabsf(over), fabsf(under)) <= a.near) { // compared as the formula does
-                            const double D = (double)s[e] - (double)o[e];
-                            above = D > (Ae >= 0.0f ? a.log_high : a.log_dual);
-                            flat = above || (Ae < 0.0f && D < a.log_low);
+                        const float d = s[e] - o[e];
+                        odd |= !(fabsf(d) <= kNear);
+                        odd |= fminf(fabsf(d - high), fabsf(d - low)) <= a.near;
+                        if (a.dual_clip) odd |= fabsf(d - dual_log) <= a.near;
+                        if (KL == kK3) odd |= !(fabsf(r[e] - s[e]) <= kLargest);
+                        if (ROLLOUT) odd |= !(fabsf(o[e] - b[e]) <= kNear);
+                    }
+                    plain = !__any_sync(kAll, odd);
+                }
+                if (plain) {
+                    float term = 0.0f, kls = 0.0f, drift = 0.0f, flats = 0.0f;
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2) {
+                        float value[2], slope[2];
+                        if (KL == kK3) {
+                            const float e0 = r[e] - s[e], e1 = r[e + 1] - s[e + 1];
+                            exp_minus_line(e0, e1, value[0], value[1]);
+                            slope[0] = -(value[0] + e0);
+                            slope[1] = -(value[1] + e1);
+                        } else if (KL) {
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) kl_term<KL>(r[e + i] - s[e + i], a.k2, value[i], slope[i]);
                         }
-                        const float rho = expf(d), u = flat ? (above ? (Ae >= 0.0f ? up : dual) : down) : rho;
-                        float x = w * Ae;
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const float d = s[e + i] - o[e + i], rho = exp_near(d);
+                            float x = PER_TOKEN ? (A[e + i] - mean) * scale : (run >> (e + i) & 1 ? A_of : 0.0f);
+                            if (SEQ) x *= w;
+                            if (ROLLOUT) x *= fminf(exp_near(o[e + i] - b[e + i]), cap);
+                            const float gain = x * rho;
+                            float held = fminf(gain, x * fminf(fmaxf(rho, most_down), most_up));
+                            if (a.dual_clip) held = x < 0.0f ? fmaxf(held, x * dual) : held;
+                            float grad = held != gain ? 0.0f : slope_of * gain;
+                            flats += held != gain ? 1.0f : 0.0f;
+                            term += held;
+                            drift += d;
+                            if (KL) {
+                                kls += value[i];
+                                grad = fmaf(SEQ ? beta * w : beta, slope[i], grad);
+                            }
+                            out[e + i] = grad;
+                        }
+                    }
+                    if (run != 0xFFu) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) out[e] = run >> e & 1 ? out[e] : 0.0f;
+                    }
+                    v[1] -= (double)term;
+                    if (KL) v[2] += (double)(SEQ ? w * kls : kls);
+                    v[3] += (double)(SEQ ? w * flats : flats);
+                    v[4] -= (double)(SEQ ? w * drift : drift);
+                } else if (__any_sync(kAll, run != 0)) {
+                    // which tokens are on a flat branch, and which of these on the dual clip's
+                    uint32_t flat = 0, over = 0;
+                    bool close = false;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float Ae = PER_TOKEN ? (A[e] - mean) * scale : A_of, d = s[e] - o[e];
+                        // A >= 0: beyond the bound where d > high; A < 0: where -d > -low
+                        const bool up = Ae >= 0.0f;
+                        const float past = __uint_as_float(__float_as_uint(d) ^ (up ? 0u : 0x80000000u)) - (up ? high : -low);
+                        flat |= past > 0.0f ? 1u << e : 0u;
+                        close |= fabsf(past) <= a.near;
+                        if (a.dual_clip) {
+                            over |= !up && d > dual_log ? 1u << e : 0u;
+                            close |= fabsf(d - dual_log) <= a.near;
+                        }
+                    }
+                    if (close) { // next to a bound: compared as the formula does
+                        flat = over = 0;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const float Ae = PER_TOKEN ? (A[e] - mean) * scale : A_of;
+                            const double D = (double)s[e] - (double)o[e];
+                            if (Ae >= 0.0f ? D > a.log_high : D < a.log_low) flat |= 1u << e;
+                            if (!(Ae >= 0.0f) && D > a.log_dual) over |= 1u << e;
+                        }
+                    }
+                    flat |= over;
+                    float term = 0.0f, kls = 0.0f, drift = 0.0f;
+                    uint32_t none = 0; // tokens of no advantage
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const bool in = run >> e & 1, on_flat = flat >> e & 1;
+                        const float Ae = PER_TOKEN ? (A[e] - mean) * scale : A_of, d = s[e] - o[e];
+                        const float rho = fabsf(d) <= kNear ? exp_near(d) : expf(d); // the same bits as above where that is enough
+                        float bound = Ae >= 0.0f ? most_up : most_down;
+                        if (a.dual_clip) bound = over >> e & 1 ? dual : bound;
+                        float x = SEQ ? w * Ae : Ae;
                         if (ROLLOUT) {
-                            const float i = expf(o[e] - b[e]);
+                            const float gap = o[e] - b[e], i = fabsf(gap) <= kNear ? exp_near(gap) : expf(gap);
                             x *= i > cap ? cap : i; // NaN stays
                         }
-                        float grad = flat ? 0.0f : slope_of * x * rho;
-                        term += in ? x * u : 0.0f;
+                        const float gain = x * (on_flat ? bound : rho);
+                        float grad = on_flat ? 0.0f : slope_of * gain;
+                        term += in ? gain : 0.0f;
                         drift += in ? d : 0.0f;
-                        flats += in && flat && Ae != 0.0f;
+                        none |= Ae == 0.0f ? 1u << e : 0u;
                         if (KL) {
                             float value, slope;
                             kl_term<KL>(r[e] - s[e], a.k2, value, slope);
                             kls += in ? value : 0.0f;
-                            if (beta != 0.0f) grad = fmaf(beta * w, slope, grad);
+                            if (beta != 0.0f) grad = fmaf(SEQ ? beta * w : beta, slope, grad);
                         }
                         if (in) out[e] = grad;
                     }
+                    const int flats = __popc(flat & ~none & run);
                     v[1] -= (double)term;
-                    v[2] += (double)(w * kls);
-                    v[3] += (double)(w * (float)flats);
-                    v[4] -= (double)(w * drift);
+                    if (KL) v[2] += (double)(SEQ ? w * kls : kls);
+                    v[3] += (double)(SEQ ? w * (float)flats : (float)flats);
+                    v[4] -= (double)(SEQ ? w * drift : drift);
                 }
                 if (!SEQ || c.end > hi) break;
                 if (c.end >= stop) break; // the share ends with it
@@ -379,10 +508,13 @@ template <int KL> __global__ void __launch_bounds__(kThreads, kPerSm) policy_seq
         };
         c.at(a.q, begin, lane);
         enter();
+        Mask8 mask;
+        mask.read(a.mask, begin + lane * 8, stop, a.vec);
 #pragma unroll 1
         for (int base = begin; base < stop; base += kBlock) {
             const int k = base + lane * 8, hi = min(base + kBlock, stop);
-            const uint32_t valid = inv > 0.0 ? load_mask8(a.mask, k, hi, a.vec) : 0u;
+            const uint32_t valid = inv > 0.0 ? mask.bits(k, hi) : 0u;
+            mask.read(a.mask, k + kBlock, stop, a.vec);
             float s[8] = {}, r[8] = {}, out[8];
             if (KL && valid) {
                 load8(a.logp, k, hi, a.vec, s);
@@ -443,7 +575,7 @@ struct PreferenceArgs {
     const uint8_t *mask;
     const int64_t *N_dev;
     double N, beta, margin, margin_reward, smoothing, nll;
-    int G, loss, length_mean, vec, groups, per_cta, ctas;
+    int G, loss, length_mean, vec, groups, per_cta, team, ctas;
     Pieces pieces;
     double *coef; // [n_seq] gradient of every valid token, before the division by N
     double *partials;
@@ -451,14 +583,6 @@ struct PreferenceArgs {
     int64_t *pairs;
     float *omega;
 };
-
-// -ln sigmoid(z) and its derivative
-__device__ __forceinline__ void softplus_minus(double z, double &value, double &slope)
-{
-    const double t = exp(-fabs(z));
-    value = log1p(t) + fmax(-z, 0.0);
-    slope = z >= 0.0 ? -t / (1.0 + t) : -1.0 / (1.0 + t);
-}
 
 // A CTA takes `per_cta` whole groups at a time: scores of their sequences into shared memory, then each sequence against the
 // others of its group.
@@ -485,25 +609,30 @@ __global__ void __launch_bounds__(kThreads) preference_pairs_kernel(const __grid
             if (a.scores) a.scores[base + i] = (float)h[i];
         }
         __syncthreads();
-        for (int i = threadIdx.x; i < n; i += kThreads) {
+        // a.team neighbouring threads share the others of a response's group
+        const int part = threadIdx.x & (a.team - 1);
+        for (int i = threadIdx.x / a.team; i < n; i += kThreads / a.team) {
             const int begin = i / a.G * a.G;
             const double hi = h[i];
             const float Ri = R[i];
             double c = 0.0;
             int wins = 0;
             if (per[i] > 0.0)
-                for (int j = begin; j < begin + a.G; ++j) {
+                for (int j = begin + part; j < begin + a.G; j += a.team) {
                     const float Rj = R[j];
                     if (!(per[j] > 0.0) || !(Ri > Rj || Rj > Ri)) continue;
                     const bool won = Ri > Rj;
                     const double gap = won ? hi - h[j] : h[j] - hi;
                     const double more = a.margin_reward != 0.0 ? a.margin_reward * (won ? (double)Ri - (double)Rj : (double)Rj - (double)Ri) : 0.0;
                     const double z = gap - a.margin - more;
-                    double value, slope;
+                    double value = 0.0, slope;
                     if (a.loss == HILORE_PREF_SIGMOID) {
-                        softplus_minus(z, value, slope);
-                        if (a.smoothing != 0.0) value += a.smoothing * z; // -ln sigmoid(-z) = z - ln sigmoid(z)
-                        slope += a.smoothing;
+                        const double t = exp(-fabs(z)); // -ln sigmoid(z) and its derivative
+                        slope = a.smoothing - (z >= 0.0 ? t : 1.0) / (1.0 + t);
+                        if (won) {
+                            value = log1p(t) + fmax(-z, 0.0);
+                            if (a.smoothing != 0.0) value += a.smoothing * z; // -ln sigmoid(-z) = z - ln sigmoid(z)
+                        }
                     } else if (a.loss == HILORE_PREF_HINGE) {
                         value = z >= 1.0 ? 0.0 : 1.0 - z;
                         slope = z >= 1.0 ? 0.0 : (z < 1.0 ? -1.0 : z);
@@ -520,10 +649,18 @@ __global__ void __launch_bounds__(kThreads) preference_pairs_kernel(const __grid
                         v[2] += gap;
                     }
                 }
-            v[3] -= wins * like[i];
-            v[4] += wins;
-            c *= a.length_mean ? a.beta * per[i] : a.beta;
-            a.coef[base + i] = wins ? c - a.nll * wins * per[i] : c;
+            // teams are whole parts of a warp, and their threads take the same turns
+            const uint32_t team = a.team == 32 ? kAll : ((1u << a.team) - 1) << (threadIdx.x & 31 & ~(a.team - 1));
+            for (int by = a.team / 2; by > 0; by /= 2) {
+                c += __shfl_xor_sync(team, c, by);
+                wins += __shfl_xor_sync(team, wins, by);
+            }
+            if (part == 0) {
+                v[3] -= wins * like[i];
+                v[4] += wins;
+                c *= a.length_mean ? a.beta * per[i] : a.beta;
+                a.coef[base + i] = wins ? c - a.nll * wins * per[i] : c;
+            }
         }
         __syncthreads();
     }
@@ -560,10 +697,13 @@ __global__ void __launch_bounds__(kThreads, 6) preference_token_kernel(const __g
     Cursor c;
     c.at(a.q, begin, lane);
     float coef = inv > 0.0 ? (float)(__ldg(a.coef + c.s) * scale) : 0.0f;
+    Mask8 mask;
+    mask.read(a.mask, begin + lane * 8, stop, a.vec);
 #pragma unroll 1
     for (int base = begin; base < stop; base += kBlock) {
         const int k = base + lane * 8, hi = min(base + kBlock, stop);
-        const uint32_t valid = load_mask8(a.mask, k, hi, a.vec);
+        const uint32_t valid = mask.bits(k, hi);
+        mask.read(a.mask, k + kBlock, stop, a.vec);
         float out[8];
         zero8(out);
 #pragma unroll 1
@@ -667,11 +807,11 @@ extern "C" int hilore_policy_loss(const float *logp, const float *logp_old, cons
     a.log_low = std::log1p(-t.clip_low), a.log_high = std::log1p(t.clip_high);
     a.dual = t.dual_clip != 0.0 ? t.dual_clip : INFINITY, a.log_dual = std::log(a.dual), a.cap = t.rollout_cap, a.beta = t.beta, a.adv_eps = t.adv_eps;
     const bool sequence_ratio = t.ratio == HILORE_RATIO_SEQUENCE, per_token = t.adv_per_token != 0;
-    a.sequence_mean = t.mean == HILORE_MEAN_SEQUENCES, a.k2 = t.kl == HILORE_KL_K2;
-    double widest = 0.0; // of the bounds: a ratio's logarithm and they are rounded to fp32 where they are compared first
+    a.sequence_mean = t.mean == HILORE_MEAN_SEQUENCES, a.k2 = t.kl == HILORE_KL_K2, a.dual_clip = t.dual_clip != 0.0;
+    double widest = 0.0;
     for (double b : {a.log_low, a.log_high, a.log_dual})
         if (std::isfinite(b) && std::fabs(b) > widest) widest = std::fabs(b);
-    a.near = (float)(widest * 0x1p-21 + 0x1p-126);
+    a.near = (float)(widest * 0x1p-21 + 0x1p-20); // sixteen roundings of a ratio, and the two of a difference as large as the bound
     a.vec = vectors({logp, logp_old, logp_ref, logp_rollout, per_token ? adv : nullptr, omega}, mask);
     unsigned char *ws = static_cast<unsigned char *>(workspace);
     a.pieces = pieces_of(workspace, w);
@@ -746,7 +886,10 @@ extern "C" int hilore_preference_loss(const float *logp, const float *logp_ref, 
     a.margin_reward = t.margin_reward, a.smoothing = t.smoothing, a.nll = t.nll, a.G = G, a.loss = t.loss, a.length_mean = t.length_mean;
     a.vec = vectors({logp, logp_ref, omega}, mask);
     a.groups = (int)(n_seq / G);
-    a.per_cta = G >= kThreads ? 1 : kThreads / G;
+    // sixteen pairs of 64-bit exponentials and logarithms in a row take 15 us: up to 32 threads share them, as far as a CTA's threads go
+    a.team = 1;
+    while (a.team < 32 && 2 * a.team <= G) a.team *= 2;
+    a.per_cta = G * a.team >= kThreads ? 1 : kThreads / (G * a.team);
     unsigned char *ws = static_cast<unsigned char *>(workspace);
     a.pieces = pieces_of(workspace, w);
     a.coef = reinterpret_cast<double *>(ws + w.coef);

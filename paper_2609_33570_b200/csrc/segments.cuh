@@ -274,6 +274,25 @@ __device__ __forceinline__ uint2 mask_bytes(const uint8_t *p, int k, int n)
         if (k + e < n) w[e >> 2] |= (uint32_t)p[k + e] << (8 * (e & 3));
     return make_uint2(w[0], w[1]);
 }
+// The mask of eight tokens in two steps: read, and, a while later, made bits, since nothing that follows in a warp's program starts before
+// the first step that needs what has been read.
+struct Mask8 {
+    uint2 bytes;
+    __device__ __forceinline__ void read(const uint8_t *p, int k, int hi, bool vec)
+    {
+        bytes = make_uint2(0u, 0u);
+        if (k >= hi) return;
+        if (p == nullptr) bytes = make_uint2(0x01010101u, 0x01010101u);
+        else if (vec && k + 8 <= hi) bytes = ld_global_64_stream(p + k);
+        else bytes = mask_bytes(p, k, hi);
+    }
+    __device__ __forceinline__ uint32_t bits(int k, int hi) const
+    {
+        const uint32_t v = mask_bits(bytes);
+        return k + 8 <= hi ? v : (k < hi ? v & ((1u << (hi - k)) - 1) : 0u);
+    }
+};
+
 // Bits of the tokens k .. k + 7 that lie in [lo, hi).
 __device__ __forceinline__ uint32_t range_bits(int k, int lo, int hi)
 {
