@@ -1,7 +1,12 @@
 // Losses on token log-probabilities with their gradients: the clipped policy loss and the preference loss.
+#include <cooperative_groups.h>
+
 #include <cmath>
+#include <cstdlib>
 
 #include "segments.cuh"
+
+namespace cg = cooperative_groups;
 
 namespace hilore {
 
@@ -94,16 +99,15 @@ struct SumArgs {
     const float *x, *minus; // a: sum of x - minus (or of x)
     const float *y, *less;  // b: sum of y - less (or of y); y may be x
     Pieces out;
+    unsigned *done; // opt: a counter that the next kernel wants at zero
     int vec;
 };
 
 // Sums of every sequence over its valid tokens.  X: whether there is a first sum, Y: 0 none, 1 of y - less, 2 of x.  A lane adds its tokens
 // of the current sequence; at the sequence's end, or the share's, the warp adds the lanes up.
-template <bool X, int Y> __global__ void __launch_bounds__(kThreads, kSumsPerSm) sequence_sums_kernel(const __grid_constant__ SumArgs a)
+template <bool X, int Y> __device__ __forceinline__ void sequence_sums(const SumArgs &a)
 {
     const int lane = threadIdx.x & 31, share = blockIdx.x * kWarps + (threadIdx.x >> 5);
-    grid_dependency_wait();
-    grid_dependency_release();
     const int live = a.q.live(), tokens = a.w.per_warp * kBlock;
     if ((int64_t)share * tokens >= live)
         return;
@@ -175,6 +179,14 @@ template <bool X, int Y> __global__ void __launch_bounds__(kThreads, kSumsPerSm)
     finish(false);
 }
 
+template <bool X, int Y> __global__ void __launch_bounds__(kThreads, kSumsPerSm) sequence_sums_kernel(const __grid_constant__ SumArgs a)
+{
+    grid_dependency_wait();
+    grid_dependency_release();
+    if (a.done && blockIdx.x == 0 && threadIdx.x == 0) *a.done = 0;
+    sequence_sums<X, Y>(a);
+}
+
 // Sums of a CTA's numbers into its slots, in a fixed order.
 __device__ __forceinline__ void put_stats(const double (&v)[kStats], double *slots)
 {
@@ -197,7 +209,7 @@ __device__ __forceinline__ double sum_slots(const double *partials, int ctas, in
 {
     double t = 0.0;
 #pragma unroll 4
-    for (int c = threadIdx.x & 31; c < ctas; c += 32) t += partials[(size_t)c * kStats + i];
+    for (int c = threadIdx.x & 31; c < ctas; c += 32) t += __ldcg(partials + (size_t)c * kStats + i);
     return warp_sum(t);
 }
 
@@ -252,7 +264,10 @@ struct PolicyArgs {
     int sequence_mean, k2, dual_clip, vec;
     Pieces pieces;
     double *partials;
-    float *omega;
+    unsigned *done;
+    float *stats, *omega;
+    SumArgs sums;
+    int cluster; // the call is one cluster, which begins with the sums itself
 };
 
 __device__ __forceinline__ double inverse_norm(const PolicyArgs &a)
@@ -278,6 +293,45 @@ template <int KL> __device__ __forceinline__ void kl_term(float e, bool k2, floa
     }
 }
 
+// stats: loss, policy term, KL term, share on flat branches, mean of old - new; by a whole CTA
+__device__ __forceinline__ void policy_stats(const double *partials, int ctas, double beta, float *stats)
+{
+    __shared__ double sums[kStats];
+    const int warp = threadIdx.x >> 5;
+    if (warp < kStats) {
+        const double t = sum_slots(partials, ctas, warp);
+        if ((threadIdx.x & 31) == 0) sums[warp] = t;
+    }
+    __syncthreads();
+    if (threadIdx.x < kStats) stats[threadIdx.x] = (float)(threadIdx.x == 0 ? (beta != 0.0 ? fma(beta, sums[2], sums[1]) : sums[1]) : sums[threadIdx.x]);
+}
+__global__ void __launch_bounds__(kThreads) policy_final_kernel(const double *partials, int ctas, double beta, float *stats)
+{
+    grid_dependency_wait();
+    grid_dependency_release();
+    policy_stats(partials, ctas, beta, stats);
+}
+
+// A CTA's numbers, and by the last CTA to come, or the first one of a cluster, the statistics (otherwise the kernel behind makes them).
+__device__ __forceinline__ void policy_hand_on(const PolicyArgs &a, const double (&v)[kStats])
+{
+    __shared__ bool last;
+    put_stats(v, a.partials + (size_t)blockIdx.x * kStats);
+    if (a.cluster) {
+        cg::this_cluster().sync();
+        if (blockIdx.x == 0) policy_stats(a.partials, gridDim.x, a.beta, a.stats);
+    } else if (a.done) {
+        __threadfence();
+        __syncthreads();
+        if (threadIdx.x == 0) last = atomicAdd(a.done, 1u) == gridDim.x - 1;
+        __syncthreads();
+        if (last) {
+            __threadfence();
+            policy_stats(a.partials, gridDim.x, a.beta, a.stats);
+        }
+    }
+}
+
 // Ratios of tokens.  SEQ: there is something to a sequence, its weight or its advantage.  Which side of a bound a ratio is on is decided in
 // fp32 but for the few next to it.  What a sum has in common (1 / N, signs) is multiplied in at its end.
 template <bool SEQ, int KL, bool ROLLOUT, bool PER_TOKEN> __global__ void __launch_bounds__(kThreads, kPerSm) policy_token_kernel(const __grid_constant__ PolicyArgs a)
@@ -285,6 +339,10 @@ template <bool SEQ, int KL, bool ROLLOUT, bool PER_TOKEN> __global__ void __laun
     const int lane = threadIdx.x & 31, share = blockIdx.x * kWarps + (threadIdx.x >> 5);
     grid_dependency_wait();
     grid_dependency_release();
+    if (SEQ && a.cluster && a.sequence_mean) {
+        sequence_sums<false, 0>(a.sums);
+        cg::this_cluster().sync();
+    }
     const int live = a.q.live(), tokens = a.w.per_warp * kBlock;
     const double inv = inverse_norm(a);
     double v[kStats] = {};
@@ -469,7 +527,7 @@ template <bool SEQ, int KL, bool ROLLOUT, bool PER_TOKEN> __global__ void __laun
     }
 #pragma unroll
     for (int i = 1; i < kStats; ++i) v[i] *= inv;
-    put_stats(v, a.partials + (size_t)blockIdx.x * kStats);
+    policy_hand_on(a, v);
 }
 
 // Ratios of whole sequences: of a sequence the policy term's gradient is the same for every token.  The share that holds a sequence's
@@ -479,6 +537,11 @@ template <int KL> __global__ void __launch_bounds__(kThreads, kPerSm) policy_seq
     const int lane = threadIdx.x & 31, share = blockIdx.x * kWarps + (threadIdx.x >> 5);
     grid_dependency_wait();
     grid_dependency_release();
+    if (a.cluster) {
+        if (a.rollout) sequence_sums<true, 1>(a.sums);
+        else sequence_sums<true, 0>(a.sums);
+        cg::this_cluster().sync();
+    }
     const int live = a.q.live(), tokens = a.w.per_warp * kBlock;
     const double inv = inverse_norm(a), g = a.grad_loss ? (double)*a.grad_loss : 1.0;
     double v[kStats] = {};
@@ -548,22 +611,7 @@ template <int KL> __global__ void __launch_bounds__(kThreads, kPerSm) policy_seq
             else store8(a.omega, k, base, hi, a.vec, out);
         }
     }
-    put_stats(v, a.partials + (size_t)blockIdx.x * kStats);
-}
-
-// stats: loss, policy term, KL term, share on flat branches, mean of old - new
-__global__ void __launch_bounds__(kThreads) policy_final_kernel(const double *partials, int ctas, double beta, float *stats)
-{
-    __shared__ double sums[kStats];
-    grid_dependency_wait();
-    grid_dependency_release();
-    const int warp = threadIdx.x >> 5;
-    if (warp < kStats) {
-        const double t = sum_slots(partials, ctas, warp);
-        if ((threadIdx.x & 31) == 0) sums[warp] = t;
-    }
-    __syncthreads();
-    if (threadIdx.x < kStats) stats[threadIdx.x] = (float)(threadIdx.x == 0 ? (beta != 0.0 ? fma(beta, sums[2], sums[1]) : sums[1]) : sums[threadIdx.x]);
+    policy_hand_on(a, v);
 }
 
 // ------------------------------------------------------------------ preference loss
@@ -582,19 +630,19 @@ struct PreferenceArgs {
     float *scores, *stats;
     int64_t *pairs;
     float *omega;
+    SumArgs sums;
+    int cluster; // the call is one cluster, which does everything
 };
 
 // A CTA takes `per_cta` whole groups at a time: scores of their sequences into shared memory, then each sequence against the
 // others of its group.
-__global__ void __launch_bounds__(kThreads) preference_pairs_kernel(const __grid_constant__ PreferenceArgs a)
+__device__ __forceinline__ void preference_pairs(const PreferenceArgs &a)
 {
     extern __shared__ double smem[];
     const int room = a.per_cta * a.G;
     double *h = smem, *like = smem + room;             // score, mean log-probability
     double *per = smem + 2 * room;                     // 1 / |T| (0: no valid token)
     float *R = reinterpret_cast<float *>(smem + 3 * room);
-    grid_dependency_wait();
-    grid_dependency_release();
     double v[kStats] = {}; // loss, right order, gap, nll, pairs
     for (int64_t first = (int64_t)blockIdx.x * a.per_cta; first < a.groups; first += (int64_t)gridDim.x * a.per_cta) {
         const int n = (int)(a.groups - first < a.per_cta ? a.groups - first : a.per_cta) * a.G;
@@ -667,14 +715,27 @@ __global__ void __launch_bounds__(kThreads) preference_pairs_kernel(const __grid
     put_stats(v, a.partials + (size_t)blockIdx.x * kStats);
 }
 
+__global__ void __launch_bounds__(kThreads) preference_pairs_kernel(const __grid_constant__ PreferenceArgs a)
+{
+    grid_dependency_wait();
+    grid_dependency_release();
+    preference_pairs(a);
+}
+
 // The gradient of a sequence to each of its valid tokens.  Every CTA adds up the pairs of the CTAs before for the division by N; the first
 // one writes the statistics: loss, share of pairs in the right order, mean gap of the scores, mean -log-probability per token of the winners.
-__global__ void __launch_bounds__(kThreads, 6) preference_token_kernel(const __grid_constant__ PreferenceArgs a)
+__global__ void __launch_bounds__(kThreads, 4) preference_token_kernel(const __grid_constant__ PreferenceArgs a)
 {
     __shared__ double sums[kStats];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, share = blockIdx.x * kWarps + warp;
     grid_dependency_wait();
     grid_dependency_release();
+    if (a.cluster) {
+        sequence_sums<true, 2>(a.sums);
+        cg::this_cluster().sync();
+        preference_pairs(a);
+        cg::this_cluster().sync();
+    }
     const bool count = !a.N_dev && !(a.N > 0.0);
     if (blockIdx.x == 0 ? warp < kStats : (count && warp == kStats - 1)) {
         const double t = sum_slots(a.partials, a.ctas, warp);
@@ -696,7 +757,7 @@ __global__ void __launch_bounds__(kThreads, 6) preference_token_kernel(const __g
     const int begin = share * tokens, stop = min(live - begin, tokens) + begin;
     Cursor c;
     c.at(a.q, begin, lane);
-    float coef = inv > 0.0 ? (float)(__ldg(a.coef + c.s) * scale) : 0.0f;
+    float coef = inv > 0.0 ? (float)(__ldcg(a.coef + c.s) * scale) : 0.0f;
     Mask8 mask;
     mask.read(a.mask, begin + lane * 8, stop, a.vec);
 #pragma unroll 1
@@ -714,7 +775,7 @@ __global__ void __launch_bounds__(kThreads, 6) preference_token_kernel(const __g
             if (c.end > hi || c.end >= stop) break;
             lo = c.end;
             c.on(a.q, lo, lane);
-            coef = inv > 0.0 ? (float)(__ldg(a.coef + c.s) * scale) : 0.0f;
+            coef = inv > 0.0 ? (float)(__ldcg(a.coef + c.s) * scale) : 0.0f;
             if (lo >= hi) break;
         }
         if (a.vec && hi - base == kBlock) store8(a.omega + k, out);
@@ -736,10 +797,48 @@ static unsigned ctas_of(const Share &w)
     return (unsigned)((warps + kWarps - 1) / kWarps);
 }
 
+// A call of up to kClusterBlocks blocks is one launch: its CTAs are a thread-block cluster, which goes from one step to the next by a barrier.
+constexpr int kCluster = 8;                              // CTAs that any device grants
+constexpr int64_t kClusterBlocks = 2 * kCluster * kWarps; // two blocks of a warp at most
+static bool clusters_on()
+{
+    const char *off = std::getenv("HILORE_DISABLE_CLUSTER_LAUNCH");
+    return off == nullptr || off[0] == '\0' || (off[0] == '0' && off[1] == '\0');
+}
+static bool one_cluster(int64_t n_tok) { return n_tok > 0 && (n_tok + kBlock - 1) / kBlock <= kClusterBlocks && clusters_on(); }
+static Share cluster_share(int64_t n_tok)
+{
+    const int64_t blocks = (n_tok + kBlock - 1) / kBlock;
+    return Share{(int)blocks, blocks <= kCluster * kWarps ? 1 : 2};
+}
+static unsigned cluster_of(const Share &w) // CTAs beyond the last share have nothing to do
+{
+    unsigned n = 1;
+    while (n < ctas_of(w)) n *= 2;
+    return n;
+}
+template <typename A> static cudaError_t launch_cluster(void (*kernel)(A), unsigned ctas, size_t smem, cudaStream_t st, const A &a)
+{
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(ctas);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = ctas;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kernel, a);
+}
+
 // Layout of a workspace: the CTAs' slots, the pieces of shares and sequences, a number per sequence.
 constexpr int64_t kMostShares = 148 * 8 * kWarps; // on any device that this runs on, with up to eight CTAs of it on an SM
 struct Workspace {
-    size_t partials, head, tail, whole, coef, bytes;
+    size_t partials, done, head, tail, whole, coef, bytes;
 };
 static Workspace layout(int64_t n_seq, int64_t n_tok)
 {
@@ -747,8 +846,8 @@ static Workspace layout(int64_t n_seq, int64_t n_tok)
     const int64_t blocks = n_tok > 0 ? (n_tok + kBlock - 1) / kBlock : 0;
     const size_t shares = (size_t)(blocks < kMostShares ? blocks : kMostShares), S = n_seq > 0 ? (size_t)n_seq : 0;
     w.partials = 0;
-    w.head = w.partials + sizeof(double) * kStats * kMostCtas + 16;
-    w.head -= w.head % 16;
+    w.done = w.partials + sizeof(double) * kStats * kMostCtas;
+    w.head = w.done + 16;
     w.tail = w.head + sizeof(Piece) * shares;
     w.whole = w.tail + sizeof(Piece) * shares;
     w.coef = w.whole + sizeof(Piece) * S;
@@ -818,37 +917,50 @@ extern "C" int hilore_policy_loss(const float *logp, const float *logp_old, cons
     a.partials = reinterpret_cast<double *>(ws + w.partials);
     a.omega = omega;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    unsigned ctas = 0;
-    if (n_tok > 0 && (sequence_ratio || a.sequence_mean)) {
-        SumArgs s{};
-        s.q = a.q, s.w = share_of(n_tok, kSumsPerSm), s.mask = mask, s.vec = a.vec;
-        s.out = a.pieces;
+    a.stats = stats;
+    if (n_tok == 0)
+        return launch_dependent(policy_final_kernel, dim3(1), dim3(kThreads), 0, st, (const double *)a.partials, 0, a.beta, stats) == cudaSuccess &&
+                       cudaGetLastError() == cudaSuccess
+                   ? HILORE_OK
+                   : HILORE_CUDA;
+    const int kl = !logp_ref ? kNoKl : (t.kl == HILORE_KL_K3 ? kK3 : kEasyKl);
+    void (*kernel)(PolicyArgs) = nullptr;
+    if (sequence_ratio) {
+        kernel = kl == kNoKl ? policy_sequence_kernel<kNoKl> : (kl == kK3 ? policy_sequence_kernel<kK3> : policy_sequence_kernel<kEasyKl>);
+    } else {
+#define HILORE_KLS(SEQ, ROLL, PER) {policy_token_kernel<SEQ, kNoKl, ROLL, PER>, policy_token_kernel<SEQ, kEasyKl, ROLL, PER>, policy_token_kernel<SEQ, kK3, ROLL, PER>}
+        static void (*const kernels[3][2][3])(PolicyArgs) = {{HILORE_KLS(false, false, true), HILORE_KLS(false, true, true)},
+                                                             {HILORE_KLS(true, false, true), HILORE_KLS(true, true, true)},
+                                                             {HILORE_KLS(true, false, false), HILORE_KLS(true, true, false)}};
+#undef HILORE_KLS
+        kernel = kernels[!per_token ? 2 : (a.sequence_mean ? 1 : 0)][logp_rollout != nullptr][kl];
+    }
+    SumArgs &s = a.sums;
+    s.q = a.q, s.mask = mask, s.vec = a.vec, s.out = a.pieces;
+    if (sequence_ratio) s.x = logp, s.minus = logp_old;
+    if (sequence_ratio && logp_rollout) s.y = logp_old, s.less = logp_rollout;
+    if (one_cluster(n_tok)) {
+        a.w = s.w = cluster_share(n_tok);
         s.out.share = a.pieces.share = s.w.per_warp * kBlock;
-        if (sequence_ratio) s.x = logp, s.minus = logp_old;
-        if (sequence_ratio && logp_rollout) s.y = logp_old, s.less = logp_rollout;
+        a.cluster = 1;
+        if (launch_cluster(kernel, cluster_of(a.w), 0, st, a) == cudaSuccess)
+            return HILORE_OK;
+        (void)cudaGetLastError(); // refused: the launches below
+        a.cluster = 0;
+    }
+    s.w = share_of(n_tok, kSumsPerSm);
+    s.out.share = a.pieces.share = s.w.per_warp * kBlock;
+    if (sequence_ratio || a.sequence_mean) {
+        a.done = s.done = reinterpret_cast<unsigned *>(ws + w.done);
         void (*const sums)(SumArgs) = !sequence_ratio ? sequence_sums_kernel<false, 0> : (logp_rollout ? sequence_sums_kernel<true, 1> : sequence_sums_kernel<true, 0>);
         if (launch_dependent(sums, dim3(ctas_of(s.w)), dim3(kThreads), 0, st, s) != cudaSuccess)
             return HILORE_CUDA;
     }
-    if (n_tok > 0) {
-        a.w = share_of(n_tok, kPerSm);
-        ctas = ctas_of(a.w);
-        const int kl = !logp_ref ? kNoKl : (t.kl == HILORE_KL_K3 ? kK3 : kEasyKl);
-        void (*kernel)(PolicyArgs) = nullptr;
-        if (sequence_ratio) {
-            kernel = kl == kNoKl ? policy_sequence_kernel<kNoKl> : (kl == kK3 ? policy_sequence_kernel<kK3> : policy_sequence_kernel<kEasyKl>);
-        } else {
-#define HILORE_KLS(SEQ, ROLL, PER) {policy_token_kernel<SEQ, kNoKl, ROLL, PER>, policy_token_kernel<SEQ, kEasyKl, ROLL, PER>, policy_token_kernel<SEQ, kK3, ROLL, PER>}
-            static void (*const kernels[3][2][3])(PolicyArgs) = {{HILORE_KLS(false, false, true), HILORE_KLS(false, true, true)},
-                                                                 {HILORE_KLS(true, false, true), HILORE_KLS(true, true, true)},
-                                                                 {HILORE_KLS(true, false, false), HILORE_KLS(true, true, false)}};
-#undef HILORE_KLS
-            kernel = kernels[!per_token ? 2 : (a.sequence_mean ? 1 : 0)][logp_rollout != nullptr][kl];
-        }
-        if (launch_dependent(kernel, dim3(ctas), dim3(kThreads), 0, st, a) != cudaSuccess)
-            return HILORE_CUDA;
-    }
-    if (launch_dependent(policy_final_kernel, dim3(1), dim3(kThreads), 0, st, (const double *)a.partials, (int)ctas, a.beta, stats) != cudaSuccess)
+    a.w = share_of(n_tok, kPerSm);
+    const unsigned ctas = ctas_of(a.w);
+    if (launch_dependent(kernel, dim3(ctas), dim3(kThreads), 0, st, a) != cudaSuccess)
+        return HILORE_CUDA;
+    if (!a.done && launch_dependent(policy_final_kernel, dim3(1), dim3(kThreads), 0, st, (const double *)a.partials, (int)ctas, a.beta, stats) != cudaSuccess)
         return HILORE_CUDA;
     return cudaGetLastError() == cudaSuccess ? HILORE_OK : HILORE_CUDA;
 }
@@ -896,21 +1008,29 @@ extern "C" int hilore_preference_loss(const float *logp, const float *logp_ref, 
     a.partials = reinterpret_cast<double *>(ws + w.partials);
     a.scores = scores, a.stats = stats, a.pairs = pairs, a.omega = omega;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (n_tok > 0) {
-        SumArgs s{};
-        s.q = a.q, s.w = share_of(n_tok, kSumsPerSm), s.mask = mask, s.vec = a.vec, s.x = logp, s.minus = logp_ref;
-        s.out = a.pieces;
+    const size_t smem = (size_t)a.per_cta * G * (3 * sizeof(double) + sizeof(float));
+    SumArgs &s = a.sums;
+    s.q = a.q, s.mask = mask, s.vec = a.vec, s.x = logp, s.minus = logp_ref, s.out = a.pieces;
+    if (one_cluster(n_tok)) {
+        a.w = s.w = cluster_share(n_tok);
         s.out.share = a.pieces.share = s.w.per_warp * kBlock;
-        if (launch_dependent(sequence_sums_kernel<true, 2>, dim3(ctas_of(s.w)), dim3(kThreads), 0, st, s) != cudaSuccess)
-            return HILORE_CUDA;
+        a.cluster = 1;
+        a.ctas = (int)cluster_of(a.w);
+        if (launch_cluster(preference_token_kernel, (unsigned)a.ctas, smem, st, a) == cudaSuccess)
+            return HILORE_OK;
+        (void)cudaGetLastError(); // refused: the launches below
+        a.cluster = a.ctas = 0;
     }
+    s.w = share_of(n_tok, kSumsPerSm);
+    s.out.share = a.pieces.share = s.w.per_warp * kBlock;
+    if (n_tok > 0 && launch_dependent(sequence_sums_kernel<true, 2>, dim3(ctas_of(s.w)), dim3(kThreads), 0, st, s) != cudaSuccess)
+        return HILORE_CUDA;
     if (a.groups > 0) {
         a.ctas = grid_of((a.groups + a.per_cta - 1) / a.per_cta, kMostCtas);
-        const size_t smem = (size_t)a.per_cta * G * (3 * sizeof(double) + sizeof(float));
         if (launch_dependent(preference_pairs_kernel, dim3((unsigned)a.ctas), dim3(kThreads), smem, st, a) != cudaSuccess)
             return HILORE_CUDA;
     }
-    a.w = share_of(n_tok, 6);
+    a.w = share_of(n_tok, 4);
     if (launch_dependent(preference_token_kernel, dim3(n_tok > 0 ? ctas_of(a.w) : 1u), dim3(kThreads), 0, st, a) != cudaSuccess)
         return HILORE_CUDA;
     return cudaGetLastError() == cudaSuccess ? HILORE_OK : HILORE_CUDA;
