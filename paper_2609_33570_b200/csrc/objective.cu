@@ -112,8 +112,7 @@ template <bool X, int Y> __device__ __forceinline__ void sequence_sums(const Sum
     if ((int64_t)share * tokens >= live)
         return;
     const int begin = share * tokens, stop = min(live - begin, tokens) + begin;
-    Cursor c;
-    c.at(a.q, begin, lane);
+    Cursor c{0, 0x7FFFFFFF};
     Piece sum{0.0, 0.0, 0.0};
     int n = 0;
     auto finish = [&](bool ends) {
@@ -149,6 +148,7 @@ template <bool X, int Y> __device__ __forceinline__ void sequence_sums(const Sum
     };
     mask.read(a.mask, begin + lane * 8, stop, a.vec);
     ask(now, begin);
+    c.at(a.q, begin, lane); // while the first block is on its way
 #pragma unroll 1
     for (int base = begin; base < stop; base += kBlock) {
         const int k = base + lane * 8, hi = min(base + kBlock, stop);
@@ -157,7 +157,15 @@ template <bool X, int Y> __device__ __forceinline__ void sequence_sums(const Sum
 #pragma unroll 1
         for (int lo = base;;) { // the block's part of each sequence
             const uint32_t run = c.end >= hi && lo == base ? valid : valid & range_bits(k, lo, c.end);
-            if (__any_sync(kAll, run != 0)) {
+            if (__all_sync(kAll, run == 0xFFu)) {
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    if constexpr (X) sum.a += ((double)now.x[e] - (double)now.m[e]) + ((double)now.x[e + 1] - (double)now.m[e + 1]);
+                    if constexpr (Y == 1) sum.b += ((double)now.y[e] - (double)now.l[e]) + ((double)now.y[e + 1] - (double)now.l[e + 1]);
+                    if constexpr (Y == 2) sum.b += (double)now.x[e] + (double)now.x[e + 1];
+                }
+                n += 8;
+            } else if (__any_sync(kAll, run != 0)) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const bool in = run >> e & 1;
@@ -337,7 +345,8 @@ __device__ __forceinline__ void policy_hand_on(const PolicyArgs &a, const double
 template <bool SEQ, int KL, bool ROLLOUT, bool PER_TOKEN> __global__ void __launch_bounds__(kThreads, kPerSm) policy_token_kernel(const __grid_constant__ PolicyArgs a)
 {
     const int lane = threadIdx.x & 31, share = blockIdx.x * kWarps + (threadIdx.x >> 5);
-    grid_dependency_wait();
+    // behind the sums' launch, which waited for all before it, nothing but the sums has to be waited for
+    if (!a.done) grid_dependency_wait();
     grid_dependency_release();
     if (SEQ && a.cluster && a.sequence_mean) {
         sequence_sums<false, 0>(a.sums);
@@ -362,10 +371,6 @@ template <bool SEQ, int KL, bool ROLLOUT, bool PER_TOKEN> __global__ void __laun
             }
             if (!PER_TOKEN) A_of = (__ldg(a.adv + c.s) - mean) * scale;
         };
-        if (SEQ) {
-            c.at(a.q, begin, lane);
-            enter();
-        }
         Mask8 mask;
         mask.read(a.mask, begin + lane * 8, stop, a.vec);
 #pragma unroll 1
@@ -381,6 +386,11 @@ template <bool SEQ, int KL, bool ROLLOUT, bool PER_TOKEN> __global__ void __laun
                 if (PER_TOKEN) load8(a.adv, k, hi, a.vec, A);
             }
             mask.read(a.mask, k + kBlock, stop, a.vec);
+            if (SEQ && base == begin) { // while the first block is on its way
+                c.at(a.q, begin, lane);
+                if (a.done) grid_dependency_wait();
+                enter();
+            }
             zero8(out);
 #pragma unroll 1
             for (int lo = base;;) { // the block's part of each sequence
@@ -527,6 +537,7 @@ template <bool SEQ, int KL, bool ROLLOUT, bool PER_TOKEN> __global__ void __laun
     }
 #pragma unroll
     for (int i = 1; i < kStats; ++i) v[i] *= inv;
+    if (a.done) grid_dependency_wait(); // all threads, before anything is written
     policy_hand_on(a, v);
 }
 
@@ -535,7 +546,7 @@ template <bool SEQ, int KL, bool ROLLOUT, bool PER_TOKEN> __global__ void __laun
 template <int KL> __global__ void __launch_bounds__(kThreads, kPerSm) policy_sequence_kernel(const __grid_constant__ PolicyArgs a)
 {
     const int lane = threadIdx.x & 31, share = blockIdx.x * kWarps + (threadIdx.x >> 5);
-    grid_dependency_wait();
+    if (!a.done) grid_dependency_wait(); // as above
     grid_dependency_release();
     if (a.cluster) {
         if (a.rollout) sequence_sums<true, 1>(a.sums);
@@ -569,8 +580,6 @@ template <int KL> __global__ void __launch_bounds__(kThreads, kPerSm) policy_seq
                 v[4] -= weight * p.a;
             }
         };
-        c.at(a.q, begin, lane);
-        enter();
         Mask8 mask;
         mask.read(a.mask, begin + lane * 8, stop, a.vec);
 #pragma unroll 1
@@ -582,6 +591,11 @@ template <int KL> __global__ void __launch_bounds__(kThreads, kPerSm) policy_seq
             if (KL && valid) {
                 load8(a.logp, k, hi, a.vec, s);
                 load8(a.ref, k, hi, a.vec, r);
+            }
+            if (base == begin) {
+                c.at(a.q, begin, lane);
+                if (a.done) grid_dependency_wait();
+                enter();
             }
             zero8(out);
 #pragma unroll 1
@@ -611,6 +625,7 @@ template <int KL> __global__ void __launch_bounds__(kThreads, kPerSm) policy_seq
             else store8(a.omega, k, base, hi, a.vec, out);
         }
     }
+    if (a.done) grid_dependency_wait();
     policy_hand_on(a, v);
 }
 
@@ -632,6 +647,7 @@ struct PreferenceArgs {
     float *omega;
     SumArgs sums;
     int cluster; // the call is one cluster, which does everything
+    int behind;  // other launches of the call came first
 };
 
 // A CTA takes `per_cta` whole groups at a time: scores of their sequences into shared memory, then each sequence against the
@@ -728,7 +744,8 @@ __global__ void __launch_bounds__(kThreads, 4) preference_token_kernel(const __g
 {
     __shared__ double sums[kStats];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, share = blockIdx.x * kWarps + warp;
-    grid_dependency_wait();
+    // behind the other launches, which waited for all before them, nothing but their results has to be waited for
+    if (!a.behind) grid_dependency_wait();
     grid_dependency_release();
     if (a.cluster) {
         sequence_sums<true, 2>(a.sums);
@@ -736,6 +753,16 @@ __global__ void __launch_bounds__(kThreads, 4) preference_token_kernel(const __g
         preference_pairs(a);
         cg::this_cluster().sync();
     }
+    const int live = a.q.live(), tokens = a.w.per_warp * kBlock;
+    const bool some = (int64_t)share * tokens < live;
+    const int begin = some ? share * tokens : 0, stop = some ? min(live - begin, tokens) + begin : 0;
+    Cursor c{0, 0};
+    constexpr int kAhead = 4; // blocks whose masks are on their way: there is little else to do
+    Mask8 mask[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) mask[i].read(a.mask, begin + i * kBlock + lane * 8, stop, a.vec);
+    if (some) c.at(a.q, begin, lane);
+    if (a.behind) grid_dependency_wait();
     const bool count = !a.N_dev && !(a.N > 0.0);
     if (blockIdx.x == 0 ? warp < kStats : (count && warp == kStats - 1)) {
         const double t = sum_slots(a.partials, a.ctas, warp);
@@ -751,35 +778,38 @@ __global__ void __launch_bounds__(kThreads, 4) preference_token_kernel(const __g
         a.stats[i] = none ? 0.0f : (float)((i == 0 ? sums[0] + (a.nll != 0.0 ? a.nll * sums[3] : 0.0) : sums[i]) * inv);
     }
     const double scale = inv * (a.grad_loss ? (double)*a.grad_loss : 1.0);
-    const int live = a.q.live(), tokens = a.w.per_warp * kBlock;
-    if ((int64_t)share * tokens >= live)
+    if (!some)
         return;
-    const int begin = share * tokens, stop = min(live - begin, tokens) + begin;
-    Cursor c;
-    c.at(a.q, begin, lane);
     float coef = inv > 0.0 ? (float)(__ldcg(a.coef + c.s) * scale) : 0.0f;
-    Mask8 mask;
-    mask.read(a.mask, begin + lane * 8, stop, a.vec);
 #pragma unroll 1
-    for (int base = begin; base < stop; base += kBlock) {
-        const int k = base + lane * 8, hi = min(base + kBlock, stop);
-        const uint32_t valid = mask.bits(k, hi);
-        mask.read(a.mask, k + kBlock, stop, a.vec);
-        float out[8];
-        zero8(out);
-#pragma unroll 1
-        for (int lo = base;;) {
-            const uint32_t run = c.end >= hi && lo == base ? valid : valid & range_bits(k, lo, c.end);
+    for (int first = begin; first < stop; first += kAhead * kBlock) {
+        uint32_t valids = 0;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) out[e] = run >> e & 1 ? coef : out[e];
-            if (c.end > hi || c.end >= stop) break;
-            lo = c.end;
-            c.on(a.q, lo, lane);
-            coef = inv > 0.0 ? (float)(__ldcg(a.coef + c.s) * scale) : 0.0f;
-            if (lo >= hi) break;
+        for (int i = 0; i < kAhead; ++i) {
+            const int k = first + i * kBlock + lane * 8;
+            valids |= mask[i].bits(k, stop) << (8 * i);
+            mask[i].read(a.mask, k + kAhead * kBlock, stop, a.vec);
         }
-        if (a.vec && hi - base == kBlock) store8(a.omega + k, out);
-        else store8(a.omega, k, base, hi, a.vec, out);
+#pragma unroll 1
+        for (int base = first; base < min(first + kAhead * kBlock, stop); base += kBlock, valids >>= 8) {
+            const int k = base + lane * 8, hi = min(base + kBlock, stop);
+            const uint32_t valid = valids & 0xFFu;
+            float out[8];
+            zero8(out);
+#pragma unroll 1
+            for (int lo = base;;) {
+                const uint32_t run = c.end >= hi && lo == base ? valid : valid & range_bits(k, lo, c.end);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) out[e] = run >> e & 1 ? coef : out[e];
+                if (c.end > hi || c.end >= stop) break;
+                lo = c.end;
+                c.on(a.q, lo, lane);
+                coef = inv > 0.0 ? (float)(__ldcg(a.coef + c.s) * scale) : 0.0f;
+                if (lo >= hi) break;
+            }
+            if (a.vec && hi - base == kBlock) store8(a.omega + k, out);
+            else store8(a.omega, k, base, hi, a.vec, out);
+        }
     }
 }
 
@@ -1030,6 +1060,7 @@ extern "C" int hilore_preference_loss(const float *logp, const float *logp_ref, 
         if (launch_dependent(preference_pairs_kernel, dim3((unsigned)a.ctas), dim3(kThreads), smem, st, a) != cudaSuccess)
             return HILORE_CUDA;
     }
+    a.behind = n_tok > 0 && a.groups > 0;
     a.w = share_of(n_tok, 4);
     if (launch_dependent(preference_token_kernel, dim3(n_tok > 0 ? ctas_of(a.w) : 1u), dim3(kThreads), 0, st, a) != cudaSuccess)
         return HILORE_CUDA;
