@@ -195,30 +195,40 @@ template <bool X, int Y> __global__ void __launch_bounds__(kThreads, kSumsPerSm)
     sequence_sums<X, Y>(a);
 }
 
-// Sums of a CTA's numbers into its slots, in a fixed order.
-__device__ __forceinline__ void put_stats(const double (&v)[kStats], double *slots)
+// A CTA's numbers added up over its threads, in a fixed order: number i in every thread's copy of `sums`, which is in shared memory.
+template <int FIRST> __device__ __forceinline__ void sum_threads(const double (&v)[kStats], double (&sums)[kStats])
 {
     __shared__ double sh[kStats][kWarps];
 #pragma unroll
-    for (int i = 0; i < kStats; ++i) {
+    for (int i = FIRST; i < kStats; ++i) {
         const double t = warp_sum(v[i]);
         if ((threadIdx.x & 31) == 0) sh[i][threadIdx.x >> 5] = t;
     }
     __syncthreads();
-    if (threadIdx.x < kStats) {
+    if ((int)threadIdx.x >= FIRST && threadIdx.x < kStats) {
         double t = 0.0;
         for (int w = 0; w < kWarps; ++w) t += sh[threadIdx.x][w];
-        slots[threadIdx.x] = t;
+        sums[threadIdx.x] = t;
     }
+    __syncthreads();
 }
 
-// The sum over the CTAs' slots, number `i` of it in every lane.
-__device__ __forceinline__ double sum_slots(const double *partials, int ctas, int i)
+// Into the CTA's slots.
+__device__ __forceinline__ void put_stats(const double (&v)[kStats], double *slots)
 {
-    double t = 0.0;
-#pragma unroll 4
-    for (int c = threadIdx.x & 31; c < ctas; c += 32) t += __ldcg(partials + (size_t)c * kStats + i);
-    return warp_sum(t);
+    __shared__ double sums[kStats];
+    sum_threads<0>(v, sums);
+    if (threadIdx.x < kStats) slots[threadIdx.x] = sums[threadIdx.x];
+}
+
+// The sums over the CTAs' slots, of the numbers from FIRST on.
+template <int FIRST> __device__ __forceinline__ void sum_slots(const double *partials, int ctas, double (&sums)[kStats])
+{
+    double v[kStats] = {};
+    for (int c = threadIdx.x; c < ctas; c += kThreads)
+#pragma unroll
+        for (int i = FIRST; i < kStats; ++i) v[i] += __ldcg(partials + (size_t)c * kStats + i);
+    sum_threads<FIRST>(v, sums);
 }
 
 // ------------------------------------------------------------------ policy loss
@@ -305,12 +315,7 @@ template <int KL> __device__ __forceinline__ void kl_term(float e, bool k2, floa
 __device__ __forceinline__ void policy_stats(const double *partials, int ctas, double beta, float *stats)
 {
     __shared__ double sums[kStats];
-    const int warp = threadIdx.x >> 5;
-    if (warp < kStats) {
-        const double t = sum_slots(partials, ctas, warp);
-        if ((threadIdx.x & 31) == 0) sums[warp] = t;
-    }
-    __syncthreads();
+    sum_slots<0>(partials, ctas, sums);
     if (threadIdx.x < kStats) stats[threadIdx.x] = (float)(threadIdx.x == 0 ? (beta != 0.0 ? fma(beta, sums[2], sums[1]) : sums[1]) : sums[threadIdx.x]);
 }
 __global__ void __launch_bounds__(kThreads) policy_final_kernel(const double *partials, int ctas, double beta, float *stats)
@@ -764,11 +769,8 @@ __global__ void __launch_bounds__(kThreads, 4) preference_token_kernel(const __g
     if (some) c.at(a.q, begin, lane);
     if (a.behind) grid_dependency_wait();
     const bool count = !a.N_dev && !(a.N > 0.0);
-    if (blockIdx.x == 0 ? warp < kStats : (count && warp == kStats - 1)) {
-        const double t = sum_slots(a.partials, a.ctas, warp);
-        if (lane == 0) sums[warp] = t;
-    }
-    if (blockIdx.x == 0 || count) __syncthreads();
+    if (blockIdx.x == 0) sum_slots<0>(a.partials, a.ctas, sums);
+    else if (count) sum_slots<kStats - 1>(a.partials, a.ctas, sums);
     const double N = a.N_dev ? (double)*a.N_dev : (count ? sums[kStats - 1] : a.N);
     const double inv = N > 0.0 ? 1.0 / N : 0.0;
     if (blockIdx.x == 0 && threadIdx.x < 4) {
@@ -1028,9 +1030,9 @@ extern "C" int hilore_preference_loss(const float *logp, const float *logp_ref, 
     a.margin_reward = t.margin_reward, a.smoothing = t.smoothing, a.nll = t.nll, a.G = G, a.loss = t.loss, a.length_mean = t.length_mean;
     a.vec = vectors({logp, logp_ref, omega}, mask);
     a.groups = (int)(n_seq / G);
-    // sixteen pairs of 64-bit exponentials and logarithms in a row take 15 us: up to 32 threads share them, as far as a CTA's threads go
+    // Sixteen pairs in a row, of 64-bit exponentials and logarithms, take 15 us: threads share them as long as all of them run at once.
     a.team = 1;
-    while (a.team < 32 && 2 * a.team <= G) a.team *= 2;
+    while (a.team < 32 && 2 * a.team <= G && 2 * a.team * n_seq <= (int64_t)sm_count() * 4 * kThreads) a.team *= 2;
     a.per_cta = G * a.team >= kThreads ? 1 : kThreads / (G * a.team);
     unsigned char *ws = static_cast<unsigned char *>(workspace);
     a.pieces = pieces_of(workspace, w);
