@@ -571,8 +571,11 @@ int hilore_adamw_step(const hilore_param *params_dev, const hilore_param *params
  *   mask         opt [n_tok] u8 (0 / not 0); NULL: every token is valid.  Masked tokens (prompt, tool outputs, padding) may
  *                hold anything, NaN included: they change nothing and their outputs are 0.
  *   Tensors with an entry per token may have any address that their type allows; with fp32 at 32, bf16 at 16 and masks at 8
- *   bytes eight tokens move at a time.  Results do not depend on that, nor on scheduling; a sequence's results do not depend
- *   on the other sequences.  n_seq and n_tok at most 2^31 - 2^16 (HILORE_SHAPE).
+ *   bytes eight tokens move at a time.  Results do not depend on that, nor on scheduling: the same call gives the same bits.
+ *   Where in a call a sequence lies decides in which order sums are added up, all of them in fp64: its results may differ in a
+ *   last bit, no more, with the sequences around it.  n_seq and n_tok at most 2^31 - 2^16 (HILORE_SHAPE).
+ *   Small policy and preference losses (up to 32768 tokens) are one thread-block cluster; HILORE_DISABLE_CLUSTER_LAUNCH=1 in the
+ *   environment makes them several launches.
  *   workspace    the bytes of the call's .._workspace_bytes, 16-byte aligned, overwritten.
  * ================================================================================================================ */
 

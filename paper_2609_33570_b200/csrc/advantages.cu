@@ -677,6 +677,7 @@ __global__ void __launch_bounds__(kGradThreads, TRACE || BY_TRACE ? 5 : 8) advan
     if (!MAPS && a.second)
         st = behind_pieces<Op>(st, begin <= b ? 0 : (a.even ? chunk - b / a.chunk : (begin - b) >> a.piece), lane,
                                [&](int i) { return static_cast<const Op::Map *>(a.maps)[a.even ? b / a.chunk + i : (b + ((int64_t)i << a.piece)) / a.chunk]; }, w_before);
+    if (BY_TRACE && (uint32_t)st.pos >= (uint32_t)live) st.pos = -1; // boundaries out of order: a map that nobody made
     // The current sequence's last gradient, then on to the one that holds token `to`; those between without a token get zeros.
     auto next_sequence = [&](int to) {
         if (lane == 0) {

@@ -1,6 +1,7 @@
 // Losses on token log-probabilities with their gradients: the clipped policy loss and the preference loss.
 #include <cooperative_groups.h>
 
+#include <cfloat>
 #include <cmath>
 #include <cstdlib>
 
@@ -264,7 +265,7 @@ constexpr float kNear = 80.0f;
 // order that of what the rounding and the second part leave.
 __device__ __forceinline__ float exp_near(float d)
 {
-    constexpr float kLog2e = 1.44269502162933349609375f, kRest = 1.925963033500011079e-8f, kLn2 = 0.693147180559945309f;
+    constexpr float kLog2e = 1.44269502162933349609375f, kRest = 1.92596299112661747e-8f, kLn2 = 0.693147180559945309f;
     const float t = d * kLog2e, rest = fmaf(d, kRest, fmaf(d, kLog2e, -t));
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(t));
@@ -364,6 +365,7 @@ template <bool SEQ, int KL, bool ROLLOUT, bool PER_TOKEN> __global__ void __laun
         const int begin = share * tokens, stop = min(live - begin, tokens) + begin;
         const float g = a.grad_loss ? *a.grad_loss : 1.0f;
         const float mean = a.moments ? a.moments[0] : 0.0f, scale = a.moments ? (float)(1.0 / ((double)a.moments[1] + a.adv_eps)) : 1.0f;
+        const bool strange = !(fabsf(mean) <= FLT_MAX) || !(fabsf(scale) <= FLT_MAX); // then masked tokens must not go as zeros
         const float high = (float)a.log_high, low = (float)a.log_low, dual_log = (float)a.log_dual;
         const float most_up = (float)(1.0 + a.clip_high), most_down = (float)(1.0 - a.clip_low), dual = (float)a.dual, cap = (float)a.cap;
         const float beta = a.beta != 0.0 ? (float)(a.beta * inv * g) : 0.0f, slope_of = (float)(-inv * g);
@@ -414,14 +416,14 @@ template <bool SEQ, int KL, bool ROLLOUT, bool PER_TOKEN> __global__ void __laun
                                 if (PER_TOKEN) A[e] = mean;
                             }
                     }
-                    bool odd = false;
+                    bool odd = strange;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const float d = s[e] - o[e];
                         odd |= !(fabsf(d) <= kNear);
                         odd |= fminf(fabsf(d - high), fabsf(d - low)) <= a.near;
                         if (a.dual_clip) odd |= fabsf(d - dual_log) <= a.near;
-                        if (KL == kK3) odd |= !(fabsf(r[e] - s[e]) <= kLargest);
+                        if (KL) odd |= !(fabsf(r[e] - s[e]) <= (KL == kK3 ? kLargest : kNear));
                         if (ROLLOUT) odd |= !(fabsf(o[e] - b[e]) <= kNear);
                     }
                     plain = !__any_sync(kAll, odd);
@@ -449,8 +451,9 @@ template <bool SEQ, int KL, bool ROLLOUT, bool PER_TOKEN> __global__ void __laun
                             const float gain = x * rho;
                             float held = fminf(gain, x * fminf(fmaxf(rho, most_down), most_up));
                             if (a.dual_clip) held = x < 0.0f ? fmaxf(held, x * dual) : held;
-                            float grad = held != gain ? 0.0f : slope_of * gain;
-                            flats += held != gain ? 1.0f : 0.0f;
+                            const bool flat = held < gain || held > gain; // NaN stays
+                            float grad = flat ? 0.0f : slope_of * gain;
+                            flats += flat ? 1.0f : 0.0f;
                             term += held;
                             drift += d;
                             if (KL) {

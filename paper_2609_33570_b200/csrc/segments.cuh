@@ -1,5 +1,5 @@
-// Tokens of back-to-back sequences in tiles of 2048: which sequences a tile holds, where they end, and scans over a tile's
-// tokens that start anew at every sequence.  Shared by the kernels of objective.cu.
+// Tokens of back-to-back sequences: where sequences lie, accesses of eight neighbouring tokens a lane and of blocks of 256 a warp, masks,
+// and scans over the lanes of a warp.  Shared by advantages.cu and objective.cu.
 #pragma once
 
 #include <initializer_list>
@@ -7,11 +7,6 @@
 #include "common.cuh"
 
 namespace hilore {
-
-constexpr int kSegThreads = 256;             // threads of a CTA
-constexpr int kSegEach = 8;                  // consecutive tokens of a thread: one 256-bit access per fp32 tensor
-constexpr int kSegTile = kSegThreads * kSegEach;
-constexpr int kSegWarps = kSegThreads / 32;
 
 // The sequences of a call: packed with their boundaries, or rows of T slots (cu == nullptr).  Whatever `cu` holds, boundaries
 // lie in [0, n_tok]; tokens from bound(n_seq) on belong to no sequence.
@@ -74,37 +69,6 @@ struct Sequences {
     }
 };
 
-// What a CTA knows of its tile: tokens [lo, hi), sequences s0 .. s1 of them, and a bit for every token that ends its sequence.
-struct TileShared {
-    uint32_t ends[kSegTile / 32];
-    int s0, s1;
-};
-
-// All threads; `hi` > `lo`.  Ends with a barrier; a barrier must lie between a tile's last use of `sh` and the next call.
-__device__ __forceinline__ void tile_sequences(const Sequences &q, int lo, int hi, TileShared &sh)
-{
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    if (tid < kSegTile / 32)
-        sh.ends[tid] = 0;
-    if (warp == 2 || warp == 3) { // the first and the last sequence at the same time
-        const int s = q.owner_warp(warp == 2 ? lo : hi - 1, lane);
-        if (lane == 0) {
-            if (warp == 2) sh.s0 = s;
-            else sh.s1 = s;
-        }
-    }
-    __syncthreads();
-    for (int s = sh.s0 + tid; s <= sh.s1; s += kSegThreads) {
-        const int e = q.bound(s + 1) - 1 - lo;
-        if (e >= 0 && e < hi - lo)
-            atomicOr(&sh.ends[e >> 5], 1u << (e & 31));
-    }
-    __syncthreads();
-}
-
-// The end bits of the eight tokens of block `b` (0 .. 255) of the tile.
-__device__ __forceinline__ uint32_t block_ends(const TileShared &sh, int b) { return (sh.ends[b >> 2] >> (8 * (b & 3))) & 0xFFu; }
-
 // ---- a thread's eight tokens, from token k on; those at or beyond `hi` count as masked and read as zero ----
 __device__ __forceinline__ void load8(const float *p, int k, int hi, bool vec, float (&x)[8])
 {
@@ -119,46 +83,12 @@ __device__ __forceinline__ void load8(const float *p, int k, int hi, bool vec, f
     }
 }
 
-__device__ __forceinline__ void load8(const uint16_t *p, int k, int hi, bool vec, float (&x)[8]) // bf16
-{
-    if (vec && k + 8 <= hi) {
-        const uint4 w = ld_global_128_stream(p + k);
-        const uint32_t v[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            x[2 * e] = bf16_lo(v[e]);
-            x[2 * e + 1] = bf16_hi(v[e]);
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = k + e < hi ? __uint_as_float((uint32_t)p[k + e] << 16) : 0.0f;
-    }
-}
-
 // A bit for each of eight bytes that is not zero.
 __device__ __forceinline__ uint32_t mask_bits(uint2 w)
 {
     // the top bit of every byte that is not zero; these, 8 apart, gathered in four neighbouring bits
     const uint32_t a = (((w.x & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) | w.x) & 0x80808080u, b = (((w.y & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) | w.y) & 0x80808080u;
     return (a * 0x00204081u) >> 28 | ((b * 0x00204081u) >> 28) << 4;
-}
-
-__device__ __forceinline__ uint32_t load_mask8(const uint8_t *p, int k, int hi, bool vec)
-{
-    const int n = hi - k;
-    if (n <= 0)
-        return 0;
-    if (p == nullptr)
-        return n >= 8 ? 0xFFu : (1u << n) - 1;
-    uint32_t m = 0;
-    if (vec && n >= 8) {
-        m = mask_bits(ld_global_64_stream(p + k));
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e < n && p[k + e] != 0) m |= 1u << e;
-    }
-    return m;
 }
 
 __device__ __forceinline__ void zero8(float (&x)[8])
@@ -348,7 +278,7 @@ template <typename Op> __device__ __forceinline__ typename Op::Map warp_scan(typ
 }
 
 // ---- host side ----
-constexpr int64_t kMaxTokens = (int64_t(1) << 31) - (int64_t(1) << 16); // token numbers of a whole tile stay in 31 bits
+constexpr int64_t kMaxTokens = (int64_t(1) << 31) - (int64_t(1) << 16); // token numbers some blocks behind the last stay in 31 bits
 
 // The sequences of a call, or why there are none.
 inline int check_sequences(const int32_t *cu, int64_t n_seq, int64_t n_tok, Sequences &q)

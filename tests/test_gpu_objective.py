@@ -359,6 +359,32 @@ def test_policy_masked_tokens_may_hold_anything():
         check_policy(c, clean, t, 99)
 
 
+@pytest.mark.parametrize("mean", [0, 1])
+def test_policy_of_masked_tokens_whose_advantages_are_whitened_by_nothing(mean):
+    """A standard deviation of zero makes valid advantages infinite or NaN; where all are masked nothing may come of it."""
+    for per_token in (0, 1):
+        t = dict(TERMS, ratio=0, mean=mean, adv_per_token=per_token, adv_eps=0.0)
+        for white in ([0.5, 0.0], [np.nan, np.nan], [np.inf, 1.0]):
+            c = Call("across tiles", masked=1.0)
+            x = policy_inputs(c, t)
+            x["white"] = np.array(white, np.float32)
+            run_policy(c, x, t, 5)
+            assert not c.got("omega").any() and not c.got("stats").any()
+
+
+@pytest.mark.parametrize("mean", [0, 1])
+def test_policy_what_is_not_finite_shows(mean):
+    """A NaN advantage makes its own token's gradient NaN; a reference of -infinity without a KL weight nothing at all in the gradient."""
+    t = dict(TERMS, ratio=0, mean=mean, adv_per_token=1, beta=0.0, kl=2)
+    c = Call("across tiles", masked=None)
+    x = policy_inputs(c, t)
+    x["adv"][[77, 9100]] = np.nan
+    x["ref"][[5, 9200]] = -np.inf
+    run_policy(c, x, t, 99)
+    omega = c.got("omega")
+    assert np.flatnonzero(np.isnan(omega)).tolist() == [77, 9100] and np.isnan(c.got("stats")[:2]).all()
+
+
 @pytest.mark.parametrize("ratio,mean", [(0, 0), (0, 1), (1, 1)])
 def test_policy_of_nothing(ratio, mean):
     t = dict(TERMS, ratio=ratio, mean=mean)
@@ -615,6 +641,24 @@ def test_boundaries_of_any_content_stay_inside():
         run_backward(c, dict(ga=c.normal(), gr=None, adv=c.normal(), trace=None), 0.9, 0.9)
         for k in ("rewards", "trace", "outcome"):
             c.got(k)
+
+
+def test_boundaries_of_any_content_over_many_chunks_and_a_workspace_of_any_content():
+    """Maps of chunks that the boundaries leave unmade are whatever the workspace held: numbers, but no places."""
+    n = 60000
+    trace, adv, ga = (torch.rand(n, device="cuda") for _ in range(3))
+    for bad in ([0, 40000, 100, 59000], [0, 59999, 300, 60000], [9000, 3, 2 ** 31 - 1, 77], [0, -5, 50000, 600]):
+        ws = torch.full((api.hilore_advantages_workspace_bytes(n),), 0x7F, dtype=torch.uint8, device="cuda")
+        out = [G.Guarded(n * 4) for _ in range(3)]
+        per = [G.Guarded(3 * 4) for _ in range(2)]
+        cu = torch.tensor(bad, dtype=torch.int32, device="cuda")
+        api.hilore_advantages_backward(ga, None, adv, trace, None, cu, 3, n, 0.9, 0.9, out[0].ptr(), per[0].ptr(), out[1].ptr(), per[1].ptr(), out[2].ptr(),
+                                       ws, ws.numel())
+        torch.cuda.synchronize()
+        for g in out:
+            g.numpy(np.float32, (n,))
+        for g in per:
+            g.numpy(np.float32, (3,))
 
 
 def test_no_sequences_at_all():
