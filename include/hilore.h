@@ -574,8 +574,8 @@ int hilore_adamw_step(const hilore_param *params_dev, const hilore_param *params
  *   bytes eight tokens move at a time.  Results do not depend on that, nor on scheduling: the same call gives the same bits.
  *   Where in a call a sequence lies decides in which order sums are added up, all of them in fp64: its results may differ in a
  *   last bit, no more, with the sequences around it.  n_seq and n_tok at most 2^31 - 2^16 (HILORE_SHAPE).
- *   Small policy and preference losses (up to 32768 tokens) are one thread-block cluster; HILORE_DISABLE_CLUSTER_LAUNCH=1 in the
- *   environment makes them several launches.
+ *   Small policy losses (up to 16384 tokens, RATIO_TOKEN with MEAN_TOKENS) are one thread-block cluster, two launches with
+ *   HILORE_DISABLE_CLUSTER_LAUNCH set in the environment.
  *   workspace    the bytes of the call's .._workspace_bytes, 16-byte aligned, overwritten.
  * ================================================================================================================ */
 

@@ -1,6 +1,7 @@
 // Losses on token log-probabilities with their gradients: the clipped policy loss and the preference loss.
 #include <cooperative_groups.h>
 
+#include <algorithm>
 #include <cfloat>
 #include <cmath>
 #include <cstdlib>
@@ -14,7 +15,8 @@ namespace hilore {
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kPerSm = 2;            // CTAs of the policy kernels on an SM,
-constexpr int kSumsPerSm = 4;        // and of the sums'
+constexpr int kSumsPerSm = 4;        // of the sums',
+constexpr int kSumsPerSmOfFour = 2;  // and of those of four tensors, which need the registers
 constexpr int kStats = 5;            // sums that a CTA hands on
 constexpr int kMostCtas = 1024;      // that do so
 constexpr uint32_t kAll = 0xFFFFFFFFu;
@@ -35,14 +37,16 @@ struct Pieces {
     Piece *head, *tail, *whole;
     int share; // tokens
 
-    // By one thread.
-    __device__ __forceinline__ Piece total(const Sequences &q, int s) const
+    // By one thread, unless the sequence goes over more than `most` shares: then n is -1.
+    __device__ __forceinline__ Piece total(const Sequences &q, int s, int most = 0x7FFFFFFF) const
     {
         const int lo = q.bound(s), hi = q.bound(s + 1);
         if (hi <= lo) return Piece{0.0, 0.0, 0.0};
         const int t = lo / share, u = (hi - 1) / share;
         if (t == u) return whole[s];
+        if (u - t >= most) return Piece{0.0, 0.0, -1.0};
         Piece p = tail[t];
+#pragma unroll 4
         for (int i = t + 1; i <= u; ++i) {
             p.a += head[i].a;
             p.b += head[i].b;
@@ -58,6 +62,7 @@ struct Pieces {
         const int t = lo / share, u = (hi - 1) / share;
         if (t == u) return whole[s];
         Piece p{0.0, 0.0, 0.0};
+#pragma unroll 4
         for (int i = t + lane; i <= u; i += 32) {
             const Piece x = i == t ? tail[i] : head[i];
             p.a += x.a;
@@ -67,6 +72,10 @@ struct Pieces {
         return Piece{warp_sum(p.a), warp_sum(p.b), warp_sum(p.n)};
     }
 };
+
+// Sequences are walked one at a time by the whole warp, which takes 1 us each.  Where kMany or more end in a block, each lane walks those of its
+// own eight tokens, of all lanes at the same time: 16384 sequences of one token in 33 us instead of 620.
+constexpr int kMany = 4;
 
 // A warp's way through the sequences of its tokens: the current one, which holds the first token not yet passed, and its end.
 struct Cursor {
@@ -91,6 +100,50 @@ struct Cursor {
         }
         if (end <= token) end = 0x7FFFFFFF; // boundaries out of order
     }
+    // Whether kMany sequences or more end before token `hi`, from this one on, and then at least the last of those that do.
+    __device__ __forceinline__ bool many(const Sequences &q, int hi, int lane, int &last) const
+    {
+        const int64_t o = (int64_t)s + lane;
+        const uint32_t out = __ballot_sync(kAll, (o < q.n_seq ? q.bound((int)o + 1) : 0x7FFFFFFF) >= hi);
+        const int n = out ? __ffs(out) - 1 : 32;
+        last = out ? s + n : q.owner_warp(hi - 1, lane);
+        return n >= kMany;
+    }
+    // From here on every lane has a cursor of its own: on to the sequence of token k, no further than `last`.
+    __device__ __forceinline__ bool spread(const Sequences &q, int k, int last)
+    {
+        if (k < end) return false;
+        s = q.owner(k, s, last);
+        end = q.bound(s + 1);
+        if (end <= k) end = 0x7FFFFFFF;
+        return true;
+    }
+    __device__ __forceinline__ void next(const Sequences &q, int last) // by a lane: to the one that begins where this one ends
+    {
+        const int token = end;
+        if (s < last) ++s;
+        end = q.bound(s + 1);
+        if (end <= token) s = q.owner(token, s, last), end = q.bound(s + 1);
+        if (end <= token) end = 0x7FFFFFFF;
+    }
+    __device__ __forceinline__ void join(int from) // the cursor of lane `from`
+    {
+        s = __shfl_sync(kAll, s, from);
+        end = __shfl_sync(kAll, end, from);
+    }
+};
+
+// Sums since the last end of a sequence, if there is one.
+struct SumOp {
+    struct Map {
+        double a, b, n;
+        uint32_t flag, pad;
+    };
+    static __device__ __forceinline__ Map identity() { return Map{0.0, 0.0, 0.0, 0u, 0u}; }
+    static __device__ __forceinline__ Map then(const Map &a, const Map &b)
+    {
+        return b.flag ? b : Map{a.a + b.a, a.b + b.b, a.n + b.n, a.flag, 0u};
+    }
 };
 
 struct SumArgs {
@@ -106,8 +159,12 @@ struct SumArgs {
 
 // Sums of every sequence over its valid tokens.  X: whether there is a first sum, Y: 0 none, 1 of y - less, 2 of x.  A lane adds its tokens
 // of the current sequence; at the sequence's end, or the share's, the warp adds the lanes up.
-template <bool X, int Y> __device__ __forceinline__ void sequence_sums(const SumArgs &a)
+template <bool X, int Y>
+__global__ void __launch_bounds__(kThreads, Y == 1 ? kSumsPerSmOfFour : kSumsPerSm) sequence_sums_kernel(const __grid_constant__ SumArgs a)
 {
+    grid_dependency_wait();
+    grid_dependency_release();
+    if (a.done && blockIdx.x == 0 && threadIdx.x == 0) *a.done = 0;
     const int lane = threadIdx.x & 31, share = blockIdx.x * kWarps + (threadIdx.x >> 5);
     const int live = a.q.live(), tokens = a.w.per_warp * kBlock;
     if ((int64_t)share * tokens >= live)
@@ -155,6 +212,44 @@ template <bool X, int Y> __device__ __forceinline__ void sequence_sums(const Sum
         const int k = base + lane * 8, hi = min(base + kBlock, stop);
         const uint32_t valid = now.valid;
         ask(then, base + kBlock);
+        int last;
+        if (c.end < hi && c.many(a.q, hi, lane, last)) {
+            const Piece before{X ? warp_sum(sum.a) : 0.0, Y ? warp_sum(sum.b) : 0.0, (double)__reduce_add_sync(kAll, (unsigned)n)};
+            SumOp::Map mine = SumOp::identity(), first = mine, all; // since the last end in the lane's tokens; before the first
+            int s_first = 0;
+            if (k < hi) c.spread(a.q, k, last);
+#pragma unroll 1
+            for (int e = 0; k + e < hi && e < 8; ++e) { // read once more, as registers for it would cost all blocks
+                if (valid >> e & 1) {
+                    const double x = X ? (double)a.x[k + e] : 0.0;
+                    if (X) mine.a += a.minus ? x - (double)a.minus[k + e] : x;
+                    if (Y == 1) mine.b += (double)a.y[k + e] - (a.less ? (double)a.less[k + e] : 0.0);
+                    if (Y == 2) mine.b += x;
+                    mine.n += 1.0;
+                }
+                if (k + e + 1 < c.end) continue;
+                if (mine.flag) a.out.whole[c.s] = Piece{mine.a, mine.b, mine.n};
+                else first = mine, s_first = c.s;
+                mine = SumOp::Map{0.0, 0.0, 0.0, 1u, 0u};
+                if (e < 7 && k + e + 1 < hi) c.next(a.q, last);
+            }
+            __syncwarp();
+            SumOp::Map in = warp_scan<SumOp>(mine, lane, all);
+            if (!in.flag) in.a += before.a, in.b += before.b, in.n += before.n;
+            if (mine.flag) {
+                const Piece p{in.a + first.a, in.b + first.b, in.n + first.n};
+                if (a.q.bound(s_first) < begin) a.out.head[share] = p;
+                else a.out.whole[s_first] = p;
+            }
+            all = shfl_words(all, 31); // an end is in it
+            sum = lane == 0 ? Piece{all.a, all.b, 0.0} : Piece{0.0, 0.0, 0.0};
+            n = lane == 0 ? (int)all.n : 0;
+            c.join((hi - 1 - base) >> 3);
+            if (c.end <= hi) {
+                if (c.end >= stop) return;
+                c.on(a.q, hi, lane);
+            }
+        } else
 #pragma unroll 1
         for (int lo = base;;) { // the block's part of each sequence
             const uint32_t run = c.end >= hi && lo == base ? valid : valid & range_bits(k, lo, c.end);
@@ -186,14 +281,6 @@ template <bool X, int Y> __device__ __forceinline__ void sequence_sums(const Sum
         now = then;
     }
     finish(false);
-}
-
-template <bool X, int Y> __global__ void __launch_bounds__(kThreads, kSumsPerSm) sequence_sums_kernel(const __grid_constant__ SumArgs a)
-{
-    grid_dependency_wait();
-    grid_dependency_release();
-    if (a.done && blockIdx.x == 0 && threadIdx.x == 0) *a.done = 0;
-    sequence_sums<X, Y>(a);
 }
 
 // A CTA's numbers added up over its threads, in a fixed order: number i in every thread's copy of `sums`, which is in shared memory.
@@ -285,8 +372,7 @@ struct PolicyArgs {
     double *partials;
     unsigned *done;
     float *stats, *omega;
-    SumArgs sums;
-    int cluster; // the call is one cluster, which begins with the sums itself
+    int cluster; // the call is one cluster
 };
 
 __device__ __forceinline__ double inverse_norm(const PolicyArgs &a)
@@ -354,10 +440,6 @@ template <bool SEQ, int KL, bool ROLLOUT, bool PER_TOKEN> __global__ void __laun
     // behind the sums' launch, which waited for all before it, nothing but the sums has to be waited for
     if (!a.done) grid_dependency_wait();
     grid_dependency_release();
-    if (SEQ && a.cluster && a.sequence_mean) {
-        sequence_sums<false, 0>(a.sums);
-        cg::this_cluster().sync();
-    }
     const int live = a.q.live(), tokens = a.w.per_warp * kBlock;
     const double inv = inverse_norm(a);
     double v[kStats] = {};
@@ -371,13 +453,12 @@ template <bool SEQ, int KL, bool ROLLOUT, bool PER_TOKEN> __global__ void __laun
         const float beta = a.beta != 0.0 ? (float)(a.beta * inv * g) : 0.0f, slope_of = (float)(-inv * g);
         Cursor c{0, 0x7FFFFFFF};
         float w = 1.0f, A_of = 0.0f; // of the sequence: weight / inv, advantage
-        auto enter = [&]() {
-            if (a.sequence_mean) {
-                const Piece p = a.pieces.total_warp(a.q, c.s, lane);
-                w = p.n > 0.0 ? (float)(1.0 / p.n) : 0.0f;
-            }
+        auto entered = [&](double n) {
+            if (a.sequence_mean) w = n > 0.0 ? (float)(1.0 / n) : 0.0f;
             if (!PER_TOKEN) A_of = (__ldg(a.adv + c.s) - mean) * scale;
         };
+        auto enter = [&]() { entered(a.sequence_mean ? a.pieces.total_warp(a.q, c.s, lane).n : 0.0); };
+        auto enter_lane = [&]() { entered(a.sequence_mean ? a.pieces.total(a.q, c.s).n : 0.0); };
         Mask8 mask;
         mask.read(a.mask, begin + lane * 8, stop, a.vec);
 #pragma unroll 1
@@ -399,12 +480,15 @@ template <bool SEQ, int KL, bool ROLLOUT, bool PER_TOKEN> __global__ void __laun
                 enter();
             }
             zero8(out);
+            int last = 0;
+            const bool many = SEQ && c.end < hi && c.many(a.q, hi, lane, last);
+            if (many && k < hi && c.spread(a.q, k, last)) enter_lane();
 #pragma unroll 1
-            for (int lo = base;;) { // the block's part of each sequence
+            for (int lo = base;;) { // the block's, or the lane's, part of each sequence
                 const uint32_t run = !SEQ || (c.end >= hi && lo == base) ? valid : valid & range_bits(k, lo, c.end);
                 // Nearly always a block has one sequence, no ratio within rounding of a bound, and nothing far out: then masked tokens go as
                 // zeros, which add nothing to any sum, and the objective is the smaller of two products.
-                bool plain = !SEQ || (lo == base && c.end >= hi);
+                bool plain = !SEQ || (!many && lo == base && c.end >= hi);
                 if (plain) {
                     if (run != 0xFFu) {
 #pragma unroll
@@ -532,7 +616,18 @@ template <bool SEQ, int KL, bool ROLLOUT, bool PER_TOKEN> __global__ void __laun
                     v[3] += (double)(SEQ ? w * (float)flats : (float)flats);
                     v[4] -= (double)(SEQ ? w * drift : drift);
                 }
-                if (!SEQ || c.end > hi) break;
+                if (!SEQ) break;
+                if (many) {
+                    const bool more = c.end < min(k + 8, hi);
+                    lo = more ? c.end : hi;
+                    if (more) c.next(a.q, last), enter_lane();
+                    if (__any_sync(kAll, more)) continue;
+                    const int from = (hi - 1 - base) >> 3;
+                    c.join(from);
+                    w = __shfl_sync(kAll, w, from);
+                    A_of = __shfl_sync(kAll, A_of, from);
+                }
+                if (c.end > hi) break;
                 if (c.end >= stop) break; // the share ends with it
                 lo = c.end;
                 c.on(a.q, lo, lane);
@@ -556,11 +651,6 @@ template <int KL> __global__ void __launch_bounds__(kThreads, kPerSm) policy_seq
     const int lane = threadIdx.x & 31, share = blockIdx.x * kWarps + (threadIdx.x >> 5);
     if (!a.done) grid_dependency_wait(); // as above
     grid_dependency_release();
-    if (a.cluster) {
-        if (a.rollout) sequence_sums<true, 1>(a.sums);
-        else sequence_sums<true, 0>(a.sums);
-        cg::this_cluster().sync();
-    }
     const int live = a.q.live(), tokens = a.w.per_warp * kBlock;
     const double inv = inverse_norm(a), g = a.grad_loss ? (double)*a.grad_loss : 1.0;
     double v[kStats] = {};
@@ -568,8 +658,7 @@ template <int KL> __global__ void __launch_bounds__(kThreads, kPerSm) policy_seq
         const int begin = share * tokens, stop = min(live - begin, tokens) + begin;
         Cursor c{0, 0x7FFFFFFF};
         float w = 0.0f, slope_of = 0.0f, beta = 0.0f;
-        auto enter = [&]() {
-            const Piece p = a.pieces.total_warp(a.q, c.s, lane);
+        auto entered = [&](const Piece &p, bool counts) {
             w = slope_of = beta = 0.0f;
             if (!(p.n > 0.0) || !(inv > 0.0)) return;
             const double weight = a.sequence_mean ? inv / p.n : inv, d = p.a / p.n;
@@ -582,12 +671,14 @@ template <int KL> __global__ void __launch_bounds__(kThreads, kPerSm) policy_seq
             beta = (float)(a.beta * weight * g);
             if (flat) u = A >= 0.0 ? 1.0 + a.clip_high : (d < a.log_low ? 1.0 - a.clip_low : a.dual);
             else slope_of = (float)(-weight * i * A * u * g);
-            if (lane == 0 && a.q.bound(c.s) >= begin) {
+            if (counts) {
                 v[1] -= p.n * weight * i * A * u;
                 if (flat && A != 0.0) v[3] += p.n * weight;
                 v[4] -= weight * p.a;
             }
         };
+        auto enter = [&]() { entered(a.pieces.total_warp(a.q, c.s, lane), lane == 0 && a.q.bound(c.s) >= begin); };
+        auto enter_lane = [&](int k) { entered(a.pieces.total(a.q, c.s), a.q.bound(c.s) >= k); }; // the lane that holds its first token
         Mask8 mask;
         mask.read(a.mask, begin + lane * 8, stop, a.vec);
 #pragma unroll 1
@@ -606,6 +697,9 @@ template <int KL> __global__ void __launch_bounds__(kThreads, kPerSm) policy_seq
                 enter();
             }
             zero8(out);
+            int last = 0;
+            const bool many = c.end < hi && c.many(a.q, hi, lane, last);
+            if (many && k < hi && c.spread(a.q, k, last)) enter_lane(k);
 #pragma unroll 1
             for (int lo = base;;) {
                 const uint32_t run = c.end >= hi && lo == base ? valid : valid & range_bits(k, lo, c.end);
@@ -623,6 +717,17 @@ template <int KL> __global__ void __launch_bounds__(kThreads, kPerSm) policy_seq
                     if (in) out[e] = grad;
                 }
                 if (KL) v[2] += (double)(w * kls);
+                if (many) {
+                    const bool more = c.end < min(k + 8, hi);
+                    lo = more ? c.end : hi;
+                    if (more) c.next(a.q, last), enter_lane(k);
+                    if (__any_sync(kAll, more)) continue;
+                    const int from = (hi - 1 - base) >> 3;
+                    c.join(from);
+                    w = __shfl_sync(kAll, w, from);
+                    slope_of = __shfl_sync(kAll, slope_of, from);
+                    beta = __shfl_sync(kAll, beta, from);
+                }
                 if (c.end > hi || c.end >= stop) break;
                 lo = c.end;
                 c.on(a.q, lo, lane);
@@ -646,44 +751,59 @@ struct PreferenceArgs {
     const uint8_t *mask;
     const int64_t *N_dev;
     double N, beta, margin, margin_reward, smoothing, nll;
-    int G, loss, length_mean, vec, groups, per_cta, team, ctas;
+    int G, loss, length_mean, vec, groups, per_cta, slices, team, ctas;
     Pieces pieces;
     double *coef; // [n_seq] gradient of every valid token, before the division by N
     double *partials;
     float *scores, *stats;
     int64_t *pairs;
     float *omega;
-    SumArgs sums;
-    int cluster; // the call is one cluster, which does everything
     int behind;  // other launches of the call came first
 };
 
-// A CTA takes `per_cta` whole groups at a time: scores of their sequences into shared memory, then each sequence against the
-// others of its group.
-__device__ __forceinline__ void preference_pairs(const PreferenceArgs &a)
+// A CTA takes `per_cta` whole groups at a time, or one of the `slices` of the responses of a larger one: scores of all sequences of these
+// groups into shared memory, then each sequence against the others of its group.
+__global__ void __launch_bounds__(kThreads) preference_pairs_kernel(const __grid_constant__ PreferenceArgs a)
 {
+    grid_dependency_wait();
+    grid_dependency_release();
     extern __shared__ double smem[];
-    const int room = a.per_cta * a.G;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, room = a.per_cta * a.G;
     double *h = smem, *like = smem + room;             // score, mean log-probability
     double *per = smem + 2 * room;                     // 1 / |T| (0: no valid token)
     float *R = reinterpret_cast<float *>(smem + 3 * room);
     double v[kStats] = {}; // loss, right order, gap, nll, pairs
-    for (int64_t first = (int64_t)blockIdx.x * a.per_cta; first < a.groups; first += (int64_t)gridDim.x * a.per_cta) {
+    const int64_t items = a.slices > 1 ? (int64_t)a.groups * a.slices : (a.groups + a.per_cta - 1) / a.per_cta;
+    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const int64_t first = a.slices > 1 ? item / a.slices : item * a.per_cta;
+        const int slice = a.slices > 1 ? (int)(item - first * a.slices) : 0;
         const int n = (int)(a.groups - first < a.per_cta ? a.groups - first : a.per_cta) * a.G;
+        const int each = a.slices > 1 ? (n + a.slices - 1) / a.slices : n, from = slice * each, to = min(n, from + each);
         const int64_t base = first * a.G;
-        for (int i = threadIdx.x; i < n; i += kThreads) {
-            const Piece p = a.pieces.total(a.q, (int)(base + i));
+        auto put = [&](int i, const Piece &p) {
             const double inv = p.n > 0.0 ? 1.0 / p.n : 0.0;
-            h[i] = p.n > 0.0 ? a.beta * (a.length_mean ? p.a / p.n : p.a) : 0.0;
-            like[i] = p.n > 0.0 ? p.b / p.n : 0.0;
+            h[i] = p.n > 0.0 ? a.beta * (a.length_mean ? p.a * inv : p.a) : 0.0;
+            like[i] = p.n > 0.0 ? p.b * inv : 0.0;
             per[i] = inv;
             R[i] = a.rewards[base + i];
-            if (a.scores) a.scores[base + i] = (float)h[i];
+            if (a.scores && i >= from && i < to) a.scores[base + i] = (float)h[i];
+        };
+        bool far = false;
+        for (int i = threadIdx.x; i < n; i += kThreads) {
+            const Piece p = a.pieces.total(a.q, (int)(base + i), kThreads);
+            far |= p.n < 0.0;
+            put(i, p);
         }
-        __syncthreads();
+        if (__syncthreads_or(far)) {
+            for (int i = warp; i < n; i += kWarps) {
+                const Piece p = a.pieces.total_warp(a.q, (int)(base + i), lane);
+                if (lane == 0) put(i, p);
+            }
+            __syncthreads();
+        }
         // a.team neighbouring threads share the others of a response's group
         const int part = threadIdx.x & (a.team - 1);
-        for (int i = threadIdx.x / a.team; i < n; i += kThreads / a.team) {
+        for (int i = from + threadIdx.x / a.team; i < to; i += kThreads / a.team) {
             const int begin = i / a.G * a.G;
             const double hi = h[i];
             const float Ri = R[i];
@@ -739,13 +859,6 @@ __device__ __forceinline__ void preference_pairs(const PreferenceArgs &a)
     put_stats(v, a.partials + (size_t)blockIdx.x * kStats);
 }
 
-__global__ void __launch_bounds__(kThreads) preference_pairs_kernel(const __grid_constant__ PreferenceArgs a)
-{
-    grid_dependency_wait();
-    grid_dependency_release();
-    preference_pairs(a);
-}
-
 // The gradient of a sequence to each of its valid tokens.  Every CTA adds up the pairs of the CTAs before for the division by N; the first
 // one writes the statistics: loss, share of pairs in the right order, mean gap of the scores, mean -log-probability per token of the winners.
 __global__ void __launch_bounds__(kThreads, 4) preference_token_kernel(const __grid_constant__ PreferenceArgs a)
@@ -755,12 +868,6 @@ __global__ void __launch_bounds__(kThreads, 4) preference_token_kernel(const __g
     // behind the other launches, which waited for all before them, nothing but their results has to be waited for
     if (!a.behind) grid_dependency_wait();
     grid_dependency_release();
-    if (a.cluster) {
-        sequence_sums<true, 2>(a.sums);
-        cg::this_cluster().sync();
-        preference_pairs(a);
-        cg::this_cluster().sync();
-    }
     const int live = a.q.live(), tokens = a.w.per_warp * kBlock;
     const bool some = (int64_t)share * tokens < live;
     const int begin = some ? share * tokens : 0, stop = some ? min(live - begin, tokens) + begin : 0;
@@ -785,7 +892,9 @@ __global__ void __launch_bounds__(kThreads, 4) preference_token_kernel(const __g
     const double scale = inv * (a.grad_loss ? (double)*a.grad_loss : 1.0);
     if (!some)
         return;
-    float coef = inv > 0.0 ? (float)(__ldcg(a.coef + c.s) * scale) : 0.0f;
+    float coef;
+    auto enter = [&]() { coef = inv > 0.0 ? (float)(__ldcg(a.coef + c.s) * scale) : 0.0f; };
+    enter();
 #pragma unroll 1
     for (int first = begin; first < stop; first += kAhead * kBlock) {
         uint32_t valids = 0;
@@ -801,15 +910,27 @@ __global__ void __launch_bounds__(kThreads, 4) preference_token_kernel(const __g
             const uint32_t valid = valids & 0xFFu;
             float out[8];
             zero8(out);
+            int last = 0;
+            const bool many = c.end < hi && c.many(a.q, hi, lane, last);
+            if (many && k < hi && c.spread(a.q, k, last)) enter();
 #pragma unroll 1
             for (int lo = base;;) {
                 const uint32_t run = c.end >= hi && lo == base ? valid : valid & range_bits(k, lo, c.end);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) out[e] = run >> e & 1 ? coef : out[e];
+                if (many) {
+                    const bool more = c.end < min(k + 8, hi);
+                    lo = more ? c.end : hi;
+                    if (more) c.next(a.q, last), enter();
+                    if (__any_sync(kAll, more)) continue;
+                    const int from = (hi - 1 - base) >> 3;
+                    c.join(from);
+                    coef = __shfl_sync(kAll, coef, from);
+                }
                 if (c.end > hi || c.end >= stop) break;
                 lo = c.end;
                 c.on(a.q, lo, lane);
-                coef = inv > 0.0 ? (float)(__ldcg(a.coef + c.s) * scale) : 0.0f;
+                enter();
                 if (lo >= hi) break;
             }
             if (a.vec && hi - base == kBlock) store8(a.omega + k, out);
@@ -832,20 +953,16 @@ static unsigned ctas_of(const Share &w)
     return (unsigned)((warps + kWarps - 1) / kWarps);
 }
 
-// A call of up to kClusterBlocks blocks is one launch: its CTAs are a thread-block cluster, which goes from one step to the next by a barrier.
-constexpr int kCluster = 8;                              // CTAs that any device grants
-constexpr int64_t kClusterBlocks = 2 * kCluster * kWarps; // two blocks of a warp at most
+// A call of up to kClusterBlocks blocks without sums of sequences is one launch: its CTAs are a thread-block cluster, whose barrier lies
+// before the statistics (8192 tokens one call after the other: 5 us, 8 us as two launches).  With sums it gains nothing.
+constexpr int kCluster = 8;                          // CTAs that any device grants
+constexpr int64_t kClusterBlocks = kCluster * kWarps; // a block of a warp
 static bool clusters_on()
 {
     const char *off = std::getenv("HILORE_DISABLE_CLUSTER_LAUNCH");
     return off == nullptr || off[0] == '\0' || (off[0] == '0' && off[1] == '\0');
 }
 static bool one_cluster(int64_t n_tok) { return n_tok > 0 && (n_tok + kBlock - 1) / kBlock <= kClusterBlocks && clusters_on(); }
-static Share cluster_share(int64_t n_tok)
-{
-    const int64_t blocks = (n_tok + kBlock - 1) / kBlock;
-    return Share{(int)blocks, blocks <= kCluster * kWarps ? 1 : 2};
-}
 static unsigned cluster_of(const Share &w) // CTAs beyond the last share have nothing to do
 {
     unsigned n = 1;
@@ -970,25 +1087,25 @@ extern "C" int hilore_policy_loss(const float *logp, const float *logp_old, cons
 #undef HILORE_KLS
         kernel = kernels[!per_token ? 2 : (a.sequence_mean ? 1 : 0)][logp_rollout != nullptr][kl];
     }
-    SumArgs &s = a.sums;
+    SumArgs s{};
     s.q = a.q, s.mask = mask, s.vec = a.vec, s.out = a.pieces;
     if (sequence_ratio) s.x = logp, s.minus = logp_old;
     if (sequence_ratio && logp_rollout) s.y = logp_old, s.less = logp_rollout;
-    if (one_cluster(n_tok)) {
-        a.w = s.w = cluster_share(n_tok);
-        s.out.share = a.pieces.share = s.w.per_warp * kBlock;
+    const bool sums = sequence_ratio || a.sequence_mean;
+    if (!sums && one_cluster(n_tok)) {
+        a.w = share_of(n_tok, 1);
         a.cluster = 1;
         if (launch_cluster(kernel, cluster_of(a.w), 0, st, a) == cudaSuccess)
             return HILORE_OK;
         (void)cudaGetLastError(); // refused: the launches below
         a.cluster = 0;
     }
-    s.w = share_of(n_tok, kSumsPerSm);
+    s.w = share_of(n_tok, s.y ? kSumsPerSmOfFour : kSumsPerSm);
     s.out.share = a.pieces.share = s.w.per_warp * kBlock;
-    if (sequence_ratio || a.sequence_mean) {
+    if (sums) {
         a.done = s.done = reinterpret_cast<unsigned *>(ws + w.done);
-        void (*const sums)(SumArgs) = !sequence_ratio ? sequence_sums_kernel<false, 0> : (logp_rollout ? sequence_sums_kernel<true, 1> : sequence_sums_kernel<true, 0>);
-        if (launch_dependent(sums, dim3(ctas_of(s.w)), dim3(kThreads), 0, st, s) != cudaSuccess)
+        void (*const sum)(SumArgs) = !sequence_ratio ? sequence_sums_kernel<false, 0> : (logp_rollout ? sequence_sums_kernel<true, 1> : sequence_sums_kernel<true, 0>);
+        if (launch_dependent(sum, dim3(ctas_of(s.w)), dim3(kThreads), 0, st, s) != cudaSuccess)
             return HILORE_CUDA;
     }
     a.w = share_of(n_tok, kPerSm);
@@ -1036,7 +1153,9 @@ extern "C" int hilore_preference_loss(const float *logp, const float *logp_ref, 
     // Sixteen pairs in a row, of 64-bit exponentials and logarithms, take 15 us: threads share them as long as all of them run at once.
     a.team = 1;
     while (a.team < 32 && 2 * a.team <= G && 2 * a.team * n_seq <= (int64_t)sm_count() * 4 * kThreads) a.team *= 2;
-    a.per_cta = G * a.team >= kThreads ? 1 : kThreads / (G * a.team);
+    // Few responses go over all SMs, as 64-bit arithmetic is what takes long: 64 pairs on one SM 14 us, on 32 of them 12.
+    a.per_cta = (int)std::max<int64_t>(1, std::min<int64_t>(kThreads / (G * a.team), (a.groups + sm_count() - 1) / sm_count()));
+    a.slices = (G * a.team + kThreads - 1) / kThreads;
     unsigned char *ws = static_cast<unsigned char *>(workspace);
     a.pieces = pieces_of(workspace, w);
     a.coef = reinterpret_cast<double *>(ws + w.coef);
@@ -1044,24 +1163,14 @@ extern "C" int hilore_preference_loss(const float *logp, const float *logp_ref, 
     a.scores = scores, a.stats = stats, a.pairs = pairs, a.omega = omega;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const size_t smem = (size_t)a.per_cta * G * (3 * sizeof(double) + sizeof(float));
-    SumArgs &s = a.sums;
+    SumArgs s{};
     s.q = a.q, s.mask = mask, s.vec = a.vec, s.x = logp, s.minus = logp_ref, s.out = a.pieces;
-    if (one_cluster(n_tok)) {
-        a.w = s.w = cluster_share(n_tok);
-        s.out.share = a.pieces.share = s.w.per_warp * kBlock;
-        a.cluster = 1;
-        a.ctas = (int)cluster_of(a.w);
-        if (launch_cluster(preference_token_kernel, (unsigned)a.ctas, smem, st, a) == cudaSuccess)
-            return HILORE_OK;
-        (void)cudaGetLastError(); // refused: the launches below
-        a.cluster = a.ctas = 0;
-    }
     s.w = share_of(n_tok, kSumsPerSm);
     s.out.share = a.pieces.share = s.w.per_warp * kBlock;
     if (n_tok > 0 && launch_dependent(sequence_sums_kernel<true, 2>, dim3(ctas_of(s.w)), dim3(kThreads), 0, st, s) != cudaSuccess)
         return HILORE_CUDA;
     if (a.groups > 0) {
-        a.ctas = grid_of((a.groups + a.per_cta - 1) / a.per_cta, kMostCtas);
+        a.ctas = grid_of(a.slices > 1 ? (int64_t)a.groups * a.slices : (a.groups + a.per_cta - 1) / a.per_cta, kMostCtas);
         if (launch_dependent(preference_pairs_kernel, dim3((unsigned)a.ctas), dim3(kThreads), smem, st, a) != cudaSuccess)
             return HILORE_CUDA;
     }

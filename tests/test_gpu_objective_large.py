@@ -29,6 +29,8 @@ def lengths_of(kind):
     r = np.random.default_rng(3)
     if kind == "pieces":      # more tokens than warps that run at once take in even chunks, some sequences longer than a piece
         return np.concatenate([r.integers(0, 6000, 2600), [20001, 8192, 8193, 70000, 0, 1], r.integers(1, 40, 2000)])
+    if kind == "short":       # blocks with many ends, sequences without a token among them
+        return np.concatenate([r.integers(0, 40, 20000), [700, 0, 0, 3000], np.zeros(3000, int), r.integers(1, 3, 9000), [1]])
     if kind == "wave":        # 1.2 waves of the largest chunks
         return np.concatenate([r.integers(0, 9000, 3800), [31000]])
     return np.concatenate([r.integers(0, 3000, 400), [150000, 1, 0, 5000], r.integers(0, 9, 3000)])  # even chunks
@@ -52,7 +54,7 @@ def close(got, want, scale):
     assert bool((off <= U * 1.0001 * want.abs() + 2.0 ** -36 * scale).all()), float(off.max())
 
 
-@pytest.mark.parametrize("kind", ["even", "pieces", "wave"])
+@pytest.mark.parametrize("kind", ["even", "pieces", "wave", "short"])
 @pytest.mark.parametrize("trace", [False, True])
 def test_advantages_and_their_gradient(kind, trace):
     lengths = lengths_of(kind)
@@ -111,9 +113,10 @@ def policy_inputs(seq, n, S, normal, ratio, per_token):
                 white=torch.tensor([0.1, 0.9], device="cuda") if per_token else None)
 
 
+@pytest.mark.parametrize("kind", ["even", "short"])
 @pytest.mark.parametrize("ratio,mean,kl,per_token", [(0, 0, 3, True), (0, 1, 3, True), (0, 1, 1, False), (1, 1, 2, False), (1, 0, 3, False)])
-def test_policy(ratio, mean, kl, per_token):
-    lengths = lengths_of("even")
+def test_policy(kind, ratio, mean, kl, per_token):
+    lengths = lengths_of(kind)
     cu, seq, mask, n, normal = ragged(2, lengths)
     S, N = len(lengths), 12345
     x = policy_inputs(seq, n, S, normal, ratio, per_token)
@@ -146,9 +149,11 @@ def test_policy(ratio, mean, kl, per_token):
     assert bool(((stats.double() - sums).abs() <= 32 * U * big).all())
 
 
+@pytest.mark.parametrize("kind", ["even", "short"])
 @pytest.mark.parametrize("loss,length_mean,group", [(0, 1, 4), (1, 0, 2), (2, 1, 851)])
-def test_preference(loss, length_mean, group):
-    lengths = lengths_of("even")[:3404]
+def test_preference(kind, loss, length_mean, group):
+    lengths = lengths_of(kind)
+    lengths = lengths[:len(lengths) // 851 // 4 * 851 * 4]
     cu, seq, mask, n, normal = ragged(4, lengths)
     S = len(lengths)
     assert S % group == 0
@@ -187,7 +192,7 @@ def test_preference(loss, length_mean, group):
 
 @pytest.mark.parametrize("off", ["1", "0"])
 def test_small_calls_as_one_cluster_or_as_several_launches(off, monkeypatch):
-    """Up to 32768 tokens are one cluster of CTAs: the same results, to the roundings of sums in another order, without it."""
+    """Small policy losses are one cluster of CTAs: the same results, to the roundings of sums in another order, without it."""
     monkeypatch.setenv("HILORE_DISABLE_CLUSTER_LAUNCH", off)
     for lengths in ([5], [300, 0, 17, 4000], [128] * 200, [32768], [32769]):
         cu, seq, mask, n, normal = ragged(5, lengths)
