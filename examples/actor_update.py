@@ -1,7 +1,10 @@
 """A small actor trained by the library's calls from end to end: sampling under rules, rewards, log-probabilities under the
-same rules, GRPO coefficients, the gradient of the logits, and a clipped AdamW step with 8-bit moments.
+same rules, the loss's gradient by them, the gradient of the logits, and a clipped AdamW step with 8-bit moments.
 
-    python examples/actor_update.py [iterations]
+    python examples/actor_update.py [iterations] [grpo | policy | preference]
+
+grpo: the coefficients of the paper's loss.  policy: advantages of a critic, a value per token, and the clipped policy loss with a
+KL term to the actor as it was at the start.  preference: every pair of responses to a prompt of which one earned more.
 
 The actor knows the previous token alone: logits = emb[previous] @ head + bias.  A response earns the share of its tokens
 that are even.  PyTorch does the two products of the actor and draws the samples; the rest are calls of the C ABI.
@@ -89,20 +92,63 @@ def rollout(actor, gen, allow, dev):
     return seq, mask
 
 
-def train(iterations=40, epochs=2, lr=0.02, seed=0):
-    """Returns the mean reward of each iteration's responses, and the last gradient norm."""
+class Loss:
+    """What turns log-probabilities and rewards into omega, the gradient of the loss by the log-probabilities."""
+
+    def __init__(self, kind, dev):
+        self.kind = kind
+        self.omega = torch.empty(ROWS, T, device=dev)
+        self.valid = torch.zeros(1, dtype=torch.int64, device=dev)
+        self.critic = torch.zeros(V, device=dev)                                 # what is still to come behind a token
+        self.adv, self.returns, self.moments = torch.empty(ROWS, T, device=dev), torch.empty(ROWS, T, device=dev), torch.empty(2, device=dev)
+        self.stats = torch.empty(5, device=dev)
+        n = ROWS * T
+        self.policy = api.make_policy_terms(clip_low=0.2, clip_high=0.28, dual_clip=3.0, beta=0.01, kl=api.KL_K3, mean=api.MEAN_SEQUENCES,
+                                            adv_per_token=True)
+        self.preference = api.make_preference_terms(beta=0.5, nll=0.05)
+        self.ws = torch.empty(max(api.hilore_advantages_workspace_bytes(n), api.hilore_policy_loss_workspace_bytes(ROWS, n),
+                                  api.hilore_preference_loss_workspace_bytes(ROWS, n)), dtype=torch.uint8, device=dev)
+
+    def begin(self, previous, reward, mask):
+        """Once for a batch of responses."""
+        n = ROWS * T
+        api.hilore_mask_count(mask, n, self.valid)
+        if self.kind == "policy":
+            values = self.critic[previous]
+            api.hilore_advantages(None, reward, values, api.F32, None, None, mask, None, ROWS, n, 1.0, 0.95, self.adv, self.returns, self.moments,
+                                  self.ws, self.ws.numel())
+            count = torch.zeros(V, device=values.device).index_add_(0, previous, mask.view(-1).float())
+            miss = torch.zeros(V, device=values.device).index_add_(0, previous, (self.returns.view(-1) - values) * mask.view(-1))
+            self.critic += 0.5 * miss / count.clamp_min(1)
+
+    def __call__(self, logp, old, ref, reward, mask):
+        n = ROWS * T
+        if self.kind == "policy":
+            api.hilore_policy_loss(logp, old, ref, None, mask, self.adv, self.moments, None, ROWS, n, self.policy, ROWS, None, None, self.stats,
+                                   self.omega, self.ws, self.ws.numel())
+        elif self.kind == "preference":
+            api.hilore_preference_loss(logp, ref, mask, reward, G, None, ROWS, n, self.preference, 0, None, None, None, None, self.stats,
+                                       self.omega, self.ws, self.ws.numel())
+        else:
+            api.hilore_grpo_coeffs(reward, ROWS, G, 0, ROWS, T, logp.view(ROWS, T), old.view(ROWS, T), None, mask, 0, self.valid, 0.2, 0.0,
+                                   1e-6, None, self.omega, None, None)
+        return self.omega
+
+
+def train(iterations=40, epochs=2, lr=0.02, seed=0, kind="grpo", watch=None):
+    """Returns the mean reward of each iteration's responses, and the last gradient norm.  `watch` is called with the tensors of every
+    step before the parameters move."""
     dev = torch.device("cuda")
     gen = torch.Generator(device=dev).manual_seed(seed)
-    actor = Actor(gen, dev)
+    actor, loss = Actor(gen, dev), Loss(kind, dev)
+    start = {k: w.clone() for k, w in actor.w.items()}
     allow = torch.full((1, -(-V // 32)), -1, dtype=torch.int32, device=dev)
     allow[0, 0] = ~0b11                                                          # tokens 0 and 1 are never sampled
     begin = (torch.arange(ROWS, device=dev) * L).repeat_interleave(T)
     end = begin + P + torch.arange(T, device=dev).repeat(ROWS)
     n = ROWS * T
-    logp, lse, entropy = (torch.empty(n, device=dev) for _ in range(3))
-    omega = torch.empty(ROWS, T, device=dev)
+    logp, lse, entropy, ref = (torch.empty(n, device=dev) for _ in range(4))
     dlogits = torch.empty(n, V, dtype=torch.bfloat16, device=dev)
-    valid = torch.zeros(1, dtype=torch.int64, device=dev)
     rewards, t = [], 0
     for _ in range(iterations):
         seq, mask = rollout(actor, gen, allow, dev)
@@ -112,24 +158,29 @@ def train(iterations=40, epochs=2, lr=0.02, seed=0):
         r = rules(seq.view(-1), begin, begin + P, end, allow, dev)               # row (i, t): prefixes of sequence i
         targets = token.reshape(-1).contiguous()                                 # -1: a slot without a token
         previous = seq[:, P - 1:-1].reshape(-1).clamp_min(0).long()
-        api.hilore_mask_count(mask, n, valid)
+        loss.begin(previous, reward, mask)
+        if kind != "grpo":
+            now, actor.w = actor.w, start
+            api.hilore_token_logp(actor.logits(previous)[1], api.BF16, n, V, V, r, targets, ref, lse, None)
+            actor.w = now
         old = None
         for _ in range(epochs):
             h, x = actor.logits(previous)
             api.hilore_token_logp(x, api.BF16, n, V, V, r, targets, logp, lse, entropy)
             if old is None:
                 old = logp.clone()
-            api.hilore_grpo_coeffs(reward, ROWS, G, 0, ROWS, T, logp.view(ROWS, T), old.view(ROWS, T), None, mask, 0, valid, 0.2, 0.0,
-                                   1e-6, None, omega, None, None)
+            omega = loss(logp, old, ref, reward, mask)
             api.hilore_token_logp_backward(x, api.BF16, n, V, V, r, targets, lse, omega, dlogits, V)
             actor.backward(previous, h, dlogits)
+            if watch:
+                watch(dict(x=x, seq=seq, mask=mask, reward=reward, logp=logp, old=old, ref=ref, omega=omega, dlogits=dlogits, loss=loss))
             t += 1
             actor.step(t, lr)
     return rewards, float(actor.norm)
 
 
 if __name__ == "__main__":
-    got, norm = train(int(sys.argv[1]) if len(sys.argv) > 1 else 40)
+    got, norm = train(int(sys.argv[1]) if len(sys.argv) > 1 else 40, kind=sys.argv[2] if len(sys.argv) > 2 else "grpo")
     for i, r in enumerate(got):
         print(f"iteration {i:3d}  mean reward {r:.3f}")
     print(f"last gradient norm {norm:.4f}")
