@@ -73,43 +73,49 @@ struct Pieces {
     }
 };
 
-// Sequences are walked one at a time by the whole warp, which takes 1 us each.  Where kMany or more end in a block, each lane walks those of its
-// own eight tokens, of all lanes at the same time: 16384 sequences of one token in 33 us instead of 620.
-constexpr int kMany = 4;
-
-// A warp's way through the sequences of its tokens: the current one, which holds the first token not yet passed, and its end.
+// A warp's way through the sequences of its tokens: the current one, which holds the first token not yet passed, and its end.  Lane i knows
+// where sequence first + i ends, so that the next one is most often found without a load.
 struct Cursor {
-    int s, end;
+    int s, end, first, ends;
+    // The window of 32 sequences from s on.
+    __device__ __forceinline__ void fill(const Sequences &q, int lane)
+    {
+        first = s;
+        ends = (int64_t)s + lane < q.n_seq ? q.bound(s + lane + 1) : 0x7FFFFFFF;
+    }
     __device__ __forceinline__ void at(const Sequences &q, int token, int lane)
     {
         s = q.owner_warp(token, lane);
-        end = q.bound(s + 1);
+        fill(q, lane);
+        end = __shfl_sync(kAll, ends, 0);
     }
-    // On to the sequence of `token`, which is not in this one but behind it.
-    __device__ __forceinline__ void on(const Sequences &q, int token, int lane)
+    // On to the sequence of `token`, which is not in this one but behind it.  Whether the window is another one.
+    __device__ __forceinline__ bool on(const Sequences &q, int token, int lane)
     {
-        const int64_t o = (int64_t)s + 1 + lane;
-        const int e = o < q.n_seq ? q.bound((int)o + 1) : 0x7FFFFFFF;
-        const uint32_t hit = __ballot_sync(kAll, e > token);
-        if (hit == 0) {
-            at(q, token, lane);
-        } else {
+        const uint32_t hit = __ballot_sync(kAll, ends > token);
+        if (hit) {
             const int j = __ffs(hit) - 1;
-            s = (int)(s + 1 + j < q.n_seq ? s + 1 + j : q.n_seq - 1);
-            end = __shfl_sync(kAll, e, j);
+            s = (int)((int64_t)first + j < q.n_seq ? first + j : q.n_seq - 1);
+            end = __shfl_sync(kAll, ends, j);
+        } else {
+            at(q, token, lane);
         }
         if (end <= token) end = 0x7FFFFFFF; // boundaries out of order
+        return hit == 0;
     }
-    // Whether kMany sequences or more end before token `hi`, from this one on, and then at least the last of those that do.
-    __device__ __forceinline__ bool many(const Sequences &q, int hi, int lane, int &last) const
+    // How many sequences of the window end before token hi, from this one on; 32: perhaps more.
+    __device__ __forceinline__ int inside(int hi, int lane) const
     {
-        const int64_t o = (int64_t)s + lane;
-        const uint32_t out = __ballot_sync(kAll, (o < q.n_seq ? q.bound((int)o + 1) : 0x7FFFFFFF) >= hi);
-        const int n = out ? __ffs(out) - 1 : 32;
-        last = out ? s + n : q.owner_warp(hi - 1, lane);
-        return n >= kMany;
+        const uint32_t in = __ballot_sync(kAll, ends < hi && lane >= s - first);
+        return in >> 31 ? 32 : __popc(in);
     }
-    // From here on every lane has a cursor of its own: on to the sequence of token k, no further than `last`.
+    // Where so many end that every lane walks those of its own eight tokens: the sequence of token hi - 1, or one before it.
+    __device__ __forceinline__ int ahead(const Sequences &q, int hi, int lane) const
+    {
+        const uint32_t out = __ballot_sync(kAll, ends >= hi && lane >= s - first);
+        return out ? first + __ffs(out) - 1 : q.owner_warp(hi - 1, lane);
+    }
+    // On to the sequence of token k, no further than `last`.
     __device__ __forceinline__ bool spread(const Sequences &q, int k, int last)
     {
         if (k < end) return false;
@@ -118,7 +124,7 @@ struct Cursor {
         if (end <= k) end = 0x7FFFFFFF;
         return true;
     }
-    __device__ __forceinline__ void next(const Sequences &q, int last) // by a lane: to the one that begins where this one ends
+    __device__ __forceinline__ void next(const Sequences &q, int last) // to the one that begins where this one ends
     {
         const int token = end;
         if (s < last) ++s;
@@ -126,12 +132,21 @@ struct Cursor {
         if (end <= token) s = q.owner(token, s, last), end = q.bound(s + 1);
         if (end <= token) end = 0x7FFFFFFF;
     }
-    __device__ __forceinline__ void join(int from) // the cursor of lane `from`
+    __device__ __forceinline__ void join(const Sequences &q, int from, int lane) // the cursor of lane `from` is everyone's
     {
         s = __shfl_sync(kAll, s, from);
         end = __shfl_sync(kAll, end, from);
+        fill(q, lane);
     }
 };
+// Sequences that end in a block are taken one after the other up to this many, behind that by all lanes at the same time, each those of its tokens.
+#ifndef KFEW
+#define KFEW 8
+#endif
+#ifndef KFEWSUMS
+#define KFEWSUMS 3
+#endif
+constexpr int kFew = KFEW, kFewSums = KFEWSUMS;
 
 // Sums since the last end of a sequence, if there is one.
 struct SumOp {
@@ -170,16 +185,18 @@ __global__ void __launch_bounds__(kThreads, Y == 1 ? kSumsPerSmOfFour : kSumsPer
     if ((int64_t)share * tokens >= live)
         return;
     const int begin = share * tokens, stop = min(live - begin, tokens) + begin;
-    Cursor c{0, 0x7FFFFFFF};
+    Cursor c{0, 0x7FFFFFFF, 0, 0};
     Piece sum{0.0, 0.0, 0.0};
     int n = 0;
+    bool opened = true; // whether the current sequence begins in the share
     auto finish = [&](bool ends) {
         const Piece p{X ? warp_sum(sum.a) : 0.0, Y ? warp_sum(sum.b) : 0.0, (double)__reduce_add_sync(kAll, (unsigned)n)};
         if (lane == 0) {
-            if (a.q.bound(c.s) < begin) a.out.head[share] = p;
+            if (!opened) a.out.head[share] = p;
             else if (ends) a.out.whole[c.s] = p;
             else a.out.tail[share] = p;
         }
+        opened = true;
         sum = Piece{0.0, 0.0, 0.0};
         n = 0;
     };
@@ -207,13 +224,14 @@ __global__ void __launch_bounds__(kThreads, Y == 1 ? kSumsPerSmOfFour : kSumsPer
     mask.read(a.mask, begin + lane * 8, stop, a.vec);
     ask(now, begin);
     c.at(a.q, begin, lane); // while the first block is on its way
+    opened = a.q.bound(c.s) >= begin;
 #pragma unroll 1
     for (int base = begin; base < stop; base += kBlock) {
         const int k = base + lane * 8, hi = min(base + kBlock, stop);
         const uint32_t valid = now.valid;
         ask(then, base + kBlock);
-        int last;
-        if (c.end < hi && c.many(a.q, hi, lane, last)) {
+        if (c.end < hi && c.inside(hi, lane) > kFewSums) {
+            const int last = c.ahead(a.q, hi, lane);
             const Piece before{X ? warp_sum(sum.a) : 0.0, Y ? warp_sum(sum.b) : 0.0, (double)__reduce_add_sync(kAll, (unsigned)n)};
             SumOp::Map mine = SumOp::identity(), first = mine, all; // since the last end in the lane's tokens; before the first
             int s_first = 0;
@@ -244,39 +262,41 @@ __global__ void __launch_bounds__(kThreads, Y == 1 ? kSumsPerSmOfFour : kSumsPer
             all = shfl_words(all, 31); // an end is in it
             sum = lane == 0 ? Piece{all.a, all.b, 0.0} : Piece{0.0, 0.0, 0.0};
             n = lane == 0 ? (int)all.n : 0;
-            c.join((hi - 1 - base) >> 3);
+            c.join(a.q, (hi - 1 - base) >> 3, lane);
             if (c.end <= hi) {
                 if (c.end >= stop) return;
                 c.on(a.q, hi, lane);
             }
-        } else
+            opened = true;
+        } else {
 #pragma unroll 1
-        for (int lo = base;;) { // the block's part of each sequence
-            const uint32_t run = c.end >= hi && lo == base ? valid : valid & range_bits(k, lo, c.end);
-            if (__all_sync(kAll, run == 0xFFu)) {
+            for (int lo = base;;) { // the block's part of each sequence
+                const uint32_t run = c.end >= hi && lo == base ? valid : valid & range_bits(k, lo, c.end);
+                if (__all_sync(kAll, run == 0xFFu)) {
 #pragma unroll
-                for (int e = 0; e < 8; e += 2) {
-                    if constexpr (X) sum.a += ((double)now.x[e] - (double)now.m[e]) + ((double)now.x[e + 1] - (double)now.m[e + 1]);
-                    if constexpr (Y == 1) sum.b += ((double)now.y[e] - (double)now.l[e]) + ((double)now.y[e + 1] - (double)now.l[e + 1]);
-                    if constexpr (Y == 2) sum.b += (double)now.x[e] + (double)now.x[e + 1];
-                }
-                n += 8;
-            } else if (__any_sync(kAll, run != 0)) {
+                    for (int e = 0; e < 8; e += 2) {
+                        if constexpr (X) sum.a += ((double)now.x[e] - (double)now.m[e]) + ((double)now.x[e + 1] - (double)now.m[e + 1]);
+                        if constexpr (Y == 1) sum.b += ((double)now.y[e] - (double)now.l[e]) + ((double)now.y[e + 1] - (double)now.l[e + 1]);
+                        if constexpr (Y == 2) sum.b += (double)now.x[e] + (double)now.x[e + 1];
+                    }
+                    n += 8;
+                } else if (__any_sync(kAll, run != 0)) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const bool in = run >> e & 1;
-                    if constexpr (X) sum.a += pick(in, (double)now.x[e] - (double)now.m[e], 0.0);
-                    if constexpr (Y == 1) sum.b += pick(in, (double)now.y[e] - (double)now.l[e], 0.0);
-                    if constexpr (Y == 2) sum.b += pick(in, (double)now.x[e], 0.0);
+                    for (int e = 0; e < 8; ++e) {
+                        const bool in = run >> e & 1;
+                        if constexpr (X) sum.a += pick(in, (double)now.x[e] - (double)now.m[e], 0.0);
+                        if constexpr (Y == 1) sum.b += pick(in, (double)now.y[e] - (double)now.l[e], 0.0);
+                        if constexpr (Y == 2) sum.b += pick(in, (double)now.x[e], 0.0);
+                    }
+                    n += __popc(run);
                 }
-                n += __popc(run);
+                if (c.end > hi) break;
+                finish(true);
+                if (c.end >= stop) return; // the share ends with it
+                lo = c.end;
+                c.on(a.q, lo, lane);
+                if (lo >= hi) break;
             }
-            if (c.end > hi) break;
-            finish(true);
-            if (c.end >= stop) return; // the share ends with it
-            lo = c.end;
-            c.on(a.q, lo, lane);
-            if (lo >= hi) break;
         }
         now = then;
     }
@@ -451,14 +471,34 @@ template <bool SEQ, int KL, bool ROLLOUT, bool PER_TOKEN> __global__ void __laun
         const float high = (float)a.log_high, low = (float)a.log_low, dual_log = (float)a.log_dual;
         const float most_up = (float)(1.0 + a.clip_high), most_down = (float)(1.0 - a.clip_low), dual = (float)a.dual, cap = (float)a.cap;
         const float beta = a.beta != 0.0 ? (float)(a.beta * inv * g) : 0.0f, slope_of = (float)(-inv * g);
-        Cursor c{0, 0x7FFFFFFF};
+        Cursor c{0, 0x7FFFFFFF, 0, 0};
         float w = 1.0f, A_of = 0.0f; // of the sequence: weight / inv, advantage
-        auto entered = [&](double n) {
-            if (a.sequence_mean) w = n > 0.0 ? (float)(1.0 / n) : 0.0f;
+        float w_of = 1.0f, A_lane = 0.0f; // of the window's sequences,
+        bool far = false;                 // or not, as its sums lie over many shares
+        auto weight = [&](double n) { return n > 0.0 ? (float)(1.0 / n) : 0.0f; };
+        auto look = [&]() { // the window's: of sequences that begin in the share, and of the first one
+            const int before = __shfl_up_sync(kAll, c.ends, 1);
+            const int o = c.first + lane;
+            far = false;
+            if (o >= a.q.n_seq || (lane > 0 && before >= stop)) return;
+            if (a.sequence_mean) {
+                const double n = a.pieces.total(a.q, o, 4).n;
+                far = n < 0.0;
+                w_of = weight(n);
+            }
+            if (!PER_TOKEN) A_lane = (__ldg(a.adv + o) - mean) * scale;
+        };
+        auto enter = [&](bool other) {
+            if (other) look();
+            const int i = c.s - c.first;
+            w = __shfl_sync(kAll, w_of, i);
+            A_of = __shfl_sync(kAll, A_lane, i);
+            if (__ballot_sync(kAll, far) >> i & 1) w = weight(a.pieces.total_warp(a.q, c.s, lane).n);
+        };
+        auto enter_lane = [&]() {
+            if (a.sequence_mean) w = weight(a.pieces.total(a.q, c.s).n);
             if (!PER_TOKEN) A_of = (__ldg(a.adv + c.s) - mean) * scale;
         };
-        auto enter = [&]() { entered(a.sequence_mean ? a.pieces.total_warp(a.q, c.s, lane).n : 0.0); };
-        auto enter_lane = [&]() { entered(a.sequence_mean ? a.pieces.total(a.q, c.s).n : 0.0); };
         Mask8 mask;
         mask.read(a.mask, begin + lane * 8, stop, a.vec);
 #pragma unroll 1
@@ -477,163 +517,182 @@ template <bool SEQ, int KL, bool ROLLOUT, bool PER_TOKEN> __global__ void __laun
             if (SEQ && base == begin) { // while the first block is on its way
                 c.at(a.q, begin, lane);
                 if (a.done) grid_dependency_wait();
-                enter();
+                enter(true);
             }
             zero8(out);
-            int last = 0;
-            const bool many = SEQ && c.end < hi && c.many(a.q, hi, lane, last);
-            if (many && k < hi && c.spread(a.q, k, last)) enter_lane();
+            float wt[8]; // weights / inv; and advantages, if they are of sequences
+            const bool whole = !SEQ || c.end >= hi;
+            if (SEQ) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    wt[e] = w;
+                    if (!PER_TOKEN) A[e] = A_of;
+                }
+            }
+            if (!whole) {
+                if (c.inside(hi, lane) > kFew) {
+                    const int last = c.ahead(a.q, hi, lane), rim = min(k + 8, hi);
+                    bool going = false;
+                    if (k < hi) {
+                        const bool moved = c.spread(a.q, k, last);
+                        if (moved) enter_lane();
+                        going = moved || c.end < rim;
+                    }
+                    int lo = k;
 #pragma unroll 1
-            for (int lo = base;;) { // the block's, or the lane's, part of each sequence
-                const uint32_t run = !SEQ || (c.end >= hi && lo == base) ? valid : valid & range_bits(k, lo, c.end);
-                // Nearly always a block has one sequence, no ratio within rounding of a bound, and nothing far out: then masked tokens go as
-                // zeros, which add nothing to any sum, and the objective is the smaller of two products.
-                bool plain = !SEQ || (!many && lo == base && c.end >= hi);
-                if (plain) {
-                    if (run != 0xFFu) {
+                    while (__any_sync(kAll, going)) {
+                        if (going) {
+                            const uint32_t run = range_bits(k, lo, c.end);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if (!(run >> e & 1)) {
-                                s[e] = o[e] = 0.0f;
-                                if (KL) r[e] = 0.0f;
-                                if (ROLLOUT) b[e] = 0.0f;
-                                if (PER_TOKEN) A[e] = mean;
-                            }
-                    }
-                    bool odd = strange;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float d = s[e] - o[e];
-                        odd |= !(fabsf(d) <= kNear);
-                        odd |= fminf(fabsf(d - high), fabsf(d - low)) <= a.near;
-                        if (a.dual_clip) odd |= fabsf(d - dual_log) <= a.near;
-                        if (KL) odd |= !(fabsf(r[e] - s[e]) <= (KL == kK3 ? kLargest : kNear));
-                        if (ROLLOUT) odd |= !(fabsf(o[e] - b[e]) <= kNear);
-                    }
-                    plain = !__any_sync(kAll, odd);
-                }
-                if (plain) {
-                    float term = 0.0f, kls = 0.0f, drift = 0.0f, flats = 0.0f;
-#pragma unroll
-                    for (int e = 0; e < 8; e += 2) {
-                        float value[2], slope[2];
-                        if (KL == kK3) {
-                            const float e0 = r[e] - s[e], e1 = r[e + 1] - s[e + 1];
-                            exp_minus_line(e0, e1, value[0], value[1]);
-                            slope[0] = -(value[0] + e0);
-                            slope[1] = -(value[1] + e1);
-                        } else if (KL) {
-#pragma unroll
-                            for (int i = 0; i < 2; ++i) kl_term<KL>(r[e + i] - s[e + i], a.k2, value[i], slope[i]);
-                        }
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const float d = s[e + i] - o[e + i], rho = exp_near(d);
-                            float x = PER_TOKEN ? (A[e + i] - mean) * scale : (run >> (e + i) & 1 ? A_of : 0.0f);
-                            if (SEQ) x *= w;
-                            if (ROLLOUT) x *= fminf(exp_near(o[e + i] - b[e + i]), cap);
-                            const float gain = x * rho;
-                            float held = fminf(gain, x * fminf(fmaxf(rho, most_down), most_up));
-                            if (a.dual_clip) held = x < 0.0f ? fmaxf(held, x * dual) : held;
-                            const bool flat = held < gain || held > gain; // NaN stays
-                            float grad = flat ? 0.0f : slope_of * gain;
-                            flats += flat ? 1.0f : 0.0f;
-                            term += held;
-                            drift += d;
-                            if (KL) {
-                                kls += value[i];
-                                grad = fmaf(SEQ ? beta * w : beta, slope[i], grad);
-                            }
-                            out[e + i] = grad;
+                            for (int e = 0; e < 8; ++e)
+                                if (run >> e & 1) {
+                                    wt[e] = w;
+                                    if (!PER_TOKEN) A[e] = A_of;
+                                }
+                            going = c.end < rim;
+                            if (going) lo = c.end, c.next(a.q, last), enter_lane();
                         }
                     }
-                    if (run != 0xFFu) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) out[e] = run >> e & 1 ? out[e] : 0.0f;
-                    }
-                    v[1] -= (double)term;
-                    if (KL) v[2] += (double)(SEQ ? w * kls : kls);
-                    v[3] += (double)(SEQ ? w * flats : flats);
-                    v[4] -= (double)(SEQ ? w * drift : drift);
-                } else if (__any_sync(kAll, run != 0)) {
-                    // which tokens are on a flat branch, and which of these on the dual clip's
-                    uint32_t flat = 0, over = 0;
-                    bool close = false;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float Ae = PER_TOKEN ? (A[e] - mean) * scale : A_of, d = s[e] - o[e];
-                        // A >= 0: beyond the bound where d > high; A < 0: where -d > -low
-                        const bool up = Ae >= 0.0f;
-                        const float past = __uint_as_float(__float_as_uint(d) ^ (up ? 0u : 0x80000000u)) - (up ? high : -low);
-                        flat |= past > 0.0f ? 1u << e : 0u;
-                        close |= fabsf(past) <= a.near;
-                        if (a.dual_clip) {
-                            over |= !up && d > dual_log ? 1u << e : 0u;
-                            close |= fabsf(d - dual_log) <= a.near;
-                        }
-                    }
-                    if (close) { // next to a bound: compared as the formula does
-                        flat = over = 0;
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const float Ae = PER_TOKEN ? (A[e] - mean) * scale : A_of;
-                            const double D = (double)s[e] - (double)o[e];
-                            if (Ae >= 0.0f ? D > a.log_high : D < a.log_low) flat |= 1u << e;
-                            if (!(Ae >= 0.0f) && D > a.log_dual) over |= 1u << e;
-                        }
-                    }
-                    flat |= over;
-                    float term = 0.0f, kls = 0.0f, drift = 0.0f;
-                    uint32_t none = 0; // tokens of no advantage
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const bool in = run >> e & 1, on_flat = flat >> e & 1;
-                        const float Ae = PER_TOKEN ? (A[e] - mean) * scale : A_of, d = s[e] - o[e];
-                        const float rho = fabsf(d) <= kNear ? exp_near(d) : expf(d); // the same bits as above where that is enough
-                        float bound = Ae >= 0.0f ? most_up : most_down;
-                        if (a.dual_clip) bound = over >> e & 1 ? dual : bound;
-                        float x = SEQ ? w * Ae : Ae;
-                        if (ROLLOUT) {
-                            const float gap = o[e] - b[e], i = fabsf(gap) <= kNear ? exp_near(gap) : expf(gap);
-                            x *= i > cap ? cap : i; // NaN stays
-                        }
-                        const float gain = x * (on_flat ? bound : rho);
-                        float grad = on_flat ? 0.0f : slope_of * gain;
-                        term += in ? gain : 0.0f;
-                        drift += in ? d : 0.0f;
-                        none |= Ae == 0.0f ? 1u << e : 0u;
-                        if (KL) {
-                            float value, slope;
-                            kl_term<KL>(r[e] - s[e], a.k2, value, slope);
-                            kls += in ? value : 0.0f;
-                            if (beta != 0.0f) grad = fmaf(SEQ ? beta * w : beta, slope, grad);
-                        }
-                        if (in) out[e] = grad;
-                    }
-                    const int flats = __popc(flat & ~none & run);
-                    v[1] -= (double)term;
-                    if (KL) v[2] += (double)(SEQ ? w * kls : kls);
-                    v[3] += (double)(SEQ ? w * (float)flats : (float)flats);
-                    v[4] -= (double)(SEQ ? w * drift : drift);
-                }
-                if (!SEQ) break;
-                if (many) {
-                    const bool more = c.end < min(k + 8, hi);
-                    lo = more ? c.end : hi;
-                    if (more) c.next(a.q, last), enter_lane();
-                    if (__any_sync(kAll, more)) continue;
                     const int from = (hi - 1 - base) >> 3;
-                    c.join(from);
                     w = __shfl_sync(kAll, w, from);
                     A_of = __shfl_sync(kAll, A_of, from);
+                    c.join(a.q, from, lane);
+                    look();
+                } else {
+#pragma unroll 1
+                    while (c.end < hi) {
+                        const int lo = c.end;
+                        enter(c.on(a.q, lo, lane));
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (k + e >= lo) {
+                                wt[e] = w;
+                                if (!PER_TOKEN) A[e] = A_of;
+                            }
+                    }
                 }
-                if (c.end > hi) break;
-                if (c.end >= stop) break; // the share ends with it
-                lo = c.end;
-                c.on(a.q, lo, lane);
-                enter();
-                if (lo >= hi) break;
             }
+            // Nearly always a block has no ratio within rounding of a bound and nothing far out: then masked tokens go as zeros, which add
+            // nothing to any sum, and the objective is the smaller of two products.
+            if (valid != 0xFFu) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (!(valid >> e & 1)) {
+                        s[e] = o[e] = 0.0f;
+                        if (KL) r[e] = 0.0f;
+                        if (ROLLOUT) b[e] = 0.0f;
+                        A[e] = PER_TOKEN ? mean : 0.0f;
+                    }
+            }
+            bool odd = strange;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float d = s[e] - o[e];
+                odd |= !(fabsf(d) <= kNear);
+                odd |= fminf(fabsf(d - high), fabsf(d - low)) <= a.near;
+                if (a.dual_clip) odd |= fabsf(d - dual_log) <= a.near;
+                if (KL) odd |= !(fabsf(r[e] - s[e]) <= (KL == kK3 ? kLargest : kNear));
+                if (ROLLOUT) odd |= !(fabsf(o[e] - b[e]) <= kNear);
+            }
+            float term = 0.0f, kls = 0.0f, drift = 0.0f, flats = 0.0f;
+            if (!__any_sync(kAll, odd)) {
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    float value[2], slope[2];
+                    if (KL == kK3) {
+                        const float e0 = r[e] - s[e], e1 = r[e + 1] - s[e + 1];
+                        exp_minus_line(e0, e1, value[0], value[1]);
+                        slope[0] = -(value[0] + e0);
+                        slope[1] = -(value[1] + e1);
+                    } else if (KL) {
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) kl_term<KL>(r[e + i] - s[e + i], a.k2, value[i], slope[i]);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const float d = s[e + i] - o[e + i], rho = exp_near(d);
+                        float x = PER_TOKEN ? (A[e + i] - mean) * scale : A[e + i];
+                        if (SEQ) x *= wt[e + i];
+                        if (ROLLOUT) x *= fminf(exp_near(o[e + i] - b[e + i]), cap);
+                        const float gain = x * rho;
+                        float held = fminf(gain, x * fminf(fmaxf(rho, most_down), most_up));
+                        if (a.dual_clip) held = x < 0.0f ? fmaxf(held, x * dual) : held;
+                        const bool flat = held < gain || held > gain; // NaN stays
+                        float grad = flat ? 0.0f : slope_of * gain;
+                        flats += flat ? (SEQ ? wt[e + i] : 1.0f) : 0.0f;
+                        term += held;
+                        drift = SEQ ? fmaf(wt[e + i], d, drift) : drift + d;
+                        if (KL) {
+                            kls = SEQ ? fmaf(wt[e + i], value[i], kls) : kls + value[i];
+                            grad = fmaf(SEQ ? beta * wt[e + i] : beta, slope[i], grad);
+                        }
+                        out[e + i] = grad;
+                    }
+                }
+                if (valid != 0xFFu) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) out[e] = valid >> e & 1 ? out[e] : 0.0f;
+                }
+            } else {
+                // which tokens are on a flat branch, and which of these on the dual clip's
+                uint32_t flat = 0, over = 0;
+                bool close = false;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float Ae = PER_TOKEN ? (A[e] - mean) * scale : A[e], d = s[e] - o[e];
+                    // A >= 0: beyond the bound where d > high; A < 0: where -d > -low
+                    const bool up = Ae >= 0.0f;
+                    const float past = __uint_as_float(__float_as_uint(d) ^ (up ? 0u : 0x80000000u)) - (up ? high : -low);
+                    flat |= past > 0.0f ? 1u << e : 0u;
+                    close |= fabsf(past) <= a.near;
+                    if (a.dual_clip) {
+                        over |= !up && d > dual_log ? 1u << e : 0u;
+                        close |= fabsf(d - dual_log) <= a.near;
+                    }
+                }
+                if (close) { // next to a bound: compared as the formula does
+                    flat = over = 0;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float Ae = PER_TOKEN ? (A[e] - mean) * scale : A[e];
+                        const double D = (double)s[e] - (double)o[e];
+                        if (Ae >= 0.0f ? D > a.log_high : D < a.log_low) flat |= 1u << e;
+                        if (!(Ae >= 0.0f) && D > a.log_dual) over |= 1u << e;
+                    }
+                }
+                flat |= over;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const bool in = valid >> e & 1, on_flat = flat >> e & 1;
+                    const float Ae = PER_TOKEN ? (A[e] - mean) * scale : A[e], d = s[e] - o[e];
+                    const float rho = fabsf(d) <= kNear ? exp_near(d) : expf(d); // the same bits as above where that is enough
+                    float bound = Ae >= 0.0f ? most_up : most_down;
+                    if (a.dual_clip) bound = over >> e & 1 ? dual : bound;
+                    const float we = SEQ ? wt[e] : 1.0f;
+                    float x = SEQ ? Ae * we : Ae;
+                    if (ROLLOUT) {
+                        const float gap = o[e] - b[e], i = fabsf(gap) <= kNear ? exp_near(gap) : expf(gap);
+                        x *= i > cap ? cap : i; // NaN stays
+                    }
+                    const float gain = x * (on_flat ? bound : rho);
+                    float grad = on_flat ? 0.0f : slope_of * gain;
+                    term += in ? gain : 0.0f;
+                    drift = in ? fmaf(we, d, drift) : drift;
+                    flats += in && on_flat && Ae != 0.0f ? we : 0.0f;
+                    if (KL) {
+                        float value, slope;
+                        kl_term<KL>(r[e] - s[e], a.k2, value, slope);
+                        kls = in ? fmaf(we, value, kls) : kls;
+                        if (beta != 0.0f) grad = fmaf(SEQ ? beta * we : beta, slope, grad);
+                    }
+                    if (in) out[e] = grad;
+                }
+            }
+            v[1] -= (double)term;
+            if (KL) v[2] += (double)kls;
+            v[3] += (double)flats;
+            v[4] -= (double)drift;
+            if (SEQ && c.end <= hi && c.end < stop) enter(c.on(a.q, hi, lane));
             if (a.vec && hi - base == kBlock) store8(a.omega + k, out);
             else store8(a.omega, k, base, hi, a.vec, out);
         }
@@ -656,19 +715,20 @@ template <int KL> __global__ void __launch_bounds__(kThreads, kPerSm) policy_seq
     double v[kStats] = {};
     if ((int64_t)share * tokens < live) {
         const int begin = share * tokens, stop = min(live - begin, tokens) + begin;
-        Cursor c{0, 0x7FFFFFFF};
-        float w = 0.0f, slope_of = 0.0f, beta = 0.0f;
-        auto entered = [&](const Piece &p, bool counts) {
-            w = slope_of = beta = 0.0f;
+        Cursor c{0, 0x7FFFFFFF, 0, 0};
+        const float beta = (float)(a.beta * g);
+        float w = 0.0f, slope_of = 0.0f;
+        // Into w and slope_of; counts: into the statistics as well.
+        auto entered = [&](int o, const Piece &p, bool counts) {
+            w = slope_of = 0.0f;
             if (!(p.n > 0.0) || !(inv > 0.0)) return;
-            const double weight = a.sequence_mean ? inv / p.n : inv, d = p.a / p.n;
-            double A = (double)__ldg(a.adv + c.s);
+            const double per = 1.0 / p.n, weight = a.sequence_mean ? inv * per : inv, d = p.a * per;
+            double A = (double)__ldg(a.adv + o);
             if (a.moments) A = (A - (double)a.moments[0]) / ((double)a.moments[1] + a.adv_eps);
-            const double gap = a.rollout ? exp(p.b / p.n) : 1.0, i = a.rollout && gap > a.cap ? a.cap : gap; // NaN stays
+            const double gap = a.rollout ? exp(p.b * per) : 1.0, i = a.rollout && gap > a.cap ? a.cap : gap; // NaN stays
             const bool flat = A >= 0.0 ? d > a.log_high : (d < a.log_low || d > a.log_dual);
             double u = exp(d);
             w = (float)weight;
-            beta = (float)(a.beta * weight * g);
             if (flat) u = A >= 0.0 ? 1.0 + a.clip_high : (d < a.log_low ? 1.0 - a.clip_low : a.dual);
             else slope_of = (float)(-weight * i * A * u * g);
             if (counts) {
@@ -677,8 +737,36 @@ template <int KL> __global__ void __launch_bounds__(kThreads, kPerSm) policy_seq
                 v[4] -= weight * p.a;
             }
         };
-        auto enter = [&]() { entered(a.pieces.total_warp(a.q, c.s, lane), lane == 0 && a.q.bound(c.s) >= begin); };
-        auto enter_lane = [&](int k) { entered(a.pieces.total(a.q, c.s), a.q.bound(c.s) >= k); }; // the lane that holds its first token
+        float w_of = 0.0f, slope_lane = 0.0f; // of the window's sequences,
+        bool far = false;                     // or not, as its sums lie over many shares
+        int counted = begin;                  // the tokens before it are those of sequences that the statistics have
+        auto look = [&]() { // the window's: of sequences that begin in the share, and of the first one
+            int before = __shfl_up_sync(kAll, c.ends, 1);
+            const int o = c.first + lane;
+            far = false;
+            if (o < a.q.n_seq && (lane == 0 || before < stop)) {
+                const Piece p = a.pieces.total(a.q, o, 4);
+                far = p.n < 0.0;
+                if (lane == 0) before = a.q.bound(o);
+                entered(o, p, before >= counted);
+                w_of = w, slope_lane = slope_of;
+            }
+            counted = __shfl_sync(kAll, c.ends, 31);
+        };
+        auto enter = [&](bool other) {
+            if (other) look();
+            const int i = c.s - c.first;
+            w = __shfl_sync(kAll, w_of, i);
+            slope_of = __shfl_sync(kAll, slope_lane, i);
+            if (__ballot_sync(kAll, far) >> i & 1) entered(c.s, a.pieces.total_warp(a.q, c.s, lane), lane == 0 && a.q.bound(c.s) >= begin);
+        };
+        auto enter_lane = [&](int k) { // by the lane of token k: what no window has, and begins there, counts
+            Piece p = a.pieces.total(a.q, c.s, 4);
+            const int b = a.q.bound(c.s);
+            const bool no = p.n < 0.0;
+            if (no) p = a.pieces.total(a.q, c.s);
+            entered(c.s, p, b >= k && (no || b >= counted));
+        };
         Mask8 mask;
         mask.read(a.mask, begin + lane * 8, stop, a.vec);
 #pragma unroll 1
@@ -694,46 +782,64 @@ template <int KL> __global__ void __launch_bounds__(kThreads, kPerSm) policy_seq
             if (base == begin) {
                 c.at(a.q, begin, lane);
                 if (a.done) grid_dependency_wait();
-                enter();
+                enter(true);
             }
-            zero8(out);
-            int last = 0;
-            const bool many = c.end < hi && c.many(a.q, hi, lane, last);
-            if (many && k < hi && c.spread(a.q, k, last)) enter_lane(k);
-#pragma unroll 1
-            for (int lo = base;;) {
-                const uint32_t run = c.end >= hi && lo == base ? valid : valid & range_bits(k, lo, c.end);
-                float kls = 0.0f;
+            float wt[8], slopes[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const bool in = run >> e & 1;
-                    float grad = slope_of;
-                    if (KL) {
-                        float value, slope;
-                        kl_term<KL>(r[e] - s[e], a.k2, value, slope);
-                        kls += in ? value : 0.0f;
-                        if (beta != 0.0f) grad = fmaf(beta, slope, grad);
+            for (int e = 0; e < 8; ++e) wt[e] = w, slopes[e] = slope_of;
+            if (c.end < hi) {
+                if (c.inside(hi, lane) > kFew) {
+                    const int last = c.ahead(a.q, hi, lane), rim = min(k + 8, hi);
+                    bool going = false;
+                    if (k < hi) {
+                        const bool moved = c.spread(a.q, k, last);
+                        if (moved) enter_lane(k);
+                        going = moved || c.end < rim;
                     }
-                    if (in) out[e] = grad;
-                }
-                if (KL) v[2] += (double)(w * kls);
-                if (many) {
-                    const bool more = c.end < min(k + 8, hi);
-                    lo = more ? c.end : hi;
-                    if (more) c.next(a.q, last), enter_lane(k);
-                    if (__any_sync(kAll, more)) continue;
+                    int lo = k;
+#pragma unroll 1
+                    while (__any_sync(kAll, going)) {
+                        if (going) {
+                            const uint32_t run = range_bits(k, lo, c.end);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                if (run >> e & 1) wt[e] = w, slopes[e] = slope_of;
+                            going = c.end < rim;
+                            if (going) lo = c.end, c.next(a.q, last), enter_lane(k);
+                        }
+                    }
                     const int from = (hi - 1 - base) >> 3;
-                    c.join(from);
-                    w = __shfl_sync(kAll, w, from);
-                    slope_of = __shfl_sync(kAll, slope_of, from);
-                    beta = __shfl_sync(kAll, beta, from);
+                    const float w_last = __shfl_sync(kAll, w, from), slope_last = __shfl_sync(kAll, slope_of, from);
+                    c.join(a.q, from, lane);
+                    counted = max(counted, c.end);
+                    look();
+                    w = w_last, slope_of = slope_last;
+                } else {
+#pragma unroll 1
+                    while (c.end < hi) {
+                        const int lo = c.end;
+                        enter(c.on(a.q, lo, lane));
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (k + e >= lo) wt[e] = w, slopes[e] = slope_of;
+                    }
                 }
-                if (c.end > hi || c.end >= stop) break;
-                lo = c.end;
-                c.on(a.q, lo, lane);
-                enter();
-                if (lo >= hi) break;
             }
+            float kls = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const bool in = valid >> e & 1;
+                float grad = slopes[e];
+                if (KL) {
+                    float value, slope;
+                    kl_term<KL>(r[e] - s[e], a.k2, value, slope);
+                    kls = in ? fmaf(wt[e], value, kls) : kls;
+                    if (beta != 0.0f) grad = fmaf(beta * wt[e], slope, grad);
+                }
+                out[e] = in ? grad : 0.0f;
+            }
+            if (KL) v[2] += (double)kls;
+            if (c.end <= hi && c.end < stop) enter(c.on(a.q, hi, lane));
             if (a.vec && hi - base == kBlock) store8(a.omega + k, out);
             else store8(a.omega, k, base, hi, a.vec, out);
         }
@@ -790,7 +896,7 @@ __global__ void __launch_bounds__(kThreads) preference_pairs_kernel(const __grid
         };
         bool far = false;
         for (int i = threadIdx.x; i < n; i += kThreads) {
-            const Piece p = a.pieces.total(a.q, (int)(base + i), kThreads);
+            const Piece p = a.pieces.total(a.q, (int)(base + i), 32);
             far |= p.n < 0.0;
             put(i, p);
         }
@@ -871,7 +977,7 @@ __global__ void __launch_bounds__(kThreads, 4) preference_token_kernel(const __g
     const int live = a.q.live(), tokens = a.w.per_warp * kBlock;
     const bool some = (int64_t)share * tokens < live;
     const int begin = some ? share * tokens : 0, stop = some ? min(live - begin, tokens) + begin : 0;
-    Cursor c{0, 0};
+    Cursor c{0, 0, 0, 0};
     constexpr int kAhead = 4; // blocks whose masks are on their way: there is little else to do
     Mask8 mask[kAhead];
 #pragma unroll
@@ -892,9 +998,13 @@ __global__ void __launch_bounds__(kThreads, 4) preference_token_kernel(const __g
     const double scale = inv * (a.grad_loss ? (double)*a.grad_loss : 1.0);
     if (!some)
         return;
-    float coef;
-    auto enter = [&]() { coef = inv > 0.0 ? (float)(__ldcg(a.coef + c.s) * scale) : 0.0f; };
-    enter();
+    float coef, coef_of = 0.0f; // of the sequence, of the window's
+    auto of = [&](int o) { return inv > 0.0 ? (float)(__ldcg(a.coef + o) * scale) : 0.0f; };
+    auto enter = [&](bool other) {
+        if (other && c.first + lane < a.q.n_seq) coef_of = of(c.first + lane);
+        coef = __shfl_sync(kAll, coef_of, c.s - c.first);
+    };
+    enter(true);
 #pragma unroll 1
     for (int first = begin; first < stop; first += kAhead * kBlock) {
         uint32_t valids = 0;
@@ -909,30 +1019,42 @@ __global__ void __launch_bounds__(kThreads, 4) preference_token_kernel(const __g
             const int k = base + lane * 8, hi = min(base + kBlock, stop);
             const uint32_t valid = valids & 0xFFu;
             float out[8];
-            zero8(out);
-            int last = 0;
-            const bool many = c.end < hi && c.many(a.q, hi, lane, last);
-            if (many && k < hi && c.spread(a.q, k, last)) enter();
-#pragma unroll 1
-            for (int lo = base;;) {
-                const uint32_t run = c.end >= hi && lo == base ? valid : valid & range_bits(k, lo, c.end);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) out[e] = run >> e & 1 ? coef : out[e];
-                if (many) {
-                    const bool more = c.end < min(k + 8, hi);
-                    lo = more ? c.end : hi;
-                    if (more) c.next(a.q, last), enter();
-                    if (__any_sync(kAll, more)) continue;
-                    const int from = (hi - 1 - base) >> 3;
-                    c.join(from);
-                    coef = __shfl_sync(kAll, coef, from);
+            for (int e = 0; e < 8; ++e) out[e] = valid >> e & 1 ? coef : 0.0f;
+            if (c.end < hi) {
+                if (c.inside(hi, lane) > kFew) {
+                    const int last = c.ahead(a.q, hi, lane), rim = min(k + 8, hi);
+                    bool going = false;
+                    if (k < hi) {
+                        const bool moved = c.spread(a.q, k, last);
+                        if (moved) coef = of(c.s);
+                        going = moved || c.end < rim;
+                    }
+                    int lo = k;
+#pragma unroll 1
+                    while (__any_sync(kAll, going)) {
+                        if (going) {
+                            const uint32_t run = valid & range_bits(k, lo, c.end);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) out[e] = run >> e & 1 ? coef : out[e];
+                            going = c.end < rim;
+                            if (going) lo = c.end, c.next(a.q, last), coef = of(c.s);
+                        }
+                    }
+                    c.join(a.q, (hi - 1 - base) >> 3, lane);
+                    enter(true);
+                } else {
+#pragma unroll 1
+                    while (c.end < hi) {
+                        const int lo = c.end;
+                        enter(c.on(a.q, lo, lane));
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (k + e >= lo) out[e] = valid >> e & 1 ? coef : 0.0f;
+                    }
                 }
-                if (c.end > hi || c.end >= stop) break;
-                lo = c.end;
-                c.on(a.q, lo, lane);
-                enter();
-                if (lo >= hi) break;
             }
+            if (c.end <= hi && c.end < stop) enter(c.on(a.q, hi, lane));
             if (a.vec && hi - base == kBlock) store8(a.omega + k, out);
             else store8(a.omega, k, base, hi, a.vec, out);
         }
