@@ -1,6 +1,7 @@
 // Advantages and returns by a gated linear recurrence over the valid tokens of a sequence, and the backward pass of it.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "segments.cuh"
 
@@ -379,20 +380,95 @@ template <bool TRACE, bool MOMENTS, bool MAPS> __global__ void __launch_bounds__
                     st = Op::State{0.0, terminal(s)};
                 }
                 Stage *x = feed.mem->stage[slot];
+                float r[8], v[8], c[8];
+                double D[8];
+                auto read = [&]() {
+                    if (a.rewards) read8(x[0], 31 - lane, r);
+                    else zero8(r);
+                    if (!a.values) zero8(v);
+                    else if (a.values_bf16) read8_bf16(x[1], 31 - lane, v);
+                    else read8(x[1], 31 - lane, v);
+                    if (TRACE) read8(x[kTensors - 1], 31 - lane, c);
+                };
+                // Tokens of which some are masked.  CUTS: sequence number j, from the right, is that of the lane's last token but for the ends of
+                // sequences among its tokens; behind number n there is later[n].
+                auto uneven = [&](auto has_cuts, uint32_t ends, int j, const double *later) {
+                    constexpr bool CUTS = decltype(has_cuts)::value;
+                    // masked tokens hold the value that follows them, and leave B and z as they are
+                    float leftmost = v[0];
+#pragma unroll
+                    for (int e = 7; e >= 0; --e)
+                        if (valid >> e & 1) leftmost = v[e];
+                    const uint32_t right = some & ((1u << lane) - 1);
+                    const int near = right ? 31 - __clz(right) : 0;
+                    const float from = __shfl_sync(kAll, leftmost, near);
+                    const int j_left = CUTS && valid ? j + __popc(ends >> (__ffs(valid) - 1)) : 0;
+                    int j_before = CUTS ? __shfl_sync(kAll, j_left, near) : 0; // of the valid token before
+                    if (CUTS && !right) j_before = 0;
+                    uint32_t cuts = 0; // valid tokens that are the last of their sequence
+                    double q = right ? a.gamma * (double)from : st.q;
+                    Line m{1.0, 0.0};
+                    bool apart = MAPS && TRACE && count == 0 && right == 0; // this lane's first weight may be the piece's rightmost
+#pragma unroll
+                    for (int e = 7; e >= 0; --e) {
+                        const bool in = valid >> e & 1;
+                        const double V = (double)v[e];
+                        double w = TRACE ? a.weight * (double)c[e] : a.weight;
+                        if (CUTS) {
+                            j += ends >> e & 1;
+                            if (in && j != j_before) {
+                                q = later[j];
+                                w = 0.0;
+                                cuts |= 1u << e;
+                            }
+                            if (in) j_before = j;
+                        }
+                        D[e] = ((double)r[e] - V) + q;
+                        if (in) m.B = fma(w, m.B, D[e]);
+                        if (in) q = a.gamma * V;
+                        if (TRACE) {
+                            if (in && !apart) m.P *= w;
+                            if (MAPS && in && apart) w_right = w, apart = false;
+                        }
+                    }
+                    if (!TRACE) m.P = CUTS && cuts ? 0.0 : a.small[__popc(valid)];
+                    if (MAPS && TRACE && count == 0) w_right = __shfl_sync(kAll, w_right, __ffs(some) - 1);
+                    const Line before = scan_lines(m, lane);
+                    double z = fma(before.P, st.x, before.B);
+#pragma unroll
+                    for (int e = 7; e >= 0; --e) {
+                        adv[e] = ret[e] = 0.0f;
+                        double w = TRACE ? a.weight * (double)c[e] : a.weight;
+                        if (CUTS && (cuts >> e & 1)) w = 0.0;
+                        if (valid >> e & 1) z = fma(w, z, D[e]);
+                        D[e] = z;
+                        if (valid >> e & 1) adv[e] = (float)z;
+                        if (valid >> e & 1) ret[e] = (float)(z + (double)v[e]);
+                    }
+                    if (MAPS && TRACE) P_all *= __shfl_sync(kAll, m.P, 31);
+                    st.x = __shfl_sync(kAll, z, 31);
+                    st.q = a.gamma * (double)__shfl_sync(kAll, leftmost, 31 - __clz(some));
+                    if (MAPS) count += TRACE ? 1 : (int)__reduce_add_sync(kAll, (unsigned)__popc(valid));
+                    if (MOMENTS) {
+                        // an advantage of the warp's first block: where the lane with the first bit ended
+                        if (!known) shift = __shfl_sync(kAll, z, __ffs(some) - 1), known = true;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const double d = D[e] - shift;
+                            if (valid >> e & 1) sum += d;
+                            if (valid >> e & 1) squares = fma(d, d, squares);
+                        }
+                        n += (double)__popc(valid);
+                    }
+                    return CUTS ? __shfl_sync(kAll, j_left, 31 - __clz(some)) : 0; // number of the sequence of the block's first valid token
+                };
                 if (MAPS || cur <= lo) {
                     if (some == 0) {
                         feed.release(slot, fetch);
                         zero8(adv);
                         zero8(ret);
                     } else {
-                        float r[8], v[8], c[8];
-                        double D[8];
-                        if (a.rewards) read8(x[0], 31 - lane, r);
-                        else zero8(r);
-                        if (!a.values) zero8(v);
-                        else if (a.values_bf16) read8_bf16(x[1], 31 - lane, v);
-                        else read8(x[1], 31 - lane, v);
-                        if (TRACE) read8(x[kTensors - 1], 31 - lane, c);
+                        read();
                         feed.release(slot, fetch);
                         if (!TRACE && __all_sync(kAll, valid == 0xFFu)) { // every lane's P is weight^8
                             const float from = __shfl_up_sync(kAll, v[0], 1);
@@ -428,55 +504,7 @@ template <bool TRACE, bool MOMENTS, bool MAPS> __global__ void __launch_bounds__
                                 n += 8.0;
                             }
                         } else {
-                            // masked tokens hold the value that follows them, and leave B and z as they are
-                            float leftmost = v[0];
-#pragma unroll
-                            for (int e = 7; e >= 0; --e)
-                                if (valid >> e & 1) leftmost = v[e];
-                            const uint32_t right = some & ((1u << lane) - 1);
-                            const float from = __shfl_sync(kAll, leftmost, right ? 31 - __clz(right) : 0);
-                            double q = right ? a.gamma * (double)from : st.q;
-                            Line m{1.0, 0.0};
-                            bool apart = MAPS && TRACE && count == 0 && right == 0; // this lane's first weight may be the piece's rightmost
-#pragma unroll
-                            for (int e = 7; e >= 0; --e) {
-                                const bool in = valid >> e & 1;
-                                const double V = (double)v[e], w = TRACE ? a.weight * (double)c[e] : a.weight;
-                                D[e] = ((double)r[e] - V) + q;
-                                if (in) m.B = fma(w, m.B, D[e]);
-                                if (in) q = a.gamma * V;
-                                if (TRACE) {
-                                    if (in && !apart) m.P *= w;
-                                    if (MAPS && in && apart) w_right = w, apart = false;
-                                }
-                            }
-                            if (!TRACE) m.P = a.small[__popc(valid)];
-                            if (MAPS && TRACE && count == 0) w_right = __shfl_sync(kAll, w_right, __ffs(some) - 1);
-                            const Line before = scan_lines(m, lane);
-                            double z = fma(before.P, st.x, before.B);
-#pragma unroll
-                            for (int e = 7; e >= 0; --e) {
-                                adv[e] = ret[e] = 0.0f;
-                                if (valid >> e & 1) z = fma(TRACE ? a.weight * (double)c[e] : a.weight, z, D[e]);
-                                D[e] = z;
-                                if (valid >> e & 1) adv[e] = (float)z;
-                                if (valid >> e & 1) ret[e] = (float)(z + (double)v[e]);
-                            }
-                            if (MAPS && TRACE) P_all *= __shfl_sync(kAll, m.P, 31);
-                            st.x = __shfl_sync(kAll, z, 31);
-                            st.q = a.gamma * (double)__shfl_sync(kAll, leftmost, 31 - __clz(some));
-                            if (MAPS) count += TRACE ? 1 : (int)__reduce_add_sync(kAll, (unsigned)__popc(valid));
-                            if (MOMENTS) {
-                                // an advantage of the warp's first block: where the lane with the first bit ended
-                                if (!known) shift = __shfl_sync(kAll, z, __ffs(some) - 1), known = true;
-#pragma unroll
-                                for (int e = 0; e < 8; ++e) {
-                                    const double d = D[e] - shift;
-                                    if (valid >> e & 1) sum += d;
-                                    if (valid >> e & 1) squares = fma(d, d, squares);
-                                }
-                                n += (double)__popc(valid);
-                            }
+                            uneven(std::false_type(), 0u, 0, nullptr);
                         }
                     }
                     if (!MAPS) {
@@ -488,7 +516,46 @@ template <bool TRACE, bool MOMENTS, bool MAPS> __global__ void __launch_bounds__
                             if (a.returns) store8(a.returns, k, lo, hi, a.vec, ret);
                         }
                     }
-                } else if (!MAPS) {
+                    continue;
+                }
+                if (MAPS) continue; // parts of one sequence
+                const int begins = s >= lane ? a.q.bound(s - lane) : 0; // sequence s - lane
+                const uint32_t out = __ballot_sync(kAll, begins <= lo);
+                if (out != 0) { // few enough sequences
+                    const int others = __ffs(out) - 1, of = 31 - lane, begins_right = __shfl_up_sync(kAll, begins, 1);
+                    const bool there = lane == 0 || (lane <= others && begins < begins_right); // not empty
+                    const uint32_t there_all = __ballot_sync(kAll, there);
+                    const double q = lane > 0 && there ? terminal(s - lane) : 0.0;
+                    read();
+                    __syncwarp();
+                    double *later = reinterpret_cast<double *>(x[0].x); // what was there has been read
+                    if (there) later[__popc(there_all & ((1u << lane) - 1))] = q;
+                    uint32_t ends = 0;
+                    int j = 0, at_before = -1;
+#pragma unroll 1
+                    for (int i = 0; i < others; ++i) {
+                        const int at = __shfl_sync(kAll, begins, i) - 1 - base;
+                        if (at == at_before) continue;
+                        at_before = at;
+                        if ((at >> 3) == of) ends |= 1u << (at & 7);
+                        j += (at >> 3) > of;
+                    }
+                    s -= others;
+                    cur = __shfl_sync(kAll, begins, others);
+                    __syncwarp();
+                    int j_first = 0;
+                    if (some != 0) {
+                        j_first = uneven(std::true_type(), ends, j, later);
+                    } else {
+                        zero8(adv);
+                        zero8(ret);
+                    }
+                    const int j_last = __popc(there_all) - 1;
+                    if (j_first != j_last) st = Op::State{0.0, later[j_last]};
+                    feed.release(slot, fetch);
+                    if (a.adv) store8(a.adv, k, lo, hi, a.vec, adv);
+                    if (a.returns) store8(a.returns, k, lo, hi, a.vec, ret);
+                } else {
                     const int s_right = s;
                     const uint32_t ends = ends_inside<true>(a.q, base, lo, hi, lane, 31 - lane, s, [](int, int) {});
                     cur = a.q.bound(s);
