@@ -1,5 +1,6 @@
 // Advantages and returns by a gated linear recurrence over the valid tokens of a sequence, and the backward pass of it.
 #include <algorithm>
+#include <climits>
 #include <cmath>
 #include <type_traits>
 
@@ -111,19 +112,19 @@ __device__ __forceinline__ int part_from(const AdvantageArgs &a, int t, int s, i
     return (int)(at < t ? t : (at > live ? live : at)); // boundaries out of order stay inside
 }
 
-// The state behind the maps of `n` pieces, first to last; maps(i) gives the map of piece i.
+// The state behind the maps of `n` pieces, first to last; maps(i) gives the map of piece i.  A lane takes neighbouring ones: one scan of
+// the warp, where a scan for each 32 of them took 14 us for a sequence of 640.
 template <typename Op, typename F> __device__ __forceinline__ typename Op::State behind_pieces(typename Op::State s, int n, int lane, F maps, double &wl)
 {
-#pragma unroll 1
-    for (int done = 0; done < n; done += 32) {
-        typename Op::Map m = Op::identity(), all;
-        if (done + lane < n) m = maps(done + lane);
-        warp_scan<Op>(m, lane, all);
-        all = shfl_words(all, 31);
-        s = Op::apply(all, s);
-        wl = Op::last_weight(all, wl);
-    }
-    return s;
+    if (n <= 0) return s;
+    const int each = (n + 31) / 32, end = min(n, (lane + 1) * each);
+    typename Op::Map m = Op::identity(), all;
+#pragma unroll 2
+    for (int i = lane * each; i < end; ++i) m = Op::then(m, maps(i));
+    warp_scan<Op>(m, lane, all);
+    all = shfl_words(all, 31);
+    wl = Op::last_weight(all, wl);
+    return Op::apply(all, s);
 }
 
 struct Moments { // count, mean and sum of squared deviations of a set of values
@@ -176,16 +177,38 @@ __device__ __forceinline__ Line scan_lines(Line &m, int lane)
     return lane == 0 ? Line{1.0, 0.0} : before;
 }
 
-// The same where every lane's P is powers[0].
-__device__ __forceinline__ double scan_even(double B, const double (&powers)[5], int lane)
+// The same where a lane's tokens may begin anew, so that nothing comes through them, not even what is not finite.
+__device__ __forceinline__ Line scan_cuts(Line &m, bool &cut, int lane)
 {
+#pragma unroll
+    for (int by = 1; by < 32; by *= 2) {
+        const double P = __shfl_up_sync(kAll, m.P, by), B = __shfl_up_sync(kAll, m.B, by);
+        const bool c = __shfl_up_sync(kAll, (int)cut, by);
+        if (lane >= by && !cut) {
+            m.B = fma(m.P, B, m.B);
+            m.P *= P;
+            cut = c;
+        }
+    }
+    Line before;
+    before.P = __shfl_up_sync(kAll, m.P, 1);
+    before.B = __shfl_up_sync(kAll, m.B, 1);
+    cut = __shfl_up_sync(kAll, (int)cut, 1);
+    if (lane == 0) cut = false;
+    return lane == 0 ? Line{1.0, 0.0} : before;
+}
+
+// The same where every lane's P is powers[0], with x before the first lane.
+__device__ __forceinline__ double scan_even(double B, const double (&powers)[5], int lane, double x)
+{
+    if (lane == 0) B = fma(powers[0], x, B);
 #pragma unroll
     for (int i = 0; i < 5; ++i) {
         const double before = __shfl_up_sync(kAll, B, 1 << i);
         if (lane >= (1 << i)) B = fma(powers[i], before, B);
     }
     const double before = __shfl_up_sync(kAll, B, 1);
-    return lane == 0 ? 0.0 : before;
+    return lane == 0 ? x : before;
 }
 
 // A warp's way through the blocks of 256 tokens of [begin, end), from the last to the first (BACK: lane 0 has the last eight) or from
@@ -266,32 +289,6 @@ template <bool BACK, int TENSORS> struct Feed {
     }
 };
 
-// A block's tokens that end their sequence, with another beginning inside (lo, hi): bits of the eight tokens of block place `of`.
-// Sequences are walked from `s` on, up or down, and s becomes the one that holds the block's last (first) token.
-template <bool BACK, typename F>
-__device__ __forceinline__ uint32_t ends_inside(const Sequences &q, int base, int lo, int hi, int lane, int of, int &s, F passed)
-{
-    uint32_t mine = 0;
-    for (;;) {
-        const int64_t o = (int64_t)s + (BACK ? -lane : lane);
-        // the token at which sequence o (BACK) or the one behind it begins
-        const int p = BACK ? (o >= 0 ? q.bound((int)o) : 0) : (o < q.n_seq ? q.bound((int)o + 1) : 0x7FFFFFFF);
-        const uint32_t out = __ballot_sync(kAll, BACK ? p <= lo : p >= hi);
-        const int n = out ? __ffs(out) - 1 : 32;
-        if (lane < n) passed((int)o, p);
-#pragma unroll 1
-        for (int j = 0; j < n; ++j) {
-            const int at = __shfl_sync(kAll, p, j) - 1 - base;
-            if ((at >> 3) == of) mine |= 1u << (at & 7);
-        }
-        s += BACK ? -n : n;
-        if (out) break;
-    }
-    if (s < 0) s = 0;
-    if (s >= q.n_seq) s = (int)q.n_seq - 1;
-    return mine;
-}
-
 // MAPS: the map of the piece that begins in the chunk and is not its sequence's first.  Otherwise the outputs.
 //   Blocks inside one sequence (nearly all): a lane's rightmost valid token takes the discounted value that follows it from the
 //   nearest lane to the right, so that each lane's tokens are x' = P x + B; a scan of these gives every lane what comes in.
@@ -302,12 +299,14 @@ template <bool TRACE, bool MOMENTS, bool MAPS> __global__ void __launch_bounds__
     constexpr int kTensors = TRACE ? 3 : 2;
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ Moments joined[kAdvWarps];
+    __shared__ uint32_t ends_of[kAdvWarps][kBlock / 32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, chunk = blockIdx.x * kAdvWarps + warp;
     if (MAPS || !a.second) grid_dependency_wait();
     grid_dependency_release();
     const int live = a.q.live();
-    double n = 0.0, shift = 0.0, sum = 0.0, squares = 0.0; // moments about a value of the warp's own,
-    bool known = false;                                    // once there is one
+    double shift = 0.0, sum = 0.0, squares = 0.0; // moments about a value of the warp's own,
+    bool known = false;                           // once there is one
+    int taken = 0;                                // of so many
     if (chunk < a.chunks && (int64_t)chunk * a.chunk < live) {
         const int t0 = chunk * a.chunk, t1 = min(live - t0, a.chunk) + t0;
         int s, s1, begin = 0, end = 0, cur = 0; // cur: where the current sequence begins
@@ -362,11 +361,8 @@ template <bool TRACE, bool MOMENTS, bool MAPS> __global__ void __launch_bounds__
                     const int far = behind - 1 - i;
                     return static_cast<const Op::Map *>(a.maps)[a.even ? chunk + 1 + far : (end + ((int64_t)far << a.piece)) / a.chunk]; }, none);
             }
-            double P_all = 1.0, w_right = a.weight, ahead = 1.0; // MAPS: product of the weights but the rightmost one's, and that; weight^(8 lane)
+            double P_all = 1.0, w_right = a.weight; // MAPS: product of the weights but the rightmost one's, and that
             int count = 0;
-            if (!TRACE)
-                for (int i = 0; i < 5; ++i)
-                    if (lane >> i & 1) ahead *= a.powers[i];
             int slot = 0;
 #pragma unroll 1
             for (; feed.left > 0; feed.next(), slot = slot + 1 == kStages ? 0 : slot + 1) {
@@ -413,12 +409,12 @@ template <bool TRACE, bool MOMENTS, bool MAPS> __global__ void __launch_bounds__
                     for (int e = 7; e >= 0; --e) {
                         const bool in = valid >> e & 1;
                         const double V = (double)v[e];
-                        double w = TRACE ? a.weight * (double)c[e] : a.weight;
+                        const double w = TRACE ? a.weight * (double)c[e] : a.weight;
                         if (CUTS) {
                             j += ends >> e & 1;
                             if (in && j != j_before) {
                                 q = later[j];
-                                w = 0.0;
+                                m.B = 0.0;
                                 cuts |= 1u << e;
                             }
                             if (in) j_before = j;
@@ -431,16 +427,16 @@ template <bool TRACE, bool MOMENTS, bool MAPS> __global__ void __launch_bounds__
                             if (MAPS && in && apart) w_right = w, apart = false;
                         }
                     }
-                    if (!TRACE) m.P = CUTS && cuts ? 0.0 : a.small[__popc(valid)];
+                    if (!TRACE) m.P = a.small[__popc(valid)];
                     if (MAPS && TRACE && count == 0) w_right = __shfl_sync(kAll, w_right, __ffs(some) - 1);
-                    const Line before = scan_lines(m, lane);
-                    double z = fma(before.P, st.x, before.B);
+                    bool cut = cuts != 0;
+                    const Line before = CUTS ? scan_cuts(m, cut, lane) : scan_lines(m, lane);
+                    double z = CUTS && cut ? before.B : fma(before.P, st.x, before.B);
 #pragma unroll
                     for (int e = 7; e >= 0; --e) {
                         adv[e] = ret[e] = 0.0f;
-                        double w = TRACE ? a.weight * (double)c[e] : a.weight;
-                        if (CUTS && (cuts >> e & 1)) w = 0.0;
-                        if (valid >> e & 1) z = fma(w, z, D[e]);
+                        if (CUTS && (cuts >> e & 1)) z = 0.0;
+                        if (valid >> e & 1) z = fma(TRACE ? a.weight * (double)c[e] : a.weight, z, D[e]);
                         D[e] = z;
                         if (valid >> e & 1) adv[e] = (float)z;
                         if (valid >> e & 1) ret[e] = (float)(z + (double)v[e]);
@@ -458,7 +454,7 @@ template <bool TRACE, bool MOMENTS, bool MAPS> __global__ void __launch_bounds__
                             if (valid >> e & 1) sum += d;
                             if (valid >> e & 1) squares = fma(d, d, squares);
                         }
-                        n += (double)__popc(valid);
+                        taken += __popc(valid);
                     }
                     return CUTS ? __shfl_sync(kAll, j_left, 31 - __clz(some)) : 0; // number of the sequence of the block's first valid token
                 };
@@ -480,7 +476,7 @@ template <bool TRACE, bool MOMENTS, bool MAPS> __global__ void __launch_bounds__
                                 q = a.gamma * V;
                                 B = fma(a.weight, B, D[e]);
                             }
-                            double z = fma(ahead, st.x, scan_even(B, a.powers, lane));
+                            double z = scan_even(B, a.powers, lane, st.x);
 #pragma unroll
                             for (int e = 7; e >= 0; --e) {
                                 D[e] = z = fma(a.weight, z, D[e]);
@@ -501,7 +497,7 @@ template <bool TRACE, bool MOMENTS, bool MAPS> __global__ void __launch_bounds__
                                 }
                                 sum += s1[0] + s1[1];
                                 squares += s2[0] + s2[1];
-                                n += 8.0;
+                                taken += 8;
                             }
                         } else {
                             uneven(std::false_type(), 0u, 0, nullptr);
@@ -519,106 +515,47 @@ template <bool TRACE, bool MOMENTS, bool MAPS> __global__ void __launch_bounds__
                     continue;
                 }
                 if (MAPS) continue; // parts of one sequence
-                const int begins = s >= lane ? a.q.bound(s - lane) : 0; // sequence s - lane
-                const uint32_t out = __ballot_sync(kAll, begins <= lo);
-                if (out != 0) { // few enough sequences
-                    const int others = __ffs(out) - 1, of = 31 - lane, begins_right = __shfl_up_sync(kAll, begins, 1);
-                    const bool there = lane == 0 || (lane <= others && begins < begins_right); // not empty
+                // Sequences end inside, number 0 (from the right) is s.  The state behind each goes into memory that the tensors have left.
+                read();
+                uint32_t *bits = ends_of[warp];
+                if (lane < kBlock / 32) bits[lane] = 0;
+                __syncwarp();
+                double *later = reinterpret_cast<double *>(x[0].x);
+                int numbers = 0, right = 0x7FFFFFFF, others;
+                for (;; s -= 32) {
+                    const int o = s - lane, begins = o >= 0 ? a.q.bound(o) : 0;
+                    int next = __shfl_up_sync(kAll, begins, 1);
+                    if (lane == 0) next = right;
+                    const uint32_t out = __ballot_sync(kAll, begins <= lo);
+                    others = out ? __ffs(out) - 1 : 32;
+                    const bool there = lane <= others && begins < next; // not empty
                     const uint32_t there_all = __ballot_sync(kAll, there);
-                    const double q = lane > 0 && there ? terminal(s - lane) : 0.0;
-                    read();
-                    __syncwarp();
-                    double *later = reinterpret_cast<double *>(x[0].x); // what was there has been read
-                    if (there) later[__popc(there_all & ((1u << lane) - 1))] = q;
-                    uint32_t ends = 0;
-                    int j = 0, at_before = -1;
-#pragma unroll 1
-                    for (int i = 0; i < others; ++i) {
-                        const int at = __shfl_sync(kAll, begins, i) - 1 - base;
-                        if (at == at_before) continue;
-                        at_before = at;
-                        if ((at >> 3) == of) ends |= 1u << (at & 7);
-                        j += (at >> 3) > of;
+                    if (there) later[min(numbers + __popc(there_all & ((1u << lane) - 1)), kBlock - 1)] = terminal(max(o, 0));
+                    if (there && lane < others && begins <= hi) atomicOr(&bits[(begins - 1 - base) >> 5], 1u << ((begins - 1 - base) & 31));
+                    numbers += __popc(there_all);
+                    right = __shfl_sync(kAll, begins, 31);
+                    if (out) {
+                        cur = __shfl_sync(kAll, begins, others);
+                        break;
                     }
-                    s -= others;
-                    cur = __shfl_sync(kAll, begins, others);
-                    __syncwarp();
-                    int j_first = 0;
-                    if (some != 0) {
-                        j_first = uneven(std::true_type(), ends, j, later);
-                    } else {
-                        zero8(adv);
-                        zero8(ret);
-                    }
-                    const int j_last = __popc(there_all) - 1;
-                    if (j_first != j_last) st = Op::State{0.0, later[j_last]};
-                    feed.release(slot, fetch);
-                    if (a.adv) store8(a.adv, k, lo, hi, a.vec, adv);
-                    if (a.returns) store8(a.returns, k, lo, hi, a.vec, ret);
-                } else {
-                    const int s_right = s;
-                    const uint32_t ends = ends_inside<true>(a.q, base, lo, hi, lane, 31 - lane, s, [](int, int) {});
-                    cur = a.q.bound(s);
-                    auto number = [&](int tensor, int e) -> float { return stage_at(x[tensor], feed.off + e); };
-                    if (a.values && a.values_bf16) widen(x[1], lane);
-                    auto advantage = [&](int e, double &d, double &V, double &w) {
-                        V = a.values ? (double)number(1, e) : 0.0;
-                        d = (a.rewards ? (double)number(0, e) : 0.0) - V;
-                        w = TRACE ? a.weight * (double)number(kTensors - 1, e) : a.weight;
-                    };
-                    Op::Map mine = Op::identity();
-                    double d, V, w;
-#pragma unroll 1
-                    for (int e = 7; e >= 0; --e) {
-                        if (ends >> e & 1) mine = Op::Map{0.0, 0.0, 0.0, terminal(a.q.owner(k + e, s, s_right)), 2u, 0u};
-                        if (valid >> e & 1) {
-                            advantage(e, d, V, w);
-                            if (mine.flag == 0) mine = Op::Map{w, 1.0, d, a.gamma * V, 1u, 0u};
-                            else mine = Op::Map{w * mine.P, w * mine.Q, fma(w, mine.B, d + mine.c), a.gamma * V, mine.flag, 0u};
-                        }
-                    }
-                    Op::Map all;
-                    const Op::Map before = warp_scan<Op>(mine, lane, all);
-                    Op::State z = Op::apply(before, st);
-                    double own = shift, m0 = 0.0, m1 = 0.0, m2 = 0.0; // about the lane's first advantage while the warp has none
-#pragma unroll 1
-                    for (int e = 7; e >= 0; --e) {
-                        if (ends >> e & 1) z = Op::State{0.0, terminal(a.q.owner(k + e, s, s_right))};
-                        float A = 0.0f, R = 0.0f;
-                        if (valid >> e & 1) {
-                            advantage(e, d, V, w);
-                            z.x = fma(w, z.x, d + z.q);
-                            z.q = a.gamma * V;
-                            A = (float)z.x;
-                            R = (float)(z.x + V);
-                            if (MOMENTS) {
-                                if (!known && m0 == 0.0) own = z.x;
-                                const double o = z.x - own;
-                                m0 += 1.0;
-                                m1 += o;
-                                m2 = fma(o, o, m2);
-                            }
-                        }
-                        stage_at(x[0], feed.off + e) = A;
-                        stage_at(x[1], feed.off + e) = R;
-                    }
-                    if (MOMENTS && some != 0) {
-                        if (!known) shift = __shfl_sync(kAll, own, __ffs(some) - 1), known = true;
-                        const double d0 = own - shift;
-                        if (m0 > 0.0) {
-                            n += m0;
-                            squares += m2 + d0 * (2.0 * m1 + m0 * d0);
-                            sum += m1 + m0 * d0;
-                        }
-                    }
-                    st = shfl_words(z, 31);
-                    __syncwarp();
-                    read8(x[0], 31 - lane, adv);
-                    read8(x[1], 31 - lane, ret);
-                    feed.release(slot, fetch);
-                    if (a.adv) store8(a.adv, k, lo, hi, a.vec, adv);
-                    if (a.returns) store8(a.returns, k, lo, hi, a.vec, ret);
                 }
+                s = max(s - others, 0);
+                __syncwarp();
+                const uint32_t word = bits[feed.off >> 5], ends = word >> (feed.off & 31) & 0xFFu;
+                int j = __popc(word >> (feed.off & 31) >> 8); // ends behind the lane's tokens
+                for (int i = (feed.off >> 5) + 1; i < kBlock / 32; ++i) j += __popc(bits[i]);
+                int j_first = 0;
+                if (some != 0) {
+                    j_first = uneven(std::true_type(), ends, j, later);
+                } else {
+                    zero8(adv);
+                    zero8(ret);
+                }
+                numbers = min(numbers, kBlock) - 1;
+                if (j_first != numbers) st = Op::State{0.0, later[numbers]};
+                feed.release(slot, fetch);
+                if (a.adv) store8(a.adv, k, lo, hi, a.vec, adv);
+                if (a.returns) store8(a.returns, k, lo, hi, a.vec, ret);
             }
             if (MAPS && lane == 0) {
                 // x' = Q (w x + q) + B,  q' = c
@@ -629,7 +566,7 @@ template <bool TRACE, bool MOMENTS, bool MAPS> __global__ void __launch_bounds__
     }
     if (!MAPS && a.second) grid_dependency_wait(); // no CTA ends before the maps' launch has
     if (MOMENTS) {
-        n = warp_sum(n);
+        const double n = (double)__reduce_add_sync(kAll, (unsigned)taken);
         sum = warp_sum(sum);
         squares = warp_sum(squares);
         if (lane == 0) joined[warp] = n > 0.0 ? Moments{n, shift + sum / n, squares - sum * sum / n} : Moments{0.0, 0.0, 0.0};
@@ -675,11 +612,12 @@ constexpr int kGradWarps = kGradThreads / 32;
 // valid token takes the weight of the valid token before it from the nearest lane to the left.  d c of a token needs the advantage
 // of its follower: where that is in a later block, the token stays open until then.
 template <bool TRACE, bool BY_TRACE, bool MAPS>
-__global__ void __launch_bounds__(kGradThreads, TRACE || BY_TRACE ? 5 : 8) advantage_grad_kernel(const __grid_constant__ AdvantageArgs a)
+__global__ void __launch_bounds__(kGradThreads, BY_TRACE ? 4 : (TRACE ? 5 : 8)) advantage_grad_kernel(const __grid_constant__ AdvantageArgs a)
 {
     using Op = AdvantageGradOp;
     constexpr int kTensors = 2 + TRACE + BY_TRACE;
     extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ uint32_t ends_of[kGradWarps][kBlock / 32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, chunk = blockIdx.x * kGradWarps + warp;
     if (MAPS || !a.second) grid_dependency_wait();
     grid_dependency_release();
@@ -766,11 +704,8 @@ __global__ void __launch_bounds__(kGradThreads, TRACE || BY_TRACE ? 5 : 8) advan
         st = Op::start();
         w_before = 0.0;
     };
-    double P_all = 1.0, ahead = 1.0; // MAPS: product of the weights but the last one's; weight^(8 lane)
+    double P_all = 1.0; // MAPS: product of the weights but the last one's
     int count = 0;
-    if (!TRACE)
-        for (int i = 0; i < 5; ++i)
-            if (lane >> i & 1) ahead *= a.powers[i];
     int slot = 0;
 #pragma unroll 1
     for (; feed.left > 0; feed.next(), slot = slot + 1 == kStages ? 0 : slot + 1) {
@@ -781,6 +716,128 @@ __global__ void __launch_bounds__(kGradThreads, TRACE || BY_TRACE ? 5 : 8) advan
         Stage *x = feed.mem->stage[slot];
         float dr[8], dv[8], dc[8];
         int open = -1; // this lane's token that waits for its follower
+        float ga[8], gr[8], c[8], A[8];
+        double g[8];
+        auto read = [&]() {
+            if (a.grad_adv) read8(x[0], lane, ga);
+            else zero8(ga);
+            if (a.grad_returns) read8(x[1], lane, gr);
+            else zero8(gr);
+            if (TRACE) read8(x[2], lane, c);
+            if (BY_TRACE) read8(x[kTensors - 1], lane, A);
+        };
+        auto store = [&]() {
+            if (a.vec && hi - lo == kBlock) {
+                if (a.grad_rewards) store8(a.grad_rewards + k, dr);
+                if (a.grad_values) store8(a.grad_values + k, dv);
+            } else {
+                if (a.grad_rewards) store8(a.grad_rewards, k, lo, hi, a.vec, dr);
+                if (a.grad_values) store8(a.grad_values, k, lo, hi, a.vec, dv);
+            }
+            if (BY_TRACE) {
+                if (open < 0) store8(a.grad_trace, k, lo, hi, a.vec, dc);
+                else
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (k + e >= lo && k + e < hi && k + e != open) a.grad_trace[k + e] = dc[e];
+            }
+        };
+        // The gradient by the trace of the block's tokens, whose own gradients are in g.  CUTS: as below, n the number of the last sequence.
+        auto by_trace = [&](auto has_cuts, uint32_t ends, int j, int n) {
+            constexpr bool CUTS = decltype(has_cuts)::value;
+            const uint32_t left = some & ((1u << lane) - 1), right = lane == 31 ? 0u : some & (0xFFFFFFFEu << lane);
+            float first_A = 0.0f;
+#pragma unroll
+            for (int e = 7; e >= 0; --e) first_A = valid >> e & 1 ? A[e] : first_A;
+            const int j_first = CUTS && valid ? j + __popc(ends & ((1u << (__ffs(valid) - 1)) - 1)) : 0;
+            if (!left && valid && st.pos >= 0) // the token left open by a block before
+                a.grad_trace[st.pos] = CUTS && j_first != 0 ? 0.0f : (float)(a.weight * (double)first_A * st.G);
+            const int near = right ? __ffs(right) - 1 : 0;
+            float next_A = __shfl_sync(kAll, first_A, near);
+            int j_next = CUTS ? __shfl_sync(kAll, j_first, near) : 0;
+            bool known = right != 0;
+#pragma unroll
+            for (int e = 7; e >= 0; --e) {
+                const bool in = valid >> e & 1;
+                const int j_of = CUTS ? j + __popc(ends & ((1u << e) - 1)) : 0;
+                dc[e] = in && (!CUTS || (known && j_next == j_of)) ? (float)(a.weight * (double)next_A * g[e]) : 0.0f;
+                if (in && !known && (!CUTS || j_of == n)) open = k + e;
+                if (in) next_A = A[e], j_next = j_of;
+                known = known || in;
+            }
+        };
+        // Tokens of which some are masked.  CUTS: `ends` are those of the lane's tokens that end their sequence, the first of them is of sequence
+        // number j, counted from the left; the last gradient of number j, if it ends, goes to lasts[j].
+        auto uneven = [&](auto has_cuts, uint32_t ends, int j, double *lasts) {
+            constexpr bool CUTS = decltype(has_cuts)::value;
+            const uint32_t left = some & ((1u << lane) - 1);
+            const int from = left ? 31 - __clz(left) : 0, tail = 31 - __clz(some);
+            double w_in = a.weight;
+            if (TRACE) {
+                float c_last = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) c_last = valid >> e & 1 ? c[e] : c_last;
+                const float before = __shfl_sync(kAll, c_last, from);
+                w_in = left ? a.weight * (double)before : w_before;
+                w_before = a.weight * (double)__shfl_sync(kAll, c_last, tail);
+            }
+            const int j_last = CUTS && valid ? j + __popc(ends & ((1u << (31 - __clz(valid))) - 1)) : 0;
+            int j_before = CUTS ? __shfl_sync(kAll, j_last, from) : 0; // of the valid token before
+            if (CUTS && !left) j_before = 0;
+            const int j_in = j_before;
+            int j_now = j;
+            uint32_t cuts = 0; // valid tokens that are the first of their sequence
+            Line m{1.0, 0.0};
+            double w = MAPS && TRACE && count == 0 && !left ? 1.0 : w_in; // the weight of what comes into the piece is applied to it before
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const bool in = valid >> e & 1;
+                if (CUTS && in && j_now != j_before) cuts |= 1u << e, m.B = w = 0.0;
+                if (CUTS && in) j_before = j_now;
+                if (CUTS) j_now += ends >> e & 1;
+                const double sum = (double)ga[e] + (double)gr[e], B = fma(w, m.B, sum);
+                if (!CUTS) g[e] = sum;
+                m.B = in ? B : m.B;
+                if (TRACE) {
+                    const double P = w * m.P;
+                    m.P = in ? P : m.P;
+                    w = in ? a.weight * (double)c[e] : w;
+                } else if (CUTS) {
+                    w = a.weight;
+                }
+            }
+            if (!TRACE) m.P = a.small[__popc(valid)];
+            bool cut = cuts != 0;
+            const Line before = CUTS ? scan_cuts(m, cut, lane) : scan_lines(m, lane);
+            double G = CUTS && cut ? before.B : fma(before.P, st.G, before.B);
+            if (MAPS && TRACE) P_all *= __shfl_sync(kAll, m.P, 31);
+            w = w_in;
+            j_before = j_in;
+            if (CUTS) { // once more, as registers to hold it would cost all blocks
+                __syncwarp();
+                read();
+                __syncwarp();
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const bool in = valid >> e & 1;
+                if (CUTS && (cuts >> e & 1)) G = w = 0.0;
+                const double now = fma(w, G, CUTS ? (double)ga[e] + (double)gr[e] : g[e]);
+                dr[e] = in ? (float)now : 0.0f;
+                dv[e] = in ? (float)(fma(a.gamma, G, (double)gr[e]) - now) : 0.0f;
+                g[e] = now;
+                G = in ? now : G;
+                if (TRACE) w = in ? a.weight * (double)c[e] : w;
+                else if (CUTS) w = a.weight;
+                if (CUTS) {
+                    if (in) j_before = j;
+                    if (ends >> e & 1) lasts[min(j, kBlock - 1)] = j_before == j ? G : 0.0, ++j;
+                }
+            }
+            st.G = __shfl_sync(kAll, G, tail);
+            return CUTS ? __shfl_sync(kAll, j_last, tail) : 0; // number of the sequence of the block's last valid token
+        };
+        const int last_of = valid ? k + 31 - __clz(valid) : -1;
         if (MAPS || e_cur >= hi) {
             if (some == 0) {
                 feed.release(slot, fetch);
@@ -788,17 +845,8 @@ __global__ void __launch_bounds__(kGradThreads, TRACE || BY_TRACE ? 5 : 8) advan
                 zero8(dv);
                 if (BY_TRACE) zero8(dc);
             } else {
-                float ga[8], gr[8], c[8], A[8];
-                if (a.grad_adv) read8(x[0], lane, ga);
-                else zero8(ga);
-                if (a.grad_returns) read8(x[1], lane, gr);
-                else zero8(gr);
-                if (TRACE) read8(x[2], lane, c);
-                if (BY_TRACE) read8(x[kTensors - 1], lane, A);
+                read();
                 feed.release(slot, fetch);
-                const uint32_t left = some & ((1u << lane) - 1);
-                const int from = left ? 31 - __clz(left) : 0, tail = 31 - __clz(some);
-                double g[8], G;
                 if (!TRACE && __all_sync(kAll, valid == 0xFFu)) { // every lane's P is weight^8
                     double B = 0.0;
 #pragma unroll
@@ -806,7 +854,7 @@ __global__ void __launch_bounds__(kGradThreads, TRACE || BY_TRACE ? 5 : 8) advan
                         g[e] = (double)ga[e] + (double)gr[e];
                         B = fma(a.weight, B, g[e]);
                     }
-                    G = fma(ahead, st.G, scan_even(B, a.powers, lane));
+                    double G = scan_even(B, a.powers, lane, st.G);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const double now = fma(a.weight, G, g[e]);
@@ -814,143 +862,91 @@ __global__ void __launch_bounds__(kGradThreads, TRACE || BY_TRACE ? 5 : 8) advan
                         dv[e] = (float)(fma(a.gamma, G, (double)gr[e]) - now);
                         G = g[e] = now;
                     }
+                    if (BY_TRACE && !MAPS) by_trace(std::false_type(), 0u, 0, 0);
+                    st.G = __shfl_sync(kAll, G, 31);
                 } else {
-                    double w_in = a.weight;
-                    if (TRACE) {
-                        float c_last = 0.0f;
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) c_last = valid >> e & 1 ? c[e] : c_last;
-                        const float before = __shfl_sync(kAll, c_last, from);
-                        w_in = left ? a.weight * (double)before : w_before;
-                        w_before = a.weight * (double)__shfl_sync(kAll, c_last, tail);
-                    }
-                    Line m{1.0, 0.0};
-                    double w = MAPS && TRACE && count == 0 && !left ? 1.0 : w_in; // the weight of what comes into the piece is applied to it before
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const bool in = valid >> e & 1;
-                        g[e] = (double)ga[e] + (double)gr[e];
-                        const double B = fma(w, m.B, g[e]);
-                        m.B = in ? B : m.B;
-                        if (TRACE) {
-                            const double P = w * m.P;
-                            m.P = in ? P : m.P;
-                            w = in ? a.weight * (double)c[e] : w;
-                        }
-                    }
-                    if (!TRACE) m.P = a.small[__popc(valid)];
-                    const Line before = scan_lines(m, lane);
-                    G = fma(before.P, st.G, before.B);
-                    if (MAPS && TRACE) P_all *= __shfl_sync(kAll, m.P, 31);
-                    w = w_in;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const bool in = valid >> e & 1;
-                        const double now = fma(w, G, g[e]);
-                        dr[e] = in ? (float)now : 0.0f;
-                        dv[e] = in ? (float)(fma(a.gamma, G, (double)gr[e]) - now) : 0.0f;
-                        g[e] = now;
-                        G = in ? now : G;
-                        if (TRACE) w = in ? a.weight * (double)c[e] : w;
+                    const double G_before = st.G;
+                    uneven(std::false_type(), 0u, 0, nullptr);
+                    if (BY_TRACE && !MAPS) {
+                        const double G_now = st.G;
+                        st.G = G_before;
+                        by_trace(std::false_type(), 0u, 0, 0);
+                        st.G = G_now;
                     }
                 }
-                const int last_of = valid ? k + 31 - __clz(valid) : -1;
-                if (BY_TRACE && !MAPS) {
-                    float first_A = 0.0f;
-#pragma unroll
-                    for (int e = 7; e >= 0; --e) first_A = valid >> e & 1 ? A[e] : first_A;
-                    if (!left && valid && st.pos >= 0) // the token left open by a block before
-                        a.grad_trace[st.pos] = (float)(a.weight * (double)first_A * st.G);
-                    const uint32_t right = lane == 31 ? 0u : some & (0xFFFFFFFEu << lane);
-                    float next_A = __shfl_sync(kAll, first_A, right ? __ffs(right) - 1 : 0);
-                    bool known = right != 0;
-#pragma unroll
-                    for (int e = 7; e >= 0; --e) {
-                        const bool in = valid >> e & 1;
-                        dc[e] = in ? (float)(a.weight * (double)next_A * g[e]) : 0.0f;
-                        if (in && !known) open = k + e;
-                        next_A = in ? A[e] : next_A;
-                        known = known || in;
-                    }
-                }
-                st.G = __shfl_sync(kAll, G, tail);
-                st.pos = __shfl_sync(kAll, last_of, tail);
+                st.pos = __shfl_sync(kAll, last_of, 31 - __clz(some));
                 if (MAPS) count += TRACE ? 1 : (int)__reduce_add_sync(kAll, (unsigned)__popc(valid));
             }
-            if (!MAPS) {
-                if (a.vec && hi - lo == kBlock) {
-                    if (a.grad_rewards) store8(a.grad_rewards + k, dr);
-                    if (a.grad_values) store8(a.grad_values + k, dv);
-                } else {
-                    if (a.grad_rewards) store8(a.grad_rewards, k, lo, hi, a.vec, dr);
-                    if (a.grad_values) store8(a.grad_values, k, lo, hi, a.vec, dv);
-                }
-                if (BY_TRACE) {
-                    if (open < 0) store8(a.grad_trace, k, lo, hi, a.vec, dc);
-                    else
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if (k + e >= lo && k + e < hi && k + e != open) a.grad_trace[k + e] = dc[e];
-                }
-            }
-        } else if (!MAPS) { // sequences end inside
-            const int s_left = s;
-            const uint32_t ends = ends_inside<false>(a.q, base, lo, hi, lane, lane, s, [&](int o, int p) {
-                if (per_sequence && p <= a.q.bound(o)) put(o, 0.0);
-            });
-            e_cur = a.q.bound(s + 1);
-            if (e_cur < hi) e_cur = live; // boundaries out of order
-            auto number = [&](int tensor, int e) -> double { return (double)stage_at(x[tensor], feed.off + e); };
-            auto token = [&](int e, double &g, double &r, double &w) {
-                r = a.grad_returns ? number(1, e) : 0.0;
-                g = (a.grad_adv ? number(0, e) : 0.0) + r;
-                w = TRACE ? a.weight * number(2, e) : a.weight;
-            };
-            Op::Map mine = Op::identity();
-            double g, r, w;
-#pragma unroll 1
-            for (int e = 0; e < 8; ++e) {
-                if (valid >> e & 1) {
-                    token(e, g, r, w);
-                    if (mine.flag == 0) mine = Op::Map{1.0, g, w, k + e, 1u};
-                    else mine = Op::Map{mine.wl * mine.P, fma(mine.wl, mine.B, g), w, k + e, mine.flag};
-                }
-                if (ends >> e & 1) mine = Op::Map{0.0, 0.0, 0.0, -1, 2u};
-            }
-            Op::Map all;
-            const Op::Map before = warp_scan<Op>(mine, lane, all);
-            st.y = (TRACE ? w_before : a.weight) * st.G;
-            Op::State z = Op::apply(before, st);
-#pragma unroll 1
-            for (int e = 0; e < 8; ++e) {
-                float R = 0.0f, V = 0.0f;
-                if (valid >> e & 1) {
-                    token(e, g, r, w);
-                    const double G = g + z.y;
-                    if (BY_TRACE && z.pos >= 0) a.grad_trace[z.pos] = (float)(a.weight * number(kTensors - 1, e) * z.G);
-                    R = (float)G;
-                    V = (float)(fma(a.gamma, z.G, r) - G);
-                    z = Op::State{w * G, G, k + e, 0};
-                } else if (BY_TRACE && k + e >= lo && k + e < hi) {
-                    a.grad_trace[k + e] = 0.0f;
-                }
-                if (ends >> e & 1) {
-                    if (BY_TRACE && z.pos >= 0) a.grad_trace[z.pos] = 0.0f;
-                    if (per_sequence) put(a.q.owner(k + e, s_left, s), z.G);
-                    z = Op::start();
-                }
-                stage_at(x[0], feed.off + e) = R;
-                stage_at(x[1], feed.off + e) = V;
-            }
-            st = shfl_words(z, 31);
-            w_before = Op::last_weight(shfl_words(all, 31), w_before);
-            __syncwarp();
-            read8(x[0], lane, dr);
-            read8(x[1], lane, dv);
-            feed.release(slot, fetch);
-            if (a.grad_rewards) store8(a.grad_rewards, k, lo, hi, a.vec, dr);
-            if (a.grad_values) store8(a.grad_values, k, lo, hi, a.vec, dv);
+            if (!MAPS) store();
+            continue;
         }
+        if (MAPS) continue; // parts of one sequence
+        // Sequences end inside, number 0 (from the left) is s.
+        uint32_t *bits = ends_of[warp];
+        if (lane < kBlock / 32) bits[lane] = 0;
+        __syncwarp();
+        const int s_left = s;
+        int numbers = 0, others;
+        // all of them: f(sequence, its number, whether it ends inside, where) by a lane of each that is not empty, and empty(sequence)
+        auto each = [&](auto f, auto empty) {
+            numbers = 0;
+            int left = INT_MIN;
+            for (int from = s_left;; from += 32) {
+                const int64_t o = (int64_t)from + lane;
+                const int behind = o < a.q.n_seq ? a.q.bound((int)o + 1) : 0x7FFFFFFF;
+                int before = __shfl_up_sync(kAll, behind, 1);
+                if (lane == 0) before = left;
+                const uint32_t out = __ballot_sync(kAll, behind >= hi);
+                others = out ? __ffs(out) - 1 : 32;
+                const bool there = lane <= others && behind > before;
+                const uint32_t there_all = __ballot_sync(kAll, there);
+                if (there) f((int)o, min(numbers + __popc(there_all & ((1u << lane) - 1)), kBlock - 1), lane < others, behind);
+                else if (lane < others) empty((int)o);
+                numbers += __popc(there_all);
+                left = __shfl_sync(kAll, behind, 31);
+                if (out) {
+                    s = (int)min((int64_t)from + others, a.q.n_seq - 1);
+                    e_cur = __shfl_sync(kAll, behind, others);
+                    if (e_cur == 0x7FFFFFFF) e_cur = live;
+                    break;
+                }
+            }
+        };
+        each([&](int, int, bool ends, int behind) {
+            if (ends && behind > base) atomicOr(&bits[(behind - 1 - base) >> 5], 1u << ((behind - 1 - base) & 31)); }, [&](int) {});
+        __syncwarp();
+        const uint32_t word = bits[feed.off >> 5], ends = word >> (feed.off & 31) & 0xFFu;
+        int j = __popc(word & ((1u << (feed.off & 31)) - 1)); // ends before the lane's tokens
+        for (int i = 0; i < feed.off >> 5; ++i) j += __popc(bits[i]);
+        numbers = min(numbers, kBlock) - 1;
+        double *lasts = reinterpret_cast<double *>(x[0].x); // in the tensors' place once they have been read
+        int j_last = 0;
+        const int n = numbers;
+        if (some != 0) {
+            read();
+            const double G_before = st.G;
+            j_last = uneven(std::true_type(), ends, j, lasts);
+            if (BY_TRACE) {
+                const double G_now = st.G;
+                st.G = G_before;
+                by_trace(std::true_type(), ends, j, n);
+                st.G = G_now;
+            }
+            st.pos = __shfl_sync(kAll, last_of, 31 - __clz(some));
+        } else {
+            zero8(dr);
+            zero8(dv);
+            if (BY_TRACE) zero8(dc);
+            if (BY_TRACE && lane == 0 && st.pos >= 0) a.grad_trace[st.pos] = 0.0f; // nothing follows
+            for (int i = lane; i < n; i += 32) lasts[i] = i == 0 ? st.G : 0.0;
+        }
+        __syncwarp();
+        if (per_sequence)
+            each([&](int o, int number, bool ends, int) {
+                if (ends) put(o, lasts[number]); }, [&](int o) { put(o, 0.0); });
+        if (j_last != n) st = Op::start(), w_before = 0.0;
+        feed.release(slot, fetch);
+        store();
     }
     if (MAPS) {
         const double P = TRACE ? P_all : (count > 0 ? pow(a.weight, (double)(count - 1)) : 1.0);

@@ -166,7 +166,6 @@ __device__ __forceinline__ void fetch_block(Stage &to, int lane, const uint16_t 
         }
     }
 }
-__device__ __forceinline__ float &stage_at(Stage &s, int t) { return reinterpret_cast<float *>(&s.x[swapped(t >> 2)])[t & 3]; }
 // Tokens 8 at .. 8 at + 7 of the block.
 __device__ __forceinline__ void read8(const Stage &from, int at, float (&x)[8])
 {
@@ -182,17 +181,6 @@ __device__ __forceinline__ void read8_bf16(const Stage &from, int at, float (&x)
         x[2 * e] = bf16_lo(v[e]);
         x[2 * e + 1] = bf16_hi(v[e]);
     }
-}
-
-// bf16 to fp32 in place, by the whole warp.
-__device__ __forceinline__ void widen(Stage &s, int lane)
-{
-    float x[8];
-    read8_bf16(s, lane, x);
-    __syncwarp();
-    s.x[swapped(2 * lane)] = make_float4(x[0], x[1], x[2], x[3]);
-    s.x[swapped(2 * lane + 1)] = make_float4(x[4], x[5], x[6], x[7]);
-    __syncwarp();
 }
 
 // The eight mask bytes from token k on, those at or behind n as zeros.

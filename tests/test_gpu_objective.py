@@ -200,6 +200,43 @@ def test_what_is_not_finite_stays_in_its_sequence(bad):
     close(got[~hit], want[~hit], (once(want) + slack)[~hit])
 
 
+@pytest.mark.parametrize("bad", [np.nan, np.inf])
+@pytest.mark.parametrize("trace", [False, True])
+def test_what_is_not_finite_stays_in_its_short_sequence(bad, trace):
+    """Many sequences to a block: nothing comes through their ends, forward or backward."""
+    c = Call("many short", seed=5, masked=0.2)
+    c.bounds = np.concatenate([[0], np.cumsum(np.tile([40, 1, 0, 7, 3, 30], 40))])
+    c.S, c.n = len(c.bounds) - 1, int(c.bounds[-1])
+    c.live, c.cu = c.n, G.dev(c.bounds.astype(np.int32))
+    c.mask = (c.rng.random(c.n) >= 0.2).astype(np.uint8)
+    x = reward_inputs(c, trace=trace)
+    seqs = [3, 6, 60, 100, 150, 201]  # of seven, forty and one tokens
+    at = np.array([int(c.bounds[s + 1]) - 1 - (int(c.bounds[s + 1] - c.bounds[s]) > 2) for s in seqs])
+    c.mask[at] = 1
+    x["rewards"][at] = bad
+    run_advantages(c, x, 1.0, 0.95, moments=False)
+    got = c.got("adv")
+    clean = dict(x, rewards=np.where(np.isin(np.arange(c.n), at), 0, x["rewards"]))
+    want, *_, slack = R.advantages(*[clean[k] for k in ("rewards", "outcome", "values", "bootstrap", "trace")], c.mask, c.bounds, c.n, 1.0, 0.95)
+    hit = np.zeros(c.n, bool)
+    for s, t in zip(seqs, at):
+        hit[c.bounds[s]:t + 1] = c.mask[c.bounds[s]:t + 1] > 0
+    assert not np.isfinite(got[hit]).any()
+    close(got[~hit], want[~hit], (once(want) + slack)[~hit])
+    back = dict(ga=c.normal(), gr=c.normal(), adv=c.normal(), trace=x["trace"])
+    back["ga"][at] = bad
+    names = run_backward(c, back, 1.0, 0.95)
+    ga = np.where(np.isin(np.arange(c.n), at), 0, back["ga"]).astype(np.float32)
+    want, slack = R.advantages_backward(ga, back["gr"], back["adv"], back["trace"], c.mask, c.bounds, c.n, 1.0, 0.95)
+    hit = np.zeros(c.n, bool)
+    for s, t in zip(seqs, at):
+        hit[t:c.bounds[s + 1]] = True
+    for k in names:
+        ok = ~hit if k in ("rewards", "values", "trace") else ~np.isin(np.arange(c.S), seqs)
+        close(c.got(k)[ok], want[k][ok], (once(want[k]) + slack[k])[ok], k)
+        assert not np.isfinite(c.got("rewards")[at]).any()
+
+
 def run_backward(c, x, gamma, lam, only=None):
     ws = torch.empty(api.hilore_advantages_workspace_bytes(c.n), dtype=torch.uint8, device="cuda")
     p = {k: c.put(v) for k, v in x.items()}
