@@ -963,17 +963,21 @@ static bool all_vectors(const AdvantageArgs &a)
            aligned(a.values, a.values_bf16 ? 16 : 32);
 }
 
-// Of a whole rollout (16 M tokens in sequences of 2000) pieces in chunks for one wave of warps take 76 us, in chunks of 4096 tokens 92 and
-// even chunks 101; of 2 M tokens in 24 sequences even chunks take 28 us, pieces 35.
+// Even chunks read most of a long sequence twice, for its maps and for itself, pieces are uneven work.  Forward, us, even chunks and pieces:
+// 8 M tokens in sequences of 2000: 59, 46; of 130 K: 49, 101.  40 M tokens in sequences of 2000: 189, 145; of 6700: 184, 157; of 13 K: 185, 232;
+// of 400 K: 180, 247.  16 M tokens in 2000 sequences: 90, 92.  So pieces need sequences for most warps, of a length that few of them pass.
+// Largest chunks: of 40 M tokens in even chunks of 16 blocks 180 us, in one wave of 43 212; in pieces from chunks of 16 blocks 154 us, of 24 145,
+// of 32 157.
 constexpr int64_t kWarps = 148 * 24; // warps that run at once
-constexpr int kLargest = 16;         // blocks of a chunk where warps do not all run at once
+constexpr int kLargestEven = 16, kLargestPieces = 24; // blocks of a chunk where warps do not all run at once
 static void deal(AdvantageArgs &a)
 {
     const int64_t share = (a.q.n_tok + kWarps * kBlock - 1) / (kWarps * kBlock); // blocks of a warp if all run at once
-    a.even = share <= 8;
-    a.chunk = kBlock * (int)(share < 1 ? 1 : (share > kLargest + kLargest / 2 ? kLargest : share));
+    a.even = share <= 8 || a.q.n_seq < kWarps * 7 / 10 || a.q.n_tok / a.q.n_seq >= 8192;
+    const int largest = a.even ? kLargestEven : kLargestPieces;
+    a.chunk = kBlock * (int)(share < 1 ? 1 : (share > largest + largest / 2 ? largest : share));
     if (a.q.n_tok <= 4 * kBlock) a.chunk = 4 * kBlock; // one launch instead of two
-    a.piece = 13;
+    a.piece = 14;
     a.chunks = (int)((a.q.n_tok + a.chunk - 1) / a.chunk);
     for (int i = 0; i < 9; ++i) a.small[i] = std::pow(a.weight, i);
     a.powers[0] = a.small[8];
@@ -993,9 +997,9 @@ using namespace hilore;
 
 extern "C" size_t hilore_advantages_workspace_bytes(int64_t n_tok)
 {
-    // chunks of any number of tokens up to n_tok: no more than run at once, or of the largest size
+    // chunks of any number of tokens up to n_tok: no more than run at once, or of the smaller of the largest sizes
     const int64_t blocks = n_tok > 0 ? (n_tok + kBlock - 1) / kBlock : 0;
-    const size_t chunks = (size_t)std::max(std::min(blocks, kWarps), (blocks + kLargest - 1) / kLargest);
+    const size_t chunks = (size_t)std::max(std::min(blocks, kWarps), (blocks + kLargestEven - 1) / kLargestEven);
     return (chunks + 1) * sizeof(AdvantageOp::Map) + (chunks / kAdvWarps + 1) * 3 * sizeof(double);
 }
 

@@ -28,11 +28,13 @@ def ragged(seed, lengths, masked=0.2):
 def lengths_of(kind):
     r = np.random.default_rng(3)
     if kind == "pieces":      # more tokens than warps that run at once take in even chunks, some sequences longer than a piece
-        return np.concatenate([r.integers(0, 6000, 2600), [20001, 8192, 8193, 70000, 0, 1], r.integers(1, 40, 2000)])
+        return np.concatenate([r.integers(0, 6000, 2600), [20001, 16384, 16385, 70000, 0, 1], r.integers(1, 40, 2000)])
     if kind == "short":       # blocks with many ends, sequences without a token among them
         return np.concatenate([r.integers(0, 40, 20000), [700, 0, 0, 3000], np.zeros(3000, int), r.integers(1, 3, 9000), [1]])
-    if kind == "wave":        # 1.2 waves of the largest chunks
-        return np.concatenate([r.integers(0, 9000, 3800), [31000]])
+    if kind == "waves":       # pieces in more chunks than warps run at once
+        return np.concatenate([r.integers(0, 9000, 7600), [31000]])
+    if kind == "long":        # even chunks, more than warps run at once
+        return np.concatenate([r.integers(0, 900000, 50), r.integers(0, 9, 500)])
     return np.concatenate([r.integers(0, 3000, 400), [150000, 1, 0, 5000], r.integers(0, 9, 3000)])  # even chunks
 
 
@@ -54,7 +56,7 @@ def close(got, want, scale):
     assert bool((off <= U * 1.0001 * want.abs() + 2.0 ** -36 * scale).all()), float(off.max())
 
 
-@pytest.mark.parametrize("kind", ["even", "pieces", "wave", "short"])
+@pytest.mark.parametrize("kind", ["even", "pieces", "waves", "long", "short"])
 @pytest.mark.parametrize("trace", [False, True])
 def test_advantages_and_their_gradient(kind, trace):
     lengths = lengths_of(kind)
