@@ -950,13 +950,13 @@ __global__ void __launch_bounds__(kGradThreads, BY_TRACE ? 4 : (TRACE ? 5 : 8)) 
             if (BY_TRACE && lane == 0 && st.pos >= 0) a.grad_trace[st.pos] = 0.0f; // nothing follows
             for (int i = lane; i < n; i += 32) lasts[i] = i == 0 ? st.G : 0.0;
         }
+        store();
         __syncwarp();
         if (per_sequence)
             each([&](int o, int number, bool ends, int) {
                 if (ends) put(o, lasts[number]); }, [&](int o) { put(o, 0.0); });
         if (j_last != n) st = Op::start(), w_before = 0.0;
         feed.release(slot, fetch);
-        store();
     }
     if (MAPS) {
         const double P = TRACE ? P_all : (count > 0 ? pow(a.weight, (double)(count - 1)) : 1.0);

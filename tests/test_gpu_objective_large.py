@@ -218,3 +218,29 @@ def test_small_calls_as_one_cluster_or_as_several_launches(off, monkeypatch):
             found.append((omega, stats, scores))
         for a, b in zip(*found):
             assert bool(((a - b).abs() <= 4 * U * a.abs().max()).all())
+
+
+@pytest.mark.parametrize("n,S", [(1, 1), (1024, 700), (1025, 3), (65537, 9), (910000, 900), (1300001, 2), (7400001, 4000), (23000001, 6)])
+def test_nothing_is_written_behind_a_workspace(n, S):
+    """Workspaces of just the size that is asked for, with bytes behind them that have to stay, and with any content."""
+    cu = torch.linspace(0, n, S + 1, device="cuda", dtype=torch.float64).round().int()
+    seq_input, x = torch.ones(S, device="cuda"), torch.zeros(n, device="cuda")
+    R = torch.arange(S, device="cuda", dtype=torch.float32)
+    out, more, few, per = torch.empty(n, device="cuda"), torch.empty(n, device="cuda"), torch.empty(5, device="cuda"), torch.empty(S, device="cuda")
+    group = next(g for g in (7, 3, 2, 1) if S % g == 0)
+    calls = {
+        api.hilore_advantages_workspace_bytes(n): [
+            lambda w, b: api.hilore_advantages(x, seq_input, x, api.F32, None, None, None, cu, S, n, 1.0, 0.9, out, more, few, w, b),
+            lambda w, b: api.hilore_advantages_backward(x, x, x, x, None, cu, S, n, 1.0, 0.9, out, per, more, None, None, w, b)],
+        api.hilore_policy_loss_workspace_bytes(S, n): [
+            lambda w, b, r=r, m=m: api.hilore_policy_loss(x, x, x, x, None, seq_input, None, cu, S, n, api.make_policy_terms(ratio=r, mean=m), n, None, None, few,
+                                                          out, w, b) for r in (0, 1) for m in (0, 1)],
+        api.hilore_preference_loss_workspace_bytes(S, n) + 16: [  # a key of its own
+            lambda w, b: api.hilore_preference_loss(x, x, None, R, group, cu, S, n, api.make_preference_terms(), 0, None, None, None, None, few, out, w, b - 16)]}
+    for size, some in calls.items():
+        buf = torch.full((size + 4096,), 0x7F, dtype=torch.uint8, device="cuda")
+        for call in some:
+            call(buf, size)
+        torch.cuda.synchronize()
+        assert bool((buf[size:] == 0x7F).all()) and bool(torch.isfinite(few[:4]).all())
+    assert bool((buf[size - 16:] == 0x7F).all())
