@@ -226,7 +226,7 @@ def test_nothing_is_written_behind_a_workspace(n, S):
     cu = torch.linspace(0, n, S + 1, device="cuda", dtype=torch.float64).round().int()
     seq_input, x = torch.ones(S, device="cuda"), torch.zeros(n, device="cuda")
     R = torch.arange(S, device="cuda", dtype=torch.float32)
-    out, more, few, per = torch.empty(n, device="cuda"), torch.empty(n, device="cuda"), torch.empty(5, device="cuda"), torch.empty(S, device="cuda")
+    out, more, few, per = (torch.zeros(m, device="cuda") for m in (n, n, 5, S))  # moments are two numbers, statistics four or five
     group = next(g for g in (7, 3, 2, 1) if S % g == 0)
     calls = {
         api.hilore_advantages_workspace_bytes(n): [
