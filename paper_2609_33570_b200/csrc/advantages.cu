@@ -289,6 +289,18 @@ template <bool BACK, int TENSORS> struct Feed {
     }
 };
 
+// By lane i of the first eight: how many bits a block's words have from word i on.
+__device__ __forceinline__ int bits_from(const uint32_t *bits, int lane)
+{
+    int n = __popc(bits[lane & 7]);
+#pragma unroll
+    for (int by = 1; by < 8; by *= 2) {
+        const int more = __shfl_down_sync(kAll, n, by, 8);
+        if ((lane & 7) + by < 8) n += more;
+    }
+    return n;
+}
+
 // MAPS: the map of the part of the chunk that goes on in the chunk before (even chunks), or of the piece that begins in it and is not its
 // sequence's first.  Otherwise the outputs, from the chunk's last block of 256 tokens to its first, eight tokens to a lane.
 //   A block inside one sequence: a lane's rightmost valid token takes the discounted value that follows it from the nearest lane to the right,
@@ -550,7 +562,8 @@ template <bool TRACE, bool MOMENTS, bool MAPS> __global__ void __launch_bounds__
                 __syncwarp();
                 const uint32_t word = bits[feed.off >> 5], ends = word >> (feed.off & 31) & 0xFFu;
                 int j = __popc(word >> (feed.off & 31) >> 8); // ends behind the lane's tokens
-                for (int i = (feed.off >> 5) + 1; i < kBlock / 32; ++i) j += __popc(bits[i]);
+                const int rest = bits_from(bits, lane), in_rest = __shfl_sync(kAll, rest, ((feed.off >> 5) + 1) & 7);
+                if (feed.off >> 5 < kBlock / 32 - 1) j += in_rest;
                 int j_first = 0;
                 if (some != 0) {
                     j_first = uneven(std::true_type(), ends, j, later);
@@ -927,7 +940,8 @@ __global__ void __launch_bounds__(kGradThreads, BY_TRACE ? 4 : (TRACE ? 5 : 8)) 
         __syncwarp();
         const uint32_t word = bits[feed.off >> 5], ends = word >> (feed.off & 31) & 0xFFu;
         int j = __popc(word & ((1u << (feed.off & 31)) - 1)); // ends before the lane's tokens
-        for (int i = 0; i < feed.off >> 5; ++i) j += __popc(bits[i]);
+        const int rest = bits_from(bits, lane);
+        j += __shfl_sync(kAll, rest, 0) - __shfl_sync(kAll, rest, feed.off >> 5);
         numbers = min(numbers, kBlock) - 1;
         double *lasts = reinterpret_cast<double *>(x[0].x); // in the tensors' place once they have been read
         int j_last = 0;
