@@ -289,16 +289,17 @@ template <bool BACK, int TENSORS> struct Feed {
     }
 };
 
-// By lane i of the first eight: how many bits a block's words have from word i on.
-__device__ __forceinline__ int bits_from(const uint32_t *bits, int lane)
+// How many bits the lanes before this one have.
+__device__ __forceinline__ int bits_before(uint32_t bits, int lane)
 {
-    int n = __popc(bits[lane & 7]);
+    const int own = __popc(bits);
+    int n = own;
 #pragma unroll
-    for (int by = 1; by < 8; by *= 2) {
-        const int more = __shfl_down_sync(kAll, n, by, 8);
-        if ((lane & 7) + by < 8) n += more;
+    for (int by = 1; by < 32; by *= 2) {
+        const int more = __shfl_up_sync(kAll, n, by);
+        if (lane >= by) n += more;
     }
-    return n;
+    return n - own;
 }
 
 // MAPS: the map of the part of the chunk that goes on in the chunk before (even chunks), or of the piece that begins in it and is not its
@@ -560,10 +561,8 @@ template <bool TRACE, bool MOMENTS, bool MAPS> __global__ void __launch_bounds__
                 }
                 s = max(s - others, 0);
                 __syncwarp();
-                const uint32_t word = bits[feed.off >> 5], ends = word >> (feed.off & 31) & 0xFFu;
-                int j = __popc(word >> (feed.off & 31) >> 8); // ends behind the lane's tokens
-                const int rest = bits_from(bits, lane), in_rest = __shfl_sync(kAll, rest, ((feed.off >> 5) + 1) & 7);
-                if (feed.off >> 5 < kBlock / 32 - 1) j += in_rest;
+                const uint32_t ends = bits[feed.off >> 5] >> (feed.off & 31) & 0xFFu;
+                const int j = bits_before(ends, lane); // ends behind the lane's tokens
                 int j_first = 0;
                 if (some != 0) {
                     j_first = uneven(std::true_type(), ends, j, later);
@@ -938,10 +937,8 @@ __global__ void __launch_bounds__(kGradThreads, BY_TRACE ? 4 : (TRACE ? 5 : 8)) 
         each([&](int, int, bool ends, int behind) {
             if (ends && behind > base) atomicOr(&bits[(behind - 1 - base) >> 5], 1u << ((behind - 1 - base) & 31)); }, [&](int) {});
         __syncwarp();
-        const uint32_t word = bits[feed.off >> 5], ends = word >> (feed.off & 31) & 0xFFu;
-        int j = __popc(word & ((1u << (feed.off & 31)) - 1)); // ends before the lane's tokens
-        const int rest = bits_from(bits, lane);
-        j += __shfl_sync(kAll, rest, 0) - __shfl_sync(kAll, rest, feed.off >> 5);
+        const uint32_t ends = bits[feed.off >> 5] >> (feed.off & 31) & 0xFFu;
+        const int j = bits_before(ends, lane); // ends before the lane's tokens
         numbers = min(numbers, kBlock) - 1;
         double *lasts = reinterpret_cast<double *>(x[0].x); // in the tensors' place once they have been read
         int j_last = 0;
