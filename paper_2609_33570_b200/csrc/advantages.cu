@@ -48,11 +48,11 @@ struct AdvantageGradOp {
         uint32_t flag; // as above; 2: holds a sequence's start
     };
     struct State {
-        double y, G;
+        double G;
         int32_t pos, pad;
     };
     static __device__ __forceinline__ Map identity() { return Map{1.0, 0.0, 0.0, -1, 0u}; }
-    static __device__ __forceinline__ State start() { return State{0.0, 0.0, -1, 0}; }
+    static __device__ __forceinline__ State start() { return State{0.0, -1, 0}; }
     static __device__ __forceinline__ Map then(const Map &a, const Map &b)
     {
         if (b.flag == 2 || a.flag == 0) return b;
@@ -60,12 +60,8 @@ struct AdvantageGradOp {
         const double k = b.P * a.wl;
         return Map{k * a.P, fma(k, a.B, b.B), b.wl, b.pos, a.flag};
     }
-    static __device__ __forceinline__ State apply(const Map &m, const State &s)
-    {
-        if (m.flag == 0) return s;
-        const double G = m.flag == 2 ? m.B : fma(m.P, s.y, m.B);
-        return State{m.wl * G, G, m.pos, 0};
-    }
+    // Maps are joined from the beginning of a sequence on, where nothing comes in.
+    static __device__ __forceinline__ State apply(const Map &m, const State &s) { return m.flag ? State{m.B, m.pos, 0} : s; }
     static __device__ __forceinline__ double last_weight(const Map &m, double w) { return m.flag ? m.wl : w; }
 };
 
