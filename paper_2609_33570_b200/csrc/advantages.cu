@@ -307,8 +307,8 @@ __device__ __forceinline__ int bits_before(uint32_t bits, int lane)
 //   that of the valid token before it takes what is behind its sequence instead, and lets nothing through, not even what is not finite.
 // The first form needs nothing but its own sequence's state, so a block's 17 bytes a token are on their way long before (copies into shared memory,
 // three blocks ahead, masks eight ahead as they say what to copy).  What bounds it: memory for many tokens in sequences without masked parts (67 M
-// tokens of padded rows 168 us, 6.8 TB/s counted over all of them, though masked parts are not read); latency of the steps of a block otherwise: 4.3 M tokens in 2048 sequences with masked parts 43 us, 15 of maps, 25 of outputs and 5 of moments, partly behind
-// one another.
+// tokens of padded rows 168 us, 6.8 TB/s counted over all of them, though masked parts are not read); latency of the steps of a block otherwise
+// (4.3 M tokens in 2048 sequences with masked parts 43 us, 15 of maps, 25 of outputs and 5 of moments, partly behind one another).
 // 24 warps an SM with all of its registers: a form that spilled 36 bytes of a thread took 184 us where this one takes 168.
 template <bool TRACE, bool MOMENTS, bool MAPS> __global__ void __launch_bounds__(kAdvThreads, TRACE ? 5 : 6) advantage_kernel(const __grid_constant__ AdvantageArgs a)
 {
