@@ -244,3 +244,37 @@ def test_nothing_is_written_behind_a_workspace(n, S):
         torch.cuda.synchronize()
         assert bool((buf[size:] == 0x7F).all()) and bool(torch.isfinite(few[:4]).all())
     assert bool((buf[size - 16:] == 0x7F).all())
+
+
+@pytest.mark.parametrize("T", [2000, 140000])
+def test_tensors_of_more_than_two_to_the_31_bytes(T):
+    """Rows at the end of a call whose tensors pass 2^31 bytes are what a call over these rows alone gives."""
+    S = 560_000_000 // T
+    n, few = S * T, 4
+    tail = few * T
+    g = torch.Generator(device="cuda").manual_seed(6)
+    lp = torch.empty(n, device="cuda").normal_(-1.5, 0.7, generator=g)
+    old = torch.empty(n, device="cuda").normal_(-1.5, 0.7, generator=g)
+    mask = torch.empty(n, dtype=torch.uint8, device="cuda").random_(0, 4, generator=g)
+    R = torch.empty(S, device="cuda").normal_(generator=g)
+
+    def run(lp, old, mask, R, S, n):
+        ws = torch.empty(max(api.hilore_advantages_workspace_bytes(n), api.hilore_policy_loss_workspace_bytes(S, n),
+                             api.hilore_preference_loss_workspace_bytes(S, n)), dtype=torch.uint8, device="cuda")
+        out, stats, found = torch.empty(n, device="cuda"), torch.empty(5, device="cuda"), []
+        keep = lambda: found.append(out[-tail:].clone())  # noqa: E731
+        api.hilore_advantages(lp, R, old, api.F32, None, None, mask, None, S, n, 1.0, 0.99, out, None, None, ws, ws.numel())
+        keep()
+        api.hilore_advantages_backward(lp, old, None, None, mask, None, S, n, 1.0, 0.99, None, None, out, None, None, ws, ws.numel())
+        keep()
+        for ratio, mean in ((0, 0), (0, 1), (1, 1)):
+            api.hilore_policy_loss(lp, old, None, None, mask, R, None, None, S, n, api.make_policy_terms(ratio=ratio, mean=mean), 1000, None, None, stats, out,
+                                   ws, ws.numel())
+            keep()
+        api.hilore_preference_loss(lp, old, mask, R, 2, None, S, n, api.make_preference_terms(length_mean=True), 1000, None, None, None, None, stats, out,
+                                   ws, ws.numel())
+        keep()
+        return found
+
+    for whole, part in zip(run(lp, old, mask, R, S, n), run(lp[-tail:].clone(), old[-tail:].clone(), mask[-tail:].clone(), R[-few:].clone(), few, tail)):
+        assert bool((whole.double() - part.double()).abs().max() <= 4 * U * part.abs().max())
