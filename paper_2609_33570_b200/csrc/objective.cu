@@ -959,7 +959,7 @@ __global__ void __launch_bounds__(kThreads) preference_pairs_kernel(const __grid
                 wins += __shfl_xor_sync(team, wins, by);
             }
             if (part == 0) {
-                v[3] -= wins * like[i];
+                if (wins) v[3] -= wins * like[i]; // not 0 * infinity of a response that wins nothing
                 v[4] += wins;
                 c *= a.length_mean ? a.beta * per[i] : a.beta;
                 a.coef[base + i] = wins ? c - a.nll * wins * per[i] : c;

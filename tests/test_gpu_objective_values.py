@@ -1,0 +1,85 @@
+"""Policy and preference loss at values that are not finite or hardly larger than nothing: infinite advantages on flat branches, tokens
+that could not be sampled, responses that win nothing."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2609_33570_b200 import api
+from tests import test_gpu_objective as T
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+INF, NAN = math.inf, math.nan
+
+
+def case(lengths, masked=None, seed=0):
+    c = T.Call("one token", seed=seed)
+    c.bounds = np.concatenate([[0], np.cumsum(lengths)]).astype(np.int64)
+    c.S, c.n = len(lengths), int(c.bounds[-1])
+    c.live, c.cu = c.n, T.G.dev(c.bounds.astype(np.int32))
+    c.mask = None if masked is None else (c.rng.random(c.n) >= masked).astype(np.uint8)
+    return c
+
+
+# ------------------------------------------------------------------------------------------------------- preference loss
+def pairs_of(c, x, t, group):
+    """Winners and losers, scores, means, and the loss of each pair, one after the other in 64 bits."""
+    lp = x["logp"].astype(np.float64)
+    d = lp - (0.0 if x["ref"] is None else x["ref"].astype(np.float64))
+    valid = np.ones(c.n, bool) if c.mask is None else c.mask > 0
+    at = [np.flatnonzero(valid[a:b]) + a for a, b in zip(c.bounds[:-1], c.bounds[1:])]
+    h = np.array([t["beta"] * (d[a].mean() if t["length_mean"] else d[a].sum()) for a in at])
+    mean = np.array([lp[a].mean() for a in at])
+    R, found = x["rewards"], []
+    for i in range(c.S):
+        for j in range(i // group * group, i // group * group + group):
+            if R[i] > R[j]:
+                z = h[i] - h[j]
+                sm = t["smoothing"]
+                lose, win = (0.0 if q == INF else -q if q < -700 else math.log1p(math.exp(-q)) for q in (z, -z))
+                each = {0: (lose if sm < 1 else 0.0) * (1 - sm) + (sm * win if sm else 0.0), 1: max(0.0, 1 - z), 2: ((z - 0.5) / t["beta"]) ** 2}[t["loss"]]
+                found.append((i, j, z, each))
+    return found, h, mean
+
+
+@pytest.mark.parametrize("group", [2, 16, 300])  # threads of their own, teams, a group over several CTAs
+@pytest.mark.parametrize("loss,length_mean,nll", [(0, 0, 0.0), (0, 1, 0.3), (1, 0, 0.3)])
+def test_a_loser_with_a_token_that_could_not_be_sampled(group, loss, length_mean, nll):
+    """Its score is -infinity and every pair with it is in order: loss, order and the winners' likelihood are as finite as they are."""
+    c = case([3, 5] * group, seed=group)
+    t = dict(T.PREF, loss=loss, length_mean=length_mean, nll=nll)
+    x = T.preference_inputs(c)
+    x["rewards"] = np.tile(np.arange(group, dtype=np.float32), 2)
+    x["logp"][c.bounds[group]] = -INF  # the first response of the second group, which wins nothing
+    T.run_preference(c, x, t, group)
+    found, h, mean = pairs_of(c, x, t, group)
+    N = len(found)
+    assert N == group * (group - 1) and int(c.got("pairs", np.int64)[0]) == N
+    nlls = sum(-mean[i] for i, *_ in found) / N
+    want = [sum(p[3] for p in found) / N + nll * nlls, sum(p[2] > 0 for p in found) / N, INF, nlls]
+    T.close(c.got("stats"), want, [1.01 * U * abs(w) + 1e-9 if math.isfinite(w) else 0 for w in want], "stats")
+    assert np.isfinite(c.got("omega")).all() and np.isneginf(c.got("scores")[group])
+
+
+@pytest.mark.parametrize("bad", [-INF, NAN])
+@pytest.mark.parametrize("group", [2, 16, 300])
+def test_a_response_without_a_pair_changes_nothing(bad, group):
+    """All rewards of its group are equal: whatever its log-probabilities are, no statistic and no gradient has anything of it."""
+    t = dict(T.PREF, nll=0.5, length_mean=1)
+    found = []
+    for value in (-1.0, bad):
+        c = case([4] * (2 * group), seed=3)
+        x = T.preference_inputs(c)
+        x["rewards"] = np.concatenate([np.zeros(group), np.arange(group)]).astype(np.float32)
+        x["logp"][5] = value
+        T.run_preference(c, x, t, group)
+        found.append([c.got(k).tobytes() for k in ("stats", "omega")])
+        assert np.isfinite(c.got("stats")).all() and c.got("stats")[3] > 0
+    assert found[0] == found[1]
+    c = case([4] * group, seed=3)  # and alone in its call
+    x = dict(T.preference_inputs(c), rewards=np.zeros(group, np.float32))
+    x["logp"][2] = bad
+    T.run_preference(c, x, t, group)
+    assert not c.got("stats").any() and not c.got("omega").any() and int(c.got("pairs", np.int64)[0]) == 0
