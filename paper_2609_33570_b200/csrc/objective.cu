@@ -932,9 +932,10 @@ __global__ void __launch_bounds__(kThreads) preference_pairs_kernel(const __grid
                     if (a.loss == HILORE_PREF_SIGMOID) {
                         const double t = exp(-fabs(z)); // -ln sigmoid(z) and its derivative
                         slope = a.smoothing - (z >= 0.0 ? t : 1.0) / (1.0 + t);
-                        if (won) {
-                            value = log1p(t) + fmax(-z, 0.0);
-                            if (a.smoothing != 0.0) value += a.smoothing * z; // -ln sigmoid(-z) = z - ln sigmoid(z)
+                        if (won) { // each logarithm with its weight: one of them may be infinite, or all but nothing beside the other
+                            const double both = log1p(t);
+                            if (a.smoothing < 1.0) value = (1.0 - a.smoothing) * (both + fmax(-z, 0.0));
+                            if (a.smoothing > 0.0) value += a.smoothing * (both + fmax(z, 0.0));
                         }
                     } else if (a.loss == HILORE_PREF_HINGE) {
                         value = z >= 1.0 ? 0.0 : 1.0 - z;

@@ -83,3 +83,41 @@ def test_a_response_without_a_pair_changes_nothing(bad, group):
     x["logp"][2] = bad
     T.run_preference(c, x, t, group)
     assert not c.got("stats").any() and not c.got("omega").any() and int(c.got("pairs", np.int64)[0]) == 0
+
+
+@pytest.mark.parametrize("smoothing", [0.0, 0.1, 0.5, 1.0])
+@pytest.mark.parametrize("sign", [-1, 1])
+def test_smoothing_at_infinite_gaps(smoothing, sign):
+    """-(1 - e) ln sigma(z) - e ln sigma(-z) at z of either infinity: infinite unless the infinite logarithm has no weight; the slope is
+    e - 1 or e."""
+    c = case([4] * 4)
+    t = dict(T.PREF, smoothing=smoothing, beta=0.5)
+    x = dict(T.preference_inputs(c), rewards=np.array([1, 0, 0, 1], np.float32))  # the second pair is finite
+    x["logp"][1 if sign < 0 else 5] = -INF  # of the winner or the loser
+    T.run_preference(c, x, t, 2)
+    stats, omega = c.got("stats"), c.got("omega")
+    weight = 1 - smoothing if sign < 0 else smoothing  # of the infinite logarithm
+    found, h, _ = pairs_of(c, x, t, 2)
+    if weight:
+        assert np.isposinf(stats[0])
+    else:
+        want = found[1][3] / 2  # the finite pair's loss, as the other one's is 0
+        T.close(stats[:1], [want], [1.01 * U * abs(want)])
+    slope = (smoothing - 1 if sign < 0 else smoothing) * 0.5 / 2
+    T.close(omega[:8], np.repeat([slope, -slope], 4), 1.01 * U * abs(slope) + 1e-45)
+    assert stats[1] == (0 if sign < 0 else 0.5) + 0.5 * (found[1][2] > 0)
+
+
+def test_smoothing_of_ordinary_gaps_against_the_definition():
+    """Both logarithms with their weights, from gaps of 2^-30 to some hundreds on either side."""
+    r = np.random.default_rng(1)
+    gaps = np.concatenate([r.normal(0, 1, 40), r.normal(0, 100, 20), [2.0 ** -30, -2.0 ** -30, 0.0, 40.0, -40.0]])
+    for smoothing in (0.0, 0.25, 1.0):
+        t = dict(T.PREF, smoothing=smoothing, beta=1.0)
+        for gap in gaps:
+            c = case([1, 1])
+            x = dict(logp=np.array([gap, 0.0], np.float32), ref=None, rewards=np.array([1, 0], np.float32))
+            T.run_preference(c, x, t, 2)
+            z = float(x["logp"][0])
+            want = (1 - smoothing) * np.logaddexp(0, -z) + smoothing * np.logaddexp(0, z)
+            T.close(c.got("stats")[:1], [want], [U * abs(want) * 1.01 + 1e-45])
