@@ -576,7 +576,7 @@ template <bool SEQ, int KL, bool ROLLOUT, bool PER_TOKEN> __global__ void __laun
                 }
             }
             // Nearly always a block has no ratio within rounding of a bound and nothing far out: then masked tokens go as zeros, which add
-            // nothing to any sum, and the objective is the smaller of two products.
+            // nothing to any sum, and a ratio that a bound moves is on a flat branch.
             if (valid != 0xFFu) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
@@ -615,13 +615,15 @@ template <bool SEQ, int KL, bool ROLLOUT, bool PER_TOKEN> __global__ void __laun
                     for (int i = 0; i < 2; ++i) {
                         const float d = s[e + i] - o[e + i], rho = exp_near(d);
                         float x = PER_TOKEN ? (A[e + i] - mean) * scale : A[e + i];
+                        // the ratio's bounds; none where x is NaN, which stays, nor where it is 0
+                        const float least = x < 0.0f ? most_down : 0.0f;
+                        float most = x > 0.0f ? most_up : INFINITY;
+                        if (a.dual_clip) most = x < 0.0f ? dual : most;
                         if (SEQ) x *= wt[e + i];
                         if (ROLLOUT) x *= fminf(exp_near(o[e + i] - b[e + i]), cap);
-                        const float gain = x * rho;
-                        float held = fminf(gain, x * fminf(fmaxf(rho, most_down), most_up));
-                        if (a.dual_clip) held = x < 0.0f ? fmaxf(held, x * dual) : held;
-                        const bool flat = held < gain || held > gain; // NaN stays
-                        float grad = flat ? 0.0f : slope_of * gain;
+                        const float u = fminf(fmaxf(rho, least), most), held = x * u;
+                        const bool flat = u != rho; // by the ratio: products of an infinite or a tiny x would be equal
+                        float grad = flat ? 0.0f : slope_of * held;
                         flats += flat ? (SEQ ? wt[e + i] : 1.0f) : 0.0f;
                         term += held;
                         drift = SEQ ? fmaf(wt[e + i], d, drift) : drift + d;
@@ -643,13 +645,13 @@ template <bool SEQ, int KL, bool ROLLOUT, bool PER_TOKEN> __global__ void __laun
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const float Ae = PER_TOKEN ? (A[e] - mean) * scale : A[e], d = s[e] - o[e];
-                    // A >= 0: beyond the bound where d > high; A < 0: where -d > -low
+                    // A >= 0: beyond the bound where d > high; A < 0: where -d > -low; NaN: never
                     const bool up = Ae >= 0.0f;
                     const float past = __uint_as_float(__float_as_uint(d) ^ (up ? 0u : 0x80000000u)) - (up ? high : -low);
-                    flat |= past > 0.0f ? 1u << e : 0u;
+                    flat |= past > 0.0f && Ae == Ae ? 1u << e : 0u;
                     close |= fabsf(past) <= a.near;
                     if (a.dual_clip) {
-                        over |= !up && d > dual_log ? 1u << e : 0u;
+                        over |= Ae < 0.0f && d > dual_log ? 1u << e : 0u;
                         close |= fabsf(d - dual_log) <= a.near;
                     }
                 }
@@ -659,8 +661,8 @@ template <bool SEQ, int KL, bool ROLLOUT, bool PER_TOKEN> __global__ void __laun
                     for (int e = 0; e < 8; ++e) {
                         const float Ae = PER_TOKEN ? (A[e] - mean) * scale : A[e];
                         const double D = (double)s[e] - (double)o[e];
-                        if (Ae >= 0.0f ? D > a.log_high : D < a.log_low) flat |= 1u << e;
-                        if (!(Ae >= 0.0f) && D > a.log_dual) over |= 1u << e;
+                        if (Ae >= 0.0f ? D > a.log_high : Ae < 0.0f && D < a.log_low) flat |= 1u << e;
+                        if (Ae < 0.0f && D > a.log_dual) over |= 1u << e;
                     }
                 }
                 flat |= over;
@@ -730,7 +732,7 @@ template <int KL> __global__ void __launch_bounds__(kThreads, kPerSm) policy_seq
             double A = (double)__ldg(a.adv + o);
             if (a.moments) A = (A - (double)a.moments[0]) / ((double)a.moments[1] + a.adv_eps);
             const double gap = a.rollout ? exp(p.b * per) : 1.0, i = a.rollout && gap > a.cap ? a.cap : gap; // NaN stays
-            const bool flat = A >= 0.0 ? d > a.log_high : (d < a.log_low || d > a.log_dual);
+            const bool flat = A >= 0.0 ? d > a.log_high : A < 0.0 && (d < a.log_low || d > a.log_dual);
             double u = exp(d);
             w = (float)weight;
             if (flat) u = A >= 0.0 ? 1.0 + a.clip_high : (d < a.log_low ? 1.0 - a.clip_low : a.dual);

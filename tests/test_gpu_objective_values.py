@@ -121,3 +121,108 @@ def test_smoothing_of_ordinary_gaps_against_the_definition():
             z = float(x["logp"][0])
             want = (1 - smoothing) * np.logaddexp(0, -z) + smoothing * np.logaddexp(0, z)
             T.close(c.got("stats")[:1], [want], [U * abs(want) * 1.01 + 1e-45])
+
+
+# ----------------------------------------------------------------------------------------------------------- policy loss
+FLAT = [(1.0, 0.6), (-1.0, -0.6), (-1.0, 0.9)]            # sign of the advantage, s - s_old: beyond 1.28, below 0.8, beyond a dual clip of 2
+OPEN = [(1.0, -0.6), (1.0, 0.1), (-1.0, 0.3), (-1.0, 0.0)]  # and on no bound
+
+
+def policy_case(tokens, ratio, per_token, near, rollout=False, mean=0):
+    """A sequence of 16 equal tokens for each (advantage, s - s_old), among ordinary ones in blocks of 256 tokens.  near: every block has
+    a token whose ratio is a rounding from its bound, so that sides are decided in 64 bits, and one whose reference is far away."""
+    t = dict(T.TERMS, dual_clip=2.0, beta=0.0, ratio=ratio, mean=mean, adv_per_token=int(per_token))
+    seqs = [(float(x), 0.05) for x in np.random.default_rng(0).normal(size=40)]
+    at = [3, 12, 21, 30, 39, 10, 19]
+    for i, k in enumerate(tokens):
+        seqs[at[i]] = k
+    c = case([16] * 40)
+    d = np.repeat([k[1] for k in seqs], 16).astype(np.float32)
+    x = dict(logp=np.zeros(c.n, np.float32), old=-d, ref=None, rollout=-d if rollout else None, white=None,
+             adv=np.array([k[0] for k in seqs], np.float32))
+    if near:
+        x["old"][::128] = -np.float32(math.log1p(0.28))  # the sequences of these tokens are numbers 0, 8, 16, 24, 32
+        x["ref"] = x["logp"] - np.float32(0.1)
+        x["ref"][::128] = 5.0
+    if per_token:
+        x["adv"] = np.repeat(x["adv"], 16)
+    where = np.zeros(c.n, bool)
+    for i in at[:len(tokens)]:
+        where[16 * i:16 * i + 16] = True
+    assert not where[::128].any()
+    return c, t, x, where
+
+
+FORMS = [(0, True, 0), (0, True, 1), (0, False, 0), (0, False, 1), (1, False, 0), (1, False, 1)]  # ratio, advantages per token, mean
+
+
+@pytest.mark.parametrize("near", [False, True])
+@pytest.mark.parametrize("ratio,per_token,mean", FORMS)
+@pytest.mark.parametrize("size", [INF, 1.4e-45, 3.4e38])
+def test_flat_branches_of_advantages_of_any_size(size, ratio, per_token, mean, near):
+    """The gradient there is exactly zero and the tokens count as clipped, whatever their neighbours hold."""
+    c, t, x, where = policy_case([(s * size, d) for s, d in FLAT], ratio, per_token, near, mean=mean)
+    T.run_policy(c, x, t, 100, grad=2.0 ** 20)
+    omega, stats = c.got("omega"), c.got("stats")
+    assert not omega[where].any() and np.isfinite(omega).all()
+    w = 1 / 100 if mean == 0 else 1 / 1600
+    share = 48 * w
+    if near and ratio == 0:  # ln 1.28 in fp32 is beyond or not, and the others' advantages have either sign
+        beyond = float(np.float32(math.log1p(0.28))) > math.log1p(0.28)
+        A = x["adv"][::128] if per_token else x["adv"][::8]
+        share += w * (A > 0).sum() * beyond
+    T.close(stats[3:4], [share], 100 * U * share)
+
+
+@pytest.mark.parametrize("near", [False, True])
+@pytest.mark.parametrize("ratio,per_token,mean", FORMS)
+def test_infinite_advantages_on_no_bound_show(ratio, per_token, mean, near):
+    c, t, x, where = policy_case([(s * INF, d) for s, d in OPEN], ratio, per_token, near, mean=mean)
+    T.run_policy(c, x, t, 100)
+    A = x["adv"] if per_token else np.repeat(x["adv"], 16)
+    omega = c.got("omega")
+    assert np.isinf(omega[where]).all() and np.isfinite(omega[~where]).all() and (np.sign(omega[where]) == -np.sign(A[where])).all()
+
+
+@pytest.mark.parametrize("near", [False, True])
+@pytest.mark.parametrize("ratio,per_token,mean", FORMS)
+def test_advantages_that_are_no_number_show_on_either_side_of_the_bounds(ratio, per_token, mean, near):
+    c, t, x, where = policy_case([(NAN, d) for _, d in FLAT + OPEN], ratio, per_token, near, mean=mean)
+    T.run_policy(c, x, t, 100)
+    omega, stats = c.got("omega"), c.got("stats")
+    assert np.isnan(omega[where]).all() and np.isfinite(omega[~where]).all() and np.isnan(stats[:2]).all() and np.isfinite(stats[2:]).all()
+
+
+@pytest.mark.parametrize("mean", [0, 1])
+@pytest.mark.parametrize("near", [False, True])
+def test_flat_branches_of_tokens_with_tiny_rollout_weights(near, mean):
+    """Rollout weights of exp(-79) times small advantages leave the range of normal numbers: still flat, still counted."""
+    c, t, x, where = policy_case([(s * 1e-10, d) for s, d in FLAT], 0, True, near, rollout=True, mean=mean)
+    x["rollout"][where] = x["old"][where] + 79.0
+    T.run_policy(c, x, t, 100, grad=2.0 ** 20)
+    assert not c.got("omega")[where].any()
+    count = 48 + (near and float(np.float32(math.log1p(0.28))) > math.log1p(0.28)) * (x["adv"][::128] > 0).sum()
+    share = count * (1 / 100 if mean == 0 else 1 / 1600)
+    T.close(c.got("stats")[3:4], [share], 100 * U * share)
+
+
+@pytest.mark.parametrize("beta", [0.0, 0.05])
+@pytest.mark.parametrize("ratio,per_token,mean", FORMS)
+def test_results_do_not_depend_on_what_makes_a_block_look_closer(ratio, per_token, mean, beta):
+    """The same tokens beside a neighbour that is next to a bound, and beside one that is not: the same bits."""
+    found = []
+    for shift in (0.0, 0.02):
+        r = np.random.default_rng(2)
+        t = dict(T.TERMS, dual_clip=2.0, beta=beta, ratio=ratio, mean=mean, adv_per_token=int(per_token))
+        c = case([16] * 40)
+        x = dict(logp=np.zeros(c.n, np.float32), old=r.normal(0, 0.5, c.n).astype(np.float32), ref=r.normal(0, 0.5, c.n).astype(np.float32), white=None,
+                 rollout=None, adv=r.normal(size=c.n if per_token else c.S).astype(np.float32))
+        x["rollout"] = (x["old"] + r.normal(0, 0.05, c.n)).astype(np.float32)
+        x["old"][::128] = -np.float32(math.log1p(0.28)) - np.float32(shift)
+        T.run_policy(c, x, t, 100)
+        keep = np.ones(c.n, bool)
+        keep[::128] = False
+        if ratio:  # their sequences move with them
+            keep = ~np.repeat(np.arange(40) % 8 == 0, 16)
+        found.append(c.got("omega")[keep])
+    assert np.array_equal(*found)
