@@ -675,11 +675,13 @@ template <bool SEQ, int KL, bool ROLLOUT, bool PER_TOKEN> __global__ void __laun
                     if (a.dual_clip) bound = over >> e & 1 ? dual : bound;
                     const float we = SEQ ? wt[e] : 1.0f;
                     float x = SEQ ? Ae * we : Ae;
+                    bool none = Ae == 0.0f && fabsf(d) <= FLT_MAX; // nothing, though ratio or weight may be beyond fp32
                     if (ROLLOUT) {
                         const float gap = o[e] - b[e], i = fabsf(gap) <= kNear ? exp_near(gap) : expf(gap);
                         x *= i > cap ? cap : i; // NaN stays
+                        none = none && fabsf(gap) <= FLT_MAX;
                     }
-                    const float gain = x * (on_flat ? bound : rho);
+                    const float gain = none ? 0.0f : x * (on_flat ? bound : rho);
                     float grad = on_flat ? 0.0f : slope_of * gain;
                     term += in ? gain : 0.0f;
                     drift = in ? fmaf(we, d, drift) : drift;
@@ -731,9 +733,10 @@ template <int KL> __global__ void __launch_bounds__(kThreads, kPerSm) policy_seq
             const double per = 1.0 / p.n, weight = a.sequence_mean ? inv * per : inv, d = p.a * per;
             double A = (double)__ldg(a.adv + o);
             if (a.moments) A = (A - (double)a.moments[0]) / ((double)a.moments[1] + a.adv_eps);
-            const double gap = a.rollout ? exp(p.b * per) : 1.0, i = a.rollout && gap > a.cap ? a.cap : gap; // NaN stays
+            const bool none = A == 0.0 && fabs(d) <= DBL_MAX && (!a.rollout || fabs(p.b) <= DBL_MAX); // nothing, though u or i may be beyond fp64
+            const double gap = a.rollout && !none ? exp(p.b * per) : 1.0, i = a.rollout && gap > a.cap ? a.cap : gap; // NaN stays
             const bool flat = A >= 0.0 ? d > a.log_high : A < 0.0 && (d < a.log_low || d > a.log_dual);
-            double u = exp(d);
+            double u = none ? 1.0 : exp(d);
             w = (float)weight;
             if (flat) u = A >= 0.0 ? 1.0 + a.clip_high : (d < a.log_low ? 1.0 - a.clip_low : a.dual);
             else slope_of = (float)(-weight * i * A * u * g);

@@ -226,3 +226,19 @@ def test_results_do_not_depend_on_what_makes_a_block_look_closer(ratio, per_toke
             keep = ~np.repeat(np.arange(40) % 8 == 0, 16)
         found.append(c.got("omega")[keep])
     assert np.array_equal(*found)
+
+
+@pytest.mark.parametrize("ratio,per_token,mean", FORMS)
+@pytest.mark.parametrize("far", ["ratio", "weight", "both"])
+def test_advantages_of_nothing_at_ratios_beyond_every_number(ratio, per_token, mean, far):
+    """Without bounds a ratio of exp(800) is infinite in any type here; times an advantage of 0 it is nothing."""
+    t = dict(T.TERMS, clip_high=INF, rollout_cap=INF, beta=0.0, ratio=ratio, mean=mean, adv_per_token=int(per_token))
+    for d in (100.0, 800.0):
+        c, _, x, where = policy_case([(0.0, 0.0)], ratio, per_token, False, rollout=True, mean=mean)
+        if far != "weight":
+            x["logp"][where] += np.float32(d)
+        if far != "ratio":
+            x["rollout"][where] -= np.float32(d)
+        T.run_policy(c, x, t, 100)
+        omega, stats = c.got("omega"), c.got("stats")
+        assert not omega[where].any() and np.isfinite(omega).all() and omega.any() and np.isfinite(stats).all()
