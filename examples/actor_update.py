@@ -92,6 +92,9 @@ def rollout(actor, gen, allow, dev):
     return seq, mask
 
 
+KINDS = ("grpo", "policy", "preference")
+
+
 class Loss:
     """What turns log-probabilities and rewards into omega, the gradient of the loss by the log-probabilities."""
 
@@ -138,6 +141,8 @@ class Loss:
 def train(iterations=40, epochs=2, lr=0.02, seed=0, kind="grpo", watch=None):
     """Returns the mean reward of each iteration's responses, and the last gradient norm.  `watch` is called with the tensors of every
     step before the parameters move."""
+    if kind not in KINDS:
+        raise ValueError(f"kind: one of {', '.join(KINDS)}, not {kind!r}")
     dev = torch.device("cuda")
     gen = torch.Generator(device=dev).manual_seed(seed)
     actor, loss = Actor(gen, dev), Loss(kind, dev)
