@@ -566,14 +566,16 @@ int hilore_adamw_step(const hilore_param *params_dev, const hilore_param *params
  * Sequences, in every call of this part:
  *   cu_seqlens   [n_seq + 1] int32 as in hilore_grpo_coeffs_packed, or NULL: n_seq rows of n_tok / n_seq slots each
  *                (n_tok % n_seq must be 0, HILORE_SHAPE).  cu_seqlens[0] counts as 0.  Tokens from cu_seqlens[n_seq] on
- *                belong to no sequence: nothing of theirs is read or written, so a captured call serves batches of any
- *                number of tokens up to n_tok.  Whatever cu_seqlens holds, no kernel indexes outside [0, n_seq] or [0, n_tok).
+ *                belong to no sequence: whatever they hold changes nothing and nothing of theirs is written, so a captured call serves
+ *                batches of any number of tokens up to n_tok (which the tensors have; blocks of 256 tokens are read whole).
+ *                Whatever cu_seqlens holds, no kernel indexes outside [0, n_seq] or [0, n_tok).
  *   mask         opt [n_tok] u8 (0 / not 0); NULL: every token is valid.  Masked tokens (prompt, tool outputs, padding) may
  *                hold anything, NaN included: they change nothing and their outputs are 0.
  *   Tensors with an entry per token may have any address that their type allows; with fp32 at 32, bf16 at 16 and masks at 8
  *   bytes eight tokens move at a time.  Results do not depend on that, nor on scheduling: the same call gives the same bits.
- *   Where in a call a sequence lies decides in which order sums are added up, all of them in fp64: its results may differ in a
- *   last bit, no more, with the sequences around it.  n_seq and n_tok at most 2^31 - 2^16 (HILORE_SHAPE).
+ *   Where in a call a sequence lies decides in which order sums are added up: its results may differ in a last bit, no more, with the
+ *   sequences around it.  Sums are fp64; the statistics of RATIO_TOKEN add eight neighbouring tokens in fp32 first.  n_seq and
+ *   n_tok at most 2^31 - 2^16 (HILORE_SHAPE).
  *   Small policy losses (up to 16384 tokens, RATIO_TOKEN with MEAN_TOKENS) are one thread-block cluster, two launches with
  *   HILORE_DISABLE_CLUSTER_LAUNCH set in the environment.
  *   workspace    the bytes of the call's .._workspace_bytes, 16-byte aligned, overwritten.
@@ -592,6 +594,7 @@ int hilore_adamw_step(const hilore_param *params_dev, const hilore_param *params
  *   adv, returns    opt [n_tok] fp32.    moments  opt [2] fp32: mean and population standard deviation of the advantages of the call's
  *                valid tokens (0, 0 where there are none), in a fixed order of additions.  At least one of the three.
  *   What is not finite makes the tokens before it in its sequence NaN or infinite, and no others; so do products of trace beyond fp64.
+ *   Time grows faster than the length of a single sequence beyond some ten million tokens: 16 M 0.2 ms, 60 M 1.4 ms, 240 M 27 ms.
  *
  * hilore_advantages_backward: the gradients of sum_k (grad_adv_k A_k + grad_returns_k returns_k),
  *     G_k = grad_adv_k + grad_returns_k + gamma lambda c_{k-1} G_{k-1};     d r_k = G_k
@@ -635,7 +638,9 @@ typedef struct hilore_policy_terms {
  *     w   = 1 / N (HILORE_MEAN_TOKENS), 1 / (N |T_s|) with the sequence's valid tokens |T_s| (HILORE_MEAN_SEQUENCES)
  *     L   = sum_t w ( -i A u + beta kl );     omega_t = dL/ds_t * grad_loss
  * On a flat branch (u a bound) the policy term's gradient is exactly 0; rho on its bound is not beyond it.  Which side a
- * token is on is decided on s - s_old in fp64, so it is decided as the formula does.
+ * token is on is decided on s - s_old in fp64, so it is decided as the formula does.  An infinite advantage is on a flat branch like
+ * any other; one that is NaN is on none, and makes its tokens' omega NaN.  exp(e), and for RATIO_TOKEN ratios and weights, are fp32:
+ * from a logarithm of 88.7 on they are infinite where no bound holds them.  An A of 0 is nothing even there.
  *   logp, logp_old   [n_tok] fp32.    logp_ref  opt [n_tok] fp32, needed unless beta = 0.    logp_rollout  opt [n_tok] fp32,
  *                    what the engine that sampled reported.
  *   adv              [n_tok] or [n_seq] fp32.    adv_moments  opt [2] fp32 as written by hilore_advantages:
@@ -670,14 +675,15 @@ typedef struct hilore_preference_terms {
  * the two has no valid token or a reward is NaN:
  *     h  = beta * sum (or mean) over the valid tokens of s - s_ref
  *     z  = h_w - h_l - margin - margin_reward (R_w - R_l)
- *     l  = SIGMOID -(1 - smoothing) ln sigma(z) - smoothing ln sigma(-z);   HINGE max(0, 1 - z);   SQUARE ((z - 1/2) / beta)^2
+ *     l  = SIGMOID -(1 - smoothing) ln sigma(z) - smoothing ln sigma(-z), a logarithm of weight 0 left out;   HINGE max(0, 1 - z);
+ *          SQUARE ((z - 1/2) / beta)^2
  *     L  = 1/N sum over pairs of ( l + nll * (-mean over the winner's valid tokens of s) );     omega_t = dL/ds_t * grad_loss
  *   logp         [n_tok] fp32.    logp_ref  opt [n_tok] fp32 (NULL: without a reference).    rewards  [n_seq] fp32.
  *                G in [1, 1024], n_seq % G must be 0 (HILORE_SHAPE).
  *   N_norm, N_norm_dev   pairs of the whole batch; N_norm = 0: those of this call.  A device value <= 0 gives omega = 0 and stats 0.
  *   scores       opt [n_seq] fp32: h (0 without a valid token).    pairs  opt one int64 on the device: the pairs of this call.
  *   stats        [4] fp32, each the sum over this call's pairs divided by N: L; pairs with h_w > h_l; h_w - h_l; the mean
- *                above, -mean s of the winner.
+ *                above, -mean s of the winner.  Responses in no pair have no part in them, losers none in the last.
  *   omega        [n_tok] fp32.    grad_loss as in hilore_policy_loss.
  */
 int hilore_preference_loss(const float *logp, const float *logp_ref, const uint8_t *mask, const float *rewards, int32_t G,

@@ -92,7 +92,7 @@ struct AdvantageArgs {
     float *grad_rewards, *grad_outcome, *grad_values, *grad_bootstrap, *grad_trace;
     void *maps;       // [chunks]
     double *partials; // [CTAs][3] count, mean, sum of squared deviations
-    int chunks, chunk, piece, vec, moments;
+    int chunks, chunk, piece, vec;
     int even;
     int second; // second: a launch of this call came first, and what it did not write is there without waiting for it
 };
@@ -309,7 +309,8 @@ __device__ __forceinline__ int bits_before(uint32_t bits, int lane)
 // three blocks ahead, masks eight ahead as they say what to copy).  What bounds it: memory for many tokens in sequences without masked parts (67 M
 // tokens of padded rows 168 us, 6.8 TB/s counted over all of them, though masked parts are not read); latency of the steps of a block otherwise
 // (4.3 M tokens in 2048 sequences with masked parts 43 us, 15 of maps, 25 of outputs and 5 of moments, partly behind one another).
-// 24 warps an SM with all of its registers: a form that spilled 36 bytes of a thread took 184 us where this one takes 168.
+// 24 warps an SM with all of its registers, 20 with a trace; with moments 8 bytes of a thread are spilled, 38 with a trace as well.  A form without
+// a trace that spilled 36 took 184 us where this one takes 168.
 template <bool TRACE, bool MOMENTS, bool MAPS> __global__ void __launch_bounds__(kAdvThreads, TRACE ? 5 : 6) advantage_kernel(const __grid_constant__ AdvantageArgs a)
 {
     using Op = AdvantageOp;
@@ -598,7 +599,8 @@ template <bool TRACE, bool MOMENTS, bool MAPS> __global__ void __launch_bounds__
     }
 }
 
-// Joins the CTAs' counts, means and sums of squared deviations: at most 1600 of them, one launch of 5 us.
+// Joins the CTAs' counts, means and sums of squared deviations in one launch: 845 of them for 4.3 M tokens, 5 us, 2731 for 67 M padded ones, one for every
+// 16384 tokens (24576 in pieces) beyond some 20 M.
 constexpr int kMomentThreads = 1024;
 
 __global__ void __launch_bounds__(kMomentThreads) advantage_moments_kernel(const double *partials, int ctas, float *moments)
@@ -628,8 +630,9 @@ constexpr int kGradWarps = kGradThreads / 32;
 // the chunk and is not its sequence's last.  Blocks as in the forward kernel; here a lane's first valid token takes the weight of the valid token
 // before it from the nearest lane to the left, and every sequence that ends gives its last gradient.  d c of a token needs the advantage of its
 // follower: where that is in a later block, the token stays open until then.
-// 16 M tokens in 8000 sequences 76 us (3.6 TB/s): eight CTAs on an SM, 24 warps; with seven 86, with six 97.  By the trace as well (25 bytes a token,
-// 150 registers) 13 M tokens with masked parts take 150 us with four CTAs, 169 with five, which spill.
+// 16 M tokens in 8000 sequences 75 us (3.6 TB/s): eight CTAs on an SM, 24 warps; with seven 86, with six 97, though with eight the outputs' form without a
+// trace spills (52 bytes of a thread stored, 64 read).  By the trace as well (29 bytes a token, 150 registers) 13 M tokens with masked parts take 147 us
+// with four CTAs, 169 with five, which spill.
 template <bool TRACE, bool BY_TRACE, bool MAPS>
 __global__ void __launch_bounds__(kGradThreads, BY_TRACE ? 4 : (TRACE ? 5 : 8)) advantage_grad_kernel(const __grid_constant__ AdvantageArgs a)
 {
@@ -984,9 +987,11 @@ static bool all_vectors(const AdvantageArgs &a)
 // Even chunks read most of a long sequence twice, for its maps and for itself, pieces are uneven work.  Forward, us, even chunks and pieces:
 // 8 M tokens in sequences of 2000: 59, 46; of 130 K: 49, 101.  40 M tokens in sequences of 2000: 189, 145; of 6700: 184, 157; of 13 K: 185, 232;
 // of 400 K: 180, 247.  16 M tokens in 2000 sequences: 90, 92.  So pieces need sequences for most warps, of a length that few of them pass.
+// A warp joins the maps of all chunks of its last sequence behind its own, so a sequence's maps are read half its chunks' square times: a call of one
+// sequence of 16 M tokens takes 172 us, of 60 M 1370, of 240 M 27000, most of it this.
 // Largest chunks: of 40 M tokens in even chunks of 16 blocks 180 us, in one wave of 43 212; in pieces from chunks of 16 blocks 154 us, of 24 145,
 // of 32 157.
-constexpr int64_t kWarps = 148 * 24; // warps that run at once
+constexpr int64_t kWarps = 148 * 24; // warps that run at once without a trace; with one 148 * 20, in the gradient 148 * 15, or 12 by the trace
 constexpr int kLargestEven = 16, kLargestPieces = 24; // blocks of a chunk where warps do not all run at once
 static void deal(AdvantageArgs &a)
 {
@@ -1035,7 +1040,7 @@ extern "C" int hilore_advantages(const float *rewards, const float *outcome, con
     if (!workspace || (n_tok > 0 && !adv && !returns && !moments))
         return HILORE_INVALID_ARG;
     a.rewards = rewards, a.outcome = outcome, a.values = values, a.values_bf16 = values_dtype == HILORE_BF16, a.bootstrap = bootstrap;
-    a.trace = trace, a.mask = mask, a.gamma = gamma, a.weight = gamma * lambda, a.adv = adv, a.returns = returns, a.moments = moments != nullptr;
+    a.trace = trace, a.mask = mask, a.gamma = gamma, a.weight = gamma * lambda, a.adv = adv, a.returns = returns;
     if (!aligned(rewards, 4) || !aligned(outcome, 4) || !aligned(bootstrap, 4) || !aligned(trace, 4) || !aligned(adv, 4) || !aligned(returns, 4) ||
         !aligned(moments, 4) || !aligned(values, a.values_bf16 ? 2 : 4) || !aligned(workspace, 16))
         return HILORE_ALIGN;

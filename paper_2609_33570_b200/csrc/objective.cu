@@ -140,7 +140,8 @@ struct Cursor {
     }
 };
 // Sequences that end in a block are taken one after the other up to this many, from the window (sums: with a reduction each).  Where more do,
-// all lanes walk those of their own tokens at the same time.  Policy loss of 40000 sequences of 25 and 100 tokens with 4, 8, 16: 30, 30, 27 and 54,
+// all lanes walk those of their own tokens at the same time, and one lane adds up the shares of a long sequence behind them (500 K tokens behind twenty
+// sequences of three, means of sequences: 134 us for 17 without the twenty).  Policy loss of 40000 sequences of 25 and 100 tokens with 4, 8, 16: 30, 30, 27 and 54,
 // 47, 47 us; their preference loss with 1, 3, 8 in the sums: 25, 25, 30 and 46, 46, 47 us.
 constexpr int kFew = 16, kFewSums = 3;
 
@@ -451,10 +452,12 @@ __device__ __forceinline__ void policy_hand_on(const PolicyArgs &a, const double
 
 // Ratios of tokens.  SEQ: there is something to a sequence, its weight or its advantage, which a lane looks up for one sequence of a window of 32.
 // Which side of a bound a ratio is on is decided in fp32 but for the few next to it, which are compared in fp64, as the formula does.  What a sum has
-// in common (1 / N, signs) is multiplied in at its end.  A kernel for each kind of terms, as a term that is not asked for costs registers and
+// in common (1 / N, signs) is multiplied in at its end.  A lane's eight tokens of a block are added up in fp32, as these are: seven roundings beside
+// theirs, and eight conversions less; then in fp64.  A kernel for each kind of terms, as a term that is not asked for costs registers and
 // instructions all the same.
-// Memory and issue slots bound it alike: 60 M tokens with whitened advantages and K3 to a reference 210 us, 6.0 TB/s, 515 instructions of a warp for 256
-// tokens.  It was 530 in tiles of 2048 tokens with one kernel for all terms, 237 with shares of warps and a kernel for each kind, and the rest is
+// Memory and issue slots bound it alike: 60 M tokens with advantages per token and K3 to a reference 214 us, 5.9 TB/s, 508 instructions of a warp for 256
+// tokens.  Blocks with a ratio next to a bound, or with what is far out (K3: |s_ref - s| > 2), go token by token through both forms of each term: with one
+// such token in 2560 211 us, in 256 250, in 10 279, for 206 without one.  It was 530 in tiles of 2048 tokens with one kernel for all terms, 237 with shares of warps and a kernel for each kind, and the rest is
 // masks read a block ahead and products in place of branches.
 // 13 M tokens in 40000 sequences of 327, weights per sequence, 75 us; 133 with each sequence looked up when it came.
 template <bool SEQ, int KL, bool ROLLOUT, bool PER_TOKEN> __global__ void __launch_bounds__(kThreads, kPerSm) policy_token_kernel(const __grid_constant__ PolicyArgs a)
